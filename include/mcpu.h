@@ -83,7 +83,8 @@ typedef enum mcpu_status {
   MCPU_ERR_INTERNAL = 8,             /* device: work plan overflowed its bound */
   MCPU_ERR_POOL_EXHAUSTED = 9,       /* device: the free-page stack ran empty */
   MCPU_ERR_UNSUPPORTED_ROW = 10      /* device: a row the called variant does not handle was
-                                        skipped (an append row given to the fp8 forward) */
+                                        skipped (an append row given to the fp8 forward, a
+                                        tree with more nodes than its mask has bits) */
 } mcpu_status;
 
 typedef struct mcpu_dims {
@@ -397,6 +398,151 @@ mcpu_status mcpu_host_stage_wait(mcpu_host_stage* stage, mcpu_stream_t stream);
 /* Blocks the calling thread until every output copy the stage has enqueued
  * so far is complete. */
 mcpu_status mcpu_host_stage_sync(mcpu_host_stage* stage);
+
+/*
+ * One round of tree-drafted decoding (no counterpart in the paper, whose
+ * engine is a black box to it): a draft model proposes a small tree of tokens
+ * for every row, the model scores all of them in one forward pass, and the
+ * accepted path stays in the cache. The L_r query tokens of row r are the
+ * nodes of its tree, at slots C_r .. S_r - 1 of its cache, C_r = S_r - L_r
+ * (its context length). The calls of a round, per layer unless noted:
+ *   mcpu_grow_block_tables       (once) pages for the drafted tokens
+ *   mcpu_norm_rope_kv_append     q/k norm, rotation at the nodes' positions, K/V to the pages
+ *   mcpu_tree_attention_forward  every node over the context and its ancestors
+ *   mcpu_compact_kv              (once, all layers) accepted nodes' K/V rows to the front
+ *   mcpu_shrink_block_tables     (once) pages past the new lengths back to the stack
+ * and, when samples are added to a running prompt, mcpu_fork_block_tables
+ * followed by mcpu_copy_pages.
+ */
+
+/*
+ * Per-head RMS norm of q and k, rotary embedding and KV append in one pass.
+ * For each query token t of row r and every q and kv head, in fp32 and
+ * rounded once to bf16:
+ *   n_d = x_d * w_d / sqrt(mean_e(x_e^2) + eps)
+ *   y_i = n_i cos_i - n_{i+32} sin_i,  y_{i+32} = n_{i+32} cos_i + n_i sin_i   (i < 32)
+ * with w = q_weight or k_weight (float [D]) and the angles of cos_sin's row
+ * p_t (laid out as for mcpu_rope_kv_append). p_t = positions[t] (device int32
+ * [T]; a tree's nodes sit at C_r + depth) or, with positions NULL,
+ * S_r - L_r + i. Rotated q goes to q_out [T, H_q, D] (dense; may be q itself
+ * when q is dense), rotated k and v (bit for bit) to the row's pages at slot
+ * S_r - L_r + i as mcpu_kv_append places them.
+ * q, k_new, v_new: bf16 with the heads of one token dense ([H, D]) and
+ * *_stride elements from one token to the next (a multiple of 8, at least
+ * H * D: q, k and v may be slices of one projection's output); 16-byte
+ * aligned. eps >= 0, finite. An all-zero vector with eps = 0 gives zeros.
+ * Errors as mcpu_rope_kv_append: a position outside [0, max_position) or
+ * inconsistent lengths set MCPU_ERR_BAD_LENGTHS and leave the token
+ * untouched, a bad page skips its K/V write (MCPU_ERR_BAD_PAGE).
+ */
+mcpu_status mcpu_norm_rope_kv_append(const void* q, int64_t q_stride, const void* k_new, int64_t k_stride,
+                                     const void* v_new, int64_t v_stride, const float* q_weight,
+                                     const float* k_weight, float eps, const int32_t* positions,
+                                     const float* cos_sin, int32_t max_position, void* q_out, void* k_cache,
+                                     void* v_cache, const int32_t* block_table, const int32_t* seq_lens,
+                                     const int32_t* query_start_loc, const mcpu_dims* dims, int32_t* status_word,
+                                     mcpu_stream_t stream);
+
+/*
+ * Paged attention of drafted-token trees: node i of row r (query token
+ * t = query_start_loc[r] + i) sees
+ *   - context key j < C_r iff sliding_window <= 0 or positions[t] - j < sliding_window;
+ *   - node key n < L_r (slot C_r + n) iff bit n % 32 of
+ *     tree_mask[t * mask_words + n / 32] is set (for a tree: its ancestors and
+ *     itself; nothing is implied, and the window does not apply to nodes).
+ * out, lse, softmax_scale and sinks (float [H_q] or NULL) as for
+ * mcpu_paged_attention_forward; a node that sees nothing gets out = 0 and
+ * lse = -inf (or its sink). Rows may have any L_r <= 32 * mask_words
+ * (mask_words 1 .. MCPU_MAX_TREE_WORDS); a longer one is skipped and reported
+ * as MCPU_ERR_UNSUPPORTED_ROW. positions (device int32 [T]) is read only with
+ * a window (NULL otherwise is fine) and must lie in [C_r, S_r): a value
+ * outside counts as the nearest inside. The K/V rows of nodes are read from
+ * the pages, so append them first. Slots that no node of the row sees may
+ * hold anything; a node key that some nodes see and others do not has to be
+ * finite, as its value reaches the others with weight 0.
+ * Long rows are split over the SMs and merged by log-sum-exp in a fixed
+ * order: the same inputs give the same bits on the same device. workspace:
+ * mcpu_tree_workspace_size(dims) bytes, 256-byte aligned; its first word is
+ * the status word (zero it once). Capturable, as the other forward calls.
+ */
+#define MCPU_MAX_TREE_WORDS 8
+size_t mcpu_tree_workspace_size(const mcpu_dims* dims);
+mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, const void* v_cache,
+                                        const int32_t* block_table, const int32_t* seq_lens,
+                                        const int32_t* query_start_loc, const uint32_t* tree_mask,
+                                        int32_t mask_words, const int32_t* positions, int32_t sliding_window,
+                                        float softmax_scale, const float* sinks, const mcpu_dims* dims, void* out,
+                                        float* lse, void* workspace, size_t workspace_bytes, mcpu_stream_t stream);
+
+/*
+ * Keeps an accepted path of each row's tree: for i < accept_len[r], the K/V
+ * row of node n = accept_path[r * max_accept + i] moves from slot C_r + n to
+ * slot C_r + i, for every kv head of every pool, and
+ * new_seq_lens[r] = C_r + accept_len[r]. A path is strictly increasing with
+ * 0 <= n < L_r (nodes come after their ancestors), so moves never overwrite a
+ * row still to be read. A row whose path or lengths break these rules, or
+ * whose pages are invalid, is left as it is (new_seq_lens[r] = S_r) and
+ * reported (MCPU_ERR_BAD_LENGTHS / MCPU_ERR_BAD_PAGE).
+ * pools: host array of num_pools (0 .. MCPU_MAX_POOLS) device pointers to
+ * bf16 pools [num_pages, H_kv, 16, 64] that share block_table (K and V of
+ * every layer), read during the call. new_seq_lens must not be seq_lens.
+ */
+#define MCPU_MAX_POOLS 128
+mcpu_status mcpu_compact_kv(void* const* pools, int32_t num_pools, const int32_t* block_table,
+                            const int32_t* seq_lens, const int32_t* query_start_loc, const int32_t* accept_path,
+                            int32_t max_accept, const int32_t* accept_len, const mcpu_dims* dims,
+                            int32_t* new_seq_lens, int32_t* status_word, mcpu_stream_t stream);
+
+/*
+ * Shared pages. page_refs (device int32 [num_pages]) counts a page's holders
+ * beyond the first: 0 for a page that one row holds (as
+ * mcpu_grow_block_tables hands it out) and for a free page. free_pages
+ * [num_pages] and free_count are the stack of mcpu_grow_block_tables.
+ * page_scratch: MCPU_PAGE_SCRATCH int32, zeroed once before its first use
+ * (the calls leave it zero). All calls that touch one stack must be ordered
+ * (one stream). They use num_seqs, max_pages_per_seq and num_pages of dims;
+ * page and stack sizes are not otherwise limited.
+ *
+ * mcpu_fork_block_tables: row dst_rows[f] becomes a copy of row src_rows[f]
+ * (device int32 [num_forks], num_forks <= 2048): its S / 16 full pages are
+ * shared (page_refs + 1; negative entries stay negative), a partial last page
+ * is replaced by a fresh page, entries past it are -1, and seq_lens[dst] =
+ * seq_lens[src] = S. copy_src[f], copy_dst[f] receive the partial page and
+ * its replacement for mcpu_copy_pages, or -1. Fresh pages are popped in the
+ * order of f. The dst rows must hold no page (shrink them to length 0
+ * first), be distinct, and not be a src row of the same call. If the stack
+ * runs empty the tail entry stays -1 (MCPU_ERR_POOL_EXHAUSTED).
+ *
+ * mcpu_shrink_block_tables: the reverse of mcpu_grow_block_tables. Every
+ * entry >= 0 of row r at or past ceil(S_r / 16), and with sliding_window
+ * W > 0 every entry whose keys no query at a position >= S_r can see
+ * (page < (S_r - W + 1) / 16), is released and set to -1: page_refs - 1, or,
+ * for the last holder, back to the stack. S_r = 0 frees the row. Pages that
+ * return are pushed in ascending order. A page that is released more often
+ * than it is held is reported (MCPU_ERR_BAD_PAGE).
+ *
+ * mcpu_copy_pages: for each f < num_copies with copy_src[f], copy_dst[f] >= 0,
+ * copies page copy_src[f] to page copy_dst[f] in every pool: page_bytes
+ * contiguous bytes at page * page_bytes (H_kv * 2048 for a bf16 pool,
+ * H_kv * 2176 for an fp8 pool; a multiple of 16). A page may be the source of
+ * several copies; a destination must not occur twice or be a source of
+ * another copy of the call. Ids past num_pages are reported
+ * (MCPU_ERR_BAD_PAGE) and skipped.
+ */
+#define MCPU_PAGE_SCRATCH 64
+#define MCPU_MAX_FORKS 2048
+mcpu_status mcpu_fork_block_tables(int32_t* block_table, int32_t* seq_lens, const int32_t* src_rows,
+                                   const int32_t* dst_rows, int32_t num_forks, const mcpu_dims* dims,
+                                   int32_t* page_refs, const int32_t* free_pages, int32_t* free_count,
+                                   int32_t* copy_src, int32_t* copy_dst, int32_t* page_scratch, int32_t* status_word,
+                                   mcpu_stream_t stream);
+mcpu_status mcpu_shrink_block_tables(int32_t* block_table, const int32_t* seq_lens, int32_t sliding_window,
+                                     const mcpu_dims* dims, int32_t* page_refs, int32_t* free_pages,
+                                     int32_t* free_count, int32_t* page_scratch, int32_t* status_word,
+                                     mcpu_stream_t stream);
+mcpu_status mcpu_copy_pages(void* const* pools, int32_t num_pools, int64_t page_bytes, int32_t num_pages,
+                            const int32_t* copy_src, const int32_t* copy_dst, int32_t num_copies,
+                            int32_t* status_word, mcpu_stream_t stream);
 
 /* Synchronises `stream`, reads the workspace status word and maps it to the
  * most severe mcpu_status (MCPU_OK if clear). The raw bits go to

@@ -143,6 +143,24 @@ _lib.mcpu_paged_attention_host_fp8.argtypes = [
     ctypes.c_size_t, ctypes.POINTER(Options), ctypes.c_int32, _P,
 ]
 _lib.mcpu_paged_attention_host_fp8.restype = ctypes.c_int
+_I32, _I64, _F32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+_DIMS = ctypes.POINTER(Dims)
+_lib.mcpu_norm_rope_kv_append.argtypes = [_P, _I64, _P, _I64, _P, _I64, _P, _P, _F32, _P, _P, _I32, _P, _P, _P, _P, _P,
+                                          _P, _DIMS, _P, _P]
+_lib.mcpu_norm_rope_kv_append.restype = ctypes.c_int
+_lib.mcpu_tree_workspace_size.argtypes = [_DIMS]
+_lib.mcpu_tree_workspace_size.restype = ctypes.c_size_t
+_lib.mcpu_tree_attention_forward.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I32, _P, _I32, _F32, _P, _DIMS, _P, _P, _P,
+                                             ctypes.c_size_t, _P]
+_lib.mcpu_tree_attention_forward.restype = ctypes.c_int
+_lib.mcpu_compact_kv.argtypes = [_P, _I32, _P, _P, _P, _P, _I32, _P, _DIMS, _P, _P, _P]
+_lib.mcpu_compact_kv.restype = ctypes.c_int
+_lib.mcpu_fork_block_tables.argtypes = [_P, _P, _P, _P, _I32, _DIMS, _P, _P, _P, _P, _P, _P, _P, _P]
+_lib.mcpu_fork_block_tables.restype = ctypes.c_int
+_lib.mcpu_shrink_block_tables.argtypes = [_P, _P, _I32, _DIMS, _P, _P, _P, _P, _P, _P]
+_lib.mcpu_shrink_block_tables.restype = ctypes.c_int
+_lib.mcpu_copy_pages.argtypes = [_P, _I32, _I64, _I32, _P, _P, _I32, _P, _P]
+_lib.mcpu_copy_pages.restype = ctypes.c_int
 
 MAX_HOST_SLICES = 8
 MAX_HOST_SLOTS = 4
@@ -496,3 +514,180 @@ def mcpu_paged_attention_host_fp8(stage, q_host, k_new_host, v_new_host, kv8, bl
         "mcpu_paged_attention_host_fp8",
     )
     stage._pending.append((q_host, k_new_host, v_new_host, out_host, lse_host, sl, qsl, opts))
+
+
+# ------------------------------------------------------- tree-drafted decoding
+MAX_TREE_WORDS = 8
+MAX_POOLS = 128
+MAX_FORKS = 2048
+PAGE_SCRATCH = 64
+
+
+def _raw(t):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(stream):
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+
+
+def _token_stride(x, what):
+    """Elements from one token to the next of a [T, H, D] tensor whose tokens are dense inside."""
+    s = x.stride()
+    if x.dim() != 3 or x.dtype != torch.bfloat16 or s[2] != 1 or s[1] != x.shape[2]:
+        raise ValueError(f"{what} must be a bfloat16 [T, H, D] tensor with the heads of a token dense")
+    return s[0] if x.shape[0] > 1 else max(s[0], s[1] * x.shape[1])
+
+
+def _int32(x, what):
+    if x.dtype != torch.int32 or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor")
+    return x.data_ptr()
+
+
+def mcpu_norm_rope_kv_append(q, k_new, v_new, q_weight, k_weight, eps, positions, cos_sin, q_out, k_cache, v_cache,
+                             block_table, seq_lens, query_start_loc, status_word, stream=None):
+    """RMS norm of every q and k head (float32 weights [D]), rotation at
+    positions (int32 [T], or None for the tokens' own slots), q to q_out, K
+    and V to the pages. q, k_new and v_new may be slices of one projection's
+    output (any token stride that is a multiple of 8 elements)."""
+    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or cos_sin.shape[1] != q.shape[2] or \
+            not cos_sin.is_contiguous():
+        raise ValueError("cos_sin must be a contiguous float32 [max_position, head_dim] tensor")
+    for w in (q_weight, k_weight):
+        if w.dtype != torch.float32 or w.numel() != q.shape[2] or not w.is_contiguous():
+            raise ValueError("q_weight and k_weight must be contiguous float32 [head_dim] tensors")
+    if q_out.dtype != torch.bfloat16 or q_out.shape != q.shape or not q_out.is_contiguous():
+        raise ValueError("q_out must be a contiguous bfloat16 tensor of q's shape")
+    if positions is not None and positions.numel() != q.shape[0]:
+        raise ValueError("positions must have one entry per query token")
+    if k_new.shape != v_new.shape or k_new.shape[0] != q.shape[0] or k_new.shape[1] != k_cache.shape[1]:
+        raise ValueError("k_new and v_new must be [T, H_kv, D]")
+    d = dims(q, k_cache, block_table, seq_lens)
+    code = _lib.mcpu_norm_rope_kv_append(
+        q.data_ptr(), _token_stride(q, "q"), k_new.data_ptr(), _token_stride(k_new, "k_new"), v_new.data_ptr(),
+        _token_stride(v_new, "v_new"), q_weight.data_ptr(), k_weight.data_ptr(), eps,
+        None if positions is None else _int32(positions, "positions"), cos_sin.data_ptr(), cos_sin.shape[0],
+        q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+        query_start_loc.data_ptr(), d, status_word.data_ptr(), _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_norm_rope_kv_append")
+
+
+def mcpu_tree_workspace_size(d: Dims) -> int:
+    return int(_lib.mcpu_tree_workspace_size(d))
+
+
+def new_tree_workspace(d: Dims, device="cuda") -> torch.Tensor:
+    """A zeroed workspace of the size mcpu_tree_workspace_size(d) asks for."""
+    n = mcpu_tree_workspace_size(d)
+    if n == 0:
+        raise McpuError(1, "mcpu_tree_workspace_size")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def mcpu_tree_attention_forward(q, k_cache, v_cache, block_table, seq_lens, query_start_loc, tree_mask, positions,
+                                sliding_window, softmax_scale, out, lse, workspace, sinks=None, stream=None):
+    """Attention of drafted-token trees: node i of a row sees the row's
+    context (inside the window of its position) and the nodes whose bit is
+    set in its tree_mask row (int32 [T, words], 32 nodes a word). positions
+    (int32 [T]) may be None without a window; sinks: float32 [H_q] or None."""
+    if tree_mask.dim() != 2 or tree_mask.shape[0] != q.shape[0]:
+        raise ValueError("tree_mask must be an int32 [T, words] tensor")
+    if sinks is not None and (sinks.dtype != torch.float32 or sinks.numel() != q.shape[1] or not sinks.is_cuda):
+        raise ValueError("sinks must be a float32 CUDA tensor with one value per q head")
+    d = dims(q, k_cache, block_table, seq_lens)
+    code = _lib.mcpu_tree_attention_forward(
+        q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+        query_start_loc.data_ptr(), _int32(tree_mask, "tree_mask"), tree_mask.shape[1], _raw(positions), sliding_window,
+        softmax_scale, _raw(sinks), d, out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_tree_attention_forward")
+
+
+class PoolList:
+    """The pools that one block table serves (K and V of every layer), as the
+    array of pointers the calls over many pools take. Keeps the tensors."""
+
+    def __init__(self, pools):
+        self.pools = list(pools)
+        if not 1 <= len(self.pools) <= MAX_POOLS:
+            raise ValueError(f"1 to {MAX_POOLS} pools")
+        first = self.pools[0]
+        for x in self.pools:
+            if x.shape != first.shape or x.dtype != first.dtype or not x.is_contiguous():
+                raise ValueError("pools must be contiguous and of one shape and type")
+        self.pointers = (ctypes.c_void_p * len(self.pools))(*[x.data_ptr() for x in self.pools])
+        self.num_pages = int(first.shape[0])
+        self.num_kv_heads = int(first.shape[1])
+        self.page_bytes = int(first[0].numel() * first.element_size()) if self.num_pages else 0
+
+
+def mcpu_compact_kv(pools, block_table, seq_lens, query_start_loc, accept_path, accept_len, new_seq_lens, status_word,
+                    stream=None):
+    """Moves the accepted nodes' K/V rows (accept_path: int32 [B, max_accept]
+    node numbers, the first accept_len[r] of each row) behind the row's
+    context, in every pool of the PoolList (bf16 pools); new_seq_lens receives
+    the rows' lengths."""
+    p0 = pools.pools[0]
+    if p0.dim() != 4 or p0.dtype != torch.bfloat16:
+        raise ValueError("mcpu_compact_kv takes bfloat16 [num_pages, H_kv, 16, 64] pools")
+    if accept_path.dim() != 2 or accept_path.shape[0] != seq_lens.shape[0]:
+        raise ValueError("accept_path must be an int32 [B, max_accept] tensor")
+    d = Dims(seq_lens.shape[0], 0, block_table.shape[1], pools.num_pages, pools.num_kv_heads, pools.num_kv_heads,
+             p0.shape[3], p0.shape[2])
+    code = _lib.mcpu_compact_kv(
+        pools.pointers, len(pools.pools), block_table.data_ptr(), seq_lens.data_ptr(), query_start_loc.data_ptr(),
+        _int32(accept_path, "accept_path"), accept_path.shape[1], _int32(accept_len, "accept_len"), d,
+        new_seq_lens.data_ptr(), status_word.data_ptr(), _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_compact_kv")
+
+
+def _page_dims(block_table, page_refs) -> Dims:
+    return Dims(block_table.shape[0], 0, block_table.shape[1], page_refs.shape[0], 1, 1, 64, 16)
+
+
+def mcpu_fork_block_tables(block_table, seq_lens, src_rows, dst_rows, page_refs, free_pages, free_count, copy_src,
+                           copy_dst, page_scratch, status_word, stream=None):
+    """Makes rows dst_rows copies of src_rows: full pages shared (page_refs),
+    a partial last page replaced by a fresh one whose contents
+    mcpu_copy_pages(pools, copy_src, copy_dst, ...) brings over."""
+    n = src_rows.shape[0]
+    if dst_rows.shape[0] != n or copy_src.shape[0] < n or copy_dst.shape[0] < n or page_scratch.numel() < PAGE_SCRATCH:
+        raise ValueError("dst_rows, copy_src and copy_dst must have one entry per fork, page_scratch PAGE_SCRATCH")
+    code = _lib.mcpu_fork_block_tables(
+        block_table.data_ptr(), seq_lens.data_ptr(), _int32(src_rows, "src_rows"), _int32(dst_rows, "dst_rows"), n,
+        _page_dims(block_table, page_refs), page_refs.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+        _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), page_scratch.data_ptr(), status_word.data_ptr(),
+        _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_fork_block_tables")
+
+
+def mcpu_shrink_block_tables(block_table, seq_lens, sliding_window, page_refs, free_pages, free_count, page_scratch,
+                             status_word, stream=None):
+    """Releases every page past the rows' lengths (and, with a window, before
+    it); pages without another holder return to the stack."""
+    if free_pages.shape[0] < page_refs.shape[0] or page_scratch.numel() < PAGE_SCRATCH:
+        raise ValueError("free_pages must hold as many pages as page_refs counts, page_scratch PAGE_SCRATCH words")
+    code = _lib.mcpu_shrink_block_tables(
+        block_table.data_ptr(), seq_lens.data_ptr(), sliding_window, _page_dims(block_table, page_refs),
+        page_refs.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), page_scratch.data_ptr(),
+        status_word.data_ptr(), _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_shrink_block_tables")
+
+
+def mcpu_copy_pages(pools, copy_src, copy_dst, status_word, stream=None):
+    """Copies page copy_src[f] to copy_dst[f] in every pool of the PoolList
+    (bf16 or fp8); pairs with a negative page are skipped."""
+    n = copy_src.shape[0]
+    if copy_dst.shape[0] != n:
+        raise ValueError("copy_src and copy_dst must have the same length")
+    code = _lib.mcpu_copy_pages(pools.pointers, len(pools.pools), pools.page_bytes, pools.num_pages,
+                                _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), n, status_word.data_ptr(),
+                                _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_copy_pages")

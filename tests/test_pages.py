@@ -1,0 +1,364 @@
+"""Forking, shrinking and copying pages, and compacting accepted paths,
+against plain models of the tables, counts and stack (exact)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+gpu = pytest.mark.gpu
+
+
+def _i32(a):
+    return torch.from_numpy(np.ascontiguousarray(a).astype(np.int32)).cuda()
+
+
+class Model:
+    """Block tables, holder counts and the page stack on the host."""
+
+    def __init__(self, rows, width, pages, seed):
+        self.rng = np.random.default_rng(seed)
+        self.bt = np.full((rows, width), -1, np.int64)
+        self.sl = np.zeros(rows, np.int64)
+        self.refs = np.zeros(pages, np.int64)
+        self.free = [int(p) for p in self.rng.permutation(pages)]
+        self.pages = pages
+
+    def fill(self, r, n, first=0):
+        for j in range(first, (n + 15) // 16):
+            self.bt[r, j] = self.free.pop()
+        self.sl[r] = n
+
+    def fork(self, src, dst):
+        cs, cd, exhausted = [], [], False
+        for s, d in zip(src, dst):
+            n = int(self.sl[s])
+            full = n // 16
+            self.bt[d] = -1
+            self.bt[d, :full] = self.bt[s, :full]
+            for p in self.bt[d, :full]:
+                if p >= 0:
+                    self.refs[p] += 1
+            self.sl[d] = n
+            cs.append(-1)
+            cd.append(-1)
+            if n % 16:
+                if self.free:
+                    self.bt[d, full] = cd[-1] = self.free.pop()
+                    cs[-1] = int(self.bt[s, full])
+                else:
+                    exhausted = True
+        return cs, cd, exhausted
+
+    def shrink(self, keep, window=0):
+        gone = []
+        for r in range(len(self.sl)):
+            end = (keep[r] + 15) // 16
+            begin = max(0, keep[r] - window + 1) // 16 if window > 0 else 0
+            for j in range(self.bt.shape[1]):
+                p = int(self.bt[r, j])
+                if p >= 0 and not begin <= j < end:
+                    self.bt[r, j] = -1
+                    self.refs[p] -= 1
+                    if self.refs[p] < 0:
+                        self.refs[p] = 0
+                        gone.append(p)
+        self.free += sorted(gone)
+
+    def device(self):
+        free = np.zeros(self.pages, np.int64)
+        free[:len(self.free)] = self.free
+        return dict(bt=_i32(self.bt), sl=_i32(self.sl), refs=_i32(self.refs), free=_i32(free),
+                    count=_i32([len(self.free)]), scratch=torch.zeros(64, dtype=torch.int32, device="cuda"),
+                    status=torch.zeros(1, dtype=torch.int32, device="cuda"))
+
+    def same(self, d, status=0):
+        assert np.array_equal(d["bt"].cpu().numpy(), self.bt)
+        assert np.array_equal(d["sl"].cpu().numpy(), self.sl)
+        assert np.array_equal(d["refs"].cpu().numpy(), self.refs)
+        n = int(d["count"].item())
+        assert n == len(self.free) and d["free"][:n].cpu().tolist() == self.free
+        assert int(d["status"].item()) == status and not d["scratch"].any()
+
+
+def _fork(d, src, dst):
+    from paper_2608_22167_gb300 import mcpu
+
+    cs, cd = (torch.full((len(src),), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    mcpu.mcpu_fork_block_tables(d["bt"], d["sl"], _i32(src), _i32(dst), d["refs"], d["free"], d["count"], cs, cd,
+                                d["scratch"], d["status"])
+    return cs, cd
+
+
+def _shrink(d, keep, window=0):
+    from paper_2608_22167_gb300 import mcpu
+
+    mcpu.mcpu_shrink_block_tables(d["bt"], _i32(keep), window, d["refs"], d["free"], d["count"], d["scratch"],
+                                  d["status"])
+
+
+@gpu
+@pytest.mark.parametrize("rows,width,pages", [(9, 5, 60), (300, 40, 9001), (2048, 7, 30000)])
+def test_rounds_of_forks_and_releases(rows, width, pages):
+    m = Model(rows, width, pages, rows)
+    g = max(1, rows // 5)
+    for r in range(g):
+        m.fill(r, int(m.rng.integers(0, width * 16 + 1)))
+    d = m.device()
+    for _ in range(4):
+        n = int(m.rng.integers(1, rows - g + 1))
+        src = m.rng.integers(0, g, n)
+        dst = g + m.rng.permutation(rows - g)[:n]
+        cs, cd = _fork(d, src, dst)
+        ms, md, exhausted = m.fork(src, dst)
+        assert not exhausted and cs.cpu().tolist() == ms and cd.cpu().tolist() == md
+        m.same(d)
+        # some samples shrink a little, the rest leave
+        keep = m.sl.copy()
+        for r in range(g, rows):
+            keep[r] = 0 if m.rng.random() < 0.6 else int(m.rng.integers(0, m.sl[r] + 1))
+        _shrink(d, keep)
+        m.shrink(keep)
+        m.same(d)
+        keep[g:] = 0  # all samples leave before the next round
+        m.sl[g:] = 0
+        _shrink(d, keep)
+        m.shrink(keep)
+        d["sl"].copy_(_i32(m.sl))
+        m.same(d)
+    # a prompt leaves while a sample still holds its pages, then the sample
+    m.fork([0], [g])
+    _fork(d, [0], [g])
+    for gone in (0, g):
+        keep = m.sl.copy()
+        keep[gone] = m.sl[gone] = 0
+        d["sl"].copy_(_i32(m.sl))
+        _shrink(d, keep)
+        m.shrink(keep)
+        m.same(d)
+
+
+@gpu
+def test_shrink_before_a_window():
+    m = Model(40, 64, 3000, 5)
+    for r in range(40):
+        m.fill(r, int(m.rng.integers(0, 1025)))
+    d = m.device()
+    for window in (2000, 128, 100, 17, 16, 1):  # each keeps less than the one before
+        _shrink(d, m.sl, window)
+        m.shrink(m.sl, window)
+        m.same(d)
+
+
+@gpu
+def test_fork_with_an_empty_stack():
+    from paper_2608_22167_gb300 import mcpu
+
+    m = Model(6, 8, 12, 7)
+    m.fill(0, 100)
+    m.fill(1, 64)
+    m.free = m.free[:1]
+    d = m.device()
+    cs, cd = _fork(d, [0, 1, 0, 0], [2, 3, 4, 5])
+    ms, md, exhausted = m.fork([0, 1, 0, 0], [2, 3, 4, 5])
+    assert exhausted and cs.cpu().tolist() == ms and cd.cpu().tolist() == md
+    m.same(d, mcpu.STATUS_POOL_EXHAUSTED)
+
+
+@gpu
+def test_invalid_rows_pages_and_double_releases():
+    from paper_2608_22167_gb300 import mcpu
+
+    m = Model(6, 8, 60, 8)
+    m.fill(0, 100)
+    m.fill(1, 40)
+    d = m.device()
+    cs, cd = _fork(d, [0, 9, 0, -1, 1], [2, 3, 0, 4, 77])  # only the first is a valid pair
+    ms, md, _ = m.fork([0], [2])
+    assert cs.cpu().tolist() == ms + [-1] * 4 and cd.cpu().tolist() == md + [-1] * 4
+    m.same(d, mcpu.STATUS_BAD_LENGTHS)
+    d["status"].zero_()
+    # lengths outside the table: the row is left alone
+    keep = m.sl.copy()
+    keep[0], keep[1] = -1, 129
+    _shrink(d, keep)
+    m.same(d, mcpu.STATUS_BAD_LENGTHS)
+    d["status"].zero_()
+    # an entry outside the pool is cleared and reported
+    d["bt"][5, 3] = 60
+    _shrink(d, m.sl)
+    m.same(d, mcpu.STATUS_BAD_PAGE)
+    d["status"].zero_()
+    # a page in two tables without a holder count: it returns once
+    d["bt"][5, 0] = int(m.bt[1, 0])
+    keep = m.sl.copy()
+    keep[1] = 0
+    m.sl[1] = 0
+    d["sl"][1] = 0
+    _shrink(d, keep)
+    m.shrink(keep)
+    m.same(d, mcpu.STATUS_BAD_PAGE)
+
+
+@gpu
+@pytest.mark.parametrize("shape,dtype", [((50, 8, 16, 64), torch.bfloat16), ((50, 1, 16, 64), torch.bfloat16),
+                                         ((50, 3, 2176), torch.uint8)])
+@pytest.mark.parametrize("pools", [1, 3, 128])
+def test_copy_pages(shape, dtype, pools):
+    from paper_2608_22167_gb300 import mcpu
+
+    rng = np.random.default_rng(pools)
+    raw = [torch.from_numpy(rng.integers(0, 256, (shape[0], int(np.prod(shape[1:])) * dtype.itemsize), dtype=np.uint8))
+           for _ in range(pools)]
+    dev = [r.cuda().view(dtype).view(shape) for r in raw]
+    perm = rng.permutation(50)
+    src = np.concatenate([perm[:5], perm[:5], [-1, 4]])
+    dst = np.concatenate([perm[5:15], [3, -1]])
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    mcpu.mcpu_copy_pages(mcpu.PoolList(dev), _i32(src), _i32(dst), status)
+    for r, x in zip(raw, dev):
+        want = r.clone()
+        want[perm[5:15]] = r[src[:10]]
+        assert torch.equal(x.view(torch.uint8).view(50, -1).cpu(), want)
+    assert int(status.item()) == 0
+    mcpu.mcpu_copy_pages(mcpu.PoolList(dev), _i32([50, 1]), _i32([1, 50]), status)
+    assert int(status.item()) == mcpu.STATUS_BAD_PAGE
+
+
+def _compact_case(ctx, lens, taken, hkv, pools, seed, most=None):
+    rng = np.random.default_rng(seed)
+    ctx, lens, taken = (np.asarray(x, np.int64) for x in (ctx, lens, taken))
+    S = ctx + lens
+    last = (S + 15) // 16
+    P = int(last.sum()) + 1
+    ids = rng.permutation(P)
+    bt = np.full((len(S), max(1, int(last.max()))), -1, np.int64)
+    k = 0
+    for r in range(len(S)):
+        bt[r, :last[r]] = ids[k:k + last[r]]
+        k += int(last[r])
+    most = most or max(1, int(taken.max()))
+    path = np.full((len(S), most), 12345, np.int64)
+    for r in range(len(S)):
+        path[r, :taken[r]] = np.sort(rng.permutation(int(lens[r]))[:taken[r]])
+    host = [torch.from_numpy(rng.integers(-30000, 30000, (P, hkv, 16, 64)).astype(np.int16)) for _ in range(pools)]
+    return dict(ctx=ctx, lens=lens, taken=taken, S=S, bt=bt, path=path, host=host,
+                dev=[h.cuda().view(torch.bfloat16) for h in host], new=_i32(np.full(len(S), -5)),
+                status=torch.zeros(1, dtype=torch.int32, device="cuda"))
+
+
+def _compact(c):
+    from paper_2608_22167_gb300 import mcpu
+
+    qsl = np.concatenate([[0], np.cumsum(c["lens"])])
+    mcpu.mcpu_compact_kv(mcpu.PoolList(c["dev"]), _i32(c["bt"]), _i32(c["S"]), _i32(qsl), _i32(c["path"]),
+                         _i32(c["taken"]), c["new"], c["status"])
+
+
+def _compact_same(c, skip=()):
+    for h, x in zip(c["host"], c["dev"]):
+        want = h.clone()
+        for r in range(len(c["S"])):
+            if r in skip:
+                continue
+            old = c["ctx"][r] + c["path"][r, :c["taken"][r]]
+            new = c["ctx"][r] + np.arange(c["taken"][r])
+            want[c["bt"][r, new // 16], :, new % 16] = h[c["bt"][r, old // 16], :, old % 16]
+        assert torch.equal(x.view(torch.int16).cpu(), want)
+    want = [int(c["S"][r]) if r in skip else int(c["ctx"][r] + c["taken"][r]) for r in range(len(c["S"]))]
+    assert c["new"].cpu().tolist() == want
+
+
+@gpu
+@pytest.mark.parametrize("hkv,pools", [(8, 2), (2, 1), (1, 5), (3, 128), (16, 7)])
+def test_compact(hkv, pools):
+    rng = np.random.default_rng(hkv)
+    ctx = np.concatenate([[0, 15, 16, 1, 255], rng.integers(0, 100, 20)])
+    lens = np.concatenate([[1, 2, 0, 300, 33], rng.integers(0, 64, 20)])
+    taken = np.array([int(rng.integers(0, n + 1)) for n in lens])
+    taken[3] = 290
+    c = _compact_case(ctx, lens, taken, hkv, pools, 3)
+    _compact(c)
+    _compact_same(c)
+    assert int(c["status"].item()) == 0
+
+
+@gpu
+def test_compact_leaves_wrong_rows_alone():
+    from paper_2608_22167_gb300 import mcpu
+
+    c = _compact_case([5, 6, 7, 8, 9, 10, 40], [9] * 7, [4, 4, 4, 4, 4, 4, 4], 2, 3, 4, most=6)
+    c["path"][0, :4] = [1, 1, 2, 3]    # not increasing
+    c["path"][1, :4] = [0, 2, 4, 9]    # past the nodes
+    c["path"][2, :4] = [-1, 0, 1, 2]
+    c["taken"][3] = 7                  # more than the path holds
+    c["taken"][4] = -1
+    _compact(c)
+    _compact_same(c, skip=(0, 1, 2, 3, 4))
+    assert int(c["status"].item()) == mcpu.STATUS_BAD_LENGTHS
+    c = _compact_case([5, 30], [20, 9], [3, 4], 2, 3, 5)
+    c["path"][0] = [1, 3, 15, 0][:c["path"].shape[1]]
+    good = c["bt"].copy()
+    c["bt"][0, 1] = 1 << 20
+    _compact(c)
+    c["bt"] = good
+    _compact_same(c, skip=(0,))
+    assert int(c["status"].item()) == mcpu.STATUS_BAD_PAGE
+
+
+def test_host_checks():
+    from paper_2608_22167_gb300 import mcpu
+
+    P = 1 << 20
+    D = mcpu.Dims
+    lib = mcpu._lib
+    ptrs = (ctypes.c_void_p * 3)(P, P, P)
+    odd = (ctypes.c_void_p * 3)(P, P + 8, P)
+    nul = (ctypes.c_void_p * 3)(P, None, P)
+    d, d0 = D(4, 9, 19, 34, 2, 2, 64, 16), D(0, 0, 19, 34, 2, 2, 64, 16)
+    bad = D(4, 9, 19, -1, 2, 2, 64, 16)
+
+    def compact(pools=ptrs, n=3, bt=P, sl=P, qsl=P, path=P, most=4, taken=P, dims=d, new=P + 64, st=P):
+        return lib.mcpu_compact_kv(pools, n, bt, sl, qsl, path, most, taken, ctypes.byref(dims), new, st, None)
+
+    assert compact(pools=None) == 1 and compact(pools=odd) == 1 and compact(pools=nul) == 1
+    assert compact(n=-1) == 1 and compact(n=129) == 1 and compact(most=-1) == 1 and compact(path=None) == 1
+    assert compact(new=P) == 1 and compact(st=None) == 1 and compact(taken=P + 2) == 1 and compact(bt=None) == 1
+    assert compact(dims=bad) == 1 and compact(dims=D(4, 9, 19, 34, 2, 2, 32, 16)) == 2 and compact(dims=d0) == 0
+
+    def fork(n=3, dims=d, **kw):
+        names = ("bt", "sl", "src", "dst", "refs", "free", "count", "cs", "cd", "scratch", "st")
+        a = [kw.get(k, P) for k in names]
+        return lib.mcpu_fork_block_tables(*a[:4], n, ctypes.byref(dims), *a[4:], None)
+
+    for k in ("bt", "sl", "src", "dst", "refs", "free", "count", "cs", "cd", "scratch", "st"):
+        assert fork(**{k: None}) == 1 and fork(**{k: P + 1}) == 1, k
+    assert fork(n=-1) == 1 and fork(n=2049) == 2 and fork(n=0) == 0 and fork(dims=bad) == 1
+
+    def shrink(dims=d, **kw):
+        a = [kw.get(k, P) for k in ("bt", "sl", "refs", "free", "count", "scratch", "st")]
+        return lib.mcpu_shrink_block_tables(*a[:2], 0, ctypes.byref(dims), *a[2:], None)
+
+    for k in ("bt", "sl", "refs", "free", "count", "scratch", "st"):
+        assert shrink(**{k: None}) == 1 and shrink(**{k: P + 1}) == 1, k
+    assert shrink(dims=bad) == 1 and shrink(dims=d0) == 0
+
+    def copy(pools=ptrs, n=3, size=2048, pages=9, cs=P, cd=P, m=4, st=P):
+        return lib.mcpu_copy_pages(pools, n, size, pages, cs, cd, m, st, None)
+
+    assert copy(pools=odd) == 1 and copy(size=0) == 1 and copy(size=24) == 1 and copy(pages=-1) == 1 and copy(m=-1) == 1
+    assert copy(cs=None) == 1 and copy(cd=P + 2) == 1 and copy(st=None) == 1 and copy(m=0) == 0 and copy(n=0) == 0
+    assert copy(size=1 << 31) == 2
+
+
+def test_pool_lists():
+    from paper_2608_22167_gb300 import mcpu
+
+    a, b = torch.zeros(3, 2, 16, 64, dtype=torch.bfloat16), torch.zeros(4, 2, 16, 64, dtype=torch.bfloat16)
+    assert mcpu.PoolList([a, a.clone()]).page_bytes == 2 * 2048
+    for bad in ([], [a, b], [a, a.half()], [a[:, :1]], [a] * 129):
+        with pytest.raises(ValueError):
+            mcpu.PoolList(bad)
+    with pytest.raises(ValueError):
+        mcpu.mcpu_compact_kv(mcpu.PoolList([torch.zeros(3, 2, 2176, dtype=torch.uint8)]), None, None, None, None, None,
+                             None, None)
