@@ -48,6 +48,7 @@ cudaError_t launch_kv_append_fp8(const void* k_new, const void* v_new, void* kv8
 cudaError_t launch_decode_fp8(const void* kv8, const AttnParams& p, int grid, bool cascade, cudaStream_t stream,
                               bool programmatic);
 cudaError_t prepare_fp8_kernels(int* bpsm_decode, int* bpsm_cascade);
+cudaError_t prepare_tree_kernels();
 }  // namespace mcpu
 
 namespace {
@@ -97,6 +98,7 @@ mcpu_status device_state(DeviceState** out) {
     if ((e = prepare_merge_kernel()) != cudaSuccess) return cuda_fail(e);
     if ((e = prepare_kv_append_kernel()) != cudaSuccess) return cuda_fail(e);
     if ((e = prepare_fp8_kernels(&st.bpsm_fp8, &st.bpsm_fp8_cascade)) != cudaSuccess) return cuda_fail(e);
+    if ((e = prepare_tree_kernels()) != cudaSuccess) return cuda_fail(e);
     if (st.bpsm_decode < 1 || st.bpsm_cascade < 1 || st.bpsm_append < 1 || st.bpsm_append_tc < 1 ||
         st.bpsm_fp8 < 1 || st.bpsm_fp8_cascade < 1)
       return MCPU_ERR_CUDA;
@@ -109,33 +111,6 @@ mcpu_status device_state(DeviceState** out) {
   }
   *out = &st;
   return MCPU_OK;
-}
-
-// 2-D view of a pool: rows of D = 64 bf16 (128 bytes), num_pages*H_kv*16 rows;
-// boxes of one (page, kv head) block = 16 rows, 128-byte swizzle.
-bool encode_pool(CUtensorMap* map, const void* pool, int64_t rows) {
-  cuuint64_t dims[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)rows};
-  cuuint64_t strides[1] = {(cuuint64_t)kRowBytes};
-  cuuint32_t box[2] = {(cuuint32_t)kHeadDim, (cuuint32_t)kPage};
-  cuuint32_t estr[2] = {1, 1};
-  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides, box, estr,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS;
-}
-
-// 3-D view of q [T, H_q, D]: boxes of (256 / g) tokens x the g heads of one kv
-// head x 64 dims, i.e. the two 128-row query tiles of an append item, 128-byte
-// swizzle.
-bool encode_query(CUtensorMap* map, const void* q, int32_t total_q, int32_t num_q_heads, int32_t group) {
-  cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)num_q_heads, (cuuint64_t)total_q};
-  cuuint64_t strides[2] = {(cuuint64_t)kRowBytes, (cuuint64_t)kRowBytes * num_q_heads};
-  cuuint32_t box[3] = {(cuuint32_t)kHeadDim, (cuuint32_t)group, (cuuint32_t)(kAppendTcRows / group)};
-  cuuint32_t estr[3] = {1, 1, 1};
-  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, estr,
-                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS;
 }
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -169,6 +144,40 @@ mcpu_status check_dims(const mcpu_dims* d) {
 }
 
 mcpu_status from_cuda(cudaError_t e) { return e == cudaSuccess ? MCPU_OK : cuda_fail(e); }
+
+mcpu_status device_sms(int* sms) {
+  DeviceState* dev = nullptr;
+  const mcpu_status st = device_state(&dev);
+  if (st == MCPU_OK) *sms = dev->sms;
+  return st;
+}
+
+// 2-D view of a pool: rows of D = 64 bf16 (128 bytes), num_pages*H_kv*16 rows;
+// boxes of one (page, kv head) block = 16 rows, 128-byte swizzle.
+bool encode_pool(CUtensorMap* map, const void* pool, int64_t rows) {
+  cuuint64_t dims[2] = {(cuuint64_t)kHeadDim, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)kRowBytes};
+  cuuint32_t box[2] = {(cuuint32_t)kHeadDim, (cuuint32_t)kPage};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(pool), dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
+
+// 3-D view of q [T, H_q, D]: boxes of (rows / g) tokens x the g heads of one kv
+// head x 64 dims (256 rows: the two 128-row query tiles of an append item),
+// 128-byte swizzle.
+bool encode_query(CUtensorMap* map, const void* q, int32_t total_q, int32_t num_q_heads, int32_t group, int32_t rows) {
+  cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)num_q_heads, (cuuint64_t)total_q};
+  cuuint64_t strides[2] = {(cuuint64_t)kRowBytes, (cuuint64_t)kRowBytes * num_q_heads};
+  cuuint32_t box[3] = {(cuuint32_t)kHeadDim, (cuuint32_t)group, (cuuint32_t)(rows / group)};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, estr,
+                        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS;
+}
 
 }  // namespace mcpu
 
@@ -287,7 +296,7 @@ mcpu_status mcpu_paged_attention_forward(const void* q, const void* k_cache, con
   const int group = dims->num_q_heads / dims->num_kv_heads;
   CUtensorMap kmap, vmap, qmap;
   if (!encode_pool(&kmap, k_cache, rows) || !encode_pool(&vmap, v_cache, rows)) return MCPU_ERR_INVALID_ARG;
-  if (!legacy_append && !encode_query(&qmap, q, dims->total_q, dims->num_q_heads, group)) return MCPU_ERR_INVALID_ARG;
+  if (!legacy_append && !encode_query(&qmap, q, dims->total_q, dims->num_q_heads, group, kAppendTcRows)) return MCPU_ERR_INVALID_ARG;
 
   AttnParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);
@@ -517,7 +526,7 @@ mcpu_status mcpu_selftest_append_abort(const void* q, const void* k_cache, const
   const int group = dims->num_q_heads / dims->num_kv_heads;
   CUtensorMap kmap, vmap, qmap;
   if (!encode_pool(&kmap, k_cache, rows) || !encode_pool(&vmap, v_cache, rows) ||
-      !encode_query(&qmap, q, dims->total_q, dims->num_q_heads, group))
+      !encode_query(&qmap, q, dims->total_q, dims->num_q_heads, group, kAppendTcRows))
     return MCPU_ERR_INVALID_ARG;
   AttnParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);

@@ -1,9 +1,10 @@
 // Host-side pieces shared by the translation units of the C ABI (api.cu,
-// api_noalloc.cu): the dimension checks every forward entry point applies,
-// and the recording of the failed CUDA call behind an MCPU_ERR_CUDA (read
+// api_noalloc.cu, api_tree.cu): the dimension checks every forward entry point
+// applies, the tensor maps of pools and queries, and the recording of the failed CUDA call behind an MCPU_ERR_CUDA (read
 // back with mcpu_last_cuda_error).
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "../../include/mcpu.h"
@@ -22,5 +23,15 @@ mcpu_status cuda_fail(cudaError_t e);
 
 // MCPU_OK for cudaSuccess, else cuda_fail(e).
 mcpu_status from_cuda(cudaError_t e);
+
+// One-time setup of the current device (kernel attributes, tensor-map entry
+// point); its SM count. Needed before the encoders below.
+mcpu_status device_sms(int* sms);
+
+// Tensor map of a bf16 pool as `rows` rows of 64 values, one box per (page,
+// kv head) block; and of q [T, H_q, D], one box per `rows` query rows (rows /
+// group tokens x the group's heads). False if the map cannot be made.
+bool encode_pool(CUtensorMap* map, const void* pool, int64_t rows);
+bool encode_query(CUtensorMap* map, const void* q, int32_t total_q, int32_t num_q_heads, int32_t group, int32_t rows);
 
 }  // namespace mcpu

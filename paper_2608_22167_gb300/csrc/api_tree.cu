@@ -33,6 +33,20 @@ mcpu_status check_page_dims(const mcpu_dims* d) {
   return MCPU_OK;
 }
 
+// Workspace: the status word, the plan, the parts of split items. Returns its
+// size; with `p`, sets p's pointers into `ws`.
+size_t tree_layout(uint8_t* ws, int32_t num_seqs, TreeParams* p) {
+  const size_t plan = 256, lse = align_up(plan + sizeof(int64_t) * ((size_t)num_seqs + 2), 256);
+  const size_t o = align_up(lse + sizeof(float) * 2 * kTreeMaxCtas * 256, 256);
+  if (p) {
+    p->status = reinterpret_cast<int32_t*>(ws);
+    p->plan = reinterpret_cast<int64_t*>(ws + plan);
+    p->lse_part = reinterpret_cast<float*>(ws + lse);
+    p->o_part = reinterpret_cast<float*>(ws + o);
+  }
+  return align_up(o + sizeof(float) * 2 * kTreeMaxCtas * 256 * kHeadDim, 256);
+}
+
 }  // namespace
 
 extern "C" {
@@ -91,7 +105,7 @@ mcpu_status mcpu_norm_rope_kv_append(const void* q, int64_t q_stride, const void
 
 size_t mcpu_tree_workspace_size(const mcpu_dims* dims) {
   if (check_dims(dims) != MCPU_OK) return 0;
-  return 256;
+  return tree_layout(nullptr, dims->num_seqs, nullptr);
 }
 
 mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, const void* v_cache,
@@ -115,10 +129,18 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
     return MCPU_ERR_INVALID_ARG;
   if (sliding_window > 0 && !positions) return MCPU_ERR_INVALID_ARG;
   if (dims->num_pages < 1 || dims->max_pages_per_seq < 1) return MCPU_ERR_INVALID_ARG;
+  int sms = 0;
+  st = device_sms(&sms);
+  if (st != MCPU_OK) return st;
+  const int group = dims->num_q_heads / dims->num_kv_heads;
+  const int64_t rows = (int64_t)dims->num_pages * dims->num_kv_heads * kPage;
+  CUtensorMap kmap, vmap, qmap, qmap_alt;
+  if (!encode_pool(&kmap, k_cache, rows) || !encode_pool(&vmap, v_cache, rows) ||
+      !encode_query(&qmap, q, dims->total_q, dims->num_q_heads, group, 256) ||
+      !encode_query(&qmap_alt, q, dims->total_q, dims->num_q_heads, group, 128))
+    return MCPU_ERR_INVALID_ARG;
   TreeParams p;
-  p.q = static_cast<const __nv_bfloat16*>(q);
-  p.k_cache = static_cast<const __nv_bfloat16*>(k_cache);
-  p.v_cache = static_cast<const __nv_bfloat16*>(v_cache);
+  tree_layout(static_cast<uint8_t*>(workspace), dims->num_seqs, &p);
   p.block_table = block_table;
   p.seq_lens = seq_lens;
   p.qsl = query_start_loc;
@@ -127,7 +149,6 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
   p.sinks = sinks;
   p.out = static_cast<__nv_bfloat16*>(out);
   p.lse = lse;
-  p.status = static_cast<int32_t*>(workspace);
   p.words = mask_words;
   p.window = sliding_window > 0 ? sliding_window : 0;
   p.num_seqs = dims->num_seqs;
@@ -136,9 +157,10 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
   p.num_pages = dims->num_pages;
   p.num_q_heads = dims->num_q_heads;
   p.num_kv_heads = dims->num_kv_heads;
-  p.group = dims->num_q_heads / dims->num_kv_heads;
+  p.group = group;
+  p.oob_row = (int32_t)rows;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
-  return from_cuda(launch_tree(p, reinterpret_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_tree(kmap, vmap, qmap, qmap_alt, p, sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 mcpu_status mcpu_compact_kv(void* const* pools, int32_t num_pools, const int32_t* block_table,

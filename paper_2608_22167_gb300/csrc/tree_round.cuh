@@ -24,7 +24,6 @@ struct NormRopeParams {
 cudaError_t launch_norm_rope(const NormRopeParams& p, cudaStream_t stream);
 
 struct TreeParams {
-  const __nv_bfloat16 *q, *k_cache, *v_cache;
   const int32_t *block_table, *seq_lens, *qsl;
   const uint32_t* mask;      // [T, words]
   const int32_t* positions;  // [T], read with a window only
@@ -32,10 +31,16 @@ struct TreeParams {
   __nv_bfloat16* out;
   float* lse;
   int32_t* status;
+  int64_t* plan;    // the quota of a CTA, then the prefix sums of the rows' costs [num_seqs + 1]
+  float* lse_part;  // [2 * kTreeMaxCtas][256] base-2 normalisers of split items' parts
+  float* o_part;    // [2 * kTreeMaxCtas][256][64], normalised
   int32_t words, window, num_seqs, total_q, max_pages, num_pages, num_q_heads, num_kv_heads, group;
+  int32_t oob_row;   // a pool row past the end: read as zeros
   float scale_log2;  // softmax scale * log2(e)
 };
-cudaError_t launch_tree(const TreeParams& p, cudaStream_t stream);
+constexpr int kTreeMaxCtas = 160;  // CTAs the workspace has room for (one per SM)
+cudaError_t launch_tree(const CUtensorMap& kmap, const CUtensorMap& vmap, const CUtensorMap& qmap,
+                        const CUtensorMap& qmap_alt, const TreeParams& p, int sms, cudaStream_t stream);
 
 struct PoolPtrs {
   uint8_t* p[MCPU_MAX_POOLS];
