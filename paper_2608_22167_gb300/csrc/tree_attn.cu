@@ -161,6 +161,27 @@ __device__ __forceinline__ bool wait_poll(uint32_t bar, uint32_t parity, volatil
   return true;
 }
 
+// A 2-D box load issued by one elected lane of a warp that runs in step: its
+// operands stay in the uniform datapath (from a lone lane every operand is
+// moved there first, which made the issue of a block's 16 boxes take longer
+// than their transfer).
+__device__ __forceinline__ void tma_load_2d_e(uint32_t dst, const CUtensorMap* map, int32_t y, uint32_t bar,
+                                              uint64_t policy) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%2, %3}], [%4], %5;\n\t}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(y), "r"(bar), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void arrive_expect_tx_e(uint32_t bar, uint32_t bytes) {
+  asm volatile(
+      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
+      "r"(bytes)
+      : "memory");
+}
+
 // ------------------------------------------------------------------ softmax
 // the low n bits (none for n <= 0, all for n >= 32)
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
@@ -227,6 +248,40 @@ __device__ __forceinline__ float chunk_weights(const uint32_t (&sv)[2][32], floa
 
 __device__ __forceinline__ void zero_smem16(uint32_t addr) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0u) : "memory");
+}
+
+// What the masks say about the block of keys at kb: seen[c], the keys kb + 32c ..
+// that the thread's node (token t, window from key lo) sees; returns whether
+// the slot kb + 32 wq + lane holds a V row that no node of the row sees.
+__device__ __forceinline__ bool block_masks(const TreeParams& p, const Part& a, int t, int lo, int kb, int wq, int lane,
+                                            uint32_t (&seen)[4]) {
+  const int ctx = a.ctx, len = a.len, j = kb + 32 * wq + lane;
+  uint32_t mw[5] = {0, 0, 0, 0, 0};
+  const int n0 = kb - ctx, w0 = n0 >> 5;  // node of the block's first key, and its mask word
+  bool dead = j < a.key_begin;
+  if (n0 > -kBlockKeys) {
+#pragma unroll
+    for (int c = 0; c < 5; ++c)
+      if (w0 + c >= 0 && w0 + c < p.words) mw[c] = __ldg(p.mask + (size_t)t * p.words + w0 + c);
+    uint32_t u0 = 0, u1 = 0;  // union over the row's nodes of the two words with this warp's slots
+    for (int k = lane; k < len - ctx; k += 32) {
+      const uint32_t* m = p.mask + (size_t)(a.token - a.node + k) * p.words;
+      if (w0 + wq >= 0 && w0 + wq < p.words) u0 |= __ldg(m + w0 + wq);
+      if (w0 + wq + 1 >= 0 && w0 + wq + 1 < p.words) u1 |= __ldg(m + w0 + wq + 1);
+    }
+    u0 = __reduce_or_sync(0xffffffffu, u0);
+    u1 = __reduce_or_sync(0xffffffffu, u1);
+    const uint32_t any = __funnelshift_r(u0, u1, n0 & 31);
+    // past the row's end only its last page holds anything: later pages arrive as zeros
+    dead |= j >= len ? j < ((len + kPage - 1) & ~(kPage - 1)) : j >= ctx && !(any >> lane & 1u);
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const int k0 = kb + 32 * c;
+    seen[c] = (low_bits(ctx - k0) & ~low_bits(lo - k0)) |
+              (__funnelshift_r(mw[c], mw[c + 1], n0 & 31) & low_bits(len - k0));
+  }
+  return dead;
 }
 
 __device__ __forceinline__ float tree_sink(const TreeParams& p, int h) {
@@ -434,13 +489,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         if (it >= (uint32_t)nst &&
             !__all_sync(0xffffffffu, wait_sleep(bar(empty[s]), ((it / nst) - 1) & 1, abort_flag)))
           return false;
-        if (lane == 0) {
-          const uint32_t dst = (is_k ? sK : sV) + s * kBlockBytes;
-          mbar_arrive_expect_tx(bar(full[s]), kBlockBytes);
+        const uint32_t dst = (is_k ? sK : sV) + s * kBlockBytes;
+        arrive_expect_tx_e(bar(full[s]), kBlockBytes);
 #pragma unroll
-          for (int j = 0; j < kBlockPages; ++j)
-            tma_load_2d(dst + j * kTileBytes, is_k ? &kmap : &vmap, 0, y[j], bar(full[s]), pol);
-        }
+        for (int j = 0; j < kBlockPages; ++j)
+          tma_load_2d_e(dst + j * kTileBytes, is_k ? &kmap : &vmap, y[j], bar(full[s]), pol);
         (is_k ? k_issued : v_issued) = it + 1;
         return true;
       };
@@ -554,96 +607,90 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const int slot = i & 1;
       ok = __all_sync(0xffffffffu, wait_poll(bar(st.part_full[slot]), (i >> 1) & 1, abort_flag));
       if (!ok) break;
-      const Part a = st.parts[slot];
+      const Part& a = st.parts[slot];  // valid until part_empty; re-read where needed to save registers
       if (a.row < 0) break;
+      const bool alt = a.alt;
       const int n = a.b1 - a.b0;
-      const int nx = a.alt ? (n + 1 - x) / 2 : n;
-      const int tok = (a.alt ? 0 : x * (kTileRows / g)) + tok0;
-      const bool valid = tok < a.n_tok;
+      const int nx = alt ? (n + 1 - x) / 2 : n;
+      const int tok = (alt ? 0 : x * (kTileRows / g)) + tok0;
+      const bool busy = (alt ? 0 : x * kTileRows) + wq * 32 < a.n_tok * g;  // this warp has rows
       const int t = a.token + min(tok, a.n_tok - 1);
-      const bool busy = (a.alt ? 0 : x * kTileRows) + wq * 32 < a.n_tok * g;  // this warp has rows
-      const uint32_t* mrow = p.mask + (size_t)t * p.words;
-      const int first_tok = a.token - a.node, L = a.len - a.ctx;
       int lo = 0;
       if (p.window > 0) lo = min(max(__ldg(p.positions + t), a.ctx), a.len - 1) - p.window + 1;
-      // keys [plain_lo, ctx) are seen by every node
-      const int plain_lo = p.window > 0 ? a.len - p.window : 0;
+      // blocks that need no mask: keys [plain_lo, ctx) are seen by every node
+      const int plain_lo = p.window > 0 ? a.len - p.window : 0, plain_hi = a.ctx - kBlockKeys;
+      int kb = a.kb0 + (a.b0 + (alt ? x : 0)) * kBlockKeys;
+      uint32_t it = kv_it + (alt ? x : 0);
       float m_ref = -INFINITY, l = 0.f;
-      for (int b = 0; b < nx; ++b, ++cnt) {
-        const int bb = a.alt ? 2 * b + x : b;  // block of the part
-        const uint32_t it = kv_it + bb;
-        const int kb = a.kb0 + (a.b0 + bb) * kBlockKeys;
-        const bool nodes = kb + kBlockKeys > a.ctx;
-        const bool masked = nodes || kb < plain_lo;
-        // what the masks say about this block, read while S is computed: the
-        // thread's own words, and whether any node sees the slot whose V row
-        // this thread would clear
-        uint32_t mw[5] = {0, 0, 0, 0, 0};
-        const int w0 = (kb - a.ctx) >> 5;
-        bool dead = false;
-        if (nodes) {
+      // V rows that no node sees may hold anything, and a zero weight does not
+      // cancel a NaN: they are cleared before the tile's PV reads them
+      auto clear_dead = [&](bool dead) -> bool {
+        if (!__any_sync(0xffffffffu, dead)) return true;
+        const uint32_t s = it % kVStages;
+        if (!__all_sync(0xffffffffu, wait_poll(bar(st.v_full[s]), (it / kVStages) & 1, abort_flag))) return false;
+        if (dead) {
 #pragma unroll
-          for (int c = 0; c < 5; ++c)
-            if (w0 + c >= 0 && w0 + c < p.words) mw[c] = __ldg(mrow + w0 + c);
-          const int n0 = kb + wq * 32 - a.ctx;  // node of this warp's first slot
-          uint32_t u0w = 0, u1w = 0;
-          const int ua = n0 >> 5;
-          for (int k = lane; k < L; k += 32) {
-            const uint32_t* mk = p.mask + (size_t)(first_tok + k) * p.words;
-            if (ua >= 0 && ua < p.words) u0w |= __ldg(mk + ua);
-            if (ua + 1 >= 0 && ua + 1 < p.words) u1w |= __ldg(mk + ua + 1);
-          }
-          u0w = __reduce_or_sync(0xffffffffu, u0w);
-          u1w = __reduce_or_sync(0xffffffffu, u1w);
-          const uint32_t any = __funnelshift_r(u0w, u1w, n0 & 31);
-          const int j = kb + row;
-          // past the row's end only the last page holds anything: later pages arrive as zeros
-          dead = j >= a.len ? j < ((a.len + kPage - 1) & ~(kPage - 1)) : j >= a.ctx && !(any >> lane & 1u);
+          for (int c = 0; c < 8; ++c) zero_smem16(sV + s * kBlockBytes + row * kRowBytes + c * 16);
         }
-        dead |= kb + row < a.key_begin;
-        ok = __all_sync(0xffffffffu, wait_poll(bar(st.s_full[x]), cnt & 1, abort_flag));
-        if (!ok) break;
-        tc_fence_after();
-        auto seen = [&](int c) -> uint32_t {  // keys kb + 32c ..: bit e set if this thread's node sees it
-          const int k0 = kb + 32 * c;
-          const uint32_t ctx = low_bits(a.ctx - k0) & ~low_bits(lo - k0);
-          const uint32_t node = __funnelshift_r(mw[c], mw[c + 1], (kb - a.ctx) & 31) & low_bits(a.len - k0);
-          return ctx | node;
-        };
-        uint32_t sv[2][32], pk[32];
-        float alpha = 1.f, l0 = 0.f, l1 = 0.f;
-        if (busy) {
+        fence_proxy_async();
+        return true;
+      };
+      const int kb_step = alt ? 2 * kBlockKeys : kBlockKeys;
+      if (!busy) {  // none of this warp's rows is a query: it only keeps the barriers and clears V rows
+        for (int b = 0; b < nx; ++b, ++cnt, kb += kb_step, it += alt ? 2 : 1) {
+          uint32_t seen[4];
+          const bool dead = (kb > plain_hi || kb < plain_lo) && block_masks(p, a, t, lo, kb, wq, lane, seen);
+          ok = __all_sync(0xffffffffu, wait_poll(bar(st.s_full[x]), cnt & 1, abort_flag));
+          if (!ok) break;
+          if (lane == 0) mbar_arrive(bar(st.s_free[x]));
+          // in step with the other warps: one arrival per phase
+          if (cnt >= 1) {
+            ok = __all_sync(0xffffffffu, wait_poll(bar(st.o_ready[x]), (cnt - 1) & 1, abort_flag));
+            if (!ok) break;
+          }
+          ok = clear_dead(dead);
+          if (!ok) break;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(st.p_full[x]));
+        }
+      } else {
+        for (int b = 0; b < nx; ++b, ++cnt, kb += kb_step, it += alt ? 2 : 1) {
+          const bool masked = kb > plain_hi || kb < plain_lo;
+          uint32_t seen[4];  // bit e of word c: this thread's node sees key kb + 32c + e
+          bool dead = false;
+          if (masked) dead = block_masks(p, a, t, lo, kb, wq, lane, seen);
+          ok = __all_sync(0xffffffffu, wait_poll(bar(st.s_full[x]), cnt & 1, abort_flag));
+          if (!ok) break;
+          tc_fence_after();
+          uint32_t sv[2][32], pk[32];
           tmem_ld32(cS, sv[0]);
           tmem_ld32(cS + 32, sv[1]);
           tmem_ld_wait();
           if (masked) {
-            hide(sv[0], seen(0));
-            hide(sv[1], seen(1));
+            hide(sv[0], seen[0]);
+            hide(sv[1], seen[1]);
           }
-          l0 = chunk_weights(sv, p.scale_log2, m_ref, alpha, pk);
-        }
-        // the P buffer was last read by the tile's previous PV
-        if (cnt >= 1) {
-          ok = __all_sync(0xffffffffu, wait_poll(bar(st.o_ready[x]), (cnt - 1) & 1, abort_flag));
-          if (!ok) break;
-          tc_fence_after();
-        }
-        if (busy) {
+          float alpha = 1.f;
+          float l0 = chunk_weights(sv, p.scale_log2, m_ref, alpha, pk);
+          // the P buffer was last read by the tile's previous PV
+          if (cnt >= 1) {
+            ok = __all_sync(0xffffffffu, wait_poll(bar(st.o_ready[x]), (cnt - 1) & 1, abort_flag));
+            if (!ok) break;
+            tc_fence_after();
+          }
           tmem_st32(cP, pk);
           tmem_ld32(cS + 64, sv[0]);
           tmem_ld32(cS + 96, sv[1]);
           tmem_ld_wait();
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(st.s_free[x]));
-        if (busy) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(st.s_free[x]));
           if (masked) {
-            hide(sv[0], seen(2));
-            hide(sv[1], seen(3));
+            hide(sv[0], seen[2]);
+            hide(sv[1], seen[3]);
           }
           float a1 = 1.f;
-          l1 = chunk_weights(sv, p.scale_log2, m_ref, a1, pk);
+          const float l1 = chunk_weights(sv, p.scale_log2, m_ref, a1, pk);
           if (__any_sync(0xffffffffu, a1 != 1.f)) {  // the reference rose: rescale the first half's weights too
             tmem_st_wait();
             uint32_t pv[32];
@@ -660,34 +707,24 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           }
           tmem_st32(cP + 32, pk);
           l = l * alpha + (l0 + l1);
-        }
-        // V rows that no node sees may hold anything, and a zero weight does
-        // not cancel a NaN: they are cleared before the tile's PV reads them
-        if (__any_sync(0xffffffffu, dead)) {
-          const uint32_t s = it % kVStages;
-          ok = __all_sync(0xffffffffu, wait_poll(bar(st.v_full[s]), (it / kVStages) & 1, abort_flag));
+          ok = clear_dead(dead);
           if (!ok) break;
-          if (dead) {
+          if (b > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+            uint32_t ov[32];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) zero_smem16(sV + s * kBlockBytes + row * kRowBytes + c * 16);
+            for (int h = 0; h < 2; ++h) {
+              tmem_ld32(cO + 32 * h, ov);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
+              tmem_st32(cO + 32 * h, ov);
+            }
           }
-          fence_proxy_async();
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(st.p_full[x]));
         }
-        if (busy && b > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
-          uint32_t ov[32];
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            tmem_ld32(cO + 32 * h, ov);
-            tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
-            tmem_st32(cO + 32 * h, ov);
-          }
-        }
-        if (busy) tmem_st_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(st.p_full[x]));
       }
       if (!ok) break;
       kv_it += n;
@@ -706,14 +743,15 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 #pragma unroll
         for (int e = 0; e < 32; ++e) ov[0][e] = ov[1][e] = 0u;
       }
+      const int token = a.token, kvh = a.kvh, part_slot = a.slot;
+      bool writes = tok < a.n_tok;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(bar(st.o_free[x]));
         mbar_arrive(bar(st.part_empty[slot]));
       }
-      bool writes = valid;
-      if (a.alt) {  // tile B hands its state to tile A
+      if (alt) {  // tile B hands its state to tile A
         const uint32_t ph = n_xch & 1;
         if (x == 1) {
           if (n_xch >= 1) {
@@ -750,10 +788,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       if (writes) {
         float inv = l > 0.f ? 1.f / l : 0.f;
         float lse2 = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
-        const int h = a.kvh * g + head;
-        if (a.slot < 0) {
+        const int h = kvh * g + head;
+        if (part_slot < 0) {
           if (p.sinks != nullptr) inv = finish_with_sink(m_ref, l, tree_sink(p, h), &lse2);
-          const size_t orow = (size_t)(a.token + tok) * Hq + h;
+          const size_t orow = (size_t)(token + tok) * Hq + h;
           uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kHeadDim);
 #pragma unroll
           for (int v = 0; v < 8; ++v) {
@@ -766,7 +804,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           }
           p.lse[orow] = lse2 * 0.69314718055994531f;
         } else {
-          const size_t prow = (size_t)a.slot * kItemRows + (a.alt ? 0 : x * kTileRows) + row;
+          const size_t prow = (size_t)part_slot * kItemRows + (alt ? 0 : x * kTileRows) + row;
           float4* dst = reinterpret_cast<float4*>(p.o_part + prow * kHeadDim);
 #pragma unroll
           for (int v = 0; v < 16; ++v) {
