@@ -14,14 +14,14 @@
 // CTA derives the line from seq_lens and query_start_loc itself (a prefix sum
 // over the rows), so there is no planning launch.
 //
-// One CTA, 11 warps:
+// One CTA, 12 warps:
 //   warps 0-3  softmax of tile A, warps 4-7 of tile B: thread t owns row
 //              t & 127 (TMEM lane). Running max and sum in fp32, P to TMEM as
 //              bf16 (as the append kernel does, the rounding of each p_j is
 //              2^-8 relative at most), O rescaled only when the max rises by
 //              more than 2^8;
-//   warp 8     producer: finds the CTA's parts, loads query tiles and K / V
-//              blocks by TMA into two rings;
+//   warps 8, 11  producers: find the CTA's parts, load query tiles and K (8) and V
+//              (11) blocks by TMA into a ring each;
 //   warps 9, 10  MMA issuers of tile A and B: S = Q K^T (M 128, N 128, K 64),
 //              then O += P V (M 128, N 64, K 128, P from TMEM).
 // An item with more than 128 query rows runs as two tiles over the same K/V
@@ -46,8 +46,8 @@ constexpr int kBlockBytes = kBlockKeys * kRowBytes;  // one K or V block: 16 KiB
 constexpr int kKStages = 4, kVStages = 4;
 constexpr int kQBytes = kItemRows * kRowBytes;
 constexpr int kTileQBytes = kTileRows * kRowBytes;
-constexpr int kProducerWarp = 8, kIssueWarpA = 9;
-constexpr int kTreeThreads = 352;
+constexpr int kProducerWarpK = 8, kIssueWarpA = 9, kProducerWarpV = 11;
+constexpr int kTreeThreads = 384;
 constexpr uint32_t kTmemCols = 512;
 // cost of a part's set-up and end, of a block walked by both tiles, and of a
 // block that one of two alternating tiles walks
@@ -387,17 +387,24 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   tc_fence_after();
   const uint32_t tmem = st.tmem_base;
 
-  if (warp == kProducerWarp) {
-    // ------------------------------------------------------------- producer
+  if (warp == kProducerWarpK || warp == kProducerWarpV) {
+    // ------------------------------------------------------------ producers
+    // Both walk the CTA's parts; the K producer also hands them out and loads
+    // the query tiles. Two warps, because the issue of a block's 16 boxes by
+    // one took longer than their transfer.
+    const bool is_k = warp == kProducerWarpK;
     if (lane == 0) {
-      prefetch_tensormap(&kmap);
-      prefetch_tensormap(&vmap);
+      prefetch_tensormap(is_k ? &kmap : &vmap);
       prefetch_tensormap(&qmap);
       prefetch_tensormap(&qmap_alt);
     }
     // one pass over the cache, re-read only by the row's other tiles
     const uint64_t pol = policy_evict_last();
-    uint32_t kv_it = 0, k_issued = 0, v_issued = 0, q_issued = 0;
+    const uint32_t ring = is_k ? sK : sV, stages = is_k ? kKStages : kVStages;
+    const CUtensorMap* map = is_k ? &kmap : &vmap;
+    uint64_t* full = is_k ? st.k_full : st.v_full;
+    uint64_t* empty = is_k ? st.k_empty : st.v_empty;
+    uint32_t kv_it = 0, q_issued = 0;
     int row = 0;
     {
       int lo = 0, hi = B;  // prefix[lo] <= u0 < prefix[hi]
@@ -449,12 +456,14 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         }
         if (a.row >= 0) break;
       }
-      const int slot = i & 1;
-      if (i >= 2 && !__all_sync(0xffffffffu, wait_sleep(bar(st.part_empty[slot]), ((i >> 1) - 1) & 1, abort_flag)))
-        break;
-      if (lane == 0) {
-        st.parts[slot] = a;
-        mbar_arrive(bar(st.part_full[slot]));
+      if (is_k) {
+        const int slot = i & 1;
+        if (i >= 2 && !__all_sync(0xffffffffu, wait_sleep(bar(st.part_empty[slot]), ((i >> 1) - 1) & 1, abort_flag)))
+          break;
+        if (lane == 0) {
+          st.parts[slot] = a;
+          mbar_arrive(bar(st.part_full[slot]));
+        }
       }
       if (a.row < 0) break;
       const int* bt_row = p.block_table + (size_t)a.row * p.max_pages;
@@ -473,61 +482,44 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         return v;
       };
       int ids = load_ids(0), ids_next = load_ids(1);
-      if (i >= 1 && !__all_sync(0xffffffffu, wait_sleep(bar(st.q_empty), (i - 1) & 1, abort_flag))) break;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(bar(st.q_full), a.alt ? kTileQBytes : kQBytes);
-        tma_load_3d(sQ, a.alt ? &qmap_alt : &qmap, 0, a.kvh * g, a.token, bar(st.q_full));
+      if (is_k) {
+        if (i >= 1 && !__all_sync(0xffffffffu, wait_sleep(bar(st.q_empty), (i - 1) & 1, abort_flag))) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar(st.q_full), a.alt ? kTileQBytes : kQBytes);
+          tma_load_3d(sQ, a.alt ? &qmap_alt : &qmap, 0, a.kvh * g, a.token, bar(st.q_full));
+        }
+        q_issued = i + 1;
       }
-      q_issued = ++i;
+      ++i;
       bool ok = true;
-      int y_prev[kBlockPages];
-      auto load_block = [&](bool is_k, uint32_t it, const int (&y)[kBlockPages]) -> bool {
-        const int nst = is_k ? kKStages : kVStages;
-        const int s = it % nst;
-        uint64_t* full = is_k ? st.k_full : st.v_full;
-        uint64_t* empty = is_k ? st.k_empty : st.v_empty;
-        if (it >= (uint32_t)nst &&
-            !__all_sync(0xffffffffu, wait_sleep(bar(empty[s]), ((it / nst) - 1) & 1, abort_flag)))
-          return false;
-        const uint32_t dst = (is_k ? sK : sV) + s * kBlockBytes;
-        arrive_expect_tx_e(bar(full[s]), kBlockBytes);
-#pragma unroll
-        for (int j = 0; j < kBlockPages; ++j)
-          tma_load_2d_e(dst + j * kTileBytes, is_k ? &kmap : &vmap, y[j], bar(full[s]), pol);
-        (is_k ? k_issued : v_issued) = it + 1;
-        return true;
-      };
       const int n = a.b1 - a.b0;
       for (int b = 0; b < n; ++b, ++kv_it) {
         if (b > 0 && (b * kBlockPages) % 32 == 0) {
           ids = ids_next;
           ids_next = load_ids(b * kBlockPages / 32 + 1);
         }
-        int y[kBlockPages];
+        const uint32_t s = kv_it % stages;
+        if (kv_it >= stages) {
+          ok = __all_sync(0xffffffffu, wait_sleep(bar(empty[s]), (kv_it / stages - 1) & 1, abort_flag));
+          if (!ok) break;
+        }
+        arrive_expect_tx_e(bar(full[s]), kBlockBytes);
 #pragma unroll
         for (int j = 0; j < kBlockPages; ++j) {
           const int pid = __shfl_sync(0xffffffffu, ids, (b * kBlockPages) % 32 + j);
-          y[j] = pid < 0 ? p.oob_row : (pid * Hkv + a.kvh) * kPage;
+          const int y = pid < 0 ? p.oob_row : (pid * Hkv + a.kvh) * kPage;
+          tma_load_2d_e(ring + s * kBlockBytes + j * kTileBytes, map, y, bar(full[s]), pol);
         }
-        if (!load_block(true, kv_it, y) || (b > 0 && !load_block(false, kv_it - 1, y_prev))) {
-          ok = false;
-          break;
-        }
-#pragma unroll
-        for (int j = 0; j < kBlockPages; ++j) y_prev[j] = y[j];
       }
-      if (ok && !load_block(false, kv_it - 1, y_prev)) ok = false;
       if (!ok) break;
     }
-    // after an abort: wait (bounded) for the copies still in flight into the rings
+    // after an abort: wait (bounded) for the copies still in flight
     if (*abort_flag && lane == 0) {
-      for (uint32_t it = k_issued > (uint32_t)kKStages ? k_issued - kKStages : 0; it < k_issued; ++it)
-        mbar_wait(bar(st.k_full[it % kKStages]), (it / kKStages) & 1);
-      for (uint32_t it = v_issued > (uint32_t)kVStages ? v_issued - kVStages : 0; it < v_issued; ++it)
-        mbar_wait(bar(st.v_full[it % kVStages]), (it / kVStages) & 1);
+      for (uint32_t it = kv_it > stages ? kv_it - stages : 0; it < kv_it; ++it)
+        mbar_wait(bar(full[it % stages]), (it / stages) & 1);
       if (q_issued > 0) mbar_wait(bar(st.q_full), (q_issued - 1) & 1);
     }
-  } else if (warp >= kIssueWarpA) {
+  } else if (warp == kIssueWarpA || warp == kIssueWarpA + 1) {
     // ---------------------------------------------------------- MMA issuers
     constexpr uint32_t idS = idesc_bf16(kTileRows, kBlockKeys, false, false);
     constexpr uint32_t idO = idesc_bf16(kTileRows, kHeadDim, false, true);
