@@ -33,18 +33,19 @@ mcpu_status check_page_dims(const mcpu_dims* d) {
   return MCPU_OK;
 }
 
-// Workspace: the status word, the plan, the parts of split items. Returns its
-// size; with `p`, sets p's pointers into `ws`.
-size_t tree_layout(uint8_t* ws, int32_t num_seqs, TreeParams* p) {
-  const size_t plan = 256, lse = align_up(plan + sizeof(int64_t) * ((size_t)num_seqs + 2), 256);
-  const size_t o = align_up(lse + sizeof(float) * 2 * kTreeMaxCtas * 256, 256);
+// Workspace: the status word, the cut tiles, their parts. Returns its size;
+// with `p`, sets p's pointers into `ws`.
+size_t tree_layout(uint8_t* ws, TreeParams* p) {
+  constexpr size_t cuts = 256, lse = cuts + sizeof(int4) * 4 * kTreeMaxCtas;
+  constexpr size_t o = lse + sizeof(float) * kTreeSlots * kTreeTileRows;
+  static_assert(lse % 256 == 0 && o % 256 == 0, "alignment");
   if (p) {
     p->status = reinterpret_cast<int32_t*>(ws);
-    p->plan = reinterpret_cast<int64_t*>(ws + plan);
+    p->cuts = reinterpret_cast<int4*>(ws + cuts);
     p->lse_part = reinterpret_cast<float*>(ws + lse);
     p->o_part = reinterpret_cast<float*>(ws + o);
   }
-  return align_up(o + sizeof(float) * 2 * kTreeMaxCtas * 256 * kHeadDim, 256);
+  return o + sizeof(float) * kTreeSlots * kTreeTileRows * kHeadDim;
 }
 
 }  // namespace
@@ -105,7 +106,7 @@ mcpu_status mcpu_norm_rope_kv_append(const void* q, int64_t q_stride, const void
 
 size_t mcpu_tree_workspace_size(const mcpu_dims* dims) {
   if (check_dims(dims) != MCPU_OK) return 0;
-  return tree_layout(nullptr, dims->num_seqs, nullptr);
+  return tree_layout(nullptr, nullptr);
 }
 
 mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, const void* v_cache,
@@ -134,13 +135,12 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
   if (st != MCPU_OK) return st;
   const int group = dims->num_q_heads / dims->num_kv_heads;
   const int64_t rows = (int64_t)dims->num_pages * dims->num_kv_heads * kPage;
-  CUtensorMap kmap, vmap, qmap, qmap_alt;
+  CUtensorMap kmap, vmap, qmap;
   if (!encode_pool(&kmap, k_cache, rows) || !encode_pool(&vmap, v_cache, rows) ||
-      !encode_query(&qmap, q, dims->total_q, dims->num_q_heads, group, 256) ||
-      !encode_query(&qmap_alt, q, dims->total_q, dims->num_q_heads, group, 128))
+      !encode_query(&qmap, q, dims->total_q, dims->num_q_heads, group, 128))
     return MCPU_ERR_INVALID_ARG;
   TreeParams p;
-  tree_layout(static_cast<uint8_t*>(workspace), dims->num_seqs, &p);
+  tree_layout(static_cast<uint8_t*>(workspace), &p);
   p.block_table = block_table;
   p.seq_lens = seq_lens;
   p.qsl = query_start_loc;
@@ -160,7 +160,7 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
   p.group = group;
   p.oob_row = (int32_t)rows;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
-  return from_cuda(launch_tree(kmap, vmap, qmap, qmap_alt, p, sms, reinterpret_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_tree(kmap, vmap, qmap, p, sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 mcpu_status mcpu_compact_kv(void* const* pools, int32_t num_pools, const int32_t* block_table,

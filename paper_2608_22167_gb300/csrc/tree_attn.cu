@@ -5,29 +5,29 @@
 // where V(t) holds the row's context keys (inside the window of t's position)
 // and the nodes whose bit is set in t's mask.
 //
-// Work: an item is one (row, kv head, tile of 256 query rows = 256 / g nodes x
-// the g heads); it walks the row's keys in blocks of 128 (8 pages). The blocks
-// of all items, weighted by what a block costs, form one line that is cut into
-// equal pieces, one per CTA (one CTA per SM): whatever the lengths, every SM
-// gets the same share, and an item that crosses a cut is computed in parts
-// that merge_tree_kernel joins by log-sum-exp in the order of the CTAs. Every
-// CTA derives the line from seq_lens and query_start_loc itself (a prefix sum
-// over the rows), so there is no planning launch.
+// Work: a tile is 128 query rows of one (row, kv head): 128 / g nodes x the g
+// heads; it walks the row's keys in blocks of 128 (8 pages). One CTA per SM
+// runs two lanes, each a complete pipeline for one tile at a time (softmax,
+// MMA issue, TMA, rings and barriers of its own), so that one lane's latencies
+// are the other's work. The tiles are laid on two lines, each block weighing
+// one and each tile kCostItem more:
+//   solo   a row's last tile when their number is odd (all of a tree of up to
+//          16 nodes at g = 8); cut into equal pieces, one per lane;
+//   joint  the other tiles, in pairs that read the same keys; cut into equal
+//          pieces, one per CTA, whose two lanes walk the pair side by side,
+//          so that the second read of a K/V block finds it in L2.
+// Whatever the lengths, every lane gets the same share. A tile that crosses a
+// cut is computed in parts that merge_tree_kernel joins by log-sum-exp in the
+// order of the pieces. Every CTA derives the lines from seq_lens and
+// query_start_loc itself (prefix sums over the rows): no planning launch.
 //
-// One CTA, 12 warps:
-//   warps 0-3  softmax of tile A, warps 4-7 of tile B: thread t owns row
-//              t & 127 (TMEM lane). Running max and sum in fp32, P to TMEM as
-//              bf16 (as the append kernel does, the rounding of each p_j is
-//              2^-8 relative at most), O rescaled only when the max rises by
-//              more than 2^8;
-//   warps 8, 11  producers: find the CTA's parts, load query tiles and K (8) and V
-//              (11) blocks by TMA into a ring each;
-//   warps 9, 10  MMA issuers of tile A and B: S = Q K^T (M 128, N 128, K 64),
-//              then O += P V (M 128, N 64, K 128, P from TMEM).
-// An item with more than 128 query rows runs as two tiles over the same K/V
-// blocks. One with at most 128 rows (up to 16 nodes at g = 8) would leave
-// tile B idle, so the two tiles then hold the same rows and take alternate key
-// blocks; their two states are joined in shared memory at the end.
+// Warps: 0-3 / 4-7 softmax of lane 0 / 1 (thread t owns row t & 127, a TMEM
+// lane: running max and sum in fp32, P to TMEM as bf16 - each weight rounded
+// once, 2^-8 relative - and O rescaled only when the max rises by more than
+// 2^8); 8, 9 MMA issue (S = Q K^T: M 128, N 128, K 64; O += P V: M 128, N 64,
+// K 128, P from TMEM); 10, 11 producers (the lane's parts, what the softmax
+// needs of their masks, Q tiles and K / V blocks by TMA, one 2 KiB box per
+// page). TMEM: per lane S 128, O 64, P 64 columns.
 //
 // Waits are bounded (common.cuh); one that runs out raises an abort flag that
 // ends every role, and TMEM is freed after the issuers' MMAs have drained.
@@ -38,63 +38,63 @@ namespace mcpu {
 
 namespace {
 
-constexpr int kTileRows = 128;  // query rows of one tile (TMEM lanes)
-constexpr int kItemRows = 256;
+constexpr int kTileRows = kTreeTileRows;  // query rows of one tile (TMEM lanes)
 constexpr int kBlockKeys = 128;
 constexpr int kBlockPages = kBlockKeys / kPage;
 constexpr int kBlockBytes = kBlockKeys * kRowBytes;  // one K or V block: 16 KiB
-constexpr int kKStages = 4, kVStages = 4;
-constexpr int kQBytes = kItemRows * kRowBytes;
-constexpr int kTileQBytes = kTileRows * kRowBytes;
-constexpr int kProducerWarpK = 8, kIssueWarpA = 9, kProducerWarpV = 11;
+constexpr int kKStages = 3, kVStages = 2;            // per lane
+constexpr int kQBytes = kTileRows * kRowBytes;
+constexpr int kLaneBytes = kQBytes + (kKStages + kVStages) * kBlockBytes;
 constexpr int kTreeThreads = 384;
 constexpr uint32_t kTmemCols = 512;
-// cost of a part's set-up and end, of a block walked by both tiles, and of a
-// block that one of two alternating tiles walks
-constexpr int kCostItem = 2, kCostPair = 2, kCostAlt = 1;
-constexpr int kMinQuota = 4;  // smallest piece of the line worth a CTA of its own
+constexpr int kCostItem = 3;  // a tile's set-up and end, in blocks
+constexpr int kMinQuota = 5;  // smallest piece worth a lane of its own
 constexpr float kRescale = 8.f;  // log2 units: P may reach 2^8 before O is rescaled
-constexpr int kStateRows = kHeadDim + 2;  // O, m and l of a row in the exchange buffer
-constexpr int kXchBytes = kStateRows * kTileRows * 4;
 
-// TMEM columns of tile x
-__device__ __forceinline__ uint32_t col_s(int x) { return x ? 128u : 0u; }
-__device__ __forceinline__ uint32_t col_o(int x) { return x ? 320u : 256u; }
-__device__ __forceinline__ uint32_t col_p(int x) { return x ? 448u : 384u; }
-
-struct Part {  // a run of key blocks of one item
-  int32_t row;  // -1: no more parts
+struct Part {  // a run of key blocks of one tile
+  int32_t row;                 // -1: no more parts
   int32_t token, n_tok, node;  // first query token, tokens, first node of the tile
   int32_t ctx, len, kvh;
   int32_t kb0, key_begin;  // key of block 0 (a page start), first key any node can see
   int32_t b0, b1;
-  int32_t slot;  // partial slot, or -1: the part is the whole item
-  int32_t alt;
+  int32_t slot;  // partial slot, or -1: the part is the whole tile
+};
+
+struct Meta {  // what the softmax needs to know of a part's nodes
+  uint32_t seen_by_any[MCPU_MAX_TREE_WORDS];  // nodes that some node of the row sees
+  float sinks[kMaxGroup];                     // base-2 sink logits of the kv head's query heads
+  int32_t lo[kTileRows];                      // first context key in each node's window
+  uint32_t mask[kTileRows * MCPU_MAX_TREE_WORDS];  // [node of the tile][words]
+};
+
+struct Lane {
+  uint64_t q_full, q_empty;
+  uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
+  uint64_t s_full, s_free, p_full, o_ready, o_free;
+  uint64_t part_full[2], part_empty[2], meta_full[2];
+  uint64_t drain;
+  Part parts[2];
+  Meta meta[2];
 };
 
 struct TreeSmem {
-  uint64_t q_full, q_empty;
-  uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
-  uint64_t s_full[2], s_free[2], p_full[2], o_ready[2], o_free[2];
-  uint64_t part_full[2], part_empty[2];
-  uint64_t xch_full, xch_empty;
-  uint64_t drain[2];
-  Part parts[2];
-  int64_t scan[kTreeThreads / 32];
+  Lane lane[2];
+  int64_t scan[2][kTreeThreads / 32];
+  int64_t first_off[3];  // where a piece begins in its first row: solo of lane 0, of lane 1, joint
+  int32_t first_row[3];
   uint32_t tmem_base;
   int32_t abort_flag;
 };
 
-size_t tree_smem_bytes() {
-  return 1024 + kQBytes + (size_t)(kKStages + kVStages) * kBlockBytes + kXchBytes + sizeof(TreeSmem) +
-         sizeof(int64_t) * (kMaxSeqs + 1);
-}
+static_assert(2 * kLaneBytes >= 2 * (kMaxSeqs + 1) * (int)sizeof(int64_t), "the prefix sums use the rings first");
 
-// ------------------------------------------------------------ the work line
+size_t tree_smem_bytes() { return 1024 + 2 * (size_t)kLaneBytes + sizeof(TreeSmem); }
+
+// ----------------------------------------------------------- the work lines
 struct RowGeom {
-  int q0, L, S, C, key_begin, kb0, nb, tiles;
-  int64_t pair_cost, last_cost;  // of the row's full tiles and of its last one
-  __device__ int64_t head_cost() const { return (tiles - 1) * pair_cost + last_cost; }
+  int q0, L, S, C, key_begin, kb0, nb;
+  int pairs, solo;  // joint pairs of tiles, and 1 if a last tile stands alone
+  __device__ int64_t cost() const { return kCostItem + nb; }  // of one tile
 };
 
 // Geometry of row r; false (L = 0: nothing wrong) if it has no work, with the
@@ -117,29 +117,38 @@ __device__ __forceinline__ bool row_geom(const TreeParams& p, int r, RowGeom* w,
   w->key_begin = p.window > 0 ? max(0, w->C - p.window + 1) : 0;
   w->kb0 = w->key_begin / kPage * kPage;
   w->nb = (w->S - w->kb0 + kBlockKeys - 1) / kBlockKeys;
-  const int rows = w->L * p.group;
-  w->tiles = (rows + kItemRows - 1) / kItemRows;
-  const int last = rows - (w->tiles - 1) * kItemRows;
-  w->pair_cost = kCostItem + (int64_t)w->nb * kCostPair;
-  w->last_cost = last <= kTileRows ? kCostItem + (int64_t)w->nb * kCostAlt : w->pair_cost;
+  const int tiles = (w->L * p.group + kTileRows - 1) / kTileRows;
+  w->pairs = tiles >> 1;
+  w->solo = tiles & 1;
   return true;
 }
 
-// Blocks of an item of `nb` blocks that lie before `x` units of it.
-__device__ __forceinline__ int blocks_before(int64_t x, int nb, int64_t cost) {
-  if (x <= kCostItem) return 0;
-  if (x >= cost) return nb;
-  // cost = kCostItem + nb * weight, weight 1 or 2
-  const int64_t weight = cost - kCostItem == nb ? 1 : kCostPair;
-  const int64_t b = (x - kCostItem + weight - 1) / weight;
-  return b < nb ? (int)b : nb;
+// Blocks of a tile of nb blocks that lie before x units of it.
+__device__ __forceinline__ int blocks_before(int64_t x, int nb) {
+  return x <= kCostItem ? 0 : x >= kCostItem + nb ? nb : (int)(x - kCostItem);
+}
+
+// 64-bit division in one place (its code is long).
+__device__ __noinline__ int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Whether a part names rows of this call: what is read from shared memory
+// becomes addresses, so every role checks it before it uses it.
+__device__ __forceinline__ bool part_ok(const TreeParams& p, const Part& a) {
+  return a.row < p.num_seqs && a.token >= 0 && a.n_tok >= 1 && a.n_tok * p.group <= kTileRows &&
+         a.token <= p.total_q - a.n_tok && a.kvh >= 0 && a.kvh < p.num_kv_heads && a.b0 >= 0 && a.b1 > a.b0 &&
+         a.slot >= -1 && a.slot < kTreeSlots && a.ctx >= 0 && a.len <= p.max_pages * kPage && a.node >= 0 &&
+         a.node + a.n_tok <= a.len - a.ctx && a.len - a.ctx <= 32 * p.words;
 }
 
 // ------------------------------------------------------------------- waits
-__device__ __forceinline__ bool wait_sleep(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
-  if (mbar_try_wait(bar, parity)) return true;
+// Bounded waits that also end when another role has aborted. Only the first
+// test is inlined: the loop that follows it is in one place, since the code of
+// this kernel is about as large as the instruction cache. The softmax warps
+// poll; the other roles, which wait most of the time, sleep in the test.
+template <bool kSleep>
+__device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
   const uint64_t t0 = global_timer_ns();
-  while (!mbar_try_wait_sleep(bar, parity, 10000)) {
+  while (!(kSleep ? mbar_try_wait_sleep(bar, parity, 10000) : mbar_try_wait(bar, parity))) {
     if (*abort_flag) return false;
     if (global_timer_ns() - t0 > kWaitTimeoutNs) {
       *abort_flag = 1;
@@ -148,17 +157,11 @@ __device__ __forceinline__ bool wait_sleep(uint32_t bar, uint32_t parity, volati
   }
   return true;
 }
+__device__ __forceinline__ bool wait_sleep(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
+  return mbar_try_wait(bar, parity) || wait_more<true>(bar, parity, abort_flag);
+}
 __device__ __forceinline__ bool wait_poll(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = global_timer_ns();
-  while (!mbar_try_wait(bar, parity)) {
-    if (*abort_flag) return false;
-    if (global_timer_ns() - t0 > kWaitTimeoutNs) {
-      *abort_flag = 1;
-      return false;
-    }
-  }
-  return true;
+  return mbar_try_wait(bar, parity) || wait_more<false>(bar, parity, abort_flag);
 }
 
 // A 2-D box load issued by one elected lane of a warp that runs in step: its
@@ -187,6 +190,7 @@ __device__ __forceinline__ void arrive_expect_tx_e(uint32_t bar, uint32_t bytes)
 __device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
 __device__ __forceinline__ void hide(uint32_t (&sv)[32], uint32_t seen) {
+  if (!__any_sync(0xffffffffu, seen != 0xffffffffu)) return;  // most words of a masked block are plain context
 #pragma unroll
   for (int e = 0; e < 32; ++e)
     if (!(seen >> e & 1u)) sv[e] = 0xff800000u;
@@ -229,21 +233,20 @@ __device__ __forceinline__ float weights(const uint32_t (&sv)[2][32], float scal
 // weights.
 __device__ __forceinline__ float chunk_weights(const uint32_t (&sv)[2][32], float scale_log2, float& m_ref,
                                                float& alpha, uint32_t (&pk)[32]) {
-  float sum = 0.f;
-  bool redo = m_ref == -INFINITY;
-  if (!redo) {
-    sum = weights(sv, scale_log2, -m_ref, pk);
-    redo = !(sum < 256.f);
-  }
-  if (redo) {
-    const float mx = scores_max(sv) * scale_log2;
-    if (mx > m_ref + kRescale) {
-      alpha *= ex2_approx(m_ref - mx);  // 0 before the first reference
-      m_ref = mx;
+  bool take_max = m_ref == -INFINITY, last = false;
+  for (;;) {  // at most twice
+    if (take_max) {
+      const float mx = scores_max(sv) * scale_log2;
+      if (mx > m_ref + kRescale) {
+        alpha *= ex2_approx(m_ref - mx);  // 0 before the first reference
+        m_ref = mx;
+      }
+      last = true;
     }
-    sum = weights(sv, scale_log2, m_ref == -INFINITY ? 0.f : -m_ref, pk);
+    const float sum = weights(sv, scale_log2, m_ref == -INFINITY ? 0.f : -m_ref, pk);
+    if (last || sum < 256.f) return sum;
+    take_max = true;
   }
-  return sum;
 }
 
 __device__ __forceinline__ void zero_smem16(uint32_t addr) {
@@ -251,27 +254,21 @@ __device__ __forceinline__ void zero_smem16(uint32_t addr) {
 }
 
 // What the masks say about the block of keys at kb: seen[c], the keys kb + 32c ..
-// that the thread's node (token t, window from key lo) sees; returns whether
-// the slot kb + 32 wq + lane holds a V row that no node of the row sees.
-__device__ __forceinline__ bool block_masks(const TreeParams& p, const Part& a, int t, int lo, int kb, int wq, int lane,
-                                            uint32_t (&seen)[4]) {
+// that the thread's node (of the tile) sees; returns whether the slot
+// kb + 32 wq + lane holds a V row that no node of the row sees.
+__device__ __forceinline__ bool block_masks(const TreeParams& p, const Part& a, const Meta& m, int node, int kb, int wq,
+                                            int lane, uint32_t (&seen)[4]) {
   const int ctx = a.ctx, len = a.len, j = kb + 32 * wq + lane;
-  uint32_t mw[5] = {0, 0, 0, 0, 0};
   const int n0 = kb - ctx, w0 = n0 >> 5;  // node of the block's first key, and its mask word
+  const int lo = p.window > 0 ? m.lo[node] : 0;
+  uint32_t mw[5] = {0, 0, 0, 0, 0};
   bool dead = j < a.key_begin;
   if (n0 > -kBlockKeys) {
+    auto word = [&](const uint32_t* w, int i) { return i >= 0 && i < p.words ? w[i] : 0u; };
 #pragma unroll
-    for (int c = 0; c < 5; ++c)
-      if (w0 + c >= 0 && w0 + c < p.words) mw[c] = __ldg(p.mask + (size_t)t * p.words + w0 + c);
-    uint32_t u0 = 0, u1 = 0;  // union over the row's nodes of the two words with this warp's slots
-    for (int k = lane; k < len - ctx; k += 32) {
-      const uint32_t* m = p.mask + (size_t)(a.token - a.node + k) * p.words;
-      if (w0 + wq >= 0 && w0 + wq < p.words) u0 |= __ldg(m + w0 + wq);
-      if (w0 + wq + 1 >= 0 && w0 + wq + 1 < p.words) u1 |= __ldg(m + w0 + wq + 1);
-    }
-    u0 = __reduce_or_sync(0xffffffffu, u0);
-    u1 = __reduce_or_sync(0xffffffffu, u1);
-    const uint32_t any = __funnelshift_r(u0, u1, n0 & 31);
+    for (int c = 0; c < 5; ++c) mw[c] = word(m.mask + node * p.words, w0 + c);
+    const uint32_t any =
+        __funnelshift_r(word(m.seen_by_any, w0 + wq), word(m.seen_by_any, w0 + wq + 1), n0 & 31);
     // past the row's end only its last page holds anything: later pages arrive as zeros
     dead |= j >= len ? j < ((len + kPage - 1) & ~(kPage - 1)) : j >= ctx && !(any >> lane & 1u);
   }
@@ -284,6 +281,16 @@ __device__ __forceinline__ bool block_masks(const TreeParams& p, const Part& a, 
   return dead;
 }
 
+// 16 columns of TMEM, for the short loops that end a part
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr));
+}
+
 __device__ __forceinline__ float tree_sink(const TreeParams& p, int h) {
   return p.sinks ? p.sinks[h] * 1.4426950408889634f : -INFINITY;
 }
@@ -291,335 +298,399 @@ __device__ __forceinline__ float tree_sink(const TreeParams& p, int h) {
 // --------------------------------------------------------------- the kernel
 __global__ void __launch_bounds__(kTreeThreads, 1)
     tree_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
-                const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap qmap_alt,
-                const TreeParams p) {
+                const __grid_constant__ CUtensorMap qmap, const TreeParams p) {
   extern __shared__ uint8_t smem_raw[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t raw = smem_addr(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
-  const uint32_t sQ = base, sK = sQ + kQBytes, sV = sK + kKStages * kBlockBytes;
-  uint8_t* after = smem_raw + (base - raw) + kQBytes + (kKStages + kVStages) * kBlockBytes;
-  float* xch = reinterpret_cast<float*>(after);  // [kStateRows][kTileRows]
-  TreeSmem& st = *reinterpret_cast<TreeSmem*>(after + kXchBytes);
-  int64_t* prefix = reinterpret_cast<int64_t*>(after + kXchBytes + sizeof(TreeSmem));
+  uint8_t* base_ptr = smem_raw + (base - raw);
+  TreeSmem& st = *reinterpret_cast<TreeSmem*>(base_ptr + 2 * kLaneBytes);
+  int64_t* prefix = reinterpret_cast<int64_t*>(base_ptr);  // [2][B + 1], until the parts begin
   volatile int32_t* abort_flag = &st.abort_flag;
   auto bar = [&](uint64_t& b) { return smem_addr(&b); };
   const int B = p.num_seqs, g = p.group, Hkv = p.num_kv_heads, Hq = p.num_q_heads;
 
+  // no cut tile begins in this CTA's pieces, as far as is known
+  if (threadIdx.x < 4)
+    p.cuts[(threadIdx.x >> 1) * 2 * gridDim.x + 2 * blockIdx.x + (threadIdx.x & 1)] = make_int4(-1, 0, 0, 0);
   if (p.qsl[0] != 0 || p.qsl[B] != p.total_q) {
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-      atomicOr(p.status, kStatusBadLengths);
-      p.plan[0] = 0;
-    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, kStatusBadLengths);
     return;
   }
-  // ---- the work line: prefix[r] = cost of the rows before r
+  // ---- the lines: prefix[l][r] = cost of line l's tiles in the rows before r
   {
     const int per = (B + kTreeThreads - 1) / kTreeThreads;
     const int r0 = min(B, (int)threadIdx.x * per), r1 = min(B, r0 + per);
-    int64_t mine = 0;
+    int64_t sum[2] = {0, 0};
     int32_t bits = 0;
     RowGeom w;
     for (int r = r0; r < r1; ++r)
-      if (row_geom(p, r, &w, &bits)) mine += w.head_cost() * Hkv;
+      if (row_geom(p, r, &w, &bits)) {
+        sum[0] += w.cost() * Hkv * w.solo;
+        sum[1] += w.cost() * Hkv * w.pairs;
+      }
     if (bits && blockIdx.x == 0) atomicOr(p.status, bits);
-    int64_t incl = mine;
+    int64_t at[2];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t v = __shfl_up_sync(0xffffffffu, (long long)incl, o);
-      if (lane >= o) incl += v;
+    for (int l = 0; l < 2; ++l) {
+      int64_t incl = sum[l];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, (long long)incl, o);
+        if (lane >= o) incl += v;
+      }
+      if (lane == 31) st.scan[l][warp] = incl;
+      at[l] = incl - sum[l];
     }
-    if (lane == 31) st.scan[warp] = incl;
     __syncthreads();
-    int64_t at = incl - mine;
-    for (int i = 0; i < warp; ++i) at += st.scan[i];
-    for (int r = r0; r < r1; ++r) {
-      prefix[r] = at;
-      if (row_geom(p, r, &w, &bits)) at += w.head_cost() * Hkv;
+    for (int i = 0; i < warp; ++i) {
+      at[0] += st.scan[0][i];
+      at[1] += st.scan[1][i];
     }
-    if ((int)threadIdx.x == kTreeThreads - 1) {
-      prefix[B] = at;
-      if (B == 0) prefix[0] = 0;
+    for (int r = r0; r < r1; ++r) {
+      prefix[r] = at[0];
+      prefix[B + 1 + r] = at[1];
+      if (row_geom(p, r, &w, &bits)) {
+        at[0] += w.cost() * Hkv * w.solo;
+        at[1] += w.cost() * Hkv * w.pairs;
+      }
+    }
+    if (threadIdx.x == kTreeThreads - 1) {
+      prefix[B] = at[0];
+      prefix[2 * B + 1] = at[1];
     }
   }
-  if (threadIdx.x == 0) {
-    mbar_init(bar(st.q_full), 1);
-    mbar_init(bar(st.q_empty), 2);
+  if (threadIdx.x < 2) {
+    Lane& ln = st.lane[threadIdx.x];
+    mbar_init(bar(ln.q_full), 1);
+    mbar_init(bar(ln.q_empty), 1);
     for (int s = 0; s < kKStages; ++s) {
-      mbar_init(bar(st.k_full[s]), 1);
-      mbar_init(bar(st.k_empty[s]), 2);
+      mbar_init(bar(ln.k_full[s]), 1);
+      mbar_init(bar(ln.k_empty[s]), 1);
     }
     for (int s = 0; s < kVStages; ++s) {
-      mbar_init(bar(st.v_full[s]), 1);
-      mbar_init(bar(st.v_empty[s]), 2);
+      mbar_init(bar(ln.v_full[s]), 1);
+      mbar_init(bar(ln.v_empty[s]), 1);
     }
-    for (int x = 0; x < 2; ++x) {
-      mbar_init(bar(st.s_full[x]), 1);
-      mbar_init(bar(st.s_free[x]), 4);
-      mbar_init(bar(st.p_full[x]), 4);
-      mbar_init(bar(st.o_ready[x]), 1);
-      mbar_init(bar(st.o_free[x]), 4);
-      mbar_init(bar(st.part_full[x]), 1);
-      mbar_init(bar(st.part_empty[x]), 8 + 2);
-      mbar_init(bar(st.drain[x]), 1);
+    mbar_init(bar(ln.s_full), 1);
+    mbar_init(bar(ln.s_free), 4);
+    mbar_init(bar(ln.p_full), 4);
+    mbar_init(bar(ln.o_ready), 1);
+    mbar_init(bar(ln.o_free), 4);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(bar(ln.part_full[i]), 1);
+      mbar_init(bar(ln.part_empty[i]), 4 + 1);
+      mbar_init(bar(ln.meta_full[i]), 1);
     }
-    mbar_init(bar(st.xch_full), 4);
-    mbar_init(bar(st.xch_empty), 4);
+    mbar_init(bar(ln.drain), 1);
     st.abort_flag = 0;
     fence_barrier_init();
   }
   __syncthreads();
-  const int64_t total = prefix[B];
-  const int64_t even = (total + gridDim.x - 1) / gridDim.x;
-  const int64_t quota = even > kMinQuota ? even : kMinQuota;
-  if (blockIdx.x == 0) {  // for the merge
-    for (int r = threadIdx.x; r <= B; r += kTreeThreads) p.plan[1 + r] = prefix[r];
-    if (threadIdx.x == 0) p.plan[0] = total > 0 ? quota : 0;
+  // pieces: solo of this CTA's lanes, then joint
+  const int64_t total0 = prefix[B], total1 = prefix[2 * B + 1];
+  const int64_t quota0 = max(div_up(total0, 2 * gridDim.x), (int64_t)kMinQuota);
+  const int64_t quota1 = max(div_up(total1, gridDim.x), (int64_t)kMinQuota);
+  const int64_t begin0 = 2 * (int64_t)blockIdx.x * quota0, begin1 = (int64_t)blockIdx.x * quota1;
+  if (begin0 >= total0 && begin1 >= total1) return;  // uniform over the CTA
+  if (warp < 3) {  // the row each piece begins in: warp 0, 1 solo of their lane, 2 joint
+    const int l = warp == 2;
+    const int64_t u = l ? begin1 : begin0 + warp * quota0;
+    const int64_t* pre = prefix + l * (B + 1);
+    int r0 = 0;
+    for (int r = 1 + lane; r < B; r += 32) r0 += pre[r] <= u;  // pre[r0] <= u < pre[r0 + 1] if u is on the line
+    r0 = __reduce_add_sync(0xffffffffu, r0);
+    if (lane == 0) {
+      st.first_row[warp] = r0;
+      st.first_off[warp] = u - pre[r0];
+    }
   }
-  const int64_t u0 = (int64_t)blockIdx.x * quota, u1 = min(u0 + quota, total);
-  if (u0 >= u1) return;  // uniform over the CTA
-  if (warp == kIssueWarpA) {
+  if (warp == 8) {
     tmem_alloc(smem_addr(&st.tmem_base), kTmemCols);
     tmem_relinquish();
   }
+  fence_proxy_async();  // the rings' first TMA writes come after the reads of the prefix sums
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = st.tmem_base;
 
-  if (warp == kProducerWarpK || warp == kProducerWarpV) {
-    // ------------------------------------------------------------ producers
-    // Both walk the CTA's parts; the K producer also hands them out and loads
-    // the query tiles. Two warps, because the issue of a block's 16 boxes by
-    // one took longer than their transfer.
-    const bool is_k = warp == kProducerWarpK;
+  const int x = warp < 8 ? warp >> 2 : warp & 1;  // this warp's lane of the CTA
+  Lane& ln = st.lane[x];
+  const uint32_t sQ = base + x * kLaneBytes, sK = sQ + kQBytes, sV = sK + kKStages * kBlockBytes;
+  const uint32_t tmem = st.tmem_base + x * 256;  // S at 0, O at 128, P at 192
+  constexpr uint32_t kColO = 128, kColP = 192;
+
+  if (warp >= 10) {
+    // ------------------------------------------------------------- producer
     if (lane == 0) {
-      prefetch_tensormap(is_k ? &kmap : &vmap);
+      prefetch_tensormap(&kmap);
+      prefetch_tensormap(&vmap);
       prefetch_tensormap(&qmap);
-      prefetch_tensormap(&qmap_alt);
     }
-    // one pass over the cache, re-read only by the row's other tiles
-    const uint64_t pol = policy_evict_last();
-    const uint32_t ring = is_k ? sK : sV, stages = is_k ? kKStages : kVStages;
-    const CUtensorMap* map = is_k ? &kmap : &vmap;
-    uint64_t* full = is_k ? st.k_full : st.v_full;
-    uint64_t* empty = is_k ? st.k_empty : st.v_empty;
-    uint32_t kv_it = 0, q_issued = 0;
-    int row = 0;
-    {
-      int lo = 0, hi = B;  // prefix[lo] <= u0 < prefix[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (prefix[mid] <= u0) lo = mid; else hi = mid;
-      }
-      row = lo;
-    }
-    RowGeom w;
-    int32_t ignored = 0;
-    row_geom(p, row, &w, &ignored);
-    int64_t off = u0 - prefix[row];
-    int kvh = (int)(off / w.head_cost());
-    off -= kvh * w.head_cost();
-    int tile = (int)min(off / w.pair_cost, (int64_t)(w.tiles - 1));
-    int64_t u = u0 - (off - tile * w.pair_cost);  // start of the current item on the line
-    for (int i = 0;;) {
-      // the next part with blocks in [u0, u1)
-      Part a;
-      a.row = -1;
+    uint32_t k_it = 0, v_it = 0;
+    int i = 0;
+    bool ok = true;
+#pragma unroll 1
+    for (int line = 0; line < 2 && ok; ++line) {
+      const int64_t quota = line ? quota1 : quota0;
+      const int64_t u0 = line ? begin1 : begin0 + x * quota0, u1 = min(u0 + quota, line ? total1 : total0);
+      if (u0 >= u1) continue;
+      const int which = line ? 2 : x;
+      int row = st.first_row[which];
+      RowGeom w;
+      int32_t ignored = 0;
+      row_geom(p, row, &w, &ignored);
+      int64_t off = st.first_off[which];
+      int item = 0;  // (kv head, pair) of the row
+      for (; off >= w.cost(); off -= w.cost()) ++item;
+      int64_t u = u0 - off;  // start of the current tile on the line
+      // K/V of joint tiles is read by both lanes, of solo ones once
+      const uint64_t pol = line ? policy_evict_last() : policy_evict_first();
       while (u < u1) {
-        const int64_t cost = tile < w.tiles - 1 ? w.pair_cost : w.last_cost;
-        a.b0 = blocks_before(u0 - u, w.nb, cost);
-        a.b1 = blocks_before(u1 - u, w.nb, cost);
-        if (a.b0 < a.b1) {
-          const int tile_tok = kItemRows / g;
-          a.row = row;
-          a.node = tile * tile_tok;
-          a.token = w.q0 + a.node;
-          a.n_tok = min(tile_tok, w.L - a.node);
-          a.ctx = w.C;
-          a.len = w.S;
-          a.kvh = kvh;
-          a.kb0 = w.kb0;
-          a.key_begin = w.key_begin;
-          a.slot = a.b0 == 0 && a.b1 == w.nb ? -1 : 2 * (int)blockIdx.x + (a.b0 == 0 ? 1 : 0);
-          a.alt = a.n_tok * g <= kTileRows;
+        const int per_head = line ? w.pairs : 1, tile_tok = kTileRows / g;
+        Part a;
+        a.b0 = blocks_before(u0 - u, w.nb);
+        a.b1 = blocks_before(u1 - u, w.nb);
+        a.row = row;
+        a.kvh = item / per_head;
+        const int tile = line ? 2 * (item % per_head) + x : 2 * w.pairs;
+        a.node = tile * tile_tok;
+        a.token = w.q0 + a.node;
+        a.n_tok = min(tile_tok, w.L - a.node);
+        a.ctx = w.C;
+        a.len = w.S;
+        a.kb0 = w.kb0;
+        a.key_begin = w.key_begin;
+        const int first = a.b0 == 0 ? 1 : 0;
+        a.slot = first && a.b1 == w.nb ? -1
+                 : line                ? kTreeSoloSlots + (2 * (int)blockIdx.x + first) * 2 + x
+                                       : 2 * (2 * (int)blockIdx.x + x) + first;
+        if (first && a.slot >= 0 && a.b1 > 0 && lane == 0) {
+          // a cut tile whose first part is this one: its last piece and what the merge needs
+          const int last = (int)div_up(u + w.cost(), quota) - 1;
+          p.cuts[line * 2 * gridDim.x + 2 * blockIdx.x + x] = make_int4(last, a.token, a.n_tok, a.kvh);
         }
-        u += cost;
-        if (++tile == w.tiles) {
-          tile = 0;
-          if (++kvh == Hkv) {
-            kvh = 0;
-            do ++row;
-            while (row < B && prefix[row + 1] == prefix[row]);
-            if (row < B) row_geom(p, row, &w, &ignored);
-          }
+        u += w.cost();
+        if (++item == Hkv * per_head) {
+          item = 0;
+          do ++row;
+          while (row < B && !(row_geom(p, row, &w, &ignored) && (line ? w.pairs : w.solo) > 0));
         }
-        if (a.row >= 0) break;
-      }
-      if (is_k) {
+        if (a.b0 >= a.b1) continue;
         const int slot = i & 1;
-        if (i >= 2 && !__all_sync(0xffffffffu, wait_sleep(bar(st.part_empty[slot]), ((i >> 1) - 1) & 1, abort_flag)))
+        if (!part_ok(p, a)) {
+          atomicOr(p.status, kStatusPlanOverflow);
+          *abort_flag = 2;
+          ok = false;
           break;
-        if (lane == 0) {
-          st.parts[slot] = a;
-          mbar_arrive(bar(st.part_full[slot]));
         }
-      }
-      if (a.row < 0) break;
-      const int* bt_row = p.block_table + (size_t)a.row * p.max_pages;
-      const int pg0 = a.kb0 / kPage + a.b0 * kBlockPages;
-      const int page_end = (a.len + kPage - 1) / kPage;
-      auto load_ids = [&](int c) -> int {  // page id of page pg0 + 32c + lane, or -1
-        const int lp = pg0 + 32 * c + lane;
-        int v = -1;
-        if (lp < page_end && lp < pg0 + (a.b1 - a.b0) * kBlockPages) {
-          v = __ldg(bt_row + lp);
-          if (v < 0 || v >= p.num_pages) {
-            atomicOr(p.status, kStatusBadPage);
-            v = -1;
+        // page ids and mask words are on their way while the slot empties
+        const int* bt_row = p.block_table + (size_t)a.row * p.max_pages;
+        const int n = a.b1 - a.b0, pg0 = a.kb0 / kPage + a.b0 * kBlockPages;
+        const int page_end = min((a.len + kPage - 1) / kPage, pg0 + n * kBlockPages);
+        auto load_ids = [&](int c) -> int {  // page id of page pg0 + 32c + lane, or -1
+          const int lp = pg0 + 32 * c + lane;
+          int v = -1;
+          if (lp < page_end) {
+            v = __ldg(bt_row + lp);
+            if (v < 0 || v >= p.num_pages) {
+              atomicOr(p.status, kStatusBadPage);
+              v = -1;
+            }
           }
+          return v;
+        };
+        int ids = load_ids(0), ids_next = load_ids(1);
+        const uint32_t* rows = p.mask + (size_t)a.token * p.words;
+        const uint32_t* all = rows - (size_t)a.node * p.words;
+        const int L = a.len - a.ctx, mine = a.n_tok * p.words;
+        const uint32_t early = lane < mine ? __ldg(rows + lane) : 0u;
+        int early_pos = 0;
+        if (p.window > 0 && lane < a.n_tok) early_pos = __ldg(p.positions + a.token + lane);
+        const float sink = lane < g ? tree_sink(p, a.kvh * g + lane) : -INFINITY;
+        if (i >= 2 && !__all_sync(0xffffffffu, wait_sleep(bar(ln.part_empty[slot]), ((i >> 1) - 1) & 1, abort_flag))) {
+          ok = false;
+          break;
         }
-        return v;
-      };
-      int ids = load_ids(0), ids_next = load_ids(1);
-      if (is_k) {
-        if (i >= 1 && !__all_sync(0xffffffffu, wait_sleep(bar(st.q_empty), (i - 1) & 1, abort_flag))) break;
         if (lane == 0) {
-          mbar_arrive_expect_tx(bar(st.q_full), a.alt ? kTileQBytes : kQBytes);
-          tma_load_3d(sQ, a.alt ? &qmap_alt : &qmap, 0, a.kvh * g, a.token, bar(st.q_full));
+          ln.parts[slot] = a;
+          mbar_arrive(bar(ln.part_full[slot]));
         }
-        q_issued = i + 1;
-      }
-      ++i;
-      bool ok = true;
-      const int n = a.b1 - a.b0;
-      for (int b = 0; b < n; ++b, ++kv_it) {
-        if (b > 0 && (b * kBlockPages) % 32 == 0) {
-          ids = ids_next;
-          ids_next = load_ids(b * kBlockPages / 32 + 1);
+        if (i >= 1 && !__all_sync(0xffffffffu, wait_sleep(bar(ln.q_empty), (i - 1) & 1, abort_flag))) {
+          ok = false;
+          break;
         }
-        const uint32_t s = kv_it % stages;
-        if (kv_it >= stages) {
-          ok = __all_sync(0xffffffffu, wait_sleep(bar(empty[s]), (kv_it / stages - 1) & 1, abort_flag));
-          if (!ok) break;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar(ln.q_full), kQBytes);
+          tma_load_3d(sQ, &qmap, 0, a.kvh * g, a.token, bar(ln.q_full));
         }
-        arrive_expect_tx_e(bar(full[s]), kBlockBytes);
+        __syncwarp();
+        ++i;
+        // K of block b, then V of block b - 1: one copy of the code for both,
+        // the kernel's instructions barely fit their cache
+        int y[2][kBlockPages];
+#pragma unroll 1
+        for (int step = 0; step < 2 * n + 2 && ok; ++step) {
+          const int b = step >> 1;
+          const bool is_k = !(step & 1);
+          if (is_k) {
 #pragma unroll
-        for (int j = 0; j < kBlockPages; ++j) {
-          const int pid = __shfl_sync(0xffffffffu, ids, (b * kBlockPages) % 32 + j);
-          const int y = pid < 0 ? p.oob_row : (pid * Hkv + a.kvh) * kPage;
-          tma_load_2d_e(ring + s * kBlockBytes + j * kTileBytes, map, y, bar(full[s]), pol);
+            for (int j = 0; j < kBlockPages; ++j) y[1][j] = y[0][j];
+            if (b == n) continue;
+            if (b > 0 && (b * kBlockPages) % 32 == 0) {
+              ids = ids_next;
+              ids_next = load_ids(b * kBlockPages / 32 + 1);
+            }
+#pragma unroll
+            for (int j = 0; j < kBlockPages; ++j) {
+              const int pid = __shfl_sync(0xffffffffu, ids, (b * kBlockPages) % 32 + j);
+              y[0][j] = pid < 0 ? p.oob_row : (pid * Hkv + a.kvh) * kPage;
+            }
+          } else if (b == 0) {  // behind the first K block: what the softmax needs of the masks
+            Meta& m = ln.meta[slot];
+            auto first_key = [&](int pos) { return min(max(pos, a.ctx), a.len - 1) - p.window + 1; };
+            for (int k = lane; k < mine; k += 32) m.mask[k] = k < 32 ? early : __ldg(rows + k);
+            if (p.window > 0)
+              for (int k = lane; k < a.n_tok; k += 32)
+                m.lo[k] = first_key(k < 32 ? early_pos : __ldg(p.positions + a.token + k));
+            if (a.b1 * kBlockKeys + a.kb0 > a.ctx)  // the part reaches the nodes
+              for (int c = 0; c < p.words; ++c) {
+                uint32_t any = 0;
+                for (int k = lane; k < L; k += 32) any |= __ldg(all + (size_t)k * p.words + c);
+                any = __reduce_or_sync(0xffffffffu, any);
+                if (lane == 0) m.seen_by_any[c] = any;
+              }
+            if (lane < g) m.sinks[lane] = sink;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(ln.meta_full[slot]));
+            __syncwarp();
+            continue;
+          }
+          const uint32_t it = is_k ? k_it : v_it, stages = is_k ? kKStages : kVStages, s = it % stages;
+          uint64_t* full = is_k ? ln.k_full : ln.v_full;
+          uint64_t* empty = is_k ? ln.k_empty : ln.v_empty;
+          if (it >= stages) {
+            ok = __all_sync(0xffffffffu, wait_sleep(bar(empty[s]), (it / stages - 1) & 1, abort_flag));
+            if (!ok) break;
+          }
+          const uint32_t dst = (is_k ? sK : sV) + s * kBlockBytes;
+          const CUtensorMap* map = is_k ? &kmap : &vmap;
+          arrive_expect_tx_e(bar(full[s]), kBlockBytes);
+#pragma unroll
+          for (int j = 0; j < kBlockPages; ++j)
+            tma_load_2d_e(dst + j * kTileBytes, map, is_k ? y[0][j] : y[1][j], bar(full[s]), pol);
+          if (is_k) ++k_it; else ++v_it;
         }
+        if (!ok) break;
       }
-      if (!ok) break;
+    }
+    if (ok && (i < 2 || __all_sync(0xffffffffu, wait_sleep(bar(ln.part_empty[i & 1]), ((i >> 1) - 1) & 1, abort_flag)))) {
+      if (lane == 0) {  // no more parts
+        ln.parts[i & 1].row = -1;
+        mbar_arrive(bar(ln.part_full[i & 1]));
+      }
     }
     // after an abort: wait (bounded) for the copies still in flight
     if (*abort_flag && lane == 0) {
-      for (uint32_t it = kv_it > stages ? kv_it - stages : 0; it < kv_it; ++it)
-        mbar_wait(bar(full[it % stages]), (it / stages) & 1);
-      if (q_issued > 0) mbar_wait(bar(st.q_full), (q_issued - 1) & 1);
+      for (uint32_t it = k_it > kKStages ? k_it - kKStages : 0; it < k_it; ++it)
+        mbar_wait(bar(ln.k_full[it % kKStages]), (it / kKStages) & 1);
+      for (uint32_t it = v_it > kVStages ? v_it - kVStages : 0; it < v_it; ++it)
+        mbar_wait(bar(ln.v_full[it % kVStages]), (it / kVStages) & 1);
+      if (i > 0) mbar_wait(bar(ln.q_full), (i - 1) & 1);
     }
-  } else if (warp == kIssueWarpA || warp == kIssueWarpA + 1) {
-    // ---------------------------------------------------------- MMA issuers
+  } else if (warp >= 8) {
+    // ------------------------------------------------------------ MMA issue
     constexpr uint32_t idS = idesc_bf16(kTileRows, kBlockKeys, false, false);
     constexpr uint32_t idO = idesc_bf16(kTileRows, kHeadDim, false, true);
     constexpr uint64_t kStageStep = kBlockBytes / 16, kVStep = 16 * kRowBytes / 16;
     const uint64_t kdesc0 = smem_desc_sw128(sK, 16, 1024), vdesc0 = smem_desc_sw128(sV, 1024, 1024);
-    const int x = warp - kIssueWarpA;
-    const uint32_t scol = tmem + col_s(x), pcol = tmem + col_p(x), ocol = tmem + col_o(x);
-    uint32_t kv_it = 0, cnt = 0;  // blocks of the CTA, blocks of this tile, before the part
+    const uint64_t qd = smem_desc_sw128(sQ, 16, 1024);
+    uint32_t cnt = 0;  // blocks of the parts before
     bool ok = true;
     for (int i = 0; ok; ++i) {
       const int slot = i & 1;
-      if (!wait_sleep(bar(st.part_full[slot]), (i >> 1) & 1, abort_flag)) break;
-      const Part a = st.parts[slot];
-      if (a.row < 0) break;
-      if (!wait_sleep(bar(st.q_full), i & 1, abort_flag)) break;
-      const int n = a.b1 - a.b0;
-      const int nx = a.alt ? (n + 1 - x) / 2 : n;  // this tile's blocks: x, x + 2, ... or all
-      const uint64_t qd = smem_desc_sw128(sQ + (a.alt ? 0 : x) * kTileQBytes, 16, 1024);
-      if (nx == 0) tc_commit_e(bar(st.q_empty));
-      for (int b = 0; b <= nx && nx > 0; ++b) {
-        if (b < nx) {  // S(b)
-          const uint32_t it = kv_it + (a.alt ? 2 * b + x : b), bk = cnt + b;
-          const int s = it % kKStages;
-          if (!wait_sleep(bar(st.k_full[s]), (it / kKStages) & 1, abort_flag) ||
-              (bk >= 1 && !wait_sleep(bar(st.s_free[x]), (bk - 1) & 1, abort_flag))) {
+      if (!wait_sleep(bar(ln.part_full[slot]), (i >> 1) & 1, abort_flag)) break;
+      if (ln.parts[slot].row < 0) break;
+      const int n = ln.parts[slot].b1 - ln.parts[slot].b0;
+      if (!wait_sleep(bar(ln.q_full), i & 1, abort_flag)) break;
+      for (int b = 0; b <= n; ++b) {
+        if (b < n) {  // S(b)
+          const uint32_t bk = cnt + b;
+          const int s = bk % kKStages;
+          if (!wait_sleep(bar(ln.k_full[s]), (bk / kKStages) & 1, abort_flag) ||
+              (bk >= 1 && !wait_sleep(bar(ln.s_free), (bk - 1) & 1, abort_flag))) {
             ok = false;
             break;
           }
           tc_fence_after();
           const uint64_t kd = kdesc0 + s * kStageStep;
-          tc_mma_ss_e(scol, qd, kd, idS, 0u);
+          tc_mma_ss_e(tmem, qd, kd, idS, 0u);
 #pragma unroll
           for (int kk = 1; kk < kHeadDim / 16; ++kk)
-            tc_mma_ss_e(scol, qd + (uint64_t)(kk * 2), kd + (uint64_t)(kk * 2), idS, 1u);
-          tc_commit_e(bar(st.s_full[x]));
-          tc_commit_e(bar(st.k_empty[s]));
-          if (a.alt) tc_commit_e(bar(st.k_empty[s]));  // the other tile does not read this stage
-          if (b == nx - 1) tc_commit_e(bar(st.q_empty));
+            tc_mma_ss_e(tmem, qd + (uint64_t)(kk * 2), kd + (uint64_t)(kk * 2), idS, 1u);
+          tc_commit_e(bar(ln.s_full));
+          tc_commit_e(bar(ln.k_empty[s]));
+          if (b == n - 1) tc_commit_e(bar(ln.q_empty));
         }
         if (b >= 1) {  // O += P(b - 1) V(b - 1)
-          const uint32_t it = kv_it + (a.alt ? 2 * (b - 1) + x : b - 1), bk = cnt + b - 1;
-          const int s = it % kVStages;
-          if (!wait_sleep(bar(st.v_full[s]), (it / kVStages) & 1, abort_flag) ||
-              !wait_sleep(bar(st.p_full[x]), bk & 1, abort_flag) ||
-              (b == 1 && i >= 1 && !wait_sleep(bar(st.o_free[x]), (i - 1) & 1, abort_flag))) {
+          const uint32_t bv = cnt + b - 1;
+          const int s = bv % kVStages;
+          if (!wait_sleep(bar(ln.v_full[s]), (bv / kVStages) & 1, abort_flag) ||
+              !wait_sleep(bar(ln.p_full), bv & 1, abort_flag) ||
+              (b == 1 && i >= 1 && !wait_sleep(bar(ln.o_free), (i - 1) & 1, abort_flag))) {
             ok = false;
             break;
           }
           tc_fence_after();
           const uint64_t vd = vdesc0 + s * kStageStep;
-          tc_mma_ts_e(ocol, pcol, vd, idO, b > 1 ? 1u : 0u);
+          tc_mma_ts_e(tmem + kColO, tmem + kColP, vd, idO, b > 1 ? 1u : 0u);
 #pragma unroll
-          for (int kk = 1; kk < kBlockKeys / 16; ++kk) tc_mma_ts_e(ocol, pcol + kk * 8, vd + kk * kVStep, idO, 1u);
-          tc_commit_e(bar(st.o_ready[x]));
-          tc_commit_e(bar(st.v_empty[s]));
-          if (a.alt) tc_commit_e(bar(st.v_empty[s]));
+          for (int kk = 1; kk < kBlockKeys / 16; ++kk)
+            tc_mma_ts_e(tmem + kColO, tmem + kColP + kk * 8, vd + kk * kVStep, idO, 1u);
+          tc_commit_e(bar(ln.o_ready));
+          tc_commit_e(bar(ln.v_empty[s]));
         }
       }
       if (!ok) break;
-      cnt += nx;
-      kv_it += n;
-      if (lane == 0) mbar_arrive(bar(st.part_empty[slot]));
+      cnt += n;
+      if (lane == 0) mbar_arrive(bar(ln.part_empty[slot]));
     }
     // MMAs still in flight (after an abort) must not outlive TMEM
-    tc_commit_e(bar(st.drain[x]));
-    mbar_wait(bar(st.drain[x]), 0);
+    tc_commit_e(bar(ln.drain));
+    mbar_wait(bar(ln.drain), 0);
   } else {
     // -------------------------------------------------------------- softmax
-    const int x = warp >> 2, wq = warp & 3;
-    const int row = threadIdx.x & (kTileRows - 1);
-    const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-    const uint32_t cS = tmem + lane_off + col_s(x), cP = tmem + lane_off + col_p(x), cO = tmem + lane_off + col_o(x);
-    const int tok0 = row / g, head = row % g;
-    uint32_t kv_it = 0, cnt = 0, n_xch = 0;
+    const int wq = warp & 3, row = threadIdx.x & (kTileRows - 1);
+    const uint32_t cS = tmem + ((uint32_t)(wq * 32) << 16), cO = cS + kColO, cP = cS + kColP;
+    const int tok = row / g, head = row % g;
+    uint32_t cnt = 0;  // blocks so far: phase of every block barrier
     bool ok = true;
     for (int i = 0; ok; ++i) {
       const int slot = i & 1;
-      ok = __all_sync(0xffffffffu, wait_poll(bar(st.part_full[slot]), (i >> 1) & 1, abort_flag));
+      ok = __all_sync(0xffffffffu, wait_poll(bar(ln.part_full[slot]), (i >> 1) & 1, abort_flag));
       if (!ok) break;
-      const Part& a = st.parts[slot];  // valid until part_empty; re-read where needed to save registers
+      const Part& a = ln.parts[slot];  // valid until part_empty; re-read where needed to save registers
       if (a.row < 0) break;
-      const bool alt = a.alt;
+      if (!part_ok(p, a)) {
+        atomicOr(p.status, kStatusPlanOverflow);
+        *abort_flag = 2;
+        break;
+      }
+      ok = __all_sync(0xffffffffu, wait_poll(bar(ln.meta_full[slot]), (i >> 1) & 1, abort_flag));
+      if (!ok) break;
       const int n = a.b1 - a.b0;
-      const int nx = alt ? (n + 1 - x) / 2 : n;
-      const int tok = (alt ? 0 : x * (kTileRows / g)) + tok0;
-      const bool busy = (alt ? 0 : x * kTileRows) + wq * 32 < a.n_tok * g;  // this warp has rows
-      const int t = a.token + min(tok, a.n_tok - 1);
-      int lo = 0;
-      if (p.window > 0) lo = min(max(__ldg(p.positions + t), a.ctx), a.len - 1) - p.window + 1;
+      const int my_node = min(tok, a.n_tok - 1);
       // blocks that need no mask: keys [plain_lo, ctx) are seen by every node
       const int plain_lo = p.window > 0 ? a.len - p.window : 0, plain_hi = a.ctx - kBlockKeys;
-      int kb = a.kb0 + (a.b0 + (alt ? x : 0)) * kBlockKeys;
-      uint32_t it = kv_it + (alt ? x : 0);
+      int kb = a.kb0 + a.b0 * kBlockKeys;
       float m_ref = -INFINITY, l = 0.f;
+      const bool busy = wq * 32 < a.n_tok * g;  // this warp has rows
       // V rows that no node sees may hold anything, and a zero weight does not
-      // cancel a NaN: they are cleared before the tile's PV reads them
+      // cancel a NaN: they are cleared before the PV reads them
       auto clear_dead = [&](bool dead) -> bool {
         if (!__any_sync(0xffffffffu, dead)) return true;
-        const uint32_t s = it % kVStages;
-        if (!__all_sync(0xffffffffu, wait_poll(bar(st.v_full[s]), (it / kVStages) & 1, abort_flag))) return false;
+        const uint32_t s = cnt % kVStages;
+        if (!__all_sync(0xffffffffu, wait_poll(bar(ln.v_full[s]), (cnt / kVStages) & 1, abort_flag))) return false;
         if (dead) {
 #pragma unroll
           for (int c = 0; c < 8; ++c) zero_smem16(sV + s * kBlockBytes + row * kRowBytes + c * 16);
@@ -627,62 +698,73 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         fence_proxy_async();
         return true;
       };
-      const int kb_step = alt ? 2 * kBlockKeys : kBlockKeys;
       if (!busy) {  // none of this warp's rows is a query: it only keeps the barriers and clears V rows
-        for (int b = 0; b < nx; ++b, ++cnt, kb += kb_step, it += alt ? 2 : 1) {
+        for (int b = 0; b < n; ++b, ++cnt, kb += kBlockKeys) {
           uint32_t seen[4];
-          const bool dead = (kb > plain_hi || kb < plain_lo) && block_masks(p, a, t, lo, kb, wq, lane, seen);
-          ok = __all_sync(0xffffffffu, wait_poll(bar(st.s_full[x]), cnt & 1, abort_flag));
+          const bool dead =
+              (kb > plain_hi || kb < plain_lo) && block_masks(p, a, ln.meta[slot], my_node, kb, wq, lane, seen);
+          ok = __all_sync(0xffffffffu, wait_poll(bar(ln.s_full), cnt & 1, abort_flag));
           if (!ok) break;
-          if (lane == 0) mbar_arrive(bar(st.s_free[x]));
+          if (lane == 0) mbar_arrive(bar(ln.s_free));
           // in step with the other warps: one arrival per phase
           if (cnt >= 1) {
-            ok = __all_sync(0xffffffffu, wait_poll(bar(st.o_ready[x]), (cnt - 1) & 1, abort_flag));
+            ok = __all_sync(0xffffffffu, wait_poll(bar(ln.o_ready), (cnt - 1) & 1, abort_flag));
             if (!ok) break;
           }
           ok = clear_dead(dead);
           if (!ok) break;
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(st.p_full[x]));
+          if (lane == 0) mbar_arrive(bar(ln.p_full));
         }
       } else {
-        for (int b = 0; b < nx; ++b, ++cnt, kb += kb_step, it += alt ? 2 : 1) {
+        for (int b = 0; b < n; ++b, ++cnt, kb += kBlockKeys) {
           const bool masked = kb > plain_hi || kb < plain_lo;
           uint32_t seen[4];  // bit e of word c: this thread's node sees key kb + 32c + e
           bool dead = false;
-          if (masked) dead = block_masks(p, a, t, lo, kb, wq, lane, seen);
-          ok = __all_sync(0xffffffffu, wait_poll(bar(st.s_full[x]), cnt & 1, abort_flag));
+          if (masked) dead = block_masks(p, a, ln.meta[slot], my_node, kb, wq, lane, seen);
+          ok = __all_sync(0xffffffffu, wait_poll(bar(ln.s_full), cnt & 1, abort_flag));
           if (!ok) break;
           tc_fence_after();
           uint32_t sv[2][32], pk[32];
           tmem_ld32(cS, sv[0]);
           tmem_ld32(cS + 32, sv[1]);
           tmem_ld_wait();
+          float alpha = 1.f, l0 = 0.f;
           if (masked) {
             hide(sv[0], seen[0]);
             hide(sv[1], seen[1]);
           }
-          float alpha = 1.f;
-          float l0 = chunk_weights(sv, p.scale_log2, m_ref, alpha, pk);
-          // the P buffer was last read by the tile's previous PV
+          if (!masked || __any_sync(0xffffffffu, (seen[0] | seen[1]) != 0u)) {
+            l0 = chunk_weights(sv, p.scale_log2, m_ref, alpha, pk);
+          } else {  // no row of the warp sees a key of this half
+#pragma unroll
+            for (int e = 0; e < 32; ++e) pk[e] = 0u;
+          }
+          // the P buffer was last read by the previous PV
           if (cnt >= 1) {
-            ok = __all_sync(0xffffffffu, wait_poll(bar(st.o_ready[x]), (cnt - 1) & 1, abort_flag));
+            ok = __all_sync(0xffffffffu, wait_poll(bar(ln.o_ready), (cnt - 1) & 1, abort_flag));
             if (!ok) break;
             tc_fence_after();
           }
+          __syncwarp();  // TMEM moves need the warp in step, also after the first block's maximum
           tmem_st32(cP, pk);
           tmem_ld32(cS + 64, sv[0]);
           tmem_ld32(cS + 96, sv[1]);
           tmem_ld_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(st.s_free[x]));
+          if (lane == 0) mbar_arrive(bar(ln.s_free));
           if (masked) {
             hide(sv[0], seen[2]);
             hide(sv[1], seen[3]);
           }
-          float a1 = 1.f;
-          const float l1 = chunk_weights(sv, p.scale_log2, m_ref, a1, pk);
+          float a1 = 1.f, l1 = 0.f;
+          if (!masked || __any_sync(0xffffffffu, (seen[2] | seen[3]) != 0u)) {
+            l1 = chunk_weights(sv, p.scale_log2, m_ref, a1, pk);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) pk[e] = 0u;
+          }
           if (__any_sync(0xffffffffu, a1 != 1.f)) {  // the reference rose: rescale the first half's weights too
             tmem_st_wait();
             uint32_t pv[32];
@@ -703,7 +785,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           if (!ok) break;
           if (b > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
             uint32_t ov[32];
-#pragma unroll
+#pragma unroll 1
             for (int h = 0; h < 2; ++h) {
               tmem_ld32(cO + 32 * h, ov);
               tmem_ld_wait();
@@ -715,184 +797,140 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(st.p_full[x]));
+          if (lane == 0) mbar_arrive(bar(ln.p_full));
         }
       }
       if (!ok) break;
-      kv_it += n;
-      // ---- end of the part
-      if (nx > 0) {
-        ok = __all_sync(0xffffffffu, wait_poll(bar(st.o_ready[x]), (cnt - 1) & 1, abort_flag));
-        if (!ok) break;
-      }
+      // ---- end of the part: O / l and the log-sum-exp, 16 dims at a time
+      ok = __all_sync(0xffffffffu, wait_poll(bar(ln.o_ready), (cnt - 1) & 1, abort_flag));
+      if (!ok) break;
       tc_fence_after();
-      uint32_t ov[2][32];
-      if (busy && nx > 0) {
-        tmem_ld32(cO, ov[0]);
-        tmem_ld32(cO + 32, ov[1]);
-        tmem_ld_wait();
-      } else {
+      if (busy) {
+        const bool writes = tok < a.n_tok;
+        const int part_slot = a.slot, h = a.kvh * g + head;
+        const float sink = ln.meta[slot].sinks[head];
+        float inv = l > 0.f ? 1.f / l : 0.f;
+        float lse2 = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
+        if (part_slot < 0 && sink > -INFINITY) inv = finish_with_sink(m_ref, l, sink, &lse2);
+        const size_t orow = (size_t)(a.token + tok) * Hq + h;
+        const size_t prow = (size_t)max(part_slot, 0) * kTileRows + row;
+#pragma unroll 1
+        for (int c = 0; c < kHeadDim / 16; ++c) {
+          __syncwarp();  // TMEM moves need the warp in step
+          uint32_t ov[16];
+          tmem_ld16(cO + 16 * c, ov);
+          tmem_ld_wait();
+          if (writes && part_slot < 0) {
+            uint32_t o[8];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) ov[0][e] = ov[1][e] = 0u;
+            for (int k = 0; k < 8; ++k)
+              o[k] = pack_bf16x2(__uint_as_float(ov[2 * k]) * inv, __uint_as_float(ov[2 * k + 1]) * inv);
+            uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kHeadDim) + 2 * c;
+            dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+          } else if (writes) {
+            float4* dst = reinterpret_cast<float4*>(p.o_part + prow * kHeadDim) + 4 * c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              dst[k] = make_float4(__uint_as_float(ov[4 * k]) * inv, __uint_as_float(ov[4 * k + 1]) * inv,
+                                   __uint_as_float(ov[4 * k + 2]) * inv, __uint_as_float(ov[4 * k + 3]) * inv);
+          }
+        }
+        if (writes) {
+          if (part_slot < 0)
+            p.lse[orow] = lse2 * 0.69314718055994531f;
+          else
+            p.lse_part[prow] = lse2;
+        }
       }
-      const int token = a.token, kvh = a.kvh, part_slot = a.slot;
-      bool writes = tok < a.n_tok;
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(bar(st.o_free[x]));
-        mbar_arrive(bar(st.part_empty[slot]));
-      }
-      if (alt) {  // tile B hands its state to tile A
-        const uint32_t ph = n_xch & 1;
-        if (x == 1) {
-          if (n_xch >= 1) {
-            ok = __all_sync(0xffffffffu, wait_poll(bar(st.xch_empty), ph ^ 1, abort_flag));
-            if (!ok) break;
-          }
-          if (busy) {
-#pragma unroll
-            for (int d = 0; d < kHeadDim; ++d) xch[d * kTileRows + row] = __uint_as_float(ov[d >> 5][d & 31]);
-            xch[kHeadDim * kTileRows + row] = m_ref;
-            xch[(kHeadDim + 1) * kTileRows + row] = l;
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(st.xch_full));
-          writes = false;
-        } else {
-          ok = __all_sync(0xffffffffu, wait_poll(bar(st.xch_full), ph, abort_flag));
-          if (!ok) break;
-          if (busy) {
-            const float mb = xch[kHeadDim * kTileRows + row], lb = xch[(kHeadDim + 1) * kTileRows + row];
-            const float M = fmaxf(m_ref, mb);
-            const float fa = m_ref > -INFINITY ? exp2f(m_ref - M) : 0.f, fb = mb > -INFINITY ? exp2f(mb - M) : 0.f;
-            l = l * fa + lb * fb;
-            m_ref = M;
-#pragma unroll
-            for (int d = 0; d < kHeadDim; ++d)
-              ov[d >> 5][d & 31] = __float_as_uint(__uint_as_float(ov[d >> 5][d & 31]) * fa + xch[d * kTileRows + row] * fb);
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(st.xch_empty));
-        }
-        ++n_xch;
-      }
-      if (writes) {
-        float inv = l > 0.f ? 1.f / l : 0.f;
-        float lse2 = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
-        const int h = kvh * g + head;
-        if (part_slot < 0) {
-          if (p.sinks != nullptr) inv = finish_with_sink(m_ref, l, tree_sink(p, h), &lse2);
-          const size_t orow = (size_t)(token + tok) * Hq + h;
-          uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kHeadDim);
-#pragma unroll
-          for (int v = 0; v < 8; ++v) {
-            const int hh = v >> 2, e0 = (v & 3) * 8;
-            uint32_t o[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              o[k] = pack_bf16x2(__uint_as_float(ov[hh][e0 + 2 * k]) * inv, __uint_as_float(ov[hh][e0 + 2 * k + 1]) * inv);
-            dst[v] = make_uint4(o[0], o[1], o[2], o[3]);
-          }
-          p.lse[orow] = lse2 * 0.69314718055994531f;
-        } else {
-          const size_t prow = (size_t)part_slot * kItemRows + (alt ? 0 : x * kTileRows) + row;
-          float4* dst = reinterpret_cast<float4*>(p.o_part + prow * kHeadDim);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int hh = v >> 3, e0 = (v & 7) * 4;
-            dst[v] = make_float4(__uint_as_float(ov[hh][e0]) * inv, __uint_as_float(ov[hh][e0 + 1]) * inv,
-                                 __uint_as_float(ov[hh][e0 + 2]) * inv, __uint_as_float(ov[hh][e0 + 3]) * inv);
-          }
-          p.lse_part[prow] = lse2;
-        }
+        mbar_arrive(bar(ln.o_free));
+        mbar_arrive(bar(ln.part_empty[slot]));
       }
     }
   }
 
   __syncwarp();
-  if (threadIdx.x == 0 && *abort_flag) atomicOr(p.status, kStatusTimeout);
+  if (threadIdx.x == 0 && *abort_flag == 1) atomicOr(p.status, kStatusTimeout);
   tc_fence_before();
   __syncthreads();
-  if (warp == kIssueWarpA) {
+  if (warp == 8) {
     tc_fence_after();
-    tmem_dealloc(tmem, kTmemCols);
+    tmem_dealloc(st.tmem_base, kTmemCols);
   }
 }
 
-// Joins the parts of items that cross a cut of the line: out = sum_i 2^(b_i - b) o_i,
-// b = log2 sum_i 2^(b_i), in the order of the CTAs. One warp per (token, q
-// head), two dims a lane; heads of unsplit items leave at once.
-constexpr int kMergeWarps = 8;
+// Joins the parts of the tiles that cross a cut of their line: out = sum_i 2^(b_i - b) o_i,
+// b = log2 sum_i 2^(b_i), in the order of the pieces. Blocks (c, y): the tile
+// whose first part lies in piece c and its next ones in the pieces after it, if
+// there is one (on the joint line c counts both tiles of a pair), rows 32 y ..
+// of it; a thread takes four dims of a row, kMergeBatch parts' loads in flight
+// at once.
+constexpr int kMergeThreads = 256, kMergeRows = 32, kMergeBatch = 4;
 
-__global__ void __launch_bounds__(kMergeWarps * 32) merge_tree_kernel(const TreeParams p) {
+__global__ void __launch_bounds__(kMergeThreads) merge_tree_kernel(const TreeParams p, int ctas) {
   grid_dep_wait();
-  const int64_t quota = p.plan[0];
-  if (quota == 0) return;
-  const int64_t* prefix = p.plan + 1;
-  const int lane = threadIdx.x & 31, Hq = p.num_q_heads, g = p.group;
-  const int64_t n = (int64_t)p.total_q * Hq;
-  for (int64_t v = (int64_t)blockIdx.x * kMergeWarps + (threadIdx.x >> 5); v < n; v += (int64_t)gridDim.x * kMergeWarps) {
-    const int t = (int)(v / Hq), h = (int)(v % Hq);
-    int lo = 0, hi = p.num_seqs;  // qsl[lo] <= t < qsl[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (__ldg(p.qsl + mid) <= t) lo = mid; else hi = mid;
-    }
-    RowGeom w;
-    int32_t ignored = 0;
-    if (!row_geom(p, lo, &w, &ignored) || t < w.q0 || t >= w.q0 + w.L) continue;
-    const int tile_tok = kItemRows / g, tile = (t - w.q0) / tile_tok;
-    const int64_t cost = tile < w.tiles - 1 ? w.pair_cost : w.last_cost;
-    const int64_t u = prefix[lo] + (h / g) * w.head_cost() + tile * w.pair_cost;
-    const int c0 = (int)(u / quota), c1 = (int)((u + cost - 1) / quota);
-    const int prow = (t - w.q0 - tile * tile_tok) * g + h % g;
-    // parts of CTA c: blocks [before(c), before(c + 1))
-    float bmax = tree_sink(p, h);
-    const float s2 = bmax;
-    bool split = false;
-    for (int c = c0; c <= c1; ++c) {
-      const int b0 = blocks_before((int64_t)c * quota - u, w.nb, cost);
-      const int b1 = blocks_before((int64_t)(c + 1) * quota - u, w.nb, cost);
-      if (b0 == b1) continue;
-      if (b0 == 0 && b1 == w.nb) break;  // one part, written by its CTA
-      split = true;
-      bmax = fmaxf(bmax, p.lse_part[(size_t)(2 * c + (b0 == 0 ? 1 : 0)) * kItemRows + prow]);
-    }
-    if (!split) continue;
-    float sum = s2 > -INFINITY ? exp2f(s2 - bmax) : 0.f, o0 = 0.f, o1 = 0.f;
-    if (bmax > -INFINITY) {
-      for (int c = c0; c <= c1; ++c) {
-        const int b0 = blocks_before((int64_t)c * quota - u, w.nb, cost);
-        const int b1 = blocks_before((int64_t)(c + 1) * quota - u, w.nb, cost);
-        if (b0 == b1) continue;
-        const size_t pr = (size_t)(2 * c + (b0 == 0 ? 1 : 0)) * kItemRows + prow;
-        const float wt = exp2f(p.lse_part[pr] - bmax);
-        const float2 o = reinterpret_cast<const float2*>(p.o_part + pr * kHeadDim)[lane];
-        sum += wt;
-        o0 += wt * o.x;
-        o1 += wt * o.y;
+  const int line = (int)blockIdx.x >= 2 * ctas, rel = (int)blockIdx.x - (line ? 2 * ctas : 0);
+  const int k0 = line ? rel >> 1 : rel, x = line ? rel & 1 : 0;
+  const int g = p.group, Hq = p.num_q_heads;
+  const int4 cut = p.cuts[blockIdx.x];  // last piece, first token, tokens, kv head
+  const int c1 = cut.x, rows = cut.z * g, kvh = cut.w;
+  auto part_row = [&](int k, int r) -> size_t {
+    const int first = k == k0;
+    return (size_t)(line ? kTreeSoloSlots + (2 * k + first) * 2 + x : 2 * k + first) * kTileRows + r;
+  };
+  if (c1 <= k0) return;
+  for (int v = threadIdx.x; v < kMergeRows * 16; v += kMergeThreads) {
+    const int r = kMergeRows * blockIdx.y + (v >> 4), d = v & 15;
+    if (r >= rows) break;
+    const int h = kvh * g + r % g;
+    float m = tree_sink(p, h), sum = m > -INFINITY ? 1.f : 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = k0; k <= c1; k += kMergeBatch) {
+      float b[kMergeBatch];
+      float4 q[kMergeBatch];
+#pragma unroll
+      for (int e = 0; e < kMergeBatch; ++e) {
+        b[e] = -INFINITY;
+        q[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k + e <= c1) {
+          const size_t pr = part_row(k + e, r);
+          b[e] = p.lse_part[pr];
+          q[e] = reinterpret_cast<const float4*>(p.o_part + pr * kHeadDim)[d];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < kMergeBatch; ++e) {
+        if (b[e] == -INFINITY) continue;
+        const float mn = fmaxf(m, b[e]), f = m > -INFINITY ? exp2f(m - mn) : 0.f, wt = exp2f(b[e] - mn);
+        m = mn;
+        sum = sum * f + wt;
+        o.x = o.x * f + wt * q[e].x;
+        o.y = o.y * f + wt * q[e].y;
+        o.z = o.z * f + wt * q[e].z;
+        o.w = o.w * f + wt * q[e].w;
       }
     }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    const size_t orow = (size_t)t * Hq + h;
-    reinterpret_cast<uint32_t*>(p.out + orow * kHeadDim)[lane] = pack_bf16x2(o0 * inv, o1 * inv);
-    if (lane == 0) p.lse[orow] = sum > 0.f ? (bmax + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+    const size_t orow = (size_t)(cut.y + r / g) * Hq + h;
+    reinterpret_cast<uint2*>(p.out + orow * kHeadDim)[d] =
+        make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    if (d == 0) p.lse[orow] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
   }
 }
 
 }  // namespace
 
 cudaError_t launch_tree(const CUtensorMap& kmap, const CUtensorMap& vmap, const CUtensorMap& qmap,
-                        const CUtensorMap& qmap_alt, const TreeParams& p, int sms, cudaStream_t stream) {
+                        const TreeParams& p, int sms, cudaStream_t stream) {
   const int grid = sms < kTreeMaxCtas ? sms : kTreeMaxCtas;
-  tree_kernel<<<grid, kTreeThreads, tree_smem_bytes(), stream>>>(kmap, vmap, qmap, qmap_alt, p);
+  tree_kernel<<<grid, kTreeThreads, tree_smem_bytes(), stream>>>(kmap, vmap, qmap, p);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const int64_t heads = (int64_t)p.total_q * p.num_q_heads;
-  const int64_t want = (heads + kMergeWarps - 1) / kMergeWarps;
-  LaunchCfg lc(dim3((unsigned)(want < sms * 8 ? want : sms * 8)), dim3(kMergeWarps * 32), 0, stream, true);
-  return cudaLaunchKernelEx(&lc.cfg, merge_tree_kernel, p);
+  LaunchCfg lc(dim3(4 * grid, kTileRows / kMergeRows), dim3(kMergeThreads), 0, stream, true);
+  return cudaLaunchKernelEx(&lc.cfg, merge_tree_kernel, p, grid);
 }
 
 cudaError_t prepare_tree_kernels() {

@@ -31,16 +31,20 @@ struct TreeParams {
   __nv_bfloat16* out;
   float* lse;
   int32_t* status;
-  int64_t* plan;    // the quota of a CTA, then the prefix sums of the rows' costs [num_seqs + 1]
-  float* lse_part;  // [2 * kTreeMaxCtas][256] base-2 normalisers of split items' parts
-  float* o_part;    // [2 * kTreeMaxCtas][256][64], normalised
+  int4* cuts;       // [4 * kTreeMaxCtas] the cut tile that begins in each piece: last piece (-1: none), token, tokens, kv head
+  float* lse_part;  // [kTreeSlots][128] base-2 normalisers of cut tiles' parts
+  float* o_part;    // [kTreeSlots][128][64], normalised
   int32_t words, window, num_seqs, total_q, max_pages, num_pages, num_q_heads, num_kv_heads, group;
   int32_t oob_row;   // a pool row past the end: read as zeros
   float scale_log2;  // softmax scale * log2(e)
 };
 constexpr int kTreeMaxCtas = 160;  // CTAs the workspace has room for (one per SM)
+constexpr int kTreeTileRows = 128;
+// partial slots: two for each lane's piece of the solo line, two per tile of
+// the pair for each CTA's piece of the joint line
+constexpr int kTreeSoloSlots = 4 * kTreeMaxCtas, kTreeSlots = 8 * kTreeMaxCtas;
 cudaError_t launch_tree(const CUtensorMap& kmap, const CUtensorMap& vmap, const CUtensorMap& qmap,
-                        const CUtensorMap& qmap_alt, const TreeParams& p, int sms, cudaStream_t stream);
+                        const TreeParams& p, int sms, cudaStream_t stream);
 
 struct PoolPtrs {
   uint8_t* p[MCPU_MAX_POOLS];
