@@ -75,6 +75,9 @@ mcpu_status mcpu_norm_rope_kv_append(const void* q, int64_t q_stride, const void
     return MCPU_ERR_INVALID_ARG;
   if (q_out == q && q_stride != qd) return MCPU_ERR_INVALID_ARG;
   if (dims->num_pages < 1 || dims->max_pages_per_seq < 1) return MCPU_ERR_INVALID_ARG;
+  int sms = 0;
+  st = device_sms(&sms);
+  if (st != MCPU_OK) return st;
   NormRopeParams p;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.k = static_cast<const __nv_bfloat16*>(k_new);
@@ -101,7 +104,7 @@ mcpu_status mcpu_norm_rope_kv_append(const void* q, int64_t q_stride, const void
   p.num_q_heads = dims->num_q_heads;
   p.num_kv_heads = dims->num_kv_heads;
   p.max_position = max_position;
-  return from_cuda(launch_norm_rope(p, reinterpret_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_norm_rope(p, sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 size_t mcpu_tree_workspace_size(const mcpu_dims* dims) {

@@ -21,7 +21,7 @@ struct NormRopeParams {
   int32_t num_seqs, total_q, max_pages, num_pages, num_q_heads, num_kv_heads, max_position;
 };
 
-cudaError_t launch_norm_rope(const NormRopeParams& p, cudaStream_t stream);
+cudaError_t launch_norm_rope(const NormRopeParams& p, int sms, cudaStream_t stream);
 
 struct TreeParams {
   const int32_t *block_table, *seq_lens, *qsl;

@@ -528,15 +528,24 @@ def _raw(t):
 
 
 def _raw_stream(stream):
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    # the current device's current stream, without building a Stream object (2.9 us of a call's 16)
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return stream.cuda_stream
 
 
-def _token_stride(x, what):
+def _token_stride(x, shape, what):
     """Elements from one token to the next of a [T, H, D] tensor whose tokens are dense inside."""
     s = x.stride()
-    if x.dim() != 3 or x.dtype != torch.bfloat16 or s[2] != 1 or s[1] != x.shape[2]:
+    if x.dtype != torch.bfloat16 or len(s) != 3 or s[2] != 1 or s[1] != shape[2]:
         raise ValueError(f"{what} must be a bfloat16 [T, H, D] tensor with the heads of a token dense")
-    return s[0] if x.shape[0] > 1 else max(s[0], s[1] * x.shape[1])
+    return s[0] if shape[0] > 1 else max(s[0], s[1] * shape[1])
+
+
+def _dims(q_shape, k_cache, block_table, seq_lens) -> Dims:
+    t, hq, d = q_shape
+    p, hkv, page, _ = k_cache.shape
+    return Dims(seq_lens.shape[0], t, block_table.shape[1], p, hq, hkv, d, page)
 
 
 def _int32(x, what):
@@ -551,25 +560,25 @@ def mcpu_norm_rope_kv_append(q, k_new, v_new, q_weight, k_weight, eps, positions
     positions (int32 [T], or None for the tokens' own slots), q to q_out, K
     and V to the pages. q, k_new and v_new may be slices of one projection's
     output (any token stride that is a multiple of 8 elements)."""
-    if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or cos_sin.shape[1] != q.shape[2] or \
-            not cos_sin.is_contiguous():
+    qs, ks, cs = q.shape, k_new.shape, cos_sin.shape
+    if len(qs) != 3 or len(ks) != 3 or ks != v_new.shape or ks[0] != qs[0] or ks[1] != k_cache.shape[1]:
+        raise ValueError("q must be [T, H_q, D], k_new and v_new [T, H_kv, D]")
+    if cos_sin.dtype != torch.float32 or len(cs) != 2 or cs[1] != qs[2] or not cos_sin.is_contiguous():
         raise ValueError("cos_sin must be a contiguous float32 [max_position, head_dim] tensor")
     for w in (q_weight, k_weight):
-        if w.dtype != torch.float32 or w.numel() != q.shape[2] or not w.is_contiguous():
+        if w.dtype != torch.float32 or w.numel() != qs[2] or not w.is_contiguous():
             raise ValueError("q_weight and k_weight must be contiguous float32 [head_dim] tensors")
-    if q_out.dtype != torch.bfloat16 or q_out.shape != q.shape or not q_out.is_contiguous():
+    if q_out.dtype != torch.bfloat16 or q_out.shape != qs or not q_out.is_contiguous():
         raise ValueError("q_out must be a contiguous bfloat16 tensor of q's shape")
-    if positions is not None and positions.numel() != q.shape[0]:
+    if positions is not None and positions.numel() != qs[0]:
         raise ValueError("positions must have one entry per query token")
-    if k_new.shape != v_new.shape or k_new.shape[0] != q.shape[0] or k_new.shape[1] != k_cache.shape[1]:
-        raise ValueError("k_new and v_new must be [T, H_kv, D]")
-    d = dims(q, k_cache, block_table, seq_lens)
     code = _lib.mcpu_norm_rope_kv_append(
-        q.data_ptr(), _token_stride(q, "q"), k_new.data_ptr(), _token_stride(k_new, "k_new"), v_new.data_ptr(),
-        _token_stride(v_new, "v_new"), q_weight.data_ptr(), k_weight.data_ptr(), eps,
-        None if positions is None else _int32(positions, "positions"), cos_sin.data_ptr(), cos_sin.shape[0],
-        q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
-        query_start_loc.data_ptr(), d, status_word.data_ptr(), _raw_stream(stream))
+        q.data_ptr(), _token_stride(q, qs, "q"), k_new.data_ptr(), _token_stride(k_new, ks, "k_new"), v_new.data_ptr(),
+        _token_stride(v_new, ks, "v_new"), q_weight.data_ptr(), k_weight.data_ptr(), eps,
+        None if positions is None else _int32(positions, "positions"), cos_sin.data_ptr(), cs[0], q_out.data_ptr(),
+        k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+        query_start_loc.data_ptr(), _dims(qs, k_cache, block_table, seq_lens), status_word.data_ptr(),
+        _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_norm_rope_kv_append")
 
@@ -596,11 +605,11 @@ def mcpu_tree_attention_forward(q, k_cache, v_cache, block_table, seq_lens, quer
         raise ValueError("tree_mask must be an int32 [T, words] tensor")
     if sinks is not None and (sinks.dtype != torch.float32 or sinks.numel() != q.shape[1] or not sinks.is_cuda):
         raise ValueError("sinks must be a float32 CUDA tensor with one value per q head")
-    d = dims(q, k_cache, block_table, seq_lens)
     code = _lib.mcpu_tree_attention_forward(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
         query_start_loc.data_ptr(), _int32(tree_mask, "tree_mask"), tree_mask.shape[1], _raw(positions), sliding_window,
-        softmax_scale, _raw(sinks), d, out.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
+        softmax_scale, _raw(sinks), _dims(q.shape, k_cache, block_table, seq_lens), out.data_ptr(), lse.data_ptr(),
+        workspace.data_ptr(),
         workspace.numel() * workspace.element_size(), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_tree_attention_forward")
