@@ -237,7 +237,7 @@ mcpu_status mcpu_shrink_block_tables(int32_t* block_table, const int32_t* seq_le
                                      mcpu_stream_t stream) {
   mcpu_status st = check_page_dims(dims);
   if (st != MCPU_OK) return st;
-  if (dims->num_seqs == 0) return MCPU_OK;
+  if (dims->num_seqs == 0 || dims->max_pages_per_seq == 0) return MCPU_OK;
   if (!words_ok(block_table, seq_lens, page_refs, free_pages, free_count, page_scratch, status_word))
     return MCPU_ERR_INVALID_ARG;
   PageParams p{};

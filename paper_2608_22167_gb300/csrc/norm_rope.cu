@@ -42,32 +42,72 @@ __device__ __forceinline__ float2 unpack2(uint32_t v) {
   return __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v));
 }
 
-// Norm and rotation of a token's `rows` head rows, from x (dense) to rows
-// out_step elements apart; the warp takes rows first, first + 4 kSplit, ...
+// kSplit warps share a token. Its head rows are numbered q, then k, then v; a
+// warp takes rows first, first + kStep, ... The first batch of loads needs the
+// token's number only and is on its way while its row, position and page are
+// looked up.
 template <int kSplit>
-__device__ __forceinline__ void turn_rows(const __nv_bfloat16* x, __nv_bfloat16* out, int out_step, const float* weight,
-                                          float eps, const float (&c)[4], const float (&s)[4], int rows, int first,
-                                          int j) {
-  float w[8];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    w[e] = __ldg(weight + 4 * j + e);
-    w[4 + e] = __ldg(weight + 32 + 4 * j + e);
-  }
+__global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRopeParams p) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane >> 3, j = lane & 7;
+  const int t = blockIdx.x * (kNormWarps / kSplit) + warp / kSplit;
+  if (t >= p.total_q) return;
+  const int Hq = p.num_q_heads, Hkv = p.num_kv_heads, all = Hq + 2 * Hkv;
   constexpr int kStep = 4 * kSplit;
-  // (first & 3 differs by lane group: the bound keeps the warp together for the shuffles)
-  for (int r0 = first; r0 < rows + (first & 3); r0 += kStep * kRowBatch) {
-    uint2 lo[kRowBatch], hi[kRowBatch];
+  const int first = (warp % kSplit) * 4 + sub;
+  uint2 lo[kRowBatch], hi[kRowBatch];
+  auto load = [&](int r0) {
 #pragma unroll
     for (int b = 0; b < kRowBatch; ++b) {
       const int row = r0 + b * kStep;
       lo[b] = hi[b] = make_uint2(0u, 0u);
-      if (row < rows) {
-        const uint2* in = reinterpret_cast<const uint2*>(x + row * kHeadDim);
-        lo[b] = __ldcs(in + j);
-        hi[b] = __ldcs(in + 8 + j);
+      if (row < all) {
+        const __nv_bfloat16* x = row < Hq         ? p.q + t * p.q_stride + row * kHeadDim
+                                 : row < Hq + Hkv ? p.k + t * p.k_stride + (row - Hq) * kHeadDim
+                                                  : p.v + t * p.v_stride + (row - Hq - Hkv) * kHeadDim;
+        lo[b] = __ldcs(reinterpret_cast<const uint2*>(x) + j);
+        hi[b] = __ldcs(reinterpret_cast<const uint2*>(x) + 8 + j);
       }
     }
+  };
+  load(first);
+  if (p.qsl[0] != 0 || p.qsl[p.num_seqs] != p.total_q) {
+    if (lane == 0) atomicOr(p.status, kStatusBadLengths);
+    return;
+  }
+  float w[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    w[e] = __ldg(p.wq + 4 * j + e);
+    w[4 + e] = __ldg(p.wq + 32 + 4 * j + e);
+  }
+  // the angles come by a given position, or by the slot once the row is known
+  int pos = p.positions ? __ldg(p.positions + t) : -1;
+  float c[4], s[4];
+  auto load_angles = [&]() {
+    const float* ang = p.cos_sin + (size_t)pos * kHeadDim + 4 * j;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {  // scalar loads: the table is 4-byte aligned
+      c[e] = __ldg(ang + e);
+      s[e] = __ldg(ang + 32 + e);
+    }
+  };
+  if (pos >= 0 && pos < p.max_position) load_angles();
+  const int r = find_row(p.qsl, p.num_seqs, t, lane);
+  const int q0 = __ldg(p.qsl + r), q1 = __ldg(p.qsl + r + 1), S = __ldg(p.seq_lens + r);
+  const int L = q1 - q0, slot = S - L + (t - q0);
+  const bool fits = L >= 1 && S >= L && S <= p.max_pages * kPage && t >= q0 && t < q1;
+  if (!p.positions) pos = slot;
+  if (!fits || pos < 0 || pos >= p.max_position) {
+    if (lane == 0) atomicOr(p.status, kStatusBadLengths);
+    return;
+  }
+  const int page = __ldg(p.block_table + (size_t)r * p.max_pages + slot / kPage);
+  const bool page_ok = page >= 0 && page < p.num_pages;
+  if (!page_ok && lane == 0) atomicOr(p.status, kStatusBadPage);
+  if (!p.positions) load_angles();
+  const int rows = page_ok ? all : Hq;  // rows that are written
+  const size_t cache = ((size_t)max(page, 0) * Hkv * kPage + slot % kPage) * kHeadDim;
+  for (int r0 = first;;) {
 #pragma unroll
     for (int b = 0; b < kRowBatch; ++b) {
       const int row = r0 + b * kStep;
@@ -78,62 +118,36 @@ __device__ __forceinline__ void turn_rows(const __nv_bfloat16* x, __nv_bfloat16*
       for (int e = 0; e < 4; ++e) ss = fmaf(a[e], a[e], fmaf(d[e], d[e], ss));
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      const float mean = ss * (1.f / kHeadDim) + eps;
-      const float inv = mean > 0.f ? 1.f / sqrtf(mean) : 0.f;
-      float y[8];
+      if (row >= Hq)  // from here on: k (the rows of v ignore it)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float u = a[e] * inv * w[e], v = d[e] * inv * w[4 + e];
-        y[e] = u * c[e] - v * s[e];
-        y[4 + e] = v * c[e] + u * s[e];
+        for (int e = 0; e < 4; ++e) {
+          w[e] = __ldg(p.wk + 4 * j + e);
+          w[4 + e] = __ldg(p.wk + 32 + 4 * j + e);
+        }
+      const float mean = ss * (1.f / kHeadDim) + p.eps;
+      const float inv = mean > 0.f ? 1.f / sqrtf(mean) : 0.f;
+      if (row < Hq + Hkv) {
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float u = a[e] * inv * w[e], v = d[e] * inv * w[4 + e];
+          y[e] = u * c[e] - v * s[e];
+          y[4 + e] = v * c[e] + u * s[e];
+        }
+        lo[b] = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+        hi[b] = make_uint2(pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
       }
       if (row < rows) {
-        uint2* to = reinterpret_cast<uint2*>(out + (size_t)row * out_step);
-        to[j] = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
-        to[8 + j] = make_uint2(pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+        __nv_bfloat16* out = row < Hq         ? p.q_out + ((size_t)t * Hq + row) * kHeadDim
+                             : row < Hq + Hkv ? p.k_cache + cache + (size_t)(row - Hq) * kPage * kHeadDim
+                                              : p.v_cache + cache + (size_t)(row - Hq - Hkv) * kPage * kHeadDim;
+        reinterpret_cast<uint2*>(out)[j] = lo[b];
+        reinterpret_cast<uint2*>(out)[8 + j] = hi[b];
       }
     }
-  }
-}
-
-// kSplit warps share a token
-template <int kSplit>
-__global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRopeParams p) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane >> 3, j = lane & 7;
-  const int t = blockIdx.x * (kNormWarps / kSplit) + warp / kSplit;
-  if (t >= p.total_q) return;
-  if (p.qsl[0] != 0 || p.qsl[p.num_seqs] != p.total_q) {
-    if (lane == 0) atomicOr(p.status, kStatusBadLengths);
-    return;
-  }
-  const int r = find_row(p.qsl, p.num_seqs, t, lane);
-  const int q0 = __ldg(p.qsl + r), q1 = __ldg(p.qsl + r + 1), S = __ldg(p.seq_lens + r);
-  const int L = q1 - q0, slot = S - L + (t - q0);
-  const bool fits = L >= 1 && S >= L && S <= p.max_pages * kPage && t >= q0 && t < q1;
-  const int pos = !fits ? -1 : p.positions ? __ldg(p.positions + t) : slot;
-  if (pos < 0 || pos >= p.max_position) {
-    if (lane == 0) atomicOr(p.status, kStatusBadLengths);
-    return;
-  }
-  const int page = __ldg(p.block_table + (size_t)r * p.max_pages + slot / kPage);
-  const bool page_ok = page >= 0 && page < p.num_pages;
-  if (!page_ok && lane == 0) atomicOr(p.status, kStatusBadPage);
-  const float* ang = p.cos_sin + (size_t)pos * kHeadDim + 4 * j;
-  float c[4], s[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {  // scalar loads: the table is 4-byte aligned
-    c[e] = __ldg(ang + e);
-    s[e] = __ldg(ang + 32 + e);
-  }
-  const int Hq = p.num_q_heads, Hkv = p.num_kv_heads, first = (warp % kSplit) * 4 + sub;
-  turn_rows<kSplit>(p.q + t * p.q_stride, p.q_out + (size_t)t * Hq * kHeadDim, kHeadDim, p.wq, p.eps, c, s, Hq, first, j);
-  if (!page_ok) return;
-  const size_t cache = ((size_t)page * Hkv * kPage + slot % kPage) * kHeadDim;
-  turn_rows<kSplit>(p.k + t * p.k_stride, p.k_cache + cache, kPage * kHeadDim, p.wk, p.eps, c, s, Hkv, first, j);
-  const __nv_bfloat16* vt = p.v + t * p.v_stride;
-  for (int row = first; row < Hkv; row += 4 * kSplit) {
-    const uint4 v = __ldcs(reinterpret_cast<const uint4*>(vt + row * kHeadDim) + j);
-    reinterpret_cast<uint4*>(p.v_cache + cache + (size_t)row * kPage * kHeadDim)[j] = v;
+    r0 += kStep * kRowBatch;
+    if (r0 - sub >= rows) break;  // the whole warp
+    load(r0);
   }
 }
 
@@ -142,7 +156,7 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
 cudaError_t launch_norm_rope(const NormRopeParams& p, int sms, cudaStream_t stream) {
   // warps per token: a warp each once that makes several waves of blocks, else
   // as many as keep the SMs full
-  if (p.total_q > 64 * sms)
+  if (p.total_q > 16 * sms)
     norm_rope_kernel<1><<<(p.total_q + 7) / 8, kNormThreads, 0, stream>>>(p);
   else if (p.total_q > 4 * sms)
     norm_rope_kernel<4><<<(p.total_q + 1) / 2, kNormThreads, 0, stream>>>(p);

@@ -10,8 +10,8 @@ namespace mcpu {
 
 namespace {
 
-constexpr int kForkThreads = 128;
-constexpr int kShrinkWarps = 8;
+constexpr int kForkThreads = 128, kForkEarly = 4;
+constexpr int kReleaseThreads = 128, kReleasePer = 4, kReleaseSpan = kReleaseThreads * kReleasePer;
 constexpr int kCollectThreads = 1024, kCollectPer = 4;
 constexpr int kCopyThreads = 256;
 constexpr int kCompactThreads = 256, kCompactMoves = 128, kCompactPools = 4, kCompactBatch = 8;
@@ -46,6 +46,13 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const PageParams p) 
   const bool ok = fork_valid(p, f, &S);
   const bool partial = ok && S % kPage != 0;
   const int avail = min(max(__ldcg(p.free_count), 0), p.num_pages);
+  // the first entries of the source's table are on their way while the rank is counted
+  int early[kForkEarly];
+#pragma unroll
+  for (int i = 0; i < kForkEarly; ++i) {
+    const int j = threadIdx.x + i * kForkThreads;
+    early[i] = ok && j < S / kPage ? p.block_table[(size_t)__ldg(p.src_rows + f) * p.max_pages + j] : -1;
+  }
   int rank = 0;
   if (partial) {  // uniform over the block
     for (int e0 = 0; e0 < f; e0 += kForkThreads) {
@@ -82,10 +89,10 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const PageParams p) 
       s_page = page;
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < p.max_pages; j += kForkThreads) {
+    for (int j = threadIdx.x, i = 0; j < p.max_pages; j += kForkThreads, ++i) {
       int e = -1;
       if (j < full) {
-        e = from[j];
+        e = i == 0 ? early[0] : i == 1 ? early[1] : i == 2 ? early[2] : i == 3 ? early[3] : from[j];
         if (e >= p.num_pages) {
           atomicOr(p.status, kStatusBadPage);
           e = -1;
@@ -113,36 +120,48 @@ __host__ __device__ inline int segment_pages(int num_pages) {
   return per > 0 ? per : 1;
 }
 
-// One warp per row: releases the entries outside the row's kept pages. The
-// holder that takes a page's count below zero is its last one: the page keeps
-// the count -1 as its mark until collect_kernel has pushed it.
-__global__ void __launch_bounds__(kShrinkWarps * 32) release_kernel(const PageParams p) {
-  const int r = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
-  if (r >= p.num_seqs) return;
-  const int S = p.seq_lens[r];
-  if (S < 0 || S > p.max_pages * kPage) {
-    if (lane == 0) atomicOr(p.status, kStatusBadLengths);
-    return;
-  }
-  const int end = (S + kPage - 1) / kPage;
-  const int begin = p.window > 0 && S >= p.window ? (S - p.window + 1) / kPage : 0;
-  const int seg = segment_pages(p.num_pages);
+// Blocks (row, y): releases the entries y * kReleaseSpan .. of the row that lie
+// outside its kept pages, kReleasePer a thread with their loads and counts in
+// flight together. The holder that takes a page's count below zero is its
+// last one: the page keeps the count -1 as its mark until collect_kernel has
+// pushed it.
+__global__ void __launch_bounds__(kReleaseThreads) release_kernel(const PageParams p) {
+  const int r = blockIdx.x;
   int32_t* row = p.block_table + (size_t)r * p.max_pages;
-  for (int j = lane; j < p.max_pages; j += 32) {
-    if (j >= begin && j < end) continue;
-    const int e = row[j];
-    if (e < 0) continue;
-    row[j] = -1;
-    if (e >= p.num_pages) {
-      atomicOr(p.status, kStatusBadPage);
-      continue;
+  for (int j0 = blockIdx.y * kReleaseSpan + threadIdx.x; j0 < p.max_pages; j0 += gridDim.y * kReleaseSpan) {
+    int e[kReleasePer], old[kReleasePer];
+#pragma unroll
+    for (int i = 0; i < kReleasePer; ++i) {
+      const int j = j0 + i * kReleaseThreads;
+      e[i] = j < p.max_pages ? row[j] : -1;
     }
-    const int old = atomicSub(p.refs + e, 1);
-    if (old == 0) {
-      atomicAdd(p.scratch + e / seg, 1);
-    } else if (old < 0) {  // released more often than held
-      atomicAdd(p.refs + e, 1);
-      atomicOr(p.status, kStatusBadPage);
+    const int S = p.seq_lens[r];
+    if (S < 0 || S > p.max_pages * kPage) {
+      if (j0 == 0) atomicOr(p.status, kStatusBadLengths);
+      return;
+    }
+    const int end = (S + kPage - 1) / kPage;
+    const int begin = p.window > 0 && S >= p.window ? (S - p.window + 1) / kPage : 0;
+    const int seg = segment_pages(p.num_pages);
+#pragma unroll
+    for (int i = 0; i < kReleasePer; ++i) {
+      const int j = j0 + i * kReleaseThreads;
+      old[i] = 1;
+      if (e[i] < 0 || (j >= begin && j < end)) continue;
+      row[j] = -1;
+      if (e[i] >= p.num_pages)
+        atomicOr(p.status, kStatusBadPage);
+      else
+        old[i] = atomicSub(p.refs + e[i], 1);
+    }
+#pragma unroll
+    for (int i = 0; i < kReleasePer; ++i) {
+      if (old[i] == 0) {
+        atomicAdd(p.scratch + e[i] / seg, 1);
+      } else if (old[i] < 0) {  // released more often than held
+        atomicAdd(p.refs + e[i], 1);
+        atomicOr(p.status, kStatusBadPage);
+      }
     }
   }
 }
@@ -153,12 +172,10 @@ __global__ void __launch_bounds__(kCollectThreads) collect_kernel(const PagePara
   __shared__ int s_warp[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int count = __ldcg(p.free_count);
-  int base = max(count, 0), total = 0;
-  for (int i = 0; i < kPageSegments; ++i) {
-    const int n = __ldcg(p.scratch + i);
-    base += i < (int)blockIdx.x ? n : 0;
-    total += n;
-  }
+  const int n0 = __ldcg(p.scratch + lane), n1 = lane + 32 < kPageSegments ? __ldcg(p.scratch + lane + 32) : 0;
+  const int total = __reduce_add_sync(0xffffffffu, n0 + n1);
+  int base = max(count, 0) + __reduce_add_sync(0xffffffffu, (lane < (int)blockIdx.x ? n0 : 0) +
+                                                                (lane + 32 < (int)blockIdx.x ? n1 : 0));
   const int seg = segment_pages(p.num_pages);
   const int begin = min((int64_t)blockIdx.x * seg, (int64_t)p.num_pages);
   const int end = min((int64_t)begin + seg, (int64_t)p.num_pages);
@@ -197,10 +214,9 @@ __global__ void __launch_bounds__(kCollectThreads) collect_kernel(const PagePara
       __syncthreads();
     }
   }
-  if (last_block(p.scratch + kScratchShrinkTicket, gridDim.x) && threadIdx.x == 0) {
-    *p.free_count = min(max(count, 0) + total, p.num_pages);
-    for (int i = 0; i < kPageSegments; ++i) p.scratch[i] = 0;
-    p.scratch[kScratchShrinkTicket] = 0;
+  if (last_block(p.scratch + kScratchShrinkTicket, gridDim.x) && threadIdx.x <= kPageSegments) {
+    if (threadIdx.x == 0) *p.free_count = min(max(count, 0) + total, p.num_pages);
+    p.scratch[threadIdx.x] = 0;  // the segments' counts and the ticket after them
   }
 }
 
@@ -299,7 +315,8 @@ cudaError_t launch_fork(const PageParams& p, cudaStream_t stream) {
 }
 
 cudaError_t launch_shrink(const PageParams& p, cudaStream_t stream) {
-  release_kernel<<<(p.num_seqs + kShrinkWarps - 1) / kShrinkWarps, kShrinkWarps * 32, 0, stream>>>(p);
+  const dim3 grid(p.num_seqs, min((p.max_pages + kReleaseSpan - 1) / kReleaseSpan, 65535));
+  release_kernel<<<grid, kReleaseThreads, 0, stream>>>(p);
   const cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   collect_kernel<<<kPageSegments, kCollectThreads, 0, stream>>>(p);

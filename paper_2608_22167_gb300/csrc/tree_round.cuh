@@ -60,7 +60,9 @@ cudaError_t launch_compact(const CompactParams& p, const PoolPtrs& pools, cudaSt
 // words of page_scratch: pages returned per segment of page_refs, then tickets
 constexpr int kPageSegments = 48;
 constexpr int kScratchShrinkTicket = 48, kScratchForkTicket = 49, kScratchForkPages = 50;
-static_assert(kScratchForkPages < MCPU_PAGE_SCRATCH, "scratch words");
+static_assert(kScratchShrinkTicket == kPageSegments && kPageSegments > 32 && kPageSegments <= 64 &&
+                  kScratchForkPages < MCPU_PAGE_SCRATCH,
+              "collect_kernel reads two counts a lane and clears the ticket with them");
 
 struct PageParams {
   int32_t *block_table, *seq_lens;
