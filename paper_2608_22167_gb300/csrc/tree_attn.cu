@@ -47,8 +47,9 @@ constexpr int kQBytes = kTileRows * kRowBytes;
 constexpr int kLaneBytes = kQBytes + (kKStages + kVStages) * kBlockBytes;
 constexpr int kTreeThreads = 384;
 constexpr uint32_t kTmemCols = 512;
-constexpr int kCostItem = 3;  // a tile's set-up and end, in blocks
-constexpr int kMinQuota = 5;  // smallest piece worth a lane of its own
+constexpr int kCostItem = 5;  // a tile's set-up and end, in blocks
+constexpr int kWholeBlocks = 6;  // tiles of up to so many blocks are never cut
+constexpr int kMinQuota = 7;  // smallest piece worth a lane of its own
 constexpr float kRescale = 8.f;  // log2 units: P may reach 2^8 before O is rescaled
 
 struct Part {  // a run of key blocks of one tile
@@ -123,8 +124,11 @@ __device__ __forceinline__ bool row_geom(const TreeParams& p, int r, RowGeom* w,
   return true;
 }
 
-// Blocks of a tile of nb blocks that lie before x units of it.
+// Blocks of a tile of nb blocks that belong to the pieces ending x units into
+// it. A short tile is not cut (its parts would each pay for a set-up, and for
+// the merge): all of it belongs to the piece it begins in.
 __device__ __forceinline__ int blocks_before(int64_t x, int nb) {
+  if (nb <= kWholeBlocks) return x <= 0 ? 0 : nb;
   return x <= kCostItem ? 0 : x >= kCostItem + nb ? nb : (int)(x - kCostItem);
 }
 
@@ -281,16 +285,6 @@ __device__ __forceinline__ bool block_masks(const TreeParams& p, const Part& a, 
   return dead;
 }
 
-// 16 columns of TMEM, for the short loops that end a part
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
-      "%15}, [%16];"
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-      : "r"(taddr));
-}
-
 __device__ __forceinline__ float tree_sink(const TreeParams& p, int h) {
   return p.sinks ? p.sinks[h] * 1.4426950408889634f : -INFINITY;
 }
@@ -310,6 +304,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   auto bar = [&](uint64_t& b) { return smem_addr(&b); };
   const int B = p.num_seqs, g = p.group, Hkv = p.num_kv_heads, Hq = p.num_q_heads;
 
+  // The merge may be launched from now on (its blocks find no room until this
+  // grid's CTAs leave, and wait for its end); nothing is read before the grid
+  // that this one follows has ended.
+  grid_dep_launch();
+  grid_dep_wait();
   // no cut tile begins in this CTA's pieces, as far as is known
   if (threadIdx.x < 4)
     p.cuts[(threadIdx.x >> 1) * 2 * gridDim.x + 2 * blockIdx.x + (threadIdx.x & 1)] = make_int4(-1, 0, 0, 0);
@@ -809,29 +808,31 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         const bool writes = tok < a.n_tok;
         const int part_slot = a.slot, h = a.kvh * g + head;
         const float sink = ln.meta[slot].sinks[head];
-        float inv = l > 0.f ? 1.f / l : 0.f;
+        float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;  // l < 2^8 keys: within its range, 2 ulp
         float lse2 = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
         if (part_slot < 0 && sink > -INFINITY) inv = finish_with_sink(m_ref, l, sink, &lse2);
         const size_t orow = (size_t)(a.token + tok) * Hq + h;
         const size_t prow = (size_t)max(part_slot, 0) * kTileRows + row;
 #pragma unroll 1
-        for (int c = 0; c < kHeadDim / 16; ++c) {
+        for (int c = 0; c < kHeadDim / 32; ++c) {
           __syncwarp();  // TMEM moves need the warp in step
-          uint32_t ov[16];
-          tmem_ld16(cO + 16 * c, ov);
+          uint32_t ov[32];
+          tmem_ld32(cO + 32 * c, ov);
           tmem_ld_wait();
           if (writes && part_slot < 0) {
-            uint32_t o[8];
+            uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kHeadDim) + 4 * c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t o[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                o[e] = pack_bf16x2(__uint_as_float(ov[8 * k + 2 * e]) * inv, __uint_as_float(ov[8 * k + 2 * e + 1]) * inv);
+              dst[k] = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+          } else if (writes) {
+            float4* dst = reinterpret_cast<float4*>(p.o_part + prow * kHeadDim) + 8 * c;
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-              o[k] = pack_bf16x2(__uint_as_float(ov[2 * k]) * inv, __uint_as_float(ov[2 * k + 1]) * inv);
-            uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kHeadDim) + 2 * c;
-            dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-            dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
-          } else if (writes) {
-            float4* dst = reinterpret_cast<float4*>(p.o_part + prow * kHeadDim) + 4 * c;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
               dst[k] = make_float4(__uint_as_float(ov[4 * k]) * inv, __uint_as_float(ov[4 * k + 1]) * inv,
                                    __uint_as_float(ov[4 * k + 2]) * inv, __uint_as_float(ov[4 * k + 3]) * inv);
           }
@@ -926,8 +927,8 @@ __global__ void __launch_bounds__(kMergeThreads) merge_tree_kernel(const TreePar
 cudaError_t launch_tree(const CUtensorMap& kmap, const CUtensorMap& vmap, const CUtensorMap& qmap,
                         const TreeParams& p, int sms, cudaStream_t stream) {
   const int grid = sms < kTreeMaxCtas ? sms : kTreeMaxCtas;
-  tree_kernel<<<grid, kTreeThreads, tree_smem_bytes(), stream>>>(kmap, vmap, qmap, p);
-  cudaError_t e = cudaGetLastError();
+  LaunchCfg tc(dim3(grid), dim3(kTreeThreads), tree_smem_bytes(), stream, true);
+  const cudaError_t e = cudaLaunchKernelEx(&tc.cfg, tree_kernel, kmap, vmap, qmap, p);
   if (e != cudaSuccess) return e;
   LaunchCfg lc(dim3(4 * grid, kTileRows / kMergeRows), dim3(kMergeThreads), 0, stream, true);
   return cudaLaunchKernelEx(&lc.cfg, merge_tree_kernel, p, grid);
