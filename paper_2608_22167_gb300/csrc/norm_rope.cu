@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kNormThreads = 256;
 constexpr int kNormWarps = kNormThreads / 32;
-constexpr int kRowBatch = 4;  // head rows (of 4 per warp) whose loads are in flight together
+constexpr int kRowBatch = 5;  // head rows (of 4 per warp) whose loads are in flight together
 
 // The row r with qsl[r] <= t < qsl[r + 1] of a non-decreasing qsl, by 32-way
 // search over the whole warp (any row if there is none: the caller checks).
@@ -36,6 +36,18 @@ __device__ __forceinline__ int find_row(const int32_t* qsl, int num_seqs, int t,
     n = min(step, n - k);
   }
   return lo;
+}
+
+// Four floats at a 4-byte aligned address, in one load where `vec` says that
+// it is 16-byte aligned.
+__device__ __forceinline__ void load4(const float* p, bool vec, float* out) {
+  if (vec) {
+    const float4 v = __ldg(reinterpret_cast<const float4*>(p));
+    out[0] = v.x, out[1] = v.y, out[2] = v.z, out[3] = v.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = __ldg(p + e);
+  }
 }
 
 __device__ __forceinline__ float2 unpack2(uint32_t v) {
@@ -74,22 +86,18 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
     if (lane == 0) atomicOr(p.status, kStatusBadLengths);
     return;
   }
+  const bool vec = ((reinterpret_cast<uintptr_t>(p.wq) | reinterpret_cast<uintptr_t>(p.wk) |
+                     reinterpret_cast<uintptr_t>(p.cos_sin)) & 15) == 0;
   float w[8];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    w[e] = __ldg(p.wq + 4 * j + e);
-    w[4 + e] = __ldg(p.wq + 32 + 4 * j + e);
-  }
+  load4(p.wq + 4 * j, vec, w);
+  load4(p.wq + 32 + 4 * j, vec, w + 4);
   // the angles come by a given position, or by the slot once the row is known
   int pos = p.positions ? __ldg(p.positions + t) : -1;
   float c[4], s[4];
   auto load_angles = [&]() {
     const float* ang = p.cos_sin + (size_t)pos * kHeadDim + 4 * j;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {  // scalar loads: the table is 4-byte aligned
-      c[e] = __ldg(ang + e);
-      s[e] = __ldg(ang + 32 + e);
-    }
+    load4(ang, vec, c);
+    load4(ang + 32, vec, s);
   };
   if (pos >= 0 && pos < p.max_position) load_angles();
   const int r = find_row(p.qsl, p.num_seqs, t, lane);
@@ -118,14 +126,12 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
       for (int e = 0; e < 4; ++e) ss = fmaf(a[e], a[e], fmaf(d[e], d[e], ss));
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      if (row >= Hq)  // from here on: k (the rows of v ignore it)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          w[e] = __ldg(p.wk + 4 * j + e);
-          w[4 + e] = __ldg(p.wk + 32 + 4 * j + e);
-        }
+      if (row >= Hq) {  // from here on: k (the rows of v ignore it)
+        load4(p.wk + 4 * j, vec, w);
+        load4(p.wk + 32 + 4 * j, vec, w + 4);
+      }
       const float mean = ss * (1.f / kHeadDim) + p.eps;
-      const float inv = mean > 0.f ? 1.f / sqrtf(mean) : 0.f;
+      const float inv = mean > 0.f ? rsqrtf(mean) : 0.f;  // 2 ulp
       if (row < Hq + Hkv) {
         float y[8];
 #pragma unroll
@@ -154,8 +160,8 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
 }  // namespace
 
 cudaError_t launch_norm_rope(const NormRopeParams& p, int sms, cudaStream_t stream) {
-  // warps per token: a warp each once that makes several waves of blocks, else
-  // as many as keep the SMs full
+  // warps per token: one once that fills the SMs' warps about twice over, else
+  // as many as fill them
   if (p.total_q > 16 * sms)
     norm_rope_kernel<1><<<(p.total_q + 7) / 8, kNormThreads, 0, stream>>>(p);
   else if (p.total_q > 4 * sms)

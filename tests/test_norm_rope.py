@@ -96,6 +96,45 @@ def test_matches_the_formula(hq, hkv, packed, positions):
 
 
 @gpu
+@pytest.mark.parametrize("packed", [True, False])
+@pytest.mark.parametrize("hq,hkv", [(64, 8), (8, 2), (32, 8), (1, 1), (5, 5), (96, 12), (128, 64)])
+def test_many_tokens(hq, hkv, packed):
+    # enough tokens for every form of the kernel on any SM count of this GPU, odd totals, empty rows
+    rng = np.random.default_rng(hq + 1)
+    tab = torch.from_numpy(W.rope_table(5000)).cuda()
+    wq, wk = 1 + 0.3 * rng.standard_normal(64), 1 + 0.3 * rng.standard_normal(64)
+    for total in (700, 2431, 2433, 4999):
+        lens = rng.multinomial(total, np.ones(37) / 37)
+        lens[5] += lens[6]
+        lens[6] = 0
+        c = _case(rng.integers(0, 200, 37), lens, hq, hkv, total, packed, total % 2 == 0, gap=16)
+        _compare(c, _call(c, wq, wk, 1e-6, tab), wq, wk, 1e-6, tab)
+
+
+@gpu
+def test_many_tokens_with_errors():
+    from paper_2608_22167_gb300 import mcpu
+
+    tab = torch.from_numpy(W.rope_table(900)).cuda()
+    w = np.ones(64)
+    c = _case([0, 500, 30], [3000, 700, 900], 8, 2, 9, True, False)  # positions from 900 on lie past the table
+    c["dbt"][2, 3] = -1  # tokens at slots 48 .. 63 of row 2 have no page
+    out = _call(c, w, w, 1e-6, tab).float().cpu()
+    bad = torch.zeros(4600, dtype=torch.bool)
+    bad[900:3000] = True
+    bad[3400:3700] = True
+    bad[4570:] = True
+    assert torch.isnan(out[bad]).all() and torch.isfinite(out[~bad]).all()
+    assert int(c["status"].item()) == mcpu.STATUS_BAD_LENGTHS | mcpu.STATUS_BAD_PAGE
+    slot = np.where((c["row"] == 2) & (c["slot"] // 16 == 3), -1, c["slot"])
+    keep = (slot >= 0) & ~bad.numpy()
+    page = c["bt"][c["row"], c["slot"] // 16]
+    vc = c["vc"].double().cpu().numpy()
+    assert np.array_equal(vc[page[keep], :, c["slot"][keep] % 16], c["vals"][2][keep])
+    assert np.all(vc[page[~keep], :, c["slot"][~keep] % 16] == 7)
+
+
+@gpu
 @pytest.mark.parametrize("size", [1e-8, 1e-3, 1e8])
 def test_small_and_large_values(size):
     tab = torch.from_numpy(W.rope_table(600)).cuda()
@@ -103,6 +142,17 @@ def test_small_and_large_values(size):
     for eps in (0.0, 1e-6):
         c = _case([3, 500], [10, 1], 16, 2, 2, True, False, size=size)
         _compare(c, _call(c, w, w, eps, tab), w, w, eps, tab)
+
+
+@gpu
+def test_tables_and_weights_at_any_float():
+    big = torch.zeros(600 * 64 + 1, device="cuda")
+    big[1:] = torch.from_numpy(W.rope_table(600)).cuda().flatten()
+    tab = big[1:].view(600, 64)  # 4-byte aligned only
+    assert tab.data_ptr() % 16 == 4
+    w = np.linspace(-2, 2, 64)
+    c = _case([3, 500], [10, 1], 16, 2, 2, True, False)
+    _compare(c, _call(c, w, w, 1e-6, tab), w, w, 1e-6, tab)
 
 
 @gpu
