@@ -60,6 +60,8 @@ __device__ __forceinline__ float2 unpack2(uint32_t v) {
 // looked up.
 template <int kSplit>
 __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRopeParams p) {
+  grid_dep_launch();  // the next grid's blocks may be placed as this one's leave (they wait for its end)
+  grid_dep_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane >> 3, j = lane & 7;
   const int t = blockIdx.x * (kNormWarps / kSplit) + warp / kSplit;
   if (t >= p.total_q) return;
@@ -162,13 +164,9 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
 cudaError_t launch_norm_rope(const NormRopeParams& p, int sms, cudaStream_t stream) {
   // warps per token: one once that fills the SMs' warps about twice over, else
   // as many as fill them
-  if (p.total_q > 16 * sms)
-    norm_rope_kernel<1><<<(p.total_q + 7) / 8, kNormThreads, 0, stream>>>(p);
-  else if (p.total_q > 4 * sms)
-    norm_rope_kernel<4><<<(p.total_q + 1) / 2, kNormThreads, 0, stream>>>(p);
-  else
-    norm_rope_kernel<8><<<p.total_q, kNormThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  const int split = p.total_q > 16 * sms ? 1 : p.total_q > 4 * sms ? 4 : kNormWarps;
+  LaunchCfg lc(dim3((p.total_q + kNormWarps / split - 1) / (kNormWarps / split)), dim3(kNormThreads), 0, stream, true);
+  return cudaLaunchKernelEx(&lc.cfg, split == 1 ? norm_rope_kernel<1> : split == 4 ? norm_rope_kernel<4> : norm_rope_kernel<8>, p);
 }
 
 }  // namespace mcpu

@@ -4,6 +4,11 @@
 // mcpu_compact_kv). Integer bookkeeping and bit copies; every result is the
 // same on every run: pages return to the stack in ascending order and are
 // popped in the order of the forks, whatever order the blocks ran in.
+//
+// Every kernel is launched programmatically: its blocks may be placed while the
+// grid before it still runs, and wait for that grid's end before they read or
+// write anything (begin()). These calls are short and come in rows, so the
+// launches would otherwise be a good part of their time.
 #include "tree_round.cuh"
 
 namespace mcpu {
@@ -15,6 +20,17 @@ constexpr int kReleaseThreads = 128, kReleasePer = 4, kReleaseSpan = kReleaseThr
 constexpr int kCollectThreads = 1024, kCollectPer = 4;
 constexpr int kCopyThreads = 256;
 constexpr int kCompactThreads = 256, kCompactMoves = 128, kCompactPools = 4, kCompactBatch = 8;
+
+__device__ __forceinline__ void begin() {
+  grid_dep_launch();
+  grid_dep_wait();
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch(void (*kernel)(KArgs...), dim3 grid, int threads, cudaStream_t stream, const Args&... args) {
+  LaunchCfg lc(grid, dim3(threads), 0, stream, true);
+  return cudaLaunchKernelEx(&lc.cfg, kernel, args...);
+}
 
 // Last block to arrive at `ticket` (of n): everything the other blocks did
 // before is visible to it. Call with the whole block.
@@ -40,8 +56,10 @@ __device__ __forceinline__ bool fork_valid(const PageParams& p, int f, int* len)
 // (counted over the forks before it) says which page of the stack it takes;
 // the last block to finish lowers free_count.
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(const PageParams p) {
+  begin();
   const int f = blockIdx.x;
-  __shared__ int s_page;
+  __shared__ int s_page, s_rank;
+  if (threadIdx.x == 0) s_rank = 0;
   int S = 0;
   const bool ok = fork_valid(p, f, &S);
   const bool partial = ok && S % kPage != 0;
@@ -53,15 +71,19 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const PageParams p) 
     const int j = threadIdx.x + i * kForkThreads;
     early[i] = ok && j < S / kPage ? p.block_table[(size_t)__ldg(p.src_rows + f) * p.max_pages + j] : -1;
   }
-  int rank = 0;
-  if (partial) {  // uniform over the block
-    for (int e0 = 0; e0 < f; e0 += kForkThreads) {
-      const int e = e0 + threadIdx.x;
+  int before = 0;
+  if (partial) {
+#pragma unroll 4
+    for (int e = threadIdx.x; e < f; e += kForkThreads) {
       int len = 0;
-      const bool has = e < f && fork_valid(p, e, &len) && len % kPage != 0;
-      rank += __syncthreads_count(has);
+      if (fork_valid(p, e, &len) && len % kPage != 0) ++before;
     }
   }
+  __syncthreads();
+  before = __reduce_add_sync(0xffffffffu, before);
+  if (threadIdx.x % 32 == 0 && before > 0) atomicAdd(&s_rank, before);
+  __syncthreads();
+  const int rank = s_rank;
   if (ok) {
     const int src = __ldg(p.src_rows + f), dst = __ldg(p.dst_rows + f);
     const int full = S / kPage;
@@ -126,6 +148,7 @@ __host__ __device__ inline int segment_pages(int num_pages) {
 // last one: the page keeps the count -1 as its mark until collect_kernel has
 // pushed it.
 __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const PageParams p) {
+  begin();
   const int r = blockIdx.x;
   int32_t* row = p.block_table + (size_t)r * p.max_pages;
   for (int j0 = blockIdx.y * kReleaseSpan + threadIdx.x; j0 < p.max_pages; j0 += gridDim.y * kReleaseSpan) {
@@ -169,6 +192,7 @@ __global__ void __launch_bounds__(kReleaseThreads) release_kernel(const PagePara
 // Block b pushes the marked pages of segment b, after those of the segments
 // before it, and clears their marks.
 __global__ void __launch_bounds__(kCollectThreads) collect_kernel(const PageParams p) {
+  begin();
   __shared__ int s_warp[32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int count = __ldcg(p.free_count);
@@ -225,6 +249,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const PoolPtrs
                                                                   int64_t page_bytes, int32_t num_pages,
                                                                   const int32_t* copy_src, const int32_t* copy_dst,
                                                                   int32_t* status) {
+  begin();
   const int f = blockIdx.x / num_pools, pool = blockIdx.x % num_pools;
   const int src = __ldg(copy_src + f), dst = __ldg(copy_dst + f);
   if (src < 0 || dst < 0 || src == dst) return;
@@ -252,6 +277,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const PoolPtrs
 // the destinations written so far (node numbers increase and are at least
 // their rank), so no move overwrites what a later one reads.
 __global__ void __launch_bounds__(kCompactThreads) compact_kernel(const CompactParams p, const PoolPtrs pools) {
+  begin();
   const int r = blockIdx.x;
   __shared__ int s_src[kCompactMoves], s_dst[kCompactMoves];  // page * 16 + slot
   const int q0 = __ldg(p.qsl + r), q1 = __ldg(p.qsl + r + 1);
@@ -310,31 +336,26 @@ __global__ void __launch_bounds__(kCompactThreads) compact_kernel(const CompactP
 }  // namespace
 
 cudaError_t launch_fork(const PageParams& p, cudaStream_t stream) {
-  fork_kernel<<<p.num_forks, kForkThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  return launch(fork_kernel, dim3(p.num_forks), kForkThreads, stream, p);
 }
 
 cudaError_t launch_shrink(const PageParams& p, cudaStream_t stream) {
   const dim3 grid(p.num_seqs, min((p.max_pages + kReleaseSpan - 1) / kReleaseSpan, 65535));
-  release_kernel<<<grid, kReleaseThreads, 0, stream>>>(p);
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = launch(release_kernel, grid, kReleaseThreads, stream, p);
   if (e != cudaSuccess) return e;
-  collect_kernel<<<kPageSegments, kCollectThreads, 0, stream>>>(p);
-  return cudaGetLastError();
+  return launch(collect_kernel, dim3(kPageSegments), kCollectThreads, stream, p);
 }
 
 cudaError_t launch_copy_pages(const PoolPtrs& pools, int32_t num_pools, int64_t page_bytes, int32_t num_pages,
                               const int32_t* copy_src, const int32_t* copy_dst, int32_t num_copies, int32_t* status,
                               cudaStream_t stream) {
-  copy_pages_kernel<<<num_copies * num_pools, kCopyThreads, 0, stream>>>(pools, num_pools, page_bytes, num_pages,
-                                                                        copy_src, copy_dst, status);
-  return cudaGetLastError();
+  return launch(copy_pages_kernel, dim3(num_copies * num_pools), kCopyThreads, stream, pools, num_pools, page_bytes,
+                num_pages, copy_src, copy_dst, status);
 }
 
 cudaError_t launch_compact(const CompactParams& p, const PoolPtrs& pools, cudaStream_t stream) {
   const int groups = (p.num_pools + kCompactPools - 1) / kCompactPools;
-  compact_kernel<<<dim3(p.num_seqs, groups > 0 ? groups : 1), kCompactThreads, 0, stream>>>(p, pools);
-  return cudaGetLastError();
+  return launch(compact_kernel, dim3(p.num_seqs, groups > 0 ? groups : 1), kCompactThreads, stream, p, pools);
 }
 
 }  // namespace mcpu
