@@ -588,11 +588,13 @@ def mcpu_tree_workspace_size(d: Dims) -> int:
 
 
 def new_tree_workspace(d: Dims, device="cuda") -> torch.Tensor:
-    """A zeroed workspace of the size mcpu_tree_workspace_size(d) asks for."""
+    """A workspace of the size mcpu_tree_workspace_size(d) asks for, its status word cleared."""
     n = mcpu_tree_workspace_size(d)
     if n == 0:
         raise McpuError(1, "mcpu_tree_workspace_size")
-    return torch.zeros(n, dtype=torch.uint8, device=device)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
 
 
 def mcpu_tree_attention_forward(q, k_cache, v_cache, block_table, seq_lens, query_start_loc, tree_mask, positions,

@@ -50,6 +50,26 @@ def test_tree_sizes(n):
 
 
 @gpu
+@pytest.mark.parametrize("seed", range(12))
+def test_random_batches(seed):
+    rng = np.random.default_rng(900 + seed)
+    hkv = int(rng.choice([1, 2, 3, 8]))
+    hq = hkv * int(rng.choice([1, 2, 4, 8]))
+    rows = int(rng.integers(1, 12))
+    ctx = np.where(rng.random(rows) < 0.3, rng.integers(0, 3000, rows), rng.integers(0, 200, rows))
+    lens = np.where(rng.random(rows) < 0.2, rng.integers(0, 257, rows), rng.integers(0, 40, rows))
+    lens[0] = max(1, lens[0])
+    b = TreeBatch(ctx, lens, hq, hkv, seed, window=int(rng.choice([0, 0, 5, 64, 500])))
+    _check(b, sinks=rng.standard_normal(hq) if seed % 2 else None)
+
+
+@gpu
+def test_one_head_a_group_and_the_longest_tree():
+    _check(TreeBatch([0, 77, 1500], [256, 255, 129], 2, 2, 13))
+    _check(TreeBatch([900, 77], [256, 200], 8, 1, 14, window=100))
+
+
+@gpu
 @pytest.mark.parametrize("hq,hkv", [(64, 8), (8, 2), (2, 2)])
 def test_sinks(hq, hkv):
     rng = np.random.default_rng(3)

@@ -206,3 +206,50 @@ def test_a_captured_round_replays():
         for a, b in zip(state(), want_state):
             assert torch.equal(a, b)
     assert mcpu.mcpu_read_device_status(cache.workspace) == (0, 0)
+
+
+@gpu
+def test_pages_far_into_large_pools():
+    # byte offsets past 32 bits: 20000 pages of 128 kv heads are 5.2 GB a pool
+    from paper_2608_22167_gb300 import mcpu
+
+    hkv, pages = 128, 20000
+    pools = [torch.empty(pages, hkv, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    bt, sl, qsl = i32([[19999, 3, 19500, 19001]]), i32([50]), i32([0, 20])
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    randn = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=torch.bfloat16)  # noqa: E731
+    for p in pools:
+        p[bt[0].long()] = randn(4, hkv, 16, 64)
+    q, k, v = randn(20, hkv, 64), randn(20, hkv, 64), randn(20, hkv, 64)
+    w, tab, status = torch.ones(64, device="cuda"), torch.zeros(64, 64, device="cuda"), i32([0])
+    tab[:, :32] = 1  # no rotation
+    q_out = torch.empty_like(q)
+    mcpu.mcpu_norm_rope_kv_append(q, k, v, w, w, 0.0, None, tab, q_out, *pools, bt, sl, qsl, status)
+    slot = torch.arange(30, 50, device="cuda")
+    assert torch.equal(pools[1][bt[0, slot // 16].long(), :, slot % 16], v)
+    norm = lambda x: x.double() / x.double().square().mean(-1, keepdim=True).sqrt()  # noqa: E731
+    assert (pools[0][bt[0, slot // 16].long(), :, slot % 16].double() - norm(k)).abs().max() <= 2.0 ** -6
+    ws = mcpu.new_tree_workspace(mcpu.dims(q, pools[0], bt, sl))
+    out, lse = torch.empty_like(q), torch.empty(20, hkv, device="cuda")
+    mask = i32([[(1 << i + 1) - 1] for i in range(20)])
+    mcpu.mcpu_tree_attention_forward(q_out, *pools, bt, sl, qsl, mask, None, 0, 0.125, out, lse, ws)
+    pos = torch.arange(50, device="cuda")
+    kk, vv = (p[bt[0, pos // 16].long(), :, pos % 16].double() for p in pools)
+    x = torch.einsum("thd,jhd->thj", q_out.double(), kk) * 0.125
+    x = x.masked_fill(pos[None, None] > (30 + torch.arange(20, device="cuda"))[:, None, None], -torch.inf)
+    ref = torch.einsum("thj,jhd->thd", x.softmax(-1), vv)
+    mag = torch.einsum("thj,jhd->thd", x.softmax(-1), vv.abs())
+    assert ((out.double() - ref).abs() <= 1.01 * 2.0 ** -8 * (mag + ref.abs()) + 1e-6).all()
+    assert (lse.double() - x.logsumexp(-1)).abs().max() <= 1e-4
+    lst = mcpu.PoolList(pools)
+    new = i32([0])
+    mcpu.mcpu_compact_kv(lst, bt, sl, qsl, i32([[1, 18, 19]]), i32([3]), new, status)
+    kept = torch.tensor([31, 48, 49], device="cuda")
+    slot = torch.arange(30, 33, device="cuda")
+    assert torch.equal(pools[1][bt[0, slot // 16].long(), :, slot % 16], vv[kept].to(torch.bfloat16))
+    mcpu.mcpu_copy_pages(lst, i32([19999, 3]), i32([5, 19998]), status)
+    for p in pools:
+        assert torch.equal(p[5], p[19999]) and torch.equal(p[19998], p[3])
+    assert int(new) == 33 and int(status) == 0 and mcpu.mcpu_read_device_status(ws) == (0, 0)
