@@ -603,13 +603,15 @@ def mcpu_tree_attention_forward(q, k_cache, v_cache, block_table, seq_lens, quer
     context (inside the window of its position) and the nodes whose bit is
     set in its tree_mask row (int32 [T, words], 32 nodes a word). positions
     (int32 [T]) may be None without a window; sinks: float32 [H_q] or None."""
-    if tree_mask.dim() != 2 or tree_mask.shape[0] != q.shape[0]:
-        raise ValueError("tree_mask must be an int32 [T, words] tensor")
+    ms = tree_mask.shape
+    if len(ms) != 2 or ms[0] != q.shape[0] or not 1 <= ms[1] <= MAX_TREE_WORDS:
+        raise ValueError(f"tree_mask must be an int32 [T, words] tensor of at most {MAX_TREE_WORDS} words "
+                         "(longer chunks are the rows of mcpu_paged_attention_forward)")
     if sinks is not None and (sinks.dtype != torch.float32 or sinks.numel() != q.shape[1] or not sinks.is_cuda):
         raise ValueError("sinks must be a float32 CUDA tensor with one value per q head")
     code = _lib.mcpu_tree_attention_forward(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
-        query_start_loc.data_ptr(), _int32(tree_mask, "tree_mask"), tree_mask.shape[1], _raw(positions), sliding_window,
+        query_start_loc.data_ptr(), _int32(tree_mask, "tree_mask"), ms[1], _raw(positions), sliding_window,
         softmax_scale, _raw(sinks), _dims(q.shape, k_cache, block_table, seq_lens), out.data_ptr(), lse.data_ptr(),
         workspace.data_ptr(),
         workspace.numel() * workspace.element_size(), _raw_stream(stream))
