@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -144,7 +145,7 @@ _lib.mcpu_paged_attention_host_fp8.argtypes = [
 ]
 _lib.mcpu_paged_attention_host_fp8.restype = ctypes.c_int
 _I32, _I64, _F32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
-_DIMS = ctypes.POINTER(Dims)
+_DIMS = ctypes.c_void_p  # an mcpu_dims as bytes (_pack_dims): cheaper to make than a Dims
 _lib.mcpu_norm_rope_kv_append.argtypes = [_P, _I64, _P, _I64, _P, _I64, _P, _P, _F32, _P, _P, _I32, _P, _P, _P, _P, _P,
                                           _P, _DIMS, _P, _P]
 _lib.mcpu_norm_rope_kv_append.restype = ctypes.c_int
@@ -517,39 +518,31 @@ def mcpu_paged_attention_host_fp8(stage, q_host, k_new_host, v_new_host, kv8, bl
 
 
 # ------------------------------------------------------- tree-drafted decoding
+# These calls are made many times a step; their wrappers avoid what costs on
+# the host: torch Stream objects, ctypes structures, repeated shape queries.
 MAX_TREE_WORDS = 8
 MAX_POOLS = 128
 MAX_FORKS = 2048
 PAGE_SCRATCH = 64
 
-
-def _raw(t):
-    return None if t is None else t.data_ptr()
+_BF16, _FP32, _INT32 = torch.bfloat16, torch.float32, torch.int32
+_pack_dims = struct.Struct("8i").pack  # the fields of Dims, in order
+_current_device = torch.cuda.current_device
+_current_stream = torch._C._cuda_getCurrentRawStream
+_norm_rope = _lib.mcpu_norm_rope_kv_append
+_tree_forward = _lib.mcpu_tree_attention_forward
+_compact_kv = _lib.mcpu_compact_kv
+_fork_tables = _lib.mcpu_fork_block_tables
+_shrink_tables = _lib.mcpu_shrink_block_tables
+_copy_pages = _lib.mcpu_copy_pages
 
 
 def _raw_stream(stream):
-    # the current device's current stream, without building a Stream object (2.9 us of a call's 16)
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-    return stream.cuda_stream
-
-
-def _token_stride(x, shape, what):
-    """Elements from one token to the next of a [T, H, D] tensor whose tokens are dense inside."""
-    s = x.stride()
-    if x.dtype != torch.bfloat16 or len(s) != 3 or s[2] != 1 or s[1] != shape[2]:
-        raise ValueError(f"{what} must be a bfloat16 [T, H, D] tensor with the heads of a token dense")
-    return s[0] if shape[0] > 1 else max(s[0], s[1] * shape[1])
-
-
-def _dims(q_shape, k_cache, block_table, seq_lens) -> Dims:
-    t, hq, d = q_shape
-    p, hkv, page, _ = k_cache.shape
-    return Dims(seq_lens.shape[0], t, block_table.shape[1], p, hq, hkv, d, page)
+    return _current_stream(_current_device()) if stream is None else stream.cuda_stream
 
 
 def _int32(x, what):
-    if x.dtype != torch.int32 or not x.is_contiguous():
+    if x.dtype is not _INT32 or not x.is_contiguous():
         raise ValueError(f"{what} must be a contiguous int32 tensor")
     return x.data_ptr()
 
@@ -560,31 +553,41 @@ def mcpu_norm_rope_kv_append(q, k_new, v_new, q_weight, k_weight, eps, positions
     positions (int32 [T], or None for the tokens' own slots), q to q_out, K
     and V to the pages. q, k_new and v_new may be slices of one projection's
     output (any token stride that is a multiple of 8 elements)."""
-    qs, ks, cs = q.shape, k_new.shape, cos_sin.shape
-    if len(qs) != 3 or len(ks) != 3 or ks != v_new.shape or ks[0] != qs[0] or ks[1] != k_cache.shape[1]:
+    q_shape, k_shape = q.shape, k_new.shape
+    t, hq, d = q_shape
+    pages, hkv, page, _ = k_cache.shape
+    max_position, table_d = cos_sin.shape
+    if k_shape != (t, hkv, d) or v_new.shape != k_shape:
         raise ValueError("q must be [T, H_q, D], k_new and v_new [T, H_kv, D]")
-    if cos_sin.dtype != torch.float32 or len(cs) != 2 or cs[1] != qs[2] or not cos_sin.is_contiguous():
+    qs, ks, vs, dense = q.stride(), k_new.stride(), v_new.stride(), (d, 1)
+    if qs[1:] != dense or ks[1:] != dense or vs[1:] != dense or \
+            not (q.dtype is _BF16 and k_new.dtype is _BF16 and v_new.dtype is _BF16):
+        raise ValueError("q, k_new and v_new must be bfloat16 with the heads of a token dense")
+    if cos_sin.dtype is not _FP32 or table_d != d or not cos_sin.is_contiguous():
         raise ValueError("cos_sin must be a contiguous float32 [max_position, head_dim] tensor")
-    for w in (q_weight, k_weight):
-        if w.dtype != torch.float32 or w.numel() != qs[2] or not w.is_contiguous():
-            raise ValueError("q_weight and k_weight must be contiguous float32 [head_dim] tensors")
-    if q_out.dtype != torch.bfloat16 or q_out.shape != qs or not q_out.is_contiguous():
+    if q_weight.shape != (d,) or k_weight.shape != (d,) or q_weight.dtype is not _FP32 or \
+            k_weight.dtype is not _FP32 or not q_weight.is_contiguous() or not k_weight.is_contiguous():
+        raise ValueError("q_weight and k_weight must be contiguous float32 [head_dim] tensors")
+    if q_out.dtype is not _BF16 or q_out.shape != q_shape or not q_out.is_contiguous():
         raise ValueError("q_out must be a contiguous bfloat16 tensor of q's shape")
-    if positions is not None and positions.numel() != qs[0]:
-        raise ValueError("positions must have one entry per query token")
-    code = _lib.mcpu_norm_rope_kv_append(
-        q.data_ptr(), _token_stride(q, qs, "q"), k_new.data_ptr(), _token_stride(k_new, ks, "k_new"), v_new.data_ptr(),
-        _token_stride(v_new, ks, "v_new"), q_weight.data_ptr(), k_weight.data_ptr(), eps,
-        None if positions is None else _int32(positions, "positions"), cos_sin.data_ptr(), cs[0], q_out.data_ptr(),
-        k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
-        query_start_loc.data_ptr(), _dims(qs, k_cache, block_table, seq_lens), status_word.data_ptr(),
+    if positions is not None:
+        if positions.shape != (t,):
+            raise ValueError("positions must have one entry per query token")
+        positions = _int32(positions, "positions")
+    kv = hkv * d  # a lone token's stride says nothing
+    code = _norm_rope(
+        q.data_ptr(), qs[0] if t > 1 else hq * d, k_new.data_ptr(), ks[0] if t > 1 else kv, v_new.data_ptr(),
+        vs[0] if t > 1 else kv, q_weight.data_ptr(), k_weight.data_ptr(), eps, positions, cos_sin.data_ptr(),
+        max_position, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(),
+        seq_lens.data_ptr(), query_start_loc.data_ptr(),
+        _pack_dims(seq_lens.shape[0], t, block_table.shape[1], pages, hq, hkv, d, page), status_word.data_ptr(),
         _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_norm_rope_kv_append")
 
 
 def mcpu_tree_workspace_size(d: Dims) -> int:
-    return int(_lib.mcpu_tree_workspace_size(d))
+    return int(_lib.mcpu_tree_workspace_size(ctypes.byref(d)))
 
 
 def new_tree_workspace(d: Dims, device="cuda") -> torch.Tensor:
@@ -603,18 +606,25 @@ def mcpu_tree_attention_forward(q, k_cache, v_cache, block_table, seq_lens, quer
     context (inside the window of its position) and the nodes whose bit is
     set in its tree_mask row (int32 [T, words], 32 nodes a word). positions
     (int32 [T]) may be None without a window; sinks: float32 [H_q] or None."""
-    ms = tree_mask.shape
-    if len(ms) != 2 or ms[0] != q.shape[0] or not 1 <= ms[1] <= MAX_TREE_WORDS:
+    t, hq, d = q.shape
+    pages, hkv, page, _ = k_cache.shape
+    nodes, words = tree_mask.shape
+    if nodes != t or not 1 <= words <= MAX_TREE_WORDS:
         raise ValueError(f"tree_mask must be an int32 [T, words] tensor of at most {MAX_TREE_WORDS} words "
                          "(longer chunks are the rows of mcpu_paged_attention_forward)")
-    if sinks is not None and (sinks.dtype != torch.float32 or sinks.numel() != q.shape[1] or not sinks.is_cuda):
-        raise ValueError("sinks must be a float32 CUDA tensor with one value per q head")
-    code = _lib.mcpu_tree_attention_forward(
+    if sinks is not None:
+        if sinks.dtype is not _FP32 or sinks.shape != (hq,) or not sinks.is_cuda:
+            raise ValueError("sinks must be a float32 CUDA tensor with one value per q head")
+        sinks = sinks.data_ptr()
+    if positions is not None:
+        if positions.shape != (t,):
+            raise ValueError("positions must have one entry per query token")
+        positions = _int32(positions, "positions")
+    code = _tree_forward(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
-        query_start_loc.data_ptr(), _int32(tree_mask, "tree_mask"), ms[1], _raw(positions), sliding_window,
-        softmax_scale, _raw(sinks), _dims(q.shape, k_cache, block_table, seq_lens), out.data_ptr(), lse.data_ptr(),
-        workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _raw_stream(stream))
+        query_start_loc.data_ptr(), _int32(tree_mask, "tree_mask"), words, positions, sliding_window, softmax_scale,
+        sinks, _pack_dims(seq_lens.shape[0], t, block_table.shape[1], pages, hq, hkv, d, page), out.data_ptr(),
+        lse.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_tree_attention_forward")
 
@@ -632,6 +642,8 @@ class PoolList:
             if x.shape != first.shape or x.dtype != first.dtype or not x.is_contiguous():
                 raise ValueError("pools must be contiguous and of one shape and type")
         self.pointers = (ctypes.c_void_p * len(self.pools))(*[x.data_ptr() for x in self.pools])
+        self.num_pools = len(self.pools)
+        self.bf16_pages = first.dtype is _BF16 and tuple(first.shape[2:]) == (16, 64)
         self.num_pages = int(first.shape[0])
         self.num_kv_heads = int(first.shape[1])
         self.page_bytes = int(first[0].numel() * first.element_size()) if self.num_pages else 0
@@ -643,23 +655,19 @@ def mcpu_compact_kv(pools, block_table, seq_lens, query_start_loc, accept_path, 
     node numbers, the first accept_len[r] of each row) behind the row's
     context, in every pool of the PoolList (bf16 pools); new_seq_lens receives
     the rows' lengths."""
-    p0 = pools.pools[0]
-    if p0.dim() != 4 or p0.dtype != torch.bfloat16:
+    if not pools.bf16_pages:
         raise ValueError("mcpu_compact_kv takes bfloat16 [num_pages, H_kv, 16, 64] pools")
-    if accept_path.dim() != 2 or accept_path.shape[0] != seq_lens.shape[0]:
+    rows = seq_lens.shape[0]
+    paths, most = accept_path.shape
+    if paths != rows:
         raise ValueError("accept_path must be an int32 [B, max_accept] tensor")
-    d = Dims(seq_lens.shape[0], 0, block_table.shape[1], pools.num_pages, pools.num_kv_heads, pools.num_kv_heads,
-             p0.shape[3], p0.shape[2])
-    code = _lib.mcpu_compact_kv(
-        pools.pointers, len(pools.pools), block_table.data_ptr(), seq_lens.data_ptr(), query_start_loc.data_ptr(),
-        _int32(accept_path, "accept_path"), accept_path.shape[1], _int32(accept_len, "accept_len"), d,
+    code = _compact_kv(
+        pools.pointers, pools.num_pools, block_table.data_ptr(), seq_lens.data_ptr(), query_start_loc.data_ptr(),
+        _int32(accept_path, "accept_path"), most, _int32(accept_len, "accept_len"),
+        _pack_dims(rows, 0, block_table.shape[1], pools.num_pages, pools.num_kv_heads, pools.num_kv_heads, 64, 16),
         new_seq_lens.data_ptr(), status_word.data_ptr(), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_compact_kv")
-
-
-def _page_dims(block_table, page_refs) -> Dims:
-    return Dims(block_table.shape[0], 0, block_table.shape[1], page_refs.shape[0], 1, 1, 64, 16)
 
 
 def mcpu_fork_block_tables(block_table, seq_lens, src_rows, dst_rows, page_refs, free_pages, free_count, copy_src,
@@ -668,13 +676,14 @@ def mcpu_fork_block_tables(block_table, seq_lens, src_rows, dst_rows, page_refs,
     a partial last page replaced by a fresh one whose contents
     mcpu_copy_pages(pools, copy_src, copy_dst, ...) brings over."""
     n = src_rows.shape[0]
-    if dst_rows.shape[0] != n or copy_src.shape[0] < n or copy_dst.shape[0] < n or page_scratch.numel() < PAGE_SCRATCH:
+    rows, width = block_table.shape
+    if dst_rows.shape[0] != n or copy_src.shape[0] < n or copy_dst.shape[0] < n or page_scratch.shape[0] < PAGE_SCRATCH:
         raise ValueError("dst_rows, copy_src and copy_dst must have one entry per fork, page_scratch PAGE_SCRATCH")
-    code = _lib.mcpu_fork_block_tables(
+    code = _fork_tables(
         block_table.data_ptr(), seq_lens.data_ptr(), _int32(src_rows, "src_rows"), _int32(dst_rows, "dst_rows"), n,
-        _page_dims(block_table, page_refs), page_refs.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
-        _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), page_scratch.data_ptr(), status_word.data_ptr(),
-        _raw_stream(stream))
+        _pack_dims(rows, 0, width, page_refs.shape[0], 1, 1, 64, 16), page_refs.data_ptr(), free_pages.data_ptr(),
+        free_count.data_ptr(), _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), page_scratch.data_ptr(),
+        status_word.data_ptr(), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_fork_block_tables")
 
@@ -683,10 +692,12 @@ def mcpu_shrink_block_tables(block_table, seq_lens, sliding_window, page_refs, f
                              status_word, stream=None):
     """Releases every page past the rows' lengths (and, with a window, before
     it); pages without another holder return to the stack."""
-    if free_pages.shape[0] < page_refs.shape[0] or page_scratch.numel() < PAGE_SCRATCH:
+    rows, width = block_table.shape
+    pages = page_refs.shape[0]
+    if free_pages.shape[0] < pages or page_scratch.shape[0] < PAGE_SCRATCH:
         raise ValueError("free_pages must hold as many pages as page_refs counts, page_scratch PAGE_SCRATCH words")
-    code = _lib.mcpu_shrink_block_tables(
-        block_table.data_ptr(), seq_lens.data_ptr(), sliding_window, _page_dims(block_table, page_refs),
+    code = _shrink_tables(
+        block_table.data_ptr(), seq_lens.data_ptr(), sliding_window, _pack_dims(rows, 0, width, pages, 1, 1, 64, 16),
         page_refs.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), page_scratch.data_ptr(),
         status_word.data_ptr(), _raw_stream(stream))
     if code:
@@ -699,8 +710,8 @@ def mcpu_copy_pages(pools, copy_src, copy_dst, status_word, stream=None):
     n = copy_src.shape[0]
     if copy_dst.shape[0] != n:
         raise ValueError("copy_src and copy_dst must have the same length")
-    code = _lib.mcpu_copy_pages(pools.pointers, len(pools.pools), pools.page_bytes, pools.num_pages,
-                                _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), n, status_word.data_ptr(),
-                                _raw_stream(stream))
+    code = _copy_pages(pools.pointers, pools.num_pools, pools.page_bytes, pools.num_pages,
+                       _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), n, status_word.data_ptr(),
+                       _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_copy_pages")
