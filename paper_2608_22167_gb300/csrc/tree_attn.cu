@@ -169,31 +169,114 @@ __device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, volatile i
   }
   return true;
 }
+// A short spin, 64 tests at most.
+__device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b32 n;\n\tmov.b32 n, 64;\n"
+      "spin:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra done;\n\t"
+      "sub.s32 n, n, 1;\n\tsetp.ne.s32 q, n, 0;\n\t@q bra spin;\n"
+      "done:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ bool wait_sleep(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
   return mbar_try_wait(bar, parity) || wait_more<true>(bar, parity, abort_flag);
 }
 __device__ __forceinline__ bool wait_poll(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
   return mbar_try_wait(bar, parity) || wait_more<false>(bar, parity, abort_flag);
 }
+// The same for a warp in step, which stays so.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
+  return __all_sync(0xffffffffu, mbar_spin(bar, parity)) ||
+         __all_sync(0xffffffffu, wait_more<false>(bar, parity, abort_flag));
+}
 
-// A 2-D box load issued by one elected lane of a warp that runs in step: its
-// operands stay in the uniform datapath (from a lone lane every operand is
-// moved there first, which made the issue of a block's 16 boxes take longer
-// than their transfer).
-__device__ __forceinline__ void tma_load_2d_e(uint32_t dst, const CUtensorMap* map, int32_t y, uint32_t bar,
-                                              uint64_t policy) {
+// What one elected lane of a warp in step issues: a block's eight pages by
+// TMA, the MMAs of S and of O with the commits behind them. One election for
+// all of it, and operands that differ by constants: from a lone lane, or with
+// an election per operation, the operands' way to the uniform datapath takes
+// longer than the work that is issued.
+__device__ __forceinline__ void load_block_e(uint32_t dst, const CUtensorMap* map, const int (&y)[kBlockPages],
+                                             uint32_t bar, uint64_t policy) {
+  static_assert(kBlockPages == 8 && kTileBytes == 2048, "eight boxes of 2 KiB");
   asm volatile(
-      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "{\n\t.reg .pred e;\n\t.reg .b32 z;\n\tmov.b32 z, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%2], %4;\n\t"
       "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0], [%1, {%2, %3}], [%4], %5;\n\t}" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(y), "r"(bar), "l"(policy)
+      " [%0 + 0], [%1, {z, %5}], [%2], %3;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0 + 2048], [%1, {z, %6}], [%2], %3;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0 + 4096], [%1, {z, %7}], [%2], %3;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0 + 6144], [%1, {z, %8}], [%2], %3;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0 + 8192], [%1, {z, %9}], [%2], %3;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0 + 10240], [%1, {z, %10}], [%2], %3;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0 + 12288], [%1, {z, %11}], [%2], %3;\n\t"
+      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0 + 14336], [%1, {z, %12}], [%2], %3;\n\t"
+      "}" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "l"(policy), "n"(kBlockBytes), "r"(y[0]), "r"(y[1]), "r"(y[2]),
+      "r"(y[3]), "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7])
       : "memory");
 }
-__device__ __forceinline__ void arrive_expect_tx_e(uint32_t bar, uint32_t bytes) {
+__device__ __forceinline__ void mma_scores_e(uint32_t d, uint64_t q, uint64_t k, uint32_t idesc, uint32_t done,
+                                             uint32_t k_free) {
+  static_assert(kHeadDim == 64, "four steps of 16 dims, 32 bytes each");
+  asm volatile(
+      "{\n\t.reg .pred e, t, f;\n\t.reg .b64 a, b;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "setp.eq.u32 t, 0, 0;\n\tsetp.ne.u32 f, 0, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, f;\n\t"
+      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t"
+      "}" ::"r"(d),
+      "l"(q), "l"(k), "r"(idesc), "r"(done), "r"(k_free)
+      : "memory");
+}
+__device__ __forceinline__ void mma_values_e(uint32_t d, uint32_t pw, uint64_t v, uint32_t idesc, uint32_t add,
+                                             uint32_t done, uint32_t v_free) {
+  static_assert(kBlockKeys == 128 && 16 * kRowBytes / 16 == 128, "eight steps of 16 keys, 2 KiB of V each");
+  asm volatile(
+      "{\n\t.reg .pred e, t, f;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "setp.eq.u32 t, 0, 0;\n\tsetp.ne.u32 f, %4, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, f;\n\t"
+      "add.s32 a, %1, 8;\n\tadd.s64 b, %2, 128;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "add.s32 a, %1, 16;\n\tadd.s64 b, %2, 256;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "add.s32 a, %1, 24;\n\tadd.s64 b, %2, 384;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "add.s32 a, %1, 32;\n\tadd.s64 b, %2, 512;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "add.s32 a, %1, 40;\n\tadd.s64 b, %2, 640;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "add.s32 a, %1, 48;\n\tadd.s64 b, %2, 768;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "add.s32 a, %1, 56;\n\tadd.s64 b, %2, 896;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, t;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%5];\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t"
+      "}" ::"r"(d),
+      "r"(pw), "l"(v), "r"(idesc), "r"(add), "r"(done), "r"(v_free)
+      : "memory");
+}
+
+// A ring's position: stage and the parity of its turn, without a division.
+template <uint32_t kStages>
+struct RingAt {
+  uint32_t s = 0, parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++s == kStages) s = 0, parity ^= 1;
+  }
+};
+
+// One arrival of a warp in step.
+__device__ __forceinline__ void mbar_arrive_e(uint32_t bar) {
   asm volatile(
       "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
-      "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
-      "r"(bytes)
+      "@e mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar)
       : "memory");
 }
 
@@ -261,6 +344,46 @@ __device__ __forceinline__ float chunk_weights(const uint32_t (&sv)[2][32], floa
   }
 }
 
+// pk[at ..] = bf16(2^(s * scale - mu)) of 32 scores; their fp32 sum (before
+// rounding) goes to sum.
+template <int at>
+__device__ __forceinline__ void weights32(const uint32_t (&sv)[32], uint64_t sc, uint64_t mu, uint64_t (&sum)[2],
+                                        uint32_t (&pk)[32]) {
+#pragma unroll
+  for (int e = 0; e < 32; e += 2) {
+    const uint64_t x = fma2((uint64_t)sv[e] | ((uint64_t)sv[e + 1] << 32), sc, mu);
+    const float p0 = ex2_approx(lo_f32(x)), p1 = ex2_approx(hi_f32(x));
+    sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pack_f32x2(p0, p1));
+    pk[at + e / 2] = pack_bf16x2(p0, p1);
+  }
+}
+__device__ __forceinline__ float sum_of(const uint64_t (&sum)[2]) {
+  const uint64_t s = add2(sum[0], sum[1]);
+  return lo_f32(s) + hi_f32(s);
+}
+
+__device__ __forceinline__ float scores_max32(const uint32_t (&sv)[32]) {
+  float m[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+  for (int e = 0; e < 32; e += 4)
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+      m[k] = fmax3(m[k], __uint_as_float(sv[e + 2 * k]), __uint_as_float(sv[e + 2 * k + 1]));
+  return fmaxf(m[0], m[1]);
+}
+
+// 16 TMEM columns from the first or second half of v
+template <int at>
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16};" ::"r"(taddr),
+      "r"(v[at]), "r"(v[at + 1]), "r"(v[at + 2]), "r"(v[at + 3]), "r"(v[at + 4]), "r"(v[at + 5]), "r"(v[at + 6]),
+      "r"(v[at + 7]), "r"(v[at + 8]), "r"(v[at + 9]), "r"(v[at + 10]), "r"(v[at + 11]), "r"(v[at + 12]),
+      "r"(v[at + 13]), "r"(v[at + 14]), "r"(v[at + 15])
+      : "memory");
+}
+
 __device__ __forceinline__ void zero_smem16(uint32_t addr) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0u) : "memory");
 }
@@ -302,7 +425,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     tree_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                 const __grid_constant__ CUtensorMap qmap, const TreeParams p) {
   extern __shared__ uint8_t smem_raw[];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // (through lane 0, so that what follows from the warp's role is known to be uniform)
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t raw = smem_addr(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - raw);
@@ -434,7 +558,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       prefetch_tensormap(&vmap);
       prefetch_tensormap(&qmap);
     }
-    uint32_t k_it = 0, v_it = 0;
+    RingAt<kKStages> rk;
+    RingAt<kVStages> rv;
+    uint32_t k_it = 0, v_it = 0;  // blocks issued
     int i = 0;
     bool ok = true;
 #pragma unroll 1
@@ -495,19 +621,16 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         const int* bt_row = p.block_table + (size_t)a.row * p.max_pages;
         const int n = a.b1 - a.b0, pg0 = a.kb0 / kPage + a.b0 * kBlockPages;
         const int page_end = min((a.len + kPage - 1) / kPage, pg0 + n * kBlockPages);
-        auto load_ids = [&](int c) -> int {  // page id of page pg0 + 32c + lane, or -1
+        auto load_ids = [&](int c) -> int {  // page id of page pg0 + 32c + lane
           const int lp = pg0 + 32 * c + lane;
-          int v = -1;
-          if (lp < page_end) {
-            v = __ldg(bt_row + lp);
-            if (v < 0 || v >= p.num_pages) {
-              atomicOr(p.status, kStatusBadPage);
-              v = -1;
-            }
-          }
-          return v;
+          return lp < page_end ? __ldg(bt_row + lp) : -2;
         };
-        int ids = load_ids(0), ids_next = load_ids(1);
+        auto box_row = [&](int id) -> int {  // where the page's box begins; nothing past the last page
+          if (id >= 0 && id < p.num_pages) return (id * Hkv + a.kvh) * kPage;
+          if (id != -2) atomicOr(p.status, kStatusBadPage);
+          return p.oob_row;
+        };
+        int ids_next = load_ids(0);
         const uint32_t* rows = p.mask + (size_t)a.token * p.words;
         const uint32_t* all = rows - (size_t)a.node * p.words;
         const int L = a.len - a.ctx, mine = a.n_tok * p.words;
@@ -533,36 +656,43 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         }
         __syncwarp();
         ++i;
-        // K of block b, then V of block b - 1: one copy of the code for both,
-        // the kernel's instructions barely fit their cache
-        int y[2][kBlockPages];
+        // K of block b, then V of block b - 1
+        int y[kBlockPages], y_old[kBlockPages], at = 0;
 #pragma unroll 1
-        for (int step = 0; step < 2 * n + 2 && ok; ++step) {
-          const int b = step >> 1;
-          const bool is_k = !(step & 1);
-          if (is_k) {
-#pragma unroll
-            for (int j = 0; j < kBlockPages; ++j) y[1][j] = y[0][j];
-            if (b == n) continue;
-            if (b > 0 && (b * kBlockPages) % 32 == 0) {
-              ids = ids_next;
-              ids_next = load_ids(b * kBlockPages / 32 + 1);
+        for (int b = 0; b <= n; ++b) {
+          if (b < n) {
+            if (!(b & 3)) {  // 32 pages: a lane each, the next ones' ids on their way
+              at = box_row(ids_next);
+              ids_next = load_ids((b >> 2) + 1);
             }
 #pragma unroll
-            for (int j = 0; j < kBlockPages; ++j) {
-              const int pid = __shfl_sync(0xffffffffu, ids, (b * kBlockPages) % 32 + j);
-              y[0][j] = pid < 0 ? p.oob_row : (pid * Hkv + a.kvh) * kPage;
-            }
-          } else if (b == 0) {  // behind the first K block: what the softmax needs of the masks
+            for (int j = 0; j < kBlockPages; ++j) y[j] = __shfl_sync(0xffffffffu, at, (b & 3) * kBlockPages + j);
+            ok = wait_warp(bar(ln.k_empty[rk.s]), rk.parity ^ 1, abort_flag);
+            if (!ok) break;
+            load_block_e(sK + rk.s * kBlockBytes, &kmap, y, bar(ln.k_full[rk.s]), pol);
+            rk.next();
+            ++k_it;
+          }
+          if (b > 0) {
+            ok = wait_warp(bar(ln.v_empty[rv.s]), rv.parity ^ 1, abort_flag);
+            if (!ok) break;
+            load_block_e(sV + rv.s * kBlockBytes, &vmap, y_old, bar(ln.v_full[rv.s]), pol);
+            rv.next();
+            ++v_it;
+          } else {  // behind the first K block: what the softmax needs of the masks
             Meta& m = ln.meta[slot];
             auto first_key = [&](int pos) { return min(max(pos, a.ctx), a.len - 1) - p.window + 1; };
+#pragma unroll 1
             for (int k = lane; k < mine; k += 32) m.mask[k] = k < 32 ? early : __ldg(rows + k);
             if (p.window > 0)
+#pragma unroll 1
               for (int k = lane; k < a.n_tok; k += 32)
                 m.lo[k] = first_key(k < 32 ? early_pos : __ldg(p.positions + a.token + k));
             if (a.b1 * kBlockKeys + a.kb0 > a.ctx)  // the part reaches the nodes
+#pragma unroll 1
               for (int c = 0; c < p.words; ++c) {
                 uint32_t any = 0;
+#pragma unroll 1
                 for (int k = lane; k < L; k += 32) any |= __ldg(all + (size_t)k * p.words + c);
                 any = __reduce_or_sync(0xffffffffu, any);
                 if (lane == 0) m.seen_by_any[c] = any;
@@ -571,22 +701,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(ln.meta_full[slot]));
             __syncwarp();
-            continue;
           }
-          const uint32_t it = is_k ? k_it : v_it, stages = is_k ? kKStages : kVStages, s = it % stages;
-          uint64_t* full = is_k ? ln.k_full : ln.v_full;
-          uint64_t* empty = is_k ? ln.k_empty : ln.v_empty;
-          if (it >= stages) {
-            ok = __all_sync(0xffffffffu, wait_sleep(bar(empty[s]), (it / stages - 1) & 1, abort_flag));
-            if (!ok) break;
-          }
-          const uint32_t dst = (is_k ? sK : sV) + s * kBlockBytes;
-          const CUtensorMap* map = is_k ? &kmap : &vmap;
-          arrive_expect_tx_e(bar(full[s]), kBlockBytes);
 #pragma unroll
-          for (int j = 0; j < kBlockPages; ++j)
-            tma_load_2d_e(dst + j * kTileBytes, map, is_k ? y[0][j] : y[1][j], bar(full[s]), pol);
-          if (is_k) ++k_it; else ++v_it;
+          for (int j = 0; j < kBlockPages; ++j) y_old[j] = y[j];
         }
         if (!ok) break;
       }
@@ -609,10 +726,12 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     // ------------------------------------------------------------ MMA issue
     constexpr uint32_t idS = idesc_bf16(kTileRows, kBlockKeys, false, false);
     constexpr uint32_t idO = idesc_bf16(kTileRows, kHeadDim, false, true);
-    constexpr uint64_t kStageStep = kBlockBytes / 16, kVStep = 16 * kRowBytes / 16;
+    constexpr uint64_t kStageStep = kBlockBytes / 16;
     const uint64_t kdesc0 = smem_desc_sw128(sK, 16, 1024), vdesc0 = smem_desc_sw128(sV, 1024, 1024);
     const uint64_t qd = smem_desc_sw128(sQ, 16, 1024);
-    uint32_t cnt = 0;  // blocks of the parts before
+    RingAt<kKStages> rk;
+    RingAt<kVStages> rv;
+    uint32_t s_par = 1, p_par = 0;  // turns of s_free and p_full
     bool ok = true;
     for (int i = 0; ok; ++i) {
       const int slot = i & 1;
@@ -622,44 +741,26 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       if (!wait_sleep(bar(ln.q_full), i & 1, abort_flag)) break;
       for (int b = 0; b <= n; ++b) {
         if (b < n) {  // S(b)
-          const uint32_t bk = cnt + b;
-          const int s = bk % kKStages;
-          if (!wait_sleep(bar(ln.k_full[s]), (bk / kKStages) & 1, abort_flag) ||
-              (bk >= 1 && !wait_sleep(bar(ln.s_free), (bk - 1) & 1, abort_flag))) {
-            ok = false;
-            break;
-          }
+          ok = wait_warp(bar(ln.k_full[rk.s]), rk.parity, abort_flag) && wait_warp(bar(ln.s_free), s_par, abort_flag);
+          if (!ok) break;
           tc_fence_after();
-          const uint64_t kd = kdesc0 + s * kStageStep;
-          tc_mma_ss_e(tmem, qd, kd, idS, 0u);
-#pragma unroll
-          for (int kk = 1; kk < kHeadDim / 16; ++kk)
-            tc_mma_ss_e(tmem, qd + (uint64_t)(kk * 2), kd + (uint64_t)(kk * 2), idS, 1u);
-          tc_commit_e(bar(ln.s_full));
-          tc_commit_e(bar(ln.k_empty[s]));
+          mma_scores_e(tmem, qd, kdesc0 + rk.s * kStageStep, idS, bar(ln.s_full), bar(ln.k_empty[rk.s]));
           if (b == n - 1) tc_commit_e(bar(ln.q_empty));
+          rk.next();
+          s_par ^= 1;
         }
         if (b >= 1) {  // O += P(b - 1) V(b - 1)
-          const uint32_t bv = cnt + b - 1;
-          const int s = bv % kVStages;
-          if (!wait_sleep(bar(ln.v_full[s]), (bv / kVStages) & 1, abort_flag) ||
-              !wait_sleep(bar(ln.p_full), bv & 1, abort_flag) ||
-              (b == 1 && i >= 1 && !wait_sleep(bar(ln.o_free), (i - 1) & 1, abort_flag))) {
-            ok = false;
-            break;
-          }
+          ok = wait_warp(bar(ln.v_full[rv.s]), rv.parity, abort_flag) && wait_warp(bar(ln.p_full), p_par, abort_flag) &&
+               (b > 1 || i == 0 || wait_warp(bar(ln.o_free), (i - 1) & 1, abort_flag));
+          if (!ok) break;
           tc_fence_after();
-          const uint64_t vd = vdesc0 + s * kStageStep;
-          tc_mma_ts_e(tmem + kColO, tmem + kColP, vd, idO, b > 1 ? 1u : 0u);
-#pragma unroll
-          for (int kk = 1; kk < kBlockKeys / 16; ++kk)
-            tc_mma_ts_e(tmem + kColO, tmem + kColP + kk * 8, vd + kk * kVStep, idO, 1u);
-          tc_commit_e(bar(ln.o_ready));
-          tc_commit_e(bar(ln.v_empty[s]));
+          mma_values_e(tmem + kColO, tmem + kColP, vdesc0 + rv.s * kStageStep, idO, b > 1 ? 1u : 0u, bar(ln.o_ready),
+                       bar(ln.v_empty[rv.s]));
+          rv.next();
+          p_par ^= 1;
         }
       }
       if (!ok) break;
-      cnt += n;
       if (lane == 0) mbar_arrive(bar(ln.part_empty[slot]));
     }
     // MMAs still in flight (after an abort) must not outlive TMEM
@@ -724,7 +825,92 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           if (lane == 0) mbar_arrive(bar(ln.p_full));
         }
       } else {
+        bool unset = true;  // some row has no reference yet
         for (int b = 0; b < n; ++b, ++cnt, kb += kBlockKeys) {
+          // ---- blocks that every node sees, all references set: a loop of its
+          // own, small enough to stay in the instruction cache. Four chunks of
+          // 32 scores, the next one's load in flight while one's weights are
+          // made. Nothing is known of the scores before: weights up to 2^60 of
+          // the first three chunks are taken as they are (their row's sum shows
+          // it; else the block is done anew below), and what exceeds 2^8 is
+          // scaled down after the last.
+          if (!unset) {
+            const int stop = min(n, b + (min(plain_hi, a.kb0 + (a.b1 - 1) * kBlockKeys) - kb) / kBlockKeys + 1);
+            const uint64_t sc = pack_f32x2(p.scale_log2, p.scale_log2);
+            if (kb < plain_lo || kb > plain_hi) goto general;
+            while (b < stop) {
+              uint32_t sa[32], sb[32], pk[32];
+              uint64_t sum[2] = {0, 0};
+              const uint64_t mu = pack_f32x2(-m_ref, -m_ref);
+              ok = wait_warp(bar(ln.s_full), cnt & 1, abort_flag);
+              if (!ok) break;
+              tc_fence_after();
+              tmem_ld32(cS, sa);
+              tmem_ld_wait();
+              tmem_ld32(cS + 32, sb);
+              weights32<0>(sa, sc, mu, sum, pk);
+              tmem_ld_wait();
+              tmem_ld32(cS + 64, sa);
+              weights32<16>(sb, sc, mu, sum, pk);
+              if (cnt >= 1) {  // the P buffer was last read by the previous PV
+                ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+              }
+              tmem_st32(cP, pk);
+              tmem_ld_wait();
+              tmem_ld32(cS + 96, sb);
+              weights32<0>(sa, sc, mu, sum, pk);
+              float l0 = sum_of(sum);
+              tmem_ld_wait();
+              if (__any_sync(0xffffffffu, !(l0 < 0x1p60f))) break;  // done anew below
+              tc_fence_before();
+              mbar_arrive_e(bar(ln.s_free));
+              sum[0] = sum[1] = 0;
+              weights32<16>(sb, sc, mu, sum, pk);
+              tmem_st32(cP + 32, pk);
+              float l1 = sum_of(sum);
+              if (__any_sync(0xffffffffu, !(l0 + l1 < 256.f))) {
+                // some rows' reference rises by a whole number of octaves, so that scaling P is exact
+                float up = 0.f;
+                if (!(l0 + l1 < 256.f)) up = ceilf(fmaxf(__log2f(l0), scores_max32(sb) * p.scale_log2 - m_ref));
+                const float f = ex2_approx(-up);
+                m_ref += up;
+                l *= f;
+                l0 *= f;
+                __syncwarp();
+                tmem_st_wait();
+#pragma unroll 1
+                for (int h = 0; h < 4; ++h) {
+                  const uint32_t at = h < 2 ? cP + 32 * h : cO + 32 * (h - 2);
+                  if (h >= 2 && b == 0) break;  // O holds another part's
+                  tmem_ld32(at, sa);
+                  tmem_ld_wait();
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) {
+                    const float2 w = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sa[e]));
+                    sa[e] = h < 2 ? pack_bf16x2(w.x * f, w.y * f) : __float_as_uint(__uint_as_float(sa[e]) * f);
+                  }
+                  __syncwarp();
+                  tmem_st32(at, sa);
+                }
+                tmem_st_wait();
+                sum[0] = sum[1] = 0;  // the last chunk anew: its weights may have been infinite
+                weights32<0>(sb, sc, pack_f32x2(-m_ref, -m_ref), sum, pk);
+                l1 = sum_of(sum);
+                __syncwarp();
+                tmem_st16<0>(cP + 48, pk);
+              }
+              l += l0 + l1;
+              tmem_st_wait();
+              tc_fence_before();
+              __syncwarp();
+              mbar_arrive_e(bar(ln.p_full));
+              ++b, ++cnt, kb += kBlockKeys;
+            }
+            if (!ok || b == n) break;
+          }
+        general:
           const bool masked = kb > plain_hi || kb < plain_lo;
           uint32_t seen[4];  // bit e of word c: this thread's node sees key kb + 32c + e
           bool dead = false;
@@ -801,11 +987,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               tmem_st32(cO + 32 * h, ov);
             }
           }
-          __syncwarp();
+          unset = __any_sync(0xffffffffu, m_ref == -INFINITY);
           tmem_st_wait();
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(ln.p_full));
+          mbar_arrive_e(bar(ln.p_full));
         }
       }
       if (!ok) break;
