@@ -169,29 +169,28 @@ __device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, volatile i
   }
   return true;
 }
-// A short spin, 64 tests at most.
-__device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .b32 n;\n\tmov.b32 n, 64;\n"
-      "spin:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra done;\n\t"
-      "sub.s32 n, n, 1;\n\tsetp.ne.s32 q, n, 0;\n\t@q bra spin;\n"
-      "done:\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
 __device__ __forceinline__ bool wait_sleep(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
   return mbar_try_wait(bar, parity) || wait_more<true>(bar, parity, abort_flag);
 }
 __device__ __forceinline__ bool wait_poll(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
   return mbar_try_wait(bar, parity) || wait_more<false>(bar, parity, abort_flag);
 }
-// The same for a warp in step, which stays so.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
-  return __all_sync(0xffffffffu, mbar_spin(bar, parity)) ||
-         __all_sync(0xffffffffu, wait_more<false>(bar, parity, abort_flag));
+// The same for a warp in step, in the loops over blocks: few instructions, and
+// one outcome for the warp, so that its branches are uniform. A test returns
+// within about a hundred cycles, so 2^22 of them take some tenths of a second;
+// after that the role ends, and with it the other roles' waits.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
+  uint32_t left;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmov.b32 %0, 0x400000;\n"
+      "again:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "vote.sync.all.pred p, p, 0xffffffff;\n\t@p bra.uni done;\n\t"
+      "sub.u32 %0, %0, 1;\n\tsetp.ne.u32 p, %0, 0;\n\t@p bra.uni again;\n"
+      "done:\n\t}"
+      : "=&r"(left)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return left != 0;
 }
 
 // What one elected lane of a warp in step issues: a block's eight pages by
@@ -536,7 +535,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       st.first_off[warp] = u - pre[r0];
     }
   }
-  if (warp == 8) {
+  if (warp == 0) {
     tmem_alloc(smem_addr(&st.tmem_base), kTmemCols);
     tmem_relinquish();
   }
@@ -545,13 +544,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   __syncthreads();
   tc_fence_after();
 
-  const int x = warp < 8 ? warp >> 2 : warp & 1;  // this warp's lane of the CTA
+  const int x = warp >= 4 ? (warp >> 2) - 1 : warp & 1;  // this warp's lane of the CTA
   Lane& ln = st.lane[x];
   const uint32_t sQ = base + x * kLaneBytes, sK = sQ + kQBytes, sV = sK + kKStages * kBlockBytes;
   const uint32_t tmem = st.tmem_base + x * 256;  // S at 0, O at 128, P at 192
   constexpr uint32_t kColO = 128, kColP = 192;
 
-  if (warp >= 10) {
+  if ((warp & ~1) == 2) {
     // ------------------------------------------------------------- producer
     if (lane == 0) {
       prefetch_tensormap(&kmap);
@@ -667,14 +666,14 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             }
 #pragma unroll
             for (int j = 0; j < kBlockPages; ++j) y[j] = __shfl_sync(0xffffffffu, at, (b & 3) * kBlockPages + j);
-            ok = wait_warp(bar(ln.k_empty[rk.s]), rk.parity ^ 1, abort_flag);
+            ok = wait_warp(bar(ln.k_empty[rk.s]), rk.parity ^ 1);
             if (!ok) break;
             load_block_e(sK + rk.s * kBlockBytes, &kmap, y, bar(ln.k_full[rk.s]), pol);
             rk.next();
             ++k_it;
           }
           if (b > 0) {
-            ok = wait_warp(bar(ln.v_empty[rv.s]), rv.parity ^ 1, abort_flag);
+            ok = wait_warp(bar(ln.v_empty[rv.s]), rv.parity ^ 1);
             if (!ok) break;
             load_block_e(sV + rv.s * kBlockBytes, &vmap, y_old, bar(ln.v_full[rv.s]), pol);
             rv.next();
@@ -708,6 +707,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         if (!ok) break;
       }
     }
+    if (!ok && *abort_flag == 0) *abort_flag = 1;
     if (ok && (i < 2 || __all_sync(0xffffffffu, wait_sleep(bar(ln.part_empty[i & 1]), ((i >> 1) - 1) & 1, abort_flag)))) {
       if (lane == 0) {  // no more parts
         ln.parts[i & 1].row = -1;
@@ -722,7 +722,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         mbar_wait(bar(ln.v_full[it % kVStages]), (it / kVStages) & 1);
       if (i > 0) mbar_wait(bar(ln.q_full), (i - 1) & 1);
     }
-  } else if (warp >= 8) {
+  } else if (warp < 2) {
     // ------------------------------------------------------------ MMA issue
     constexpr uint32_t idS = idesc_bf16(kTileRows, kBlockKeys, false, false);
     constexpr uint32_t idO = idesc_bf16(kTileRows, kHeadDim, false, true);
@@ -740,8 +740,13 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const int n = ln.parts[slot].b1 - ln.parts[slot].b0;
       if (!wait_sleep(bar(ln.q_full), i & 1, abort_flag)) break;
       for (int b = 0; b <= n; ++b) {
+        // What the block loads deliver is waited for first, so that nothing
+        // lies between the softmax's arrivals and the MMAs they set off.
+        if (b < n) ok = wait_warp(bar(ln.k_full[rk.s]), rk.parity);
+        if (b >= 1) ok = ok && wait_warp(bar(ln.v_full[rv.s]), rv.parity);
+        if (!ok) break;
         if (b < n) {  // S(b)
-          ok = wait_warp(bar(ln.k_full[rk.s]), rk.parity, abort_flag) && wait_warp(bar(ln.s_free), s_par, abort_flag);
+          ok = wait_warp(bar(ln.s_free), s_par);
           if (!ok) break;
           tc_fence_after();
           mma_scores_e(tmem, qd, kdesc0 + rk.s * kStageStep, idS, bar(ln.s_full), bar(ln.k_empty[rk.s]));
@@ -750,8 +755,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           s_par ^= 1;
         }
         if (b >= 1) {  // O += P(b - 1) V(b - 1)
-          ok = wait_warp(bar(ln.v_full[rv.s]), rv.parity, abort_flag) && wait_warp(bar(ln.p_full), p_par, abort_flag) &&
-               (b > 1 || i == 0 || wait_warp(bar(ln.o_free), (i - 1) & 1, abort_flag));
+          ok = wait_warp(bar(ln.p_full), p_par) && (b > 1 || i == 0 || wait_warp(bar(ln.o_free), (i - 1) & 1));
           if (!ok) break;
           tc_fence_after();
           mma_values_e(tmem + kColO, tmem + kColP, vdesc0 + rv.s * kStageStep, idO, b > 1 ? 1u : 0u, bar(ln.o_ready),
@@ -760,7 +764,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           p_par ^= 1;
         }
       }
-      if (!ok) break;
+      if (!ok) {
+        if (*abort_flag == 0) *abort_flag = 1;
+        break;
+      }
       if (lane == 0) mbar_arrive(bar(ln.part_empty[slot]));
     }
     // MMAs still in flight (after an abort) must not outlive TMEM
@@ -842,7 +849,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               uint32_t sa[32], sb[32], pk[32];
               uint64_t sum[2] = {0, 0};
               const uint64_t mu = pack_f32x2(-m_ref, -m_ref);
-              ok = wait_warp(bar(ln.s_full), cnt & 1, abort_flag);
+              ok = wait_warp(bar(ln.s_full), cnt & 1);
               if (!ok) break;
               tc_fence_after();
               tmem_ld32(cS, sa);
@@ -853,7 +860,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               tmem_ld32(cS + 64, sa);
               weights32<16>(sb, sc, mu, sum, pk);
               if (cnt >= 1) {  // the P buffer was last read by the previous PV
-                ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1, abort_flag);
+                ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
               }
@@ -1046,13 +1053,14 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         mbar_arrive(bar(ln.part_empty[slot]));
       }
     }
+    if (!ok && *abort_flag == 0) *abort_flag = 1;
   }
 
   __syncwarp();
   if (threadIdx.x == 0 && *abort_flag == 1) atomicOr(p.status, kStatusTimeout);
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == 0) {
     tc_fence_after();
     tmem_dealloc(st.tmem_base, kTmemCols);
   }
