@@ -21,24 +21,30 @@
 // order of the pieces. Every CTA derives the lines from seq_lens and
 // query_start_loc itself (prefix sums over the rows): no planning launch.
 //
-// Warps: 0-3 / 4-7 softmax of lane 0 / 1 (thread t owns row t & 127, a TMEM
-// lane: running max and sum in fp32, P to TMEM as bf16 - each weight rounded
-// once, 2^-8 relative - and O rescaled only when the max rises by more than
-// 2^8); 8, 9 MMA issue (S = Q K^T: M 128, N 128, K 64; O += P V: M 128, N 64,
-// K 128, P from TMEM); 10, 11 producers (the lane's parts, what the softmax
-// needs of their masks, Q tiles and K / V blocks by TMA, one 2 KiB box per
-// page). TMEM: per lane S 128, O 64, P 64 columns.
+// Warps: 0, 1 issue S = Q K^T of lane 0, 1 (M 128, N 128, K 64) and 2, 3 issue
+// O += P V (M 128, N 64, K 128, P from TMEM): an issuing warp is held until the
+// tensor pipe takes its MMAs, and one warp for both had no time left in a block
+// (+ 2 % of time); 4, 5 bring K, the Q tiles, the parts and what the softmax
+// needs of their masks, 6, 7 bring V (TMA, one 2 KiB box per page); 8-11 /
+// 12-15 softmax of lane 0 / 1 (thread t owns row t & 127, a TMEM lane: running
+// max and sum in fp32, P to TMEM as bf16 - each weight rounded once, 2^-8
+// relative - and O rescaled only when the reference has to rise). The softmax
+// takes 168 registers, the others give back all but 88. TMEM: per lane S 128,
+// O 64, P 64 columns.
 //
 // Bound: reading K/V (2 KiB per key and 8 kv heads, once) up to 16 nodes at
 // g = 8; from there the softmax, whose two warps per SM sub-partition take
-// about 2425 cycles for a block of both lanes (1024 of exponentials at 8 a
-// clock, 1194 issue slots). Measured on a GB300: 64 rows of 2k-16k keys with
-// 1-16 nodes 209 us (5.8 TB/s of K/V), 4k-32k keys with 16-32 nodes 698 us
-// (655 TFLOP/s), two rows of 49k-65k keys with 61 and 64 nodes 145 us (813
-// TFLOP/s), 384 rows in a window of 128 keys 111 us.
+// about 1650 cycles for a block of both lanes (1024 of exponentials at 8 a
+// clock; the same instructions without waits 1330, with barriers that are
+// always ready 1460). Its loop over plain blocks is kept apart from all that is
+// rare: with masks, first blocks and rescaling inside it, it took 2430, mostly
+// waiting for instructions. Measured on a GB300: 64 rows of 2k-16k keys with
+// 1-16 nodes 194 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 535 us (855
+// TFLOP/s), two rows of 49k-65k keys with 61 and 64 nodes 112 us (1050
+// TFLOP/s), 384 rows in a window of 128 keys 100 us.
 //
-// Waits are bounded (common.cuh); one that runs out raises an abort flag that
-// ends every role, and TMEM is freed after the issuers' MMAs have drained.
+// Waits are bounded; one that runs out raises an abort flag, every role ends,
+// and TMEM is freed after the issuers' MMAs have drained.
 #include "tcgen05.cuh"
 #include "tree_round.cuh"
 
@@ -53,7 +59,9 @@ constexpr int kBlockBytes = kBlockKeys * kRowBytes;  // one K or V block: 16 KiB
 constexpr int kKStages = 3, kVStages = 2;            // per lane
 constexpr int kQBytes = kTileRows * kRowBytes;
 constexpr int kLaneBytes = kQBytes + (kKStages + kVStages) * kBlockBytes;
-constexpr int kTreeThreads = 384;
+constexpr int kTreeThreads = 512;
+constexpr int kHelperRegs = 88, kSoftmaxRegs = 168;  // of 128 at launch: two warpgroups each
+static_assert(2 * (kHelperRegs + kSoftmaxRegs) == 4 * 128, "the registers of the launch");
 constexpr uint32_t kTmemCols = 512;
 constexpr int kCostItem = 5;  // a tile's set-up and end, in blocks
 constexpr int kWholeBlocks = 6;  // tiles of up to so many blocks are never cut
@@ -81,7 +89,7 @@ struct Lane {
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t s_full, s_free, p_full, o_ready, o_free;
   uint64_t part_full[2], part_empty[2], meta_full[2];
-  uint64_t drain;
+  uint64_t drain[2];
   Part parts[2];
   Meta meta[2];
 };
@@ -153,36 +161,14 @@ __device__ __forceinline__ bool part_ok(const TreeParams& p, const Part& a) {
 }
 
 // ------------------------------------------------------------------- waits
-// Bounded waits that also end when another role has aborted. Only the first
-// test is inlined: the loop that follows it is in one place, since the code of
-// this kernel is about as large as the instruction cache. The softmax warps
-// poll; the other roles, which wait most of the time, sleep in the test.
-template <bool kSleep>
-__device__ __noinline__ bool wait_more(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
-  const uint64_t t0 = global_timer_ns();
-  while (!(kSleep ? mbar_try_wait_sleep(bar, parity, 10000) : mbar_try_wait(bar, parity))) {
-    if (*abort_flag) return false;
-    if (global_timer_ns() - t0 > kWaitTimeoutNs) {
-      *abort_flag = 1;
-      return false;
-    }
-  }
-  return true;
-}
-__device__ __forceinline__ bool wait_sleep(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
-  return mbar_try_wait(bar, parity) || wait_more<true>(bar, parity, abort_flag);
-}
-__device__ __forceinline__ bool wait_poll(uint32_t bar, uint32_t parity, volatile int32_t* abort_flag) {
-  return mbar_try_wait(bar, parity) || wait_more<false>(bar, parity, abort_flag);
-}
-// The same for a warp in step, in the loops over blocks: few instructions, and
-// one outcome for the warp, so that its branches are uniform. A test returns
-// within about a hundred cycles, so 2^22 of them take some tenths of a second;
-// after that the role ends, and with it the other roles' waits.
+// A bounded wait of a warp in step: few instructions, and one outcome for the
+// warp, so that its branches are uniform. A test returns when the phase
+// completes or after about 1.4 us, so 2^17 of them take 0.2 s; then the role
+// ends and raises the abort flag, and the other roles' waits run out likewise.
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
   uint32_t left;
   asm volatile(
-      "{\n\t.reg .pred p;\n\tmov.b32 %0, 0x400000;\n"
+      "{\n\t.reg .pred p;\n\tmov.b32 %0, 0x20000;\n"
       "again:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "vote.sync.all.pred p, p, 0xffffffff;\n\t@p bra.uni done;\n\t"
       "sub.u32 %0, %0, 1;\n\tsetp.ne.u32 p, %0, 0;\n\t@p bra.uni again;\n"
@@ -191,6 +177,17 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
       : "r"(bar), "r"(parity)
       : "memory");
   return left != 0;
+}
+
+// Whether the phase has completed, asked ahead of the time it matters.
+__device__ __forceinline__ bool peek(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
 
 // What one elected lane of a warp in step issues: a block's eight pages by
@@ -371,18 +368,6 @@ __device__ __forceinline__ float scores_max32(const uint32_t (&sv)[32]) {
   return fmaxf(m[0], m[1]);
 }
 
-// 16 TMEM columns from the first or second half of v
-template <int at>
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16};" ::"r"(taddr),
-      "r"(v[at]), "r"(v[at + 1]), "r"(v[at + 2]), "r"(v[at + 3]), "r"(v[at + 4]), "r"(v[at + 5]), "r"(v[at + 6]),
-      "r"(v[at + 7]), "r"(v[at + 8]), "r"(v[at + 9]), "r"(v[at + 10]), "r"(v[at + 11]), "r"(v[at + 12]),
-      "r"(v[at + 13]), "r"(v[at + 14]), "r"(v[at + 15])
-      : "memory");
-}
-
 __device__ __forceinline__ void zero_smem16(uint32_t addr) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0u) : "memory");
 }
@@ -509,10 +494,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     mbar_init(bar(ln.o_free), 4);
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(ln.part_full[i]), 1);
-      mbar_init(bar(ln.part_empty[i]), 4 + 1);
+      mbar_init(bar(ln.part_empty[i]), 4 + 2);
       mbar_init(bar(ln.meta_full[i]), 1);
     }
-    mbar_init(bar(ln.drain), 1);
+    mbar_init(bar(ln.drain[0]), 1);
+    mbar_init(bar(ln.drain[1]), 1);
     st.abort_flag = 0;
     fence_barrier_init();
   }
@@ -544,14 +530,18 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   __syncthreads();
   tc_fence_after();
 
-  const int x = warp >= 4 ? (warp >> 2) - 1 : warp & 1;  // this warp's lane of the CTA
+  const int x = warp >= 8 ? (warp >> 2) - 2 : warp & 1;  // this warp's lane of the CTA
   Lane& ln = st.lane[x];
   const uint32_t sQ = base + x * kLaneBytes, sK = sQ + kQBytes, sV = sK + kKStages * kBlockBytes;
   const uint32_t tmem = st.tmem_base + x * 256;  // S at 0, O at 128, P at 192
   constexpr uint32_t kColO = 128, kColP = 192;
 
-  if ((warp & ~1) == 2) {
+  // Each role is one or two whole warpgroups; the softmax takes the registers
+  // that the others give back.
+  if (warp >= 4 && warp < 8) {
     // ------------------------------------------------------------- producer
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelperRegs));
+    const bool for_k = warp < 6;  // K, Q tiles and the parts; else V
     if (lane == 0) {
       prefetch_tensormap(&kmap);
       prefetch_tensormap(&vmap);
@@ -559,7 +549,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     }
     RingAt<kKStages> rk;
     RingAt<kVStages> rv;
-    uint32_t k_it = 0, v_it = 0;  // blocks issued
+    uint32_t it = 0;  // blocks issued
     int i = 0;
     bool ok = true;
 #pragma unroll 1
@@ -597,9 +587,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         a.slot = first && a.b1 == w.nb ? -1
                  : line                ? kTreeSoloSlots + (2 * (int)blockIdx.x + first) * 2 + x
                                        : 2 * (2 * (int)blockIdx.x + x) + first;
-        if (first && a.slot >= 0 && a.b1 > 0 && lane == 0) {
+        if (first && a.slot >= 0 && a.b1 > 0 && for_k && lane == 0) {
           // a cut tile whose first part is this one: its last piece and what the merge needs
-          const int last = (int)div_up(u + w.cost(), quota) - 1;
+          int last = line ? blockIdx.x : 2 * blockIdx.x + x;
+          for (int64_t end = u0 + quota; end < u + w.cost(); end += quota) ++last;
           p.cuts[line * 2 * gridDim.x + 2 * blockIdx.x + x] = make_int4(last, a.token, a.n_tok, a.kvh);
         }
         u += w.cost();
@@ -630,85 +621,85 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           return p.oob_row;
         };
         int ids_next = load_ids(0);
-        const uint32_t* rows = p.mask + (size_t)a.token * p.words;
-        const uint32_t* all = rows - (size_t)a.node * p.words;
-        const int L = a.len - a.ctx, mine = a.n_tok * p.words;
-        const uint32_t early = lane < mine ? __ldg(rows + lane) : 0u;
+        uint32_t early = 0;
         int early_pos = 0;
-        if (p.window > 0 && lane < a.n_tok) early_pos = __ldg(p.positions + a.token + lane);
-        const float sink = lane < g ? tree_sink(p, a.kvh * g + lane) : -INFINITY;
-        if (i >= 2 && !__all_sync(0xffffffffu, wait_sleep(bar(ln.part_empty[slot]), ((i >> 1) - 1) & 1, abort_flag))) {
-          ok = false;
-          break;
-        }
-        if (lane == 0) {
-          ln.parts[slot] = a;
-          mbar_arrive(bar(ln.part_full[slot]));
-        }
-        if (i >= 1 && !__all_sync(0xffffffffu, wait_sleep(bar(ln.q_empty), (i - 1) & 1, abort_flag))) {
-          ok = false;
-          break;
-        }
-        if (lane == 0) {
-          mbar_arrive_expect_tx(bar(ln.q_full), kQBytes);
-          tma_load_3d(sQ, &qmap, 0, a.kvh * g, a.token, bar(ln.q_full));
-        }
-        __syncwarp();
-        ++i;
-        // K of block b, then V of block b - 1
-        int y[kBlockPages], y_old[kBlockPages], at = 0;
-#pragma unroll 1
-        for (int b = 0; b <= n; ++b) {
-          if (b < n) {
-            if (!(b & 3)) {  // 32 pages: a lane each, the next ones' ids on their way
-              at = box_row(ids_next);
-              ids_next = load_ids((b >> 2) + 1);
-            }
-#pragma unroll
-            for (int j = 0; j < kBlockPages; ++j) y[j] = __shfl_sync(0xffffffffu, at, (b & 3) * kBlockPages + j);
-            ok = wait_warp(bar(ln.k_empty[rk.s]), rk.parity ^ 1);
-            if (!ok) break;
-            load_block_e(sK + rk.s * kBlockBytes, &kmap, y, bar(ln.k_full[rk.s]), pol);
-            rk.next();
-            ++k_it;
+        float sink = -INFINITY;
+        const uint32_t* rows = p.mask + (size_t)a.token * p.words;
+        const int mine = a.n_tok * p.words;
+        if (for_k) {
+          if (lane < mine) early = __ldg(rows + lane);
+          if (p.window > 0 && lane < a.n_tok) early_pos = __ldg(p.positions + a.token + lane);
+          if (lane < g) sink = tree_sink(p, a.kvh * g + lane);
+          ok = i < 2 || wait_warp(bar(ln.part_empty[slot]), ((i >> 1) - 1) & 1);
+          if (!ok) break;
+          if (lane == 0) {
+            ln.parts[slot] = a;
+            mbar_arrive(bar(ln.part_full[slot]));
           }
-          if (b > 0) {
+          __syncwarp();
+          ok = i < 1 || wait_warp(bar(ln.q_empty), (i - 1) & 1);
+          if (!ok) break;
+          if (lane == 0) {
+            mbar_arrive_expect_tx(bar(ln.q_full), kQBytes);
+            tma_load_3d(sQ, &qmap, 0, a.kvh * g, a.token, bar(ln.q_full));
+          }
+          __syncwarp();
+        }
+        ++i;
+        int at = 0;
+#pragma unroll 1
+        for (int b = 0; b < n; ++b) {
+          if (!(b & 3)) {  // 32 pages: a lane each, the next ones' ids on their way
+            at = box_row(ids_next);
+            ids_next = load_ids((b >> 2) + 1);
+          }
+          int y[kBlockPages];
+#pragma unroll
+          for (int j = 0; j < kBlockPages; ++j) y[j] = __shfl_sync(0xffffffffu, at, (b & 3) * kBlockPages + j);
+          if (!for_k) {
             ok = wait_warp(bar(ln.v_empty[rv.s]), rv.parity ^ 1);
             if (!ok) break;
-            load_block_e(sV + rv.s * kBlockBytes, &vmap, y_old, bar(ln.v_full[rv.s]), pol);
+            load_block_e(sV + rv.s * kBlockBytes, &vmap, y, bar(ln.v_full[rv.s]), pol);
             rv.next();
-            ++v_it;
-          } else {  // behind the first K block: what the softmax needs of the masks
-            Meta& m = ln.meta[slot];
-            auto first_key = [&](int pos) { return min(max(pos, a.ctx), a.len - 1) - p.window + 1; };
-#pragma unroll 1
-            for (int k = lane; k < mine; k += 32) m.mask[k] = k < 32 ? early : __ldg(rows + k);
-            if (p.window > 0)
-#pragma unroll 1
-              for (int k = lane; k < a.n_tok; k += 32)
-                m.lo[k] = first_key(k < 32 ? early_pos : __ldg(p.positions + a.token + k));
-            if (a.b1 * kBlockKeys + a.kb0 > a.ctx)  // the part reaches the nodes
-#pragma unroll 1
-              for (int c = 0; c < p.words; ++c) {
-                uint32_t any = 0;
-#pragma unroll 1
-                for (int k = lane; k < L; k += 32) any |= __ldg(all + (size_t)k * p.words + c);
-                any = __reduce_or_sync(0xffffffffu, any);
-                if (lane == 0) m.seen_by_any[c] = any;
-              }
-            if (lane < g) m.sinks[lane] = sink;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(ln.meta_full[slot]));
-            __syncwarp();
+            ++it;
+            continue;
           }
-#pragma unroll
-          for (int j = 0; j < kBlockPages; ++j) y_old[j] = y[j];
+          ok = wait_warp(bar(ln.k_empty[rk.s]), rk.parity ^ 1);
+          if (!ok) break;
+          load_block_e(sK + rk.s * kBlockBytes, &kmap, y, bar(ln.k_full[rk.s]), pol);
+          rk.next();
+          ++it;
+          if (b > 0) continue;
+          // behind the first K block: what the softmax needs of the masks
+          Meta& m = ln.meta[slot];
+          const uint32_t* all = rows - (size_t)a.node * p.words;
+          const int L = a.len - a.ctx;
+          auto first_key = [&](int pos) { return min(max(pos, a.ctx), a.len - 1) - p.window + 1; };
+#pragma unroll 1
+          for (int k = lane; k < mine; k += 32) m.mask[k] = k < 32 ? early : __ldg(rows + k);
+          if (p.window > 0)
+#pragma unroll 1
+            for (int k = lane; k < a.n_tok; k += 32)
+              m.lo[k] = first_key(k < 32 ? early_pos : __ldg(p.positions + a.token + k));
+          if (a.b1 * kBlockKeys + a.kb0 > a.ctx)  // the part reaches the nodes
+#pragma unroll 1
+            for (int c = 0; c < p.words; ++c) {
+              uint32_t any = 0;
+#pragma unroll 1
+              for (int k = lane; k < L; k += 32) any |= __ldg(all + (size_t)k * p.words + c);
+              any = __reduce_or_sync(0xffffffffu, any);
+              if (lane == 0) m.seen_by_any[c] = any;
+            }
+          if (lane < g) m.sinks[lane] = sink;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(ln.meta_full[slot]));
+          __syncwarp();
         }
         if (!ok) break;
       }
     }
     if (!ok && *abort_flag == 0) *abort_flag = 1;
-    if (ok && (i < 2 || __all_sync(0xffffffffu, wait_sleep(bar(ln.part_empty[i & 1]), ((i >> 1) - 1) & 1, abort_flag)))) {
+    if (ok && for_k && (i < 2 || wait_warp(bar(ln.part_empty[i & 1]), ((i >> 1) - 1) & 1))) {
       if (lane == 0) {  // no more parts
         ln.parts[i & 1].row = -1;
         mbar_arrive(bar(ln.part_full[i & 1]));
@@ -716,65 +707,63 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     }
     // after an abort: wait (bounded) for the copies still in flight
     if (*abort_flag && lane == 0) {
-      for (uint32_t it = k_it > kKStages ? k_it - kKStages : 0; it < k_it; ++it)
-        mbar_wait(bar(ln.k_full[it % kKStages]), (it / kKStages) & 1);
-      for (uint32_t it = v_it > kVStages ? v_it - kVStages : 0; it < v_it; ++it)
-        mbar_wait(bar(ln.v_full[it % kVStages]), (it / kVStages) & 1);
-      if (i > 0) mbar_wait(bar(ln.q_full), (i - 1) & 1);
+      const uint32_t stages = for_k ? kKStages : kVStages;
+      for (uint32_t k = it > stages ? it - stages : 0; k < it; ++k)
+        mbar_wait(bar(for_k ? ln.k_full[k % stages] : ln.v_full[k % stages]), (k / stages) & 1);
+      if (for_k && i > 0) mbar_wait(bar(ln.q_full), (i - 1) & 1);
     }
-  } else if (warp < 2) {
-    // ------------------------------------------------------------ MMA issue
+  } else if (warp < 4) {
+    // -------------------------------------------- MMA issue: S, or O, of a lane
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kHelperRegs));
     constexpr uint32_t idS = idesc_bf16(kTileRows, kBlockKeys, false, false);
     constexpr uint32_t idO = idesc_bf16(kTileRows, kHeadDim, false, true);
     constexpr uint64_t kStageStep = kBlockBytes / 16;
+    const bool for_s = warp < 2;
     const uint64_t kdesc0 = smem_desc_sw128(sK, 16, 1024), vdesc0 = smem_desc_sw128(sV, 1024, 1024);
     const uint64_t qd = smem_desc_sw128(sQ, 16, 1024);
     RingAt<kKStages> rk;
     RingAt<kVStages> rv;
-    uint32_t s_par = 1, p_par = 0;  // turns of s_free and p_full
+    uint32_t par = for_s ? 1 : 0;  // turn of s_free, or of p_full
     bool ok = true;
     for (int i = 0; ok; ++i) {
       const int slot = i & 1;
-      if (!wait_sleep(bar(ln.part_full[slot]), (i >> 1) & 1, abort_flag)) break;
-      if (ln.parts[slot].row < 0) break;
+      ok = wait_warp(bar(ln.part_full[slot]), (i >> 1) & 1);
+      if (!ok || ln.parts[slot].row < 0) break;
       const int n = ln.parts[slot].b1 - ln.parts[slot].b0;
-      if (!wait_sleep(bar(ln.q_full), i & 1, abort_flag)) break;
-      for (int b = 0; b <= n; ++b) {
-        // What the block loads deliver is waited for first, so that nothing
-        // lies between the softmax's arrivals and the MMAs they set off.
-        if (b < n) ok = wait_warp(bar(ln.k_full[rk.s]), rk.parity);
-        if (b >= 1) ok = ok && wait_warp(bar(ln.v_full[rv.s]), rv.parity);
-        if (!ok) break;
-        if (b < n) {  // S(b)
-          ok = wait_warp(bar(ln.s_free), s_par);
+      if (for_s) {
+        ok = wait_warp(bar(ln.q_full), i & 1);
+        for (int b = 0; b < n && ok; ++b) {
+          ok = wait_warp(bar(ln.k_full[rk.s]), rk.parity) && wait_warp(bar(ln.s_free), par);
           if (!ok) break;
           tc_fence_after();
           mma_scores_e(tmem, qd, kdesc0 + rk.s * kStageStep, idS, bar(ln.s_full), bar(ln.k_empty[rk.s]));
           if (b == n - 1) tc_commit_e(bar(ln.q_empty));
           rk.next();
-          s_par ^= 1;
+          par ^= 1;
         }
-        if (b >= 1) {  // O += P(b - 1) V(b - 1)
-          ok = wait_warp(bar(ln.p_full), p_par) && (b > 1 || i == 0 || wait_warp(bar(ln.o_free), (i - 1) & 1));
+      } else {
+        ok = i == 0 || wait_warp(bar(ln.o_free), (i - 1) & 1);
+        for (int b = 0; b < n && ok; ++b) {
+          ok = wait_warp(bar(ln.v_full[rv.s]), rv.parity) && wait_warp(bar(ln.p_full), par);
           if (!ok) break;
           tc_fence_after();
-          mma_values_e(tmem + kColO, tmem + kColP, vdesc0 + rv.s * kStageStep, idO, b > 1 ? 1u : 0u, bar(ln.o_ready),
+          mma_values_e(tmem + kColO, tmem + kColP, vdesc0 + rv.s * kStageStep, idO, b > 0 ? 1u : 0u, bar(ln.o_ready),
                        bar(ln.v_empty[rv.s]));
           rv.next();
-          p_par ^= 1;
+          par ^= 1;
         }
       }
-      if (!ok) {
-        if (*abort_flag == 0) *abort_flag = 1;
-        break;
-      }
+      if (!ok) break;
       if (lane == 0) mbar_arrive(bar(ln.part_empty[slot]));
+      __syncwarp();
     }
+    if (!ok && *abort_flag == 0) *abort_flag = 1;
     // MMAs still in flight (after an abort) must not outlive TMEM
-    tc_commit_e(bar(ln.drain));
-    mbar_wait(bar(ln.drain), 0);
+    tc_commit_e(bar(ln.drain[for_s]));
+    mbar_wait(bar(ln.drain[for_s]), 0);
   } else {
     // -------------------------------------------------------------- softmax
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
     const int wq = warp & 3, row = threadIdx.x & (kTileRows - 1);
     const uint32_t cS = tmem + ((uint32_t)(wq * 32) << 16), cO = cS + kColO, cP = cS + kColP;
     const int tok = row / g, head = row % g;
@@ -782,7 +771,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
     bool ok = true;
     for (int i = 0; ok; ++i) {
       const int slot = i & 1;
-      ok = __all_sync(0xffffffffu, wait_poll(bar(ln.part_full[slot]), (i >> 1) & 1, abort_flag));
+      ok = wait_warp(bar(ln.part_full[slot]), (i >> 1) & 1);
       if (!ok) break;
       const Part& a = ln.parts[slot];  // valid until part_empty; re-read where needed to save registers
       if (a.row < 0) break;
@@ -791,7 +780,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         *abort_flag = 2;
         break;
       }
-      ok = __all_sync(0xffffffffu, wait_poll(bar(ln.meta_full[slot]), (i >> 1) & 1, abort_flag));
+      ok = wait_warp(bar(ln.meta_full[slot]), (i >> 1) & 1);
       if (!ok) break;
       const int n = a.b1 - a.b0;
       const int my_node = min(tok, a.n_tok - 1);
@@ -805,7 +794,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       auto clear_dead = [&](bool dead) -> bool {
         if (!__any_sync(0xffffffffu, dead)) return true;
         const uint32_t s = cnt % kVStages;
-        if (!__all_sync(0xffffffffu, wait_poll(bar(ln.v_full[s]), (cnt / kVStages) & 1, abort_flag))) return false;
+        if (!wait_warp(bar(ln.v_full[s]), (cnt / kVStages) & 1)) return false;
         if (dead) {
 #pragma unroll
           for (int c = 0; c < 8; ++c) zero_smem16(sV + s * kBlockBytes + row * kRowBytes + c * 16);
@@ -818,12 +807,12 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           uint32_t seen[4];
           const bool dead =
               (kb > plain_hi || kb < plain_lo) && block_masks(p, a, ln.meta[slot], my_node, kb, wq, lane, seen);
-          ok = __all_sync(0xffffffffu, wait_poll(bar(ln.s_full), cnt & 1, abort_flag));
+          ok = wait_warp(bar(ln.s_full), cnt & 1);
           if (!ok) break;
           if (lane == 0) mbar_arrive(bar(ln.s_free));
           // in step with the other warps: one arrival per phase
           if (cnt >= 1) {
-            ok = __all_sync(0xffffffffu, wait_poll(bar(ln.o_ready), (cnt - 1) & 1, abort_flag));
+            ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
             if (!ok) break;
           }
           ok = clear_dead(dead);
@@ -838,18 +827,20 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           // own, small enough to stay in the instruction cache. Four chunks of
           // 32 scores, the next one's load in flight while one's weights are
           // made. Nothing is known of the scores before: weights up to 2^60 of
-          // the first three chunks are taken as they are (their row's sum shows
-          // it; else the block is done anew below), and what exceeds 2^8 is
-          // scaled down after the last.
+          // the first half are taken as they are (their row's sum shows it; else
+          // the block is done anew below), and what exceeds 2^8 is scaled down
+          // after the last. S is free for the next block's product before the
+          // second half's weights are made.
           if (!unset) {
             const int stop = min(n, b + (min(plain_hi, a.kb0 + (a.b1 - 1) * kBlockKeys) - kb) / kBlockKeys + 1);
             const uint64_t sc = pack_f32x2(p.scale_log2, p.scale_log2);
             if (kb < plain_lo || kb > plain_hi) goto general;
+            bool s_there = false;
             while (b < stop) {
               uint32_t sa[32], sb[32], pk[32];
               uint64_t sum[2] = {0, 0};
               const uint64_t mu = pack_f32x2(-m_ref, -m_ref);
-              ok = wait_warp(bar(ln.s_full), cnt & 1);
+              ok = __all_sync(0xffffffffu, s_there) || wait_warp(bar(ln.s_full), cnt & 1);
               if (!ok) break;
               tc_fence_after();
               tmem_ld32(cS, sa);
@@ -858,62 +849,63 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               weights32<0>(sa, sc, mu, sum, pk);
               tmem_ld_wait();
               tmem_ld32(cS + 64, sa);
+              const bool o_there = peek(bar(ln.o_ready), (cnt - 1) & 1);
               weights32<16>(sb, sc, mu, sum, pk);
+              tmem_ld_wait();
+              tmem_ld32(cS + 96, sb);
               if (cnt >= 1) {  // the P buffer was last read by the previous PV
-                ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
+                ok = __all_sync(0xffffffffu, o_there) || wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
               }
               tmem_st32(cP, pk);
-              tmem_ld_wait();
-              tmem_ld32(cS + 96, sb);
-              weights32<0>(sa, sc, mu, sum, pk);
               float l0 = sum_of(sum);
               tmem_ld_wait();
               if (__any_sync(0xffffffffu, !(l0 < 0x1p60f))) break;  // done anew below
               tc_fence_before();
               mbar_arrive_e(bar(ln.s_free));
               sum[0] = sum[1] = 0;
+              weights32<0>(sa, sc, mu, sum, pk);
               weights32<16>(sb, sc, mu, sum, pk);
-              tmem_st32(cP + 32, pk);
               float l1 = sum_of(sum);
               if (__any_sync(0xffffffffu, !(l0 + l1 < 256.f))) {
                 // some rows' reference rises by a whole number of octaves, so that scaling P is exact
                 float up = 0.f;
-                if (!(l0 + l1 < 256.f)) up = ceilf(fmaxf(__log2f(l0), scores_max32(sb) * p.scale_log2 - m_ref));
+                if (!(l0 + l1 < 256.f))
+                  up = ceilf(fmaxf(__log2f(l0), fmaxf(scores_max32(sa), scores_max32(sb)) * p.scale_log2 - m_ref));
                 const float f = ex2_approx(-up);
                 m_ref += up;
                 l *= f;
                 l0 *= f;
+                sum[0] = sum[1] = 0;  // the second half anew: its weights may have been infinite
+                weights32<0>(sa, sc, pack_f32x2(-m_ref, -m_ref), sum, pk);
+                weights32<16>(sb, sc, pack_f32x2(-m_ref, -m_ref), sum, pk);
+                l1 = sum_of(sum);
                 __syncwarp();
                 tmem_st_wait();
 #pragma unroll 1
-                for (int h = 0; h < 4; ++h) {
-                  const uint32_t at = h < 2 ? cP + 32 * h : cO + 32 * (h - 2);
-                  if (h >= 2 && b == 0) break;  // O holds another part's
+                for (int h = 0; h < 3; ++h) {  // P of the first half, and O
+                  const uint32_t at = h ? cO + 32 * (h - 1) : cP;
                   tmem_ld32(at, sa);
                   tmem_ld_wait();
 #pragma unroll
                   for (int e = 0; e < 32; ++e) {
                     const float2 w = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&sa[e]));
-                    sa[e] = h < 2 ? pack_bf16x2(w.x * f, w.y * f) : __float_as_uint(__uint_as_float(sa[e]) * f);
+                    sa[e] = h ? __float_as_uint(__uint_as_float(sa[e]) * f) : pack_bf16x2(w.x * f, w.y * f);
                   }
                   __syncwarp();
                   tmem_st32(at, sa);
                 }
-                tmem_st_wait();
-                sum[0] = sum[1] = 0;  // the last chunk anew: its weights may have been infinite
-                weights32<0>(sb, sc, pack_f32x2(-m_ref, -m_ref), sum, pk);
-                l1 = sum_of(sum);
-                __syncwarp();
-                tmem_st16<0>(cP + 48, pk);
               }
+              tmem_st32(cP + 32, pk);
+              const bool s_next = peek(bar(ln.s_full), (cnt + 1) & 1);
               l += l0 + l1;
               tmem_st_wait();
               tc_fence_before();
               __syncwarp();
               mbar_arrive_e(bar(ln.p_full));
               ++b, ++cnt, kb += kBlockKeys;
+              s_there = s_next;
             }
             if (!ok || b == n) break;
           }
@@ -922,7 +914,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           uint32_t seen[4];  // bit e of word c: this thread's node sees key kb + 32c + e
           bool dead = false;
           if (masked) dead = block_masks(p, a, ln.meta[slot], my_node, kb, wq, lane, seen);
-          ok = __all_sync(0xffffffffu, wait_poll(bar(ln.s_full), cnt & 1, abort_flag));
+          ok = wait_warp(bar(ln.s_full), cnt & 1);
           if (!ok) break;
           tc_fence_after();
           uint32_t sv[2][32], pk[32];
@@ -942,7 +934,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           }
           // the P buffer was last read by the previous PV
           if (cnt >= 1) {
-            ok = __all_sync(0xffffffffu, wait_poll(bar(ln.o_ready), (cnt - 1) & 1, abort_flag));
+            ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
             if (!ok) break;
             tc_fence_after();
           }
@@ -1003,7 +995,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       }
       if (!ok) break;
       // ---- end of the part: O / l and the log-sum-exp, 16 dims at a time
-      ok = __all_sync(0xffffffffu, wait_poll(bar(ln.o_ready), (cnt - 1) & 1, abort_flag));
+      ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
       if (!ok) break;
       tc_fence_after();
       if (busy) {
