@@ -24,7 +24,7 @@
 // Warps: 0, 1 issue S = Q K^T of lane 0, 1 (M 128, N 128, K 64) and 2, 3 issue
 // O += P V (M 128, N 64, K 128, P from TMEM): an issuing warp is held until the
 // tensor pipe takes its MMAs, and one warp for both had no time left in a block
-// (+ 2 % of time); 4, 5 bring K, the Q tiles, the parts and what the softmax
+// (2 % slower); 4, 5 bring K, the Q tiles, the parts and what the softmax
 // needs of their masks, 6, 7 bring V (TMA, one 2 KiB box per page); 8-11 /
 // 12-15 softmax of lane 0 / 1 (thread t owns row t & 127, a TMEM lane: running
 // max and sum in fp32, P to TMEM as bf16 - each weight rounded once, 2^-8
@@ -37,10 +37,10 @@
 // about 1650 cycles for a block of both lanes (1024 of exponentials at 8 a
 // clock; the same instructions without waits 1330, with barriers that are
 // always ready 1460). Its loop over plain blocks is kept apart from all that is
-// rare: with masks, first blocks and rescaling inside it, it took 2430, mostly
-// waiting for instructions. Measured on a GB300: 64 rows of 2k-16k keys with
-// 1-16 nodes 194 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 535 us (855
-// TFLOP/s), two rows of 49k-65k keys with 61 and 64 nodes 112 us (1050
+// rare: with masks, first blocks and rescaling inside it, it took 2430, much of
+// it waiting for instructions. Measured on a GB300: 64 rows of 2k-16k keys with
+// 1-16 nodes 194 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 555 us (820
+// TFLOP/s), two rows of 49k-65k keys with 61 and 64 nodes 114 us (1030
 // TFLOP/s), 384 rows in a window of 128 keys 100 us.
 //
 // Waits are bounded; one that runs out raises an abort flag, every role ends,
@@ -66,7 +66,6 @@ constexpr uint32_t kTmemCols = 512;
 constexpr int kCostItem = 5;  // a tile's set-up and end, in blocks
 constexpr int kWholeBlocks = 6;  // tiles of up to so many blocks are never cut
 constexpr int kMinQuota = 7;  // smallest piece worth a lane of its own
-constexpr float kRescale = 8.f;  // log2 units: P may reach 2^8 before O is rescaled
 
 struct Part {  // a run of key blocks of one tile
   int32_t row;                 // -1: no more parts
@@ -287,63 +286,10 @@ __device__ __forceinline__ void hide(uint32_t (&sv)[32], uint32_t seen) {
     if (!(seen >> e & 1u)) sv[e] = 0xff800000u;
 }
 
-__device__ __forceinline__ float scores_max(const uint32_t (&sv)[2][32]) {
-  float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-  for (int c = 0; c < 2; ++c)
-#pragma unroll
-    for (int e = 0; e < 32; e += 8)
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        m[k] = fmax3(m[k], __uint_as_float(sv[c][e + 2 * k]), __uint_as_float(sv[c][e + 2 * k + 1]));
-  return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
-}
-
-// pk = bf16(2^(s * scale - mu)); returns their fp32 sum (before rounding)
-__device__ __forceinline__ float weights(const uint32_t (&sv)[2][32], float scale_log2, float neg_mu,
-                                         uint32_t (&pk)[32]) {
-  const uint64_t sc = pack_f32x2(scale_log2, scale_log2), mu = pack_f32x2(neg_mu, neg_mu);
-  uint64_t sum[2] = {0, 0};
-#pragma unroll
-  for (int c = 0; c < 2; ++c)
-#pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-      const uint64_t x = fma2((uint64_t)sv[c][e] | ((uint64_t)sv[c][e + 1] << 32), sc, mu);
-      const float p0 = ex2_approx(lo_f32(x)), p1 = ex2_approx(hi_f32(x));
-      sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pack_f32x2(p0, p1));
-      pk[c * 16 + e / 2] = pack_bf16x2(p0, p1);
-    }
-  const uint64_t s = add2(sum[0], sum[1]);
-  return lo_f32(s) + hi_f32(s);
-}
-
-// Weights of 64 scores against the reference m_ref (log2 units). A sum below
-// 2^8 shows that no weight exceeds 2^8, so the maximum is only taken when it
-// does not (or before the first reference): then m_ref rises if the maximum
-// exceeds it by more than kRescale, and alpha takes the factor for earlier
-// weights.
-__device__ __forceinline__ float chunk_weights(const uint32_t (&sv)[2][32], float scale_log2, float& m_ref,
-                                               float& alpha, uint32_t (&pk)[32]) {
-  bool take_max = m_ref == -INFINITY, last = false;
-  for (;;) {  // at most twice
-    if (take_max) {
-      const float mx = scores_max(sv) * scale_log2;
-      if (mx > m_ref + kRescale) {
-        alpha *= ex2_approx(m_ref - mx);  // 0 before the first reference
-        m_ref = mx;
-      }
-      last = true;
-    }
-    const float sum = weights(sv, scale_log2, m_ref == -INFINITY ? 0.f : -m_ref, pk);
-    if (last || sum < 256.f) return sum;
-    take_max = true;
-  }
-}
-
 // pk[at ..] = bf16(2^(s * scale - mu)) of 32 scores; their fp32 sum (before
 // rounding) goes to sum.
 template <int at>
-__device__ __forceinline__ void weights32(const uint32_t (&sv)[32], uint64_t sc, uint64_t mu, uint64_t (&sum)[2],
+__device__ __forceinline__ void weights(const uint32_t (&sv)[32], uint64_t sc, uint64_t mu, uint64_t (&sum)[2],
                                         uint32_t (&pk)[32]) {
 #pragma unroll
   for (int e = 0; e < 32; e += 2) {
@@ -358,7 +304,7 @@ __device__ __forceinline__ float sum_of(const uint64_t (&sum)[2]) {
   return lo_f32(s) + hi_f32(s);
 }
 
-__device__ __forceinline__ float scores_max32(const uint32_t (&sv)[32]) {
+__device__ __forceinline__ float scores_max(const uint32_t (&sv)[32]) {
   float m[2] = {-INFINITY, -INFINITY};
 #pragma unroll
   for (int e = 0; e < 32; e += 4)
@@ -368,36 +314,41 @@ __device__ __forceinline__ float scores_max32(const uint32_t (&sv)[32]) {
   return fmaxf(m[0], m[1]);
 }
 
+template <int at>
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[32]) {  // 16 TMEM columns from v[at ..]
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16};" ::"r"(taddr),
+      "r"(v[at]), "r"(v[at + 1]), "r"(v[at + 2]), "r"(v[at + 3]), "r"(v[at + 4]), "r"(v[at + 5]), "r"(v[at + 6]),
+      "r"(v[at + 7]), "r"(v[at + 8]), "r"(v[at + 9]), "r"(v[at + 10]), "r"(v[at + 11]), "r"(v[at + 12]),
+      "r"(v[at + 13]), "r"(v[at + 14]), "r"(v[at + 15])
+      : "memory");
+}
+
 __device__ __forceinline__ void zero_smem16(uint32_t addr) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0u) : "memory");
 }
 
-// What the masks say about the block of keys at kb: seen[c], the keys kb + 32c ..
-// that the thread's node (of the tile) sees; returns whether the slot
-// kb + 32 wq + lane holds a V row that no node of the row sees.
-__device__ __forceinline__ bool block_masks(const TreeParams& p, const Part& a, const Meta& m, int node, int kb, int wq,
-                                            int lane, uint32_t (&seen)[4]) {
-  const int ctx = a.ctx, len = a.len, j = kb + 32 * wq + lane;
-  const int n0 = kb - ctx, w0 = n0 >> 5;  // node of the block's first key, and its mask word
-  const int lo = p.window > 0 ? m.lo[node] : 0;
-  uint32_t mw[5] = {0, 0, 0, 0, 0};
-  bool dead = j < a.key_begin;
-  if (n0 > -kBlockKeys) {
-    auto word = [&](const uint32_t* w, int i) { return i >= 0 && i < p.words ? w[i] : 0u; };
-#pragma unroll
-    for (int c = 0; c < 5; ++c) mw[c] = word(m.mask + node * p.words, w0 + c);
-    const uint32_t any =
-        __funnelshift_r(word(m.seen_by_any, w0 + wq), word(m.seen_by_any, w0 + wq + 1), n0 & 31);
-    // past the row's end only its last page holds anything: later pages arrive as zeros
-    dead |= j >= len ? j < ((len + kPage - 1) & ~(kPage - 1)) : j >= ctx && !(any >> lane & 1u);
+// Which of the keys k0 .. k0 + 31 the thread's node (of the tile) sees.
+__device__ __forceinline__ uint32_t seen_keys(const TreeParams& p, const Part& a, const Meta& m, int node, int k0) {
+  const int lo = p.window > 0 ? m.lo[node] : 0, n0 = k0 - a.ctx;
+  uint32_t seen = low_bits(-n0) & ~low_bits(lo - k0);
+  if (n0 > -32) {  // the nodes n0 .. are bits of two mask words
+    const uint32_t* w = m.mask + node * p.words;
+    const int i = n0 >> 5;
+    const uint32_t first = i >= 0 && i < p.words ? w[i] : 0u, second = i + 1 < p.words ? w[i + 1] : 0u;
+    seen |= __funnelshift_r(first, second, n0 & 31) & low_bits(a.len - k0);
   }
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int k0 = kb + 32 * c;
-    seen[c] = (low_bits(ctx - k0) & ~low_bits(lo - k0)) |
-              (__funnelshift_r(mw[c], mw[c + 1], n0 & 31) & low_bits(len - k0));
-  }
-  return dead;
+  return seen;
+}
+
+// Whether slot j holds a V row that no node of the row sees.
+__device__ __forceinline__ bool dead_slot(const Part& a, const Meta& m, int j) {
+  const int n = j - a.ctx;
+  if (n < 0) return j < a.key_begin;
+  // past the row's end only its last page holds anything: later pages arrive as zeros
+  if (j >= a.len) return j < ((a.len + kPage - 1) & ~(kPage - 1));
+  return !(m.seen_by_any[n >> 5] >> (n & 31) & 1u);
 }
 
 __device__ __forceinline__ float tree_sink(const TreeParams& p, int h) {
@@ -804,9 +755,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       };
       if (!busy) {  // none of this warp's rows is a query: it only keeps the barriers and clears V rows
         for (int b = 0; b < n; ++b, ++cnt, kb += kBlockKeys) {
-          uint32_t seen[4];
-          const bool dead =
-              (kb > plain_hi || kb < plain_lo) && block_masks(p, a, ln.meta[slot], my_node, kb, wq, lane, seen);
+          const bool dead = (kb > plain_hi || kb < plain_lo) && dead_slot(a, ln.meta[slot], kb + row);
           ok = wait_warp(bar(ln.s_full), cnt & 1);
           if (!ok) break;
           if (lane == 0) mbar_arrive(bar(ln.s_free));
@@ -846,11 +795,11 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               tmem_ld32(cS, sa);
               tmem_ld_wait();
               tmem_ld32(cS + 32, sb);
-              weights32<0>(sa, sc, mu, sum, pk);
+              weights<0>(sa, sc, mu, sum, pk);
               tmem_ld_wait();
               tmem_ld32(cS + 64, sa);
               const bool o_there = peek(bar(ln.o_ready), (cnt - 1) & 1);
-              weights32<16>(sb, sc, mu, sum, pk);
+              weights<16>(sb, sc, mu, sum, pk);
               tmem_ld_wait();
               tmem_ld32(cS + 96, sb);
               if (cnt >= 1) {  // the P buffer was last read by the previous PV
@@ -865,21 +814,21 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               tc_fence_before();
               mbar_arrive_e(bar(ln.s_free));
               sum[0] = sum[1] = 0;
-              weights32<0>(sa, sc, mu, sum, pk);
-              weights32<16>(sb, sc, mu, sum, pk);
+              weights<0>(sa, sc, mu, sum, pk);
+              weights<16>(sb, sc, mu, sum, pk);
               float l1 = sum_of(sum);
               if (__any_sync(0xffffffffu, !(l0 + l1 < 256.f))) {
                 // some rows' reference rises by a whole number of octaves, so that scaling P is exact
                 float up = 0.f;
                 if (!(l0 + l1 < 256.f))
-                  up = ceilf(fmaxf(__log2f(l0), fmaxf(scores_max32(sa), scores_max32(sb)) * p.scale_log2 - m_ref));
-                const float f = ex2_approx(-up);
+                  up = fmaxf(0.f, ceilf(fmaxf(__log2f(l0), fmaxf(scores_max(sa), scores_max(sb)) * p.scale_log2 - m_ref)));
+                const float f = __uint_as_float((127u - min((uint32_t)up, 127u)) << 23);  // 2^-up, 0 from 2^-127 on
                 m_ref += up;
                 l *= f;
                 l0 *= f;
                 sum[0] = sum[1] = 0;  // the second half anew: its weights may have been infinite
-                weights32<0>(sa, sc, pack_f32x2(-m_ref, -m_ref), sum, pk);
-                weights32<16>(sb, sc, pack_f32x2(-m_ref, -m_ref), sum, pk);
+                weights<0>(sa, sc, pack_f32x2(-m_ref, -m_ref), sum, pk);
+                weights<16>(sb, sc, pack_f32x2(-m_ref, -m_ref), sum, pk);
                 l1 = sum_of(sum);
                 __syncwarp();
                 tmem_st_wait();
@@ -910,80 +859,80 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             if (!ok || b == n) break;
           }
         general:
+          // ---- any other block: a chunk at a time in loops that are not
+          // unrolled (in a short window every block comes this way, and its
+          // time is that of fetching the code)
           const bool masked = kb > plain_hi || kb < plain_lo;
-          uint32_t seen[4];  // bit e of word c: this thread's node sees key kb + 32c + e
-          bool dead = false;
-          if (masked) dead = block_masks(p, a, ln.meta[slot], my_node, kb, wq, lane, seen);
+          const bool dead = masked && dead_slot(a, ln.meta[slot], kb + row);
           ok = wait_warp(bar(ln.s_full), cnt & 1);
           if (!ok) break;
-          tc_fence_after();
-          uint32_t sv[2][32], pk[32];
-          tmem_ld32(cS, sv[0]);
-          tmem_ld32(cS + 32, sv[1]);
-          tmem_ld_wait();
-          float alpha = 1.f, l0 = 0.f;
-          if (masked) {
-            hide(sv[0], seen[0]);
-            hide(sv[1], seen[1]);
-          }
-          if (!masked || __any_sync(0xffffffffu, (seen[0] | seen[1]) != 0u)) {
-            l0 = chunk_weights(sv, p.scale_log2, m_ref, alpha, pk);
-          } else {  // no row of the warp sees a key of this half
-#pragma unroll
-            for (int e = 0; e < 32; ++e) pk[e] = 0u;
-          }
           // the P buffer was last read by the previous PV
           if (cnt >= 1) {
             ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
             if (!ok) break;
-            tc_fence_after();
           }
-          __syncwarp();  // TMEM moves need the warp in step, also after the first block's maximum
-          tmem_st32(cP, pk);
-          tmem_ld32(cS + 64, sv[0]);
-          tmem_ld32(cS + 96, sv[1]);
-          tmem_ld_wait();
+          tc_fence_after();
+          uint32_t sv[32], pk[32];
+          auto scores = [&](int c) -> bool {  // chunk c, what is not seen at -inf; false if no row sees any of it
+            const uint32_t seen = masked ? seen_keys(p, a, ln.meta[slot], my_node, kb + 32 * c) : 0xffffffffu;
+            if (!__any_sync(0xffffffffu, seen != 0u)) return false;
+            tmem_ld32(cS + 32 * c, sv);
+            tmem_ld_wait();
+            hide(sv, seen);
+            return true;
+          };
+          const float m_start = m_ref;
+          float lb;  // the block's sum
+          bool redo = false;
+          for (;;) {  // at most twice
+            const uint64_t sc = pack_f32x2(p.scale_log2, p.scale_log2);
+            uint64_t sum[2] = {0, 0};
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              __syncwarp();  // TMEM moves need the warp in step
+              if (scores(c)) {
+                if (unset) {  // a row's reference is the maximum of the first chunk it sees something of
+                  const float mx = scores_max(sv) * p.scale_log2;
+                  if (m_ref == -INFINITY) m_ref = mx;
+                }
+                const float neg_mu = m_ref == -INFINITY ? 0.f : -m_ref;
+                weights<0>(sv, sc, pack_f32x2(neg_mu, neg_mu), sum, pk);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) pk[e] = 0u;
+              }
+              tmem_st16<0>(cP + 16 * c, pk);
+            }
+            lb = sum_of(sum);
+            if (redo || !__any_sync(0xffffffffu, !(lb < 256.f))) break;
+            // far beyond the reference: it becomes the block's maximum, and the block is done anew
+            redo = true;
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              __syncwarp();
+              if (scores(c)) mx = fmaxf(mx, scores_max(sv));
+            }
+            mx *= p.scale_log2;
+            if (!(lb < 256.f) && mx > m_ref) m_ref = mx;
+            tmem_st_wait();
+          }
+          const float alpha = m_ref == m_start ? 1.f : ex2_approx(m_start - m_ref);  // of what earlier blocks left
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(bar(ln.s_free));
-          if (masked) {
-            hide(sv[0], seen[2]);
-            hide(sv[1], seen[3]);
-          }
-          float a1 = 1.f, l1 = 0.f;
-          if (!masked || __any_sync(0xffffffffu, (seen[2] | seen[3]) != 0u)) {
-            l1 = chunk_weights(sv, p.scale_log2, m_ref, a1, pk);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) pk[e] = 0u;
-          }
-          if (__any_sync(0xffffffffu, a1 != 1.f)) {  // the reference rose: rescale the first half's weights too
-            tmem_st_wait();
-            uint32_t pv[32];
-            tmem_ld32(cP, pv);
-            tmem_ld_wait();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&pv[e]));
-              pv[e] = pack_bf16x2(f.x * a1, f.y * a1);
-            }
-            tmem_st32(cP, pv);
-            l0 *= a1;
-            alpha *= a1;
-          }
-          tmem_st32(cP + 32, pk);
-          l = l * alpha + (l0 + l1);
+          mbar_arrive_e(bar(ln.s_free));
+          l = l * alpha + lb;
           ok = clear_dead(dead);
           if (!ok) break;
           if (b > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
-            uint32_t ov[32];
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
-              tmem_ld32(cO + 32 * h, ov);
+              __syncwarp();
+              tmem_ld32(cO + 32 * h, sv);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * alpha);
-              tmem_st32(cO + 32 * h, ov);
+              for (int e = 0; e < 32; ++e) sv[e] = __float_as_uint(__uint_as_float(sv[e]) * alpha);
+              tmem_st32(cO + 32 * h, sv);
             }
           }
           unset = __any_sync(0xffffffffu, m_ref == -INFINITY);

@@ -145,6 +145,32 @@ def test_peaked_and_large_scores():
 
 
 @gpu
+@pytest.mark.parametrize("window", [0, 700])
+@pytest.mark.parametrize("at", [(394, 450), (460, 520), (511, 700), (0, 63), (64, 130), (890, 899)])
+@pytest.mark.parametrize("levels", [(0, 10, 16), (0, 20, 60), (0, 90, 110), (0, 200, 240), (0, 240, 0), (240, 0, 100)])
+def test_scores_that_leap(levels, at, window):
+    # keys from at[0] and at[1] on score level / 2 higher (nats; level / 8, or falling, in other rows of a warp): the
+    # running reference is far too low in either half of a block, by up to 2^170
+    b = TreeBatch([900, 903], [20, 5], 16, 2, 71, window=window)
+    q, k = b.qt.clone(), b.kt.clone()
+    q[:, :, 0] = torch.tensor([4.0, 1.0, -4.0, 0.0]).repeat(7)[: q.shape[0], None]
+    for r in range(2):
+        for p in range(max(0, int(b.ctx[r]) - window + 1) if window else 0, int(b.ctx[r])):
+            k[b.bt[r, p // 16], :, p % 16, 0] = float(levels[sum(p >= x for x in at)])
+    b.qt, b.q, b.kt, b.k = q, q.double().numpy(), k, k.double().numpy()
+    from paper_2608_22167_gb300 import mcpu
+
+    out, lse, ws, _ = _run(b)
+    assert mcpu.mcpu_read_device_status(ws) == (0, 0)
+    ro, rl, mag = b.reference()
+    # |q k| sums to at most 4 * 240 + 64 * 4 * 4; the reference and lse are fp32 numbers of up to 2^8
+    ds = 64 * 2.0 ** -24 * 0.125 * (4 * 240 + 64 * 16) + 2.0 ** -15
+    got = out.double().cpu().numpy()
+    assert np.all(np.abs(got - ro) <= 1.01 * 2.0 ** -8 * (mag + np.abs(ro)) + 2 * ds * mag + 1e-6)
+    assert np.max(np.abs(lse.double().cpu().numpy() - rl)) <= 1e-4 + ds
+
+
+@gpu
 def test_positions_outside_the_tree_count_as_the_nearest_inside():
     b = TreeBatch([50, 80], [6, 9], 8, 2, 61, window=20)
     b.positions = b.positions + np.where(np.arange(15) % 2, 1000, -1000)
