@@ -85,6 +85,13 @@ def test_long_rows_are_split(ctx, n):
 
 
 @gpu
+@pytest.mark.parametrize("ctx,n,window", [(756, 12, 0), (757, 12, 0), (5003, 32, 720), (5011, 32, 721), (5003, 32, 737)])
+def test_the_longest_rows_that_are_not_split(ctx, n, window):
+    # six blocks of 128 keys: 48 pages, or nodes and window and a page
+    _check(TreeBatch([ctx, ctx - 700, ctx], [n, n, 1], 16, 2, ctx + window, window=window))
+
+
+@gpu
 def test_rows_without_nodes_and_many_rows():
     rng = np.random.default_rng(5)
     lens = rng.integers(0, 4, 300)
