@@ -39,9 +39,10 @@
 // always ready 1460). Its loop over plain blocks is kept apart from all that is
 // rare: with masks, first blocks and rescaling inside it, it took 2430, much of
 // it waiting for instructions. Measured on a GB300: 64 rows of 2k-16k keys with
-// 1-16 nodes 194 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 555 us (820
-// TFLOP/s), two rows of 49k-65k keys with 61 and 64 nodes 114 us (1030
-// TFLOP/s), 384 rows in a window of 128 keys 100 us.
+// 1-16 nodes 194 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 535-560 us
+// (815-855 TFLOP/s, by the clock that the power limit leaves), two rows of
+// 49k-65k keys with 61 and 64 nodes 112-115 us (1030-1050 TFLOP/s), 384 rows in
+// a window of 128 keys 98 us, four rows of up to 308 keys 9.8 us.
 //
 // Waits are bounded; one that runs out raises an abort flag, every role ends,
 // and TMEM is freed after the issuers' MMAs have drained.
