@@ -39,10 +39,10 @@
 // always ready 1460). Its loop over plain blocks is kept apart from all that is
 // rare: with masks, first blocks and rescaling inside it, it took 2430, much of
 // it waiting for instructions. Measured on a GB300: 64 rows of 2k-16k keys with
-// 1-16 nodes 194 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 535-560 us
+// 1-16 nodes 192 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 535-560 us
 // (815-855 TFLOP/s, by the clock that the power limit leaves), two rows of
 // 49k-65k keys with 61 and 64 nodes 112-115 us (1030-1050 TFLOP/s), 384 rows in
-// a window of 128 keys 98 us, four rows of up to 308 keys 9.8 us.
+// a window of 128 keys 93 us, four rows of up to 308 keys 9.2 us.
 //
 // Waits are bounded; one that runs out raises an abort flag, every role ends,
 // and TMEM is freed after the issuers' MMAs have drained.
@@ -68,7 +68,7 @@ constexpr int kCostItem = 5;  // a tile's set-up and end, in blocks
 constexpr int kWholeBlocks = 6;  // tiles of up to so many blocks are never cut
 constexpr int kMinQuota = 7;  // smallest piece worth a lane of its own
 
-struct Part {  // a run of key blocks of one tile
+struct alignas(16) Part {  // a run of key blocks of one tile
   int32_t row;                 // -1: no more parts
   int32_t token, n_tok, node;  // first query token, tokens, first node of the tile
   int32_t ctx, len, kvh;
@@ -743,7 +743,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const int slot = i & 1;
       ok = wait_warp(bar(ln.part_full[slot]), (i >> 1) & 1);
       if (!ok) break;
-      const Part& a = ln.parts[slot];  // valid until part_empty; re-read where needed to save registers
+      const Part a = ln.parts[slot];
       if (a.row < 0) break;
       if (!part_ok(p, a)) {
         atomicOr(p.status, kStatusPlanOverflow);
@@ -962,55 +962,53 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         }
       }
       if (!ok) break;
-      // ---- end of the part: O / l and the log-sum-exp, 16 dims at a time
+      // ---- end of the part: O / l and the log-sum-exp. O and the part's slot are
+      // free for the next part as soon as they are in registers, before anything
+      // is written (window of 128 keys: 97 -> 93 us). All warps load O, those
+      // without rows too: a condition here costs the loops above registers.
+      const bool writes = busy && tok < a.n_tok;
+      const int h = a.kvh * g + head;
+      const float sink = ln.meta[slot].sinks[head];
+      float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;  // l < 2^8 keys: within its range, 2 ulp
+      float lse2 = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
+      if (a.slot < 0 && sink > -INFINITY) inv = finish_with_sink(m_ref, l, sink, &lse2);
+      __syncwarp();
       ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
       if (!ok) break;
       tc_fence_after();
-      if (busy) {
-        const bool writes = tok < a.n_tok;
-        const int part_slot = a.slot, h = a.kvh * g + head;
-        const float sink = ln.meta[slot].sinks[head];
-        float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;  // l < 2^8 keys: within its range, 2 ulp
-        float lse2 = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
-        if (part_slot < 0 && sink > -INFINITY) inv = finish_with_sink(m_ref, l, sink, &lse2);
-        const size_t orow = (size_t)(a.token + tok) * Hq + h;
-        const size_t prow = (size_t)max(part_slot, 0) * kTileRows + row;
-#pragma unroll 1
-        for (int c = 0; c < kHeadDim / 32; ++c) {
-          __syncwarp();  // TMEM moves need the warp in step
-          uint32_t ov[32];
-          tmem_ld32(cO + 32 * c, ov);
-          tmem_ld_wait();
-          if (writes && part_slot < 0) {
-            uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kHeadDim) + 4 * c;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              uint32_t o[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                o[e] = pack_bf16x2(__uint_as_float(ov[8 * k + 2 * e]) * inv, __uint_as_float(ov[8 * k + 2 * e + 1]) * inv);
-              dst[k] = make_uint4(o[0], o[1], o[2], o[3]);
-            }
-          } else if (writes) {
-            float4* dst = reinterpret_cast<float4*>(p.o_part + prow * kHeadDim) + 8 * c;
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              dst[k] = make_float4(__uint_as_float(ov[4 * k]) * inv, __uint_as_float(ov[4 * k + 1]) * inv,
-                                   __uint_as_float(ov[4 * k + 2]) * inv, __uint_as_float(ov[4 * k + 3]) * inv);
-          }
-        }
-        if (writes) {
-          if (part_slot < 0)
-            p.lse[orow] = lse2 * 0.69314718055994531f;
-          else
-            p.lse_part[prow] = lse2;
-        }
-      }
+      uint32_t ov[2][32];
+      tmem_ld32(cO, ov[0]);
+      tmem_ld32(cO + 32, ov[1]);
+      tmem_ld_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(bar(ln.o_free));
-        mbar_arrive(bar(ln.part_empty[slot]));
+      mbar_arrive_e(bar(ln.o_free));
+      mbar_arrive_e(bar(ln.part_empty[slot]));
+      const size_t orow = (size_t)(a.token + tok) * Hq + h, prow = (size_t)max(a.slot, 0) * kTileRows + row;
+      if (writes && a.slot < 0) {
+        uint4* dst = reinterpret_cast<uint4*>(p.out + orow * kHeadDim);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          uint32_t o[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t(&v)[32] = ov[k >> 2];
+            const int i = 8 * (k & 3) + 2 * e;
+            o[e] = pack_bf16x2(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv);
+          }
+          dst[k] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+        p.lse[orow] = lse2 * 0.69314718055994531f;
+      } else if (writes) {
+        float4* dst = reinterpret_cast<float4*>(p.o_part + prow * kHeadDim);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const uint32_t(&v)[32] = ov[k >> 3];
+          const int i = 4 * (k & 7);
+          dst[k] = make_float4(__uint_as_float(v[i]) * inv, __uint_as_float(v[i + 1]) * inv,
+                               __uint_as_float(v[i + 2]) * inv, __uint_as_float(v[i + 3]) * inv);
+        }
+        p.lse_part[prow] = lse2;
       }
     }
     if (!ok && *abort_flag == 0) *abort_flag = 1;
