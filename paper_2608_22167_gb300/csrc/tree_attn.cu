@@ -920,6 +920,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) pk[e] = 0u;
               }
+              __syncwarp();
               tmem_st16<0>(cP + 16 * c, pk);
             }
             lb = sum_of(sum);
@@ -934,6 +935,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
             }
             mx *= p.scale_log2;
             if (!(lb < 256.f) && mx > m_ref) m_ref = mx;
+            __syncwarp();
             tmem_st_wait();
           }
           const float alpha = m_ref == m_start ? 1.f : ex2_approx(m_start - m_ref);  // of what earlier blocks left
