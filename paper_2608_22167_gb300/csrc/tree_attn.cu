@@ -829,7 +829,10 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
               tmem_st32(cP, pk);
               float l0 = sum_of(sum);
               tmem_ld_wait();
-              if (__any_sync(0xffffffffu, !(l0 < 0x1p60f))) break;  // done anew below
+              if (__any_sync(0xffffffffu, !(l0 < 0x1p60f))) {  // done anew below
+                tmem_st_wait();  // over the same columns: stores of one warp keep no order by themselves
+                break;
+              }
               tc_fence_before();
               mbar_arrive_e(bar(ln.s_free));
               sum[0] = sum[1] = 0;

@@ -317,3 +317,32 @@ def test_host_checks():
     assert call(bytes=need - 1) == 3
     assert call(dims=mcpu.Dims(4, 9, 19, 34, 8, 2, 128, 16)) == 2
     assert call(dims=mcpu.Dims(0, 0, 19, 34, 8, 2, 64, 16)) == 0  # nothing to do
+
+
+@gpu
+def test_blocks_given_up_halfway_are_the_same_every_time():
+    # from some key on a row's scores lie 48 nats above all before: that block's first weights are stored before their
+    # sum shows it, and the block is done anew over the same columns
+    rng = np.random.default_rng(131)
+    ctx = rng.integers(600, 1500, 40)
+    b = TreeBatch(ctx, rng.integers(1, 17, 40), 16, 2, 131)
+    q, k = b.qt.clone(), b.kt.clone()
+    q[:, :, 0] = 4.0
+    for r in range(40):
+        at = int(rng.integers(256, ctx[r] - 129))
+        for p in range(int(ctx[r])):
+            k[b.bt[r, p // 16], :, p % 16, 0] = 96.0 if p >= at else 0.0
+    b.qt, b.q, b.kt, b.k = q, q.double().numpy(), k, k.double().numpy()
+    from paper_2608_22167_gb300 import mcpu
+
+    out, lse, ws, _ = _run(b)
+    ro, rl, mag = b.reference()
+    # |q k| sums to at most 4 * 96 + 64 * 4 * 4; the reference and lse are fp32 numbers of up to 2^8
+    ds = 64 * 2.0 ** -24 * 0.125 * (4 * 96 + 64 * 16) + 2.0 ** -15
+    got = out.double().cpu().numpy()
+    assert np.all(np.abs(got - ro) <= 1.01 * 2.0 ** -8 * (mag + np.abs(ro)) + 2 * ds * mag + 1e-6)
+    assert np.max(np.abs(lse.double().cpu().numpy() - rl)) <= 1e-4 + ds
+    for _ in range(20):
+        again, lse2, _, _ = _run(b, ws=ws)
+        assert torch.equal(again, out) and torch.equal(lse2, lse)
+    assert mcpu.mcpu_read_device_status(ws) == (0, 0)
