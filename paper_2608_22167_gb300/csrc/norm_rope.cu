@@ -35,7 +35,7 @@ __device__ __forceinline__ int find_row(const int32_t* qsl, int num_seqs, int t,
   int lo = 0, n = num_seqs;
   while (n > 1) {
     const int step = (n + 31) >> 5, at = lane * step;
-    const uint32_t le = __ballot_sync(0xffffffffu, at < n && __ldg(qsl + lo + min(at, n - 1)) <= t);
+    const uint32_t le = __ballot_sync(0xffffffffu, at < n && qsl[lo + min(at, n - 1)] <= t);
     const int k = max(__popc(le) - 1, 0) * step;
     lo += k;
     n = min(step, n - k);
@@ -44,7 +44,9 @@ __device__ __forceinline__ int find_row(const int32_t* qsl, int num_seqs, int t,
 }
 
 // Four floats at a 4-byte aligned address, in one load where `vec` says that
-// it is 16-byte aligned.
+// it is 16-byte aligned. For weights and angles only: no kernel of this library
+// writes them, so they are constant from before this grid is placed, as the
+// non-coherent path asks; positions, lengths and tables need not be.
 __device__ __forceinline__ void load4(const float* p, bool vec, float* out) {
   if (vec) {
     const float4 v = __ldg(reinterpret_cast<const float4*>(p));
@@ -99,7 +101,7 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
   load4(p.wq + 4 * j, vec, w);
   load4(p.wq + 32 + 4 * j, vec, w + 4);
   // the angles come by a given position, or by the slot once the row is known
-  int pos = p.positions ? __ldg(p.positions + t) : -1;
+  int pos = p.positions ? p.positions[t] : -1;
   float c[4], s[4];
   auto load_angles = [&]() {
     const float* ang = p.cos_sin + (size_t)pos * kHeadDim + 4 * j;
@@ -108,7 +110,7 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
   };
   if (pos >= 0 && pos < p.max_position) load_angles();
   const int r = find_row(p.qsl, p.num_seqs, t, lane);
-  const int q0 = __ldg(p.qsl + r), q1 = __ldg(p.qsl + r + 1), S = __ldg(p.seq_lens + r);
+  const int q0 = p.qsl[r], q1 = p.qsl[r + 1], S = p.seq_lens[r];
   const int L = q1 - q0, slot = S - L + (t - q0);
   const bool fits = L >= 1 && S >= L && S <= p.max_pages * kPage && t >= q0 && t < q1;
   if (!p.positions) pos = slot;
@@ -116,7 +118,7 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
     if (lane == 0) atomicOr(p.status, kStatusBadLengths);
     return;
   }
-  const int page = __ldg(p.block_table + (size_t)r * p.max_pages + slot / kPage);
+  const int page = p.block_table[(size_t)r * p.max_pages + slot / kPage];
   const bool page_ok = page >= 0 && page < p.num_pages;
   if (!page_ok && lane == 0) atomicOr(p.status, kStatusBadPage);
   if (!p.positions) load_angles();

@@ -7,7 +7,8 @@
 //
 // Every kernel is launched programmatically: its blocks may be placed while the
 // grid before it still runs, and wait for that grid's end before they read or
-// write anything (begin()). These calls are short and come in rows, so the
+// write anything (begin()), by ordinary loads: the non-coherent ones are for
+// what stays constant as long as the kernel is there. These calls are short and come in rows, so the
 // launches would otherwise be a good part of their time (384 forks released,
 // made again and copied in 24 pools: 50 -> 41 us).
 #include "tree_round.cuh"
@@ -47,7 +48,7 @@ __device__ __forceinline__ bool last_block(int32_t* ticket, int n) {
 
 // A fork whose rows and length are valid; *len its source's length.
 __device__ __forceinline__ bool fork_valid(const PageParams& p, int f, int* len) {
-  const int src = __ldg(p.src_rows + f), dst = __ldg(p.dst_rows + f);
+  const int src = p.src_rows[f], dst = p.dst_rows[f];
   if (src < 0 || src >= p.num_seqs || dst < 0 || dst >= p.num_seqs || src == dst) return false;
   *len = __ldcg(p.seq_lens + src);
   return *len >= 0 && *len <= p.max_pages * kPage;
@@ -70,7 +71,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const PageParams p) 
 #pragma unroll
   for (int i = 0; i < kForkEarly; ++i) {
     const int j = threadIdx.x + i * kForkThreads;
-    early[i] = ok && j < S / kPage ? p.block_table[(size_t)__ldg(p.src_rows + f) * p.max_pages + j] : -1;
+    early[i] = ok && j < S / kPage ? p.block_table[(size_t)p.src_rows[f] * p.max_pages + j] : -1;
   }
   int before = 0;
   if (partial) {
@@ -86,7 +87,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const PageParams p) 
   __syncthreads();
   const int rank = s_rank;
   if (ok) {
-    const int src = __ldg(p.src_rows + f), dst = __ldg(p.dst_rows + f);
+    const int src = p.src_rows[f], dst = p.dst_rows[f];
     const int full = S / kPage;
     const int32_t* from = p.block_table + (size_t)src * p.max_pages;
     int32_t* to = p.block_table + (size_t)dst * p.max_pages;
@@ -253,7 +254,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(const PoolPtrs
                                                                   int32_t* status) {
   begin();
   const int f = blockIdx.x / num_pools, pool = blockIdx.x % num_pools;
-  const int src = __ldg(copy_src + f), dst = __ldg(copy_dst + f);
+  const int src = copy_src[f], dst = copy_dst[f];
   if (src < 0 || dst < 0 || src == dst) return;
   if (src >= num_pages || dst >= num_pages) {
     if (threadIdx.x == 0) atomicOr(status, kStatusBadPage);
@@ -283,8 +284,8 @@ __global__ void __launch_bounds__(kCompactThreads) compact_kernel(const CompactP
   begin();
   const int r = blockIdx.x;
   __shared__ int s_src[kCompactMoves], s_dst[kCompactMoves];  // page * 16 + slot
-  const int q0 = __ldg(p.qsl + r), q1 = __ldg(p.qsl + r + 1);
-  const int L = q1 - q0, S = __ldg(p.seq_lens + r), n = __ldg(p.taken + r);
+  const int q0 = p.qsl[r], q1 = p.qsl[r + 1];
+  const int L = q1 - q0, S = p.seq_lens[r], n = p.taken[r];
   const int C = S - L;
   const int32_t* path = p.path + (size_t)r * p.max_accept;
   const int32_t* bt = p.block_table + (size_t)r * p.max_pages;
@@ -294,11 +295,11 @@ __global__ void __launch_bounds__(kCompactThreads) compact_kernel(const CompactP
     bad = kStatusBadLengths;
   } else {
     for (int i = threadIdx.x; i < n; i += kCompactThreads) {
-      const int a = __ldg(path + i), prev = i > 0 ? __ldg(path + i - 1) : -1;
+      const int a = path[i], prev = i > 0 ? path[i - 1] : -1;
       if (a <= prev || a < i || a >= L) {
         bad |= kStatusBadLengths;
       } else if (a != i && p.num_pools > 0) {
-        const int from = __ldg(bt + (C + a) / kPage), to = __ldg(bt + (C + i) / kPage);
+        const int from = bt[(C + a) / kPage], to = bt[(C + i) / kPage];
         if (from < 0 || from >= p.num_pages || to < 0 || to >= p.num_pages) bad |= kStatusBadPage;
       }
     }
@@ -314,9 +315,9 @@ __global__ void __launch_bounds__(kCompactThreads) compact_kernel(const CompactP
     const int m = min(kCompactMoves, n - i0);
     __syncthreads();
     for (int i = threadIdx.x; i < m; i += kCompactThreads) {
-      const int a = __ldg(path + i0 + i), from = C + a, to = C + i0 + i;
-      s_src[i] = a == i0 + i ? -1 : __ldg(bt + from / kPage) * kPage + from % kPage;
-      s_dst[i] = __ldg(bt + to / kPage) * kPage + to % kPage;
+      const int a = path[i0 + i], from = C + a, to = C + i0 + i;
+      s_src[i] = a == i0 + i ? -1 : bt[from / kPage] * kPage + from % kPage;
+      s_dst[i] = bt[to / kPage] * kPage + to % kPage;
     }
     __syncthreads();
     for (int w = threadIdx.x; w < np * vecs; w += kCompactThreads) {

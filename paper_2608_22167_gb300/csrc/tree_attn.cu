@@ -46,6 +46,9 @@
 //
 // Waits are bounded; one that runs out raises an abort flag, every role ends,
 // and TMEM is freed after the issuers' MMAs have drained.
+//
+// What the caller gives is read by ordinary loads (not the non-coherent ones):
+// the grid may be placed while the one that writes it still runs.
 #include "tcgen05.cuh"
 #include "tree_round.cuh"
 
@@ -117,9 +120,9 @@ struct RowGeom {
 // Geometry of row r; false (L = 0: nothing wrong) if it has no work, with the
 // status bits of what is wrong.
 __device__ __forceinline__ bool row_geom(const TreeParams& p, int r, RowGeom* w, int32_t* bits) {
-  w->q0 = __ldg(p.qsl + r);
-  w->L = __ldg(p.qsl + r + 1) - w->q0;
-  w->S = __ldg(p.seq_lens + r);
+  w->q0 = p.qsl[r];
+  w->L = p.qsl[r + 1] - w->q0;
+  w->S = p.seq_lens[r];
   if (w->L == 0) return false;
   if (w->q0 < 0 || w->L < 0 || w->L > p.total_q - w->q0 || w->S < w->L || w->S > p.max_pages * kPage) {
     *bits |= kStatusBadLengths;
@@ -430,7 +433,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
   // no cut tile begins in this CTA's pieces, as far as is known
   if (threadIdx.x < 4)
     p.cuts[(threadIdx.x >> 1) * 2 * gridDim.x + 2 * blockIdx.x + (threadIdx.x & 1)] = make_int4(-1, 0, 0, 0);
-  const bool ends = __ldg(p.qsl) == 0 && __ldg(p.qsl + B) == p.total_q;
+  const bool ends = p.qsl[0] == 0 && p.qsl[B] == p.total_q;
   // ---- the lines: prefix[l][r] = cost of line l's tiles in the rows before r
   {
     const int per = (B + kTreeThreads - 1) / kTreeThreads;
@@ -583,7 +586,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         const int page_end = min((a.len + kPage - 1) / kPage, pg0 + n * kBlockPages);
         auto load_ids = [&](int c) -> int {  // page id of page pg0 + 32c + lane
           const int lp = pg0 + 32 * c + lane;
-          return lp < page_end ? __ldg(bt_row + lp) : -2;
+          return lp < page_end ? bt_row[lp] : -2;
         };
         auto box_row = [&](int id) -> int {  // where the page's box begins; nothing past the last page
           if (id >= 0 && id < p.num_pages) return (id * Hkv + a.kvh) * kPage;
@@ -597,8 +600,8 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         const uint32_t* rows = p.mask + (size_t)a.token * p.words;
         const int mine = a.n_tok * p.words;
         if (for_k) {
-          if (lane < mine) early = __ldg(rows + lane);
-          if (p.window > 0 && lane < a.n_tok) early_pos = __ldg(p.positions + a.token + lane);
+          if (lane < mine) early = rows[lane];
+          if (p.window > 0 && lane < a.n_tok) early_pos = p.positions[a.token + lane];
           if (lane < g) sink = tree_sink(p, a.kvh * g + lane);
           ok = i < 2 || wait_warp(bar(ln.part_empty[slot]), ((i >> 1) - 1) & 1);
           if (!ok) break;
@@ -646,17 +649,17 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           const int L = a.len - a.ctx;
           auto first_key = [&](int pos) { return min(max(pos, a.ctx), a.len - 1) - p.window + 1; };
 #pragma unroll 1
-          for (int k = lane; k < mine; k += 32) m.mask[k] = k < 32 ? early : __ldg(rows + k);
+          for (int k = lane; k < mine; k += 32) m.mask[k] = k < 32 ? early : rows[k];
           if (p.window > 0)
 #pragma unroll 1
             for (int k = lane; k < a.n_tok; k += 32)
-              m.lo[k] = first_key(k < 32 ? early_pos : __ldg(p.positions + a.token + k));
+              m.lo[k] = first_key(k < 32 ? early_pos : p.positions[a.token + k]);
           if (a.b1 * kBlockKeys + a.kb0 > a.ctx)  // the part reaches the nodes
 #pragma unroll 1
             for (int c = 0; c < p.words; ++c) {
               uint32_t any = 0;
 #pragma unroll 1
-              for (int k = lane; k < L; k += 32) any |= __ldg(all + (size_t)k * p.words + c);
+              for (int k = lane; k < L; k += 32) any |= all[(size_t)k * p.words + c];
               any = __reduce_or_sync(0xffffffffu, any);
               if (lane == 0) m.seen_by_any[c] = any;
             }
