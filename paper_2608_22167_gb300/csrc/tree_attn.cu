@@ -977,8 +977,9 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
       const bool writes = busy && tok < a.n_tok;
       const int h = a.kvh * g + head;
       const float sink = ln.meta[slot].sinks[head];
-      float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;  // l < 2^8 keys: within its range, 2 ulp
-      float lse2 = l > 0.f ? m_ref + __log2f(l) : -INFINITY;
+      // nothing seen: l is 0; a NaN among what is seen: l is NaN, and so are O and the log-sum-exp
+      float inv = l == 0.f ? 0.f : __fdividef(1.f, l);  // l < 2^8 keys: within its range, 2 ulp
+      float lse2 = l == 0.f ? -INFINITY : m_ref + __log2f(l);
       if (a.slot < 0 && sink > -INFINITY) inv = finish_with_sink(m_ref, l, sink, &lse2);
       __syncwarp();
       ok = wait_warp(bar(ln.o_ready), (cnt - 1) & 1);
@@ -1078,11 +1079,11 @@ __global__ void __launch_bounds__(kMergeThreads) merge_tree_kernel(const TreePar
         o.w = o.w * f + wt * q[e].w;
       }
     }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;  // a part's NaN reaches the sum, and stays
     const size_t orow = (size_t)(cut.y + r / g) * Hq + h;
     reinterpret_cast<uint2*>(p.out + orow * kHeadDim)[d] =
         make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-    if (d == 0) p.lse[orow] = sum > 0.f ? (m + __log2f(sum)) * 0.69314718055994531f : -INFINITY;
+    if (d == 0) p.lse[orow] = sum == 0.f ? -INFINITY : (m + __log2f(sum)) * 0.69314718055994531f;
   }
 }
 

@@ -346,3 +346,34 @@ def test_blocks_given_up_halfway_are_the_same_every_time():
         again, lse2, _, _ = _run(b, ws=ws)
         assert torch.equal(again, out) and torch.equal(lse2, lse)
     assert mcpu.mcpu_read_device_status(ws) == (0, 0)
+
+
+@gpu
+@pytest.mark.parametrize("sinks", [False, True])
+@pytest.mark.parametrize("ctx,window", [(70, 0), (400, 0), (6000, 0), (6000, 3000), (6000, 100)])
+@pytest.mark.parametrize("what", ["q", "k", "node", "all k", "inf"])
+def test_nan_reaches_what_sees_it_and_nothing_else(what, ctx, window, sinks):
+    # the longer rows are cut into parts, the shorter ones are not: both give what the formula gives
+    b = TreeBatch([ctx, 50, ctx], [9, 3, 20], 16, 2, 5 + ctx, window=window)
+    rng = np.random.default_rng(ctx)
+    if what == "q":
+        b.qt[2, 3, 7] = b.qt[10, 15, 0] = float("nan")
+    elif what == "node":  # seen by its descendants
+        p = ctx + 1
+        b.kt[b.bt[0, p // 16], 1, p % 16, 5] = float("nan")
+    else:
+        for p in (range(max(0, ctx - window + 1) if window else 0, ctx + 9) if what == "all k" else [ctx - 40]):
+            b.kt[b.bt[0, p // 16], 0, p % 16, 3] = float("inf" if what == "inf" else "nan")
+    b.q, b.k = b.qt.double().numpy(), b.kt.double().numpy()
+    sk = rng.standard_normal(16).astype(np.float32) if sinks else None
+    out, lse, ws, _ = _run(b, sk)
+    from paper_2608_22167_gb300 import mcpu
+
+    assert mcpu.mcpu_read_device_status(ws) == (0, 0)
+    with np.errstate(invalid="ignore"):
+        ro, rl, mag = b.reference(None if sk is None else sk.astype(np.float64))
+    bad = np.isnan(rl)
+    assert bad.any() and not bad.all() and np.array_equal(np.isnan(ro).all(2), bad)
+    assert torch.isnan(out.cpu()[bad]).all() and torch.isnan(lse.cpu()[bad]).all()
+    good = torch.from_numpy(~bad)
+    assert_tree_close(out.cpu()[good], lse.cpu()[good], (ro[~bad], rl[~bad], mag[~bad]))
