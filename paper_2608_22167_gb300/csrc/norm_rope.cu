@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kNormThreads, 4) norm_rope_kernel(const NormRo
         load4(p.wk + 32 + 4 * j, vec, w + 4);
       }
       const float mean = ss * (1.f / kHeadDim) + p.eps;
-      const float inv = mean > 0.f ? rsqrtf(mean) : 0.f;  // 2 ulp
+      const float inv = mean == 0.f ? 0.f : rsqrtf(mean);  // 2 ulp; a NaN of the row reaches all of it
       if (row < Hq + Hkv) {
         float y[8];
 #pragma unroll

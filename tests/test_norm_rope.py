@@ -228,3 +228,24 @@ def test_binding_checks():
                 dict(q=q.transpose(0, 1).contiguous().transpose(0, 1)), dict(positions=z(4, dtype=torch.int64))):
         with pytest.raises(ValueError):
             mcpu.mcpu_norm_rope_kv_append(**dict(args, **bad))
+
+
+@gpu
+@pytest.mark.parametrize("tokens", [11, 3000])
+def test_a_nan_reaches_all_of_its_head_and_nothing_else(tokens):
+    tab = torch.from_numpy(W.rope_table(5000)).cuda()
+    w = np.ones(64)
+    c = _case([3, 500], [tokens - 1, 1], 16, 2, 3, False, False)
+    good = _call(c, w, w, 1e-6, tab).clone()
+    kept = c["kc"].clone(), c["vc"].clone()
+    for part, token, head, dim in ((0, 4, 2, 5), (0, tokens - 1, 15, 63), (1, 4, 1, 40)):
+        c["parts"][part][token, head, dim] = float("nan")
+    out = _call(c, w, w, 1e-6, tab)
+    bad = torch.zeros(tokens, 16, dtype=torch.bool)
+    bad[4, 2] = bad[tokens - 1, 15] = True
+    assert torch.isnan(out.cpu()[bad]).all() and torch.equal(out.cpu()[~bad], good.cpu()[~bad])
+    page, slot = c["bt"][0, 7 // 16], 7
+    assert torch.isnan(c["kc"][page, 1, slot]).all()
+    c["kc"][page, 1, slot] = kept[0][page, 1, slot]
+    assert torch.equal(c["kc"], kept[0]) and torch.equal(c["vc"], kept[1])
+    assert int(c["status"].item()) == 0
