@@ -459,8 +459,10 @@ mcpu_status mcpu_norm_rope_kv_append(const void* q, int64_t q_stride, const void
  * a window (NULL otherwise is fine) and must lie in [C_r, S_r): a value
  * outside counts as the nearest inside. The K/V rows of nodes are read from
  * the pages, so append them first. Slots that no node of the row sees may
- * hold anything; a node key that some nodes see and others do not has to be
- * finite, as its value reaches the others with weight 0.
+ * hold anything, and pages of such slots alone may be missing; a key (a node,
+ * or a context key at the edge of the windows) that some nodes see and others
+ * do not has to be finite, as its value reaches the others with weight 0. A
+ * NaN score makes the node's out and lse NaN.
  * Long rows are split over the SMs and merged by log-sum-exp in a fixed
  * order: the same inputs give the same bits on the same device. workspace:
  * mcpu_tree_workspace_size(dims) bytes, 256-byte aligned; its first word is

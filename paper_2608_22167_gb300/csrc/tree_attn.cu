@@ -75,13 +75,14 @@ struct alignas(16) Part {  // a run of key blocks of one tile
   int32_t row;                 // -1: no more parts
   int32_t token, n_tok, node;  // first query token, tokens, first node of the tile
   int32_t ctx, len, kvh;
-  int32_t kb0, key_begin;  // key of block 0 (a page start), first key any node can see
+  int32_t kb0;  // key of block 0 (a page start)
   int32_t b0, b1;
   int32_t slot;  // partial slot, or -1: the part is the whole tile
 };
 
 struct Meta {  // what the softmax needs to know of a part's nodes
   uint32_t seen_by_any[MCPU_MAX_TREE_WORDS];  // nodes that some node of the row sees
+  int32_t first;                              // first context key that some node of the row sees
   float sinks[kMaxGroup];                     // base-2 sink logits of the kv head's query heads
   int32_t lo[kTileRows];                      // first context key in each node's window
   uint32_t mask[kTileRows * MCPU_MAX_TREE_WORDS];  // [node of the tile][words]
@@ -353,7 +354,7 @@ __device__ __forceinline__ uint32_t seen_keys(const TreeParams& p, const Part& a
 // Whether slot j holds a V row that no node of the row sees.
 __device__ __forceinline__ bool dead_slot(const Part& a, const Meta& m, int j) {
   const int n = j - a.ctx;
-  if (n < 0) return j < a.key_begin;
+  if (n < 0) return j < m.first;
   // past the row's end only its last page holds anything: later pages arrive as zeros
   if (j >= a.len) return j < ((a.len + kPage - 1) & ~(kPage - 1));
   return !(m.seen_by_any[n >> 5] >> (n & 31) & 1u);
@@ -555,7 +556,6 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
         a.ctx = w.C;
         a.len = w.S;
         a.kb0 = w.kb0;
-        a.key_begin = w.key_begin;
         const int first = a.b0 == 0 ? 1 : 0;
         a.slot = first && a.b1 == w.nb ? -1
                  : line                ? kTreeSoloSlots + (2 * (int)blockIdx.x + first) * 2 + x
@@ -588,20 +588,32 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           const int lp = pg0 + 32 * c + lane;
           return lp < page_end ? bt_row[lp] : -2;
         };
-        auto box_row = [&](int id) -> int {  // where the page's box begins; nothing past the last page
+        const int L = a.len - a.ctx;
+        const int32_t* row_pos = p.positions + (a.token - a.node);  // with a window only
+        auto first_key = [&](int pos) { return min(max(pos, a.ctx), a.len - 1) - p.window + 1; };
+        // where the page's box begins; nothing past the last page, nor for a missing page that no node sees (nodes
+        // may all lie past C, where the first block begins)
+        auto box_row = [&](int id, int lp) -> int {
           if (id >= 0 && id < p.num_pages) return (id * Hkv + a.kvh) * kPage;
-          if (id != -2) atomicOr(p.status, kStatusBadPage);
+          bool seen = id != -2;
+          if (seen && p.window > 0) {
+            seen = false;
+#pragma unroll 1
+            for (int k = 0; k < L && !seen; ++k) seen = lp * kPage + kPage > min(first_key(row_pos[k]), a.ctx);
+          }
+          if (seen) atomicOr(p.status, kStatusBadPage);
           return p.oob_row;
         };
         int ids_next = load_ids(0);
         uint32_t early = 0;
-        int early_pos = 0;
+        int early_pos = 0, early_row_pos = 0;
         float sink = -INFINITY;
         const uint32_t* rows = p.mask + (size_t)a.token * p.words;
         const int mine = a.n_tok * p.words;
         if (for_k) {
           if (lane < mine) early = rows[lane];
-          if (p.window > 0 && lane < a.n_tok) early_pos = p.positions[a.token + lane];
+          if (p.window > 0 && lane < a.n_tok) early_pos = row_pos[a.node + lane];
+          if (p.window > 0 && lane < L) early_row_pos = row_pos[lane];
           if (lane < g) sink = tree_sink(p, a.kvh * g + lane);
           ok = i < 2 || wait_warp(bar(ln.part_empty[slot]), ((i >> 1) - 1) & 1);
           if (!ok) break;
@@ -623,7 +635,7 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
 #pragma unroll 1
         for (int b = 0; b < n; ++b) {
           if (!(b & 3)) {  // 32 pages: a lane each, the next ones' ids on their way
-            at = box_row(ids_next);
+            at = box_row(ids_next, pg0 + kBlockPages * b + lane);
             ids_next = load_ids((b >> 2) + 1);
           }
           int y[kBlockPages];
@@ -646,14 +658,18 @@ __global__ void __launch_bounds__(kTreeThreads, 1)
           // behind the first K block: what the softmax needs of the masks
           Meta& m = ln.meta[slot];
           const uint32_t* all = rows - (size_t)a.node * p.words;
-          const int L = a.len - a.ctx;
-          auto first_key = [&](int pos) { return min(max(pos, a.ctx), a.len - 1) - p.window + 1; };
 #pragma unroll 1
           for (int k = lane; k < mine; k += 32) m.mask[k] = k < 32 ? early : rows[k];
-          if (p.window > 0)
+          int first = 0;
+          if (p.window > 0) {
 #pragma unroll 1
-            for (int k = lane; k < a.n_tok; k += 32)
-              m.lo[k] = first_key(k < 32 ? early_pos : p.positions[a.token + k]);
+            for (int k = lane; k < a.n_tok; k += 32) m.lo[k] = first_key(k < 32 ? early_pos : row_pos[a.node + k]);
+            first = a.ctx;
+#pragma unroll 1
+            for (int k = lane; k < L; k += 32) first = min(first, first_key(k < 32 ? early_row_pos : row_pos[k]));
+            first = __reduce_min_sync(0xffffffffu, first);
+          }
+          if (lane == 0) m.first = first;
           if (a.b1 * kBlockKeys + a.kb0 > a.ctx)  // the part reaches the nodes
 #pragma unroll 1
             for (int c = 0; c < p.words; ++c) {

@@ -377,3 +377,37 @@ def test_nan_reaches_what_sees_it_and_nothing_else(what, ctx, window, sinks):
     assert torch.isnan(out.cpu()[bad]).all() and torch.isnan(lse.cpu()[bad]).all()
     good = torch.from_numpy(~bad)
     assert_tree_close(out.cpu()[good], lse.cpu()[good], (ro[~bad], rl[~bad], mag[~bad]))
+
+
+@gpu
+@pytest.mark.parametrize("hq,hkv", [(16, 2), (2, 2)])
+@pytest.mark.parametrize("ctx,n,window", [(600, 60, 64), (130, 6, 20), (50, 40, 1), (6000, 200, 1500), (6000, 256, 100)])
+def test_keys_that_no_node_sees_may_hold_anything(ctx, n, window, hq, hkv):
+    # positions that all lie past the context's end: the first keys of the first node's window are seen by none, and
+    # whole pages of them may be missing
+    b = TreeBatch([ctx, 3, ctx + 7], [n, 2, n], hq, hkv, ctx + n, window=window)
+    rng = np.random.default_rng(n)
+    for r in (0, 2):
+        t = int(b.qsl[r])
+        past = n // 2
+        b.positions[t:t + n] = b.ctx[r] + rng.integers(past, n, n)
+        b.positions[t + n // 3] = b.ctx[r] + past
+        first = int(b.ctx[r]) + past - window + 1  # of the keys that are seen
+        for p in range(max(0, int(b.ctx[r]) - window + 1), min(first, int(b.ctx[r]))):
+            for x in (b.kt, b.vt):
+                x[b.bt[r, p // 16], :, p % 16] = float("nan")
+        b.bt[r, :max(0, min(first, int(b.ctx[r]))) // 16] = -1
+    _check(b)
+
+
+@gpu
+def test_a_missing_page_that_a_node_sees_is_reported():
+    from paper_2608_22167_gb300 import mcpu
+
+    # keys from 560 on are seen; or no context key at all, and page 37 holds the first nodes
+    for window, past, lost, code in ((50, 9, 34, 0), (50, 9, 35, 5), (3, 9, 36, 0), (3, 9, 37, 5)):
+        b = TreeBatch([600], [30], 16, 2, 3, window=window)
+        b.positions[:] = 600 + np.arange(30) % 20 + past
+        b.bt[0, lost] = -1
+        _, _, ws, _ = _run(b)
+        assert mcpu.mcpu_read_device_status(ws)[0] == code
