@@ -254,6 +254,19 @@ mcpu_status mcpu_grow_block_tables(int32_t* block_table, const int32_t* seq_lens
                                    mcpu_stream_t stream);
 
 /*
+ * The same for rows whose first context_lens[r] tokens (device int32
+ * [num_seqs]) are in the cache already: only the pages that the tokens from
+ * there on open are filled, from entry ceil(context_lens[r] / 16) on. Negative
+ * entries before it stay, so that pages released before a sliding window
+ * (mcpu_shrink_block_tables) are not taken again, nor is a page of the context
+ * that is missing replaced by an empty one. A negative length is reported
+ * (MCPU_ERR_BAD_LENGTHS); one above S_r leaves nothing to fill.
+ */
+mcpu_status mcpu_grow_block_tables_from(int32_t* block_table, const int32_t* seq_lens, const int32_t* context_lens,
+                                        const mcpu_dims* dims, const int32_t* free_pages, int32_t* free_count,
+                                        int32_t* status_word, mcpu_stream_t stream);
+
+/*
  * fp8 KV pages (a storage variant for the memory-bound decode; not in the
  * paper, which keeps K/V in bf16). Each (token, kv head) row x of D = 64
  * values is stored as 64 e4m3 codes (OCP "e4m3fn": bias 7, largest 448,
@@ -406,7 +419,7 @@ mcpu_status mcpu_host_stage_sync(mcpu_host_stage* stage);
  * accepted path stays in the cache. The L_r query tokens of row r are the
  * nodes of its tree, at slots C_r .. S_r - 1 of its cache, C_r = S_r - L_r
  * (its context length). The calls of a round, per layer unless noted:
- *   mcpu_grow_block_tables       (once) pages for the drafted tokens
+ *   mcpu_grow_block_tables_from  (once) pages for the drafted tokens
  *   mcpu_norm_rope_kv_append     q/k norm, rotation at the nodes' positions, K/V to the pages
  *   mcpu_tree_attention_forward  every node over the context and its ancestors
  *   mcpu_compact_kv              (once, all layers) accepted nodes' K/V rows to the front
@@ -516,13 +529,15 @@ mcpu_status mcpu_compact_kv(void* const* pools, int32_t num_pools, const int32_t
  * first), be distinct, and not be a src row of the same call. If the stack
  * runs empty the tail entry stays -1 (MCPU_ERR_POOL_EXHAUSTED).
  *
- * mcpu_shrink_block_tables: the reverse of mcpu_grow_block_tables. Every
+ * mcpu_shrink_block_tables: the reverse of mcpu_grow_block_tables_from. Every
  * entry >= 0 of row r at or past ceil(S_r / 16), and with sliding_window
  * W > 0 every entry whose keys no query at a position >= S_r can see
  * (page < (S_r - W + 1) / 16), is released and set to -1: page_refs - 1, or,
  * for the last holder, back to the stack. S_r = 0 frees the row. Pages that
  * return are pushed in ascending order. A page that is released more often
- * than it is held is reported (MCPU_ERR_BAD_PAGE).
+ * than it is held is reported (MCPU_ERR_BAD_PAGE). Rows whose first pages
+ * were released before a window grow with mcpu_grow_block_tables_from:
+ * mcpu_grow_block_tables would fill those entries again.
  *
  * mcpu_copy_pages: for each f < num_copies with copy_src[f], copy_dst[f] >= 0,
  * copies page copy_src[f] to page copy_dst[f] in every pool: page_bytes

@@ -12,7 +12,8 @@
 // grow_tables_kernel: every logical page a row needs for its S_r tokens and
 // whose block-table entry is negative gets a page popped from a device stack
 // of free page ids; entries already set (shared prompt pages, earlier pages)
-// are left alone. An empty stack sets kStatusPoolExhausted.
+// are left alone. An empty stack sets kStatusPoolExhausted. With the lengths
+// that are in the cache already, entries of their pages stay as they are too.
 #include "common.cuh"
 
 namespace mcpu {
@@ -129,20 +130,20 @@ cudaError_t launch_rope_append(void* q, const void* k_new, const void* v_new, vo
 
 // one warp per row: lanes take the row's logical pages 32 at a time
 __global__ void __launch_bounds__(256) grow_tables_kernel(int32_t* block_table, const int32_t* seq_lens,
-                                                          int32_t num_seqs, int32_t max_pages,
-                                                          const int32_t* free_pages, int32_t* free_count,
+                                                          const int32_t* context_lens, int32_t num_seqs,
+                                                          int32_t max_pages, const int32_t* free_pages, int32_t* free_count,
                                                           int32_t* status) {
   const int lane = threadIdx.x & 31;
   const int r = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
   if (r >= num_seqs) return;
-  const int S = seq_lens[r];
-  if (S < 0 || S > max_pages * kPage) {
+  const int S = seq_lens[r], C = context_lens ? context_lens[r] : 0;
+  if (S < 0 || S > max_pages * kPage || C < 0) {
     if (lane == 0) atomicOr(status, kStatusBadLengths);
     return;
   }
   const int need = (S + kPage - 1) / kPage;
   int32_t* row = block_table + (size_t)r * max_pages;
-  for (int j = lane; j < need; j += 32) {
+  for (int j = (min(C, S) + kPage - 1) / kPage + lane; j < need; j += 32) {
     if (row[j] >= 0) continue;
     const int top = atomicSub(free_count, 1);
     if (top <= 0) {
@@ -154,13 +155,13 @@ __global__ void __launch_bounds__(256) grow_tables_kernel(int32_t* block_table, 
   }
 }
 
-cudaError_t launch_grow_tables(int32_t* block_table, const int32_t* seq_lens, int32_t num_seqs, int32_t max_pages,
-                               const int32_t* free_pages, int32_t* free_count, int32_t* status,
-                               cudaStream_t stream) {
+cudaError_t launch_grow_tables(int32_t* block_table, const int32_t* seq_lens, const int32_t* context_lens,
+                               int32_t num_seqs, int32_t max_pages, const int32_t* free_pages, int32_t* free_count,
+                               int32_t* status, cudaStream_t stream) {
   const int warps_per_cta = 8;
   const int grid = (num_seqs + warps_per_cta - 1) / warps_per_cta;
-  grow_tables_kernel<<<grid, warps_per_cta * 32, 0, stream>>>(block_table, seq_lens, num_seqs, max_pages,
-                                                               free_pages, free_count, status);
+  grow_tables_kernel<<<grid, warps_per_cta * 32, 0, stream>>>(block_table, seq_lens, context_lens, num_seqs,
+                                                               max_pages, free_pages, free_count, status);
   return cudaGetLastError();
 }
 

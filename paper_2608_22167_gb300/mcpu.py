@@ -100,6 +100,8 @@ _lib.mcpu_rope_kv_append.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.
 _lib.mcpu_rope_kv_append.restype = ctypes.c_int
 _lib.mcpu_grow_block_tables.argtypes = [_P, _P, ctypes.POINTER(Dims), _P, _P, _P, _P]
 _lib.mcpu_grow_block_tables.restype = ctypes.c_int
+_lib.mcpu_grow_block_tables_from.argtypes = [_P, _P, _P, ctypes.POINTER(Dims), _P, _P, _P, _P]
+_lib.mcpu_grow_block_tables_from.restype = ctypes.c_int
 _lib.mcpu_kv_append_fp8.argtypes = [_P, _P, _P, _P, _P, _P, ctypes.POINTER(Dims), _P, _P]
 _lib.mcpu_kv_append_fp8.restype = ctypes.c_int
 _lib.mcpu_paged_attention_forward_fp8.argtypes = [
@@ -259,6 +261,24 @@ def mcpu_grow_block_tables(block_table, seq_lens, free_pages, free_count, status
         _lib.mcpu_grow_block_tables(_ptr(block_table), _ptr(seq_lens), ctypes.byref(d), _ptr(free_pages),
                                     _ptr(free_count), _ptr(status_word), _stream(stream)),
         "mcpu_grow_block_tables",
+    )
+
+
+def mcpu_grow_block_tables_from(block_table, seq_lens, context_lens, free_pages, free_count, status_word, stream=None):
+    """The same for rows whose first context_lens (int32 [B]) tokens are in the
+    cache: fills the entries from page ceil(context_lens / 16) on, so that
+    pages released before a window stay released."""
+    rows, width = block_table.shape
+    if seq_lens.shape != (rows,) or context_lens.shape != (rows,):
+        raise ValueError("seq_lens and context_lens must have one entry per row of block_table")
+    d = Dims(num_seqs=rows, total_q=0, max_pages_per_seq=width, num_pages=0, num_q_heads=1, num_kv_heads=1,
+             head_dim=64, page_size=16)
+    _check(
+        _lib.mcpu_grow_block_tables_from(
+            _int32(block_table, "block_table"), _int32(seq_lens, "seq_lens"), _int32(context_lens, "context_lens"),
+            ctypes.byref(d), _int32(free_pages, "free_pages"), _int32(free_count, "free_count"),
+            _int32(status_word, "status_word"), _stream(stream)),
+        "mcpu_grow_block_tables_from",
     )
 
 

@@ -27,16 +27,20 @@ PAGE, HEAD_DIM = 16, 64
 
 
 class PagedCache:
-    def __init__(self, layers, rows, max_pages, num_pages, num_q_heads, num_kv_heads, device="cuda"):
+    """The pools, table, page counts and stack of layers that share a block table. sliding_window > 0: all of them
+    attend within that window, and `keep` returns the pages before it."""
+
+    def __init__(self, layers, rows, max_pages, num_pages, num_q_heads, num_kv_heads, device="cuda", sliding_window=0):
         shape = (num_pages, num_kv_heads, PAGE, HEAD_DIM)
         i32 = dict(dtype=torch.int32, device=device)
         self.k = [torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(layers)]
         self.v = [torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(layers)]
         self.pools = mcpu.PoolList(self.k + self.v)
-        self.num_q_heads, self.rows = num_q_heads, rows
+        self.num_q_heads, self.rows, self.sliding_window = num_q_heads, rows, sliding_window
         self.block_table = torch.full((rows, max_pages), -1, **i32)
         self.seq_lens = torch.zeros(rows, **i32)
         self.new_lens = torch.zeros(rows, **i32)
+        self.held_lens = torch.zeros(rows, **i32)  # lengths whose pages the rows were left with: not grown again
         self.page_refs = torch.zeros(num_pages, **i32)
         self.free_pages = torch.arange(num_pages, **i32)
         self.free_count = torch.tensor([num_pages], **i32)
@@ -54,7 +58,8 @@ class PagedCache:
     def extend(self, new_lens):
         """Row lengths after the next append (int32 [rows]) and the pages for them."""
         self.seq_lens.copy_(new_lens)
-        mcpu.mcpu_grow_block_tables(self.block_table, self.seq_lens, self.free_pages, self.free_count, self.status)
+        mcpu.mcpu_grow_block_tables_from(self.block_table, self.seq_lens, self.held_lens, self.free_pages,
+                                         self.free_count, self.status)
 
     def append(self, layer, q, k, v, q_weight, k_weight, eps, cos_sin, query_start_loc, positions=None, q_out=None):
         """Norm, rotation and KV append of a layer's projected q, k and v; returns the rotated q."""
@@ -63,9 +68,11 @@ class PagedCache:
                                       self.v[layer], self.block_table, self.seq_lens, query_start_loc, self.status)
         return q_out
 
-    def attend(self, layer, q, query_start_loc, tree_mask, positions=None, sliding_window=0, scale=HEAD_DIM ** -0.5,
-               sinks=None, out=None, lse=None):
-        """Attention of every node over its row's context and the nodes its mask names."""
+    def attend(self, layer, q, query_start_loc, tree_mask, positions=None, sliding_window=None,
+               scale=HEAD_DIM ** -0.5, sinks=None, out=None, lse=None):
+        """Attention of every node over its row's context (in the cache's window, if none is given) and the nodes
+        its mask names."""
+        sliding_window = self.sliding_window if sliding_window is None else sliding_window
         out = torch.empty_like(q) if out is None else out
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
         mcpu.mcpu_tree_attention_forward(q, self.k[layer], self.v[layer], self.block_table, self.seq_lens,
@@ -79,7 +86,8 @@ class PagedCache:
         mcpu.mcpu_compact_kv(self.pools, self.block_table, self.seq_lens, query_start_loc, path, path_len,
                              self.new_lens, self.status)
         self.seq_lens.copy_(self.new_lens)
-        self._release(self.seq_lens)
+        self.held_lens.copy_(self.seq_lens)
+        self._release(self.seq_lens, self.sliding_window)
 
     def fork(self, src_rows, dst_rows):
         """Rows dst_rows (empty) become copies of src_rows: full pages shared, partial last pages copied."""
@@ -88,15 +96,17 @@ class PagedCache:
         mcpu.mcpu_fork_block_tables(self.block_table, self.seq_lens, src_rows, dst_rows, self.page_refs,
                                     self.free_pages, self.free_count, copy[0], copy[1], self.page_scratch, self.status)
         mcpu.mcpu_copy_pages(self.pools, copy[0], copy[1], self.status)
+        self.held_lens.copy_(self.seq_lens)
 
     def drop(self, rows):
         """Frees the rows (int64 indices)."""
         self.seq_lens[rows] = 0
         self._release(self.seq_lens)
 
-    def _release(self, lens):
-        mcpu.mcpu_shrink_block_tables(self.block_table, lens, 0, self.page_refs, self.free_pages, self.free_count,
-                                      self.page_scratch, self.status)
+    def _release(self, lens, sliding_window=0):
+        torch.minimum(self.held_lens, lens, out=self.held_lens)
+        mcpu.mcpu_shrink_block_tables(self.block_table, lens, sliding_window, self.page_refs, self.free_pages,
+                                      self.free_count, self.page_scratch, self.status)
 
 
 def tree_masks(parents):

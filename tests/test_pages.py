@@ -362,3 +362,106 @@ def test_pool_lists():
     with pytest.raises(ValueError):
         mcpu.mcpu_compact_kv(mcpu.PoolList([torch.zeros(3, 2, 2176, dtype=torch.uint8)]), None, None, None, None, None,
                              None, None)
+
+
+def _grow_from(d, seq_lens, context_lens):
+    from paper_2608_22167_gb300 import mcpu
+
+    mcpu.mcpu_grow_block_tables_from(d["bt"], _i32(seq_lens), _i32(context_lens), d["free"], d["count"], d["status"])
+
+
+def _grown(m, d, new):
+    """Checks the tables after growing the model's rows to `new` lengths, and takes over which page went where."""
+    n = int(d["count"].item())
+    popped, m.free = m.free[n:], m.free[:n]
+    bt = d["bt"].cpu().numpy()
+    got = []
+    for r in range(len(new)):
+        first, end = -(-int(m.sl[r]) // 16), max(-(-int(new[r]) // 16), -(-int(m.sl[r]) // 16))
+        assert np.array_equal(bt[r, :first], m.bt[r, :first]) and np.all(bt[r, end:] == -1)
+        got += [int(p) for old, p in zip(m.bt[r, first:end], bt[r, first:end]) if old < 0]
+        m.bt[r, first:end] = bt[r, first:end]
+    assert sorted(got) == sorted(popped) and min(got, default=0) >= 0
+    m.sl = np.asarray(new).copy()
+
+
+@gpu
+@pytest.mark.parametrize("window", [1, 16, 50, 128])
+def test_growing_keeps_what_a_window_released(window):
+    # rows of up to 600 tokens whose windows need 40 x (9 + 4) pages at most: a pool without room for their tables
+    m = Model(40, 64, 40 * 13, window)
+    for r in range(40):
+        m.fill(r, int(m.rng.integers(0, 130)))
+    d = m.device()
+    for _ in range(10):
+        _shrink(d, m.sl, window)
+        m.shrink(m.sl, window)
+        d["sl"].copy_(_i32(m.sl))
+        m.same(d)
+        new = m.sl + m.rng.integers(0, 49, 40) * (m.rng.random(40) < 0.8)
+        _grow_from(d, new, m.sl)
+        _grown(m, d, new)
+        d["sl"].copy_(_i32(m.sl))
+        m.same(d)
+    # forked rows keep the missing entries of their source
+    m.sl[30:] = 0
+    _shrink(d, m.sl, window)
+    m.shrink(m.sl, window)
+    d["sl"].copy_(_i32(m.sl))
+    _fork(d, range(10), range(30, 40))
+    m.fork(range(10), range(30, 40))
+    m.same(d)
+    new = m.sl + 20
+    _grow_from(d, new, m.sl)
+    _grown(m, d, new)
+    assert int(d["status"].item()) == 0
+
+
+@gpu
+def test_growing_does_not_replace_a_missing_page_of_the_context():
+    from paper_2608_22167_gb300 import mcpu
+
+    m = Model(3, 8, 30, 9)
+    m.fill(0, 60)
+    m.free, left = [], m.free
+    d = m.device()
+    _fork(d, [0], [1])  # no page for the partial last one
+    m.fork([0], [1])
+    m.same(d, mcpu.STATUS_POOL_EXHAUSTED)
+    d["status"].zero_()
+    m.free = left
+    d = m.device()
+    new = np.array([60, 70, 5])
+    _grow_from(d, new, m.sl)
+    _grown(m, d, new)
+    assert m.bt[1, 3] == -1 and int(d["status"].item()) == 0
+    # lengths that grow by nothing, a context longer than the row, and a negative one
+    _grow_from(d, [60, 20, 0], [60, 70, 0])
+    assert np.array_equal(d["bt"].cpu().numpy(), m.bt) and int(d["status"].item()) == 0
+    _grow_from(d, [60, 20, 20], [60, 70, -1])
+    assert np.array_equal(d["bt"].cpu().numpy(), m.bt) and int(d["status"].item()) == mcpu.STATUS_BAD_LENGTHS
+
+
+def test_grow_from_host_checks():
+    from paper_2608_22167_gb300 import mcpu
+
+    P = 1 << 20
+    ok = dict(bt=P, sl=P, ctx=P, dims=mcpu.Dims(4, 0, 19, 0, 1, 1, 64, 16), free=P, count=P, st=P)
+
+    def call(**kw):
+        a = dict(ok, **kw)
+        return mcpu._lib.mcpu_grow_block_tables_from(a["bt"], a["sl"], a["ctx"], a["dims"] and ctypes.byref(a["dims"]),
+                                                     a["free"], a["count"], a["st"], None)
+
+    for name in ("bt", "sl", "ctx", "free", "count", "st"):
+        assert call(**{name: None}) == 1 and call(**{name: P + 2}) == 1, name
+    assert call(dims=None) == 1 and call(dims=mcpu.Dims(-1, 0, 19, 0, 1, 1, 64, 16)) == 1
+    assert call(dims=mcpu.Dims(4, 0, 1 << 28, 0, 1, 1, 64, 16)) == 2
+    assert call(dims=mcpu.Dims(0, 0, 19, 0, 1, 1, 64, 16)) == 0
+    bt, sl = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    good = dict(block_table=bt, seq_lens=sl, context_lens=sl, free_pages=sl, free_count=sl[:1], status_word=sl[:1],
+                stream=object())
+    for bad in (dict(context_lens=sl[:1]), dict(context_lens=sl.long()), dict(seq_lens=sl.long()),
+                dict(block_table=bt[:, :2])):
+        with pytest.raises(ValueError):
+            mcpu.mcpu_grow_block_tables_from(**dict(good, **bad))

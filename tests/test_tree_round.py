@@ -253,3 +253,47 @@ def test_pages_far_into_large_pools():
     for p in pools:
         assert torch.equal(p[5], p[19999]) and torch.equal(p[19998], p[3])
     assert int(new) == 33 and int(status) == 0 and mcpu.mcpu_read_device_status(ws) == (0, 0)
+
+
+@gpu
+@pytest.mark.parametrize("window", [1, 40, 64])
+def test_rounds_in_a_window_need_the_windows_pages_only(window):
+    # the same rounds over a cache that keeps every page and one with room for the windows alone
+    from paper_2608_22167_gb300.tree_decode import PagedCache, rope_table, tree_masks
+
+    rows, nodes, hq, hkv = 5, 20, 8, 2
+    caches = [PagedCache(1, rows, 40, 240, hq, hkv), PagedCache(1, rows, 40, 16 * rows, hq, hkv, sliding_window=window)]
+    tab, w = rope_table(800), torch.ones(64, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(window)
+    lens = [0] * rows
+    for n in [200, 1, 17] + [nodes] * 10:
+        # a chain, or one of 14 nodes with others hanging off it
+        mask, depth = tree_masks([[i - 1 if i < 14 or n > nodes else i - 12 for i in range(n)]] * rows)
+        qsl = torch.arange(0, rows * n + 1, n, dtype=torch.int32, device="cuda")
+        pos = (torch.tensor(lens).repeat_interleave(n) + depth).int().cuda()
+        x = torch.randn(rows * n, hq + 2 * hkv, 64, generator=g, device="cuda", dtype=torch.bfloat16)
+        path = list(range(n if n > nodes else min(n, 14)))  # one row keeps nothing
+        taken = [0 if r == 3 else len(path) - (r == 2 and n > 1) for r in range(rows)]
+        outs = []
+        for cache in caches:
+            cache.extend(torch.tensor(lens, device="cuda") + n)
+            q = cache.append(0, x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], w, w, 1e-6, tab, qsl, pos)
+            outs.append(cache.attend(0, q, qsl, mask.cuda(), pos, sliding_window=window))
+            cache.keep(qsl, torch.tensor([path] * rows, dtype=torch.int32, device="cuda"),
+                       torch.tensor(taken, dtype=torch.int32, device="cuda"))
+            cache.check()
+        lens = [a + b for a, b in zip(lens, taken)]
+        assert caches[1].seq_lens.tolist() == lens
+        assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+        table = caches[1].block_table
+        assert (table >= 0).sum(1).tolist() == [-(-s // 16) - max(0, s - window + 1) // 16 for s in lens]
+        assert int(caches[1].free_count) == 16 * rows - table[table >= 0].unique().numel()
+        if n == 17:  # a sample of row 0 in place of row 4
+            for cache in caches:
+                cache.drop(torch.tensor([4], device="cuda"))
+                cache.fork(torch.tensor([0], dtype=torch.int32, device="cuda"),
+                           torch.tensor([4], dtype=torch.int32, device="cuda"))
+                cache.check()
+            lens[4] = lens[0]
+    assert sum(-(-s // 16) for s in lens) > 16 * rows
