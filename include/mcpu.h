@@ -261,9 +261,23 @@ mcpu_status mcpu_grow_block_tables(int32_t* block_table, const int32_t* seq_lens
  * (mcpu_shrink_block_tables) are not taken again, nor is a page of the context
  * that is missing replaced by an empty one. A negative length is reported
  * (MCPU_ERR_BAD_LENGTHS); one above S_r leaves nothing to fill.
+ *
+ * A row may end inside a page that other rows hold: one that was shortened
+ * into the full pages it shares (mcpu_fork_block_tables). Its next token must
+ * not be written there. With page_refs (as for mcpu_fork_block_tables; else
+ * NULL, and copy_src and copy_dst too) a row that grows from inside a page
+ * with other holders lets go of it and takes a fresh one: copy_src[r],
+ * copy_dst[r] (device int32 [num_seqs]) receive the two for mcpu_copy_pages,
+ * which has to follow before anything is appended, or -1 for every other row.
+ * If the stack is empty the entry becomes -1 (MCPU_ERR_POOL_EXHAUSTED). Of
+ * rows that grow from inside the same page at once one may keep it. Entries
+ * past the page of token context_lens[r] are taken to be the row's own
+ * (mcpu_shrink_block_tables releases those it shares). num_pages of dims is
+ * used with page_refs only.
  */
 mcpu_status mcpu_grow_block_tables_from(int32_t* block_table, const int32_t* seq_lens, const int32_t* context_lens,
-                                        const mcpu_dims* dims, const int32_t* free_pages, int32_t* free_count,
+                                        const mcpu_dims* dims, int32_t* page_refs, const int32_t* free_pages,
+                                        int32_t* free_count, int32_t* copy_src, int32_t* copy_dst,
                                         int32_t* status_word, mcpu_stream_t stream);
 
 /*
@@ -527,7 +541,9 @@ mcpu_status mcpu_compact_kv(void* const* pools, int32_t num_pools, const int32_t
  * its replacement for mcpu_copy_pages, or -1. Fresh pages are popped in the
  * order of f. The dst rows must hold no page (shrink them to length 0
  * first), be distinct, and not be a src row of the same call. If the stack
- * runs empty the tail entry stays -1 (MCPU_ERR_POOL_EXHAUSTED).
+ * runs empty the tail entry stays -1 (MCPU_ERR_POOL_EXHAUSTED). Fork a row
+ * whose S tokens are there to stay: between its append and its compaction
+ * mcpu_compact_kv would move rows inside the pages just shared.
  *
  * mcpu_shrink_block_tables: the reverse of mcpu_grow_block_tables_from. Every
  * entry >= 0 of row r at or past ceil(S_r / 16), and with sliding_window
@@ -537,7 +553,10 @@ mcpu_status mcpu_compact_kv(void* const* pools, int32_t num_pools, const int32_t
  * return are pushed in ascending order. A page that is released more often
  * than it is held is reported (MCPU_ERR_BAD_PAGE). Rows whose first pages
  * were released before a window grow with mcpu_grow_block_tables_from:
- * mcpu_grow_block_tables would fill those entries again.
+ * mcpu_grow_block_tables would fill those entries again. A row shortened into
+ * a page that other rows hold keeps holding it, and grows with
+ * mcpu_grow_block_tables_from and page_refs, which gives it a page of its own
+ * before anything is appended.
  *
  * mcpu_copy_pages: for each f < num_copies with copy_src[f], copy_dst[f] >= 0,
  * copies page copy_src[f] to page copy_dst[f] in every pool: page_bytes

@@ -34,9 +34,6 @@ cudaError_t launch_rope_append(void* q, const void* k_new, const void* v_new, vo
                                const float* cos_sin, int32_t max_position, int32_t* status, int32_t num_seqs,
                                int32_t total_q, int32_t max_pages, int32_t num_pages, int32_t num_q_heads,
                                int32_t num_kv_heads, cudaStream_t stream);
-cudaError_t launch_grow_tables(int32_t* block_table, const int32_t* seq_lens, const int32_t* context_lens,
-                               int32_t num_seqs, int32_t max_pages, const int32_t* free_pages, int32_t* free_count,
-                               int32_t* status, cudaStream_t stream);
 cudaError_t launch_kv_append(const void* k_new, const void* v_new, void* k_cache, void* v_cache,
                              const int32_t* block_table, const int32_t* seq_lens, const int32_t* qsl,
                              int32_t* status, int32_t num_seqs, int32_t total_q, int32_t max_pages,
@@ -262,21 +259,44 @@ mcpu_status mcpu_grow_block_tables(int32_t* block_table, const int32_t* seq_lens
   if (!aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(free_pages, 4) || !aligned(free_count, 4) ||
       !aligned(status_word, 4))
     return MCPU_ERR_INVALID_ARG;
-  return from_cuda(launch_grow_tables(block_table, seq_lens, nullptr, dims->num_seqs, dims->max_pages_per_seq,
-                                      free_pages, free_count, status_word, reinterpret_cast<cudaStream_t>(stream)));
+  GrowParams p{};
+  p.block_table = block_table;
+  p.seq_lens = seq_lens;
+  p.free_pages = free_pages;
+  p.free_count = free_count;
+  p.status = status_word;
+  p.num_seqs = dims->num_seqs;
+  p.max_pages = dims->max_pages_per_seq;
+  return from_cuda(launch_grow_tables(p, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 mcpu_status mcpu_grow_block_tables_from(int32_t* block_table, const int32_t* seq_lens, const int32_t* context_lens,
-                                        const mcpu_dims* dims, const int32_t* free_pages, int32_t* free_count,
+                                        const mcpu_dims* dims, int32_t* page_refs, const int32_t* free_pages,
+                                        int32_t* free_count, int32_t* copy_src, int32_t* copy_dst,
                                         int32_t* status_word, mcpu_stream_t stream) {
-  if (!dims || dims->num_seqs < 0 || dims->max_pages_per_seq < 0) return MCPU_ERR_INVALID_ARG;
+  if (!dims || dims->num_seqs < 0 || dims->max_pages_per_seq < 0 || dims->num_pages < 0) return MCPU_ERR_INVALID_ARG;
   if ((int64_t)dims->max_pages_per_seq * kPage >= (int64_t)0x7fff0000) return MCPU_ERR_UNSUPPORTED;
   if (dims->num_seqs == 0) return MCPU_OK;
   for (const void* a : {(const void*)block_table, (const void*)seq_lens, (const void*)context_lens,
                         (const void*)free_pages, (const void*)free_count, (const void*)status_word})
     if (!a || !aligned(a, 4)) return MCPU_ERR_INVALID_ARG;
-  return from_cuda(launch_grow_tables(block_table, seq_lens, context_lens, dims->num_seqs, dims->max_pages_per_seq,
-                                      free_pages, free_count, status_word, reinterpret_cast<cudaStream_t>(stream)));
+  // the counts and the lists come together or not at all
+  for (const void* a : {(const void*)page_refs, (const void*)copy_src, (const void*)copy_dst})
+    if (!a != !page_refs || !aligned(a, 4)) return MCPU_ERR_INVALID_ARG;
+  GrowParams p{};
+  p.block_table = block_table;
+  p.seq_lens = seq_lens;
+  p.context_lens = context_lens;
+  p.free_pages = free_pages;
+  p.refs = page_refs;
+  p.free_count = free_count;
+  p.copy_src = copy_src;
+  p.copy_dst = copy_dst;
+  p.status = status_word;
+  p.num_seqs = dims->num_seqs;
+  p.max_pages = dims->max_pages_per_seq;
+  p.num_pages = dims->num_pages;
+  return from_cuda(launch_grow_tables(p, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 mcpu_status mcpu_paged_attention_forward(const void* q, const void* k_cache, const void* v_cache,

@@ -28,6 +28,16 @@ mcpu_status from_cuda(cudaError_t e);
 // point); its SM count. Needed before the encoders below.
 mcpu_status device_sms(int* sms);
 
+// Growing block tables (rope_append.cu). context_lens: null for all of a row's
+// entries; refs, copy_src and copy_dst: null where no page is shared.
+struct GrowParams {
+  int32_t* block_table;
+  const int32_t *seq_lens, *context_lens, *free_pages;
+  int32_t *refs, *free_count, *copy_src, *copy_dst, *status;
+  int32_t num_seqs, max_pages, num_pages;
+};
+cudaError_t launch_grow_tables(const GrowParams& p, cudaStream_t stream);
+
 // Tensor map of a bf16 pool as `rows` rows of 64 values, one box per (page,
 // kv head) block; and of q [T, H_q, D], one box per `rows` query rows (rows /
 // group tokens x the group's heads). False if the map cannot be made.

@@ -13,7 +13,10 @@
 // whose block-table entry is negative gets a page popped from a device stack
 // of free page ids; entries already set (shared prompt pages, earlier pages)
 // are left alone. An empty stack sets kStatusPoolExhausted. With the lengths
-// that are in the cache already, entries of their pages stay as they are too.
+// that are in the cache already, entries of their pages stay as they are too;
+// with the pages' holder counts as well, a row whose next token would land in a
+// page that others hold lets go of it for a fresh one and a copy.
+#include "api_internal.h"
 #include "common.cuh"
 
 namespace mcpu {
@@ -129,39 +132,54 @@ cudaError_t launch_rope_append(void* q, const void* k_new, const void* v_new, vo
 }
 
 // one warp per row: lanes take the row's logical pages 32 at a time
-__global__ void __launch_bounds__(256) grow_tables_kernel(int32_t* block_table, const int32_t* seq_lens,
-                                                          const int32_t* context_lens, int32_t num_seqs,
-                                                          int32_t max_pages, const int32_t* free_pages, int32_t* free_count,
-                                                          int32_t* status) {
+__global__ void __launch_bounds__(256) grow_tables_kernel(const GrowParams p) {
   const int lane = threadIdx.x & 31;
   const int r = (blockIdx.x * blockDim.x + threadIdx.x) >> 5;
-  if (r >= num_seqs) return;
-  const int S = seq_lens[r], C = context_lens ? context_lens[r] : 0;
-  if (S < 0 || S > max_pages * kPage || C < 0) {
-    if (lane == 0) atomicOr(status, kStatusBadLengths);
+  if (r >= p.num_seqs) return;
+  const int S = p.seq_lens[r], C = p.context_lens ? p.context_lens[r] : 0;
+  if (p.refs && lane == 0) p.copy_src[r] = p.copy_dst[r] = -1;
+  if (S < 0 || S > p.max_pages * kPage || C < 0) {
+    if (lane == 0) atomicOr(p.status, kStatusBadLengths);
     return;
   }
+  auto pop = [&]() -> int {
+    const int top = atomicSub(p.free_count, 1);
+    if (top > 0) return p.free_pages[top - 1];
+    atomicAdd(p.free_count, 1);  // give the slot back: the stack is empty
+    atomicOr(p.status, kStatusPoolExhausted);
+    return -1;
+  };
   const int need = (S + kPage - 1) / kPage;
-  int32_t* row = block_table + (size_t)r * max_pages;
+  int32_t* row = p.block_table + (size_t)r * p.max_pages;
+  if (p.refs && lane == 0 && C < S && C % kPage != 0) {
+    const int page = row[C / kPage];
+    if (page >= p.num_pages) {
+      atomicOr(p.status, kStatusBadPage);
+    } else if (page >= 0) {
+      // of the rows that let go of a page at once, the last keeps it: the copies are made before anything is written
+      const int others = atomicSub(p.refs + page, 1);
+      if (others > 0) {
+        const int fresh = pop();
+        row[C / kPage] = fresh;
+        p.copy_src[r] = fresh >= 0 ? page : -1;
+        p.copy_dst[r] = fresh;
+      } else {
+        atomicAdd(p.refs + page, 1);
+        if (others < 0) atomicOr(p.status, kStatusBadPage);  // held more often than counted
+      }
+    }
+  }
   for (int j = (min(C, S) + kPage - 1) / kPage + lane; j < need; j += 32) {
     if (row[j] >= 0) continue;
-    const int top = atomicSub(free_count, 1);
-    if (top <= 0) {
-      atomicAdd(free_count, 1);  // give the slot back: the stack is empty
-      atomicOr(status, kStatusPoolExhausted);
-    } else {
-      row[j] = free_pages[top - 1];
-    }
+    const int page = pop();
+    if (page >= 0) row[j] = page;
   }
 }
 
-cudaError_t launch_grow_tables(int32_t* block_table, const int32_t* seq_lens, const int32_t* context_lens,
-                               int32_t num_seqs, int32_t max_pages, const int32_t* free_pages, int32_t* free_count,
-                               int32_t* status, cudaStream_t stream) {
+cudaError_t launch_grow_tables(const GrowParams& p, cudaStream_t stream) {
   const int warps_per_cta = 8;
-  const int grid = (num_seqs + warps_per_cta - 1) / warps_per_cta;
-  grow_tables_kernel<<<grid, warps_per_cta * 32, 0, stream>>>(block_table, seq_lens, context_lens, num_seqs,
-                                                               max_pages, free_pages, free_count, status);
+  const int grid = (p.num_seqs + warps_per_cta - 1) / warps_per_cta;
+  grow_tables_kernel<<<grid, warps_per_cta * 32, 0, stream>>>(p);
   return cudaGetLastError();
 }
 

@@ -100,7 +100,7 @@ _lib.mcpu_rope_kv_append.argtypes = [_P, _P, _P, _P, _P, _P, _P, _P, _P, ctypes.
 _lib.mcpu_rope_kv_append.restype = ctypes.c_int
 _lib.mcpu_grow_block_tables.argtypes = [_P, _P, ctypes.POINTER(Dims), _P, _P, _P, _P]
 _lib.mcpu_grow_block_tables.restype = ctypes.c_int
-_lib.mcpu_grow_block_tables_from.argtypes = [_P, _P, _P, ctypes.POINTER(Dims), _P, _P, _P, _P]
+_lib.mcpu_grow_block_tables_from.argtypes = [_P, _P, _P, ctypes.POINTER(Dims), _P, _P, _P, _P, _P, _P, _P]
 _lib.mcpu_grow_block_tables_from.restype = ctypes.c_int
 _lib.mcpu_kv_append_fp8.argtypes = [_P, _P, _P, _P, _P, _P, ctypes.POINTER(Dims), _P, _P]
 _lib.mcpu_kv_append_fp8.restype = ctypes.c_int
@@ -264,20 +264,32 @@ def mcpu_grow_block_tables(block_table, seq_lens, free_pages, free_count, status
     )
 
 
-def mcpu_grow_block_tables_from(block_table, seq_lens, context_lens, free_pages, free_count, status_word, stream=None):
+def mcpu_grow_block_tables_from(block_table, seq_lens, context_lens, free_pages, free_count, status_word,
+                                page_refs=None, copy_src=None, copy_dst=None, stream=None):
     """The same for rows whose first context_lens (int32 [B]) tokens are in the
     cache: fills the entries from page ceil(context_lens / 16) on, so that
-    pages released before a window stay released."""
+    pages released before a window stay released. With page_refs, copy_src and
+    copy_dst (int32 [B]) a row that grows from inside a page that other rows
+    hold takes one of its own, whose contents mcpu_copy_pages(pools, copy_src,
+    copy_dst, ...) brings over before anything is appended."""
     rows, width = block_table.shape
     if seq_lens.shape != (rows,) or context_lens.shape != (rows,):
         raise ValueError("seq_lens and context_lens must have one entry per row of block_table")
-    d = Dims(num_seqs=rows, total_q=0, max_pages_per_seq=width, num_pages=0, num_q_heads=1, num_kv_heads=1,
+    pages = 0
+    if page_refs is not None or copy_src is not None or copy_dst is not None:
+        if page_refs is None or copy_src is None or copy_dst is None or copy_src.shape != (rows,) or \
+                copy_dst.shape != (rows,):
+            raise ValueError("page_refs, copy_src and copy_dst come together, the last two with one entry per row")
+        pages = page_refs.shape[0]
+        page_refs, copy_src, copy_dst = (_int32(x, "page_refs, copy_src and copy_dst")
+                                         for x in (page_refs, copy_src, copy_dst))
+    d = Dims(num_seqs=rows, total_q=0, max_pages_per_seq=width, num_pages=pages, num_q_heads=1, num_kv_heads=1,
              head_dim=64, page_size=16)
     _check(
         _lib.mcpu_grow_block_tables_from(
             _int32(block_table, "block_table"), _int32(seq_lens, "seq_lens"), _int32(context_lens, "context_lens"),
-            ctypes.byref(d), _int32(free_pages, "free_pages"), _int32(free_count, "free_count"),
-            _int32(status_word, "status_word"), _stream(stream)),
+            ctypes.byref(d), page_refs, _int32(free_pages, "free_pages"), _int32(free_count, "free_count"),
+            copy_src, copy_dst, _int32(status_word, "status_word"), _stream(stream)),
         "mcpu_grow_block_tables_from",
     )
 

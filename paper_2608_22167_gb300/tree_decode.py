@@ -56,7 +56,8 @@ class PagedCache:
             raise mcpu.McpuError(code, f"device status bits {bits}")
 
     def extend(self, new_lens):
-        """Row lengths after the next append (int32 [rows]) and the pages for them."""
+        """Row lengths after the next append (int32 [rows]) and the pages for them. What is appended follows the tokens
+        that a row holds: pages before that may be shared with other rows."""
         self.seq_lens.copy_(new_lens)
         mcpu.mcpu_grow_block_tables_from(self.block_table, self.seq_lens, self.held_lens, self.free_pages,
                                          self.free_count, self.status)
@@ -90,7 +91,8 @@ class PagedCache:
         self._release(self.seq_lens, self.sliding_window)
 
     def fork(self, src_rows, dst_rows):
-        """Rows dst_rows (empty) become copies of src_rows: full pages shared, partial last pages copied."""
+        """Rows dst_rows (empty) become copies of src_rows: full pages shared, partial last pages copied. Not between
+        a row's `append` and its `keep`, which moves rows inside pages that would be shared by then."""
         n = src_rows.shape[0]
         copy = torch.empty(2, n, dtype=torch.int32, device=src_rows.device)
         mcpu.mcpu_fork_block_tables(self.block_table, self.seq_lens, src_rows, dst_rows, self.page_refs,

@@ -446,22 +446,140 @@ def test_grow_from_host_checks():
     from paper_2608_22167_gb300 import mcpu
 
     P = 1 << 20
-    ok = dict(bt=P, sl=P, ctx=P, dims=mcpu.Dims(4, 0, 19, 0, 1, 1, 64, 16), free=P, count=P, st=P)
+    ok = dict(bt=P, sl=P, ctx=P, dims=mcpu.Dims(4, 0, 19, 0, 1, 1, 64, 16), refs=None, free=P, count=P, cs=None, cd=None,
+              st=P)
 
     def call(**kw):
         a = dict(ok, **kw)
         return mcpu._lib.mcpu_grow_block_tables_from(a["bt"], a["sl"], a["ctx"], a["dims"] and ctypes.byref(a["dims"]),
-                                                     a["free"], a["count"], a["st"], None)
+                                                     a["refs"], a["free"], a["count"], a["cs"], a["cd"], a["st"], None)
 
     for name in ("bt", "sl", "ctx", "free", "count", "st"):
         assert call(**{name: None}) == 1 and call(**{name: P + 2}) == 1, name
     assert call(dims=None) == 1 and call(dims=mcpu.Dims(-1, 0, 19, 0, 1, 1, 64, 16)) == 1
     assert call(dims=mcpu.Dims(4, 0, 1 << 28, 0, 1, 1, 64, 16)) == 2
     assert call(dims=mcpu.Dims(0, 0, 19, 0, 1, 1, 64, 16)) == 0
+    assert call(dims=mcpu.Dims(4, 0, 19, -1, 1, 1, 64, 16)) == 1
+    for some in (dict(refs=P), dict(cs=P), dict(cd=P), dict(refs=P, cs=P), dict(refs=P, cd=P), dict(cs=P, cd=P),
+                 dict(refs=P + 2, cs=P, cd=P), dict(refs=P, cs=P + 2, cd=P), dict(refs=P, cs=P, cd=P + 2)):
+        assert call(**some) == 1, some
     bt, sl = torch.zeros(2, 3, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
     good = dict(block_table=bt, seq_lens=sl, context_lens=sl, free_pages=sl, free_count=sl[:1], status_word=sl[:1],
                 stream=object())
     for bad in (dict(context_lens=sl[:1]), dict(context_lens=sl.long()), dict(seq_lens=sl.long()),
-                dict(block_table=bt[:, :2])):
+                dict(block_table=bt[:, :2]), dict(page_refs=sl), dict(page_refs=sl, copy_src=sl, copy_dst=sl[:1]),
+                dict(page_refs=sl.long(), copy_src=sl, copy_dst=sl)):
         with pytest.raises(ValueError):
             mcpu.mcpu_grow_block_tables_from(**dict(good, **bad))
+
+
+@gpu
+def test_rows_that_end_inside_a_shared_page_get_their_own():
+    # samples shortened into the full pages they share with their prompt, then grown and appended to: the prompt and
+    # the other samples keep their K and V, the appending row keeps what it had
+    from paper_2608_22167_gb300 import mcpu
+
+    rng = np.random.default_rng(12)
+    rows, hkv, pages = 14, 2, 200
+    m = Model(rows, 10, pages, 12)
+    m.fill(0, 133)
+    m.fill(1, 96)
+    src, dst = [0, 0, 0, 0, 0, 0, 1, 1, 1, 1, 1, 1], list(range(2, 14))
+    m.fork(src, dst)
+    d = m.device()
+    pools = [torch.from_numpy(rng.standard_normal((pages, hkv, 16, 64)).astype(np.float32)).bfloat16().cuda()
+             for _ in range(2)]
+    # row 1 itself is shortened into a page its samples hold, three samples to the same one
+    keep = np.array([133, 90, 70, 71, 133, 64, 0, 128, 96, 95, 95, 96, 81, 5])
+    _shrink(d, keep)
+    m.shrink(keep)
+    m.sl = keep.copy()
+    d["sl"].copy_(_i32(keep))
+    m.same(d)
+
+    def held(r, n):
+        pos = torch.arange(n, device="cuda")
+        page = d["bt"][r].long()[pos // 16]
+        return torch.stack([p[page, :, pos % 16] for p in pools])
+
+    before = [held(r, int(keep[r])) for r in range(rows)]
+    grow = np.array([0, 3, 20, 1, 5, 16, 0, 0, 4, 2, 2, 0, 30, 12])
+    new = keep + grow
+    cs, cd = (torch.full((rows,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    old = d["bt"].cpu().numpy()
+    refs = d["refs"].cpu().numpy()
+    mcpu.mcpu_grow_block_tables_from(d["bt"], _i32(new), _i32(keep), d["free"], d["count"], d["status"],
+                                     page_refs=d["refs"], copy_src=cs, copy_dst=cd)
+    mcpu.mcpu_copy_pages(mcpu.PoolList(pools), cs, cd, d["status"])
+    assert int(d["status"].item()) == 0
+    bt = d["bt"].cpu().numpy()
+    # nobody else holds a page that a row is going to write, the counts are those of the table, and what was let go
+    # was copied
+    used, times = np.unique(bt[bt >= 0], return_counts=True)
+    counts = np.zeros(pages, int)
+    counts[used] = times - 1
+    assert np.array_equal(d["refs"].cpu().numpy(), counts)
+    moved = 0
+    for r in range(rows):
+        for j in range(int(keep[r]) // 16, -(-int(new[r]) // 16) if grow[r] else 0):
+            assert bt[r, j] >= 0 and counts[bt[r, j]] == 0
+        j = int(keep[r]) // 16
+        if grow[r] and keep[r] % 16 and bt[r, j] != old[r, j]:
+            assert refs[old[r, j]] > 0 and (int(cs[r]), int(cd[r])) == (old[r, j], bt[r, j])
+            moved += 1
+        else:
+            assert (int(cs[r]), int(cd[r])) == (-1, -1)
+        assert np.array_equal(bt[r, :j], old[r, :j])
+    assert moved == 7  # rows 1, 2, 3, 9, 10, 12 and 13; others hold each of their pages
+    left = int(d["count"].item())
+    in_use = set(used.tolist())
+    assert len(in_use) + left == pages and not in_use & set(d["free"][:left].tolist())
+    x = torch.randn(int(grow.sum()), hkv, 64, device="cuda").bfloat16()
+    qsl = _i32(np.concatenate([[0], np.cumsum(grow)]))
+    mcpu.mcpu_kv_append(x, x, *pools, d["bt"], _i32(new), qsl, d["status"])
+    for r in range(rows):
+        assert torch.equal(held(r, int(keep[r])), before[r]), r
+    assert int(d["status"].item()) == 0
+
+
+@gpu
+def test_a_shared_page_with_an_empty_stack():
+    from paper_2608_22167_gb300 import mcpu
+
+    m = Model(3, 4, 10, 2)
+    m.fill(0, 48)
+    m.fork([0], [1])
+    m.shrink([48, 40, 0])
+    m.sl[1] = 40
+    m.free = []
+    d = m.device()
+    cs, cd = (torch.full((3,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    shared = int(m.bt[1, 2])
+    mcpu.mcpu_grow_block_tables_from(d["bt"], _i32([48, 41, 0]), _i32([48, 40, 0]), d["free"], d["count"], d["status"],
+                                     page_refs=d["refs"], copy_src=cs, copy_dst=cd)
+    m.bt[1, 2] = -1
+    m.refs[shared] -= 1
+    m.same(d, mcpu.STATUS_POOL_EXHAUSTED)
+    assert cs.tolist() == [-1] * 3 and cd.tolist() == [-1] * 3
+
+
+@gpu
+def test_one_of_the_rows_that_grow_from_a_page_at_once_may_keep_it():
+    from paper_2608_22167_gb300 import mcpu
+
+    m = Model(4, 4, 20, 3)
+    m.fill(0, 48)
+    m.fork([0, 0, 0], [1, 2, 3])
+    d = m.device()
+    _shrink(d, [0, 40, 41, 40])
+    keep = _i32([0, 40, 41, 40])
+    cs, cd = (torch.full((4,), -7, dtype=torch.int32, device="cuda") for _ in range(2))
+    shared = int(m.bt[0, 2])
+    mcpu.mcpu_grow_block_tables_from(d["bt"], keep + 2, keep, d["free"], d["count"], d["status"], page_refs=d["refs"],
+                                     copy_src=cs, copy_dst=cd)
+    tails = d["bt"][1:, 2].tolist()
+    assert tails.count(shared) == 1 and len(set(tails)) == 3 and int(d["refs"][shared]) == 0
+    assert [int(s) for s in cs[1:]] == [-1 if t == shared else shared for t in tails]
+    assert [int(s) for s in cd[1:]] == [-1 if t == shared else t for t in tails]
+    # in use: the prompt's three pages, two in place of the shared one, one that row 0's two tokens open
+    assert int(cs[0]) == int(cd[0]) == -1 and int(d["status"].item()) == 0 and int(d["count"].item()) == 20 - 6
