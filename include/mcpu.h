@@ -540,10 +540,11 @@ mcpu_status mcpu_compact_kv(void* const* pools, int32_t num_pools, const int32_t
  * seq_lens[src] = S. copy_src[f], copy_dst[f] receive the partial page and
  * its replacement for mcpu_copy_pages, or -1. Fresh pages are popped in the
  * order of f. The dst rows must hold no page (shrink them to length 0
- * first), be distinct, and not be a src row of the same call. If the stack
- * runs empty the tail entry stays -1 (MCPU_ERR_POOL_EXHAUSTED). Fork a row
- * whose S tokens are there to stay: between its append and its compaction
- * mcpu_compact_kv would move rows inside the pages just shared.
+ * first; pages that one holds are lost, which is reported as
+ * MCPU_ERR_BAD_PAGE), be distinct, and not be a src row of the same call. If
+ * the stack runs empty the tail entry stays -1 (MCPU_ERR_POOL_EXHAUSTED). Fork
+ * a row whose S tokens are there to stay: between its append and its
+ * compaction mcpu_compact_kv would move rows inside the pages just shared.
  *
  * mcpu_shrink_block_tables: the reverse of mcpu_grow_block_tables_from. Every
  * entry >= 0 of row r at or past ceil(S_r / 16), and with sliding_window

@@ -66,12 +66,14 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const PageParams p) 
   const bool ok = fork_valid(p, f, &S);
   const bool partial = ok && S % kPage != 0;
   const int avail = min(max(__ldcg(p.free_count), 0), p.num_pages);
-  // the first entries of the source's table are on their way while the rank is counted
+  // the first entries of the source's table, and of the row's own, are on their way while the rank is counted
   int early[kForkEarly];
+  bool held = false;  // the row holds a page, which is about to be lost
 #pragma unroll
   for (int i = 0; i < kForkEarly; ++i) {
     const int j = threadIdx.x + i * kForkThreads;
     early[i] = ok && j < S / kPage ? p.block_table[(size_t)p.src_rows[f] * p.max_pages + j] : -1;
+    held |= ok && j < p.max_pages && p.block_table[(size_t)p.dst_rows[f] * p.max_pages + j] >= 0;
   }
   int before = 0;
   if (partial) {
@@ -125,8 +127,10 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(const PageParams p) 
       } else if (j == full) {
         e = s_page;
       }
+      if (i >= kForkEarly) held |= to[j] >= 0;
       to[j] = e;
     }
+    if (held) atomicOr(p.status, kStatusBadPage);
   } else if (threadIdx.x == 0) {
     atomicOr(p.status, kStatusBadLengths);
     p.copy_src[f] = p.copy_dst[f] = -1;

@@ -583,3 +583,22 @@ def test_one_of_the_rows_that_grow_from_a_page_at_once_may_keep_it():
     assert [int(s) for s in cd[1:]] == [-1 if t == shared else t for t in tails]
     # in use: the prompt's three pages, two in place of the shared one, one that row 0's two tokens open
     assert int(cs[0]) == int(cd[0]) == -1 and int(d["status"].item()) == 0 and int(d["count"].item()) == 20 - 6
+
+
+@gpu
+@pytest.mark.parametrize("at", [0, 5, 127, 511, 512, 700])
+def test_a_fork_into_a_row_that_holds_a_page_is_reported(at):
+    from paper_2608_22167_gb300 import mcpu
+
+    m = Model(4, 701, 900, at)
+    m.fill(0, 100)
+    d = m.device()
+    lost = m.free[0]  # never popped here
+    d["bt"][2, at] = lost
+    cs, cd = _fork(d, [0, 0], [1, 3])
+    ms, md, _ = m.fork([0, 0], [1, 3])
+    m.bt[2, at] = lost
+    m.same(d)  # the others' forks are fine
+    _fork(d, [0], [2])
+    m.fork([0], [2])
+    m.same(d, mcpu.STATUS_BAD_PAGE)
