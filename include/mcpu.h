@@ -477,7 +477,9 @@ mcpu_status mcpu_norm_rope_kv_append(const void* q, int64_t q_stride, const void
  *   - context key j < C_r iff sliding_window <= 0 or positions[t] - j < sliding_window;
  *   - node key n < L_r (slot C_r + n) iff bit n % 32 of
  *     tree_mask[t * mask_words + n / 32] is set (for a tree: its ancestors and
- *     itself; nothing is implied, and the window does not apply to nodes).
+ *     itself; nothing is implied. The window does not apply to nodes: in a
+ *     windowed layer the mask leaves out the ancestors whose position is
+ *     sliding_window or more below the node's).
  * out, lse, softmax_scale and sinks (float [H_q] or NULL) as for
  * mcpu_paged_attention_forward; a node that sees nothing gets out = 0 and
  * lse = -inf (or its sink). Rows may have any L_r <= 32 * mask_words

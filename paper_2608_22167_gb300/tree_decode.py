@@ -72,7 +72,7 @@ class PagedCache:
     def attend(self, layer, q, query_start_loc, tree_mask, positions=None, sliding_window=None,
                scale=HEAD_DIM ** -0.5, sinks=None, out=None, lse=None):
         """Attention of every node over its row's context (in the cache's window, if none is given) and the nodes
-        its mask names."""
+        its mask names: in a window the mask has to keep to it too (tree_masks)."""
         sliding_window = self.sliding_window if sliding_window is None else sliding_window
         out = torch.empty_like(q) if out is None else out
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
@@ -111,17 +111,24 @@ class PagedCache:
                                       self.free_count, self.page_scratch, self.status)
 
 
-def tree_masks(parents):
+def tree_masks(parents, sliding_window=0):
     """Ancestor masks (int32 [nodes, words]) and depths of trees given as lists of parents (-1: the context),
-    nodes in topological order: host tensors to copy to the device."""
+    nodes in topological order: host tensors to copy to the device. The masks are all that tree attention knows of
+    the nodes: for a layer with a sliding window, give the window here too, and a node's mask holds itself and the
+    ancestors less than the window above it only."""
     words = max(1, (max((len(p) for p in parents), default=1) + 31) // 32)
     masks, depths = [], []
     for parent in parents:
         rows, depth = [], []
+        near = []  # each node's ancestors inside the window, then itself
         for i, up in enumerate(parent):
             if not -1 <= up < i:
                 raise ValueError("a node comes after its parent")
             bits = (rows[up] if up >= 0 else 0) | 1 << i
+            if sliding_window > 0:
+                near.append((near[up] if up >= 0 else []) + [i])
+                if len(near[i]) > sliding_window:
+                    bits &= ~(1 << near[i].pop(0))
             rows.append(bits)
             depth.append(depth[up] + 1 if up >= 0 else 0)
         masks += [[(b >> 32 * w & 0xFFFFFFFF) - (1 << 32 if b >> 32 * w & 1 << 31 else 0) for w in range(words)]

@@ -297,3 +297,55 @@ def test_rounds_in_a_window_need_the_windows_pages_only(window):
                 cache.check()
             lens[4] = lens[0]
     assert sum(-(-s // 16) for s in lens) > 16 * rows
+
+
+@pytest.mark.parametrize("window", [1, 2, 5, 31, 32, 33, 100])
+def test_tree_masks_in_a_window(window):
+    from paper_2608_22167_gb300.tree_decode import tree_masks
+
+    rng = np.random.default_rng(window)
+    parents = [list(range(-1, 69)), [-1] + [int(rng.integers(max(-1, i - 3), i)) for i in range(1, 80)], [-1, -1, 0]]
+    mask, depth = tree_masks(parents, window)
+    plain, same_depth = tree_masks(parents)
+    assert torch.equal(depth, same_depth) and mask.shape == plain.shape
+    bits = mask.numpy().view(np.uint32)
+    t = 0
+    for parent in parents:
+        for i in range(len(parent)):
+            want, at = set(), i
+            while at >= 0 and len(want) < window:  # one level up, one position back
+                want.add(at)
+                at = parent[at]
+            assert {n for n in range(32 * mask.shape[1]) if bits[t, n // 32] >> np.uint32(n % 32) & 1} == want
+            t += 1
+    if window > int(depth.max()):
+        assert torch.equal(mask, plain)
+
+
+@gpu
+@pytest.mark.parametrize("window", [1, 17, 128])
+def test_a_chain_deeper_than_its_window_is_a_windowed_chunk(window):
+    # prompts fed as chains, the framework's plain windowed forward beside
+    from paper_2608_22167_gb300 import mcpu
+    from paper_2608_22167_gb300.tree_decode import PagedCache, tree_masks
+
+    lens, ctx, hq, hkv = [200, 31, 140], [0, 55, 300], 16, 2
+    cache = PagedCache(1, 3, 40, 100, hq, hkv, sliding_window=window)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(window)
+    cache.extend(torch.tensor([c + n for c, n in zip(ctx, lens)], device="cuda"))
+    for p in cache.k + cache.v:
+        p.normal_(generator=g)
+    mask, depth = tree_masks([list(range(-1, n - 1)) for n in lens], window)
+    pos = (torch.tensor(ctx).repeat_interleave(torch.tensor(lens)) + depth).int().cuda()
+    qsl = torch.tensor([0, 200, 231, 371], dtype=torch.int32, device="cuda")
+    q = torch.randn(371, hq, 64, generator=g, device="cuda", dtype=torch.bfloat16)
+    out, lse = cache.attend(0, q, qsl, mask.cuda(), pos)
+    cache.check()
+    ws = mcpu.new_workspace(mcpu.dims(q, cache.k[0], cache.block_table, cache.seq_lens))
+    o2, l2 = torch.empty_like(out), torch.empty_like(lse)
+    mcpu.mcpu_paged_attention_forward(q, cache.k[0], cache.v[0], cache.block_table, cache.seq_lens, qsl, window, 0.125,
+                                      o2, l2, ws)
+    # both round each weight and the output to bf16 once: 2^-8 of a weighted mean of |v| <= 6, twice
+    assert float((out.float() - o2.float()).abs().max()) <= 2 * 2 * 2.0 ** -8 * 6
+    assert float((lse - l2).abs().max()) <= 1e-4
