@@ -559,7 +559,7 @@ PAGE_SCRATCH = 64
 
 _BF16, _FP32, _INT32 = torch.bfloat16, torch.float32, torch.int32
 _pack_dims = struct.Struct("8i").pack  # the fields of Dims, in order
-_current_device = torch.cuda.current_device
+_current_device = torch._C._cuda_getDevice  # no Python frame: the tensors of a call have set CUDA up
 _current_stream = torch._C._cuda_getCurrentRawStream
 _norm_rope = _lib.mcpu_norm_rope_kv_append
 _tree_forward = _lib.mcpu_tree_attention_forward
@@ -579,14 +579,38 @@ def _int32(x, what):
     return x.data_ptr()
 
 
+def _rows(block_table, seq_lens, query_start_loc):
+    """Rows and width of a batch's tables, which have to be there for every row."""
+    rows, (have, width) = seq_lens.shape[0], block_table.shape
+    if block_table.dtype is not _INT32 or seq_lens.dtype is not _INT32 or query_start_loc.dtype is not _INT32 or \
+            have < rows or query_start_loc.numel() <= rows or not block_table.is_contiguous() or \
+            not seq_lens.is_contiguous() or not query_start_loc.is_contiguous():
+        raise ValueError("block_table, seq_lens and query_start_loc must be contiguous int32 tensors [B, max_pages], "
+                         "[B] and [B + 1]")
+    return rows, width
+
+
+def _pages(block_table, seq_lens, page_refs, free_pages, free_count, page_scratch):
+    """Rows and width of the tables whose pages are shared, and the pages that are counted."""
+    (rows, width), pages = block_table.shape, page_refs.shape[0]
+    if block_table.dtype is not _INT32 or seq_lens.dtype is not _INT32 or page_refs.dtype is not _INT32 or \
+            free_pages.dtype is not _INT32 or free_count.dtype is not _INT32 or page_scratch.dtype is not _INT32 or \
+            seq_lens.numel() < rows or page_scratch.numel() < PAGE_SCRATCH or not block_table.is_contiguous() or \
+            not seq_lens.is_contiguous() or not page_refs.is_contiguous() or not free_pages.is_contiguous() or \
+            not page_scratch.is_contiguous():
+        raise ValueError("block_table, seq_lens, page_refs, free_pages, free_count and page_scratch must be contiguous "
+                         "int32 tensors [B, max_pages], [B], [pages], [pages], [1] and [PAGE_SCRATCH]")
+    return rows, width, pages
+
+
 def mcpu_norm_rope_kv_append(q, k_new, v_new, q_weight, k_weight, eps, positions, cos_sin, q_out, k_cache, v_cache,
                              block_table, seq_lens, query_start_loc, status_word, stream=None):
     """RMS norm of every q and k head (float32 weights [D]), rotation at
     positions (int32 [T], or None for the tokens' own slots), q to q_out, K
     and V to the pages. q, k_new and v_new may be slices of one projection's
     output (any token stride that is a multiple of 8 elements)."""
-    q_shape, k_shape = q.shape, k_new.shape
-    t, hq, d = q_shape
+    k_shape = k_new.shape
+    t, hq, d = q.shape
     pages, hkv, page, _ = k_cache.shape
     max_position, table_d = cos_sin.shape
     if k_shape != (t, hkv, d) or v_new.shape != k_shape:
@@ -597,23 +621,26 @@ def mcpu_norm_rope_kv_append(q, k_new, v_new, q_weight, k_weight, eps, positions
         raise ValueError("q, k_new and v_new must be bfloat16 with the heads of a token dense")
     if cos_sin.dtype is not _FP32 or table_d != d or not cos_sin.is_contiguous():
         raise ValueError("cos_sin must be a contiguous float32 [max_position, head_dim] tensor")
-    if q_weight.shape != (d,) or k_weight.shape != (d,) or q_weight.dtype is not _FP32 or \
+    if q_weight.numel() != d or k_weight.numel() != d or q_weight.dtype is not _FP32 or \
             k_weight.dtype is not _FP32 or not q_weight.is_contiguous() or not k_weight.is_contiguous():
         raise ValueError("q_weight and k_weight must be contiguous float32 [head_dim] tensors")
-    if q_out.dtype is not _BF16 or q_out.shape != q_shape or not q_out.is_contiguous():
+    if q_out.dtype is not _BF16 or q_out.numel() != t * hq * d or not q_out.is_contiguous():
         raise ValueError("q_out must be a contiguous bfloat16 tensor of q's shape")
     if positions is not None:
         if positions.shape != (t,):
             raise ValueError("positions must have one entry per query token")
         positions = _int32(positions, "positions")
+    if k_cache.dtype is not _BF16 or v_cache.dtype is not _BF16 or v_cache.numel() != pages * hkv * page * d or \
+            not k_cache.is_contiguous() or not v_cache.is_contiguous():
+        raise ValueError("k_cache and v_cache must be contiguous bfloat16 tensors of one shape")
+    rows, width = _rows(block_table, seq_lens, query_start_loc)
     kv = hkv * d  # a lone token's stride says nothing
     code = _norm_rope(
         q.data_ptr(), qs[0] if t > 1 else hq * d, k_new.data_ptr(), ks[0] if t > 1 else kv, v_new.data_ptr(),
         vs[0] if t > 1 else kv, q_weight.data_ptr(), k_weight.data_ptr(), eps, positions, cos_sin.data_ptr(),
         max_position, q_out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(),
-        seq_lens.data_ptr(), query_start_loc.data_ptr(),
-        _pack_dims(seq_lens.shape[0], t, block_table.shape[1], pages, hq, hkv, d, page), status_word.data_ptr(),
-        _raw_stream(stream))
+        seq_lens.data_ptr(), query_start_loc.data_ptr(), _pack_dims(rows, t, width, pages, hq, hkv, d, page),
+        _int32(status_word, "status_word"), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_norm_rope_kv_append")
 
@@ -641,12 +668,19 @@ def mcpu_tree_attention_forward(q, k_cache, v_cache, block_table, seq_lens, quer
     t, hq, d = q.shape
     pages, hkv, page, _ = k_cache.shape
     nodes, words = tree_mask.shape
+    if q.dtype is not _BF16 or out.dtype is not _BF16 or k_cache.dtype is not _BF16 or v_cache.dtype is not _BF16 or \
+            lse.dtype is not _FP32 or out.numel() != t * hq * d or lse.numel() != t * hq or \
+            v_cache.numel() != pages * hkv * page * d or not q.is_contiguous() or not out.is_contiguous() or \
+            not lse.is_contiguous() or not k_cache.is_contiguous() or not v_cache.is_contiguous():
+        raise ValueError("q, out, k_cache and v_cache must be contiguous bfloat16 tensors, the two of a pair of one "
+                         "shape, lse a contiguous float32 [T, H_q] tensor")
+    rows, width = _rows(block_table, seq_lens, query_start_loc)
     if nodes != t or not 1 <= words <= MAX_TREE_WORDS:
         raise ValueError(f"tree_mask must be an int32 [T, words] tensor of at most {MAX_TREE_WORDS} words "
                          "(longer chunks are the rows of mcpu_paged_attention_forward)")
     if sinks is not None:
-        if sinks.dtype is not _FP32 or sinks.shape != (hq,) or not sinks.is_cuda:
-            raise ValueError("sinks must be a float32 CUDA tensor with one value per q head")
+        if sinks.dtype is not _FP32 or sinks.shape != (hq,) or not sinks.is_cuda or not sinks.is_contiguous():
+            raise ValueError("sinks must be a contiguous float32 CUDA tensor with one value per q head")
         sinks = sinks.data_ptr()
     if positions is not None:
         if positions.shape != (t,):
@@ -655,8 +689,8 @@ def mcpu_tree_attention_forward(q, k_cache, v_cache, block_table, seq_lens, quer
     code = _tree_forward(
         q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
         query_start_loc.data_ptr(), _int32(tree_mask, "tree_mask"), words, positions, sliding_window, softmax_scale,
-        sinks, _pack_dims(seq_lens.shape[0], t, block_table.shape[1], pages, hq, hkv, d, page), out.data_ptr(),
-        lse.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(stream))
+        sinks, _pack_dims(rows, t, width, pages, hq, hkv, d, page), out.data_ptr(), lse.data_ptr(),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_tree_attention_forward")
 
@@ -689,15 +723,15 @@ def mcpu_compact_kv(pools, block_table, seq_lens, query_start_loc, accept_path, 
     the rows' lengths."""
     if not pools.bf16_pages:
         raise ValueError("mcpu_compact_kv takes bfloat16 [num_pages, H_kv, 16, 64] pools")
-    rows = seq_lens.shape[0]
+    rows, width = _rows(block_table, seq_lens, query_start_loc)
     paths, most = accept_path.shape
-    if paths != rows:
-        raise ValueError("accept_path must be an int32 [B, max_accept] tensor")
+    if paths != rows or accept_len.numel() != rows or new_seq_lens.numel() != rows:
+        raise ValueError("accept_path must be an int32 [B, max_accept] tensor, accept_len and new_seq_lens int32 [B]")
     code = _compact_kv(
         pools.pointers, pools.num_pools, block_table.data_ptr(), seq_lens.data_ptr(), query_start_loc.data_ptr(),
         _int32(accept_path, "accept_path"), most, _int32(accept_len, "accept_len"),
-        _pack_dims(rows, 0, block_table.shape[1], pools.num_pages, pools.num_kv_heads, pools.num_kv_heads, 64, 16),
-        new_seq_lens.data_ptr(), status_word.data_ptr(), _raw_stream(stream))
+        _pack_dims(rows, 0, width, pools.num_pages, pools.num_kv_heads, pools.num_kv_heads, 64, 16),
+        _int32(new_seq_lens, "new_seq_lens"), _int32(status_word, "status_word"), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_compact_kv")
 
@@ -707,15 +741,15 @@ def mcpu_fork_block_tables(block_table, seq_lens, src_rows, dst_rows, page_refs,
     """Makes rows dst_rows copies of src_rows: full pages shared (page_refs),
     a partial last page replaced by a fresh one whose contents
     mcpu_copy_pages(pools, copy_src, copy_dst, ...) brings over."""
-    n = src_rows.shape[0]
-    rows, width = block_table.shape
-    if dst_rows.shape[0] != n or copy_src.shape[0] < n or copy_dst.shape[0] < n or page_scratch.shape[0] < PAGE_SCRATCH:
-        raise ValueError("dst_rows, copy_src and copy_dst must have one entry per fork, page_scratch PAGE_SCRATCH")
+    n = src_rows.numel()
+    rows, width, pages = _pages(block_table, seq_lens, page_refs, free_pages, free_count, page_scratch)
+    if dst_rows.numel() != n or copy_src.numel() < n or copy_dst.numel() < n:
+        raise ValueError("dst_rows, copy_src and copy_dst must have one entry per fork")
     code = _fork_tables(
         block_table.data_ptr(), seq_lens.data_ptr(), _int32(src_rows, "src_rows"), _int32(dst_rows, "dst_rows"), n,
-        _pack_dims(rows, 0, width, page_refs.shape[0], 1, 1, 64, 16), page_refs.data_ptr(), free_pages.data_ptr(),
+        _pack_dims(rows, 0, width, pages, 1, 1, 64, 16), page_refs.data_ptr(), free_pages.data_ptr(),
         free_count.data_ptr(), _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), page_scratch.data_ptr(),
-        status_word.data_ptr(), _raw_stream(stream))
+        _int32(status_word, "status_word"), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_fork_block_tables")
 
@@ -724,14 +758,13 @@ def mcpu_shrink_block_tables(block_table, seq_lens, sliding_window, page_refs, f
                              status_word, stream=None):
     """Releases every page past the rows' lengths (and, with a window, before
     it); pages without another holder return to the stack."""
-    rows, width = block_table.shape
-    pages = page_refs.shape[0]
-    if free_pages.shape[0] < pages or page_scratch.shape[0] < PAGE_SCRATCH:
-        raise ValueError("free_pages must hold as many pages as page_refs counts, page_scratch PAGE_SCRATCH words")
+    rows, width, pages = _pages(block_table, seq_lens, page_refs, free_pages, free_count, page_scratch)
+    if free_pages.numel() < pages:
+        raise ValueError("free_pages must hold as many pages as page_refs counts")
     code = _shrink_tables(
         block_table.data_ptr(), seq_lens.data_ptr(), sliding_window, _pack_dims(rows, 0, width, pages, 1, 1, 64, 16),
         page_refs.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(), page_scratch.data_ptr(),
-        status_word.data_ptr(), _raw_stream(stream))
+        _int32(status_word, "status_word"), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_shrink_block_tables")
 
@@ -739,11 +772,11 @@ def mcpu_shrink_block_tables(block_table, seq_lens, sliding_window, page_refs, f
 def mcpu_copy_pages(pools, copy_src, copy_dst, status_word, stream=None):
     """Copies page copy_src[f] to copy_dst[f] in every pool of the PoolList
     (bf16 or fp8); pairs with a negative page are skipped."""
-    n = copy_src.shape[0]
-    if copy_dst.shape[0] != n:
+    n = copy_src.numel()
+    if copy_dst.numel() != n:
         raise ValueError("copy_src and copy_dst must have the same length")
     code = _copy_pages(pools.pointers, pools.num_pools, pools.page_bytes, pools.num_pages,
-                       _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), n, status_word.data_ptr(),
-                       _raw_stream(stream))
+                       _int32(copy_src, "copy_src"), _int32(copy_dst, "copy_dst"), n,
+                       _int32(status_word, "status_word"), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_copy_pages")

@@ -260,3 +260,67 @@ def test_host_stage_host_checks(lib):
                                              ctypes.c_int32, ctypes.c_void_p]
     assert call(None, None, None, None, None, None, None, None, None, 0, 0.125, ctypes.byref(d), None, None, None,
                 0, None, 0, None) == 1
+
+
+def _round_args():
+    """Valid arguments of the tree-round calls (CPU tensors: nothing is launched, the stream has no handle)."""
+    from paper_2608_22167_gb300 import mcpu
+
+    def z(*shape, dtype=torch.int32):
+        return torch.zeros(shape, dtype=dtype)
+
+    bf16, f32 = torch.bfloat16, torch.float32
+    q, k, kc = z(4, 8, 64, dtype=bf16), z(4, 2, 64, dtype=bf16), z(5, 2, 16, 64, dtype=bf16)
+    tables = dict(block_table=z(3, 6), seq_lens=z(3), query_start_loc=z(4), status_word=z(1), stream=object())
+    pages = dict(block_table=z(3, 6), seq_lens=z(3), page_refs=z(5), free_pages=z(5), free_count=z(1),
+                 page_scratch=z(mcpu.PAGE_SCRATCH), status_word=z(1), stream=object())
+    tree = dict(tables, q=q, k_cache=kc, v_cache=kc.clone(), tree_mask=z(4, 1), positions=None, sliding_window=0,
+                softmax_scale=0.125, out=q.clone(), lse=z(4, 8, dtype=f32), workspace=z(256, dtype=torch.uint8))
+    del tree["status_word"]
+    pools = mcpu.PoolList([kc, kc.clone()])
+    return {
+        "mcpu_norm_rope_kv_append": dict(
+            tables, q=q, k_new=k, v_new=k.clone(), q_weight=z(64, dtype=f32), k_weight=z(64, dtype=f32), eps=1e-6,
+            positions=None, cos_sin=z(9, 64, dtype=f32), q_out=q.clone(), k_cache=kc, v_cache=kc.clone()),
+        "mcpu_tree_attention_forward": tree,
+        "mcpu_compact_kv": dict(tables, pools=pools, accept_path=z(3, 2), accept_len=z(3), new_seq_lens=z(3)),
+        "mcpu_fork_block_tables": dict(pages, src_rows=z(2), dst_rows=z(2), copy_src=z(2), copy_dst=z(2)),
+        "mcpu_shrink_block_tables": dict(pages, sliding_window=0),
+        "mcpu_copy_pages": dict(pools=pools, copy_src=z(2), copy_dst=z(2), status_word=z(1), stream=object()),
+    }
+
+
+@pytest.mark.parametrize("name", sorted(_round_args()))
+def test_tree_round_calls_refuse_what_they_would_misread(name):
+    from paper_2608_22167_gb300 import mcpu
+
+    call, args = getattr(mcpu, name), _round_args()[name]
+    with pytest.raises(AttributeError):  # the arguments as they are get as far as the stream, which has no handle
+        call(**args)
+    for key, x in args.items():
+        if not torch.is_tensor(x):
+            continue
+        wrong = [x.double() if x.is_floating_point() else x.long()] if x.dtype != torch.uint8 else []
+        if x.shape[-1] > 1 and x.dtype != torch.uint8 and not (key in ("q", "k_new", "v_new") and "norm" in name):
+            wrong.append(torch.stack([x, x], -1)[..., 0])  # every second element of a wider tensor
+        # too short; the rows are those of seq_lens, or of the table where pages are shared
+        if key in ("query_start_loc", "out", "lse", "v_cache", "q_out", "page_scratch", "dst_rows", "copy_dst",
+                   "accept_len", "new_seq_lens", "accept_path", "tree_mask") or \
+                key == ("seq_lens" if "page_refs" in args else "block_table") or key == "free_pages" and "shrink" in name:
+            wrong.append(x[:-1])
+        if key == "block_table":
+            wrong.append(torch.zeros(3, 9, dtype=torch.int32)[:, :6])  # a slice of a wider table
+        for bad in wrong:
+            with pytest.raises(ValueError):
+                call(**dict(args, **{key: bad}))
+
+
+def test_tree_attention_refuses_slices_of_a_projection_and_strided_sinks():
+    from paper_2608_22167_gb300 import mcpu
+
+    args = _round_args()["mcpu_tree_attention_forward"]
+    packed = torch.zeros(4, 12 * 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        mcpu.mcpu_tree_attention_forward(**dict(args, q=packed[:, :512].unflatten(1, (8, 64))))
+    with pytest.raises(ValueError):
+        mcpu.mcpu_tree_attention_forward(**dict(args, sinks=torch.zeros(16)[::2]))
