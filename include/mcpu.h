@@ -532,8 +532,9 @@ mcpu_status mcpu_compact_kv(void* const* pools, int32_t num_pools, const int32_t
  * [num_pages] and free_count are the stack of mcpu_grow_block_tables.
  * page_scratch: MCPU_PAGE_SCRATCH int32, zeroed once before its first use
  * (the calls leave it zero). All calls that touch one stack must be ordered
- * (one stream). They use num_seqs, max_pages_per_seq and num_pages of dims;
- * page and stack sizes are not otherwise limited.
+ * (one stream). They use num_seqs, max_pages_per_seq (of less than 0x7fff0000
+ * tokens) and num_pages (less than 0x7fff0000) of dims; page and stack sizes
+ * are not otherwise limited.
  *
  * mcpu_fork_block_tables: row dst_rows[f] becomes a copy of row src_rows[f]
  * (device int32 [num_forks], num_forks <= 2048): its S / 16 full pages are

@@ -29,7 +29,9 @@ mcpu_status check_pools(void* const* pools, int32_t num_pools, PoolPtrs* out) {
 
 mcpu_status check_page_dims(const mcpu_dims* d) {
   if (!d || d->num_seqs < 0 || d->max_pages_per_seq < 0 || d->num_pages < 0) return MCPU_ERR_INVALID_ARG;
-  if ((int64_t)d->max_pages_per_seq * kPage >= (int64_t)0x7fff0000) return MCPU_ERR_UNSUPPORTED;
+  // token positions and rounded-up page counts stay within 32 bits
+  if ((int64_t)d->max_pages_per_seq * kPage >= (int64_t)0x7fff0000 || d->num_pages >= 0x7fff0000)
+    return MCPU_ERR_UNSUPPORTED;
   return MCPU_OK;
 }
 

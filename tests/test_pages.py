@@ -602,3 +602,14 @@ def test_a_fork_into_a_row_that_holds_a_page_is_reported(at):
     _fork(d, [0], [2])
     m.fork([0], [2])
     m.same(d, mcpu.STATUS_BAD_PAGE)
+
+
+@pytest.mark.parametrize("pages", [0x7fff0000, 0x7fffffff])
+def test_page_counts_that_do_not_fit_are_refused(pages):
+    # dividing so many pages into segments would pass 32 bits
+    from paper_2608_22167_gb300 import mcpu
+
+    P = 1 << 20
+    d = mcpu.Dims(4, 0, 19, pages, 1, 1, 64, 16)
+    assert mcpu._lib.mcpu_shrink_block_tables(P, P, 0, ctypes.byref(d), P, P, P, P, P, None) == 2
+    assert mcpu._lib.mcpu_fork_block_tables(P, P, P, P, 3, ctypes.byref(d), P, P, P, P, P, P, P, None) == 2
