@@ -458,7 +458,8 @@ mcpu_status mcpu_host_stage_sync(mcpu_host_stage* stage);
  * *_stride elements from one token to the next (a multiple of 8, at least
  * H * D: q, k and v may be slices of one projection's output); 16-byte
  * aligned. eps >= 0, finite. An all-zero vector with eps = 0 gives zeros; the
- * sum of a vector's squares has to stay below 3e38.
+ * sum of a vector's squares has to stay below 3e38 (and, with eps = 0, above
+ * 1e-36: below that squares are lost). A NaN makes all of its head row NaN.
  * Errors as mcpu_rope_kv_append: a position outside [0, max_position) or
  * inconsistent lengths set MCPU_ERR_BAD_LENGTHS and leave the token
  * untouched, a bad page skips its K/V write (MCPU_ERR_BAD_PAGE).

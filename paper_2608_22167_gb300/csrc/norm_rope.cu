@@ -16,7 +16,7 @@
 // spread over up to eight warps, so that a decode step fills the GPU.
 // Measured (64 q / 8 kv heads): 33.8k tokens 115 us, 6.1 TB/s read and
 // written, 90 % of the copy rate; 4096 tokens in 256 rows 20 us; 64 tokens
-// 3.8 us in a graph. A warp per token against two or four at 4096 tokens: 22,
+// 3.7 us in a graph. A warp per token against two or four at 4096 tokens: 22,
 // 26 and 29 us (each warp pays for the lookups); rows streamed through shared
 // memory by bulk copies instead, seven warps an SM: 167 us for the 33.8k.
 #include "tree_round.cuh"

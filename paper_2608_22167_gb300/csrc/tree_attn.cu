@@ -39,10 +39,11 @@
 // always ready 1460). Its loop over plain blocks is kept apart from all that is
 // rare: with masks, first blocks and rescaling inside it, it took 2430, much of
 // it waiting for instructions. Measured on a GB300: 64 rows of 2k-16k keys with
-// 1-16 nodes 192 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 535-560 us
-// (815-855 TFLOP/s, by the clock that the power limit leaves), two rows of
-// 49k-65k keys with 61 and 64 nodes 112-115 us (1030-1050 TFLOP/s), 384 rows in
-// a window of 128 keys 93 us, four rows of up to 308 keys 9.2 us.
+// 1-16 nodes 192-195 us (6.3 TB/s of K/V), 4k-32k keys with 16-32 nodes 533-566
+// us (805-860 TFLOP/s, by the clock that the power limit leaves), two rows of
+// 49k-65k keys with 61 and 64 nodes 114-117 us (1010-1030 TFLOP/s), 384 rows in
+// a window of 128 keys 94 us, four rows of up to 308 keys 9.3 us (11.7 where a
+// wide table has the merge launched).
 //
 // Waits are bounded; one that runs out raises an abort flag, every role ends,
 // and TMEM is freed after the issuers' MMAs have drained.
@@ -1113,7 +1114,7 @@ cudaError_t launch_tree(const CUtensorMap& kmap, const CUtensorMap& vmap, const 
   if (e != cudaSuccess) return e;
   // Rows whose tables, or windows, hold no more than kWholeBlocks blocks have no
   // cut tiles, and nothing to merge: without the second launch four short rows
-  // take 9.8 us instead of 12.1, 384 rows in a window of 128 keys 98 instead of 100.
+  // take 9.3 us instead of 11.7. (The host knows the table's width, not the lengths.)
   const int64_t most_nodes = p.total_q < 32 * p.words ? p.total_q : 32 * p.words;
   int64_t keys = (int64_t)p.max_pages * kPage;
   if (p.window > 0 && keys > most_nodes + p.window + kPage) keys = most_nodes + p.window + kPage;
