@@ -82,9 +82,12 @@ typedef enum mcpu_status {
   MCPU_ERR_TIMEOUT = 7,              /* device: a bounded wait gave up */
   MCPU_ERR_INTERNAL = 8,             /* device: work plan overflowed its bound */
   MCPU_ERR_POOL_EXHAUSTED = 9,       /* device: the free-page stack ran empty */
-  MCPU_ERR_UNSUPPORTED_ROW = 10      /* device: a row the called variant does not handle was
+  MCPU_ERR_UNSUPPORTED_ROW = 10,     /* device: a row the called variant does not handle was
                                         skipped (an append row given to the fp8 forward, a
-                                        tree with more nodes than its mask has bits) */
+                                        tree with more nodes than its mask has bits, a row
+                                        to evict from that shares pages) */
+  MCPU_ERR_BAD_VALUES = 11           /* device: logits or a temperature that give no
+                                        distribution (mcpu_verify_tree) */
 } mcpu_status;
 
 typedef struct mcpu_dims {
@@ -436,6 +439,7 @@ mcpu_status mcpu_host_stage_sync(mcpu_host_stage* stage);
  *   mcpu_grow_block_tables_from  (once) pages for the drafted tokens
  *   mcpu_norm_rope_kv_append     q/k norm, rotation at the nodes' positions, K/V to the pages
  *   mcpu_tree_attention_forward  every node over the context and its ancestors
+ *   mcpu_verify_tree             (once) which nodes are accepted, and the next token
  *   mcpu_compact_kv              (once, all layers) accepted nodes' K/V rows to the front
  *   mcpu_shrink_block_tables     (once) pages past the new lengths back to the stack
  * and, when samples are added to a running prompt, mcpu_fork_block_tables
@@ -506,6 +510,56 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
                                         int32_t mask_words, const int32_t* positions, int32_t sliding_window,
                                         float softmax_scale, const float* sinks, const mcpu_dims* dims, void* out,
                                         float* lse, void* workspace, size_t workspace_bytes, mcpu_stream_t stream);
+
+/*
+ * Verification of the drafted tokens against the target model, by rejection
+ * sampling with the random numbers given, so that the tokens a row emits are
+ * distributed as if it had been sampled token by token. Row r's tree: node
+ * i (t = query_start_loc[r] + i) holds tokens[t] and hangs below node parents[t]
+ * of the row; node 0 is the row's last token. logits[t * logits_stride + y],
+ * y < vocab, are the target's for the token after node i. With T = temperature[r]
+ * and p = softmax(logits / T) of the node the walk is at (first node 0, which
+ * is always accepted), its children c are tried in ascending order:
+ *   draft_logits given:  q = softmax(draft_logits / T) of the same node, from
+ *     which its children were drawn;  rest(y) = max(p(y) - M q(y), 0)
+ *     accept c iff uniforms[t_c] m q(x_c) < rest(x_c);  else M += m, m = sum_y rest(y)
+ *   without (children chosen, not drawn):  rest(y) = p(y), 0 for the tokens of
+ *     rejected children;  accept c iff uniforms[t_c] m < rest(x_c);  else m -= rest(x_c)
+ * from M = 0, m = 1, x_c = tokens[t_c]. The walk goes on from the first
+ * accepted child; where none is (or max_accept nodes are on the path),
+ *   next_token[r] = argmax_y rest(y) / exponentials[r * exponentials_stride + y]
+ * (the lowest y among equals), which draws y with probability rest(y) / m from
+ * numbers of the exponential distribution; p stands in for rest if all of it is
+ * 0. uniforms (float [T]) lie in [0, 1), exponentials are > 0. T = 0 is
+ * greedy: the child whose token is the lowest argmax of the logits, which is
+ * next_token otherwise; no random numbers are read. temperature NULL: all rows
+ * greedy, uniforms and exponentials may be NULL.
+ * accept_path[r * max_accept ..] receives the path's nodes, then -1;
+ * accept_len[r] their number (both as mcpu_compact_kv takes them);
+ * logprobs[r * max_accept + i] (float, or NULL) log p of the token emitted
+ * after path node i - the next path node's, or next_token[r] at the end - (at
+ * temperature 1 for greedy rows), then 0.
+ * A token outside [0, vocab) (padding) is never accepted, a node whose parent
+ * does not come before it never reached. -inf logits are tokens of probability
+ * 0. Where a visited node's logits hold a NaN or +inf or nothing above -inf, or
+ * the row's temperature is neither 0 nor in [1e-20, 1e20], the walk ends with
+ * next_token = -1 and a NaN logprob, and MCPU_ERR_BAD_VALUES is reported. A row
+ * without nodes gets accept_len 0 and next_token -1, and so does one with
+ * more than MCPU_MAX_TREE_NODES (MCPU_ERR_UNSUPPORTED_ROW) or inconsistent
+ * query_start_loc (MCPU_ERR_BAD_LENGTHS).
+ * logits, draft_logits: logits_type MCPU_BF16 or MCPU_FP32 elements, any
+ * stride >= vocab. Sums and probabilities are fp32, the tests of children fp64.
+ */
+#define MCPU_MAX_TREE_NODES 256
+#define MCPU_BF16 0
+#define MCPU_FP32 1
+mcpu_status mcpu_verify_tree(const void* logits, int64_t logits_stride, const void* draft_logits,
+                             int64_t draft_stride, int32_t logits_type, int32_t vocab, const int32_t* tokens,
+                             const int32_t* parents, const int32_t* query_start_loc, const float* temperature,
+                             const float* uniforms, const float* exponentials, int64_t exponentials_stride,
+                             int32_t num_seqs, int32_t total_q, int32_t max_accept, int32_t* accept_path,
+                             int32_t* accept_len, int32_t* next_token, float* logprobs, int32_t* status_word,
+                             mcpu_stream_t stream);
 
 /*
  * Keeps an accepted path of each row's tree: for i < accept_len[r], the K/V
@@ -585,6 +639,70 @@ mcpu_status mcpu_shrink_block_tables(int32_t* block_table, const int32_t* seq_le
 mcpu_status mcpu_copy_pages(void* const* pools, int32_t num_pools, int64_t page_bytes, int32_t num_pages,
                             const int32_t* copy_src, const int32_t* copy_dst, int32_t num_copies,
                             int32_t* status_word, mcpu_stream_t stream);
+
+/*
+ * A bounded cache. Every kv head of a layer counts the attention that its keys
+ * have got, and rows that have grown past a limit are cut down to a budget of
+ * keys a head: the first ones (which softmax attention leans on), the latest,
+ * and those that got most.
+ *
+ * mcpu_accumulate_weights, after a step's attention: for every slot j < S_r of
+ * row r and kv head h
+ *   w[r][h][j] = (j < C_r ? decay * w[r][h][j] : 0)
+ *                + sum_{i: j <= p_i, p_i - j < W} sum_{u} exp(scale q_iu . k_j - lse_iu)
+ * over the queries i of the row at positions p_i = C_r + i and the q heads u of
+ * h; W = sliding_window if it is > 0, else unbounded. w is key_weights, float
+ * [num_seqs, H_kv, max_slots]; q, lse [T, H_q] and the scale are those of the
+ * attention call (lse with its sinks), made with the same window.
+ * query_path NULL: the queries are all L_r of the row, C_r = S_r - L_r. Else the
+ * row's path_len[r] query tokens query_path[r * max_path + i] (numbers in the
+ * row, 0 .. L_r - 1), C_r = S_r - path_len[r]: the accepted nodes once
+ * mcpu_compact_kv has moved them (with its new_seq_lens), or the last queries of
+ * a long prompt alone.
+ * decay in [0, 1]; 0 reads no old weights. A row without queries keeps its
+ * weights as they are, and so do slots from S_r on. A query with lse = -inf (it
+ * saw nothing) adds nothing; a NaN among a key or a query that sees it makes that
+ * key's weight NaN. A row longer than max_slots or its table, or with a path
+ * that breaks the rules, is skipped (MCPU_ERR_BAD_LENGTHS); keys of a page
+ * outside the pool keep their weights (MCPU_ERR_BAD_PAGE).
+ * Sums are fp32 in a fixed order: the same inputs give the same bits on the
+ * same device. workspace: mcpu_weights_workspace_size(dims) bytes, 256-byte
+ * aligned, the status word first (zero it once). Capturable.
+ *
+ * mcpu_evict_kv: every row with S_r > limit is cut to budget slots, for each
+ * layer m and kv head h by key_weights (float [num_layers, num_seqs, H_kv,
+ * max_slots]). Slots [0, keep_first) and the last keep_last stay; of the
+ * others the budget - keep_first - keep_last with the highest weight (the lowest
+ * slot among equals; NaN counts as lowest). Kept slots below
+ * budget - keep_last do not move; those of the others at or past it fill the
+ * holes, lowest into lowest; the last keep_last follow in order. K, V and the
+ * weights move; new_key_weights (may be key_weights) receives the weights of all
+ * slots < new_seq_lens[r], which is budget, or S_r for a row left as it is.
+ * Slots past it keep stale contents; mcpu_shrink_block_tables returns their pages.
+ * limit >= budget >= keep_first + keep_last, budget >= 1. The slot of a key no
+ * longer says its position afterwards: give positions to
+ * mcpu_norm_rope_kv_append (it rotates at any, whatever the slot), and do not
+ * use a sliding window that reaches into the evicted part.
+ * pools: host array of 2 num_layers (num_layers 0 .. MCPU_MAX_POOLS / 2) device
+ * pointers, the layers' K pools, then their V pools. page_refs (device int32
+ * [num_pages], or NULL if no page is shared): a row that holds a page with
+ * other holders among those of slots [keep_first, budget) is left as it is and
+ * reported (MCPU_ERR_UNSUPPORTED_ROW): its keys cannot move without the other
+ * rows'. A row with a page outside the pool there or up to S_r is left too
+ * (MCPU_ERR_BAD_PAGE), and one longer than its table or max_slots
+ * (MCPU_ERR_BAD_LENGTHS). new_seq_lens must not be seq_lens.
+ */
+size_t mcpu_weights_workspace_size(const mcpu_dims* dims);
+mcpu_status mcpu_accumulate_weights(const void* q, const float* lse, const void* k_cache,
+                                    const int32_t* block_table, const int32_t* seq_lens,
+                                    const int32_t* query_start_loc, const int32_t* query_path, int32_t max_path,
+                                    const int32_t* path_len, int32_t sliding_window, float softmax_scale,
+                                    float decay, const mcpu_dims* dims, float* key_weights, int32_t max_slots,
+                                    void* workspace, size_t workspace_bytes, mcpu_stream_t stream);
+mcpu_status mcpu_evict_kv(void* const* pools, int32_t num_layers, const float* key_weights, int32_t max_slots,
+                          const int32_t* block_table, const int32_t* seq_lens, int32_t limit, int32_t budget,
+                          int32_t keep_first, int32_t keep_last, const int32_t* page_refs, const mcpu_dims* dims,
+                          float* new_key_weights, int32_t* new_seq_lens, int32_t* status_word, mcpu_stream_t stream);
 
 /* Synchronises `stream`, reads the workspace status word and maps it to the
  * most severe mcpu_status (MCPU_OK if clear). The raw bits go to

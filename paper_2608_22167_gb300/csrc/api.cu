@@ -180,7 +180,7 @@ bool encode_query(CUtensorMap* map, const void* q, int32_t total_q, int32_t num_
 
 extern "C" {
 
-int32_t mcpu_abi_version(void) { return 9; }
+int32_t mcpu_abi_version(void) { return 10; }
 
 int32_t mcpu_last_cuda_error(void) { return mcpu::t_last_cuda_error; }
 
@@ -197,6 +197,7 @@ const char* mcpu_status_string(mcpu_status s) {
     case MCPU_ERR_INTERNAL: return "work plan exceeded its bound";
     case MCPU_ERR_POOL_EXHAUSTED: return "no free KV page left";
     case MCPU_ERR_UNSUPPORTED_ROW: return "a row this variant does not handle was skipped";
+    case MCPU_ERR_BAD_VALUES: return "logits or a temperature that give no distribution";
   }
   return "unknown status";
 }
@@ -608,6 +609,7 @@ mcpu_status mcpu_read_device_status(const void* workspace, mcpu_stream_t stream,
   if (bits & kStatusPlanOverflow) return MCPU_ERR_INTERNAL;
   if (bits & kStatusPoolExhausted) return MCPU_ERR_POOL_EXHAUSTED;
   if (bits & kStatusUnsupportedRow) return MCPU_ERR_UNSUPPORTED_ROW;
+  if (bits & kStatusBadValues) return MCPU_ERR_BAD_VALUES;
   return MCPU_OK;
 }
 

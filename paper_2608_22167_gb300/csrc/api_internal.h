@@ -11,6 +11,9 @@
 
 namespace mcpu {
 
+// Status bit of MCPU_ERR_BAD_VALUES (the others are in common.cuh).
+constexpr int32_t kStatusBadValues = 64;
+
 // MCPU_OK, or the error for dims the kernels cannot serve: null, negative
 // or inconsistent sizes (MCPU_ERR_INVALID_ARG); head_dim != 64,
 // page_size != 16, H_q / H_kv outside {1, 2, 4, 8}, more than 2048 rows, or

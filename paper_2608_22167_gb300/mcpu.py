@@ -36,6 +36,7 @@ STATUS = {
     8: "MCPU_ERR_INTERNAL",
     9: "MCPU_ERR_POOL_EXHAUSTED",
     10: "MCPU_ERR_UNSUPPORTED_ROW",
+    11: "MCPU_ERR_BAD_VALUES",
 }
 FLAG_NO_CASCADE = 0x1
 FLAG_MMA_SYNC_APPEND = 0x2
@@ -49,6 +50,7 @@ STATUS_TIMEOUT = 4
 STATUS_PLAN_OVERFLOW = 8
 STATUS_POOL_EXHAUSTED = 16
 STATUS_UNSUPPORTED_ROW = 32
+STATUS_BAD_VALUES = 64
 
 
 class McpuError(RuntimeError):
@@ -164,6 +166,16 @@ _lib.mcpu_shrink_block_tables.argtypes = [_P, _P, _I32, _DIMS, _P, _P, _P, _P, _
 _lib.mcpu_shrink_block_tables.restype = ctypes.c_int
 _lib.mcpu_copy_pages.argtypes = [_P, _I32, _I64, _I32, _P, _P, _I32, _P, _P]
 _lib.mcpu_copy_pages.restype = ctypes.c_int
+_lib.mcpu_verify_tree.argtypes = [_P, _I64, _P, _I64, _I32, _I32, _P, _P, _P, _P, _P, _P, _I64, _I32, _I32, _I32, _P, _P,
+                                  _P, _P, _P, _P]
+_lib.mcpu_verify_tree.restype = ctypes.c_int
+_lib.mcpu_weights_workspace_size.argtypes = [_DIMS]
+_lib.mcpu_weights_workspace_size.restype = ctypes.c_size_t
+_lib.mcpu_accumulate_weights.argtypes = [_P, _P, _P, _P, _P, _P, _P, _I32, _P, _I32, _F32, _F32, _DIMS, _P, _I32, _P,
+                                         ctypes.c_size_t, _P]
+_lib.mcpu_accumulate_weights.restype = ctypes.c_int
+_lib.mcpu_evict_kv.argtypes = [_P, _I32, _P, _I32, _P, _P, _I32, _I32, _I32, _I32, _P, _DIMS, _P, _P, _P, _P]
+_lib.mcpu_evict_kv.restype = ctypes.c_int
 
 MAX_HOST_SLICES = 8
 MAX_HOST_SLOTS = 4
@@ -780,3 +792,150 @@ def mcpu_copy_pages(pools, copy_src, copy_dst, status_word, stream=None):
                        _int32(status_word, "status_word"), _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_copy_pages")
+
+
+# ------------------------------------------------- what stays after a round
+MAX_TREE_NODES = 256
+_verify_tree = _lib.mcpu_verify_tree
+_accumulate_weights = _lib.mcpu_accumulate_weights
+_evict_kv = _lib.mcpu_evict_kv
+
+
+def _row_stride(x, what, dtypes, rows, width):
+    """Elements from one row to the next of a [rows, width] tensor whose rows are dense."""
+    if x.dtype not in dtypes or x.dim() != 2 or x.shape[0] != rows or x.shape[1] != width or \
+            (width > 1 and x.stride(1) != 1):
+        raise ValueError(f"{what} must be a [{rows}, {width}] tensor of {' or '.join(map(str, dtypes))} with dense rows")
+    stride = x.stride(0) if rows > 1 else width
+    if stride < width:
+        raise ValueError(f"the rows of {what} must not overlap")
+    return stride
+
+
+def _vector(x, what, dtype, n):
+    if x.dtype is not dtype or x.shape != (n,) or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of {n} elements")
+    return x.data_ptr()
+
+
+def mcpu_verify_tree(logits, tokens, parents, query_start_loc, temperature, uniforms, exponentials, accept_path,
+                     accept_len, next_token, logprobs, status_word, draft_logits=None, stream=None):
+    """Which nodes of each row's drafted tree are accepted, and the token
+    after them. logits (and draft_logits, of what the children were drawn
+    from): bfloat16 or float32 [T, vocab]; tokens, parents int32 [T];
+    temperature float32 [B] (0: greedy) or None (all greedy, uniforms and
+    exponentials may be None); uniforms float32 [T] in [0, 1), exponentials
+    float32 [B, vocab] > 0. Writes accept_path int32 [B, max_accept] and
+    accept_len int32 [B] as mcpu_compact_kv takes them, next_token int32 [B]
+    and logprobs float32 [B, max_accept] (or None) of what is emitted."""
+    t, vocab = logits.shape
+    rows, most = accept_path.shape
+    if query_start_loc.numel() != rows + 1 or most < 1:
+        raise ValueError("accept_path must be an int32 [B, max_accept] tensor, query_start_loc int32 [B + 1]")
+    ls = _row_stride(logits, "logits", (_BF16, _FP32), t, vocab)
+    ds = 0 if draft_logits is None else _row_stride(draft_logits, "draft_logits", (logits.dtype,), t, vocab)
+    es = 0
+    if temperature is not None:
+        if uniforms is None or exponentials is None:
+            raise ValueError("sampling needs uniforms and exponentials")
+        es = _row_stride(exponentials, "exponentials", (_FP32,), rows, vocab)
+        temperature = _vector(temperature, "temperature", _FP32, rows)
+        uniforms = _vector(uniforms, "uniforms", _FP32, t)
+        exponentials = exponentials.data_ptr()
+    else:
+        uniforms = exponentials = None
+    if logprobs is not None:
+        if logprobs.dtype is not _FP32 or logprobs.shape != (rows, most) or not logprobs.is_contiguous():
+            raise ValueError("logprobs must be a contiguous float32 tensor of accept_path's shape")
+        logprobs = logprobs.data_ptr()
+    code = _verify_tree(
+        logits.data_ptr(), ls, None if draft_logits is None else draft_logits.data_ptr(), ds,
+        0 if logits.dtype is _BF16 else 1, vocab, _vector(tokens, "tokens", _INT32, t),
+        _vector(parents, "parents", _INT32, t), _int32(query_start_loc, "query_start_loc"), temperature, uniforms,
+        exponentials, es, rows, t, most, _int32(accept_path, "accept_path"),
+        _vector(accept_len, "accept_len", _INT32, rows), _vector(next_token, "next_token", _INT32, rows), logprobs,
+        _int32(status_word, "status_word"), _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_verify_tree")
+
+
+def mcpu_weights_workspace_size(d: Dims) -> int:
+    return int(_lib.mcpu_weights_workspace_size(ctypes.byref(d)))
+
+
+def new_weights_workspace(d: Dims, device="cuda") -> torch.Tensor:
+    """A workspace of the size mcpu_weights_workspace_size(d) asks for, its status word cleared."""
+    n = mcpu_weights_workspace_size(d)
+    if n == 0:
+        raise McpuError(1, "mcpu_weights_workspace_size")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def mcpu_accumulate_weights(q, lse, k_cache, block_table, seq_lens, query_start_loc, sliding_window, softmax_scale,
+                            decay, key_weights, workspace, query_path=None, path_len=None, stream=None):
+    """Adds to key_weights (float32 [B, H_kv, max_slots]) the attention that
+    the step's queries gave every key of their row: exp(scale q . k - lse),
+    summed over the queries and the q heads of a kv head; older weights are
+    multiplied by decay first, those of the queries' own slots start anew.
+    query_path (int32 [B, max_path]) and path_len (int32 [B]) name the queries
+    of each row (numbers in the row) whose keys are its last slots; None: all."""
+    t, hq, d = q.shape
+    pages, hkv, page, _ = k_cache.shape
+    if q.dtype is not _BF16 or k_cache.dtype is not _BF16 or lse.dtype is not _FP32 or lse.numel() != t * hq or \
+            not q.is_contiguous() or not k_cache.is_contiguous() or not lse.is_contiguous():
+        raise ValueError("q and k_cache must be contiguous bfloat16 tensors, lse a contiguous float32 [T, H_q] tensor")
+    rows, width = _rows(block_table, seq_lens, query_start_loc)
+    if key_weights.dtype is not _FP32 or key_weights.dim() != 3 or key_weights.shape[:2] != (rows, hkv) or \
+            not key_weights.is_contiguous():
+        raise ValueError("key_weights must be a contiguous float32 [B, H_kv, max_slots] tensor")
+    most = 0
+    if query_path is not None:
+        if path_len is None or query_path.dim() != 2 or query_path.shape[0] != rows:
+            raise ValueError("query_path must be an int32 [B, max_path] tensor, with path_len")
+        most = query_path.shape[1]
+        query_path, path_len = _int32(query_path, "query_path"), _vector(path_len, "path_len", _INT32, rows)
+    elif path_len is not None:
+        raise ValueError("path_len comes with query_path")
+    code = _accumulate_weights(
+        q.data_ptr(), lse.data_ptr(), k_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+        query_start_loc.data_ptr(), query_path, most, path_len, sliding_window, softmax_scale, decay,
+        _pack_dims(rows, t, width, pages, hq, hkv, d, page), key_weights.data_ptr(), key_weights.shape[2],
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_accumulate_weights")
+
+
+def mcpu_evict_kv(pools, key_weights, block_table, seq_lens, limit, budget, keep_first, keep_last, new_key_weights,
+                  new_seq_lens, status_word, page_refs=None, stream=None):
+    """Cuts rows longer than `limit` to `budget` slots per layer and kv head:
+    the first keep_first, the last keep_last and those of the highest
+    key_weights (float32 [layers, B, H_kv, max_slots]) between. pools: a
+    PoolList of the layers' K pools and then their V pools. new_key_weights
+    (may be key_weights) receives the weights of the slots that stay,
+    new_seq_lens the lengths. page_refs (int32 [num_pages]): rows that share
+    pages which would be written are left alone and reported."""
+    if not pools.bf16_pages or pools.num_pools % 2:
+        raise ValueError("mcpu_evict_kv takes the bfloat16 [num_pages, H_kv, 16, 64] K pools of every layer, then V")
+    layers, hkv = pools.num_pools // 2, pools.num_kv_heads
+    rows, width = seq_lens.shape[0], block_table.shape[1]
+    if block_table.dtype is not _INT32 or seq_lens.dtype is not _INT32 or block_table.shape[0] < rows or \
+            not block_table.is_contiguous() or not seq_lens.is_contiguous():
+        raise ValueError("block_table and seq_lens must be contiguous int32 tensors [B, max_pages] and [B]")
+    shape = key_weights.shape
+    if key_weights.dtype is not _FP32 or len(shape) != 4 or shape[:3] != (layers, rows, hkv) or \
+            not key_weights.is_contiguous() or new_key_weights.dtype is not _FP32 or \
+            new_key_weights.shape != shape or not new_key_weights.is_contiguous():
+        raise ValueError("key_weights and new_key_weights must be contiguous float32 [layers, B, H_kv, max_slots] tensors")
+    old, new = key_weights.data_ptr(), new_key_weights.data_ptr()
+    if old != new and abs(old - new) < 4 * key_weights.numel():
+        raise ValueError("new_key_weights must be key_weights or apart from it")
+    if page_refs is not None:
+        page_refs = _vector(page_refs, "page_refs", _INT32, pools.num_pages)
+    code = _evict_kv(
+        pools.pointers, layers, old, shape[3], block_table.data_ptr(), seq_lens.data_ptr(), limit, budget, keep_first,
+        keep_last, page_refs, _pack_dims(rows, 0, width, pools.num_pages, hkv, hkv, 64, 16), new,
+        _vector(new_seq_lens, "new_seq_lens", _INT32, rows), _int32(status_word, "status_word"), _raw_stream(stream))
+    if code:
+        raise McpuError(code, "mcpu_evict_kv")
