@@ -15,8 +15,10 @@ bool words_ok(const T*... p) {
   return ((p != nullptr && aligned(p, 4)) && ...);
 }
 
-// The workspace of mcpu_accumulate_weights: the status word.
-constexpr size_t kWeightsWorkspace = 256;
+// The workspace of mcpu_accumulate_weights: the status word, the cut units, their parts.
+constexpr size_t kWeightsCuts = 256, kWeightsParts = kWeightsCuts + sizeof(int4) * kWeightCtas;
+constexpr size_t kWeightsWorkspace = kWeightsParts + sizeof(float) * 2 * kWeightCtas * 256;
+static_assert(kWeightsParts % 256 == 0, "alignment");
 
 }  // namespace
 
@@ -95,7 +97,16 @@ mcpu_status mcpu_accumulate_weights(const void* q, const float* lse, const void*
   int sms = 0;
   st = device_sms(&sms);
   if (st != MCPU_OK) return st;
+  const int64_t rows = (int64_t)dims->num_pages * dims->num_kv_heads * kPage;
+  const int group = dims->num_q_heads / dims->num_kv_heads;
+  CUtensorMap kmap, qmap;
+  if (!encode_pool(&kmap, k_cache, rows) || !encode_query(&qmap, q, dims->total_q, dims->num_q_heads, group, 128))
+    return MCPU_ERR_INVALID_ARG;
   WeightParams p;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.cuts = reinterpret_cast<int4*>(ws + kWeightsCuts);
+  p.parts = reinterpret_cast<float*>(ws + kWeightsParts);
+  p.oob_row = (int32_t)rows;
   p.q = static_cast<const __nv_bfloat16*>(q);
   p.k_cache = static_cast<const __nv_bfloat16*>(k_cache);
   p.lse = lse;
@@ -115,10 +126,10 @@ mcpu_status mcpu_accumulate_weights(const void* q, const float* lse, const void*
   p.num_pages = dims->num_pages;
   p.num_q_heads = dims->num_q_heads;
   p.num_kv_heads = dims->num_kv_heads;
-  p.group = dims->num_q_heads / dims->num_kv_heads;
+  p.group = group;
   p.decay = decay;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
-  return from_cuda(launch_weights(p, sms, reinterpret_cast<cudaStream_t>(stream)));
+  return from_cuda(launch_weights(kmap, qmap, p, sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 
 mcpu_status mcpu_evict_kv(void* const* pools, int32_t num_layers, const float* key_weights, int32_t max_slots,

@@ -28,10 +28,15 @@ struct WeightParams {
   const int32_t *block_table, *seq_lens, *qsl, *path, *path_len;
   float* weights;  // [B, Hkv, max_slots]
   int32_t* status;
+  int4* cuts;    // [kWeightCtas] the cut unit that begins in each piece: last piece (-1: none), row, kv head, first key
+  float* parts;  // [2 * kWeightCtas][256] sums of cut units' parts
   int32_t max_path, max_slots, window, num_seqs, total_q, max_pages, num_pages, num_q_heads, num_kv_heads, group;
+  int32_t oob_row;  // a pool row past the end: read as zeros
   float decay, scale_log2;
 };
-cudaError_t launch_weights(const WeightParams& p, int sms, cudaStream_t stream);
+constexpr int kWeightCtas = 160;  // CTAs the workspace has room for (one per SM)
+cudaError_t launch_weights(const CUtensorMap& kmap, const CUtensorMap& qmap, const WeightParams& p, int sms,
+                           cudaStream_t stream);
 
 struct EvictParams {
   const float* weights;  // [layers, B, Hkv, max_slots]

@@ -1,114 +1,659 @@
-// Attention weights per cached key (mcpu_accumulate_weights):
+// Attention weights per cached key (mcpu_accumulate_weights) on the
+// 5th-generation tensor cores:
 //   w_j = decay w_j [j < C] + sum_{i: j <= p_i, p_i - j < W} sum_u exp(scale q_iu . k_j - lse_iu)
-// One thread per key, its 64 values in registers; the queries come through
-// shared memory, 16 rows at a time.
+//
+// The keys are the rows of the product: S = K Q^T with 128 keys in TMEM's
+// lanes, so that a thread owns a key and the sum over queries stays in its
+// registers; with the log-sum-exps given there is no maximum to carry and
+// nothing to exchange. A unit is 256 keys (two tiles over one stream of
+// queries, which halves its traffic from L2) of one (row, kv head); it walks
+// the row's queries in blocks of 128 columns (128 / g queries x g heads), those
+// that see some of its keys.
+//
+// Work: units lie on a line, each weighing 2 and each block 2 more (a unit
+// whose queries fit 32 columns weighs 3: there the keys' way from HBM counts);
+// the line is cut into equal pieces, one per CTA. A unit of more than
+// kWholeBlocks blocks may be cut between blocks: its parts are summed by
+// merge_weights_kernel in the order of the pieces. Every CTA derives the line
+// from the lengths itself: no planning launch.
+//
+// Warps: 0 walks the line and brings the keys (TMA, one box per page), 1 issues
+// the MMAs, 4-7 bring the queries (one box for 128 contiguous columns, else 16
+// bytes a lane, which also gathers the queries of a path) and their
+// log-sum-exps, 8-11 / 12-15 take the exponentials of the first / second 128
+// keys. TMEM: two buffers of 128 columns for each.
 #include "keep.cuh"
+#include "warp_pipe.cuh"
 
 namespace mcpu {
 
 namespace {
 
-constexpr int kThreads = 128, kRows = 16;
+constexpr int kTileKeys = kBlockKeys, kUnitKeys = 2 * kTileKeys, kCols = 128;
+constexpr int kStageBytes = 2 * kBlockBytes, kQBytes = kCols * kRowBytes;
+constexpr int kKStages = 4, kQStages = 3, kUnits = 4;
+constexpr int kThreads = 512;
+constexpr uint32_t kTmemCols = 512;
+constexpr int kWholeBlocks = 3;  // units of up to so many blocks are never cut
+constexpr int kMinQuota = 3;
+constexpr int kRingBytes = kKStages * kStageBytes + kQStages * kQBytes;
 
-__global__ void __launch_bounds__(kThreads) weights_kernel(const WeightParams p) {
-  __shared__ float q[kRows][kHeadDim];
-  __shared__ float lse2[kRows];
-  __shared__ int bad_path;
-  const int h = blockIdx.y, r = blockIdx.z, g = p.group;
-  const int q0 = p.qsl[r], L = p.qsl[r + 1] - q0, S = p.seq_lens[r];
-  const bool first = blockIdx.x == 0 && h == 0 && threadIdx.x == 0;
-  const int n = p.path ? p.path_len[r] : L;
-  if (threadIdx.x == 0) bad_path = 0;
-  __syncthreads();
-  if (p.qsl[0] != 0 || p.qsl[p.num_seqs] != p.total_q || q0 < 0 || L < 0 || L > p.total_q - q0 || n < 0 || n > S ||
-      (p.path && n > p.max_path) || S > p.max_pages * kPage || S > p.max_slots) {
-    if (first) atomicOr(p.status, kStatusBadLengths);
-    return;
+struct alignas(16) Unit {
+  int32_t row;  // -1: no more units
+  int32_t kvh, k0, len, n, q0;  // first key, row length, queries, first query token
+  int32_t b0, b1;               // query blocks to do here (none: old weights only decay)
+  int32_t slot;                 // partial slot, or -1: the whole unit
+  uint32_t pages;               // which of its 16 pages exist
+};
+
+struct WeightsSmem {
+  uint64_t unit_full[kUnits], unit_empty[kUnits];
+  uint64_t k_full[kKStages], k_empty[kKStages], q_full[kQStages], q_empty[kQStages];
+  uint64_t s_full[2][2], s_empty[2][2];  // [tile][buffer]
+  uint64_t drain;
+  Unit units[kUnits];
+  alignas(16) float neg_lse[kQStages][kCols];  // -lse log2(e) of each column, -inf: the column adds nothing
+  int64_t scan[kThreads / 32];
+  int64_t prefix[kMaxSeqs + 1];  // cost of the rows before each
+  uint32_t tmem_base;
+  int32_t abort_flag;
+};
+
+size_t weights_smem_bytes() { return 1024 + kRingBytes + sizeof(WeightsSmem); }
+
+// ------------------------------------------------------------ the work line
+struct RowGeom {
+  int q0, L, S, n, C, window;  // window 0: none that matters
+  int tok;                     // queries of a block
+  int nb;                      // blocks of all its queries
+  int u0, u1;                  // units
+  bool small;                  // its queries fit 32 columns
+
+  // the blocks of unit u whose queries see some key of it
+  __device__ __forceinline__ void blocks(int u, int* b0, int* b1) const {
+    const int k0 = u * kUnitKeys, last = min(k0 + kUnitKeys, S) - 1;
+    const int i0 = max(0, k0 - C);
+    const int i1 = window > 0 ? min(n, last - C + window) : n;
+    *b0 = i0 / tok;
+    *b1 = i1 > i0 ? (i1 + tok - 1) / tok : *b0;
   }
-  if (n == 0) return;
-  const int32_t* path = p.path ? p.path + (size_t)r * p.max_path : nullptr;
-  if (path) {
-    for (int i = threadIdx.x; i < n; i += kThreads)
-      if (path[i] < 0 || path[i] >= L) bad_path = 1;
-    __syncthreads();
-    if (bad_path) {
-      if (first) atomicOr(p.status, kStatusBadLengths);
-      return;
+  __device__ __forceinline__ int cost(int u) const {
+    int b0, b1;
+    blocks(u, &b0, &b1);
+    return b1 == b0 ? 1 : small ? 3 : 2 + 2 * (b1 - b0);
+  }
+};
+
+// Geometry of row r; false if it has no work, with the status bits of what is wrong.
+__device__ __forceinline__ bool row_geom(const WeightParams& p, int r, RowGeom* w, int32_t* bits) {
+  w->q0 = p.qsl[r];
+  w->L = p.qsl[r + 1] - w->q0;
+  w->S = p.seq_lens[r];
+  w->n = p.path ? p.path_len[r] : w->L;
+  if (w->q0 < 0 || w->L < 0 || w->L > p.total_q - w->q0 || w->n < 0 || w->n > w->S ||
+      (p.path && w->n > p.max_path) || w->S > p.max_pages * kPage || w->S > p.max_slots) {
+    *bits |= kStatusBadLengths;
+    return false;
+  }
+  if (w->n == 0) return false;
+  w->C = w->S - w->n;
+  w->window = p.window >= w->S ? 0 : p.window;
+  w->tok = kCols / p.group;
+  w->nb = (w->n + w->tok - 1) / w->tok;
+  // weights before the first window change only if they decay
+  w->u0 = w->window > 0 && p.decay == 1.f ? max(0, w->C - w->window + 1) / kUnitKeys : 0;
+  w->u1 = (w->S + kUnitKeys - 1) / kUnitKeys;
+  w->small = w->n * (int64_t)p.group <= 32;
+  return true;
+}
+
+// Whether a row's path names queries of the row.
+__device__ __forceinline__ bool path_ok(const WeightParams& p, int r, const RowGeom& w) {
+  if (!p.path) return true;
+  const int32_t* path = p.path + (size_t)r * p.max_path;
+  bool ok = true;
+#pragma unroll 8
+  for (int i = 0; i < w.n; ++i) {
+    const int x = path[i];
+    ok &= x >= 0 && x < w.L;
+  }
+  return ok;
+}
+
+// Cost of one kv head of the row.
+__device__ __forceinline__ int64_t head_cost(const RowGeom& w) {
+  int64_t sum = 0;
+  int u = w.u0;
+  if (w.window == 0) {  // all blocks see the keys before the first query
+    const int all = min(w.u1, (w.C + w.tok - 1) / kUnitKeys + 1);
+    sum = (int64_t)(w.small ? 3 : 2 + 2 * w.nb) * all;
+    u = all;
+  }
+  for (; u < w.u1; ++u) sum += w.cost(u);
+  return sum;
+}
+
+// Blocks of a unit that belong to the pieces ending x units of cost into it.
+__device__ __forceinline__ int blocks_before(int64_t x, int nb) {
+  if (nb <= kWholeBlocks) return x <= 0 ? 0 : nb;
+  return x <= 2 ? 0 : x >= 2 + 2 * nb ? nb : (int)((x - 1) / 2);
+}
+
+__device__ __forceinline__ bool unit_ok(const WeightParams& p, const Unit& a) {
+  return a.row < p.num_seqs && a.kvh >= 0 && a.kvh < p.num_kv_heads && a.k0 >= 0 && a.k0 < a.len &&
+         a.len <= p.max_slots && a.n >= 1 && a.n <= a.len && a.b0 >= 0 && a.b1 >= a.b0 &&
+         (int64_t)(a.b1 - 1) * (kCols / p.group) < a.n && a.q0 >= 0 && a.q0 < p.total_q && a.slot < 2 * kWeightCtas;
+}
+
+// S = K Q^T of one tile by one elected lane of a warp in step, and the commit behind it.
+__device__ __forceinline__ void mma_keys_e(uint32_t d, uint64_t k, uint64_t q, uint32_t idesc, uint32_t done) {
+  static_assert(kHeadDim == 64, "four steps of 16 dims, 32 bytes each");
+  asm volatile(
+      "{\n\t.reg .pred e, t, f;\n\t.reg .b64 a, b;\n\telect.sync _|e, 0xffffffff;\n\t"
+      "setp.eq.u32 t, 0, 0;\n\tsetp.ne.u32 f, 0, 0;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, f;\n\t"
+      "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t"
+      "}" ::"r"(d),
+      "l"(k), "l"(q), "r"(idesc), "r"(done)
+      : "memory");
+}
+
+// Columns of block b of a unit: those of its queries, and rounded up to the MMA's step.
+__device__ __forceinline__ int block_cols(const Unit& a, int b, int g) { return min(kCols, (a.n - b * (kCols / g)) * g); }
+
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[32]) {  // into the first 16
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, "
+      "[%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(taddr));
+}
+
+// sum += 2^(s scale + neg_lse) over kN columns; masked: only columns lo <= c < hi.
+template <int kN, bool kMasked>
+__device__ __forceinline__ void add_columns(const uint32_t (&sv)[32], const float* neg_lse, uint64_t sc, int lo, int hi,
+                                            uint64_t (&sum)[2]) {
+#pragma unroll
+  for (int e = 0; e < kN; e += 4) {
+    const ulonglong2 nl = *reinterpret_cast<const ulonglong2*>(neg_lse + e);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int c = e + 2 * k;
+      const uint64_t x = fma2((uint64_t)sv[c] | ((uint64_t)sv[c + 1] << 32), sc, k ? nl.y : nl.x);
+      float x0 = lo_f32(x), x1 = hi_f32(x);
+      if (kMasked) {
+        x0 = c >= lo && c < hi ? x0 : -INFINITY;
+        x1 = c + 1 >= lo && c + 1 < hi ? x1 : -INFINITY;
+      }
+      sum[k] = add2(sum[k], pack_f32x2(ex2_approx(x0), ex2_approx(x1)));
     }
   }
-  const int C = S - n;
-  for (int64_t j0 = (int64_t)blockIdx.x * kThreads; j0 < S; j0 += (int64_t)gridDim.x * kThreads) {
-    const int j = (int)j0 + threadIdx.x;
-    // queries that see a key of this block: i >= j - C, i < j + W - C
-    const int i0 = max(0, (int)j0 - C);
-    const int last = min((int)j0 + kThreads, S) - 1;
-    const int i1 = p.window > 0 ? (int)min((int64_t)n, (int64_t)last + p.window - C) : n;
-    float k[kHeadDim];
-    const bool live = j < S;
-    bool page_ok = false;
-    if (live && i0 < i1) {
-      const int page = p.block_table[(size_t)r * p.max_pages + j / kPage];
-      page_ok = page >= 0 && page < p.num_pages;
-      if (page_ok) {
-        const uint4* src = reinterpret_cast<const uint4*>(
-            p.k_cache + (((size_t)page * p.num_kv_heads + h) * kPage + j % kPage) * kHeadDim);
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+    weights_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap qmap,
+                   const WeightParams p) {
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t raw = smem_addr(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - raw);
+  WeightsSmem& st = *reinterpret_cast<WeightsSmem*>(base_ptr + kRingBytes);
+  volatile int32_t* abort_flag = &st.abort_flag;
+  auto bar = [&](uint64_t& b) { return smem_addr(&b); };
+  const int B = p.num_seqs, g = p.group, Hkv = p.num_kv_heads, Hq = p.num_q_heads;
+  const uint32_t sK = base, sQ = base + kKStages * kStageBytes;
+
+  // Before anything is read: TMEM, the barriers, the tensor maps.
+  if (warp == 0) {
+    tmem_alloc(smem_addr(&st.tmem_base), kTmemCols);
+    tmem_relinquish();
+  }
+  if (threadIdx.x == 32) {
+    for (int i = 0; i < kUnits; ++i) {
+      mbar_init(bar(st.unit_full[i]), 1);
+      mbar_init(bar(st.unit_empty[i]), 1 + 4 + 8);
+    }
+    for (int i = 0; i < kKStages; ++i) {
+      mbar_init(bar(st.k_full[i]), 2);
+      mbar_init(bar(st.k_empty[i]), 1);
+    }
+    for (int i = 0; i < kQStages; ++i) {
+      mbar_init(bar(st.q_full[i]), 4);
+      mbar_init(bar(st.q_empty[i]), 1 + 8);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(bar(st.s_full[i >> 1][i & 1]), 1);
+      mbar_init(bar(st.s_empty[i >> 1][i & 1]), 4);
+    }
+    mbar_init(bar(st.drain), 1);
+    st.abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (threadIdx.x == 64) {
+    prefetch_tensormap(&kmap);
+    prefetch_tensormap(&qmap);
+  }
+  auto leave = [&] {  // the whole CTA
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) {
+      tc_fence_after();
+      tmem_dealloc(st.tmem_base, kTmemCols);
+    }
+    if (threadIdx.x == 0 && *abort_flag == 1) atomicOr(p.status, kStatusTimeout);
+  };
+  grid_dep_launch();
+  grid_dep_wait();
+  if (threadIdx.x == 0) p.cuts[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  const bool ends = p.qsl[0] == 0 && p.qsl[B] == p.total_q;
+  // ---- the line: prefix[r] = cost of the rows before r
+  {
+    const int per = (B + kThreads - 1) / kThreads;
+    const int r0 = min(B, (int)threadIdx.x * per), r1 = min(B, r0 + per);
+    int64_t sum = 0;
+    int32_t bits = 0;
+    RowGeom w;
+    for (int r = r0; r < r1; ++r) {
+      st.prefix[r] = sum;
+      if (!row_geom(p, r, &w, &bits)) continue;
+      if (!path_ok(p, r, w)) {
+        bits |= kStatusBadLengths;
+        continue;
+      }
+      sum += head_cost(w) * Hkv;
+    }
+    if (!ends) bits = threadIdx.x == 0 ? kStatusBadLengths : 0;
+    if (bits && blockIdx.x == 0) atomicOr(p.status, bits);
+    int64_t incl = sum;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint4 v = src[e];
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t v = __shfl_up_sync(0xffffffffu, (long long)incl, o);
+      if (lane >= o) incl += v;
+    }
+    if (lane == 31) st.scan[warp] = incl;
+    __syncthreads();
+    int64_t at = incl - sum;
+    for (int i = 0; i < warp; ++i) at += st.scan[i];
+    for (int r = r0; r < r1; ++r) st.prefix[r] += at;
+    if (threadIdx.x == kThreads - 1) st.prefix[B] = at + sum;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const int64_t total = st.prefix[B];
+  const int64_t quota = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kMinQuota);
+  const int64_t begin = (int64_t)blockIdx.x * quota, end = min(begin + quota, total);
+  if (!ends || begin >= total) return leave();  // uniform over the CTA
+
+  if (warp == 0) {
+    // ------------------------------------------------- the line, and the keys
+    bool ok = true;
+    RingAt<kKStages> rk;
+    RingAt<kUnits> ru;
+    uint32_t loaded = 0;
+    int row = 0;
+    for (int r = 1 + lane; r < B; r += 32) row += st.prefix[r] <= begin;
+    row = __reduce_add_sync(0xffffffffu, row);  // the last row that begins at or before
+    RowGeom w;
+    int32_t ignored = 0;
+    row_geom(p, row, &w, &ignored);
+    const int64_t per_head = (st.prefix[row + 1] - st.prefix[row]) / Hkv;
+    const int64_t off = begin - st.prefix[row];
+    int kvh = (int)(off / per_head);
+    const int64_t rem = off - kvh * per_head;
+    int u = w.u0;
+    int64_t pos = 0;  // cost of the head's units before u
+    for (;; u += 32) {
+      int64_t incl = u + lane < w.u1 ? w.cost(u + lane) : 0;
 #pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w[d]));
-            k[8 * e + 2 * d] = f.x;
-            k[8 * e + 2 * d + 1] = f.y;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, (long long)incl, o);
+        if (lane >= o) incl += v;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, pos + incl > rem);
+      if (past || u + 32 >= w.u1) {
+        const int k = past ? __ffs(past) - 1 : 0;
+        const int64_t before = __shfl_sync(0xffffffffu, (long long)incl, max(k - 1, 0));
+        if (k > 0) pos += before;
+        u += k;
+        break;
+      }
+      pos += __shfl_sync(0xffffffffu, (long long)incl, 31);
+    }
+    pos += begin - rem;  // where the unit begins on the line
+    auto page_of = [&](int r, int unit) -> int {  // page id `lane` of a unit (lanes 0 .. 15)
+      const int64_t lp = (int64_t)unit * (kUnitKeys / kPage) + lane;
+      return lane < 16 && lp < p.max_pages ? p.block_table[(size_t)r * p.max_pages + lp] : -1;
+    };
+    int id = page_of(row, u);
+    while (pos < end && ok) {
+      int b0, b1;
+      w.blocks(u, &b0, &b1);
+      const int nb = b1 - b0, c = w.cost(u);
+      const int s0 = blocks_before(begin - pos, nb), s1 = blocks_before(end - pos, nb);
+      Unit a;
+      a.row = row;
+      a.kvh = kvh;
+      a.k0 = u * kUnitKeys;
+      a.len = w.S;
+      a.n = w.n;
+      a.q0 = w.q0;
+      a.b0 = b0 + s0;
+      a.b1 = b0 + s1;
+      a.slot = s0 == 0 && s1 == nb ? -1 : 2 * (int)blockIdx.x + (s0 == 0 ? 1 : 0);
+      const bool mine = s1 > s0 || (nb == 0 && begin <= pos);
+      if (mine && a.slot >= 0 && s0 == 0 && lane == 0) {
+        int last = blockIdx.x;
+        for (int64_t e = end; blocks_before(e - pos, nb) < nb; e += quota) ++last;
+        p.cuts[blockIdx.x] = make_int4(last, row, kvh, a.k0);
+      }
+      // this unit's pages, and the next unit
+      const int C = w.C, W = w.window, this_id = id;
+      pos += c;
+      if (++u == w.u1) {
+        u = w.u0;
+        if (++kvh == Hkv) {
+          kvh = 0;
+          do ++row;
+          while (row < B && st.prefix[row + 1] == st.prefix[row]);
+          if (row < B) {
+            row_geom(p, row, &w, &ignored);
+            u = w.u0;
           }
         }
-      } else if (j >= C || p.window <= 0 || j > C - p.window) {
-        atomicOr(p.status, kStatusBadPage);
       }
-    }
-    float sum = 0.f;
-    for (int64_t row0 = (int64_t)i0 * g; row0 < (int64_t)i1 * g; row0 += kRows) {
-      __syncthreads();
-      for (int e = threadIdx.x; e < kRows * kHeadDim; e += kThreads) {
-        const int64_t row = row0 + e / kHeadDim;
-        const int i = (int)(row / g), u = (int)(row % g);
-        if (i < i1) {
-          const size_t t = q0 + (path ? path[i] : i);
-          const size_t at = t * p.num_q_heads + (size_t)h * g + u;
-          q[e / kHeadDim][e % kHeadDim] = __bfloat162float(p.q[at * kHeadDim + e % kHeadDim]);
-          if (e % kHeadDim == 0) lse2[e / kHeadDim] = p.lse[at] == -INFINITY ? INFINITY : p.lse[at] * 1.4426950408889634f;
-        }
+      if (pos < end) id = page_of(row, u);
+      if (!mine) continue;
+      const int pk = a.k0 + lane * kPage, pl = min(pk + kPage, a.len) - 1;  // the page's keys
+      const bool exists = this_id >= 0 && this_id < p.num_pages;
+      const bool seen = lane < 16 && pk < a.len && (W == 0 || pl >= C || pl + W > C);
+      if (seen && !exists && a.b1 > a.b0) atomicOr(p.status, kStatusBadPage);
+      a.pages = __ballot_sync(0xffffffffu, exists) & 0xffffu;
+      const int y = exists && pk < a.len ? (this_id * Hkv + a.kvh) * kPage : p.oob_row;
+      if (!unit_ok(p, a)) {
+        atomicOr(p.status, kStatusPlanOverflow);
+        *abort_flag = 2;
+        ok = false;
+        break;
       }
-      __syncthreads();
-      if (!page_ok) continue;
-      for (int e = 0; e < kRows && row0 + e < (int64_t)i1 * g; ++e) {
-        const int i = (int)((row0 + e) / g);
-        if (j > C + i || (p.window > 0 && C + i - j >= p.window)) continue;
-        float s = 0.f;
+      ok = wait_warp(bar(st.unit_empty[ru.s]), ru.parity ^ 1);
+      if (!ok) break;
+      if (lane == 0) {
+        st.units[ru.s] = a;
+        mbar_arrive(bar(st.unit_full[ru.s]));
+      }
+      __syncwarp();
+      ru.next();
+      if (a.b0 == a.b1) continue;
+      ok = wait_warp(bar(st.k_empty[rk.s]), rk.parity ^ 1);
+      if (!ok) break;
+      int ys[kBlockPages];
 #pragma unroll
-        for (int d = 0; d < kHeadDim; ++d) s = fmaf(q[e][d], k[d], s);
-        sum += lse2[e] == INFINITY ? 0.f : exp2f(s * p.scale_log2 - lse2[e]);
+      for (int j = 0; j < kBlockPages; ++j) ys[j] = __shfl_sync(0xffffffffu, y, j);
+      load_block_e(sK + rk.s * kStageBytes, &kmap, ys, bar(st.k_full[rk.s]), policy_evict_first());
+#pragma unroll
+      for (int j = 0; j < kBlockPages; ++j) ys[j] = __shfl_sync(0xffffffffu, y, kBlockPages + j);
+      load_block_e(sK + rk.s * kStageBytes + kBlockBytes, &kmap, ys, bar(st.k_full[rk.s]), policy_evict_first());
+      rk.next();
+      ++loaded;
+    }
+    if (!ok && *abort_flag == 0) *abort_flag = 1;
+    if (ok && wait_warp(bar(st.unit_empty[ru.s]), ru.parity ^ 1)) {
+      if (lane == 0) {  // no more units
+        st.units[ru.s].row = -1;
+        mbar_arrive(bar(st.unit_full[ru.s]));
       }
     }
-    if (!live) continue;
-    float* w = p.weights + ((size_t)r * p.num_kv_heads + h) * p.max_slots + j;
-    const bool seen = j >= C || (p.window <= 0 || (int64_t)j + p.window > C);  // by the first query, or its own
-    if (seen && !page_ok) continue;
-    const float old = j < C && p.decay != 0.f ? p.decay * *w : 0.f;
-    *w = old + sum;
+    // after an abort: wait (bounded) for the copies still in flight
+    if (*abort_flag && lane == 0)
+      for (uint32_t k = loaded > kKStages ? loaded - kKStages : 0; k < loaded; ++k)
+        mbar_wait(bar(st.k_full[k % kKStages]), (k / kKStages) & 1);
+  } else if (warp == 1) {
+    // -------------------------------------------------------------- MMA issue
+    const uint64_t kdesc0 = smem_desc_sw128(sK, 16, 1024), qdesc0 = smem_desc_sw128(sQ, 16, 1024);
+    RingAt<kKStages> rk;
+    RingAt<kQStages> rq;
+    RingAt<kUnits> ru;
+    RingAt<2> rs;
+    bool ok = true;
+    while (ok) {
+      ok = wait_warp(bar(st.unit_full[ru.s]), ru.parity);
+      if (!ok) break;
+      const Unit a = st.units[ru.s];
+      if (a.row < 0) break;
+      if (a.b0 < a.b1) {
+        ok = wait_warp(bar(st.k_full[rk.s]), rk.parity);
+        for (int b = a.b0; b < a.b1 && ok; ++b) {
+          const uint32_t cols = (block_cols(a, b, g) + 15) & ~15;
+          const uint32_t idesc = idesc_bf16(kTileKeys, 0, false, false) | ((cols >> 3) << 17);
+          ok = wait_warp(bar(st.q_full[rq.s]), rq.parity);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            ok = ok && wait_warp(bar(st.s_empty[t][rs.s]), rs.parity ^ 1);
+            if (!ok) break;
+            tc_fence_after();
+            mma_keys_e(st.tmem_base + t * 256 + rs.s * 128,
+                       kdesc0 + (rk.s * kStageBytes + t * kBlockBytes) / 16, qdesc0 + rq.s * (kQBytes / 16), idesc,
+                       bar(st.s_full[t][rs.s]));
+          }
+          if (!ok) break;
+          tc_commit_e(bar(st.q_empty[rq.s]));
+          rq.next();
+          rs.next();
+        }
+        if (!ok) break;
+        tc_commit_e(bar(st.k_empty[rk.s]));
+        rk.next();
+      }
+      if (lane == 0) mbar_arrive(bar(st.unit_empty[ru.s]));
+      __syncwarp();
+      ru.next();
+    }
+    if (!ok && *abort_flag == 0) *abort_flag = 1;
+    tc_commit_e(bar(st.drain));  // MMAs still in flight must not outlive TMEM
+    mbar_wait(bar(st.drain), 0);
+  } else if (warp >= 4 && warp < 8) {
+    // ---------------------------------------------------------------- queries
+    const int w = warp - 4;  // rows 32 w .. of every block
+    RingAt<kQStages> rq;
+    RingAt<kUnits> ru;
+    uint32_t boxes = 0, last_box = 0, last_parity = 0;
+    bool ok = true;
+    while (ok) {
+      ok = wait_warp(bar(st.unit_full[ru.s]), ru.parity);
+      if (!ok) break;
+      const Unit a = st.units[ru.s];
+      if (a.row < 0) break;
+      const int32_t* path = p.path ? p.path + (size_t)a.row * p.max_path : nullptr;
+      for (int b = a.b0; b < a.b1; ++b) {
+        const int cols = block_cols(a, b, g), t0 = b * (kCols / g);
+        const bool box = !path && cols == kCols;
+        // (query token, q head) row of a column
+        auto source = [&](int c) -> size_t {
+          const int i = t0 + c / g;
+          return (size_t)(a.q0 + (path ? path[i] : i)) * Hq + a.kvh * g + c % g;
+        };
+        const int c0 = 32 * w + lane;
+        float nl = -INFINITY;
+        if (c0 < cols) {
+          const float lse = p.lse[source(c0)];
+          nl = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
+        }
+        uint4 v[8];
+        if (!box && 32 * w < cols) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int c = 32 * w + 4 * k + (lane >> 3);
+            v[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (c < cols) v[k] = reinterpret_cast<const uint4*>(p.q + source(c) * kHeadDim)[lane & 7];
+          }
+        }
+        ok = wait_warp(bar(st.q_empty[rq.s]), rq.parity ^ 1);
+        if (!ok) break;
+        st.neg_lse[rq.s][c0] = nl;
+        if (!box && 32 * w < cols) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int c = 32 * w + 4 * k + (lane >> 3);
+            *reinterpret_cast<uint4*>(base_ptr + (sQ - base) + rq.s * kQBytes + swz128(c, lane & 7)) = v[k];
+          }
+          fence_proxy_async();
+        }
+        __syncwarp();
+        if (lane == 0) {
+          if (box && w == 0) {
+            mbar_arrive_expect_tx(bar(st.q_full[rq.s]), kQBytes);
+            tma_load_3d(sQ + rq.s * kQBytes, &qmap, 0, a.kvh * g, a.q0 + t0, bar(st.q_full[rq.s]));
+          } else {
+            mbar_arrive(bar(st.q_full[rq.s]));
+          }
+        }
+        __syncwarp();
+        if (box) ++boxes, last_box = rq.s, last_parity = rq.parity;
+        rq.next();
+      }
+      if (!ok) break;
+      if (lane == 0) mbar_arrive(bar(st.unit_empty[ru.s]));
+      __syncwarp();
+      ru.next();
+    }
+    if (!ok && *abort_flag == 0) *abort_flag = 1;
+    // after an abort: the last box may still be in flight (the ones before it were waited for by its stage's turn, or
+    // lie in the other stages: each is waited for)
+    if (*abort_flag && w == 0 && lane == 0 && boxes > 0) {
+      mbar_wait(bar(st.q_full[last_box]), last_parity);
+      for (uint32_t s = 0; s < kQStages; ++s)
+        if (s != last_box) mbar_wait(bar(st.q_full[s]), s < rq.s ? rq.parity : rq.parity ^ 1);
+    }
+  } else if (warp >= 8) {
+    // ----------------------------------------------------------- exponentials
+    const int t = (warp - 8) >> 2, key = (warp & 3) * 32 + lane;  // tile, TMEM lane
+    const uint32_t lane_base = st.tmem_base + t * 256 + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint64_t sc = pack_f32x2(p.scale_log2, p.scale_log2);
+    RingAt<kQStages> rq;
+    RingAt<kUnits> ru;
+    RingAt<2> rs;
+    bool ok = true;
+    while (ok) {
+      ok = wait_warp(bar(st.unit_full[ru.s]), ru.parity);
+      if (!ok) break;
+      const Unit a = st.units[ru.s];
+      if (a.row < 0) break;
+      const int C = a.len - a.n, first = a.k0 + t * kTileKeys + (warp & 3) * 32, j = first + lane;
+      const int W = p.window;
+      const bool live = j < a.len, busy = first < a.len;
+      const bool exists = a.pages >> ((j - a.k0) / kPage) & 1u;
+      // a key that some query sees, on a page that is missing, keeps its weight
+      const bool seen = j >= C || W == 0 || (int64_t)j + W > C;
+      const bool writes = live && (exists || !seen);
+      float* w = p.weights + ((size_t)a.row * Hkv + a.kvh) * p.max_slots + j;
+      float old = 0.f;
+      if (a.slot < 0 && writes && j < C && p.decay != 0.f) old = *w;
+      float total_sum = 0.f;
+      for (int b = a.b0; b < a.b1; ++b) {
+        const int cols = (block_cols(a, b, g) + 15) & ~15, t0 = b * (kCols / g);
+        ok = wait_warp(bar(st.q_full[rq.s]), rq.parity) && wait_warp(bar(st.s_full[t][rs.s]), rs.parity);
+        if (!ok) break;
+        tc_fence_after();
+        const float* nl = st.neg_lse[rq.s];
+        const uint32_t s = lane_base + rs.s * 128;
+        uint64_t sum[2] = {0, 0};
+        uint32_t sv[32];
+        // hidden from some query of the block: keys behind its first, or before the window of its last
+        const int tl = min(t0 + kCols / g, a.n) - 1;
+        const bool plain = first + 31 <= C + t0 && (W == 0 || C + tl - first < W);
+        if (busy && plain) {
+          for (int c = 0; c + 32 <= cols; c += 32) {
+            tmem_ld32(s + c, sv);
+            tmem_ld_wait();
+            add_columns<32, false>(sv, nl + c, sc, 0, 0, sum);
+          }
+          if (cols & 16) {
+            tmem_ld16(s + (cols & ~31), sv);
+            tmem_ld_wait();
+            add_columns<16, false>(sv, nl + (cols & ~31), sc, 0, 0, sum);
+          }
+        } else if (busy) {
+          const int lo = min(max(j - C - t0, 0), kCols) * g;
+          const int hi = W == 0 ? kCols * kMaxGroup : (int)min(max((int64_t)j + W - C - t0, (int64_t)0), (int64_t)kCols) * g;
+          for (int c = 0; c + 32 <= cols; c += 32) {
+            tmem_ld32(s + c, sv);
+            tmem_ld_wait();
+            add_columns<32, true>(sv, nl + c, sc, lo - c, hi - c, sum);
+          }
+          if (cols & 16) {
+            const int c = cols & ~31;
+            tmem_ld16(s + c, sv);
+            tmem_ld_wait();
+            add_columns<16, true>(sv, nl + c, sc, lo - c, hi - c, sum);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        mbar_arrive_e(bar(st.s_empty[t][rs.s]));
+        mbar_arrive_e(bar(st.q_empty[rq.s]));
+        const uint64_t both = add2(sum[0], sum[1]);
+        total_sum += lo_f32(both) + hi_f32(both);
+        rq.next();
+        rs.next();
+      }
+      if (!ok) break;
+      if (a.slot >= 0) {
+        p.parts[(size_t)a.slot * kUnitKeys + t * kTileKeys + key] = total_sum;
+      } else if (writes) {
+        *w = (j < C && p.decay != 0.f ? p.decay * old : 0.f) + total_sum;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(st.unit_empty[ru.s]));
+      __syncwarp();
+      ru.next();
+    }
+    if (!ok && *abort_flag == 0) *abort_flag = 1;
   }
+  __syncwarp();
+  leave();
+}
+
+// The units that were cut: old weights and the parts, in the order of the
+// pieces. Block c: the unit whose first part lies in piece c, if there is one.
+__global__ void __launch_bounds__(kUnitKeys) merge_weights_kernel(const WeightParams p) {
+  grid_dep_wait();
+  const int4 cut = p.cuts[blockIdx.x];
+  const int last = cut.x, r = cut.y, kvh = cut.z, j = cut.w + threadIdx.x;
+  if (last < 0) return;
+  const int S = p.seq_lens[r], n = p.path ? p.path_len[r] : p.qsl[r + 1] - p.qsl[r], C = S - n;
+  if (j >= S) return;
+  const int page = p.block_table[(size_t)r * p.max_pages + j / kPage];
+  const bool seen = j >= C || p.window == 0 || (int64_t)j + p.window > C;
+  if (seen && (page < 0 || page >= p.num_pages)) return;
+  float* w = p.weights + ((size_t)r * p.num_kv_heads + kvh) * p.max_slots + j;
+  float sum = p.parts[(size_t)(2 * blockIdx.x + 1) * kUnitKeys + threadIdx.x];
+  for (int c = blockIdx.x + 1; c <= last; ++c) sum += p.parts[(size_t)(2 * c) * kUnitKeys + threadIdx.x];
+  *w = (j < C && p.decay != 0.f ? p.decay * *w : 0.f) + sum;
 }
 
 }  // namespace
 
-cudaError_t launch_weights(const WeightParams& p, int sms, cudaStream_t stream) {
-  (void)sms;
-  const int64_t slots = (int64_t)p.max_pages * kPage < p.max_slots ? (int64_t)p.max_pages * kPage : p.max_slots;
-  const int64_t blocks = (slots + kThreads - 1) / kThreads;
-  LaunchCfg lc(dim3((unsigned)(blocks < 4096 ? blocks : 4096), p.num_kv_heads, p.num_seqs), dim3(kThreads), 0, stream,
-               false);
-  return cudaLaunchKernelEx(&lc.cfg, weights_kernel, p);
+cudaError_t launch_weights(const CUtensorMap& kmap, const CUtensorMap& qmap, const WeightParams& p, int sms,
+                           cudaStream_t stream) {
+  const int grid = sms < kWeightCtas ? sms : kWeightCtas;
+  LaunchCfg lc(dim3(grid), dim3(kThreads), weights_smem_bytes(), stream, true);
+  const cudaError_t e = cudaLaunchKernelEx(&lc.cfg, weights_kernel, kmap, qmap, p);
+  if (e != cudaSuccess) return e;
+  // no row has more than kWholeBlocks blocks of queries: nothing is cut
+  const int64_t most = p.path && p.max_path < p.total_q ? p.max_path : p.total_q;
+  if (most * p.group <= kWholeBlocks * kCols) return cudaSuccess;
+  LaunchCfg mc(dim3(grid), dim3(kUnitKeys), 0, stream, true);
+  return cudaLaunchKernelEx(&mc.cfg, merge_weights_kernel, p);
+}
+
+cudaError_t prepare_weights_kernels() {
+  return cudaFuncSetAttribute(weights_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)weights_smem_bytes());
 }
 
 }  // namespace mcpu

@@ -52,15 +52,13 @@
 // the grid may be placed while the one that writes it still runs.
 #include "tcgen05.cuh"
 #include "tree_round.cuh"
+#include "warp_pipe.cuh"
 
 namespace mcpu {
 
 namespace {
 
 constexpr int kTileRows = kTreeTileRows;  // query rows of one tile (TMEM lanes)
-constexpr int kBlockKeys = 128;
-constexpr int kBlockPages = kBlockKeys / kPage;
-constexpr int kBlockBytes = kBlockKeys * kRowBytes;  // one K or V block: 16 KiB
 constexpr int kKStages = 3, kVStages = 2;            // per lane
 constexpr int kQBytes = kTileRows * kRowBytes;
 constexpr int kLaneBytes = kQBytes + (kKStages + kVStages) * kBlockBytes;
@@ -169,68 +167,8 @@ __device__ __forceinline__ bool part_ok(const TreeParams& p, const Part& a) {
          a.node + a.n_tok <= a.len - a.ctx && a.len - a.ctx <= 32 * p.words;
 }
 
-// ------------------------------------------------------------------- waits
-// A bounded wait of a warp in step: few instructions, and one outcome for the
-// warp, so that its branches are uniform. A test returns when the phase
-// completes or after about 1.4 us, so 2^17 of them take 0.2 s; then the role
-// ends and raises the abort flag, and the other roles' waits run out likewise.
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) {
-  uint32_t left;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tmov.b32 %0, 0x20000;\n"
-      "again:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "vote.sync.all.pred p, p, 0xffffffff;\n\t@p bra.uni done;\n\t"
-      "sub.u32 %0, %0, 1;\n\tsetp.ne.u32 p, %0, 0;\n\t@p bra.uni again;\n"
-      "done:\n\t}"
-      : "=&r"(left)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return left != 0;
-}
-
-// Whether the phase has completed, asked ahead of the time it matters.
-__device__ __forceinline__ bool peek(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-
-// What one elected lane of a warp in step issues: a block's eight pages by
-// TMA, the MMAs of S and of O with the commits behind them. One election for
-// all of it, and operands that differ by constants: from a lone lane, or with
-// an election per operation, the operands' way to the uniform datapath takes
-// longer than the work that is issued.
-__device__ __forceinline__ void load_block_e(uint32_t dst, const CUtensorMap* map, const int (&y)[kBlockPages],
-                                             uint32_t bar, uint64_t policy) {
-  static_assert(kBlockPages == 8 && kTileBytes == 2048, "eight boxes of 2 KiB");
-  asm volatile(
-      "{\n\t.reg .pred e;\n\t.reg .b32 z;\n\tmov.b32 z, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
-      "@e mbarrier.arrive.expect_tx.shared::cta.b64 _, [%2], %4;\n\t"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0 + 0], [%1, {z, %5}], [%2], %3;\n\t"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0 + 2048], [%1, {z, %6}], [%2], %3;\n\t"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0 + 4096], [%1, {z, %7}], [%2], %3;\n\t"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0 + 6144], [%1, {z, %8}], [%2], %3;\n\t"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0 + 8192], [%1, {z, %9}], [%2], %3;\n\t"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0 + 10240], [%1, {z, %10}], [%2], %3;\n\t"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0 + 12288], [%1, {z, %11}], [%2], %3;\n\t"
-      "@e cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0 + 14336], [%1, {z, %12}], [%2], %3;\n\t"
-      "}" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "l"(policy), "n"(kBlockBytes), "r"(y[0]), "r"(y[1]), "r"(y[2]),
-      "r"(y[3]), "r"(y[4]), "r"(y[5]), "r"(y[6]), "r"(y[7])
-      : "memory");
-}
+// The MMAs of S and of O with the commits behind them, issued by one elected
+// lane of a warp in step.
 __device__ __forceinline__ void mma_scores_e(uint32_t d, uint64_t q, uint64_t k, uint32_t idesc, uint32_t done,
                                              uint32_t k_free) {
   static_assert(kHeadDim == 64, "four steps of 16 dims, 32 bytes each");
@@ -265,23 +203,6 @@ __device__ __forceinline__ void mma_values_e(uint32_t d, uint32_t pw, uint64_t v
       "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%6];\n\t"
       "}" ::"r"(d),
       "r"(pw), "l"(v), "r"(idesc), "r"(add), "r"(done), "r"(v_free)
-      : "memory");
-}
-
-// A ring's position: stage and the parity of its turn, without a division.
-template <uint32_t kStages>
-struct RingAt {
-  uint32_t s = 0, parity = 0;
-  __device__ __forceinline__ void next() {
-    if (++s == kStages) s = 0, parity ^= 1;
-  }
-};
-
-// One arrival of a warp in step.
-__device__ __forceinline__ void mbar_arrive_e(uint32_t bar) {
-  asm volatile(
-      "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
-      "@e mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar)
       : "memory");
 }
 
