@@ -18,10 +18,11 @@
 // from the lengths itself: no planning launch.
 //
 // Warps: 0 walks the line and brings the keys (TMA, one box per page), 1 issues
-// the MMAs, 4-7 bring the queries (one box for 128 contiguous columns, else 16
-// bytes a lane, which also gathers the queries of a path) and their
-// log-sum-exps, 8-11 / 12-15 take the exponentials of the first / second 128
-// keys. TMEM: two buffers of 128 columns for each.
+// the MMAs, 2 brings the earlier weights, 4-7 bring the queries (one box for 128
+// contiguous columns, else 16 bytes a lane, which also gathers the queries of a
+// path) and their log-sum-exps, 8-15 and 16-23 take the exponentials, blocks in turn (a warp's
+// waits and loads are the other group's work). TMEM: two buffers of 128 columns
+// for each half of a unit's keys.
 #include "keep.cuh"
 #include "warp_pipe.cuh"
 
@@ -31,10 +32,11 @@ namespace {
 
 constexpr int kTileKeys = kBlockKeys, kUnitKeys = 2 * kTileKeys, kCols = 128;
 constexpr int kStageBytes = 2 * kBlockBytes, kQBytes = kCols * kRowBytes;
-constexpr int kKStages = 4, kQStages = 3, kUnits = 4;
-constexpr int kThreads = 512;
+constexpr int kKStages = 4, kQStages = 4, kOldStages = 8, kUnits = 4;
+constexpr int kThreads = 768, kGroupWarps = 8;  // warps that take the exponentials of a block
 constexpr uint32_t kTmemCols = 512;
 constexpr int kWholeBlocks = 3;  // units of up to so many blocks are never cut
+constexpr int kCostShort = 3;    // of a unit of a row with one block of queries
 constexpr int kMinQuota = 3;
 constexpr int kRingBytes = kKStages * kStageBytes + kQStages * kQBytes;
 
@@ -43,15 +45,20 @@ struct alignas(16) Unit {
   int32_t kvh, k0, len, n, q0;  // first key, row length, queries, first query token
   int32_t b0, b1;               // query blocks to do here (none: old weights only decay)
   int32_t slot;                 // partial slot, or -1: the whole unit
-  uint32_t pages;               // which of its 16 pages exist
+  int32_t pairs;                // a run of units with the same one block of queries
 };
 
 struct WeightsSmem {
   uint64_t unit_full[kUnits], unit_empty[kUnits];
   uint64_t k_full[kKStages], k_empty[kKStages], q_full[kQStages], q_empty[kQStages];
   uint64_t s_full[2][2], s_empty[2][2];  // [tile][buffer]
+  uint64_t old_full[kOldStages], old_empty[kOldStages];
+  uint64_t sum_full[kGroupWarps], sum_empty[kGroupWarps];
   uint64_t drain;
   Unit units[kUnits];
+  uint32_t pages[kKStages];  // which of a unit's 16 pages exist
+  float old[kOldStages][kUnitKeys];  // earlier weights
+  float sums[kUnitKeys];             // the second group's, for the first
   alignas(16) float neg_lse[kQStages][kCols];  // -lse log2(e) of each column, -inf: the column adds nothing
   int64_t scan[kThreads / 32];
   int64_t prefix[kMaxSeqs + 1];  // cost of the rows before each
@@ -67,7 +74,6 @@ struct RowGeom {
   int tok;                     // queries of a block
   int nb;                      // blocks of all its queries
   int u0, u1;                  // units
-  bool small;                  // its queries fit 32 columns
 
   // the blocks of unit u whose queries see some key of it
   __device__ __forceinline__ void blocks(int u, int* b0, int* b1) const {
@@ -80,7 +86,7 @@ struct RowGeom {
   __device__ __forceinline__ int cost(int u) const {
     int b0, b1;
     blocks(u, &b0, &b1);
-    return b1 == b0 ? 1 : small ? 3 : 2 + 2 * (b1 - b0);
+    return b1 == b0 ? 1 : nb == 1 ? kCostShort : 2 + 2 * (b1 - b0);
   }
 };
 
@@ -103,7 +109,6 @@ __device__ __forceinline__ bool row_geom(const WeightParams& p, int r, RowGeom* 
   // weights before the first window change only if they decay
   w->u0 = w->window > 0 && p.decay == 1.f ? max(0, w->C - w->window + 1) / kUnitKeys : 0;
   w->u1 = (w->S + kUnitKeys - 1) / kUnitKeys;
-  w->small = w->n * (int64_t)p.group <= 32;
   return true;
 }
 
@@ -126,7 +131,7 @@ __device__ __forceinline__ int64_t head_cost(const RowGeom& w) {
   int u = w.u0;
   if (w.window == 0) {  // all blocks see the keys before the first query
     const int all = min(w.u1, (w.C + w.tok - 1) / kUnitKeys + 1);
-    sum = (int64_t)(w.small ? 3 : 2 + 2 * w.nb) * all;
+    sum = (int64_t)(w.nb == 1 ? kCostShort : 2 + 2 * w.nb) * all;
     u = all;
   }
   for (; u < w.u1; ++u) sum += w.cost(u);
@@ -142,7 +147,8 @@ __device__ __forceinline__ int blocks_before(int64_t x, int nb) {
 __device__ __forceinline__ bool unit_ok(const WeightParams& p, const Unit& a) {
   return a.row < p.num_seqs && a.kvh >= 0 && a.kvh < p.num_kv_heads && a.k0 >= 0 && a.k0 < a.len &&
          a.len <= p.max_slots && a.n >= 1 && a.n <= a.len && a.b0 >= 0 && a.b1 >= a.b0 &&
-         (int64_t)(a.b1 - 1) * (kCols / p.group) < a.n && a.q0 >= 0 && a.q0 < p.total_q && a.slot < 2 * kWeightCtas;
+         (int64_t)(a.b1 - 1) * (kCols / p.group) < a.n && a.q0 >= 0 && a.q0 < p.total_q && a.slot < 2 * kWeightCtas && a.pairs >= 1 &&
+         (int64_t)a.k0 + (int64_t)(a.pairs - 1) * kUnitKeys < a.len && (a.pairs == 1 || a.b1 == a.b0 + 1);
 }
 
 // S = K Q^T of one tile by one elected lane of a warp in step, and the commit behind it.
@@ -161,6 +167,16 @@ __device__ __forceinline__ void mma_keys_e(uint32_t d, uint64_t k, uint64_t q, u
       : "memory");
 }
 
+// One word from global to shared memory, asynchronously; the arrival of this
+// thread on a barrier once all its copies so far have landed; the wait for them.
+__device__ __forceinline__ void copy_word(uint32_t dst, const float* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
 // Columns of block b of a unit: those of its queries, and rounded up to the MMA's step.
 __device__ __forceinline__ int block_cols(const Unit& a, int b, int g) { return min(kCols, (a.n - b * (kCols / g)) * g); }
 
@@ -171,6 +187,15 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[32]) {  
       : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
         "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
       : "r"(taddr));
+#pragma unroll
+  for (int e = 16; e < 32; ++e) v[e] = 0u;
+}
+
+// Waits for this thread's TMEM loads; what they loaded is not used before.
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[32]) {
+  tmem_ld_wait();
+#pragma unroll
+  for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(v[e]));
 }
 
 // sum += 2^(s scale + neg_lse) over kN columns; masked: only columns lo <= c < hi.
@@ -216,19 +241,27 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 32) {
     for (int i = 0; i < kUnits; ++i) {
       mbar_init(bar(st.unit_full[i]), 1);
-      mbar_init(bar(st.unit_empty[i]), 1 + 4 + 8);
+      mbar_init(bar(st.unit_empty[i]), 1 + 1 + 4 + 2 * kGroupWarps);
     }
     for (int i = 0; i < kKStages; ++i) {
       mbar_init(bar(st.k_full[i]), 2);
-      mbar_init(bar(st.k_empty[i]), 1);
+      mbar_init(bar(st.k_empty[i]), 1 + kGroupWarps);
     }
     for (int i = 0; i < kQStages; ++i) {
-      mbar_init(bar(st.q_full[i]), 4);
-      mbar_init(bar(st.q_empty[i]), 1 + 8);
+      mbar_init(bar(st.q_full[i]), 2);
+      mbar_init(bar(st.q_empty[i]), 1 + 2 * kGroupWarps);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(st.s_full[i >> 1][i & 1]), 1);
       mbar_init(bar(st.s_empty[i >> 1][i & 1]), 4);
+    }
+    for (int i = 0; i < kOldStages; ++i) {
+      mbar_init(bar(st.old_full[i]), 32);
+      mbar_init(bar(st.old_empty[i]), kGroupWarps);
+    }
+    for (int i = 0; i < kGroupWarps; ++i) {
+      mbar_init(bar(st.sum_full[i]), 1);
+      mbar_init(bar(st.sum_empty[i]), 1);
     }
     mbar_init(bar(st.drain), 1);
     st.abort_flag = 0;
@@ -326,11 +359,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       pos += __shfl_sync(0xffffffffu, (long long)incl, 31);
     }
     pos += begin - rem;  // where the unit begins on the line
-    auto page_of = [&](int r, int unit) -> int {  // page id `lane` of a unit (lanes 0 .. 15)
+    // page ids of a row from a unit on, two units' at a time
+    auto page_of = [&](int r, int unit) -> int {
       const int64_t lp = (int64_t)unit * (kUnitKeys / kPage) + lane;
-      return lane < 16 && lp < p.max_pages ? p.block_table[(size_t)r * p.max_pages + lp] : -1;
+      return lp < p.max_pages ? p.block_table[(size_t)r * p.max_pages + lp] : -1;
     };
-    int id = page_of(row, u);
+    int ids = page_of(row, u);
     while (pos < end && ok) {
       int b0, b1;
       w.blocks(u, &b0, &b1);
@@ -346,16 +380,23 @@ __global__ void __launch_bounds__(kThreads, 1)
       a.b0 = b0 + s0;
       a.b1 = b0 + s1;
       a.slot = s0 == 0 && s1 == nb ? -1 : 2 * (int)blockIdx.x + (s0 == 0 ? 1 : 0);
+      a.pairs = 1;
       const bool mine = s1 > s0 || (nb == 0 && begin <= pos);
+      // units that begin in this piece, all with the same block of queries
+      if (mine && w.nb == 1 && w.window == 0)
+        a.pairs = (int)min((int64_t)(w.u1 - u), (end - pos + kCostShort - 1) / kCostShort);
       if (mine && a.slot >= 0 && s0 == 0 && lane == 0) {
         int last = blockIdx.x;
         for (int64_t e = end; blocks_before(e - pos, nb) < nb; e += quota) ++last;
         p.cuts[blockIdx.x] = make_int4(last, row, kvh, a.k0);
       }
-      // this unit's pages, and the next unit
-      const int C = w.C, W = w.window, this_id = id;
-      pos += c;
-      if (++u == w.u1) {
+      // the next unit
+      const int C = w.C, W = w.window;
+      int these = ids, next_ids = -1;
+      const int second = u + 2;
+      pos += (int64_t)c * a.pairs;
+      u += a.pairs;
+      if (u == w.u1) {
         u = w.u0;
         if (++kvh == Hkv) {
           kvh = 0;
@@ -367,20 +408,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
-      if (pos < end) id = page_of(row, u);
+      if (pos < end) ids = page_of(row, u);
       if (!mine) continue;
-      const int pk = a.k0 + lane * kPage, pl = min(pk + kPage, a.len) - 1;  // the page's keys
-      const bool exists = this_id >= 0 && this_id < p.num_pages;
-      const bool seen = lane < 16 && pk < a.len && (W == 0 || pl >= C || pl + W > C);
-      if (seen && !exists && a.b1 > a.b0) atomicOr(p.status, kStatusBadPage);
-      a.pages = __ballot_sync(0xffffffffu, exists) & 0xffffu;
-      const int y = exists && pk < a.len ? (this_id * Hkv + a.kvh) * kPage : p.oob_row;
       if (!unit_ok(p, a)) {
         atomicOr(p.status, kStatusPlanOverflow);
         *abort_flag = 2;
         ok = false;
         break;
       }
+      if (a.pairs > 2) next_ids = page_of(a.row, second);
       ok = wait_warp(bar(st.unit_empty[ru.s]), ru.parity ^ 1);
       if (!ok) break;
       if (lane == 0) {
@@ -390,17 +426,33 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       ru.next();
       if (a.b0 == a.b1) continue;
-      ok = wait_warp(bar(st.k_empty[rk.s]), rk.parity ^ 1);
-      if (!ok) break;
-      int ys[kBlockPages];
+#pragma unroll 1
+      for (int i = 0; i < a.pairs; ++i) {
+        if (i > 0 && !(i & 1)) {
+          these = next_ids;
+          if (i + 2 < a.pairs) next_ids = page_of(a.row, second + i);
+        }
+        const int id = __shfl_sync(0xffffffffu, these, (i & 1) * 16 + (lane & 15));
+        const int pk = a.k0 + i * kUnitKeys + (lane & 15) * kPage, pl = min(pk + kPage, a.len) - 1;  // the page's keys
+        const bool exists = id >= 0 && id < p.num_pages;
+        const bool seen = pk < a.len && (W == 0 || pl >= C || pl + W > C);
+        if (seen && !exists && lane < 16) atomicOr(p.status, kStatusBadPage);
+        const uint32_t pages = __ballot_sync(0xffffffffu, exists) & 0xffffu;
+        const int y = exists && pk < a.len ? (id * Hkv + a.kvh) * kPage : p.oob_row;
+        ok = wait_warp(bar(st.k_empty[rk.s]), rk.parity ^ 1);
+        if (!ok) break;
+        st.pages[rk.s] = pages;
+        __syncwarp();
+        int ys[kBlockPages];
 #pragma unroll
-      for (int j = 0; j < kBlockPages; ++j) ys[j] = __shfl_sync(0xffffffffu, y, j);
-      load_block_e(sK + rk.s * kStageBytes, &kmap, ys, bar(st.k_full[rk.s]), policy_evict_first());
+        for (int j = 0; j < kBlockPages; ++j) ys[j] = __shfl_sync(0xffffffffu, y, j);
+        load_block_e(sK + rk.s * kStageBytes, &kmap, ys, bar(st.k_full[rk.s]), policy_evict_first());
 #pragma unroll
-      for (int j = 0; j < kBlockPages; ++j) ys[j] = __shfl_sync(0xffffffffu, y, kBlockPages + j);
-      load_block_e(sK + rk.s * kStageBytes + kBlockBytes, &kmap, ys, bar(st.k_full[rk.s]), policy_evict_first());
-      rk.next();
-      ++loaded;
+        for (int j = 0; j < kBlockPages; ++j) ys[j] = __shfl_sync(0xffffffffu, y, kBlockPages + j);
+        load_block_e(sK + rk.s * kStageBytes + kBlockBytes, &kmap, ys, bar(st.k_full[rk.s]), policy_evict_first());
+        rk.next();
+        ++loaded;
+      }
     }
     if (!ok && *abort_flag == 0) *abort_flag = 1;
     if (ok && wait_warp(bar(st.unit_empty[ru.s]), ru.parity ^ 1)) {
@@ -426,12 +478,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) break;
       const Unit a = st.units[ru.s];
       if (a.row < 0) break;
-      if (a.b0 < a.b1) {
+      for (int i = 0; i < (a.b0 < a.b1 ? a.pairs : 0) && ok; ++i) {
         ok = wait_warp(bar(st.k_full[rk.s]), rk.parity);
         for (int b = a.b0; b < a.b1 && ok; ++b) {
           const uint32_t cols = (block_cols(a, b, g) + 15) & ~15;
           const uint32_t idesc = idesc_bf16(kTileKeys, 0, false, false) | ((cols >> 3) << 17);
-          ok = wait_warp(bar(st.q_full[rq.s]), rq.parity);
+          if (i == 0) ok = wait_warp(bar(st.q_full[rq.s]), rq.parity);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             ok = ok && wait_warp(bar(st.s_empty[t][rs.s]), rs.parity ^ 1);
@@ -442,14 +494,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                        bar(st.s_full[t][rs.s]));
           }
           if (!ok) break;
-          tc_commit_e(bar(st.q_empty[rq.s]));
-          rq.next();
+          if (i == a.pairs - 1) {  // a run of units keeps its block of queries
+            tc_commit_e(bar(st.q_empty[rq.s]));
+            rq.next();
+          }
           rs.next();
         }
         if (!ok) break;
         tc_commit_e(bar(st.k_empty[rk.s]));
         rk.next();
       }
+      if (!ok) break;
       if (lane == 0) mbar_arrive(bar(st.unit_empty[ru.s]));
       __syncwarp();
       ru.next();
@@ -457,12 +512,44 @@ __global__ void __launch_bounds__(kThreads, 1)
     if (!ok && *abort_flag == 0) *abort_flag = 1;
     tc_commit_e(bar(st.drain));  // MMAs still in flight must not outlive TMEM
     mbar_wait(bar(st.drain), 0);
+  } else if (warp == 2) {
+    // ---------------------------------------------------------- earlier weights
+    RingAt<kUnits> ru;
+    RingAt<kOldStages> ro;
+    bool ok = true;
+    while (ok) {
+      ok = wait_warp(bar(st.unit_full[ru.s]), ru.parity);
+      if (!ok) break;
+      const Unit a = st.units[ru.s];
+      if (a.row < 0) break;
+      const int old_end = a.slot < 0 && p.decay != 0.f ? a.len - a.n : 0;
+      const float* w = p.weights + ((size_t)a.row * Hkv + a.kvh) * p.max_slots;
+      for (int i = 0, k0 = a.k0; i < a.pairs; ++i, k0 += kUnitKeys) {
+        ok = wait_warp(bar(st.old_empty[ro.s]), ro.parity ^ 1);
+        if (!ok) break;
+#pragma unroll
+        for (int k = 0; k < kUnitKeys / 32; ++k) {
+          const int x = 32 * k + lane;
+          if (k0 + x < old_end) copy_word(smem_addr(&st.old[ro.s][x]), w + k0 + x);
+        }
+        copies_arrive(bar(st.old_full[ro.s]));
+        ro.next();
+      }
+      if (!ok) break;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(st.unit_empty[ru.s]));
+      __syncwarp();
+      ru.next();
+    }
+    if (!ok && *abort_flag == 0) *abort_flag = 1;
+    copies_wait();  // none in flight when the block ends
   } else if (warp >= 4 && warp < 8) {
     // ---------------------------------------------------------------- queries
-    const int w = warp - 4;  // rows 32 w .. of every block
+    // The four warps take turns, a block each, so that four are on their way.
     RingAt<kQStages> rq;
     RingAt<kUnits> ru;
-    uint32_t boxes = 0, last_box = 0, last_parity = 0;
+    const int log_g = __ffs(g) - 1;
+    uint32_t boxes = 0, turn = warp - 4;
     bool ok = true;
     while (ok) {
       ok = wait_warp(bar(st.unit_full[ru.s]), ru.parity);
@@ -470,52 +557,61 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Unit a = st.units[ru.s];
       if (a.row < 0) break;
       const int32_t* path = p.path ? p.path + (size_t)a.row * p.max_path : nullptr;
-      for (int b = a.b0; b < a.b1; ++b) {
-        const int cols = block_cols(a, b, g), t0 = b * (kCols / g);
+      for (int b = a.b0; b < a.b1; ++b, rq.next(), turn = (turn - 1) & 3) {
+        if (turn != 0) continue;
+        const int cols = block_cols(a, b, g), t0 = b * (kCols >> log_g);
         const bool box = !path && cols == kCols;
         // (query token, q head) row of a column
         auto source = [&](int c) -> size_t {
-          const int i = t0 + c / g;
-          return (size_t)(a.q0 + (path ? path[i] : i)) * Hq + a.kvh * g + c % g;
+          const int i = t0 + (c >> log_g);
+          return (size_t)(a.q0 + (path ? path[i] : i)) * Hq + (a.kvh << log_g) + (c & (g - 1));
         };
-        const int c0 = 32 * w + lane;
-        float nl = -INFINITY;
-        if (c0 < cols) {
-          const float lse = p.lse[source(c0)];
-          nl = lse == -INFINITY ? -INFINITY : -lse * 1.4426950408889634f;
+        float nl[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          nl[k] = INFINITY;
+          if (32 * k + lane < cols) nl[k] = p.lse[source(32 * k + lane)];
         }
-        uint4 v[8];
-        if (!box && 32 * w < cols) {
+        uint4 v[8];  // 32 columns' rows, four of them at a time
+        auto load = [&](int c0) {
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const int c = 32 * w + 4 * k + (lane >> 3);
+            const int c = c0 + 4 * k + (lane >> 3);
             v[k] = make_uint4(0u, 0u, 0u, 0u);
             if (c < cols) v[k] = reinterpret_cast<const uint4*>(p.q + source(c) * kHeadDim)[lane & 7];
           }
-        }
+        };
+        if (!box) load(0);
         ok = wait_warp(bar(st.q_empty[rq.s]), rq.parity ^ 1);
         if (!ok) break;
-        st.neg_lse[rq.s][c0] = nl;
-        if (!box && 32 * w < cols) {
+        if (box) {
+          if (lane == 0) {
+            mbar_arrive_expect_tx(bar(st.q_full[rq.s]), kQBytes);
+            tma_load_3d(sQ + rq.s * kQBytes, &qmap, 0, a.kvh << log_g, a.q0 + t0, bar(st.q_full[rq.s]));
+          }
+          __syncwarp();
+        } else {
+#pragma unroll 1
+          for (int c0 = 0; c0 < cols; c0 += 32) {
+            if (c0 > 0) load(c0);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int c = 32 * w + 4 * k + (lane >> 3);
-            *reinterpret_cast<uint4*>(base_ptr + (sQ - base) + rq.s * kQBytes + swz128(c, lane & 7)) = v[k];
+            for (int k = 0; k < 8; ++k) {
+              const int c = c0 + 4 * k + (lane >> 3);
+              *reinterpret_cast<uint4*>(base_ptr + (sQ - base) + rq.s * kQBytes + swz128(c, lane & 7)) = v[k];
+            }
           }
           fence_proxy_async();
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          st.neg_lse[rq.s][32 * k + lane] = nl[k] == -INFINITY ? -INFINITY : -nl[k] * 1.4426950408889634f;
         __syncwarp();
         if (lane == 0) {
-          if (box && w == 0) {
-            mbar_arrive_expect_tx(bar(st.q_full[rq.s]), kQBytes);
-            tma_load_3d(sQ + rq.s * kQBytes, &qmap, 0, a.kvh * g, a.q0 + t0, bar(st.q_full[rq.s]));
-          } else {
-            mbar_arrive(bar(st.q_full[rq.s]));
-          }
+          if (!box) mbar_arrive(bar(st.q_full[rq.s]));
+          mbar_arrive(bar(st.q_full[rq.s]));
         }
         __syncwarp();
-        if (box) ++boxes, last_box = rq.s, last_parity = rq.parity;
-        rq.next();
+        if (box) boxes |= 1u << (2 * rq.s + rq.parity);  // stages and turns it has sent a box to
       }
       if (!ok) break;
       if (lane == 0) mbar_arrive(bar(st.unit_empty[ru.s]));
@@ -523,91 +619,128 @@ __global__ void __launch_bounds__(kThreads, 1)
       ru.next();
     }
     if (!ok && *abort_flag == 0) *abort_flag = 1;
-    // after an abort: the last box may still be in flight (the ones before it were waited for by its stage's turn, or
-    // lie in the other stages: each is waited for)
-    if (*abort_flag && w == 0 && lane == 0 && boxes > 0) {
-      mbar_wait(bar(st.q_full[last_box]), last_parity);
-      for (uint32_t s = 0; s < kQStages; ++s)
-        if (s != last_box) mbar_wait(bar(st.q_full[s]), s < rq.s ? rq.parity : rq.parity ^ 1);
-    }
+    // after an abort: wait (bounded) for boxes still in flight
+    if (*abort_flag && lane == 0)
+      for (uint32_t s = 0; s < 2 * kQStages; ++s)
+        if (boxes >> s & 1u) mbar_wait(bar(st.q_full[s >> 1]), s & 1u);
   } else if (warp >= 8) {
     // ----------------------------------------------------------- exponentials
-    const int t = (warp - 8) >> 2, key = (warp & 3) * 32 + lane;  // tile, TMEM lane
-    const uint32_t lane_base = st.tmem_base + t * 256 + ((uint32_t)((warp & 3) * 32) << 16);
+    // Two groups of eight warps take the blocks in turn, the second buffer of S
+    // the second group's. Where a unit's blocks are one, the group that has it
+    // finishes the unit; else the first group, with the second's sums.
+    const int group = (warp - 8) >> 3, part = warp & 7, t = part >> 2;  // tile t
+    const int key = part * 32 + lane;                                  // of the unit
+    const uint32_t tmem_s = st.tmem_base + t * 256 + group * 128 + ((uint32_t)((warp & 3) * 32) << 16);
     const uint64_t sc = pack_f32x2(p.scale_log2, p.scale_log2);
+    RingAt<kKStages> rk;
     RingAt<kQStages> rq;
+    RingAt<kOldStages> ro;
     RingAt<kUnits> ru;
-    RingAt<2> rs;
+    uint32_t cnt = 0, sums = 0;  // blocks, sums handed over
+    const int W = p.window;
     bool ok = true;
     while (ok) {
       ok = wait_warp(bar(st.unit_full[ru.s]), ru.parity);
       if (!ok) break;
       const Unit a = st.units[ru.s];
       if (a.row < 0) break;
-      const int C = a.len - a.n, first = a.k0 + t * kTileKeys + (warp & 3) * 32, j = first + lane;
-      const int W = p.window;
-      const bool live = j < a.len, busy = first < a.len;
-      const bool exists = a.pages >> ((j - a.k0) / kPage) & 1u;
-      // a key that some query sees, on a page that is missing, keeps its weight
-      const bool seen = j >= C || W == 0 || (int64_t)j + W > C;
-      const bool writes = live && (exists || !seen);
-      float* w = p.weights + ((size_t)a.row * Hkv + a.kvh) * p.max_slots + j;
-      float old = 0.f;
-      if (a.slot < 0 && writes && j < C && p.decay != 0.f) old = *w;
-      float total_sum = 0.f;
-      for (int b = a.b0; b < a.b1; ++b) {
-        const int cols = (block_cols(a, b, g) + 15) & ~15, t0 = b * (kCols / g);
-        ok = wait_warp(bar(st.q_full[rq.s]), rq.parity) && wait_warp(bar(st.s_full[t][rs.s]), rs.parity);
-        if (!ok) break;
-        tc_fence_after();
-        const float* nl = st.neg_lse[rq.s];
-        const uint32_t s = lane_base + rs.s * 128;
-        uint64_t sum[2] = {0, 0};
-        uint32_t sv[32];
-        // hidden from some query of the block: keys behind its first, or before the window of its last
-        const int tl = min(t0 + kCols / g, a.n) - 1;
-        const bool plain = first + 31 <= C + t0 && (W == 0 || C + tl - first < W);
-        if (busy && plain) {
-          for (int c = 0; c + 32 <= cols; c += 32) {
-            tmem_ld32(s + c, sv);
-            tmem_ld_wait();
-            add_columns<32, false>(sv, nl + c, sc, 0, 0, sum);
-          }
-          if (cols & 16) {
-            tmem_ld16(s + (cols & ~31), sv);
-            tmem_ld_wait();
-            add_columns<16, false>(sv, nl + (cols & ~31), sc, 0, 0, sum);
-          }
-        } else if (busy) {
-          const int lo = min(max(j - C - t0, 0), kCols) * g;
-          const int hi = W == 0 ? kCols * kMaxGroup : (int)min(max((int64_t)j + W - C - t0, (int64_t)0), (int64_t)kCols) * g;
-          for (int c = 0; c + 32 <= cols; c += 32) {
-            tmem_ld32(s + c, sv);
-            tmem_ld_wait();
-            add_columns<32, true>(sv, nl + c, sc, lo - c, hi - c, sum);
-          }
-          if (cols & 16) {
-            const int c = cols & ~31;
-            tmem_ld16(s + c, sv);
-            tmem_ld_wait();
-            add_columns<16, true>(sv, nl + c, sc, lo - c, hi - c, sum);
-          }
+      const int C = a.len - a.n, blocks = a.b1 - a.b0;
+      float* w = p.weights + ((size_t)a.row * Hkv + a.kvh) * p.max_slots;
+      const int old_end = a.slot < 0 && p.decay != 0.f ? C : 0;
+      int j = a.k0 + key;
+      for (int i = 0; i < a.pairs; ++i, j += kUnitKeys) {
+        const int first = j - lane;
+        const bool busy = first < a.len;
+        const bool finishes = blocks == 1 ? (int)(cnt & 1) == group : group == 0;
+        uint32_t pages = 0;
+        if (finishes && blocks > 0) {
+          ok = wait_warp(bar(st.k_full[rk.s]), rk.parity);
+          if (!ok) break;
+          pages = st.pages[rk.s];
+          __syncwarp();
+          mbar_arrive_e(bar(st.k_empty[rk.s]));
         }
-        tc_fence_before();
-        __syncwarp();
-        mbar_arrive_e(bar(st.s_empty[t][rs.s]));
-        mbar_arrive_e(bar(st.q_empty[rq.s]));
-        const uint64_t both = add2(sum[0], sum[1]);
-        total_sum += lo_f32(both) + hi_f32(both);
-        rq.next();
-        rs.next();
+        if (blocks > 0) rk.next();
+        float total = 0.f;
+        for (int b = a.b0; b < a.b1; ++b, ++cnt) {
+          const bool last_use = i >= a.pairs - 2;  // of the block of queries, by this group
+          if ((int)(cnt & 1) != group) {
+            if (i == a.pairs - 1) rq.next();
+            continue;
+          }
+          const int cols = (block_cols(a, b, g) + 15) & ~15, t0 = b * (kCols / g);
+          ok = (i > 1 || wait_warp(bar(st.q_full[rq.s]), rq.parity)) && wait_warp(bar(st.s_full[t][group]), (cnt >> 1) & 1);
+          if (!ok) break;
+          tc_fence_after();
+          const float* nl = st.neg_lse[rq.s];
+          uint64_t sum[2] = {0, 0};
+          // hidden from some query of the block: keys behind its first, or before the window of its last
+          const int tl = min(t0 + kCols / g, a.n) - 1;
+          const bool plain = first + 31 <= C + t0 && (W == 0 || C + tl - first < W);
+          if (busy) {
+            const int lo = min(max(j - C - t0, 0), kCols) * g;
+            const int hi = W == 0 ? kCols * kMaxGroup
+                                  : (int)min(max((int64_t)j + W - C - t0, (int64_t)0), (int64_t)kCols) * g;
+            uint32_t sv[32];
+#pragma unroll 1
+            for (int c = 0; c < cols; c += 32) {
+              if (c + 32 <= cols) {
+                tmem_ld32(tmem_s + c, sv);
+                tmem_ld_wait_for(sv);
+                if (plain) add_columns<32, false>(sv, nl + c, sc, 0, 0, sum);
+                else add_columns<32, true>(sv, nl + c, sc, lo - c, hi - c, sum);
+              } else {
+                tmem_ld16(tmem_s + c, sv);
+                tmem_ld_wait_for(sv);
+                if (plain) add_columns<16, false>(sv, nl + c, sc, 0, 0, sum);
+                else add_columns<16, true>(sv, nl + c, sc, lo - c, hi - c, sum);
+              }
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          mbar_arrive_e(bar(st.s_empty[t][group]));
+          if (last_use) {
+            mbar_arrive_e(bar(st.q_empty[rq.s]));
+            if (a.pairs == 1) mbar_arrive_e(bar(st.q_empty[rq.s]));  // for the other group, which does not read it
+          }
+          const uint64_t both = add2(sum[0], sum[1]);
+          total += lo_f32(both) + hi_f32(both);
+          if (i == a.pairs - 1) rq.next();
+        }
+        if (!ok) break;
+        if (blocks > 1) {
+          if (group == 1) {
+            ok = wait_warp(bar(st.sum_empty[part]), (sums & 1) ^ 1);
+            if (!ok) break;
+            st.sums[key] = total;
+            __syncwarp();
+            mbar_arrive_e(bar(st.sum_full[part]));
+          } else {
+            ok = wait_warp(bar(st.sum_full[part]), sums & 1);
+            if (!ok) break;
+            total += st.sums[key];
+            __syncwarp();
+            mbar_arrive_e(bar(st.sum_empty[part]));
+          }
+          ++sums;
+        }
+        if (finishes) {
+          ok = wait_warp(bar(st.old_full[ro.s]), ro.parity);
+          if (!ok) break;
+          const float old = j < old_end ? st.old[ro.s][key] : 0.f;
+          __syncwarp();
+          mbar_arrive_e(bar(st.old_empty[ro.s]));
+          // a key that some query sees, on a page that is missing, keeps its weight
+          const bool seen = j >= C || W == 0 || (int64_t)j + W > C;
+          if (a.slot >= 0)
+            p.parts[(size_t)a.slot * kUnitKeys + key] = total;
+          else if (j < a.len && (!seen || (pages >> (key / kPage) & 1u)))
+            w[j] = p.decay * old + total;
+        }
+        ro.next();
       }
       if (!ok) break;
-      if (a.slot >= 0) {
-        p.parts[(size_t)a.slot * kUnitKeys + t * kTileKeys + key] = total_sum;
-      } else if (writes) {
-        *w = (j < C && p.decay != 0.f ? p.decay * old : 0.f) + total_sum;
-      }
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(st.unit_empty[ru.s]));
       __syncwarp();
