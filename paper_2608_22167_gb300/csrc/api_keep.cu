@@ -84,7 +84,7 @@ mcpu_status mcpu_accumulate_weights(const void* q, const float* lse, const void*
                                     void* workspace, size_t workspace_bytes, mcpu_stream_t stream) {
   mcpu_status st = check_dims(dims);
   if (st != MCPU_OK) return st;
-  if (!(softmax_scale > 0.f) || softmax_scale > 3.0e38f) return MCPU_ERR_INVALID_ARG;
+  if (!(softmax_scale >= 1e-30f && softmax_scale <= 1e30f)) return MCPU_ERR_INVALID_ARG;
   if (!(decay >= 0.f && decay <= 1.f) || max_slots < 1) return MCPU_ERR_INVALID_ARG;
   if (query_path ? !path_len || max_path < 0 : path_len != nullptr) return MCPU_ERR_INVALID_ARG;
   if (!workspace || !aligned(workspace, 256)) return MCPU_ERR_INVALID_ARG;
@@ -129,6 +129,7 @@ mcpu_status mcpu_accumulate_weights(const void* q, const float* lse, const void*
   p.group = group;
   p.decay = decay;
   p.scale_log2 = softmax_scale * 1.4426950408889634f;
+  p.inv_scale = 1.f / softmax_scale;
   return from_cuda(launch_weights(kmap, qmap, p, sms, reinterpret_cast<cudaStream_t>(stream)));
 }
 

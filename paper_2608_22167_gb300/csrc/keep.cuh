@@ -32,7 +32,7 @@ struct WeightParams {
   float* parts;  // [2 * kWeightCtas][256] sums of cut units' parts
   int32_t max_path, max_slots, window, num_seqs, total_q, max_pages, num_pages, num_q_heads, num_kv_heads, group;
   int32_t oob_row;  // a pool row past the end: read as zeros
-  float decay, scale_log2;
+  float decay, scale_log2, inv_scale;
 };
 constexpr int kWeightCtas = 160;  // CTAs the workspace has room for (one per SM)
 cudaError_t launch_weights(const CUtensorMap& kmap, const CUtensorMap& qmap, const WeightParams& p, int sms,

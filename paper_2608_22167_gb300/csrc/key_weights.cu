@@ -18,7 +18,7 @@
 // from the lengths itself: no planning launch.
 //
 // Warps: 0 walks the line and brings the keys (TMA, one box per page), 1 issues
-// the MMAs, 2 brings the earlier weights, 4-7 bring the queries (one box for 128
+// the MMAs, 2 brings the earlier weights, 4-6 bring the queries (one box for 128
 // contiguous columns, else 16 bytes a lane, which also gathers the queries of a
 // path) and their log-sum-exps, 8-15 and 16-23 take the exponentials, blocks in turn (a warp's
 // waits and loads are the other group's work). TMEM: two buffers of 128 columns
@@ -32,13 +32,21 @@ namespace {
 
 constexpr int kTileKeys = kBlockKeys, kUnitKeys = 2 * kTileKeys, kCols = 128;
 constexpr int kStageBytes = 2 * kBlockBytes, kQBytes = kCols * kRowBytes;
-constexpr int kKStages = 4, kQStages = 4, kOldStages = 8, kUnits = 4;
+constexpr int kKStages = 4, kQStages = 3, kOldStages = 8, kUnits = 4;
+constexpr int kQueryWarps = 3;
+// each fills a stage of its own: a warp that came to another's stage two turns
+// early would take an older phase of the same parity for its own
+static_assert(kQueryWarps == kQStages, "a stage each");
 constexpr int kThreads = 768, kGroupWarps = 8;  // warps that take the exponentials of a block
 constexpr uint32_t kTmemCols = 512;
 constexpr int kWholeBlocks = 3;  // units of up to so many blocks are never cut
 constexpr int kCostShort = 3;    // of a unit of a row with one block of queries
 constexpr int kMinQuota = 3;
-constexpr int kRingBytes = kKStages * kStageBytes + kQStages * kQBytes;
+// A fifth step of the product, over 16 dims of which three are used: 1 for every
+// key, and -lse / scale of a column in three bf16 pieces (24 bits). As 8 x 16
+// byte matrices without swizzle: first dims 0-7 of all rows, then 8-15.
+constexpr int kExtraHalf = kCols * 16, kExtraBytes = 2 * kExtraHalf;
+constexpr int kRingBytes = kKStages * kStageBytes + kQStages * (kQBytes + kExtraBytes) + kExtraBytes;
 
 struct alignas(16) Unit {
   int32_t row;  // -1: no more units
@@ -59,7 +67,6 @@ struct WeightsSmem {
   uint32_t pages[kKStages];  // which of a unit's 16 pages exist
   float old[kOldStages][kUnitKeys];  // earlier weights
   float sums[kUnitKeys];             // the second group's, for the first
-  alignas(16) float neg_lse[kQStages][kCols];  // -lse log2(e) of each column, -inf: the column adds nothing
   int64_t scan[kThreads / 32];
   int64_t prefix[kMaxSeqs + 1];  // cost of the rows before each
   uint32_t tmem_base;
@@ -151,8 +158,15 @@ __device__ __forceinline__ bool unit_ok(const WeightParams& p, const Unit& a) {
          (int64_t)a.k0 + (int64_t)(a.pairs - 1) * kUnitKeys < a.len && (a.pairs == 1 || a.b1 == a.b0 + 1);
 }
 
-// S = K Q^T of one tile by one elected lane of a warp in step, and the commit behind it.
-__device__ __forceinline__ void mma_keys_e(uint32_t d, uint64_t k, uint64_t q, uint32_t idesc, uint32_t done) {
+// Descriptor of the fifth step's operands.
+__device__ __forceinline__ uint64_t extra_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(kExtraHalf >> 4) << 16 | (uint64_t)(128 >> 4) << 32 |
+         (uint64_t)1 << 46;
+}
+
+// S = K Q^T - lse / scale of one tile by one elected lane of a warp in step, and the commit behind it.
+__device__ __forceinline__ void mma_keys_e(uint32_t d, uint64_t k, uint64_t q, uint64_t ones, uint64_t lse,
+                                           uint32_t idesc, uint32_t done) {
   static_assert(kHeadDim == 64, "four steps of 16 dims, 32 bytes each");
   asm volatile(
       "{\n\t.reg .pred e, t, f;\n\t.reg .b64 a, b;\n\telect.sync _|e, 0xffffffff;\n\t"
@@ -161,9 +175,10 @@ __device__ __forceinline__ void mma_keys_e(uint32_t d, uint64_t k, uint64_t q, u
       "add.s64 a, %1, 2;\n\tadd.s64 b, %2, 2;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
       "add.s64 a, %1, 4;\n\tadd.s64 b, %2, 4;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
       "add.s64 a, %1, 6;\n\tadd.s64 b, %2, 6;\n\t@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, t;\n\t"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %5, %6, %3, t;\n\t"
       "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%4];\n\t"
       "}" ::"r"(d),
-      "l"(k), "l"(q), "r"(idesc), "r"(done)
+      "l"(k), "l"(q), "r"(idesc), "r"(done), "l"(ones), "l"(lse)
       : "memory");
 }
 
@@ -191,6 +206,12 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&v)[32]) {  
   for (int e = 16; e < 32; ++e) v[e] = 0u;
 }
 
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 // Waits for this thread's TMEM loads; what they loaded is not used before.
 __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[32]) {
   tmem_ld_wait();
@@ -198,24 +219,18 @@ __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[32]) {
   for (int e = 0; e < 32; ++e) asm volatile("" : "+r"(v[e]));
 }
 
-// sum += 2^(s scale + neg_lse) over kN columns; masked: only columns lo <= c < hi.
+// sum += 2^(s scale) over kN columns; masked: only columns lo <= c < hi.
 template <int kN, bool kMasked>
-__device__ __forceinline__ void add_columns(const uint32_t (&sv)[32], const float* neg_lse, uint64_t sc, int lo, int hi,
-                                            uint64_t (&sum)[2]) {
+__device__ __forceinline__ void add_columns(const uint32_t (&sv)[32], uint64_t sc, int lo, int hi, uint64_t (&sum)[2]) {
 #pragma unroll
-  for (int e = 0; e < kN; e += 4) {
-    const ulonglong2 nl = *reinterpret_cast<const ulonglong2*>(neg_lse + e);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int c = e + 2 * k;
-      const uint64_t x = fma2((uint64_t)sv[c] | ((uint64_t)sv[c + 1] << 32), sc, k ? nl.y : nl.x);
-      float x0 = lo_f32(x), x1 = hi_f32(x);
-      if (kMasked) {
-        x0 = c >= lo && c < hi ? x0 : -INFINITY;
-        x1 = c + 1 >= lo && c + 1 < hi ? x1 : -INFINITY;
-      }
-      sum[k] = add2(sum[k], pack_f32x2(ex2_approx(x0), ex2_approx(x1)));
+  for (int c = 0; c < kN; c += 2) {
+    const uint64_t x = mul2((uint64_t)sv[c] | ((uint64_t)sv[c + 1] << 32), sc);
+    float x0 = lo_f32(x), x1 = hi_f32(x);
+    if (kMasked) {
+      x0 = c >= lo && c < hi ? x0 : -INFINITY;
+      x1 = c + 1 >= lo && c + 1 < hi ? x1 : -INFINITY;
     }
+    sum[(c >> 1) & 1] = add2(sum[(c >> 1) & 1], pack_f32x2(ex2_approx(x0), ex2_approx(x1)));
   }
 }
 
@@ -231,7 +246,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int32_t* abort_flag = &st.abort_flag;
   auto bar = [&](uint64_t& b) { return smem_addr(&b); };
   const int B = p.num_seqs, g = p.group, Hkv = p.num_kv_heads, Hq = p.num_q_heads;
-  const uint32_t sK = base, sQ = base + kKStages * kStageBytes;
+  const uint32_t sK = base, sQ = base + kKStages * kStageBytes, sLse = sQ + kQStages * kQBytes,
+                 sOnes = sLse + kQStages * kExtraBytes;
 
   // Before anything is read: TMEM, the barriers, the tensor maps.
   if (warp == 0) {
@@ -241,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (threadIdx.x == 32) {
     for (int i = 0; i < kUnits; ++i) {
       mbar_init(bar(st.unit_full[i]), 1);
-      mbar_init(bar(st.unit_empty[i]), 1 + 1 + 4 + 2 * kGroupWarps);
+      mbar_init(bar(st.unit_empty[i]), 1 + 1 + kQueryWarps + 2 * kGroupWarps);
     }
     for (int i = 0; i < kKStages; ++i) {
       mbar_init(bar(st.k_full[i]), 2);
@@ -249,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kQStages; ++i) {
       mbar_init(bar(st.q_full[i]), 2);
-      mbar_init(bar(st.q_empty[i]), 1 + 2 * kGroupWarps);
+      mbar_init(bar(st.q_empty[i]), 1);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(bar(st.s_full[i >> 1][i & 1]), 1);
@@ -267,6 +283,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     st.abort_flag = 0;
     fence_barrier_init();
   }
+  for (int i = threadIdx.x; i < (kQStages + 1) * kExtraBytes / 16; i += kThreads) {
+    const bool ones = i >= kQStages * kExtraBytes / 16 && i < (kQStages * kExtraBytes + kExtraHalf) / 16;
+    *reinterpret_cast<uint4*>(base_ptr + (sLse - base) + 16 * i) = ones ? make_uint4(0x3f803f80u, 0x3f80u, 0u, 0u)
+                                                                        : make_uint4(0u, 0u, 0u, 0u);
+  }
+  fence_proxy_async();
   if (threadIdx.x == 64) {
     prefetch_tensormap(&kmap);
     prefetch_tensormap(&qmap);
@@ -468,6 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 1) {
     // -------------------------------------------------------------- MMA issue
     const uint64_t kdesc0 = smem_desc_sw128(sK, 16, 1024), qdesc0 = smem_desc_sw128(sQ, 16, 1024);
+    const uint64_t ldesc0 = extra_desc(sLse), ones = extra_desc(sOnes);
     RingAt<kKStages> rk;
     RingAt<kQStages> rq;
     RingAt<kUnits> ru;
@@ -490,7 +513,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!ok) break;
             tc_fence_after();
             mma_keys_e(st.tmem_base + t * 256 + rs.s * 128,
-                       kdesc0 + (rk.s * kStageBytes + t * kBlockBytes) / 16, qdesc0 + rq.s * (kQBytes / 16), idesc,
+                       kdesc0 + (rk.s * kStageBytes + t * kBlockBytes) / 16, qdesc0 + rq.s * (kQBytes / 16), ones,
+                       ldesc0 + rq.s * (kExtraBytes / 16), idesc,
                        bar(st.s_full[t][rs.s]));
           }
           if (!ok) break;
@@ -543,9 +567,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (!ok && *abort_flag == 0) *abort_flag = 1;
     copies_wait();  // none in flight when the block ends
-  } else if (warp >= 4 && warp < 8) {
+  } else if (warp >= 4 && warp < 4 + kQueryWarps) {
     // ---------------------------------------------------------------- queries
-    // The four warps take turns, a block each, so that four are on their way.
+    // The warps take turns, a block each, so that as many are on their way.
     RingAt<kQStages> rq;
     RingAt<kUnits> ru;
     const int log_g = __ffs(g) - 1;
@@ -557,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Unit a = st.units[ru.s];
       if (a.row < 0) break;
       const int32_t* path = p.path ? p.path + (size_t)a.row * p.max_path : nullptr;
-      for (int b = a.b0; b < a.b1; ++b, rq.next(), turn = (turn - 1) & 3) {
+      for (int b = a.b0; b < a.b1; ++b, rq.next(), turn = turn == 0 ? kQueryWarps - 1 : turn - 1) {
         if (turn != 0) continue;
         const int cols = block_cols(a, b, g), t0 = b * (kCols >> log_g);
         const bool box = !path && cols == kCols;
@@ -600,11 +624,22 @@ __global__ void __launch_bounds__(kThreads, 1)
               *reinterpret_cast<uint4*>(base_ptr + (sQ - base) + rq.s * kQBytes + swz128(c, lane & 7)) = v[k];
             }
           }
-          fence_proxy_async();
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          st.neg_lse[rq.s][32 * k + lane] = nl[k] == -INFINITY ? -INFINITY : -nl[k] * 1.4426950408889634f;
+        for (int k = 0; k < 4; ++k) {
+          // an infinite lse, of a query that saw nothing too, leaves weights of 0
+          const int c = 32 * k + lane;
+          const float x = nl[k] == -INFINITY ? -INFINITY : -nl[k] * p.inv_scale;
+          const __nv_bfloat16 hi = __float2bfloat16_rn(x);
+          const float r1 = x - __bfloat162float(hi);
+          const __nv_bfloat16 mid = __float2bfloat16_rn(r1);
+          const float r2 = r1 - __bfloat162float(mid);
+          const bool inf = fabsf(x) == INFINITY;
+          *reinterpret_cast<uint4*>(base_ptr + (sLse - base) + rq.s * kExtraBytes + 16 * c) =
+              make_uint4((uint32_t)__bfloat16_as_ushort(hi) | (inf ? 0u : (uint32_t)__bfloat16_as_ushort(mid) << 16),
+                         inf ? 0u : pack_bf16x2(r2, 0.f), 0u, 0u);
+        }
+        fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
           if (!box) mbar_arrive(bar(st.q_full[rq.s]));
@@ -633,7 +668,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tmem_s = st.tmem_base + t * 256 + group * 128 + ((uint32_t)((warp & 3) * 32) << 16);
     const uint64_t sc = pack_f32x2(p.scale_log2, p.scale_log2);
     RingAt<kKStages> rk;
-    RingAt<kQStages> rq;
     RingAt<kOldStages> ro;
     RingAt<kUnits> ru;
     uint32_t cnt = 0, sums = 0;  // blocks, sums handed over
@@ -663,16 +697,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (blocks > 0) rk.next();
         float total = 0.f;
         for (int b = a.b0; b < a.b1; ++b, ++cnt) {
-          const bool last_use = i >= a.pairs - 2;  // of the block of queries, by this group
-          if ((int)(cnt & 1) != group) {
-            if (i == a.pairs - 1) rq.next();
-            continue;
-          }
+          if ((int)(cnt & 1) != group) continue;
           const int cols = (block_cols(a, b, g) + 15) & ~15, t0 = b * (kCols / g);
-          ok = (i > 1 || wait_warp(bar(st.q_full[rq.s]), rq.parity)) && wait_warp(bar(st.s_full[t][group]), (cnt >> 1) & 1);
+          ok = wait_warp(bar(st.s_full[t][group]), (cnt >> 1) & 1);
           if (!ok) break;
           tc_fence_after();
-          const float* nl = st.neg_lse[rq.s];
           uint64_t sum[2] = {0, 0};
           // hidden from some query of the block: keys behind its first, or before the window of its last
           const int tl = min(t0 + kCols / g, a.n) - 1;
@@ -682,31 +711,35 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int hi = W == 0 ? kCols * kMaxGroup
                                   : (int)min(max((int64_t)j + W - C - t0, (int64_t)0), (int64_t)kCols) * g;
             uint32_t sv[32];
-#pragma unroll 1
-            for (int c = 0; c < cols; c += 32) {
-              if (c + 32 <= cols) {
+            if (plain && cols == kCols) {
+#pragma unroll
+              for (int c = 0; c < kCols; c += 32) {
                 tmem_ld32(tmem_s + c, sv);
                 tmem_ld_wait_for(sv);
-                if (plain) add_columns<32, false>(sv, nl + c, sc, 0, 0, sum);
-                else add_columns<32, true>(sv, nl + c, sc, lo - c, hi - c, sum);
-              } else {
-                tmem_ld16(tmem_s + c, sv);
-                tmem_ld_wait_for(sv);
-                if (plain) add_columns<16, false>(sv, nl + c, sc, 0, 0, sum);
-                else add_columns<16, true>(sv, nl + c, sc, lo - c, hi - c, sum);
+                add_columns<32, false>(sv, sc, 0, 0, sum);
+              }
+            } else {
+#pragma unroll 1
+              for (int c = 0; c < cols; c += 32) {
+                if (c + 32 <= cols) {
+                  tmem_ld32(tmem_s + c, sv);
+                  tmem_ld_wait_for(sv);
+                  if (plain) add_columns<32, false>(sv, sc, 0, 0, sum);
+                  else add_columns<32, true>(sv, sc, lo - c, hi - c, sum);
+                } else {
+                  tmem_ld16(tmem_s + c, sv);
+                  tmem_ld_wait_for(sv);
+                  if (plain) add_columns<16, false>(sv, sc, 0, 0, sum);
+                  else add_columns<16, true>(sv, sc, lo - c, hi - c, sum);
+                }
               }
             }
           }
           tc_fence_before();
           __syncwarp();
           mbar_arrive_e(bar(st.s_empty[t][group]));
-          if (last_use) {
-            mbar_arrive_e(bar(st.q_empty[rq.s]));
-            if (a.pairs == 1) mbar_arrive_e(bar(st.q_empty[rq.s]));  // for the other group, which does not read it
-          }
           const uint64_t both = add2(sum[0], sum[1]);
           total += lo_f32(both) + hi_f32(both);
-          if (i == a.pairs - 1) rq.next();
         }
         if (!ok) break;
         if (blocks > 1) {
