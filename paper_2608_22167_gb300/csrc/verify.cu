@@ -16,34 +16,34 @@
 // barrier every warp joins them all in the same order: all take the same
 // decisions, and nothing is sent back.
 //
-// Sums: 8 terms at a time in fp32, each group added to an fp32 pair by an exact
-// two-sum, joined in fp64 (a plain chain of fp32 additions loses 1e-6 of a peaked
-// distribution's tail). Exponentials by ex2.approx (2^-22).
+// Everything is fp32. Sums are pairs: 8 terms at a time, each group added by an
+// exact two-sum (a plain chain of additions loses 1e-6 of a peaked
+// distribution's tail; so does a maximum times log2(e) taken out of the
+// difference). Exponentials by ex2.approx (2^-22).
 #include "keep.cuh"
 
 namespace mcpu {
 
 namespace {
 
-constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32, kMaxCluster = 8;
+constexpr int kMaxThreads = 1024, kMinThreads = 256, kMaxWarps = kMaxThreads / 32, kMaxCluster = 8;
 constexpr int kMaxNodes = MCPU_MAX_TREE_NODES;
 constexpr float kLowest = -3.402823466e38f;  // a finite maximum to begin with: -inf logits weigh nothing against it
+constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.925963033500e-08f;  // log2(e) = the sum of both
 
 struct Stats {  // of a distribution: maximum, the lowest token that has it, sum of e^((l - max) / T)
   float max;
   int32_t at;
-  double sum;
+  float sum, low;  // the sum of both
 };
 
 struct VerifySmem {
   Stats stats[2][2][kMaxCluster * kMaxWarps];  // [turn][target, draft][warp of the cluster]
-  double sums[2][kMaxCluster * kMaxWarps];
+  float2 sums[2][kMaxCluster * kMaxWarps];
   uint64_t best[2][kMaxCluster * kMaxWarps];
-  int32_t parents[kMaxNodes], tokens[kMaxNodes];
-  float uniforms[kMaxNodes];
-  int32_t gone[kMaxNodes];                            // tokens of the rejected children of the node
+  int32_t gone[kMaxNodes];  // tokens of the rejected children of the node
   int32_t path[kMaxNodes];
-  double log_arg[kMaxNodes], log_sum[kMaxNodes];      // log p of what was emitted: the difference of arg and log sum
+  float log_arg[kMaxNodes], log_sum[kMaxNodes], log_low[kMaxNodes];  // log p of what was emitted: arg - log(sum + low)
 };
 
 // ----------------------------------------------------------- the cluster
@@ -57,17 +57,20 @@ __device__ __forceinline__ uint32_t cluster_size() {
   asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
   return r;
 }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  cluster_arrive();
+  cluster_wait();
 }
-// Address of a shared-memory object in block `rank` of the cluster.
+// Stores to a shared-memory object in block `rank` of the cluster.
 __device__ __forceinline__ uint32_t peer_addr(const void* p, uint32_t rank) {
   uint32_t a;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
   return a;
 }
-__device__ __forceinline__ void peer_store(uint32_t addr, uint64_t v) {
-  asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+__device__ __forceinline__ void peer_store(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
 }
 
 // ----------------------------------------------------- eight values of a row
@@ -84,33 +87,37 @@ template <typename T>
 constexpr uint32_t kNegInf = sizeof(T) == 4 ? 0xff800000u : 0xff80u;
 
 // The slice of the vocabulary that a block has, and how its threads share it:
-// eight neighbouring values a thread where all rows in use start at 16 bytes
-// (step 1), else eight a block apart, one coalesced load each (rows of an odd
-// number of tokens start anywhere).
+// eight neighbouring values a thread where every row starts at 16 bytes and
+// ends with a whole eight (kVec), else eight that are a block apart, one
+// coalesced load each.
+template <bool kVec>
 struct Slice {
-  int begin, end, step;
+  int begin, end;
   __device__ __forceinline__ int first(int k) const {  // first value of the thread's group k
-    return begin + (step == 1 ? 8 * (k * (int)blockDim.x + (int)threadIdx.x) : 8 * k * (int)blockDim.x + (int)threadIdx.x);
+    return begin + (kVec ? 8 * (k * (int)blockDim.x + (int)threadIdx.x) : 8 * k * (int)blockDim.x + (int)threadIdx.x);
   }
+  __device__ __forceinline__ int token(int at, int i) const { return at + (kVec ? i : i * (int)blockDim.x); }
   __device__ __forceinline__ int groups() const {
     return (end - begin + 8 * (int)blockDim.x - 1) / (8 * (int)blockDim.x);
   }
 };
 
-// Values at, at + step, .. of a row, `fill` (as bits of one) from `end` on.
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int at, const Slice& s, uint32_t fill, Raw<T>& r) {
-  if (s.step == 1 && at + 8 <= s.end) {
+// The group of a row that begins at value `at`; `fill` (as bits of one) past the end.
+template <typename T, bool kVec>
+__device__ __forceinline__ void load8(const T* row, int at, const Slice<kVec>& s, uint32_t fill, Raw<T>& r) {
+  if (kVec) {
+    const uint32_t two = sizeof(T) == 4 ? fill : fill << 16 | fill;
 #pragma unroll
     for (int k = 0; k < Raw<T>::kWords / 4; ++k) {
-      const uint4 x = __ldcg(reinterpret_cast<const uint4*>(row + at) + k);
+      uint4 x = make_uint4(two, two, two, two);
+      if (at < s.end) x = __ldcg(reinterpret_cast<const uint4*>(row + at) + k);
       r.w[4 * k] = x.x, r.w[4 * k + 1] = x.y, r.w[4 * k + 2] = x.z, r.w[4 * k + 3] = x.w;
     }
     return;
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int j = at + i * s.step;
+    const int j = s.token(at, i);
     uint32_t v = fill;
     if (j < s.end) v = sizeof(T) == 4 ? __ldcg(reinterpret_cast<const uint32_t*>(row) + j)
                                       : __ldcg(reinterpret_cast<const uint16_t*>(row) + j);
@@ -118,6 +125,13 @@ __device__ __forceinline__ void load8(const T* row, int at, const Slice& s, uint
     else if (i & 1) r.w[i >> 1] |= v << 16;
     else r.w[i >> 1] = v;
   }
+}
+
+// A slice of a row into L2, ahead of its use.
+template <typename T, bool kVec>
+__device__ __forceinline__ void prefetch_slice(const T* row, const Slice<kVec>& s) {
+  for (int i = s.begin + threadIdx.x * (128 / (int)sizeof(T)); i < s.end; i += blockDim.x * (128 / (int)sizeof(T)))
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
 }
 
 __device__ __forceinline__ float at_token(const __nv_bfloat16* x, int i) { return __bfloat162float(x[i]); }
@@ -129,26 +143,42 @@ __device__ __forceinline__ void add_exact(float& hi, float& lo, float x) {
   lo += (hi - (s - b)) + (x - b);
   hi = s;
 }
-
-// Calls f(first value, values of a) for this thread's groups of eight, as many
-// as 64 bytes loaded together.
-template <typename T, typename F>
-__device__ __forceinline__ void for_groups(const T* a, const Slice& s, F f) {
-  constexpr int kFlight = 8 / sizeof(T);
-  const int n = s.groups();
-  for (int k0 = 0; k0 < n; k0 += kFlight) {
-    Raw<T> r[kFlight];
+__device__ __forceinline__ void warp_add_exact(float& hi, float& lo) {
 #pragma unroll
-    for (int e = 0; e < kFlight; ++e) load8(a, k0 + e < n ? s.first(k0 + e) : s.end, s, kNegInf<T>, r[e]);
-#pragma unroll
-    for (int e = 0; e < kFlight; ++e)
-      if (k0 + e < n) f(s.first(k0 + e), r[e]);
+  for (int o = 16; o > 0; o >>= 1) {
+    const float oh = __shfl_xor_sync(0xffffffffu, hi, o), ol = __shfl_xor_sync(0xffffffffu, lo, o);
+    lo += ol;
+    add_exact(hi, lo, oh);  // (the error is exact: both sides of a pair get the same bits)
   }
 }
+__device__ __forceinline__ void warp_max(float& m, int& at) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float om = __shfl_xor_sync(0xffffffffu, m, o);
+    const int oat = __shfl_xor_sync(0xffffffffu, at, o);
+    if (om > m || (om == m && oat < at)) m = om, at = oat;
+  }
+}
+__device__ __forceinline__ uint64_t warp_best(uint64_t key) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const uint64_t other = __shfl_xor_sync(0xffffffffu, (unsigned long long)key, o);
+    if (other > key) key = other;
+  }
+  return key;
+}
 
+// e^((v - m) / T) of the two values 2 i, 2 i + 1 of a group, times f; c = log2(e) / T
 template <typename T>
-__global__ void __launch_bounds__(kMaxThreads, 2) verify_kernel(const VerifyParams p) {
+__device__ __forceinline__ float2 weights2(const Raw<T>& v, int i, float m, float c) {
+  return make_float2(ex2_approx((v.get(2 * i) - m) * c), ex2_approx((v.get(2 * i + 1) - m) * c));
+}
+
+template <typename T, bool kVec>
+__global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyParams p, int ahead) {
+  constexpr int kFlight = kVec ? 8 / sizeof(T) : 2;  // groups loaded together
   __shared__ VerifySmem s;
+  cluster_arrive();  // (every block of the cluster is there before the first store into its memory)
   grid_dep_launch();
   grid_dep_wait();
   const uint32_t rank = cluster_rank(), size = cluster_size();
@@ -156,240 +186,281 @@ __global__ void __launch_bounds__(kMaxThreads, 2) verify_kernel(const VerifyPara
   const int parts = (int)size * warps, mine = (int)rank * warps + warp;
   const int r = blockIdx.x / size, V = p.vocab;
   const int q0 = p.qsl[r], L = p.qsl[r + 1] - q0;
+  const float heat = p.temperature ? p.temperature[r] : 0.f;
   int32_t bits = 0;
   if (p.qsl[0] != 0 || p.qsl[p.num_seqs] != p.total_q || q0 < 0 || L < 0 || L > p.total_q - q0) bits = kStatusBadLengths;
   else if (L > kMaxNodes) bits = kStatusUnsupportedRow;
-  const float heat = p.temperature ? p.temperature[r] : 0.f;
-  const bool greedy = heat == 0.f;
+  const bool greedy = heat == 0.f, walks = !bits && L > 0;
   bool bad = !greedy && !(heat >= 1e-20f && heat <= 1e20f);
-  const bool walks = !bits && L > 0;
   int cur = 0, len = walks ? 1 : 0, next = -1;
-  if (walks && !bad) {  // the same in all blocks of the cluster
-    for (int i = threadIdx.x; i < L; i += blockDim.x) {
-      s.parents[i] = p.parents[q0 + i];
-      s.tokens[i] = p.tokens[q0 + i];
-      s.uniforms[i] = greedy ? 0.f : p.uniforms[q0 + i];
-    }
-    if (threadIdx.x == 0) s.path[0] = 0;
-    // before the first store into another block's memory all have to be there
-    cluster_sync();
-  }
-  const double T_inv = greedy ? 1.0 : 1.0 / (double)heat;
-  const float c = (float)(1.4426950408889634 * T_inv);
+  const float div = greedy ? 1.f : heat;
+  float c = __fdividef(kLog2e, div);
+  c += __fdividef(fmaf(-c, div, kLog2e) + kLog2eLow, div);  // log2(e) / T, rounded once
   const int per = (V + 8 * (int)size - 1) / (8 * (int)size) * 8;
-  Slice slice;
+  Slice<kVec> slice;
   slice.begin = min(V, (int)rank * per);
   slice.end = min(V, slice.begin + per);
-  uint32_t turn = 0;  // of the exchange buffers
+  const int n = slice.groups();
   const float* noise = greedy ? nullptr : p.noise + (size_t)r * p.noise_stride;
-  auto whole = [](const void* row) { return (reinterpret_cast<uintptr_t>(row) & 15) == 0; };
-
-  // e^((l - max) / T) relative to 2 ulp, for single tokens
-  auto weight = [&](const T* row, const Stats& st, int token) -> double {
-    const double x = ((double)at_token(row, token) - (double)st.max) * T_inv;
-    const float hi = (float)fmax(x, -200.0);
-    return (double)expf(hi) * (1.0 + (fmax(x, -200.0) - (double)hi));
-  };
+  uint32_t turn = 0;  // of the exchange buffers
+  cluster_wait();
+  if (walks && !bad && !greedy && ahead) prefetch_slice(noise, slice);
 
   while (walks && !bad) {
     const T* x = static_cast<const T*>(p.logits) + (size_t)(q0 + cur) * p.logits_stride;
     const T* y = p.draft && !greedy ? static_cast<const T*>(p.draft) + (size_t)(q0 + cur) * p.draft_stride : nullptr;
-    slice.step = whole(x) && whole(y) && whole(noise) ? 1 : (int)blockDim.x;
+    // the nodes after this one, up to 32: their loads are on their way during the pass
+    const int w1 = (cur + 1) & ~31;
+    int up = -1, token = -1;
+    float u = 0.f;
+    if (w1 + lane < L) {
+      up = p.parents[q0 + w1 + lane];
+      token = p.tokens[q0 + w1 + lane];
+      if (!greedy) u = p.uniforms[q0 + w1 + lane];
+    }
     // ---- maximum and sum of the node's distributions
     Stats st[2];
-    const int dists = y ? 2 : 1;
+    float lx = 0.f, ly = 0.f;  // the child's own logits
+    bool kid = false;
 #pragma unroll 1
-    for (int d = 0; d < dists; ++d) {
+    for (int d = 0; d < (y ? 2 : 1); ++d) {
+      const T* row = d ? y : x;
       float m = kLowest, z = 0.f, zl = 0.f;
       int at = 0x7fffffff;
-      for_groups(d ? y : x, slice, [&](int j, const Raw<T>& v) {
-        float top = v.get(0);
+#pragma unroll 1
+      for (int k0 = 0; k0 < n; k0 += kFlight) {
+        Raw<T> v[kFlight];
 #pragma unroll
-        for (int i = 1; i < 8; ++i) top = fmaxf(top, v.get(i));
-        if (top > m || (top == m && at == 0x7fffffff)) {
-          const float f = exp2f((m - top) * c);
-          z *= f;
-          zl *= f;
-          m = top;
+        for (int e = 0; e < kFlight; ++e) load8(row, slice.first(k0 + e), slice, kNegInf<T>, v[e]);
 #pragma unroll
-          for (int i = 7; i >= 0; --i)
-            if (v.get(i) == top) at = j + i * slice.step;
+        for (int e = 0; e < kFlight; ++e) {
+          float top = fmaxf(v[e].get(0), v[e].get(1));
+#pragma unroll
+          for (int i = 2; i < 8; i += 2) top = fmax3(top, v[e].get(i), v[e].get(i + 1));
+          if (top > m) {
+            const float f = ex2_approx((m - top) * c);
+            z *= f;
+            zl *= f;
+            m = top;
+            if (greedy) {
+#pragma unroll
+              for (int i = 7; i >= 0; --i)
+                if (v[e].get(i) == top) at = slice.token(slice.first(k0 + e), i);
+            }
+          }
+          float2 sum = weights2(v[e], 0, m, c);
+#pragma unroll
+          for (int i = 1; i < 4; ++i) {
+            const float2 w = weights2(v[e], i, m, c);
+            sum.x += w.x;
+            sum.y += w.y;
+          }
+          add_exact(z, zl, sum.x + sum.y);
         }
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += ex2_approx((v.get(i) - m) * c);
-        add_exact(z, zl, sum);
-      });
-      float wm = m;
-      int wat = at;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, wm, o);
-        const int oat = __shfl_xor_sync(0xffffffffu, wat, o);
-        if (om > wm || (om == wm && oat < wat)) wm = om, wat = oat;
       }
-      double wz = ((double)z + (double)zl) * (double)exp2f((m - wm) * c);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) wz += __shfl_xor_sync(0xffffffffu, wz, o);
+      if (d == 0) {
+        kid = up == cur && w1 + lane > cur && token >= 0 && token < V && len < p.max_accept;
+        const uint32_t kids = __ballot_sync(0xffffffffu, kid);
+        if (kid) {
+          lx = at_token(x, token);
+          if (y) ly = at_token(y, token);
+        }
+        if (ahead && kids) {  // the likeliest node to come
+          const size_t child = q0 + w1 + __ffs(kids) - 1;
+          prefetch_slice(static_cast<const T*>(p.logits) + child * p.logits_stride, slice);
+          if (y) prefetch_slice(static_cast<const T*>(p.draft) + child * p.draft_stride, slice);
+        }
+      }
+      float wm = m;
+      warp_max(wm, at);
+      const float f = ex2_approx((m - wm) * c);
+      z *= f;
+      zl *= f;
+      warp_add_exact(z, zl);
       if (lane < (int)size) {
         const uint32_t to = peer_addr(&s.stats[turn][d][mine], lane);
-        peer_store(to, (uint64_t)__float_as_uint(wm) | (uint64_t)(uint32_t)wat << 32);
-        peer_store(to + 8, (uint64_t)__double_as_longlong(wz));
+        peer_store(to, __float_as_uint(wm), (uint32_t)at);
+        peer_store(to + 8, __float_as_uint(z), __float_as_uint(zl));
       }
     }
     cluster_sync();
-#pragma unroll 1
-    for (int d = 0; d < dists; ++d) {
-      Stats b{kLowest, 0x7fffffff, 0.0};
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      if (d == 1 && !y) break;
+      float m = kLowest, z = 0.f, zl = 0.f;
+      int at = 0x7fffffff;
       for (int i = lane; i < parts; i += 32) {
         const Stats o = s.stats[turn][d][i];
-        if (o.max > b.max || (o.max == b.max && o.at < b.at)) b.max = o.max, b.at = o.at;
+        if (o.max > m || (o.max == m && o.at < at)) m = o.max, at = o.at;
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, b.max, o);
-        const int oat = __shfl_xor_sync(0xffffffffu, b.at, o);
-        if (om > b.max || (om == b.max && oat < b.at)) b.max = om, b.at = oat;
-      }
+      warp_max(m, at);
       for (int i = lane; i < parts; i += 32) {
         const Stats o = s.stats[turn][d][i];
-        b.sum += o.sum * (double)exp2f((o.max - b.max) * c);
+        const float f = ex2_approx((o.max - m) * c);
+        add_exact(z, zl, o.sum * f);
+        zl += o.low * f;
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) b.sum += __shfl_xor_sync(0xffffffffu, b.sum, o);
-      st[d] = b;
-      bad |= !(b.sum > 0.0 && b.sum < 1e300);
+      warp_add_exact(z, zl);
+      st[d] = Stats{m, at, z, zl};
+      bad |= !(z > 0.f && z < 3e38f);  // no token, NaN or +inf
     }
     turn ^= 1;
     if (bad) break;
 
     // ---- the children, in ascending order (every warp alike)
+    const float ip = 1.f / (st[0].sum + st[0].low), iq = y ? 1.f / (st[1].sum + st[1].low) : 1.f;
     int went = -1, rejected = 0;
-    double mass = 1.0, gone = 0.0;
-    if (len < p.max_accept) {
-      for (int w0 = cur + 1 & ~31; w0 < L && went < 0; w0 += 32) {
-        const int i = w0 + lane;
-        const int token = i < L ? s.tokens[i] : -1;
-        const bool kid = i > cur && i < L && s.parents[i] == cur && token >= 0 && token < V;
-        uint32_t kids = __ballot_sync(0xffffffffu, kid);
-        if (greedy) {
-          const uint32_t hit = __ballot_sync(0xffffffffu, kid && token == st[0].at);
-          if (hit) went = w0 + __ffs(hit) - 1;
+    float mass = 1.f, gone = 0.f;
+#pragma unroll 1
+    for (int w0 = w1; w0 < L && went < 0 && len < p.max_accept; w0 += 32) {
+      if (w0 > w1) {  // trees of more than 32 nodes
+        up = token = -1;
+        if (w0 + lane < L) {
+          up = p.parents[q0 + w0 + lane];
+          token = p.tokens[q0 + w0 + lane];
+          if (!greedy) u = p.uniforms[q0 + w0 + lane];
+        }
+        kid = up == cur && token >= 0 && token < V;
+        if (kid) {
+          lx = at_token(x, token);
+          if (y) ly = at_token(y, token);
+        }
+      }
+      uint32_t kids = __ballot_sync(0xffffffffu, kid);
+      if (greedy) {
+        const uint32_t hit = __ballot_sync(0xffffffffu, kid && token == st[0].at);
+        if (hit) went = w0 + __ffs(hit) - 1;
+        continue;
+      }
+      const float px = ex2_approx((lx - st[0].max) * c) * ip, qx = y ? ex2_approx((ly - st[1].max) * c) * iq : 1.f;
+#pragma unroll 1
+      for (; kids && went < 0; kids &= kids - 1) {
+        const int l = __ffs(kids) - 1;
+        const int kt = __shfl_sync(0xffffffffu, token, l);
+        const float kp = __shfl_sync(0xffffffffu, px, l), kq = __shfl_sync(0xffffffffu, qx, l);
+        const float ku = __shfl_sync(0xffffffffu, u, l);
+        float rest = kp;
+        if (y) {
+          rest = fmaxf(kp - gone * kq, 0.f);
+        } else {
+          bool again = false;
+          for (int e = lane; e < rejected; e += 32) again |= s.gone[e] == kt;
+          if (__any_sync(0xffffffffu, again)) rest = 0.f;
+        }
+        if (ku * mass * kq < rest) {
+          went = w0 + l;
+          break;
+        }
+        ++rejected;
+        if (!y) {
+          mass = fmaxf(mass - rest, 0.f);
+          __syncwarp();
+          s.gone[rejected - 1] = kt;  // (every thread of the block writes the same)
+          __syncwarp();
           continue;
         }
-        const double px = kid ? weight(x, st[0], token) / st[0].sum : 0.0;
-        const double qx = kid && y ? weight(y, st[1], token) / st[1].sum : 1.0;
-        for (; kids && went < 0; kids &= kids - 1) {
-          const int l = __ffs(kids) - 1;
-          const int kt = __shfl_sync(0xffffffffu, token, l);
-          const double kp = __shfl_sync(0xffffffffu, px, l), kq = __shfl_sync(0xffffffffu, qx, l);
-          const double u = (double)s.uniforms[w0 + l];
-          if (!y) {
-            bool again = false;
-            for (int e = lane; e < rejected; e += 32) again |= s.gone[e] == kt;
-            const double rest = __any_sync(0xffffffffu, again) ? 0.0 : kp;
-            if (u * mass < rest) {
-              went = w0 + l;
-            } else {
-              mass = fmax(mass - rest, 0.0);
-              __syncwarp();
-              s.gone[rejected++] = kt;  // (every thread of the block writes the same)
-              __syncwarp();
-            }
-            continue;
-          }
-          if (u * mass * kq < fmax(kp - gone * kq, 0.0)) {
-            went = w0 + l;
-            break;
-          }
-          gone += mass;
-          ++rejected;
-          // the residual's mass, if another child is to be tried
-          bool more = (kids & (kids - 1)) != 0;
-          for (int v0 = w0 + 32; v0 < L && !more; v0 += 32) {
-            const int j = v0 + lane;
-            more = __any_sync(0xffffffffu, j < L && s.parents[j] == cur && s.tokens[j] >= 0 && s.tokens[j] < V);
-          }
-          if (!more) break;
-          const float ip = (float)(1.0 / st[0].sum), iq = (float)(gone / st[1].sum);
-          float z = 0.f, zl = 0.f;
-          for_groups(x, slice, [&](int j, const Raw<T>& v) {
-            Raw<T> d;
-            load8(y, j, slice, kNegInf<T>, d);
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              sum += fmaxf(ex2_approx((v.get(e) - st[0].max) * c) * ip - ex2_approx((d.get(e) - st[1].max) * c) * iq, 0.f);
-            add_exact(z, zl, sum);
-          });
-          double wz = (double)z + (double)zl;
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) wz += __shfl_xor_sync(0xffffffffu, wz, o);
-          if (lane < (int)size) peer_store(peer_addr(&s.sums[turn][mine], lane), (uint64_t)__double_as_longlong(wz));
-          cluster_sync();
-          mass = 0.0;
-          for (int e = lane; e < parts; e += 32) mass += s.sums[turn][e];
-#pragma unroll
-          for (int o = 16; o > 0; o >>= 1) mass += __shfl_xor_sync(0xffffffffu, mass, o);
-          turn ^= 1;
+        gone += mass;
+        // the residual's mass, if another child is to be tried
+        bool more = (kids & (kids - 1)) != 0;
+        for (int v0 = w0 + 32; v0 < L && !more; v0 += 32) {
+          const int i = v0 + lane;
+          const int t = i < L && p.parents[q0 + i] == cur ? p.tokens[q0 + i] : -1;
+          more = __any_sync(0xffffffffu, t >= 0 && t < V);
         }
+        if (!more) break;
+        const float fq = gone * iq;
+        float z = 0.f, zl = 0.f;
+#pragma unroll 1
+        for (int k = 0; k < n; ++k) {
+          Raw<T> a, b;
+          load8(x, slice.first(k), slice, kNegInf<T>, a);
+          load8(y, slice.first(k), slice, kNegInf<T>, b);
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 wp = weights2(a, i, st[0].max, c), wq = weights2(b, i, st[1].max, c);
+            sum += fmaxf(wp.x * ip - wq.x * fq, 0.f) + fmaxf(wp.y * ip - wq.y * fq, 0.f);
+          }
+          add_exact(z, zl, sum);
+        }
+        warp_add_exact(z, zl);
+        if (lane < (int)size) peer_store(peer_addr(&s.sums[turn][mine], lane), __float_as_uint(z), __float_as_uint(zl));
+        cluster_sync();
+        z = zl = 0.f;
+        for (int e = lane; e < parts; e += 32) {
+          add_exact(z, zl, s.sums[turn][e].x);
+          zl += s.sums[turn][e].y;
+        }
+        warp_add_exact(z, zl);
+        mass = z + zl;
+        turn ^= 1;
       }
     }
 
     // ---- no child: the race for the next token
-    int out = went >= 0 ? s.tokens[went] : st[0].at;
+    int out = went >= 0 ? p.tokens[q0 + went] : st[0].at;
     if (went < 0 && !greedy) {
-      const float ip = (float)(1.0 / st[0].sum), iq = y ? (float)(gone / st[1].sum) : 0.f;
+      float fq = gone * iq;
+      int lost = y ? 0 : rejected;
       out = 0x7fffffff;
 #pragma unroll 1
-      for (int tries = 0; tries < 2 && out == 0x7fffffff; ++tries) {
+      for (int tries = 0; tries < 2 && out == 0x7fffffff; ++tries, fq = 0.f, lost = 0) {
         float best = 0.f;
         int best_at = 0x7fffffff;
-        for_groups(x, slice, [&](int j, const Raw<T>& v) {
+#pragma unroll 1
+        for (int k = 0; k < n; ++k) {
+          const int at = slice.first(k);
+          Raw<T> a, b;
           Raw<float> e;
-          load8(noise, j, slice, 0x3f800000u, e);
-          float rest[8];
+          load8(noise, at, slice, 0x3f800000u, e);
+          load8(x, at, slice, kNegInf<T>, a);
+          if (fq > 0.f) load8(y, at, slice, kNegInf<T>, b);
+          float v[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) rest[i] = ex2_approx((v.get(i) - st[0].max) * c) * ip;
-          if (iq > 0.f && tries == 0) {
-            Raw<T> d;
-            load8(y, j, slice, kNegInf<T>, d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) rest[i] -= ex2_approx((d.get(i) - st[1].max) * c) * iq;
+          for (int i = 0; i < 4; ++i) {
+            const float2 w = weights2(a, i, st[0].max, c);
+            v[2 * i] = w.x * ip;
+            v[2 * i + 1] = w.y * ip;
           }
+          if (fq > 0.f) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float a = rest[i] > 0.f ? __fdiv_rn(rest[i], e.get(i)) : 0.f;
-            if (a > best) {
-              bool lost = false;
-              if (!y && tries == 0)
-                for (int k = 0; k < rejected; ++k) lost |= s.gone[k] == j + i * slice.step;
-              if (!lost) best = a, best_at = j + i * slice.step;
+            for (int i = 0; i < 4; ++i) {
+              const float2 w = weights2(b, i, st[1].max, c);
+              v[2 * i] -= w.x * fq;
+              v[2 * i + 1] -= w.y * fq;
             }
           }
-        });
-        uint64_t key = (uint64_t)__float_as_uint(best) << 32 | (uint32_t)~best_at;
+          float top = 0.f;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          const uint64_t other = __shfl_xor_sync(0xffffffffu, (unsigned long long)key, o);
-          if (other > key) key = other;
+          for (int i = 0; i < 8; ++i) {
+            v[i] = __fdividef(v[i], e.get(i));
+            top = fmaxf(top, v[i]);
+          }
+          if (!(top > best)) continue;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (!(v[i] > best)) continue;
+            const int t = slice.token(at, i);
+            bool out_of_race = false;
+#pragma unroll 1
+            for (int j = 0; j < lost; ++j) out_of_race |= s.gone[j] == t;
+            if (!out_of_race) best = v[i], best_at = t;
+          }
         }
-        if (lane < (int)size) peer_store(peer_addr(&s.best[turn][mine], lane), key);
+        uint64_t key = warp_best((uint64_t)__float_as_uint(best) << 32 | (uint32_t)~best_at);
+        if (lane < (int)size) peer_store(peer_addr(&s.best[turn][mine], lane), (uint32_t)key, (uint32_t)(key >> 32));
         cluster_sync();
         key = 0;
         for (int e = lane; e < parts; e += 32) key = max(key, s.best[turn][e]);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          const uint64_t other = __shfl_xor_sync(0xffffffffu, (unsigned long long)key, o);
-          if (other > key) key = other;
-        }
+        key = warp_best(key);
         turn ^= 1;
         if (key >> 32) out = (int)~(uint32_t)key;
       }
     }
     if (threadIdx.x == 0 && rank == 0) {
-      if (out < V) s.log_arg[len - 1] = ((double)at_token(x, out) - (double)st[0].max) * T_inv;
+      s.log_arg[len - 1] = out < V ? (at_token(x, out) - st[0].max) / div : 0.f;
       s.log_sum[len - 1] = st[0].sum;
+      s.log_low[len - 1] = st[0].low;
       if (went >= 0) s.path[len] = went;
     }
     if (went < 0) {
@@ -406,7 +477,9 @@ __global__ void __launch_bounds__(kMaxThreads, 2) verify_kernel(const VerifyPara
     p.path[(size_t)r * p.max_accept + i] = i < len ? (i == 0 ? 0 : s.path[i]) : -1;
     if (p.logprobs) {
       float v = 0.f;
-      if (i < len) v = bad && i == len - 1 ? __int_as_float(0x7fffffff) : (float)(s.log_arg[i] - log(s.log_sum[i]));
+      if (i < len)
+        v = bad && i == len - 1 ? __int_as_float(0x7fffffff)
+                                : s.log_arg[i] - (logf(s.log_sum[i]) + s.log_low[i] / s.log_sum[i]);
       p.logprobs[(size_t)r * p.max_accept + i] = v;
     }
   }
@@ -421,10 +494,16 @@ __global__ void __launch_bounds__(kMaxThreads, 2) verify_kernel(const VerifyPara
 }  // namespace
 
 cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_t stream) {
-  // blocks a row: as many as two per SM give, and a group of eight logits for each thread
-  int size = 1;
-  while (size < kMaxCluster && 2 * size * p.num_seqs <= 2 * sms && 2 * size * kMaxThreads * 8 <= p.vocab) size *= 2;
-  const int threads = p.num_seqs > 2 * sms ? kMaxThreads / 2 : kMaxThreads;
+  // up to one block per SM large ones, several a row; more rows share the SMs in smaller ones
+  int size = 1, threads = p.num_seqs <= sms ? kMaxThreads : p.num_seqs <= 2 * sms ? kMaxThreads / 2 : kMinThreads;
+  while (size < kMaxCluster && 2 * size * p.num_seqs <= sms && 2 * size * kMinThreads * 8 <= p.vocab) size *= 2;
+  while (threads > kMinThreads && size * threads * 4 > p.vocab) threads /= 2;
+  const size_t bytes = fp32 ? 4 : 2;
+  auto whole = [&](const void* q, int64_t stride, size_t b) {
+    return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && stride * b % 16 == 0);
+  };
+  const bool vec = p.vocab % 8 == 0 && whole(p.logits, p.logits_stride, bytes) &&
+                   whole(p.draft, p.draft_stride, bytes) && whole(p.noise, p.noise_stride, 4);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(size * p.num_seqs);
   cfg.blockDim = dim3(threads);
@@ -437,7 +516,10 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, fp32 ? verify_kernel<float> : verify_kernel<__nv_bfloat16>, p);
+  const int ahead = p.num_seqs <= sms;
+  if (fp32)
+    return cudaLaunchKernelEx(&cfg, vec ? verify_kernel<float, true> : verify_kernel<float, false>, p, ahead);
+  return cudaLaunchKernelEx(&cfg, vec ? verify_kernel<__nv_bfloat16, true> : verify_kernel<__nv_bfloat16, false>, p, ahead);
 }
 
 }  // namespace mcpu
