@@ -26,7 +26,7 @@ namespace mcpu {
 
 namespace {
 
-constexpr int kMaxThreads = 1024, kMinThreads = 256, kMaxWarps = kMaxThreads / 32, kMaxCluster = 8;
+constexpr int kMaxThreads = 512, kMinThreads = 256, kMaxWarps = kMaxThreads / 32, kMaxCluster = 8;
 constexpr int kMaxNodes = MCPU_MAX_TREE_NODES;
 constexpr float kLowest = -3.402823466e38f;  // a finite maximum to begin with: -inf logits weigh nothing against it
 constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.925963033500e-08f;  // log2(e) = the sum of both
@@ -43,7 +43,8 @@ struct VerifySmem {
   uint64_t best[2][kMaxCluster * kMaxWarps];
   int32_t gone[kMaxNodes];  // tokens of the rejected children of the node
   int32_t path[kMaxNodes];
-  float log_arg[kMaxNodes], log_sum[kMaxNodes], log_low[kMaxNodes];  // log p of what was emitted: arg - log(sum + low)
+  int32_t out[kMaxNodes];    // what was emitted after each node of the path,
+  Stats node[kMaxNodes];     // and that node's distribution
 };
 
 // ----------------------------------------------------------- the cluster
@@ -86,50 +87,68 @@ struct Raw {  // as they are loaded
 template <typename T>
 constexpr uint32_t kNegInf = sizeof(T) == 4 ? 0xff800000u : 0xff80u;
 
-// The slice of the vocabulary that a block has, and how its threads share it:
-// eight neighbouring values a thread where every row starts at 16 bytes and
-// ends with a whole eight (kVec), else eight that are a block apart, one
-// coalesced load each.
-template <bool kVec>
+// The slice of the vocabulary that a block has; thread t's group k is the eight
+// values from begin + 8 (k threads + t) on.
 struct Slice {
-  int begin, end;
-  __device__ __forceinline__ int first(int k) const {  // first value of the thread's group k
-    return begin + (kVec ? 8 * (k * (int)blockDim.x + (int)threadIdx.x) : 8 * k * (int)blockDim.x + (int)threadIdx.x);
-  }
-  __device__ __forceinline__ int token(int at, int i) const { return at + (kVec ? i : i * (int)blockDim.x); }
+  int begin, end, vocab;
+  __device__ __forceinline__ int first(int k) const { return begin + 8 * (k * (int)blockDim.x + (int)threadIdx.x); }
   __device__ __forceinline__ int groups() const {
     return (end - begin + 8 * (int)blockDim.x - 1) / (8 * (int)blockDim.x);
   }
 };
 
-// The group of a row that begins at value `at`; `fill` (as bits of one) past the end.
-template <typename T, bool kVec>
-__device__ __forceinline__ void load8(const T* row, int at, const Slice<kVec>& s, uint32_t fill, Raw<T>& r) {
-  if (kVec) {
-    const uint32_t two = sizeof(T) == 4 ? fill : fill << 16 | fill;
+// The eight values of a row from `at` on; `fill` (as bits of one) past the end.
+// kWhole: every row starts at 16 bytes and its length is a multiple of 8. Else
+// the row starts anywhere: one more vector, and shifts by the row's offset (the
+// same for all threads); where that vector would leave the row, one by one.
+template <bool kWhole, typename T>
+__device__ __forceinline__ void load8(const T* row, int at, const Slice& s, uint32_t fill, Raw<T>& r) {
+  constexpr int kWords = Raw<T>::kWords;
+  const uint32_t two = sizeof(T) == 4 ? fill : fill << 16 | fill;
+  if (kWhole) {
 #pragma unroll
-    for (int k = 0; k < Raw<T>::kWords / 4; ++k) {
+    for (int k = 0; k < kWords / 4; ++k) {
       uint4 x = make_uint4(two, two, two, two);
       if (at < s.end) x = __ldcg(reinterpret_cast<const uint4*>(row + at) + k);
       r.w[4 * k] = x.x, r.w[4 * k + 1] = x.y, r.w[4 * k + 2] = x.z, r.w[4 * k + 3] = x.w;
     }
     return;
   }
+  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row + at) & 15);
+  const bool inside = at + 8 + (off ? (int)((16 - off) / sizeof(T)) : 0) <= s.vocab && (off == 0 || at > 0);
+  if (at < s.end && inside) {
+    const uint4* v = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row + at) - off);
+    uint32_t w[kWords + 4];
+#pragma unroll
+    for (int k = 0; k <= kWords / 4; ++k) {
+      if (k == kWords / 4 && off == 0) continue;
+      const uint4 x = v[k];  // (through L1: the neighbour's vector too)
+      w[4 * k] = x.x, w[4 * k + 1] = x.y, w[4 * k + 2] = x.z, w[4 * k + 3] = x.w;
+    }
+    // words first, then the half word
+#pragma unroll
+    for (int k = 0; k < kWords + 2; ++k) w[k] = off & 8 ? w[k + 2] : w[k];
+#pragma unroll
+    for (int k = 0; k < kWords + 1; ++k) w[k] = off & 4 ? w[k + 1] : w[k];
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) r.w[k] = sizeof(T) == 2 && off & 2 ? __funnelshift_r(w[k], w[k + 1], 16) : w[k];
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kWords; ++k) r.w[k] = two;
+  if (at >= s.end) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int j = s.token(at, i);
-    uint32_t v = fill;
-    if (j < s.end) v = sizeof(T) == 4 ? __ldcg(reinterpret_cast<const uint32_t*>(row) + j)
-                                      : __ldcg(reinterpret_cast<const uint16_t*>(row) + j);
-    if (sizeof(T) == 4) r.w[i] = v;
-    else if (i & 1) r.w[i >> 1] |= v << 16;
-    else r.w[i >> 1] = v;
+    if (at + i >= s.vocab) break;
+    if (sizeof(T) == 4) r.w[i] = reinterpret_cast<const uint32_t*>(row)[at + i];
+    else if (i & 1) r.w[i >> 1] = (r.w[i >> 1] & 0xffffu) | (uint32_t)reinterpret_cast<const uint16_t*>(row)[at + i] << 16;
+    else r.w[i >> 1] = (r.w[i >> 1] & 0xffff0000u) | reinterpret_cast<const uint16_t*>(row)[at + i];
   }
 }
 
 // A slice of a row into L2, ahead of its use.
-template <typename T, bool kVec>
-__device__ __forceinline__ void prefetch_slice(const T* row, const Slice<kVec>& s) {
+template <typename T>
+__device__ __forceinline__ void prefetch_slice(const T* row, const Slice& s) {
   for (int i = s.begin + threadIdx.x * (128 / (int)sizeof(T)); i < s.end; i += blockDim.x * (128 / (int)sizeof(T)))
     asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
 }
@@ -168,15 +187,24 @@ __device__ __forceinline__ uint64_t warp_best(uint64_t key) {
   return key;
 }
 
-// e^((v - m) / T) of the two values 2 i, 2 i + 1 of a group, times f; c = log2(e) / T
+// Packed: e^((v - m) / T) of the values 2 i, 2 i + 1 of a group, from -m and c = log2(e) / T twice each.
 template <typename T>
-__device__ __forceinline__ float2 weights2(const Raw<T>& v, int i, float m, float c) {
-  return make_float2(ex2_approx((v.get(2 * i) - m) * c), ex2_approx((v.get(2 * i + 1) - m) * c));
+__device__ __forceinline__ uint64_t weights2(const Raw<T>& v, int i, uint64_t neg_m, uint64_t c) {
+  uint64_t x = add2(pack_f32x2(v.get(2 * i), v.get(2 * i + 1)), neg_m);
+  asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(x) : "l"(c));
+  return pack_f32x2(ex2_approx(lo_f32(x)), ex2_approx(hi_f32(x)));
 }
 
-template <typename T, bool kVec>
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+template <typename T, bool kWhole>
 __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyParams p, int ahead) {
-  constexpr int kFlight = kVec ? 8 / sizeof(T) : 2;  // groups loaded together
+  constexpr int kFlight = 8 / sizeof(T);               // groups of a row loaded together
+  constexpr int kRace = (kWhole ? 8 : 4) / sizeof(T);  // and of the two or three rows of the last passes
   __shared__ VerifySmem s;
   cluster_arrive();  // (every block of the cluster is there before the first store into its memory)
   grid_dep_launch();
@@ -196,8 +224,10 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
   const float div = greedy ? 1.f : heat;
   float c = __fdividef(kLog2e, div);
   c += __fdividef(fmaf(-c, div, kLog2e) + kLog2eLow, div);  // log2(e) / T, rounded once
+  const uint64_t cc = pack_f32x2(c, c);
   const int per = (V + 8 * (int)size - 1) / (8 * (int)size) * 8;
-  Slice<kVec> slice;
+  Slice slice;
+  slice.vocab = V;
   slice.begin = min(V, (int)rank * per);
   slice.end = min(V, slice.begin + per);
   const int n = slice.groups();
@@ -227,36 +257,53 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
       const T* row = d ? y : x;
       float m = kLowest, z = 0.f, zl = 0.f;
       int at = 0x7fffffff;
-#pragma unroll 1
-      for (int k0 = 0; k0 < n; k0 += kFlight) {
-        Raw<T> v[kFlight];
+      auto load = [&](Raw<T>(&v)[kFlight], int k0) {
 #pragma unroll
-        for (int e = 0; e < kFlight; ++e) load8(row, slice.first(k0 + e), slice, kNegInf<T>, v[e]);
+        for (int e = 0; e < kFlight; ++e) load8<kWhole>(row, slice.first(k0 + e), slice, kNegInf<T>, v[e]);
+      };
+      auto add = [&](const Raw<T>(&v)[kFlight], int k0) {
+        float tops[kFlight], top = -INFINITY;
 #pragma unroll
         for (int e = 0; e < kFlight; ++e) {
-          float top = fmaxf(v[e].get(0), v[e].get(1));
+          tops[e] = fmaxf(v[e].get(0), v[e].get(1));
 #pragma unroll
-          for (int i = 2; i < 8; i += 2) top = fmax3(top, v[e].get(i), v[e].get(i + 1));
-          if (top > m) {
-            const float f = ex2_approx((m - top) * c);
-            z *= f;
-            zl *= f;
-            m = top;
-            if (greedy) {
-#pragma unroll
-              for (int i = 7; i >= 0; --i)
-                if (v[e].get(i) == top) at = slice.token(slice.first(k0 + e), i);
-            }
-          }
-          float2 sum = weights2(v[e], 0, m, c);
-#pragma unroll
-          for (int i = 1; i < 4; ++i) {
-            const float2 w = weights2(v[e], i, m, c);
-            sum.x += w.x;
-            sum.y += w.y;
-          }
-          add_exact(z, zl, sum.x + sum.y);
+          for (int i = 2; i < 8; i += 2) tops[e] = fmax3(tops[e], v[e].get(i), v[e].get(i + 1));
+          top = fmaxf(top, tops[e]);
         }
+        if (top > m) {
+          const float f = ex2_approx((m - top) * c);
+          z *= f;
+          zl *= f;
+          m = top;
+          if (greedy) {  // the lowest token that has it
+#pragma unroll
+            for (int e = kFlight - 1; e >= 0; --e)
+              if (tops[e] == top) {
+#pragma unroll
+                for (int i = 7; i >= 0; --i)
+                  if (v[e].get(i) == top) at = slice.first(k0 + e) + i;
+              }
+          }
+        }
+        const uint64_t neg = pack_f32x2(-m, -m);
+#pragma unroll
+        for (int e = 0; e < kFlight; ++e) {
+          uint64_t sum = weights2(v[e], 0, neg, cc);
+#pragma unroll
+          for (int i = 1; i < 4; ++i) sum = add2(sum, weights2(v[e], i, neg, cc));
+          add_exact(z, zl, lo_f32(sum) + hi_f32(sum));
+        }
+      };
+      // one flight's arithmetic while the next one's loads are on their way
+      Raw<T> va[kFlight], vb[kFlight];
+      load(va, 0);
+#pragma unroll 1
+      for (int k0 = 0; k0 < n; k0 += 2 * kFlight) {
+        load(vb, k0 + kFlight);
+        add(va, k0);
+        if (k0 + kFlight >= n) break;
+        load(va, k0 + 2 * kFlight);
+        add(vb, k0 + kFlight);
       }
       if (d == 0) {
         kid = up == cur && w1 + lane > cur && token >= 0 && token < V && len < p.max_accept;
@@ -370,18 +417,26 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
         if (!more) break;
         const float fq = gone * iq;
         float z = 0.f, zl = 0.f;
+        const uint64_t neg_x = pack_f32x2(-st[0].max, -st[0].max), neg_y = pack_f32x2(-st[1].max, -st[1].max);
+        const uint64_t ipp = pack_f32x2(ip, ip), fqq = pack_f32x2(-fq, -fq);
 #pragma unroll 1
-        for (int k = 0; k < n; ++k) {
-          Raw<T> a, b;
-          load8(x, slice.first(k), slice, kNegInf<T>, a);
-          load8(y, slice.first(k), slice, kNegInf<T>, b);
-          float sum = 0.f;
+        for (int k0 = 0; k0 < n; k0 += kRace) {
+          Raw<T> a[kRace], b[kRace];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 wp = weights2(a, i, st[0].max, c), wq = weights2(b, i, st[1].max, c);
-            sum += fmaxf(wp.x * ip - wq.x * fq, 0.f) + fmaxf(wp.y * ip - wq.y * fq, 0.f);
+          for (int e = 0; e < kRace; ++e) {
+            load8<kWhole>(x, slice.first(k0 + e), slice, kNegInf<T>, a[e]);
+            load8<kWhole>(y, slice.first(k0 + e), slice, kNegInf<T>, b[e]);
           }
-          add_exact(z, zl, sum);
+#pragma unroll
+          for (int e = 0; e < kRace; ++e) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint64_t w = fma2(weights2(a[e], i, neg_x, cc), ipp, mul2(weights2(b[e], i, neg_y, cc), fqq));
+              sum += fmaxf(lo_f32(w), 0.f) + fmaxf(hi_f32(w), 0.f);
+            }
+            add_exact(z, zl, sum);
+          }
         }
         warp_add_exact(z, zl);
         if (lane < (int)size) peer_store(peer_addr(&s.sums[turn][mine], lane), __float_as_uint(z), __float_as_uint(zl));
@@ -407,44 +462,43 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
       for (int tries = 0; tries < 2 && out == 0x7fffffff; ++tries, fq = 0.f, lost = 0) {
         float best = 0.f;
         int best_at = 0x7fffffff;
+        const uint64_t neg_x = pack_f32x2(-st[0].max, -st[0].max), neg_y = y ? pack_f32x2(-st[1].max, -st[1].max) : 0;
+        const uint64_t ipp = pack_f32x2(ip, ip), fqq = pack_f32x2(-fq, -fq);
 #pragma unroll 1
-        for (int k = 0; k < n; ++k) {
-          const int at = slice.first(k);
-          Raw<T> a, b;
-          Raw<float> e;
-          load8(noise, at, slice, 0x3f800000u, e);
-          load8(x, at, slice, kNegInf<T>, a);
-          if (fq > 0.f) load8(y, at, slice, kNegInf<T>, b);
-          float v[8];
+        for (int k0 = 0; k0 < n; k0 += kRace) {
+          Raw<T> a[kRace], b[kRace];
+          Raw<float> e[kRace];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 w = weights2(a, i, st[0].max, c);
-            v[2 * i] = w.x * ip;
-            v[2 * i + 1] = w.y * ip;
+          for (int k = 0; k < kRace; ++k) {
+            load8<kWhole>(noise, slice.first(k0 + k), slice, 0x3f800000u, e[k]);
+            load8<kWhole>(x, slice.first(k0 + k), slice, kNegInf<T>, a[k]);
+            if (fq > 0.f) load8<kWhole>(y, slice.first(k0 + k), slice, kNegInf<T>, b[k]);
           }
-          if (fq > 0.f) {
+#pragma unroll
+          for (int k = 0; k < kRace; ++k) {
+            float v[8], top = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const float2 w = weights2(b, i, st[1].max, c);
-              v[2 * i] -= w.x * fq;
-              v[2 * i + 1] -= w.y * fq;
+              uint64_t w = mul2(weights2(a[k], i, neg_x, cc), ipp);
+              if (fq > 0.f) w = fma2(weights2(b[k], i, neg_y, cc), fqq, w);
+              v[2 * i] = __fdividef(lo_f32(w), e[k].get(2 * i));
+              v[2 * i + 1] = __fdividef(hi_f32(w), e[k].get(2 * i + 1));
             }
-          }
-          float top = 0.f;
+            const int at = slice.first(k0 + k);
+            for (int j = 0; j < lost; ++j) {  // tokens of rejected children do not take part
+              const int i = s.gone[j] - at;
+              if (i >= 0 && i < 8) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            v[i] = __fdividef(v[i], e.get(i));
-            top = fmaxf(top, v[i]);
-          }
-          if (!(top > best)) continue;
+                for (int d = 0; d < 8; ++d) v[d] = d == i ? 0.f : v[d];
+              }
+            }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (!(v[i] > best)) continue;
-            const int t = slice.token(at, i);
-            bool out_of_race = false;
-#pragma unroll 1
-            for (int j = 0; j < lost; ++j) out_of_race |= s.gone[j] == t;
-            if (!out_of_race) best = v[i], best_at = t;
+            for (int i = 0; i < 8; i += 2) top = fmax3(top, v[i], v[i + 1]);
+            if (top > best) {
+              best = top;
+#pragma unroll
+              for (int i = 7; i >= 0; --i) best_at = v[i] == top ? at + i : best_at;
+            }
           }
         }
         uint64_t key = warp_best((uint64_t)__float_as_uint(best) << 32 | (uint32_t)~best_at);
@@ -457,10 +511,9 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
         if (key >> 32) out = (int)~(uint32_t)key;
       }
     }
-    if (threadIdx.x == 0 && rank == 0) {
-      s.log_arg[len - 1] = out < V ? (at_token(x, out) - st[0].max) / div : 0.f;
-      s.log_sum[len - 1] = st[0].sum;
-      s.log_low[len - 1] = st[0].low;
+    if (threadIdx.x == 0) {
+      s.out[len - 1] = out;
+      s.node[len - 1] = st[0];
       if (went >= 0) s.path[len] = went;
     }
     if (went < 0) {
@@ -474,12 +527,17 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
   if (rank != 0) return;
   __syncthreads();
   for (int i = threadIdx.x; i < p.max_accept; i += blockDim.x) {
-    p.path[(size_t)r * p.max_accept + i] = i < len ? (i == 0 ? 0 : s.path[i]) : -1;
+    const int at = i > 0 && i < len ? s.path[i] : 0;
+    p.path[(size_t)r * p.max_accept + i] = i < len ? at : -1;
     if (p.logprobs) {
       float v = 0.f;
-      if (i < len)
-        v = bad && i == len - 1 ? __int_as_float(0x7fffffff)
-                                : s.log_arg[i] - (logf(s.log_sum[i]) + s.log_low[i] / s.log_sum[i]);
+      if (i < len && bad && i == len - 1) {
+        v = __int_as_float(0x7fffffff);
+      } else if (i < len) {
+        const Stats o = s.node[i];
+        const float l = at_token(static_cast<const T*>(p.logits) + (size_t)(q0 + at) * p.logits_stride, s.out[i]);
+        v = (l - o.max) / div - (logf(o.sum) + o.low / o.sum);
+      }
       p.logprobs[(size_t)r * p.max_accept + i] = v;
     }
   }
@@ -502,7 +560,7 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   auto whole = [&](const void* q, int64_t stride, size_t b) {
     return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && stride * b % 16 == 0);
   };
-  const bool vec = p.vocab % 8 == 0 && whole(p.logits, p.logits_stride, bytes) &&
+  const bool aligned = p.vocab % 8 == 0 && whole(p.logits, p.logits_stride, bytes) &&
                    whole(p.draft, p.draft_stride, bytes) && whole(p.noise, p.noise_stride, 4);
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(size * p.num_seqs);
@@ -518,8 +576,8 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   cfg.numAttrs = 2;
   const int ahead = p.num_seqs <= sms;
   if (fp32)
-    return cudaLaunchKernelEx(&cfg, vec ? verify_kernel<float, true> : verify_kernel<float, false>, p, ahead);
-  return cudaLaunchKernelEx(&cfg, vec ? verify_kernel<__nv_bfloat16, true> : verify_kernel<__nv_bfloat16, false>, p, ahead);
+    return cudaLaunchKernelEx(&cfg, aligned ? verify_kernel<float, true> : verify_kernel<float, false>, p, ahead);
+  return cudaLaunchKernelEx(&cfg, aligned ? verify_kernel<__nv_bfloat16, true> : verify_kernel<__nv_bfloat16, false>, p, ahead);
 }
 
 }  // namespace mcpu
