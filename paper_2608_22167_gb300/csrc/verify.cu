@@ -16,17 +16,21 @@
 // barrier every warp joins them all in the same order: all take the same
 // decisions, and nothing is sent back.
 //
-// Everything is fp32. Sums are pairs: 8 terms at a time, each group added by an
-// exact two-sum (a plain chain of additions loses 1e-6 of a peaked
-// distribution's tail; so does a maximum times log2(e) taken out of the
-// difference). Exponentials by ex2.approx (2^-22).
+// A pass streams the rows through shared memory: every thread copies vectors of
+// its own ahead (cp.async) and takes them out again, with no barrier, so that the
+// loop that is executed stays small (unrolled over as many loads as a slice needs
+// in flight, its instructions came from L2: 14000 cycles for one group of eight).
+//
+// Everything is fp32. Sums are pairs: 8 terms at a time, added by an exact two-sum
+// (a plain chain of additions loses 1e-6 of a peaked distribution's tail).
+// Exponentials by ex2.approx (2^-22).
 #include "keep.cuh"
 
 namespace mcpu {
 
 namespace {
 
-constexpr int kMaxThreads = 512, kMinThreads = 256, kMaxWarps = kMaxThreads / 32, kMaxCluster = 8;
+constexpr int kThreads = 256, kWarps = kThreads / 32, kMaxCluster = 8;
 constexpr int kMaxNodes = MCPU_MAX_TREE_NODES;
 constexpr float kLowest = -3.402823466e38f;  // a finite maximum to begin with: -inf logits weigh nothing against it
 constexpr float kLog2e = 1.4426950408889634f, kLog2eLow = 1.925963033500e-08f;  // log2(e) = the sum of both
@@ -38,9 +42,9 @@ struct Stats {  // of a distribution: maximum, the lowest token that has it, sum
 };
 
 struct VerifySmem {
-  Stats stats[2][2][kMaxCluster * kMaxWarps];  // [turn][target, draft][warp of the cluster]
-  float2 sums[2][kMaxCluster * kMaxWarps];
-  uint64_t best[2][kMaxCluster * kMaxWarps];
+  Stats stats[2][2][kMaxCluster * kWarps];  // [turn][target, draft][warp of the cluster]
+  float2 sums[2][kMaxCluster * kWarps];
+  uint64_t best[2][kMaxCluster * kWarps];
   int32_t gone[kMaxNodes];  // tokens of the rejected children of the node
   int32_t path[kMaxNodes];
   int32_t out[kMaxNodes];    // what was emitted after each node of the path,
@@ -87,70 +91,134 @@ struct Raw {  // as they are loaded
 template <typename T>
 constexpr uint32_t kNegInf = sizeof(T) == 4 ? 0xff800000u : 0xff80u;
 
-// The slice of the vocabulary that a block has; thread t's group k is the eight
-// values from begin + 8 (k threads + t) on.
+// The slice of the vocabulary that a block has. Its threads take groups of eight
+// values, kGroups of them a step; `shift` moves the groups to where the row has
+// its 16-byte vectors, so that the first one may begin before the slice.
 struct Slice {
-  int begin, end, vocab;
-  __device__ __forceinline__ int first(int k) const { return begin + 8 * (k * (int)blockDim.x + (int)threadIdx.x); }
-  __device__ __forceinline__ int groups() const {
-    return (end - begin + 8 * (int)blockDim.x - 1) / (8 * (int)blockDim.x);
+  int begin, end, shift;
+  // first value of the block's step k, of a thread's group e of it
+  __device__ __forceinline__ int step(int k, int groups) const { return begin - shift + 8 * groups * k * kThreads; }
+  static __device__ __forceinline__ int group(int step, int e) {
+    return step + 8 * (e * kThreads + (int)threadIdx.x);
+  }
+  __device__ __forceinline__ int steps(int groups) const {
+    const int per = 8 * groups * kThreads;
+    return begin < end ? (end - begin + shift + per - 1) / per : 0;
   }
 };
 
-// The eight values of a row from `at` on; `fill` (as bits of one) past the end.
-// kWhole: every row starts at 16 bytes and its length is a multiple of 8. Else
-// the row starts anywhere: one more vector, and shifts by the row's offset (the
-// same for all threads); where that vector would leave the row, one by one.
-template <bool kWhole, typename T>
-__device__ __forceinline__ void load8(const T* row, int at, const Slice& s, uint32_t fill, Raw<T>& r) {
-  constexpr int kWords = Raw<T>::kWords;
-  const uint32_t two = sizeof(T) == 4 ? fill : fill << 16 | fill;
-  if (kWhole) {
-#pragma unroll
-    for (int k = 0; k < kWords / 4; ++k) {
-      uint4 x = make_uint4(two, two, two, two);
-      if (at < s.end) x = __ldcg(reinterpret_cast<const uint4*>(row + at) + k);
-      r.w[4 * k] = x.x, r.w[4 * k + 1] = x.y, r.w[4 * k + 2] = x.z, r.w[4 * k + 3] = x.w;
-    }
-    return;
-  }
-  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row + at) & 15);
-  const bool inside = at + 8 + (off ? (int)((16 - off) / sizeof(T)) : 0) <= s.vocab && (off == 0 || at > 0);
-  if (at < s.end && inside) {
-    const uint4* v = reinterpret_cast<const uint4*>(reinterpret_cast<const uint8_t*>(row + at) - off);
-    uint32_t w[kWords + 4];
-#pragma unroll
-    for (int k = 0; k <= kWords / 4; ++k) {
-      if (k == kWords / 4 && off == 0) continue;
-      const uint4 x = v[k];  // (through L1: the neighbour's vector too)
-      w[4 * k] = x.x, w[4 * k + 1] = x.y, w[4 * k + 2] = x.z, w[4 * k + 3] = x.w;
-    }
-    // words first, then the half word
-#pragma unroll
-    for (int k = 0; k < kWords + 2; ++k) w[k] = off & 8 ? w[k + 2] : w[k];
-#pragma unroll
-    for (int k = 0; k < kWords + 1; ++k) w[k] = off & 4 ? w[k + 1] : w[k];
-#pragma unroll
-    for (int k = 0; k < kWords; ++k) r.w[k] = sizeof(T) == 2 && off & 2 ? __funnelshift_r(w[k], w[k + 1], 16) : w[k];
-    return;
-  }
-#pragma unroll
-  for (int k = 0; k < kWords; ++k) r.w[k] = two;
-  if (at >= s.end) return;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (at + i >= s.vocab) break;
-    if (sizeof(T) == 4) r.w[i] = reinterpret_cast<const uint32_t*>(row)[at + i];
-    else if (i & 1) r.w[i >> 1] = (r.w[i >> 1] & 0xffffu) | (uint32_t)reinterpret_cast<const uint16_t*>(row)[at + i] << 16;
-    else r.w[i >> 1] = (r.w[i >> 1] & 0xffff0000u) | reinterpret_cast<const uint16_t*>(row)[at + i];
+template <typename T>
+__device__ __forceinline__ uint32_t offset16(const T* p) {
+  return (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15);
+}
+
+// A slot of the ring holds a step's vectors of every row of the pass, each vector
+// in a plane of its own ([plane][thread]). A group of T takes kVectors<T> planes,
+// and one more in a row that need not have its vectors where the groups begin.
+template <typename T>
+constexpr int kVectors = 8 * sizeof(T) / 16;
+
+__device__ __forceinline__ uint8_t* plane_at(uint8_t* slot, int plane) {
+  return slot + (plane * kThreads + threadIdx.x) * 16;
+}
+__device__ __forceinline__ void copy16(uint8_t* dst, const uint8_t* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+}
+
+// A group whose vectors would leave the row, value by value.
+template <typename T>
+__device__ __noinline__ void fetch_edge(uint8_t* first_plane, const T* row, int j, int before, int planes, int n) {
+#pragma unroll 1
+  for (int i = 0; i < planes * 16 / (int)sizeof(T); ++i) {
+    const int at = j - before + i;
+    if (at >= 0 && at < n)
+      reinterpret_cast<T*>(first_plane + i / (16 / (int)sizeof(T)) * (kThreads * 16))[i % (16 / (int)sizeof(T))] = row[at];
   }
 }
 
-// A slice of a row into L2, ahead of its use.
-template <typename T>
-__device__ __forceinline__ void prefetch_slice(const T* row, const Slice& s) {
-  for (int i = s.begin + threadIdx.x * (128 / (int)sizeof(T)); i < s.end; i += blockDim.x * (128 / (int)sizeof(T)))
-    asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
+// Starts the copies of step k of a row of n values (kExtra: with the extra plane).
+template <int kGroups, bool kExtra, typename T>
+__device__ __forceinline__ void fetch(uint8_t* slot, const T* row, const Slice& s, int k, int n) {
+  constexpr int kPlanes = kVectors<T> + kExtra;
+  const int first = s.step(k, kGroups);
+  const uint32_t off = kExtra ? offset16(row + first) : 0u;
+  const int before = off / sizeof(T), planes = kVectors<T> + (off ? 1 : 0);
+  const uint8_t* src = reinterpret_cast<const uint8_t*>(row + first) - off + threadIdx.x * (8 * sizeof(T));
+#pragma unroll
+  for (int e = 0; e < kGroups; ++e) {
+    const int j = s.group(first, e);
+    if (j - before >= 0 && j - before + planes * (16 / (int)sizeof(T)) <= n) {
+#pragma unroll
+      for (int v = 0; v < kPlanes; ++v)
+        if (v < kVectors<T> || off) copy16(plane_at(slot, e * kPlanes + v), src + e * (kThreads * (8 * sizeof(T))) + 16 * v);
+    } else if (j < s.end && j + 8 > s.begin) {
+      fetch_edge(plane_at(slot, e * kPlanes), row, j, before, planes, n);
+    }
+  }
+}
+
+// Takes group e of step k out again; values outside the slice become `fill` (as bits of one).
+template <int kGroups, bool kExtra, typename T>
+__device__ __forceinline__ void take(uint8_t* slot, const T* row, const Slice& s, int k, int e, uint32_t fill, Raw<T>& r) {
+  constexpr int kWords = Raw<T>::kWords, kPlanes = kVectors<T> + kExtra;
+  const int first = s.step(k, kGroups), per = 8 * kGroups * kThreads;
+  const uint32_t off = kExtra ? offset16(row + first) : 0u;
+#pragma unroll
+  for (int v = 0; v < kVectors<T>; ++v) {
+    const uint4 x = *reinterpret_cast<const uint4*>(plane_at(slot, e * kPlanes + v));
+    r.w[4 * v] = x.x, r.w[4 * v + 1] = x.y, r.w[4 * v + 2] = x.z, r.w[4 * v + 3] = x.w;
+  }
+  if (kExtra && off) {
+    const uint4 x = *reinterpret_cast<const uint4*>(plane_at(slot, e * kPlanes + kVectors<T>));
+    uint32_t w[kWords + 4];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = r.w[i];
+    w[kWords] = x.x, w[kWords + 1] = x.y, w[kWords + 2] = x.z, w[kWords + 3] = x.w;
+    const uint32_t bits = (off & 3) * 8;
+    // by two words, by one, by half of one
+#pragma unroll
+    for (int i = 0; i < kWords + 2; ++i) w[i] = off & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i < kWords + 1; ++i) w[i] = off & 4 ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) r.w[i] = sizeof(T) == 2 ? __funnelshift_r(w[i], w[i + 1], bits) : w[i];
+  }
+  if (first >= s.begin && first + per <= s.end) return;
+  const int j = s.group(first, e);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (j + i >= s.begin && j + i < s.end) continue;
+    if (sizeof(T) == 4) r.w[i] = fill;
+    else if (i & 1) r.w[i >> 1] = (r.w[i >> 1] & 0xffffu) | fill << 16;
+    else r.w[i >> 1] = (r.w[i >> 1] & 0xffff0000u) | fill;
+  }
+}
+
+// Streams: issue(k, slot) for the steps k < n runs up to kDepth ahead of
+// use(k, slot). prime() sets the first copies on their way, once those of an
+// earlier stream have landed.
+template <int kDepth, typename Issue>
+__device__ __forceinline__ void prime(uint8_t* ring, int planes, int n, Issue issue) {
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll 1
+  for (int k = 0; k < kDepth - 1; ++k) {
+    if (k < n) issue(k, ring + k * planes * (kThreads * 16));
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+}
+template <int kDepth, typename Issue, typename Use>
+__device__ __forceinline__ void stream(uint8_t* ring, int planes, int n, Issue issue, Use use) {
+  int at = kDepth - 1;
+#pragma unroll 1
+  for (int k = 0; k < n; ++k) {
+    // step k + kDepth - 1 goes where step k - 1 was
+    uint8_t* slot = ring + at * planes * (kThreads * 16);
+    if (++at == kDepth) at = 0;
+    if (k + kDepth - 1 < n) issue(k + kDepth - 1, slot);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+    use(k, ring + at * planes * (kThreads * 16));
+  }
 }
 
 __device__ __forceinline__ float at_token(const __nv_bfloat16* x, int i) { return __bfloat162float(x[i]); }
@@ -170,13 +238,16 @@ __device__ __forceinline__ void warp_add_exact(float& hi, float& lo) {
     add_exact(hi, lo, oh);  // (the error is exact: both sides of a pair get the same bits)
   }
 }
+// Largest value of the warp, and the lowest `at` of those that have it (no NaN).
+__device__ __forceinline__ float warp_max(float m) {
+  const uint32_t u = __float_as_uint(m);
+  const uint32_t top = __reduce_max_sync(0xffffffffu, u & 0x80000000u ? ~u : u | 0x80000000u);
+  return __uint_as_float(top & 0x80000000u ? top & 0x7fffffffu : ~top);
+}
 __device__ __forceinline__ void warp_max(float& m, int& at) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float om = __shfl_xor_sync(0xffffffffu, m, o);
-    const int oat = __shfl_xor_sync(0xffffffffu, at, o);
-    if (om > m || (om == m && oat < at)) m = om, at = oat;
-  }
+  const float most = warp_max(m);
+  at = __reduce_min_sync(0xffffffffu, m == most ? at : 0x7fffffff);
+  m = most;
 }
 __device__ __forceinline__ uint64_t warp_best(uint64_t key) {
 #pragma unroll
@@ -201,17 +272,41 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   return d;
 }
 
-template <typename T, bool kWhole>
-__global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyParams p, int ahead) {
-  constexpr int kFlight = 8 / sizeof(T);               // groups of a row loaded together
-  constexpr int kRace = (kWhole ? 8 : 4) / sizeof(T);  // and of the two or three rows of the last passes
+template <typename T>
+__device__ __forceinline__ float top_of(const Raw<T>& v) {
+  float top = fmaxf(v.get(0), v.get(1));
+#pragma unroll
+  for (int i = 2; i < 8; i += 2) top = fmax3(top, v.get(i), v.get(i + 1));
+  return top;
+}
+
+// The ring, and what a pass makes of it: groups a step, planes, steps in flight.
+constexpr int kRingBytes = 64 * 1024, kRingPlanes = kRingBytes / (16 * kThreads);
+template <typename T>
+struct PassOne {  // one row
+  static constexpr int kGroups = 8 / sizeof(T), kPlanes = kGroups * kVectors<T>, kDepth = kRingPlanes / kPlanes;
+};
+template <typename T>
+struct PassTwo {  // target and draft
+  static constexpr int kGroups = 4 / sizeof(T), kDraft = kGroups * kVectors<T>,
+                       kPlanes = kDraft + kGroups * (kVectors<T> + 1), kDepth = kRingPlanes / kPlanes;
+};
+template <typename T>
+struct PassThree {  // target, exponentials, draft
+  static constexpr int kNoise = kVectors<T>, kDraft = kNoise + kVectors<float> + 1, kPlanes = kDraft + kVectors<T> + 1,
+                       kDepth = kRingPlanes / kPlanes;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams p) {
   __shared__ VerifySmem s;
+  extern __shared__ __align__(16) uint8_t ring[];
   cluster_arrive();  // (every block of the cluster is there before the first store into its memory)
   grid_dep_launch();
   grid_dep_wait();
   const uint32_t rank = cluster_rank(), size = cluster_size();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int parts = (int)size * warps, mine = (int)rank * warps + warp;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int parts = (int)size * kWarps, mine = (int)rank * kWarps + warp;
   const int r = blockIdx.x / size, V = p.vocab;
   const int q0 = p.qsl[r], L = p.qsl[r + 1] - q0;
   const float heat = p.temperature ? p.temperature[r] : 0.f;
@@ -227,14 +322,13 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
   const uint64_t cc = pack_f32x2(c, c);
   const int per = (V + 8 * (int)size - 1) / (8 * (int)size) * 8;
   Slice slice;
-  slice.vocab = V;
+  slice.shift = 0;
   slice.begin = min(V, (int)rank * per);
   slice.end = min(V, slice.begin + per);
-  const int n = slice.groups();
   const float* noise = greedy ? nullptr : p.noise + (size_t)r * p.noise_stride;
   uint32_t turn = 0;  // of the exchange buffers
+  int primed = -1;    // node whose first logits are on their way into the ring
   cluster_wait();
-  if (walks && !bad && !greedy && ahead) prefetch_slice(noise, slice);
 
   while (walks && !bad) {
     const T* x = static_cast<const T*>(p.logits) + (size_t)(q0 + cur) * p.logits_stride;
@@ -254,72 +348,81 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
     bool kid = false;
 #pragma unroll 1
     for (int d = 0; d < (y ? 2 : 1); ++d) {
+      using Pass = PassOne<T>;
       const T* row = d ? y : x;
+      slice.shift = offset16(row + slice.begin) / (int)sizeof(T);
       float m = kLowest, z = 0.f, zl = 0.f;
-      int at = 0x7fffffff;
-      auto load = [&](Raw<T>(&v)[kFlight], int k0) {
+      int best_step = 0;  // that holds the thread's maximum
+      auto issue = [&](int k, uint8_t* slot) { fetch<Pass::kGroups, false>(slot, row, slice, k, V); };
+      if (d == 1 || primed != cur) prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), issue);
+      stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), issue, [&](int k, uint8_t* slot) {
+        Raw<T> v[Pass::kGroups];
 #pragma unroll
-        for (int e = 0; e < kFlight; ++e) load8<kWhole>(row, slice.first(k0 + e), slice, kNegInf<T>, v[e]);
-      };
-      auto add = [&](const Raw<T>(&v)[kFlight], int k0) {
-        float tops[kFlight], top = -INFINITY;
+        for (int e = 0; e < Pass::kGroups; ++e) take<Pass::kGroups, false>(slot, row, slice, k, e, kNegInf<T>, v[e]);
+        float top = top_of(v[0]);
 #pragma unroll
-        for (int e = 0; e < kFlight; ++e) {
-          tops[e] = fmaxf(v[e].get(0), v[e].get(1));
-#pragma unroll
-          for (int i = 2; i < 8; i += 2) tops[e] = fmax3(tops[e], v[e].get(i), v[e].get(i + 1));
-          top = fmaxf(top, tops[e]);
-        }
+        for (int e = 1; e < Pass::kGroups; ++e) top = fmaxf(top, top_of(v[e]));
         if (top > m) {
           const float f = ex2_approx((m - top) * c);
           z *= f;
           zl *= f;
           m = top;
-          if (greedy) {  // the lowest token that has it
-#pragma unroll
-            for (int e = kFlight - 1; e >= 0; --e)
-              if (tops[e] == top) {
-#pragma unroll
-                for (int i = 7; i >= 0; --i)
-                  if (v[e].get(i) == top) at = slice.first(k0 + e) + i;
-              }
-          }
+          best_step = k;
         }
         const uint64_t neg = pack_f32x2(-m, -m);
+        uint64_t sum[2] = {0, 0};
 #pragma unroll
-        for (int e = 0; e < kFlight; ++e) {
-          uint64_t sum = weights2(v[e], 0, neg, cc);
+        for (int e = 0; e < Pass::kGroups; ++e)
 #pragma unroll
-          for (int i = 1; i < 4; ++i) sum = add2(sum, weights2(v[e], i, neg, cc));
-          add_exact(z, zl, lo_f32(sum) + hi_f32(sum));
-        }
-      };
-      // one flight's arithmetic while the next one's loads are on their way
-      Raw<T> va[kFlight], vb[kFlight];
-      load(va, 0);
-#pragma unroll 1
-      for (int k0 = 0; k0 < n; k0 += 2 * kFlight) {
-        load(vb, k0 + kFlight);
-        add(va, k0);
-        if (k0 + kFlight >= n) break;
-        load(va, k0 + 2 * kFlight);
-        add(vb, k0 + kFlight);
-      }
+          for (int i = 0; i < 4; ++i) sum[i & 1] = add2(sum[i & 1], weights2(v[e], i, neg, cc));
+        sum[0] = add2(sum[0], sum[1]);
+        add_exact(z, zl, lo_f32(sum[0]) + hi_f32(sum[0]));
+      });
       if (d == 0) {
         kid = up == cur && w1 + lane > cur && token >= 0 && token < V && len < p.max_accept;
-        const uint32_t kids = __ballot_sync(0xffffffffu, kid);
         if (kid) {
           lx = at_token(x, token);
           if (y) ly = at_token(y, token);
         }
-        if (ahead && kids) {  // the likeliest node to come
-          const size_t child = q0 + w1 + __ffs(kids) - 1;
-          prefetch_slice(static_cast<const T*>(p.logits) + child * p.logits_stride, slice);
-          if (y) prefetch_slice(static_cast<const T*>(p.draft) + child * p.draft_stride, slice);
+      }
+      const float wm = warp_max(m);
+      int at = 0x7fffffff;
+      if (greedy) {
+        if (m == wm) {  // the lowest token that has it, among this thread's of that step
+          const bool held = best_step >= slice.steps(Pass::kGroups) - Pass::kDepth;  // it is in the ring still
+          uint8_t* slot = ring + best_step % Pass::kDepth * Pass::kPlanes * kThreads * 16;
+#pragma unroll 1
+          for (int e = Pass::kGroups - 1; e >= 0; --e) {
+            const int j = slice.group(slice.step(best_step, Pass::kGroups), e);
+            Raw<T> v;
+            if (held) {
+              take<Pass::kGroups, false>(slot, row, slice, best_step, e, kNegInf<T>, v);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const float l = j + i >= slice.begin && j + i < slice.end ? at_token(row, j + i) : -INFINITY;
+                if (sizeof(T) == 4) v.w[i] = __float_as_uint(l);
+                else if (i & 1) v.w[i >> 1] |= __float_as_uint(l) & 0xffff0000u;
+                else v.w[i >> 1] = __float_as_uint(l) >> 16;
+              }
+            }
+#pragma unroll
+            for (int i = 7; i >= 0; --i) at = v.get(i) == wm ? j + i : at;
+          }
+        }
+        at = __reduce_min_sync(0xffffffffu, at);
+      }
+      if (d == (y ? 1 : 0)) {  // the likeliest node to come: its logits meanwhile
+        const uint32_t kids = __ballot_sync(0xffffffffu, kid);
+        primed = kids ? w1 + __ffs(kids) - 1 : -1;
+        if (primed >= 0) {
+          const T* child = static_cast<const T*>(p.logits) + (size_t)(q0 + primed) * p.logits_stride;
+          slice.shift = offset16(child + slice.begin) / (int)sizeof(T);
+          prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), [&](int k, uint8_t* slot) {
+            fetch<Pass::kGroups, false>(slot, child, slice, k, V);
+          });
         }
       }
-      float wm = m;
-      warp_max(wm, at);
       const float f = ex2_approx((m - wm) * c);
       z *= f;
       zl *= f;
@@ -419,25 +522,28 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
         float z = 0.f, zl = 0.f;
         const uint64_t neg_x = pack_f32x2(-st[0].max, -st[0].max), neg_y = pack_f32x2(-st[1].max, -st[1].max);
         const uint64_t ipp = pack_f32x2(ip, ip), fqq = pack_f32x2(-fq, -fq);
-#pragma unroll 1
-        for (int k0 = 0; k0 < n; k0 += kRace) {
-          Raw<T> a[kRace], b[kRace];
+        slice.shift = offset16(x + slice.begin) / (int)sizeof(T);
+        using Pass = PassTwo<T>;
+        auto issue = [&](int k, uint8_t* slot) {
+          fetch<Pass::kGroups, false>(slot, x, slice, k, V);
+          fetch<Pass::kGroups, true>(slot + Pass::kDraft * kThreads * 16, y, slice, k, V);
+        };
+        prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), issue);
+        stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), issue, [&](int k, uint8_t* slot) {
 #pragma unroll
-          for (int e = 0; e < kRace; ++e) {
-            load8<kWhole>(x, slice.first(k0 + e), slice, kNegInf<T>, a[e]);
-            load8<kWhole>(y, slice.first(k0 + e), slice, kNegInf<T>, b[e]);
-          }
-#pragma unroll
-          for (int e = 0; e < kRace; ++e) {
+          for (int e = 0; e < Pass::kGroups; ++e) {
+            Raw<T> a, b;
+            take<Pass::kGroups, false>(slot, x, slice, k, e, kNegInf<T>, a);
+            take<Pass::kGroups, true>(slot + Pass::kDraft * kThreads * 16, y, slice, k, e, kNegInf<T>, b);
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const uint64_t w = fma2(weights2(a[e], i, neg_x, cc), ipp, mul2(weights2(b[e], i, neg_y, cc), fqq));
+              const uint64_t w = fma2(weights2(a, i, neg_x, cc), ipp, mul2(weights2(b, i, neg_y, cc), fqq));
               sum += fmaxf(lo_f32(w), 0.f) + fmaxf(hi_f32(w), 0.f);
             }
             add_exact(z, zl, sum);
           }
-        }
+        });
         warp_add_exact(z, zl);
         if (lane < (int)size) peer_store(peer_addr(&s.sums[turn][mine], lane), __float_as_uint(z), __float_as_uint(zl));
         cluster_sync();
@@ -464,43 +570,60 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
         int best_at = 0x7fffffff;
         const uint64_t neg_x = pack_f32x2(-st[0].max, -st[0].max), neg_y = y ? pack_f32x2(-st[1].max, -st[1].max) : 0;
         const uint64_t ipp = pack_f32x2(ip, ip), fqq = pack_f32x2(-fq, -fq);
-#pragma unroll 1
-        for (int k0 = 0; k0 < n; k0 += kRace) {
-          Raw<T> a[kRace], b[kRace];
-          Raw<float> e[kRace];
+        slice.shift = offset16(x + slice.begin) / (int)sizeof(T);
+        using Pass = PassThree<T>;
+        const int off_e = Pass::kNoise * kThreads * 16, off_y = Pass::kDraft * kThreads * 16;
+        auto issue = [&](int k, uint8_t* slot) {
+          fetch<1, false>(slot, x, slice, k, V);
+          fetch<1, true>(slot + off_e, noise, slice, k, V);
+          if (fq > 0.f) fetch<1, true>(slot + off_y, y, slice, k, V);
+        };
+        prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue);
+        stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue, [&](int k, uint8_t* slot) {
+          const int j = slice.group(slice.step(k, 1), 0);
+          Raw<T> a;
+          Raw<float> e;
+          take<1, false>(slot, x, slice, k, 0, kNegInf<T>, a);
+          take<1, true>(slot + off_e, noise, slice, k, 0, 0x3f800000u, e);
+          uint64_t rest[4];
 #pragma unroll
-          for (int k = 0; k < kRace; ++k) {
-            load8<kWhole>(noise, slice.first(k0 + k), slice, 0x3f800000u, e[k]);
-            load8<kWhole>(x, slice.first(k0 + k), slice, kNegInf<T>, a[k]);
-            if (fq > 0.f) load8<kWhole>(y, slice.first(k0 + k), slice, kNegInf<T>, b[k]);
+          for (int i = 0; i < 4; ++i) rest[i] = weights2(a, i, neg_x, cc);
+          if (fq > 0.f) {
+            take<1, true>(slot + off_y, y, slice, k, 0, kNegInf<T>, a);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) rest[i] = fma2(weights2(a, i, neg_y, cc), fqq, mul2(rest[i], ipp));
           }
+          // rest / e > best where rest - best e > 0: no division but for what comes to lead
+          const uint64_t neg_best = pack_f32x2(-best, -best);
+          float top = 0.f;
 #pragma unroll
-          for (int k = 0; k < kRace; ++k) {
-            float v[8], top = 0.f;
+          for (int i = 0; i < 4; ++i) {
+            const uint64_t lead = fma2(pack_f32x2(e.get(2 * i), e.get(2 * i + 1)), neg_best, rest[i]);
+            top = fmax3(top, lo_f32(lead), hi_f32(lead));
+          }
+          if (!(top > 0.f)) return;
+          float v[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint64_t w = mul2(weights2(a[k], i, neg_x, cc), ipp);
-              if (fq > 0.f) w = fma2(weights2(b[k], i, neg_y, cc), fqq, w);
-              v[2 * i] = __fdividef(lo_f32(w), e[k].get(2 * i));
-              v[2 * i + 1] = __fdividef(hi_f32(w), e[k].get(2 * i + 1));
-            }
-            const int at = slice.first(k0 + k);
-            for (int j = 0; j < lost; ++j) {  // tokens of rejected children do not take part
-              const int i = s.gone[j] - at;
-              if (i >= 0 && i < 8) {
+          for (int i = 0; i < 8; ++i) {
+            const float w = i & 1 ? hi_f32(rest[i >> 1]) : lo_f32(rest[i >> 1]);
+            v[i] = w > 0.f ? __fdividef(w, e.get(i)) : 0.f;
+          }
+          for (int g = 0; g < lost; ++g) {  // tokens of rejected children do not take part
+            const int i = s.gone[g] - j;
+            if (i >= 0 && i < 8) {
 #pragma unroll
-                for (int d = 0; d < 8; ++d) v[d] = d == i ? 0.f : v[d];
-              }
-            }
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) top = fmax3(top, v[i], v[i + 1]);
-            if (top > best) {
-              best = top;
-#pragma unroll
-              for (int i = 7; i >= 0; --i) best_at = v[i] == top ? at + i : best_at;
+              for (int d = 0; d < 8; ++d) v[d] = d == i ? 0.f : v[d];
             }
           }
-        }
+          top = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) top = fmax3(top, v[i], v[i + 1]);
+          if (top > best) {
+            best = top;
+#pragma unroll
+            for (int i = 7; i >= 0; --i) best_at = v[i] == top ? j + i : best_at;
+          }
+        });
         uint64_t key = warp_best((uint64_t)__float_as_uint(best) << 32 | (uint32_t)~best_at);
         if (lane < (int)size) peer_store(peer_addr(&s.best[turn][mine], lane), (uint32_t)key, (uint32_t)(key >> 32));
         cluster_sync();
@@ -526,7 +649,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
   }
   if (rank != 0) return;
   __syncthreads();
-  for (int i = threadIdx.x; i < p.max_accept; i += blockDim.x) {
+  for (int i = threadIdx.x; i < p.max_accept; i += kThreads) {
     const int at = i > 0 && i < len ? s.path[i] : 0;
     p.path[(size_t)r * p.max_accept + i] = i < len ? at : -1;
     if (p.logprobs) {
@@ -552,19 +675,16 @@ __global__ void __launch_bounds__(kMaxThreads, 1) verify_kernel(const VerifyPara
 }  // namespace
 
 cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_t stream) {
-  // up to one block per SM large ones, several a row; more rows share the SMs in smaller ones
-  int size = 1, threads = p.num_seqs <= sms ? kMaxThreads : p.num_seqs <= 2 * sms ? kMaxThreads / 2 : kMinThreads;
-  while (size < kMaxCluster && 2 * size * p.num_seqs <= sms && 2 * size * kMinThreads * 8 <= p.vocab) size *= 2;
-  while (threads > kMinThreads && size * threads * 4 > p.vocab) threads /= 2;
-  const size_t bytes = fp32 ? 4 : 2;
-  auto whole = [&](const void* q, int64_t stride, size_t b) {
-    return !q || (reinterpret_cast<uintptr_t>(q) % 16 == 0 && stride * b % 16 == 0);
-  };
-  const bool aligned = p.vocab % 8 == 0 && whole(p.logits, p.logits_stride, bytes) &&
-                   whole(p.draft, p.draft_stride, bytes) && whole(p.noise, p.noise_stride, 4);
+  // blocks a row: as many as keep four per SM (64 rows of 131072 logits: 8 blocks
+  // a row 48 us, 4 50, 2 64, 1 91), two at least (384 rows: 1 block a row 330 us,
+  // 2 257, 4 255, 8 308), but a step of the ring for each
+  int size = 1;
+  const int step = PassOne<__nv_bfloat16>::kGroups * 8 * kThreads;
+  while (size < kMaxCluster && (size < 2 || 2 * size * p.num_seqs <= 4 * sms) && 2 * size * step <= 2 * p.vocab) size *= 2;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(size * p.num_seqs);
-  cfg.blockDim = dim3(threads);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kRingBytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -574,10 +694,13 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const int ahead = p.num_seqs <= sms;
-  if (fp32)
-    return cudaLaunchKernelEx(&cfg, aligned ? verify_kernel<float, true> : verify_kernel<float, false>, p, ahead);
-  return cudaLaunchKernelEx(&cfg, aligned ? verify_kernel<__nv_bfloat16, true> : verify_kernel<__nv_bfloat16, false>, p, ahead);
+  return cudaLaunchKernelEx(&cfg, fp32 ? verify_kernel<float> : verify_kernel<__nv_bfloat16>, p);
+}
+
+cudaError_t prepare_verify_kernels() {
+  const cudaError_t e = cudaFuncSetAttribute(verify_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(verify_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
 }
 
 }  // namespace mcpu
