@@ -48,6 +48,7 @@ cudaError_t prepare_fp8_kernels(int* bpsm_decode, int* bpsm_cascade);
 cudaError_t prepare_tree_kernels();
 cudaError_t prepare_weights_kernels();
 cudaError_t prepare_verify_kernels();
+cudaError_t prepare_evict_kernels();
 }  // namespace mcpu
 
 namespace {
@@ -100,6 +101,7 @@ mcpu_status device_state(DeviceState** out) {
     if ((e = prepare_tree_kernels()) != cudaSuccess) return cuda_fail(e);
     if ((e = prepare_weights_kernels()) != cudaSuccess) return cuda_fail(e);
     if ((e = prepare_verify_kernels()) != cudaSuccess) return cuda_fail(e);
+    if ((e = prepare_evict_kernels()) != cudaSuccess) return cuda_fail(e);
     if (st.bpsm_decode < 1 || st.bpsm_cascade < 1 || st.bpsm_append < 1 || st.bpsm_append_tc < 1 ||
         st.bpsm_fp8 < 1 || st.bpsm_fp8_cascade < 1)
       return MCPU_ERR_CUDA;

@@ -2,21 +2,28 @@
 //
 // One block per (layer, row, kv head). Of the N = n - first - last middle slots
 // the K = budget - first - last with the highest weight stay: the K-th largest
-// is found by a radix select over the weights' bits (8 at a time), and among
-// the slots that equal it the lowest are taken. Kept slots below
-// inner = budget - last stay where they are; there are as many holes below it
-// as kept slots past it, and the i-th of these moves into the i-th hole. The
-// last ones follow as one shift towards the front. No list of slots is ever
-// stored: both regions are walked in step, a block of slots at a time.
+// is found by a radix select over the weights' bits (11, 11 and 10 of them, one
+// histogram each), and among the slots that equal it the lowest are taken. Kept
+// slots below inner = budget - last stay where they are; there are as many holes
+// below it as kept slots past it, and the i-th of these moves into the i-th
+// hole. The last ones follow as one shift towards the front. Both regions are
+// walked in step, a block of slots at a time, and only as much of the two lists
+// is held as the next moves need.
+//
+// Bound by the moves (K and V rows read and written, scattered 128-byte rows);
+// for rows just past their budget by the chain lengths -> weights -> three
+// histograms -> ranks -> pages -> rows.
+#include <type_traits>
+
 #include "keep.cuh"
 
 namespace mcpu {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kQueue = 2 * kThreads;
+constexpr int kPer = 4;                       // slots a thread ranks at a time
 constexpr int kRowVecs = 2 * kRowBytes / 16;  // 16-byte pieces of a slot's K and V
+constexpr int kBins = 2048;
 
 // Unsigned order of the weights: NaN lowest, the two zeros equal.
 __device__ __forceinline__ uint32_t order(float w) {
@@ -25,56 +32,73 @@ __device__ __forceinline__ uint32_t order(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// kThreads threads; the orders of kKeys middle slots and as many pages are held.
+template <int kThreads_, int kKeys_, int kTable_>
 struct EvictSmem {
-  uint32_t hist[256];
-  int32_t scan[kWarps];
-  int32_t total;
-  uint32_t prefix;
+  static constexpr int kThreads = kThreads_, kWarps = kThreads / 32, kKeys = kKeys_, kTable = kTable_;
+  static constexpr int kBlock = kPer * kThreads;  // slots ranked at a time
+  static constexpr int kQueue = 2 * kBlock;       // slots waiting for their partners
+  static constexpr int kMoves = kThreads;         // pairs moved at a time
+  static_assert(kMoves + kBlock <= kQueue && kBins % kThreads == 0, "sizes");
+  uint32_t keys[kKeys];
+  union {
+    uint32_t hist[kBins];
+    struct {  // (once the cutoff is known)
+      int32_t src[kQueue], dst[kQueue];
+    };
+  };
+  int32_t table[kTable];
+  int32_t scan[2][kWarps];
+  uint32_t cutoff;
   int32_t want;
-  int32_t bad;
-  int32_t src[kQueue], dst[kQueue];
 };
 
-// Exclusive prefix sum of a 0/1 flag over the block, and its total.
-__device__ __forceinline__ int block_rank(bool flag, EvictSmem& s, int* total) {
+// Exclusive prefix sum over the block, and the total. `turn` alternates between calls.
+template <typename S>
+__device__ __forceinline__ int block_scan(int x, S& s, int turn, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t vote = __ballot_sync(0xffffffffu, flag);
-  if (lane == 0) s.scan[warp] = __popc(vote);
-  __syncthreads();
-  int before = 0, all = 0;
-  for (int w = 0; w < kWarps; ++w) {
-    const int n = s.scan[w];
-    before += w < warp ? n : 0;
-    all += n;
+  int incl = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
   }
+  if (lane == 31) s.scan[turn][warp] = incl;
   __syncthreads();
-  *total = all;
-  return before + __popc(vote & ((1u << lane) - 1u));
+  const int w = lane < S::kWarps ? s.scan[turn][lane] : 0;
+  const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
+  *total = __reduce_add_sync(0xffffffffu, w);
+  return before + incl - x;
 }
 
-__global__ void __launch_bounds__(kThreads) evict_kernel(const EvictParams p, const __grid_constant__ PoolPtrs pools) {
-  __shared__ EvictSmem s;
+template <typename S>
+__global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
+    evict_kernel(const EvictParams p, const __grid_constant__ PoolPtrs pools) {
+  constexpr int kThreads = S::kThreads, kBlock = S::kBlock, kQueue = S::kQueue, kMoves = S::kMoves;
+  extern __shared__ __align__(16) uint8_t smem[];
+  S& s = *reinterpret_cast<S*>(smem);
+  grid_dep_launch();
+  grid_dep_wait();
   const int h = blockIdx.x, r = blockIdx.y, m = blockIdx.z, Hkv = p.num_kv_heads;
   const int n = p.seq_lens[r];
   const bool speaks = h == 0 && m == 0 && threadIdx.x == 0;
   const int32_t* table = p.block_table + (size_t)r * p.max_pages;
   bool cut = n > p.limit;
   int32_t bits = 0;
+  const int page0 = p.first / kPage, pages = (n + kPage - 1) / kPage;
   if (n < 0 || n > p.max_pages * kPage || n > p.max_slots) {
     bits = kStatusBadLengths;
   } else if (cut) {
-    if (threadIdx.x == 0) s.bad = 0;
-    __syncthreads();
-    const int end = (n + kPage - 1) / kPage, mine = p.first < p.budget ? (p.budget + kPage - 1) / kPage : 0;
+    const int mine = p.first < p.budget ? (p.budget + kPage - 1) / kPage : 0;
     int32_t bad = 0;
-    for (int j = p.first / kPage + threadIdx.x; j < end; j += kThreads) {
+    for (int j = page0 + threadIdx.x; j < pages; j += kThreads) {
       const int page = table[j];
+      if (j - page0 < S::kTable) s.table[j - page0] = page;
       if (page < 0 || page >= p.num_pages) bad |= kStatusBadPage;
       else if (p.refs && j < mine && p.refs[page] > 0) bad |= kStatusUnsupportedRow;
     }
-    if (bad) atomicOr(&s.bad, bad);
-    __syncthreads();
-    bits = s.bad;
+    bits = (__syncthreads_or(bad & kStatusBadPage) ? kStatusBadPage : 0) |
+           (__syncthreads_or(bad & kStatusUnsupportedRow) ? kStatusUnsupportedRow : 0);
   }
   if (bits) cut = false;
   if (speaks) {
@@ -86,125 +110,194 @@ __global__ void __launch_bounds__(kThreads) evict_kernel(const EvictParams p, co
   const float* w = p.weights + at;
   float* nw = p.new_weights + at;
   const int inner = p.budget - p.last;
-  if (nw != w)
-    for (int j = threadIdx.x; j < (cut ? inner : n); j += kThreads) nw[j] = w[j];
-  if (!cut) return;
   const int first = p.first, end = n - p.last, K = inner - first;
+  // the weights that stay where they are, if they go elsewhere (those of the middle with the first histogram)
+  if (nw != w)
+    for (int j = threadIdx.x; j < (cut ? first : n); j += kThreads) nw[j] = w[j];
+  if (!cut) return;
 
   // ---- the K-th largest weight of the middle: its order, and how many that equal it stay
-  if (threadIdx.x == 0) {
-    s.prefix = 0;
-    s.want = K;
-  }
-  __syncthreads();
+  uint32_t cutoff = 0xffffffffu;
+  int ties = 0, turn = 0;
+  const bool cached = end - first <= S::kKeys;
+  auto key = [&](int j) { return cached ? s.keys[j - first] : order(__ldcg(w + j)); };
   if (K > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = threadIdx.x; i < 256; i += kThreads) s.hist[i] = 0;
+    int want = K;
+    uint32_t prefix = 0;
+    constexpr int kLoads = 8;
+#pragma unroll 1
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, width = pass == 2 ? 10 : 11;
+      for (int i = threadIdx.x; i < kBins; i += kThreads) s.hist[i] = 0;
       __syncthreads();
-      const uint32_t prefix = s.prefix;
-      for (int j = first + threadIdx.x; j < end; j += kThreads) {
-        const uint32_t u = order(w[j]);
-        if (shift == 24 || (u >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s.hist[(u >> shift) & 255], 1u);
+      auto count = [&](uint32_t u) {
+        if (pass == 0 || (u >> (shift + width)) == (prefix >> (shift + width)))
+          atomicAdd(&s.hist[(u >> shift) & ((1u << width) - 1u)], 1u);
+      };
+      if (cached && pass > 0) {
+        for (int j = threadIdx.x; j < end - first; j += kThreads) count(s.keys[j]);
+      } else {
+        for (int j0 = first + threadIdx.x; j0 < end; j0 += kLoads * kThreads) {
+          float v[kLoads];
+#pragma unroll
+          for (int e = 0; e < kLoads; ++e) v[e] = j0 + e * kThreads < end ? __ldcg(w + j0 + e * kThreads) : 0.f;
+#pragma unroll
+          for (int e = 0; e < kLoads; ++e) {
+            const int j = j0 + e * kThreads;
+            if (j >= end) continue;
+            const uint32_t u = order(v[e]);
+            if (cached) s.keys[j - first] = u;
+            if (pass == 0 && nw != w && j < inner) nw[j] = v[e];
+            count(u);
+          }
+        }
       }
       __syncthreads();
-      if (threadIdx.x == 0) {
-        int want = s.want, b = 255;
-        for (; b > 0 && (int)s.hist[b] < want; --b) want -= s.hist[b];
-        s.prefix = prefix | ((uint32_t)b << shift);
-        s.want = want;
+      // bins from the highest down: thread t has bins kBins - 1 - 4 t ..
+      constexpr int kEach = kBins / kThreads;
+      int c[kEach], sum = 0, total;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        c[e] = s.hist[kBins - 1 - (kEach * threadIdx.x + e)];
+        sum += c[e];
+      }
+      int before = block_scan(sum, s, turn, &total);
+      turn ^= 1;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        if (before < want && before + c[e] >= want) {
+          s.cutoff = prefix | (uint32_t)(kBins - 1 - (kEach * threadIdx.x + e)) << shift;
+          s.want = want - before;
+        }
+        before += c[e];
       }
       __syncthreads();
+      prefix = s.cutoff;
+      want = s.want;
     }
+    cutoff = prefix;
+    ties = want;
   }
-  const uint32_t cutoff = s.prefix;
-  const int ties = s.want;  // of the slots equal to the cutoff so many stay, the lowest
-  __syncthreads();
 
   // ---- kept slots at or past inner fill the holes before it, in order
-  int eq_a = 0;  // slots equal to the cutoff before inner
-  {
-    int mine = 0;
-    for (int j = first + threadIdx.x; j < inner; j += kThreads) mine += order(w[j]) == cutoff;
-    for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    if ((threadIdx.x & 31) == 0) s.scan[threadIdx.x >> 5] = mine;
-    __syncthreads();
-    for (int i = 0; i < kWarps; ++i) eq_a += s.scan[i];
-    __syncthreads();
-  }
-  const uint8_t* row_pools[2] = {pools.p[m], pools.p[p.num_layers + m]};
+  const bool held = pages - page0 <= S::kTable;
+  auto page_of = [&](int slot) { return held ? s.table[slot / kPage - page0] : table[slot / kPage]; };
+  const uint8_t *kp = pools.p[m], *vp = pools.p[p.num_layers + m];
   auto vec = [&](int slot, int e) {  // 16-byte piece e of a slot's K and V
-    const size_t row = ((size_t)table[slot / kPage] * Hkv + h) * kPage + slot % kPage;
-    return reinterpret_cast<uint4*>(const_cast<uint8_t*>(row_pools[e >> 3]) + row * kRowBytes) + (e & 7);
+    const size_t row = ((size_t)page_of(slot) * Hkv + h) * kPage + slot % kPage;
+    return reinterpret_cast<uint4*>(const_cast<uint8_t*>(e & 8 ? vp : kp) + row * kRowBytes) + (e & 7);
   };
-  int ja = first, jb = inner, seen_a = 0, seen_b = eq_a, have_a = 0, have_b = 0, done = 0;
-  while (true) {
-    // the queues hold less than kThreads entries each here, or their region is at its end
-    while (have_b - done < kThreads && jb < end) {
-      const int j = jb + threadIdx.x;
-      const uint32_t u = j < end ? order(w[j]) : 0u;
-      const bool eq = K > 0 && j < end && u == cutoff;
-      int all;
-      const int rank = seen_b + block_rank(eq, s, &all);
-      seen_b += all;
-      const bool keep = K > 0 && j < end && (u > cutoff || (eq && rank < ties));
-      const int slot = have_b + block_rank(keep, s, &all);
-      if (keep) s.src[slot % kQueue] = j;
-      have_b += all;
-      jb += kThreads;
+  int ties_before = 0;  // slots equal to the cutoff before inner
+  if (K > 0) {
+    int mine = 0;
+    for (int j = first + threadIdx.x; j < inner; j += kThreads) mine += key(j) == cutoff;
+    block_scan(mine, s, turn, &ties_before);
+    turn ^= 1;
+  }
+  int ja = first, jb = inner, seen_a = 0, seen_b = ties_before, have_a = 0, have_b = 0, done = 0;
+  // ranks the next kBlock slots of a region: those kept (or the holes) go to the queue
+  auto walk = [&](int& j0, int stop, int& seen, int& have, bool holes, int32_t* queue) {
+    const int j = j0 + kPer * threadIdx.x;
+    uint32_t u[kPer];
+    int counts = 0, all;  // above the cutoff, and at it << 16
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      u[e] = j + e < stop ? key(j + e) : 0u;
+      if (j + e < stop) counts += u[e] > cutoff ? 1 : u[e] == cutoff ? 1 << 16 : 0;
     }
-    while (have_a - done < kThreads && ja < inner) {
-      const int j = ja + threadIdx.x;
-      const uint32_t u = j < inner ? order(w[j]) : 0u;
-      const bool eq = j < inner && u == cutoff;
-      int all;
-      const int rank = seen_a + block_rank(eq, s, &all);
-      seen_a += all;
-      const bool hole = j < inner && !(u > cutoff || (eq && rank < ties));
-      const int slot = have_a + block_rank(hole, s, &all);
-      if (hole) s.dst[slot % kQueue] = j;
-      have_a += all;
-      ja += kThreads;
+    const int before = block_scan(counts, s, turn, &all);
+    turn ^= 1;
+    // kept so far in this block: those above the cutoff, and of those at it as many as are left of the ties
+    const int left = max(ties - seen, 0), inside = min(j0 + kBlock, stop) - j0;
+    int eq = before >> 16, kept = (before & 0xffff) + min(eq, left);
+    int at = have + (holes ? min(kPer * (int)threadIdx.x, inside) - kept : kept);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      if (j + e >= stop) continue;
+      const bool keep = u[e] > cutoff || (u[e] == cutoff && eq++ < left);
+      if (keep != holes) queue[at++ % kQueue] = j + e;
     }
+    kept = (all & 0xffff) + min(all >> 16, left);
+    seen += all >> 16;
+    all = holes ? inside - kept : kept;
+    have += all;
+    j0 += kBlock;
+  };
+#pragma unroll 1
+  while (K > 0) {
+    while (have_b - done < kMoves && jb < end) walk(jb, end, seen_b, have_b, false, s.src);
+    if (have_b == done) break;
+    while (have_a - done < min(kMoves, have_b - done) && ja < inner) walk(ja, inner, seen_a, have_a, true, s.dst);
     __syncthreads();
-    const int count = min(min(have_a, have_b) - done, kThreads);
+    const int count = min(min(have_a, have_b) - done, kMoves);
     if (count <= 0) break;
-    for (int e = threadIdx.x; e < count * kRowVecs; e += kThreads) {
-      const int i = (done + e / kRowVecs) % kQueue;
-      *vec(s.dst[i], e % kRowVecs) = *vec(s.src[i], e % kRowVecs);
+    constexpr int kFlight = 8;
+    for (int e0 = threadIdx.x; e0 < count * kRowVecs; e0 += kFlight * kThreads) {
+      uint4 v[kFlight];
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        const int e = e0 + k * kThreads;
+        if (e < count * kRowVecs) v[k] = __ldcs(vec(s.src[(done + e / kRowVecs) % kQueue], e % kRowVecs));
+      }
+#pragma unroll
+      for (int k = 0; k < kFlight; ++k) {
+        const int e = e0 + k * kThreads;
+        if (e < count * kRowVecs) *vec(s.dst[(done + e / kRowVecs) % kQueue], e % kRowVecs) = v[k];
+      }
     }
     for (int e = threadIdx.x; e < count; e += kThreads) nw[s.dst[(done + e) % kQueue]] = w[s.src[(done + e) % kQueue]];
     done += count;
     __syncthreads();
   }
-  // ---- the last ones: towards the front, so a piece of them at a time, read before it is written
-  constexpr int kHeld = 4;
-  for (int i0 = 0; i0 < p.last; i0 += kHeld * kThreads / kRowVecs) {
-    const int count = min(p.last - i0, kHeld * kThreads / kRowVecs);
-    uint4 held[kHeld];
-    float held_w = 0.f;
+
+  // ---- the last ones, towards the front: a piece of them at a time, read before it is written
+  __syncthreads();
+  constexpr int kHeld = 8, kPiece = kHeld * kThreads / kRowVecs;
+  const bool apart = n - p.budget >= p.last;  // they do not overlap their new places
+#pragma unroll 1
+  for (int i0 = 0; i0 < p.last; i0 += kPiece) {
+    const int count = min(p.last - i0, kPiece);
+    uint4 v[kHeld];
+    float weight = 0.f;
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
       const int e = threadIdx.x + k * kThreads;
-      if (e < count * kRowVecs) held[k] = *vec(end + i0 + e / kRowVecs, e % kRowVecs);
+      if (e < count * kRowVecs) v[k] = __ldcs(vec(end + i0 + e / kRowVecs, e % kRowVecs));
     }
-    if (threadIdx.x < count) held_w = w[end + i0 + threadIdx.x];
-    __syncthreads();
+    if (threadIdx.x < count) weight = w[end + i0 + threadIdx.x];
+    if (!apart) __syncthreads();
 #pragma unroll
     for (int k = 0; k < kHeld; ++k) {
       const int e = threadIdx.x + k * kThreads;
-      if (e < count * kRowVecs) *vec(inner + i0 + e / kRowVecs, e % kRowVecs) = held[k];
+      if (e < count * kRowVecs) *vec(inner + i0 + e / kRowVecs, e % kRowVecs) = v[k];
     }
-    if (threadIdx.x < count) nw[inner + i0 + threadIdx.x] = held_w;
-    __syncthreads();
+    if (threadIdx.x < count) nw[inner + i0 + threadIdx.x] = weight;
+    if (!apart) __syncthreads();
   }
 }
 
 }  // namespace
 
+using Middle = EvictSmem<256, 4096, 1024>;
+using Large = EvictSmem<512, 16384, 4096>;
+
 cudaError_t launch_evict(const EvictParams& p, const PoolPtrs& pools, int sms, cudaStream_t stream) {
-  (void)sms;
-  LaunchCfg lc(dim3(p.num_kv_heads, p.num_seqs, p.num_layers > 0 ? p.num_layers : 1), dim3(kThreads), 0, stream, false);
-  return cudaLaunchKernelEx(&lc.cfg, evict_kernel, p, pools);
+  const dim3 grid(p.num_kv_heads, p.num_seqs, p.num_layers > 0 ? p.num_layers : 1);
+  const int64_t items = (int64_t)grid.x * grid.y * grid.z;
+  auto launch = [&](auto kernel, auto* smem) {
+    using S = std::remove_pointer_t<decltype(smem)>;
+    LaunchCfg lc(grid, dim3(S::kThreads), sizeof(S), stream, true);
+    return cudaLaunchKernelEx(&lc.cfg, kernel, p, pools);
+  };
+  if (items > 2 * sms) return launch(evict_kernel<Middle>, (Middle*)nullptr);
+  return launch(evict_kernel<Large>, (Large*)nullptr);
+}
+
+cudaError_t prepare_evict_kernels() {
+  constexpr auto kSmem = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(evict_kernel<Middle>, kSmem, (int)sizeof(Middle));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(evict_kernel<Large>, kSmem, (int)sizeof(Large));
+  return e;
 }
 
 }  // namespace mcpu
