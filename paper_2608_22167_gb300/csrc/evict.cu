@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
 }  // namespace
 
 using Middle = EvictSmem<256, 4096, 1024>;
-using Large = EvictSmem<512, 16384, 4096>;
+using Large = EvictSmem<512, 8192, 4096>;
 
 cudaError_t launch_evict(const EvictParams& p, const PoolPtrs& pools, int sms, cudaStream_t stream) {
   const dim3 grid(p.num_kv_heads, p.num_seqs, p.num_layers > 0 ? p.num_layers : 1);

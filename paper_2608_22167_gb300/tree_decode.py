@@ -8,14 +8,17 @@ long as the tensors stay the same):
     cache.extend(new_lens)              pages for the drafted tokens
     q = cache.append(layer, ...)        norm, rotation, K/V to the pages
     cache.attend(layer, q, ...)         every node over the context and its ancestors
+    path, path_len, ... = cache.verify(logits, ...)   which drafted tokens are accepted
     cache.keep(qsl, path, path_len)     the accepted path stays, spare pages return
+    cache.evict(budget, ...)            rows past a limit cut to the keys that got most attention
     cache.fork(src, dst)                new samples from running rows
     cache.drop(rows)                    rows leave
 
 ``python -m paper_2608_22167_gb300.tree_decode`` runs a toy model (random
 weights, two layers) with forked samples: it decodes greedily with drafted
-trees and reports the tokens accepted a round. No model of any framework is
-loaded; PyTorch does the toy model's projections.
+trees and reports the tokens accepted a round, then samples on in a cache that
+is held to a budget of keys. No model of any framework is loaded; PyTorch does
+the toy model's projections.
 """
 from __future__ import annotations
 
@@ -28,9 +31,11 @@ PAGE, HEAD_DIM = 16, 64
 
 class PagedCache:
     """The pools, table, page counts and stack of layers that share a block table. sliding_window > 0: all of them
-    attend within that window, and `keep` returns the pages before it."""
+    attend within that window, and `keep` returns the pages before it. count_weights: `keep` (or `observe`) counts the
+    attention that every key got, for `evict`; `attend` then keeps hold of each layer's q and log-sum-exps until then."""
 
-    def __init__(self, layers, rows, max_pages, num_pages, num_q_heads, num_kv_heads, device="cuda", sliding_window=0):
+    def __init__(self, layers, rows, max_pages, num_pages, num_q_heads, num_kv_heads, device="cuda", sliding_window=0,
+                 count_weights=False):
         shape = (num_pages, num_kv_heads, PAGE, HEAD_DIM)
         i32 = dict(dtype=torch.int32, device=device)
         self.k = [torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(layers)]
@@ -48,12 +53,21 @@ class PagedCache:
         d = mcpu.Dims(rows, 0, max_pages, num_pages, num_q_heads, num_kv_heads, HEAD_DIM, PAGE)
         self.workspace = mcpu.new_tree_workspace(d, device)
         self.status = mcpu.status_word(self.workspace)
+        self.evicted = torch.zeros(rows, **i32)  # keys that a row has lost: its slot s holds no earlier position than s + evicted
+        self.key_weights = self.weights_workspace = None
+        if count_weights:
+            if sliding_window > 0:
+                raise ValueError("the keys of a sliding window are let go by their age")
+            self.key_weights = torch.zeros(layers, rows, num_kv_heads, max_pages * PAGE, device=device)
+            self.weights_workspace = mcpu.new_weights_workspace(d, device)
+            self.asked = [None] * layers  # (q, lse, scale) of each layer's last attention
 
     def check(self):
         """Raises if a call so far has reported a device-side error (synchronises)."""
-        code, bits = mcpu.mcpu_read_device_status(self.workspace)
-        if code:
-            raise mcpu.McpuError(code, f"device status bits {bits}")
+        for ws in (self.workspace, self.weights_workspace):
+            code, bits = mcpu.mcpu_read_device_status(ws) if ws is not None else (0, 0)
+            if code:
+                raise mcpu.McpuError(code, f"device status bits {bits}")
 
     def extend(self, new_lens):
         """Row lengths after the next append (int32 [rows]) and the pages for them. What is appended follows the tokens
@@ -79,14 +93,56 @@ class PagedCache:
         mcpu.mcpu_tree_attention_forward(q, self.k[layer], self.v[layer], self.block_table, self.seq_lens,
                                          query_start_loc, tree_mask, positions, sliding_window, scale, out, lse,
                                          self.workspace, sinks=sinks)
+        if self.key_weights is not None:
+            self.asked[layer] = (q, lse, scale)
         return out, lse
 
-    def keep(self, query_start_loc, path, path_len):
-        """Keeps the accepted nodes path[r, :path_len[r]] of each row's tree, in every layer, and returns
-        the pages behind them."""
+    def verify(self, logits, tokens, parents, query_start_loc, max_accept, temperature=None, draft_logits=None,
+               uniforms=None, exponentials=None):
+        """Which nodes of each row's tree are accepted, from the target's logits at every node: path [rows,
+        max_accept], path_len, the token after it, and the log-probabilities of what is emitted. temperature (float32
+        [rows], 0: greedy) None: all greedy. Random numbers that are not given are drawn."""
+        dev, rows = logits.device, self.rows
+        i32 = dict(dtype=torch.int32, device=dev)
+        path, path_len, token = torch.empty(rows, max_accept, **i32), torch.empty(rows, **i32), torch.empty(rows, **i32)
+        logprobs = torch.empty(rows, max_accept, device=dev)
+        if temperature is not None:
+            if uniforms is None:
+                uniforms = torch.rand(logits.shape[0], device=dev)
+            if exponentials is None:  # (never 0, of which only rounding could make one)
+                exponentials = torch.empty(rows, logits.shape[1], device=dev).exponential_().clamp_(min=1e-30)
+        mcpu.mcpu_verify_tree(logits, tokens, parents, query_start_loc, temperature, uniforms, exponentials, path, path_len,
+                              token, logprobs, self.status, draft_logits=draft_logits)
+        return path, path_len, token, logprobs
+
+    def observe(self, query_start_loc, path=None, path_len=None, decay=1.0):
+        """Counts the attention of the last step's queries (those of the accepted nodes, once `keep` has moved their
+        keys; None: all) for every layer; earlier weights are multiplied by decay."""
+        for layer, (q, lse, scale) in enumerate(self.asked):
+            mcpu.mcpu_accumulate_weights(q, lse, self.k[layer], self.block_table, self.seq_lens, query_start_loc, 0, scale,
+                                         decay, self.key_weights[layer], self.weights_workspace, query_path=path,
+                                         path_len=path_len)
+        self.asked = [None] * len(self.asked)
+
+    def evict(self, budget, keep_first=4, keep_last=32, limit=None):
+        """Rows of more than `limit` keys (None: budget) are cut to budget: the first, the last, and those that got
+        most attention, for every kv head of every layer by itself. Rows that share pages are left alone and reported:
+        their forks would lose the keys too. Positions go on from `seq_lens + evicted`."""
+        mcpu.mcpu_evict_kv(self.pools, self.key_weights, self.block_table, self.seq_lens, budget if limit is None else limit,
+                           budget, keep_first, keep_last, self.key_weights, self.new_lens, self.status,
+                           page_refs=self.page_refs)
+        self.evicted += self.seq_lens - self.new_lens
+        self.seq_lens.copy_(self.new_lens)
+        self._release(self.seq_lens)
+
+    def keep(self, query_start_loc, path, path_len, decay=1.0):
+        """Keeps the accepted nodes path[r, :path_len[r]] of each row's tree, in every layer, counts their attention
+        if weights are counted, and returns the pages behind them."""
         mcpu.mcpu_compact_kv(self.pools, self.block_table, self.seq_lens, query_start_loc, path, path_len,
                              self.new_lens, self.status)
         self.seq_lens.copy_(self.new_lens)
+        if self.key_weights is not None:
+            self.observe(query_start_loc, path, path_len, decay)
         self.held_lens.copy_(self.seq_lens)
         self._release(self.seq_lens, self.sliding_window)
 
@@ -98,11 +154,16 @@ class PagedCache:
         mcpu.mcpu_fork_block_tables(self.block_table, self.seq_lens, src_rows, dst_rows, self.page_refs,
                                     self.free_pages, self.free_count, copy[0], copy[1], self.page_scratch, self.status)
         mcpu.mcpu_copy_pages(self.pools, copy[0], copy[1], self.status)
+        src, dst = src_rows.long(), dst_rows.long()
+        self.evicted[dst] = self.evicted[src]
+        if self.key_weights is not None:
+            self.key_weights[:, dst] = self.key_weights[:, src]
         self.held_lens.copy_(self.seq_lens)
 
     def drop(self, rows):
         """Frees the rows (int64 indices)."""
         self.seq_lens[rows] = 0
+        self.evicted[rows] = 0
         self._release(self.seq_lens)
 
     def _release(self, lens, sliding_window=0):
@@ -187,33 +248,42 @@ def accept_greedy(parents, tokens, choice):
         at = nxt
 
 
-def generate(model, cache, last, rounds, seed=0, nodes=24):
-    """Greedy decoding of the rows whose last tokens (not yet in the cache) are `last`, `rounds` rounds with a
-    drafted tree each: node 0 is the last token, the others random drafts. Returns each row's new tokens."""
+def generate(model, cache, last, rounds, seed=0, nodes=24, temperature=0.0, budget=0, keep_first=4, keep_last=32):
+    """Decoding of the rows whose last tokens (not yet in the cache) are `last`, `rounds` rounds with a drafted tree
+    each: node 0 is the last token, the others random drafts. Greedy at temperature 0, else sampled. budget > 0: rows
+    are cut to so many keys once a round (the cache counts weights). Returns each row's new tokens."""
     g = torch.Generator()
     g.manual_seed(seed)
     rows = len(last)
     dev = cache.block_table.device
+    draws = torch.Generator(device=dev)
+    draws.manual_seed(seed)
     made = [[] for _ in range(rows)]
+    heat = torch.full((rows,), float(temperature), device=dev) if temperature > 0 else None
+    qsl = torch.arange(0, rows * nodes + 1, nodes, dtype=torch.int32, device=dev)
     for _ in range(rounds):
         parents = [[-1] + [int(torch.randint(max(0, i - 6), i, (1,), generator=g)) for i in range(1, nodes)]
                    for _ in range(rows)]
         tokens = [[last[r]] + torch.randint(0, model.vocab, (nodes - 1,), generator=g).tolist() for r in range(rows)]
         mask, depth = tree_masks(parents)
+        tree = torch.tensor(parents, dtype=torch.int32, device=dev).flatten()
+        nodes_tokens = torch.tensor(tokens, device=dev).flatten()
         ctx = cache.seq_lens.clone()
-        qsl = torch.arange(0, rows * nodes + 1, nodes, dtype=torch.int32, device=dev)
-        positions = (ctx.repeat_interleave(nodes) + depth.to(dev)).int()
+        positions = ((ctx + cache.evicted).repeat_interleave(nodes) + depth.to(dev)).int()
         cache.extend(ctx + nodes)
-        logits = model.run(cache, torch.tensor(tokens, device=dev).flatten(), qsl, mask.to(dev), positions)
-        choice = logits.argmax(1).view(rows, nodes).tolist()
-        paths = []
-        for r in range(rows):
-            path, last[r] = accept_greedy(parents[r], tokens[r], choice[r])
-            made[r] += [tokens[r][i] for i in path[1:]] + [last[r]]
-            paths.append(path)
-        most = max(len(p) for p in paths)
-        cache.keep(qsl, torch.tensor([p + [0] * (most - len(p)) for p in paths], dtype=torch.int32, device=dev),
-                   torch.tensor([len(p) for p in paths], dtype=torch.int32, device=dev))
+        logits = model.run(cache, nodes_tokens, qsl, mask.to(dev), positions)
+        uniforms = exponentials = None
+        if heat is not None:
+            uniforms = torch.rand(rows * nodes, generator=draws, device=dev)
+            exponentials = torch.empty(rows, model.vocab, device=dev).exponential_(generator=draws).clamp_(min=1e-30)
+        path, path_len, token, _ = cache.verify(logits, nodes_tokens.int(), tree, qsl, nodes, heat, uniforms=uniforms,
+                                                exponentials=exponentials)
+        cache.keep(qsl, path, path_len)
+        if budget > 0:
+            cache.evict(budget, keep_first, keep_last)
+        last[:] = token.tolist()
+        for r, (way, n) in enumerate(zip(path.tolist(), path_len.tolist())):
+            made[r] += [tokens[r][i] for i in way[1:n]] + [last[r]]
     cache.check()
     return made
 
@@ -222,16 +292,19 @@ def main():
     model = ToyModel()
     prompts, samples = 4, 4
     rows = prompts * (1 + samples)
-    cache = PagedCache(2, rows, 64, 1200, model.hq, model.hkv)
     # the prompts: chains of 37 to 100 tokens in the first rows, then four samples of each
     lens = [37, 64, 81, 100]
-    parents = [list(range(-1, n - 1)) for n in lens]
-    mask, depth = tree_masks(parents)
+    mask, depth = tree_masks([list(range(-1, n - 1)) for n in lens])
     qsl = torch.tensor([0] + [sum(lens[:i + 1]) for i in range(prompts)] + [sum(lens)] * (rows - prompts),
                        dtype=torch.int32, device="cuda")
-    cache.extend(torch.tensor(lens + [0] * (rows - prompts), device="cuda"))
     tokens = torch.randint(0, model.vocab, (sum(lens),), device="cuda")
-    model.run(cache, tokens, qsl, mask.cuda(), depth.cuda())
+
+    def fill(cache):
+        cache.extend(torch.tensor(lens + [0] * (rows - prompts), device="cuda"))
+        model.run(cache, tokens, qsl, mask.cuda(), depth.cuda())
+
+    cache = PagedCache(2, rows, 64, 1200, model.hq, model.hkv)
+    fill(cache)
     src = torch.arange(prompts, dtype=torch.int32, device="cuda").repeat_interleave(samples)
     dst = torch.arange(prompts, rows, dtype=torch.int32, device="cuda")
     cache.fork(src, dst)
@@ -245,6 +318,19 @@ def main():
     cache.drop(torch.arange(rows, device="cuda"))
     cache.check()
     assert int(cache.free_count) == cache.page_refs.shape[0] and not cache.page_refs.any()
+
+    # the prompts alone, sampled on with at most 96 keys a head
+    cache = PagedCache(2, rows, 64, 1200, model.hq, model.hkv, count_weights=True)
+    fill(cache)
+    cache.observe(qsl)
+    cache.held_lens.copy_(cache.seq_lens)
+    made = generate(model, cache, [r % model.vocab for r in range(rows)], 2 * rounds, temperature=0.8, budget=96)
+    n = sum(map(len, made))
+    print(f"sampled with 96 keys a head: {n} tokens, {n / rows / (2 * rounds):.2f} a row and round; "
+          f"{int(cache.evicted.sum())} keys let go, rows of {int(cache.seq_lens.max())} keys at most")
+    cache.drop(torch.arange(rows, device="cuda"))
+    cache.check()
+    assert int(cache.free_count) == cache.page_refs.shape[0]
 
 
 if __name__ == "__main__":
