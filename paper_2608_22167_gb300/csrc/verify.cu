@@ -24,6 +24,8 @@
 // Everything is fp32. Sums are pairs: 8 terms at a time, added by an exact two-sum
 // (a plain chain of additions loses 1e-6 of a peaked distribution's tail).
 // Exponentials by ex2.approx (2^-22).
+#include <type_traits>
+
 #include "keep.cuh"
 
 namespace mcpu {
@@ -281,20 +283,25 @@ __device__ __forceinline__ float top_of(const Raw<T>& v) {
 }
 
 // The ring, and what a pass makes of it: groups a step, planes, steps in flight.
-constexpr int kRingBytes = 64 * 1024, kRingPlanes = kRingBytes / (16 * kThreads);
+// 60 KiB leave room for three blocks on an SM; the draft's fp32 logits with the
+// exponentials need 64 for two steps.
+template <typename T>
+constexpr int kRingPlanes = sizeof(T) == 2 ? 15 : 16;
+template <typename T>
+constexpr int kRingBytes = kRingPlanes<T> * 16 * kThreads;
 template <typename T>
 struct PassOne {  // one row
-  static constexpr int kGroups = 8 / sizeof(T), kPlanes = kGroups * kVectors<T>, kDepth = kRingPlanes / kPlanes;
+  static constexpr int kGroups = 8 / sizeof(T), kPlanes = kGroups * kVectors<T>, kDepth = kRingPlanes<T> / kPlanes;
 };
 template <typename T>
 struct PassTwo {  // target and draft
   static constexpr int kGroups = 4 / sizeof(T), kDraft = kGroups * kVectors<T>,
-                       kPlanes = kDraft + kGroups * (kVectors<T> + 1), kDepth = kRingPlanes / kPlanes;
+                       kPlanes = kDraft + kGroups * (kVectors<T> + 1), kDepth = kRingPlanes<T> / kPlanes;
 };
-template <typename T>
-struct PassThree {  // target, exponentials, draft
-  static constexpr int kNoise = kVectors<T>, kDraft = kNoise + kVectors<float> + 1, kPlanes = kDraft + kVectors<T> + 1,
-                       kDepth = kRingPlanes / kPlanes;
+template <typename T, bool kWithDraft>
+struct PassRace {  // target, exponentials, draft
+  static constexpr int kNoise = kVectors<T>, kDraft = kNoise + kVectors<float> + 1,
+                       kPlanes = kDraft + (kWithDraft ? kVectors<T> + 1 : 0), kDepth = kRingPlanes<T> / kPlanes;
 };
 
 template <typename T>
@@ -412,17 +419,6 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         }
         at = __reduce_min_sync(0xffffffffu, at);
       }
-      if (d == (y ? 1 : 0)) {  // the likeliest node to come: its logits meanwhile
-        const uint32_t kids = __ballot_sync(0xffffffffu, kid);
-        primed = kids ? w1 + __ffs(kids) - 1 : -1;
-        if (primed >= 0) {
-          const T* child = static_cast<const T*>(p.logits) + (size_t)(q0 + primed) * p.logits_stride;
-          slice.shift = offset16(child + slice.begin) / (int)sizeof(T);
-          prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), [&](int k, uint8_t* slot) {
-            fetch<Pass::kGroups, false>(slot, child, slice, k, V);
-          });
-        }
-      }
       const float f = ex2_approx((m - wm) * c);
       z *= f;
       zl *= f;
@@ -433,7 +429,20 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         peer_store(to + 8, __float_as_uint(z), __float_as_uint(zl));
       }
     }
-    cluster_sync();
+    cluster_arrive();
+    {  // meanwhile the likeliest node to come: its logits
+      using Pass = PassOne<T>;
+      const uint32_t kids = __ballot_sync(0xffffffffu, kid);
+      primed = kids ? w1 + __ffs(kids) - 1 : -1;
+      if (primed >= 0) {
+        const T* child = static_cast<const T*>(p.logits) + (size_t)(q0 + primed) * p.logits_stride;
+        slice.shift = offset16(child + slice.begin) / (int)sizeof(T);
+        prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), [&](int k, uint8_t* slot) {
+          fetch<Pass::kGroups, false>(slot, child, slice, k, V);
+        });
+      }
+    }
+    cluster_wait();
 #pragma unroll
     for (int d = 0; d < 2; ++d) {
       if (d == 1 && !y) break;
@@ -571,15 +580,13 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         const uint64_t neg_x = pack_f32x2(-st[0].max, -st[0].max), neg_y = y ? pack_f32x2(-st[1].max, -st[1].max) : 0;
         const uint64_t ipp = pack_f32x2(ip, ip), fqq = pack_f32x2(-fq, -fq);
         slice.shift = offset16(x + slice.begin) / (int)sizeof(T);
-        using Pass = PassThree<T>;
-        const int off_e = Pass::kNoise * kThreads * 16, off_y = Pass::kDraft * kThreads * 16;
+        constexpr int off_e = PassRace<T, true>::kNoise * kThreads * 16, off_y = PassRace<T, true>::kDraft * kThreads * 16;
         auto issue = [&](int k, uint8_t* slot) {
           fetch<1, false>(slot, x, slice, k, V);
           fetch<1, true>(slot + off_e, noise, slice, k, V);
           if (fq > 0.f) fetch<1, true>(slot + off_y, y, slice, k, V);
         };
-        prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue);
-        stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue, [&](int k, uint8_t* slot) {
+        auto use = [&](int k, uint8_t* slot) {
           const int j = slice.group(slice.step(k, 1), 0);
           Raw<T> a;
           Raw<float> e;
@@ -623,7 +630,14 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
 #pragma unroll
             for (int i = 7; i >= 0; --i) best_at = v[i] == top ? j + i : best_at;
           }
-        });
+        };
+        auto run = [&](auto with_draft) {
+          using Pass = PassRace<T, decltype(with_draft)::value>;
+          prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue);
+          stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue, use);
+        };
+        if (fq > 0.f) run(std::true_type());
+        else run(std::false_type());
         uint64_t key = warp_best((uint64_t)__float_as_uint(best) << 32 | (uint32_t)~best_at);
         if (lane < (int)size) peer_store(peer_addr(&s.best[turn][mine], lane), (uint32_t)key, (uint32_t)(key >> 32));
         cluster_sync();
@@ -680,11 +694,11 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   // 2 257, 4 255, 8 308), but a step of the ring for each
   int size = 1;
   const int step = PassOne<__nv_bfloat16>::kGroups * 8 * kThreads;
-  while (size < kMaxCluster && (size < 2 || 2 * size * p.num_seqs <= 4 * sms) && 2 * size * step <= 2 * p.vocab) size *= 2;
+  while (size < kMaxCluster && (size < 4 || 2 * size * p.num_seqs <= 4 * sms) && 2 * size * step <= 2 * p.vocab) size *= 2;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(size * p.num_seqs);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kRingBytes;
+  cfg.dynamicSmemBytes = fp32 ? kRingBytes<float> : kRingBytes<__nv_bfloat16>;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -698,9 +712,11 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
 }
 
 cudaError_t prepare_verify_kernels() {
-  const cudaError_t e = cudaFuncSetAttribute(verify_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+  const cudaError_t e = cudaFuncSetAttribute(verify_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             kRingBytes<float>);
   if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(verify_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes);
+  return cudaFuncSetAttribute(verify_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              kRingBytes<__nv_bfloat16>);
 }
 
 }  // namespace mcpu
