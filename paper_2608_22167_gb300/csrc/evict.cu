@@ -53,33 +53,85 @@ struct EvictSmem {
   int32_t want;
 };
 
-// Exclusive prefix sum over the block, and the total. `turn` alternates between calls.
+// Sum of the warps' values before this one's, and of all. `turn` alternates between calls.
 template <typename S>
-__device__ __forceinline__ int block_scan(int x, S& s, int turn, int* total) {
+__device__ __forceinline__ int warps_scan(int x, S& s, int turn, int* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int incl = x;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += v;
-  }
-  if (lane == 31) s.scan[turn][warp] = incl;
+  if (lane == 0) s.scan[turn][warp] = x;
   __syncthreads();
-  const int w = lane < S::kWarps ? s.scan[turn][lane] : 0;
-  const int before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0);
-  *total = __reduce_add_sync(0xffffffffu, w);
-  return before + incl - x;
+  const int v = lane < S::kWarps ? s.scan[turn][lane] : 0;
+  *total = __reduce_add_sync(0xffffffffu, v);
+  return __reduce_add_sync(0xffffffffu, lane < warp ? v : 0);
+}
+
+struct Walk {  // of a region: next slot, slots at the cutoff so far, slots queued so far
+  int at, seen, have;
+};
+struct Ranks {
+  const float* w;
+  int first;
+  uint32_t cutoff;
+  int ties;
+  bool cached;
+};
+
+// Ranks the next kBlock slots of a region, a warp 32 neighbours at a time: those
+// kept (or the holes) go to the queue.
+template <typename S>
+__device__ __noinline__ Walk walk(S& s, const Ranks r, Walk region, int stop, bool holes, int turn) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int j = region.at + kPer * 32 * warp + lane, inside = min(region.at + S::kBlock, stop) - region.at;
+  const uint32_t below = (1u << lane) - 1u;
+  uint32_t u[kPer], above[kPer], same[kPer];  // the warp's slots above the cutoff, and at it
+  if (r.cached) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) u[e] = j + 32 * e < stop ? s.keys[j + 32 * e - r.first] : 0u;
+  } else {
+    float v[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) v[e] = j + 32 * e < stop ? __ldcg(r.w + j + 32 * e) : 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) u[e] = order(v[e]);
+  }
+  int counts = 0, all;  // above, and at << 16
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    const bool in = j + 32 * e < stop;
+    above[e] = __ballot_sync(0xffffffffu, in && u[e] > r.cutoff);
+    same[e] = __ballot_sync(0xffffffffu, in && u[e] == r.cutoff);
+    counts += __popc(above[e]) + (__popc(same[e]) << 16);
+  }
+  const int before = warps_scan(counts, s, turn, &all);
+  // of the slots at the cutoff as many are kept as are left of the ties
+  const int left = max(r.ties - region.seen, 0);
+  int equal = before >> 16, run = (before & 0xffff) + min(equal, left);  // kept before this warp's
+  if (holes) run = min(kPer * 32 * warp, inside) - run;
+  int32_t* queue = holes ? s.dst : s.src;
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {
+    uint32_t take = above[e];
+    if (same[e]) {  // (the same for the warp)
+      take |= __ballot_sync(0xffffffffu, (same[e] >> lane & 1u) && equal + __popc(same[e] & below) < left);
+      equal += __popc(same[e]);
+    }
+    if (holes) take = ~take & __ballot_sync(0xffffffffu, j + 32 * e < stop);
+    if (take >> lane & 1u) queue[(region.have + run + __popc(take & below)) % S::kQueue] = j + 32 * e;
+    run += __popc(take);
+  }
+  const int kept = (all & 0xffff) + min(all >> 16, left);
+  return Walk{region.at + S::kBlock, region.seen + (all >> 16), region.have + (holes ? inside - kept : kept)};
 }
 
 template <typename S>
 __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
     evict_kernel(const EvictParams p, const __grid_constant__ PoolPtrs pools) {
-  constexpr int kThreads = S::kThreads, kBlock = S::kBlock, kQueue = S::kQueue, kMoves = S::kMoves;
+  constexpr int kThreads = S::kThreads, kWarps = S::kWarps, kBlock = S::kBlock, kQueue = S::kQueue, kMoves = S::kMoves;
   extern __shared__ __align__(16) uint8_t smem[];
   S& s = *reinterpret_cast<S*>(smem);
   grid_dep_launch();
   grid_dep_wait();
   const int h = blockIdx.x, r = blockIdx.y, m = blockIdx.z, Hkv = p.num_kv_heads;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n = p.seq_lens[r];
   const bool speaks = h == 0 && m == 0 && threadIdx.x == 0;
   const int32_t* table = p.block_table + (size_t)r * p.max_pages;
@@ -116,6 +168,17 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
     for (int j = threadIdx.x; j < (cut ? first : n); j += kThreads) nw[j] = w[j];
   if (!cut) return;
 
+  const bool held = pages - page0 <= S::kTable;
+  auto page_of = [&](int slot) { return held ? s.table[slot / kPage - page0] : table[slot / kPage]; };
+  // a thread moves one 16-byte piece (of K or of V) of every kThreads / 16-th slot
+  constexpr int kLanes = kThreads / kRowVecs;
+  const int mine = threadIdx.x / kRowVecs, piece = threadIdx.x % kRowVecs;
+  uint8_t* base = pools.p[piece & 8 ? p.num_layers + m : m] + (size_t)h * kTileBytes + (piece & 7) * 16;
+  const int64_t page_bytes = (int64_t)Hkv * kTileBytes;
+  auto vec = [&](int slot) {
+    return reinterpret_cast<uint4*>(base + page_of(slot) * page_bytes + slot % kPage * kRowBytes);
+  };
+
   // ---- the K-th largest weight of the middle: its order, and how many that equal it stay
   uint32_t cutoff = 0xffffffffu;
   int ties = 0, turn = 0;
@@ -135,6 +198,7 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
           atomicAdd(&s.hist[(u >> shift) & ((1u << width) - 1u)], 1u);
       };
       if (cached && pass > 0) {
+#pragma unroll 4
         for (int j = threadIdx.x; j < end - first; j += kThreads) count(s.keys[j]);
       } else {
         for (int j0 = first + threadIdx.x; j0 < end; j0 += kLoads * kThreads) {
@@ -153,23 +217,36 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
         }
       }
       __syncthreads();
-      // bins from the highest down: thread t has bins kBins - 1 - 4 t ..
-      constexpr int kEach = kBins / kThreads;
-      int c[kEach], sum = 0, total;
+      // bins from the highest down: each warp has a range of them, and the one
+      // that holds the want-th key finds its bin, 32 at a time
+      constexpr int kRows = kBins / kThreads;
+      int c[kRows], sum = 0, total;
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        c[e] = s.hist[kBins - 1 - (kEach * threadIdx.x + e)];
+      for (int e = 0; e < kRows; ++e) {
+        c[e] = s.hist[kBins - 1 - 32 * (kRows * warp + e) - lane];
         sum += c[e];
       }
-      int before = block_scan(sum, s, turn, &total);
+      sum = __reduce_add_sync(0xffffffffu, sum);
+      int before = warps_scan(sum, s, turn, &total);
       turn ^= 1;
+      if (before < want && before + sum >= want) {
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        if (before < want && before + c[e] >= want) {
-          s.cutoff = prefix | (uint32_t)(kBins - 1 - (kEach * threadIdx.x + e)) << shift;
-          s.want = want - before;
+        for (int e = 0; e < kRows; ++e) {
+          const int row = __reduce_add_sync(0xffffffffu, c[e]);
+          if (before < want && before + row >= want) {
+            int incl = c[e];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+              const int v = __shfl_up_sync(0xffffffffu, incl, o);
+              if (lane >= o) incl += v;
+            }
+            if (before + incl - c[e] < want && before + incl >= want) {
+              s.cutoff = prefix | (uint32_t)(kBins - 1 - 32 * (kRows * warp + e) - lane) << shift;
+              s.want = want - (before + incl - c[e]);
+            }
+          }
+          before += row;
         }
-        before += c[e];
       }
       __syncthreads();
       prefix = s.cutoff;
@@ -180,70 +257,39 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
   }
 
   // ---- kept slots at or past inner fill the holes before it, in order
-  const bool held = pages - page0 <= S::kTable;
-  auto page_of = [&](int slot) { return held ? s.table[slot / kPage - page0] : table[slot / kPage]; };
-  const uint8_t *kp = pools.p[m], *vp = pools.p[p.num_layers + m];
-  auto vec = [&](int slot, int e) {  // 16-byte piece e of a slot's K and V
-    const size_t row = ((size_t)page_of(slot) * Hkv + h) * kPage + slot % kPage;
-    return reinterpret_cast<uint4*>(const_cast<uint8_t*>(e & 8 ? vp : kp) + row * kRowBytes) + (e & 7);
-  };
   int ties_before = 0;  // slots equal to the cutoff before inner
   if (K > 0) {
-    int mine = 0;
-    for (int j = first + threadIdx.x; j < inner; j += kThreads) mine += key(j) == cutoff;
-    block_scan(mine, s, turn, &ties_before);
+    int same = 0;
+#pragma unroll 4
+    for (int j = first + threadIdx.x; j < inner; j += kThreads) same += key(j) == cutoff;
+    warps_scan(__reduce_add_sync(0xffffffffu, same), s, turn, &ties_before);
     turn ^= 1;
   }
-  int ja = first, jb = inner, seen_a = 0, seen_b = ties_before, have_a = 0, have_b = 0, done = 0;
-  // ranks the next kBlock slots of a region: those kept (or the holes) go to the queue
-  auto walk = [&](int& j0, int stop, int& seen, int& have, bool holes, int32_t* queue) {
-    const int j = j0 + kPer * threadIdx.x;
-    uint32_t u[kPer];
-    int counts = 0, all;  // above the cutoff, and at it << 16
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      u[e] = j + e < stop ? key(j + e) : 0u;
-      if (j + e < stop) counts += u[e] > cutoff ? 1 : u[e] == cutoff ? 1 << 16 : 0;
-    }
-    const int before = block_scan(counts, s, turn, &all);
-    turn ^= 1;
-    // kept so far in this block: those above the cutoff, and of those at it as many as are left of the ties
-    const int left = max(ties - seen, 0), inside = min(j0 + kBlock, stop) - j0;
-    int eq = before >> 16, kept = (before & 0xffff) + min(eq, left);
-    int at = have + (holes ? min(kPer * (int)threadIdx.x, inside) - kept : kept);
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      if (j + e >= stop) continue;
-      const bool keep = u[e] > cutoff || (u[e] == cutoff && eq++ < left);
-      if (keep != holes) queue[at++ % kQueue] = j + e;
-    }
-    kept = (all & 0xffff) + min(all >> 16, left);
-    seen += all >> 16;
-    all = holes ? inside - kept : kept;
-    have += all;
-    j0 += kBlock;
-  };
+  Walk a{first, 0, 0}, b{inner, ties_before, 0};
+  const Ranks ranks{w, first, cutoff, ties, cached};
+  int done = 0;
 #pragma unroll 1
   while (K > 0) {
-    while (have_b - done < kMoves && jb < end) walk(jb, end, seen_b, have_b, false, s.src);
-    if (have_b == done) break;
-    while (have_a - done < min(kMoves, have_b - done) && ja < inner) walk(ja, inner, seen_a, have_a, true, s.dst);
+    while (true) {  // kept slots for the next moves, then as many holes
+      const bool holes = b.have - done >= kMoves || b.at >= end;
+      if (holes && (a.have >= min(done + kMoves, b.have) || a.at >= inner)) break;
+      if (holes) a = walk(s, ranks, a, inner, true, turn);
+      else b = walk(s, ranks, b, end, false, turn);
+      turn ^= 1;
+    }
     __syncthreads();
-    const int count = min(min(have_a, have_b) - done, kMoves);
+    const int count = min(min(a.have, b.have) - done, kMoves);
     if (count <= 0) break;
     constexpr int kFlight = 8;
-    for (int e0 = threadIdx.x; e0 < count * kRowVecs; e0 += kFlight * kThreads) {
+#pragma unroll 1
+    for (int i0 = mine; i0 < count; i0 += kFlight * kLanes) {
       uint4 v[kFlight];
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) {
-        const int e = e0 + k * kThreads;
-        if (e < count * kRowVecs) v[k] = __ldcs(vec(s.src[(done + e / kRowVecs) % kQueue], e % kRowVecs));
-      }
+      for (int k = 0; k < kFlight; ++k)
+        if (i0 + k * kLanes < count) v[k] = __ldcs(vec(s.src[(done + i0 + k * kLanes) % kQueue]));
 #pragma unroll
-      for (int k = 0; k < kFlight; ++k) {
-        const int e = e0 + k * kThreads;
-        if (e < count * kRowVecs) *vec(s.dst[(done + e / kRowVecs) % kQueue], e % kRowVecs) = v[k];
-      }
+      for (int k = 0; k < kFlight; ++k)
+        if (i0 + k * kLanes < count) *vec(s.dst[(done + i0 + k * kLanes) % kQueue]) = v[k];
     }
     for (int e = threadIdx.x; e < count; e += kThreads) nw[s.dst[(done + e) % kQueue]] = w[s.src[(done + e) % kQueue]];
     done += count;
@@ -252,7 +298,7 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
 
   // ---- the last ones, towards the front: a piece of them at a time, read before it is written
   __syncthreads();
-  constexpr int kHeld = 8, kPiece = kHeld * kThreads / kRowVecs;
+  constexpr int kHeld = 8, kPiece = kHeld * kLanes;
   const bool apart = n - p.budget >= p.last;  // they do not overlap their new places
 #pragma unroll 1
   for (int i0 = 0; i0 < p.last; i0 += kPiece) {
@@ -260,17 +306,13 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
     uint4 v[kHeld];
     float weight = 0.f;
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) {
-      const int e = threadIdx.x + k * kThreads;
-      if (e < count * kRowVecs) v[k] = __ldcs(vec(end + i0 + e / kRowVecs, e % kRowVecs));
-    }
+    for (int k = 0; k < kHeld; ++k)
+      if (mine + k * kLanes < count) v[k] = __ldcs(vec(end + i0 + mine + k * kLanes));
     if (threadIdx.x < count) weight = w[end + i0 + threadIdx.x];
     if (!apart) __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k) {
-      const int e = threadIdx.x + k * kThreads;
-      if (e < count * kRowVecs) *vec(inner + i0 + e / kRowVecs, e % kRowVecs) = v[k];
-    }
+    for (int k = 0; k < kHeld; ++k)
+      if (mine + k * kLanes < count) *vec(inner + i0 + mine + k * kLanes) = v[k];
     if (threadIdx.x < count) nw[inner + i0 + threadIdx.x] = weight;
     if (!apart) __syncthreads();
   }
