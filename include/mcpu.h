@@ -548,7 +548,8 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
  * more than MCPU_MAX_TREE_NODES (MCPU_ERR_UNSUPPORTED_ROW) or inconsistent
  * query_start_loc (MCPU_ERR_BAD_LENGTHS).
  * logits, draft_logits: logits_type MCPU_BF16 or MCPU_FP32 elements, any
- * stride >= vocab. Sums and probabilities are fp32, the tests of children fp64.
+ * stride >= vocab. Sums and probabilities are fp32 (sums exact to about 2^-22), so
+ * that a draw within 1e-6 of a border may fall on either side of it.
  */
 #define MCPU_MAX_TREE_NODES 256
 #define MCPU_BF16 0
@@ -659,15 +660,16 @@ mcpu_status mcpu_copy_pages(void* const* pools, int32_t num_pools, int64_t page_
  * row, 0 .. L_r - 1), C_r = S_r - path_len[r]: the accepted nodes once
  * mcpu_compact_kv has moved them (with its new_seq_lens), or the last queries of
  * a long prompt alone.
- * decay in [0, 1]; 0 reads no old weights. A row without queries keeps its
- * weights as they are, and so do slots from S_r on. A query with lse = -inf (it
- * saw nothing) adds nothing; a NaN among a key or a query that sees it makes that
- * key's weight NaN. A row longer than max_slots or its table, or with a path
+ * decay in [0, 1]; 0 reads no old weights. softmax_scale in [1e-30, 1e30]. A row
+ * without queries keeps its weights as they are, and so do slots from S_r on. A
+ * query with lse = -inf (it saw nothing) or inf adds nothing to finite keys; a NaN
+ * of a key, or of a query that sees it or its lse, makes that key's weight NaN. A row longer than max_slots or its table, or with a path
  * that breaks the rules, is skipped (MCPU_ERR_BAD_LENGTHS); keys of a page
  * outside the pool keep their weights (MCPU_ERR_BAD_PAGE).
  * Sums are fp32 in a fixed order: the same inputs give the same bits on the
  * same device. workspace: mcpu_weights_workspace_size(dims) bytes, 256-byte
- * aligned, the status word first (zero it once). Capturable.
+ * aligned, the status word first (zero it once); calls that share one must be
+ * ordered. Capturable.
  *
  * mcpu_evict_kv: every row with S_r > limit is cut to budget slots, for each
  * layer m and kv head h by key_weights (float [num_layers, num_seqs, H_kv,

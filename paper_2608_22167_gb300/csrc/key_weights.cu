@@ -86,7 +86,7 @@ struct RowGeom {
   __device__ __forceinline__ void blocks(int u, int* b0, int* b1) const {
     const int k0 = u * kUnitKeys, last = min(k0 + kUnitKeys, S) - 1;
     const int i0 = max(0, k0 - C);
-    const int i1 = window > 0 ? min(n, last - C + window) : n;
+    const int i1 = window > 0 ? (int)min((int64_t)n, (int64_t)last - C + window) : n;
     *b0 = i0 / tok;
     *b1 = i1 > i0 ? (i1 + tok - 1) / tok : *b0;
   }

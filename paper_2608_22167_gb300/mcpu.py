@@ -801,6 +801,13 @@ _accumulate_weights = _lib.mcpu_accumulate_weights
 _evict_kv = _lib.mcpu_evict_kv
 
 
+def _on_one_device(*tensors):
+    """Tensors (or None) of a call on the current CUDA device: on another, or the host, the kernels would fault."""
+    where = {x.get_device() for x in tensors if x is not None}
+    if len(where) != 1 or -1 in where or _current_device() not in where:
+        raise ValueError("every tensor must be on the current CUDA device")
+
+
 def _row_stride(x, what, dtypes, rows, width):
     """Elements from one row to the next of a [rows, width] tensor whose rows are dense."""
     if x.dtype not in dtypes or x.dim() != 2 or x.shape[0] != rows or x.shape[1] != width or \
@@ -838,23 +845,28 @@ def mcpu_verify_tree(logits, tokens, parents, query_start_loc, temperature, unif
     if temperature is not None:
         if uniforms is None or exponentials is None:
             raise ValueError("sampling needs uniforms and exponentials")
+        given = (temperature, uniforms, exponentials)
         es = _row_stride(exponentials, "exponentials", (_FP32,), rows, vocab)
         temperature = _vector(temperature, "temperature", _FP32, rows)
         uniforms = _vector(uniforms, "uniforms", _FP32, t)
         exponentials = exponentials.data_ptr()
     else:
         uniforms = exponentials = None
+        given = ()
+    given += (logits, draft_logits, tokens, parents, query_start_loc, accept_path, accept_len, next_token, logprobs,
+              status_word)
     if logprobs is not None:
         if logprobs.dtype is not _FP32 or logprobs.shape != (rows, most) or not logprobs.is_contiguous():
             raise ValueError("logprobs must be a contiguous float32 tensor of accept_path's shape")
         logprobs = logprobs.data_ptr()
-    code = _verify_tree(
-        logits.data_ptr(), ls, None if draft_logits is None else draft_logits.data_ptr(), ds,
-        0 if logits.dtype is _BF16 else 1, vocab, _vector(tokens, "tokens", _INT32, t),
-        _vector(parents, "parents", _INT32, t), _int32(query_start_loc, "query_start_loc"), temperature, uniforms,
-        exponentials, es, rows, t, most, _int32(accept_path, "accept_path"),
-        _vector(accept_len, "accept_len", _INT32, rows), _vector(next_token, "next_token", _INT32, rows), logprobs,
-        _int32(status_word, "status_word"), _raw_stream(stream))
+    args = (logits.data_ptr(), ls, None if draft_logits is None else draft_logits.data_ptr(), ds,
+            0 if logits.dtype is _BF16 else 1, vocab, _vector(tokens, "tokens", _INT32, t),
+            _vector(parents, "parents", _INT32, t), _int32(query_start_loc, "query_start_loc"), temperature, uniforms,
+            exponentials, es, rows, t, most, _int32(accept_path, "accept_path"),
+            _vector(accept_len, "accept_len", _INT32, rows), _vector(next_token, "next_token", _INT32, rows), logprobs,
+            _int32(status_word, "status_word"))
+    _on_one_device(*given)
+    code = _verify_tree(*args, _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_verify_tree")
 
@@ -890,17 +902,18 @@ def mcpu_accumulate_weights(q, lse, k_cache, block_table, seq_lens, query_start_
     if key_weights.dtype is not _FP32 or key_weights.dim() != 3 or key_weights.shape[:2] != (rows, hkv) or \
             not key_weights.is_contiguous():
         raise ValueError("key_weights must be a contiguous float32 [B, H_kv, max_slots] tensor")
-    most = 0
+    most, path_ptr, len_ptr = 0, None, None
     if query_path is not None:
-        if path_len is None or query_path.dim() != 2 or query_path.shape[0] != rows:
+        if path_len is None or query_path.dim() != 2 or query_path.shape[0] != rows or query_path.shape[1] < 1:
             raise ValueError("query_path must be an int32 [B, max_path] tensor, with path_len")
         most = query_path.shape[1]
-        query_path, path_len = _int32(query_path, "query_path"), _vector(path_len, "path_len", _INT32, rows)
+        path_ptr, len_ptr = _int32(query_path, "query_path"), _vector(path_len, "path_len", _INT32, rows)
     elif path_len is not None:
         raise ValueError("path_len comes with query_path")
+    _on_one_device(q, lse, k_cache, block_table, seq_lens, query_start_loc, key_weights, workspace, query_path, path_len)
     code = _accumulate_weights(
         q.data_ptr(), lse.data_ptr(), k_cache.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
-        query_start_loc.data_ptr(), query_path, most, path_len, sliding_window, softmax_scale, decay,
+        query_start_loc.data_ptr(), path_ptr, most, len_ptr, sliding_window, softmax_scale, decay,
         _pack_dims(rows, t, width, pages, hq, hkv, d, page), key_weights.data_ptr(), key_weights.shape[2],
         workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(stream))
     if code:
@@ -931,11 +944,12 @@ def mcpu_evict_kv(pools, key_weights, block_table, seq_lens, limit, budget, keep
     old, new = key_weights.data_ptr(), new_key_weights.data_ptr()
     if old != new and abs(old - new) < 4 * key_weights.numel():
         raise ValueError("new_key_weights must be key_weights or apart from it")
-    if page_refs is not None:
-        page_refs = _vector(page_refs, "page_refs", _INT32, pools.num_pages)
+    refs = None if page_refs is None else _vector(page_refs, "page_refs", _INT32, pools.num_pages)
+    new_lens, status = _vector(new_seq_lens, "new_seq_lens", _INT32, rows), _int32(status_word, "status_word")
+    _on_one_device(pools.pools[0], key_weights, block_table, seq_lens, new_key_weights, new_seq_lens, status_word, page_refs)
     code = _evict_kv(
         pools.pointers, layers, old, shape[3], block_table.data_ptr(), seq_lens.data_ptr(), limit, budget, keep_first,
-        keep_last, page_refs, _pack_dims(rows, 0, width, pools.num_pages, hkv, hkv, 64, 16), new,
-        _vector(new_seq_lens, "new_seq_lens", _INT32, rows), _int32(status_word, "status_word"), _raw_stream(stream))
+        keep_last, refs, _pack_dims(rows, 0, width, pools.num_pages, hkv, hkv, 64, 16), new, new_lens, status,
+        _raw_stream(stream))
     if code:
         raise McpuError(code, "mcpu_evict_kv")
