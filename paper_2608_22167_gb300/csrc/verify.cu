@@ -282,6 +282,87 @@ __device__ __forceinline__ float top_of(const Raw<T>& v) {
   return top;
 }
 
+// What all warps of the cluster have of a distribution, joined in their order.
+__device__ __forceinline__ Stats join_stats(const Stats* part, int parts, float c) {
+  const int lane = threadIdx.x & 31;
+  float m = kLowest, z = 0.f, zl = 0.f;
+  int at = 0x7fffffff;
+  for (int i = lane; i < parts; i += 32) {
+    const Stats o = part[i];
+    if (o.max > m || (o.max == m && o.at < at)) m = o.max, at = o.at;
+  }
+  warp_max(m, at);
+  for (int i = lane; i < parts; i += 32) {
+    const Stats o = part[i];
+    const float f = ex2_approx((o.max - m) * c);
+    add_exact(z, zl, o.sum * f);
+    zl += o.low * f;
+  }
+  warp_add_exact(z, zl);
+  return Stats{m, at, z, zl};
+}
+
+// Adds kN groups of a row to its running maximum and sum relative to it.
+template <typename T, int kN>
+__device__ __forceinline__ bool add_groups(const Raw<T> (&v)[kN], float c, float& m, float& z, float& zl, float* scaled) {
+  float top = top_of(v[0]);
+#pragma unroll
+  for (int e = 1; e < kN; ++e) top = fmaxf(top, top_of(v[e]));
+  const bool rises = top > m;
+  if (rises) {
+    const float f = ex2_approx((m - top) * c);
+    z *= f;
+    zl *= f;
+    *scaled *= f;
+    m = top;
+  }
+  const uint64_t neg = pack_f32x2(-m, -m), cc = pack_f32x2(c, c);
+  uint64_t sum[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < kN; ++e)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i & 1] = add2(sum[i & 1], weights2(v[e], i, neg, cc));
+  sum[0] = add2(sum[0], sum[1]);
+  add_exact(z, zl, lo_f32(sum[0]) + hi_f32(sum[0]));
+  return rises;
+}
+
+// Lets the eight tokens from j on into the race: rest / e > best where
+// rest - best e > 0, so no division but for what comes to lead. Tokens of the
+// `lost` rejected children do not take part.
+__device__ __forceinline__ void race8(const uint64_t (&rest)[4], const Raw<float>& e, int j, const VerifySmem& s, int lost,
+                                      float& best, int& best_at) {
+  const uint64_t neg_best = pack_f32x2(-best, -best);
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint64_t lead = fma2(pack_f32x2(e.get(2 * i), e.get(2 * i + 1)), neg_best, rest[i]);
+    top = fmax3(top, lo_f32(lead), hi_f32(lead));
+  }
+  if (!(top > 0.f)) return;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float w = i & 1 ? hi_f32(rest[i >> 1]) : lo_f32(rest[i >> 1]);
+    v[i] = w > 0.f ? __fdividef(w, e.get(i)) : 0.f;
+  }
+  for (int g = 0; g < lost; ++g) {
+    const int i = s.gone[g] - j;
+    if (i >= 0 && i < 8) {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) v[d] = d == i ? 0.f : v[d];
+    }
+  }
+  top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) top = fmax3(top, v[i], v[i + 1]);
+  if (top > best) {
+    best = top;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) best_at = v[i] == top ? j + i : best_at;
+  }
+}
+
 // The ring, and what a pass makes of it: groups a step, planes, steps in flight.
 // 60 KiB leave room for three blocks on an SM; the draft's fp32 logits with the
 // exponentials need 64 for two steps.
@@ -334,7 +415,8 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
   slice.end = min(V, slice.begin + per);
   const float* noise = greedy ? nullptr : p.noise + (size_t)r * p.noise_stride;
   uint32_t turn = 0;  // of the exchange buffers
-  int primed = -1;    // node whose first logits are on their way into the ring
+  int primed = -1;    // node whose first logits are on their way into the ring,
+  bool primed_race = false;  // for the race
   cluster_wait();
 
   while (walks && !bad) {
@@ -349,65 +431,128 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
       token = p.tokens[q0 + w1 + lane];
       if (!greedy) u = p.uniforms[q0 + w1 + lane];
     }
+    const bool more = len < p.max_accept, token_ok = token >= 0 && token < V;
+    bool kid = more && up == cur && w1 + lane > cur && token_ok;
+    auto row_of = [&](const void* base, int64_t stride, int node) {
+      return static_cast<const T*>(base) + (size_t)(q0 + node) * stride;
+    };
+
+    // ---- a sampled node without children: its sums and the race in one pass
+    bool leaf = !greedy && !__any_sync(0xffffffffu, kid);
+    for (int w0 = w1 + 32; w0 < L && leaf && more; w0 += 32) {
+      const int t = w0 + lane < L && p.parents[q0 + w0 + lane] == cur ? p.tokens[q0 + w0 + lane] : -1;
+      leaf = !__any_sync(0xffffffffu, t >= 0 && t < V);
+    }
+    if (leaf) {
+      using Pass = PassRace<T, false>;
+      constexpr int off_e = Pass::kNoise * kThreads * 16;
+      float m = kLowest, z = 0.f, zl = 0.f, best = 0.f;
+      int best_at = 0x7fffffff;
+      slice.shift = offset16(x + slice.begin) / (int)sizeof(T);
+      auto issue = [&](int k, uint8_t* slot) {
+        fetch<1, false>(slot, x, slice, k, V);
+        fetch<1, true>(slot + off_e, noise, slice, k, V);
+      };
+      if (primed != cur || !primed_race) prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue);
+      stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue, [&](int k, uint8_t* slot) {
+        Raw<T> v[1];
+        Raw<float> e;
+        take<1, false>(slot, x, slice, k, 0, kNegInf<T>, v[0]);
+        take<1, true>(slot + off_e, noise, slice, k, 0, 0x3f800000u, e);
+        add_groups(v, c, m, z, zl, &best);
+        const uint64_t neg = pack_f32x2(-m, -m);
+        uint64_t rest[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) rest[i] = weights2(v[0], i, neg, cc);
+        race8(rest, e, slice.group(slice.step(k, 1), 0), s, 0, best, best_at);
+      });
+      const float wm = warp_max(m), f = ex2_approx((m - wm) * c);
+      z *= f;
+      zl *= f;
+      warp_add_exact(z, zl);
+      const uint64_t lead = warp_best((uint64_t)__float_as_uint(best * f) << 32 | (uint32_t)~best_at);
+      if (lane < (int)size) {
+        const uint32_t to = peer_addr(&s.stats[turn][0][mine], lane);
+        peer_store(to, __float_as_uint(wm), 0x7fffffffu);
+        peer_store(to + 8, __float_as_uint(z), __float_as_uint(zl));
+        peer_store(peer_addr(&s.best[turn][mine], lane), (uint32_t)lead, (uint32_t)(lead >> 32));
+      }
+      cluster_sync();
+      const Stats st = join_stats(s.stats[turn][0], parts, c);
+      uint64_t key = 0;
+      for (int i = lane; i < parts; i += 32) {
+        const uint64_t o = s.best[turn][i];
+        const float v = __uint_as_float((uint32_t)(o >> 32)) * ex2_approx((s.stats[turn][0][i].max - st.max) * c);
+        key = max(key, (uint64_t)__float_as_uint(v) << 32 | (uint32_t)o);
+      }
+      key = warp_best(key);
+      bad = !(st.sum > 0.f && st.sum < 3e38f) || !(key >> 32);
+      if (!bad) next = (int)~(uint32_t)key;
+      if (threadIdx.x == 0) {
+        s.out[len - 1] = max(next, 0);
+        s.node[len - 1] = st;
+      }
+      break;
+    }
+
     // ---- maximum and sum of the node's distributions
     Stats st[2];
-    float lx = 0.f, ly = 0.f;  // the child's own logits
-    bool kid = false;
-#pragma unroll 1
-    for (int d = 0; d < (y ? 2 : 1); ++d) {
-      using Pass = PassOne<T>;
-      const T* row = d ? y : x;
-      slice.shift = offset16(row + slice.begin) / (int)sizeof(T);
-      float m = kLowest, z = 0.f, zl = 0.f;
-      int best_step = 0;  // that holds the thread's maximum
-      auto issue = [&](int k, uint8_t* slot) { fetch<Pass::kGroups, false>(slot, row, slice, k, V); };
-      if (d == 1 || primed != cur) prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), issue);
-      stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), issue, [&](int k, uint8_t* slot) {
-        Raw<T> v[Pass::kGroups];
+    using One = PassOne<T>;
+    using Two = PassTwo<T>;
+    float m[2] = {kLowest, kLowest}, z[2] = {0.f, 0.f}, zl[2] = {0.f, 0.f}, none = 0.f;
+    int best_step = 0;  // that holds the thread's maximum
+    slice.shift = offset16(x + slice.begin) / (int)sizeof(T);
+    const bool ready = primed == cur && !primed_race;
+    if (!y) {
+      auto issue = [&](int k, uint8_t* slot) { fetch<One::kGroups, false>(slot, x, slice, k, V); };
+      if (!ready) prime<One::kDepth>(ring, One::kPlanes, slice.steps(One::kGroups), issue);
+      stream<One::kDepth>(ring, One::kPlanes, slice.steps(One::kGroups), issue, [&](int k, uint8_t* slot) {
+        Raw<T> v[One::kGroups];
 #pragma unroll
-        for (int e = 0; e < Pass::kGroups; ++e) take<Pass::kGroups, false>(slot, row, slice, k, e, kNegInf<T>, v[e]);
-        float top = top_of(v[0]);
-#pragma unroll
-        for (int e = 1; e < Pass::kGroups; ++e) top = fmaxf(top, top_of(v[e]));
-        if (top > m) {
-          const float f = ex2_approx((m - top) * c);
-          z *= f;
-          zl *= f;
-          m = top;
-          best_step = k;
-        }
-        const uint64_t neg = pack_f32x2(-m, -m);
-        uint64_t sum[2] = {0, 0};
-#pragma unroll
-        for (int e = 0; e < Pass::kGroups; ++e)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sum[i & 1] = add2(sum[i & 1], weights2(v[e], i, neg, cc));
-        sum[0] = add2(sum[0], sum[1]);
-        add_exact(z, zl, lo_f32(sum[0]) + hi_f32(sum[0]));
+        for (int e = 0; e < One::kGroups; ++e) take<One::kGroups, false>(slot, x, slice, k, e, kNegInf<T>, v[e]);
+        if (add_groups(v, c, m[0], z[0], zl[0], &none)) best_step = k;
       });
-      if (d == 0) {
-        kid = up == cur && w1 + lane > cur && token >= 0 && token < V && len < p.max_accept;
-        if (kid) {
-          lx = at_token(x, token);
-          if (y) ly = at_token(y, token);
-        }
-      }
-      const float wm = warp_max(m);
+    } else {
+      auto issue = [&](int k, uint8_t* slot) {
+        fetch<Two::kGroups, false>(slot, x, slice, k, V);
+        fetch<Two::kGroups, true>(slot + Two::kDraft * kThreads * 16, y, slice, k, V);
+      };
+      if (!ready) prime<Two::kDepth>(ring, Two::kPlanes, slice.steps(Two::kGroups), issue);
+      stream<Two::kDepth>(ring, Two::kPlanes, slice.steps(Two::kGroups), issue, [&](int k, uint8_t* slot) {
+        Raw<T> v[Two::kGroups];
+#pragma unroll
+        for (int e = 0; e < Two::kGroups; ++e) take<Two::kGroups, false>(slot, x, slice, k, e, kNegInf<T>, v[e]);
+        add_groups(v, c, m[0], z[0], zl[0], &none);
+#pragma unroll
+        for (int e = 0; e < Two::kGroups; ++e)
+          take<Two::kGroups, true>(slot + Two::kDraft * kThreads * 16, y, slice, k, e, kNegInf<T>, v[e]);
+        add_groups(v, c, m[1], z[1], zl[1], &none);
+      });
+    }
+    float lx = 0.f, ly = 0.f;  // the child's own logits
+    if (kid) {
+      lx = at_token(x, token);
+      if (y) ly = at_token(y, token);
+    }
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      if (d == 1 && !y) break;
+      const float wm = warp_max(m[d]);
       int at = 0x7fffffff;
       if (greedy) {
-        if (m == wm) {  // the lowest token that has it, among this thread's of that step
-          const bool held = best_step >= slice.steps(Pass::kGroups) - Pass::kDepth;  // it is in the ring still
-          uint8_t* slot = ring + best_step % Pass::kDepth * Pass::kPlanes * kThreads * 16;
+        if (m[d] == wm) {  // the lowest token that has it, among this thread's of that step
+          const bool held = best_step >= slice.steps(One::kGroups) - One::kDepth;  // it is in the ring still
+          uint8_t* slot = ring + best_step % One::kDepth * One::kPlanes * kThreads * 16;
 #pragma unroll 1
-          for (int e = Pass::kGroups - 1; e >= 0; --e) {
-            const int j = slice.group(slice.step(best_step, Pass::kGroups), e);
+          for (int e = One::kGroups - 1; e >= 0; --e) {
+            const int j = slice.group(slice.step(best_step, One::kGroups), e);
             Raw<T> v;
             if (held) {
-              take<Pass::kGroups, false>(slot, row, slice, best_step, e, kNegInf<T>, v);
+              take<One::kGroups, false>(slot, x, slice, best_step, e, kNegInf<T>, v);
             } else {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
-                const float l = j + i >= slice.begin && j + i < slice.end ? at_token(row, j + i) : -INFINITY;
+                const float l = j + i >= slice.begin && j + i < slice.end ? at_token(x, j + i) : -INFINITY;
                 if (sizeof(T) == 4) v.w[i] = __float_as_uint(l);
                 else if (i & 1) v.w[i >> 1] |= __float_as_uint(l) & 0xffff0000u;
                 else v.w[i >> 1] = __float_as_uint(l) >> 16;
@@ -419,49 +564,51 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         }
         at = __reduce_min_sync(0xffffffffu, at);
       }
-      const float f = ex2_approx((m - wm) * c);
-      z *= f;
-      zl *= f;
-      warp_add_exact(z, zl);
+      const float f = ex2_approx((m[d] - wm) * c);
+      z[d] *= f;
+      zl[d] *= f;
+      warp_add_exact(z[d], zl[d]);
       if (lane < (int)size) {
         const uint32_t to = peer_addr(&s.stats[turn][d][mine], lane);
         peer_store(to, __float_as_uint(wm), (uint32_t)at);
-        peer_store(to + 8, __float_as_uint(z), __float_as_uint(zl));
+        peer_store(to + 8, __float_as_uint(z[d]), __float_as_uint(zl[d]));
       }
     }
     cluster_arrive();
-    {  // meanwhile the likeliest node to come: its logits
-      using Pass = PassOne<T>;
+    {  // meanwhile the likeliest node to come: its logits (and, if it is known to have no children, the exponentials)
       const uint32_t kids = __ballot_sync(0xffffffffu, kid);
       primed = kids ? w1 + __ffs(kids) - 1 : -1;
+      const bool known = L <= w1 + 32 || len + 1 >= p.max_accept;
+      primed_race = !greedy && known &&
+                    (len + 1 >= p.max_accept || !__any_sync(0xffffffffu, up == primed && w1 + lane > primed && token_ok));
       if (primed >= 0) {
-        const T* child = static_cast<const T*>(p.logits) + (size_t)(q0 + primed) * p.logits_stride;
-        slice.shift = offset16(child + slice.begin) / (int)sizeof(T);
-        prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), [&](int k, uint8_t* slot) {
-          fetch<Pass::kGroups, false>(slot, child, slice, k, V);
-        });
+        const T* cx = row_of(p.logits, p.logits_stride, primed);
+        const T* cy = row_of(p.draft, p.draft_stride, primed);
+        slice.shift = offset16(cx + slice.begin) / (int)sizeof(T);
+        if (primed_race) {
+          using Pass = PassRace<T, false>;
+          prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), [&](int k, uint8_t* slot) {
+            fetch<1, false>(slot, cx, slice, k, V);
+            fetch<1, true>(slot + Pass::kNoise * kThreads * 16, noise, slice, k, V);
+          });
+        } else if (y) {
+          prime<Two::kDepth>(ring, Two::kPlanes, slice.steps(Two::kGroups), [&](int k, uint8_t* slot) {
+            fetch<Two::kGroups, false>(slot, cx, slice, k, V);
+            fetch<Two::kGroups, true>(slot + Two::kDraft * kThreads * 16, cy, slice, k, V);
+          });
+        } else {
+          prime<One::kDepth>(ring, One::kPlanes, slice.steps(One::kGroups), [&](int k, uint8_t* slot) {
+            fetch<One::kGroups, false>(slot, cx, slice, k, V);
+          });
+        }
       }
     }
     cluster_wait();
 #pragma unroll
     for (int d = 0; d < 2; ++d) {
       if (d == 1 && !y) break;
-      float m = kLowest, z = 0.f, zl = 0.f;
-      int at = 0x7fffffff;
-      for (int i = lane; i < parts; i += 32) {
-        const Stats o = s.stats[turn][d][i];
-        if (o.max > m || (o.max == m && o.at < at)) m = o.max, at = o.at;
-      }
-      warp_max(m, at);
-      for (int i = lane; i < parts; i += 32) {
-        const Stats o = s.stats[turn][d][i];
-        const float f = ex2_approx((o.max - m) * c);
-        add_exact(z, zl, o.sum * f);
-        zl += o.low * f;
-      }
-      warp_add_exact(z, zl);
-      st[d] = Stats{m, at, z, zl};
-      bad |= !(z > 0.f && z < 3e38f);  // no token, NaN or +inf
+      st[d] = join_stats(s.stats[turn][d], parts, c);
+      bad |= !(st[d].sum > 0.f && st[d].sum < 3e38f);  // no token, NaN or +inf
     }
     turn ^= 1;
     if (bad) break;
@@ -600,36 +747,7 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
 #pragma unroll
             for (int i = 0; i < 4; ++i) rest[i] = fma2(weights2(a, i, neg_y, cc), fqq, mul2(rest[i], ipp));
           }
-          // rest / e > best where rest - best e > 0: no division but for what comes to lead
-          const uint64_t neg_best = pack_f32x2(-best, -best);
-          float top = 0.f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint64_t lead = fma2(pack_f32x2(e.get(2 * i), e.get(2 * i + 1)), neg_best, rest[i]);
-            top = fmax3(top, lo_f32(lead), hi_f32(lead));
-          }
-          if (!(top > 0.f)) return;
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float w = i & 1 ? hi_f32(rest[i >> 1]) : lo_f32(rest[i >> 1]);
-            v[i] = w > 0.f ? __fdividef(w, e.get(i)) : 0.f;
-          }
-          for (int g = 0; g < lost; ++g) {  // tokens of rejected children do not take part
-            const int i = s.gone[g] - j;
-            if (i >= 0 && i < 8) {
-#pragma unroll
-              for (int d = 0; d < 8; ++d) v[d] = d == i ? 0.f : v[d];
-            }
-          }
-          top = 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; i += 2) top = fmax3(top, v[i], v[i + 1]);
-          if (top > best) {
-            best = top;
-#pragma unroll
-            for (int i = 7; i >= 0; --i) best_at = v[i] == top ? j + i : best_at;
-          }
+          race8(rest, e, j, s, lost, best, best_at);
         };
         auto run = [&](auto with_draft) {
           using Pass = PassRace<T, decltype(with_draft)::value>;
