@@ -364,26 +364,29 @@ __device__ __forceinline__ void race8(const uint64_t (&rest)[4], const Raw<float
 }
 
 // The ring, and what a pass makes of it: groups a step, planes, steps in flight.
-// 60 KiB leave room for three blocks on an SM; the draft's fp32 logits with the
-// exponentials need 64 for two steps.
-template <typename T>
-constexpr int kRingPlanes = sizeof(T) == 2 ? 15 : 16;
-template <typename T>
-constexpr int kRingBytes = kRingPlanes<T> * 16 * kThreads;
+// 60 KiB leave room for three blocks on an SM; only fp32 logits of both
+// distributions with the exponentials need 64, for two steps.
+constexpr int kRingPlanes = 15, kPlaneBytes = 16 * kThreads;
 template <typename T>
 struct PassOne {  // one row
-  static constexpr int kGroups = 8 / sizeof(T), kPlanes = kGroups * kVectors<T>, kDepth = kRingPlanes<T> / kPlanes;
+  static constexpr int kGroups = 8 / sizeof(T), kPlanes = kGroups * kVectors<T>, kDepth = kRingPlanes / kPlanes;
 };
 template <typename T>
 struct PassTwo {  // target and draft
   static constexpr int kGroups = 4 / sizeof(T), kDraft = kGroups * kVectors<T>,
-                       kPlanes = kDraft + kGroups * (kVectors<T> + 1), kDepth = kRingPlanes<T> / kPlanes;
+                       kPlanes = kDraft + kGroups * (kVectors<T> + 1), kDepth = kRingPlanes / kPlanes;
 };
 template <typename T, bool kWithDraft>
 struct PassRace {  // target, exponentials, draft
   static constexpr int kNoise = kVectors<T>, kDraft = kNoise + kVectors<float> + 1,
-                       kPlanes = kDraft + (kWithDraft ? kVectors<T> + 1 : 0), kDepth = kRingPlanes<T> / kPlanes;
+                       kPlanes = kDraft + (kWithDraft ? kVectors<T> + 1 : 0),
+                       kDepth = kRingPlanes / kPlanes > 2 ? kRingPlanes / kPlanes : 2;
 };
+
+template <typename T>
+constexpr int ring_bytes(bool draft) {
+  return kPlaneBytes * (draft && 2 * PassRace<T, true>::kPlanes > kRingPlanes ? 2 * PassRace<T, true>::kPlanes : kRingPlanes);
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams p) {
@@ -816,7 +819,7 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(size * p.num_seqs);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = fp32 ? kRingBytes<float> : kRingBytes<__nv_bfloat16>;
+  cfg.dynamicSmemBytes = fp32 ? ring_bytes<float>(p.draft) : ring_bytes<__nv_bfloat16>(p.draft);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -831,10 +834,10 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
 
 cudaError_t prepare_verify_kernels() {
   const cudaError_t e = cudaFuncSetAttribute(verify_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             kRingBytes<float>);
+                                             ring_bytes<float>(true));
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(verify_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              kRingBytes<__nv_bfloat16>);
+                              ring_bytes<__nv_bfloat16>(true));
 }
 
 }  // namespace mcpu
