@@ -16,8 +16,8 @@
 // barrier every warp joins them all in the same order: all take the same
 // decisions, and nothing is sent back.
 //
-// A pass streams the rows through shared memory: every thread copies vectors of
-// its own ahead (cp.async) and takes them out again, with no barrier, so that the
+// A pass streams the rows through shared memory: every warp copies its part
+// ahead (cp.async) and takes it out again, with no block barrier, so that the
 // loop that is executed stays small (unrolled over as many loads as a slice needs
 // in flight, its instructions came from L2: 14000 cycles for one group of eight).
 //
@@ -114,47 +114,58 @@ __device__ __forceinline__ uint32_t offset16(const T* p) {
   return (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15);
 }
 
-// A slot of the ring holds a step's vectors of every row of the pass, each vector
-// in a plane of its own ([plane][thread]). A group of T takes kVectors<T> planes,
-// and one more in a row that need not have its vectors where the groups begin.
+// Every warp has a ring of its own (warps may be at different passes). A slot
+// holds, for every row and group of a step, 256 values as they lie in the row, a
+// 16-byte vector a lane and copy: 512 bytes in one piece (a lane's own 32 bytes
+// as two copies cost twice the traffic from L2: 384 fp32 rows 208 us, so 129).
+// A row that need not have its vectors where the groups begin has one more
+// (kExtra). Vectors of fp32 rows are swapped in pairs, so that lanes that take
+// every other one meet no bank twice.
 template <typename T>
-constexpr int kVectors = 8 * sizeof(T) / 16;
+constexpr int kVectors = 8 * sizeof(T) / 16;  // of a group, per thread
+template <typename T, bool kExtra>
+constexpr int kPartBytes = 16 * (32 * kVectors<T> + kExtra);
 
-__device__ __forceinline__ uint8_t* plane_at(uint8_t* slot, int plane) {
-  return slot + (plane * kThreads + threadIdx.x) * 16;
+template <typename T>
+__device__ __forceinline__ uint8_t* vector_at(uint8_t* part, int i) {
+  return part + 16 * (sizeof(T) == 4 ? i ^ (i >> 3 & 1) : i);
 }
 __device__ __forceinline__ void copy16(uint8_t* dst, const uint8_t* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
 }
 
-// A group whose vectors would leave the row, value by value.
+// A vector that may leave the row or the slice, whose first value is the row's at-th.
 template <typename T>
-__device__ __noinline__ void fetch_edge(uint8_t* first_plane, const T* row, int j, int before, int planes, int n) {
+__device__ __noinline__ void fetch_edge(uint8_t* dst, const T* row, int at, int begin, int end, int n) {
+  constexpr int kValues = 16 / sizeof(T);
+  if (at >= end || at + kValues <= begin) return;
+  if (at >= 0 && at + kValues <= n) return copy16(dst, reinterpret_cast<const uint8_t*>(row + at));
 #pragma unroll 1
-  for (int i = 0; i < planes * 16 / (int)sizeof(T); ++i) {
-    const int at = j - before + i;
-    if (at >= 0 && at < n)
-      reinterpret_cast<T*>(first_plane + i / (16 / (int)sizeof(T)) * (kThreads * 16))[i % (16 / (int)sizeof(T))] = row[at];
-  }
+  for (int i = 0; i < kValues; ++i)
+    if (at + i >= 0 && at + i < n) reinterpret_cast<T*>(dst)[i] = row[at + i];
 }
 
-// Starts the copies of step k of a row of n values (kExtra: with the extra plane).
+// Starts the copies of step k of a row of n values (kExtra: with the extra vectors).
 template <int kGroups, bool kExtra, typename T>
 __device__ __forceinline__ void fetch(uint8_t* slot, const T* row, const Slice& s, int k, int n) {
-  constexpr int kPlanes = kVectors<T> + kExtra;
-  const int first = s.step(k, kGroups);
+  const int lane = threadIdx.x & 31, first = s.group(s.step(k, kGroups), 0) - 8 * lane;  // of the warp
   const uint32_t off = kExtra ? offset16(row + first) : 0u;
-  const int before = off / sizeof(T), planes = kVectors<T> + (off ? 1 : 0);
-  const uint8_t* src = reinterpret_cast<const uint8_t*>(row + first) - off + threadIdx.x * (8 * sizeof(T));
+  const int at = first - (int)off / (int)sizeof(T);
+  const uint8_t* src = reinterpret_cast<const uint8_t*>(row + at) + 16 * lane;
 #pragma unroll
   for (int e = 0; e < kGroups; ++e) {
-    const int j = s.group(first, e);
-    if (j - before >= 0 && j - before + planes * (16 / (int)sizeof(T)) <= n) {
+    uint8_t* part = slot + e * kPartBytes<T, kExtra>;
+    const int j = at + 8 * e * kThreads;
+    if (j >= s.begin && j + kPartBytes<T, kExtra> / (int)sizeof(T) <= s.end) {
 #pragma unroll
-      for (int v = 0; v < kPlanes; ++v)
-        if (v < kVectors<T> || off) copy16(plane_at(slot, e * kPlanes + v), src + e * (kThreads * (8 * sizeof(T))) + 16 * v);
-    } else if (j < s.end && j + 8 > s.begin) {
-      fetch_edge(plane_at(slot, e * kPlanes), row, j, before, planes, n);
+      for (int v = 0; v < kVectors<T>; ++v)
+        copy16(vector_at<T>(part, 32 * v + lane), src + e * (kThreads * 8 * (int)sizeof(T)) + 512 * v);
+      if (kExtra && off && lane == 0)
+        copy16(vector_at<T>(part, 32 * kVectors<T>), src + e * (kThreads * 8 * (int)sizeof(T)) + 512 * kVectors<T>);
+    } else {
+#pragma unroll 1
+      for (int i = lane; i < 32 * kVectors<T> + (off ? 1 : 0); i += 32)
+        fetch_edge(vector_at<T>(part, i), row, j + i * (16 / (int)sizeof(T)), s.begin, s.end, n);
     }
   }
 }
@@ -162,16 +173,17 @@ __device__ __forceinline__ void fetch(uint8_t* slot, const T* row, const Slice& 
 // Takes group e of step k out again; values outside the slice become `fill` (as bits of one).
 template <int kGroups, bool kExtra, typename T>
 __device__ __forceinline__ void take(uint8_t* slot, const T* row, const Slice& s, int k, int e, uint32_t fill, Raw<T>& r) {
-  constexpr int kWords = Raw<T>::kWords, kPlanes = kVectors<T> + kExtra;
-  const int first = s.step(k, kGroups), per = 8 * kGroups * kThreads;
+  constexpr int kWords = Raw<T>::kWords;
+  const int first = s.step(k, kGroups), per = 8 * kGroups * kThreads, lane = threadIdx.x & 31;
   const uint32_t off = kExtra ? offset16(row + first) : 0u;
+  uint8_t* part = slot + e * kPartBytes<T, kExtra>;
 #pragma unroll
   for (int v = 0; v < kVectors<T>; ++v) {
-    const uint4 x = *reinterpret_cast<const uint4*>(plane_at(slot, e * kPlanes + v));
+    const uint4 x = *reinterpret_cast<const uint4*>(vector_at<T>(part, lane * kVectors<T> + v));
     r.w[4 * v] = x.x, r.w[4 * v + 1] = x.y, r.w[4 * v + 2] = x.z, r.w[4 * v + 3] = x.w;
   }
   if (kExtra && off) {
-    const uint4 x = *reinterpret_cast<const uint4*>(plane_at(slot, e * kPlanes + kVectors<T>));
+    const uint4 x = *reinterpret_cast<const uint4*>(vector_at<T>(part, (lane + 1) * kVectors<T>));
     uint32_t w[kWords + 4];
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = r.w[i];
@@ -196,30 +208,33 @@ __device__ __forceinline__ void take(uint8_t* slot, const T* row, const Slice& s
   }
 }
 
-// Streams: issue(k, slot) for the steps k < n runs up to kDepth ahead of
-// use(k, slot). prime() sets the first copies on their way, once those of an
-// earlier stream have landed.
-template <int kDepth, typename Issue>
-__device__ __forceinline__ void prime(uint8_t* ring, int planes, int n, Issue issue) {
+// Streams: issue(k, slot) for the steps k < n runs up to Pass::kDepth ahead of
+// use(k, slot), every warp by itself. prime() sets the first copies on their way,
+// once those of an earlier stream have landed.
+template <typename Pass, typename Issue>
+__device__ __forceinline__ void prime(uint8_t* ring, int n, Issue issue) {
   asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncwarp();
 #pragma unroll 1
-  for (int k = 0; k < kDepth - 1; ++k) {
-    if (k < n) issue(k, ring + k * planes * (kThreads * 16));
+  for (int k = 0; k < Pass::kDepth - 1; ++k) {
+    if (k < n) issue(k, ring + k * Pass::kBytes);
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
 }
-template <int kDepth, typename Issue, typename Use>
-__device__ __forceinline__ void stream(uint8_t* ring, int planes, int n, Issue issue, Use use) {
-  int at = kDepth - 1;
+template <typename Pass, typename Issue, typename Use>
+__device__ __forceinline__ void stream(uint8_t* ring, int n, Issue issue, Use use) {
+  int at = Pass::kDepth - 1;
 #pragma unroll 1
   for (int k = 0; k < n; ++k) {
     // step k + kDepth - 1 goes where step k - 1 was
-    uint8_t* slot = ring + at * planes * (kThreads * 16);
-    if (++at == kDepth) at = 0;
-    if (k + kDepth - 1 < n) issue(k + kDepth - 1, slot);
+    uint8_t* slot = ring + at * Pass::kBytes;
+    if (++at == Pass::kDepth) at = 0;
+    __syncwarp();
+    if (k + Pass::kDepth - 1 < n) issue(k + Pass::kDepth - 1, slot);
     asm volatile("cp.async.commit_group;" ::: "memory");
-    asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
-    use(k, ring + at * planes * (kThreads * 16));
+    asm volatile("cp.async.wait_group %0;" ::"n"(Pass::kDepth - 1) : "memory");
+    __syncwarp();
+    use(k, ring + at * Pass::kBytes);
   }
 }
 
@@ -363,40 +378,35 @@ __device__ __forceinline__ void race8(const uint64_t (&rest)[4], const Raw<float
   }
 }
 
-// The ring, and what a pass makes of it: groups a step, planes, steps in flight.
-// 60 KiB leave room for three blocks on an SM; only fp32 logits of both
-// distributions with the exponentials need 64, for two steps.
-constexpr int kRingPlanes = 15, kPlaneBytes = 16 * kThreads;
+// The ring, and what a pass makes of it: groups a step, bytes, steps in flight.
+// 60 KiB leave room for three blocks on an SM.
+constexpr int kRingBytes = 60 * 1024, kWarpRing = kRingBytes / kWarps;
 template <typename T>
 struct PassOne {  // one row
-  static constexpr int kGroups = 8 / sizeof(T), kPlanes = kGroups * kVectors<T>, kDepth = kRingPlanes / kPlanes;
+  static constexpr int kGroups = 8 / sizeof(T), kBytes = kGroups * kPartBytes<T, false>, kDepth = kWarpRing / kBytes;
 };
 template <typename T>
 struct PassTwo {  // target and draft
-  static constexpr int kGroups = 4 / sizeof(T), kDraft = kGroups * kVectors<T>,
-                       kPlanes = kDraft + kGroups * (kVectors<T> + 1), kDepth = kRingPlanes / kPlanes;
+  static constexpr int kGroups = 4 / sizeof(T), kDraft = kGroups * kPartBytes<T, false>,
+                       kBytes = kDraft + kGroups * kPartBytes<T, true>, kDepth = kWarpRing / kBytes;
 };
 template <typename T, bool kWithDraft>
 struct PassRace {  // target, exponentials, draft
-  static constexpr int kNoise = kVectors<T>, kDraft = kNoise + kVectors<float> + 1,
-                       kPlanes = kDraft + (kWithDraft ? kVectors<T> + 1 : 0),
-                       kDepth = kRingPlanes / kPlanes > 2 ? kRingPlanes / kPlanes : 2;
+  static constexpr int kNoise = kPartBytes<T, false>, kDraft = kNoise + kPartBytes<float, true>,
+                       kBytes = kDraft + (kWithDraft ? kPartBytes<T, true> : 0), kDepth = kWarpRing / kBytes;
 };
-
-template <typename T>
-constexpr int ring_bytes(bool draft) {
-  return kPlaneBytes * (draft && 2 * PassRace<T, true>::kPlanes > kRingPlanes ? 2 * PassRace<T, true>::kPlanes : kRingPlanes);
-}
+static_assert(PassRace<float, true>::kDepth >= 2, "the deepest step");
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams p) {
   __shared__ VerifySmem s;
-  extern __shared__ __align__(16) uint8_t ring[];
+  extern __shared__ __align__(16) uint8_t rings[];
   cluster_arrive();  // (every block of the cluster is there before the first store into its memory)
   grid_dep_launch();
   grid_dep_wait();
   const uint32_t rank = cluster_rank(), size = cluster_size();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint8_t* ring = rings + warp * kWarpRing;
   const int parts = (int)size * kWarps, mine = (int)rank * kWarps + warp;
   const int r = blockIdx.x / size, V = p.vocab;
   const int q0 = p.qsl[r], L = p.qsl[r + 1] - q0;
@@ -448,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
     }
     if (leaf) {
       using Pass = PassRace<T, false>;
-      constexpr int off_e = Pass::kNoise * kThreads * 16;
+      constexpr int off_e = Pass::kNoise;
       float m = kLowest, z = 0.f, zl = 0.f, best = 0.f;
       int best_at = 0x7fffffff;
       slice.shift = offset16(x + slice.begin) / (int)sizeof(T);
@@ -456,8 +466,8 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         fetch<1, false>(slot, x, slice, k, V);
         fetch<1, true>(slot + off_e, noise, slice, k, V);
       };
-      if (primed != cur || !primed_race) prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue);
-      stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue, [&](int k, uint8_t* slot) {
+      if (primed != cur || !primed_race) prime<Pass>(ring, slice.steps(1), issue);
+      stream<Pass>(ring, slice.steps(1), issue, [&](int k, uint8_t* slot) {
         Raw<T> v[1];
         Raw<float> e;
         take<1, false>(slot, x, slice, k, 0, kNegInf<T>, v[0]);
@@ -508,8 +518,8 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
     const bool ready = primed == cur && !primed_race;
     if (!y) {
       auto issue = [&](int k, uint8_t* slot) { fetch<One::kGroups, false>(slot, x, slice, k, V); };
-      if (!ready) prime<One::kDepth>(ring, One::kPlanes, slice.steps(One::kGroups), issue);
-      stream<One::kDepth>(ring, One::kPlanes, slice.steps(One::kGroups), issue, [&](int k, uint8_t* slot) {
+      if (!ready) prime<One>(ring, slice.steps(One::kGroups), issue);
+      stream<One>(ring, slice.steps(One::kGroups), issue, [&](int k, uint8_t* slot) {
         Raw<T> v[One::kGroups];
 #pragma unroll
         for (int e = 0; e < One::kGroups; ++e) take<One::kGroups, false>(slot, x, slice, k, e, kNegInf<T>, v[e]);
@@ -518,17 +528,17 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
     } else {
       auto issue = [&](int k, uint8_t* slot) {
         fetch<Two::kGroups, false>(slot, x, slice, k, V);
-        fetch<Two::kGroups, true>(slot + Two::kDraft * kThreads * 16, y, slice, k, V);
+        fetch<Two::kGroups, true>(slot + Two::kDraft, y, slice, k, V);
       };
-      if (!ready) prime<Two::kDepth>(ring, Two::kPlanes, slice.steps(Two::kGroups), issue);
-      stream<Two::kDepth>(ring, Two::kPlanes, slice.steps(Two::kGroups), issue, [&](int k, uint8_t* slot) {
+      if (!ready) prime<Two>(ring, slice.steps(Two::kGroups), issue);
+      stream<Two>(ring, slice.steps(Two::kGroups), issue, [&](int k, uint8_t* slot) {
         Raw<T> v[Two::kGroups];
 #pragma unroll
         for (int e = 0; e < Two::kGroups; ++e) take<Two::kGroups, false>(slot, x, slice, k, e, kNegInf<T>, v[e]);
         add_groups(v, c, m[0], z[0], zl[0], &none);
 #pragma unroll
         for (int e = 0; e < Two::kGroups; ++e)
-          take<Two::kGroups, true>(slot + Two::kDraft * kThreads * 16, y, slice, k, e, kNegInf<T>, v[e]);
+          take<Two::kGroups, true>(slot + Two::kDraft, y, slice, k, e, kNegInf<T>, v[e]);
         add_groups(v, c, m[1], z[1], zl[1], &none);
       });
     }
@@ -545,7 +555,7 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
       if (greedy) {
         if (m[d] == wm) {  // the lowest token that has it, among this thread's of that step
           const bool held = best_step >= slice.steps(One::kGroups) - One::kDepth;  // it is in the ring still
-          uint8_t* slot = ring + best_step % One::kDepth * One::kPlanes * kThreads * 16;
+          uint8_t* slot = ring + best_step % One::kDepth * One::kBytes;
 #pragma unroll 1
           for (int e = One::kGroups - 1; e >= 0; --e) {
             const int j = slice.group(slice.step(best_step, One::kGroups), e);
@@ -590,17 +600,17 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         slice.shift = offset16(cx + slice.begin) / (int)sizeof(T);
         if (primed_race) {
           using Pass = PassRace<T, false>;
-          prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), [&](int k, uint8_t* slot) {
+          prime<Pass>(ring, slice.steps(1), [&](int k, uint8_t* slot) {
             fetch<1, false>(slot, cx, slice, k, V);
-            fetch<1, true>(slot + Pass::kNoise * kThreads * 16, noise, slice, k, V);
+            fetch<1, true>(slot + Pass::kNoise, noise, slice, k, V);
           });
         } else if (y) {
-          prime<Two::kDepth>(ring, Two::kPlanes, slice.steps(Two::kGroups), [&](int k, uint8_t* slot) {
+          prime<Two>(ring, slice.steps(Two::kGroups), [&](int k, uint8_t* slot) {
             fetch<Two::kGroups, false>(slot, cx, slice, k, V);
-            fetch<Two::kGroups, true>(slot + Two::kDraft * kThreads * 16, cy, slice, k, V);
+            fetch<Two::kGroups, true>(slot + Two::kDraft, cy, slice, k, V);
           });
         } else {
-          prime<One::kDepth>(ring, One::kPlanes, slice.steps(One::kGroups), [&](int k, uint8_t* slot) {
+          prime<One>(ring, slice.steps(One::kGroups), [&](int k, uint8_t* slot) {
             fetch<One::kGroups, false>(slot, cx, slice, k, V);
           });
         }
@@ -685,15 +695,15 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         using Pass = PassTwo<T>;
         auto issue = [&](int k, uint8_t* slot) {
           fetch<Pass::kGroups, false>(slot, x, slice, k, V);
-          fetch<Pass::kGroups, true>(slot + Pass::kDraft * kThreads * 16, y, slice, k, V);
+          fetch<Pass::kGroups, true>(slot + Pass::kDraft, y, slice, k, V);
         };
-        prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), issue);
-        stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(Pass::kGroups), issue, [&](int k, uint8_t* slot) {
+        prime<Pass>(ring, slice.steps(Pass::kGroups), issue);
+        stream<Pass>(ring, slice.steps(Pass::kGroups), issue, [&](int k, uint8_t* slot) {
 #pragma unroll
           for (int e = 0; e < Pass::kGroups; ++e) {
             Raw<T> a, b;
             take<Pass::kGroups, false>(slot, x, slice, k, e, kNegInf<T>, a);
-            take<Pass::kGroups, true>(slot + Pass::kDraft * kThreads * 16, y, slice, k, e, kNegInf<T>, b);
+            take<Pass::kGroups, true>(slot + Pass::kDraft, y, slice, k, e, kNegInf<T>, b);
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -730,7 +740,7 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         const uint64_t neg_x = pack_f32x2(-st[0].max, -st[0].max), neg_y = y ? pack_f32x2(-st[1].max, -st[1].max) : 0;
         const uint64_t ipp = pack_f32x2(ip, ip), fqq = pack_f32x2(-fq, -fq);
         slice.shift = offset16(x + slice.begin) / (int)sizeof(T);
-        constexpr int off_e = PassRace<T, true>::kNoise * kThreads * 16, off_y = PassRace<T, true>::kDraft * kThreads * 16;
+        constexpr int off_e = PassRace<T, true>::kNoise, off_y = PassRace<T, true>::kDraft;
         auto issue = [&](int k, uint8_t* slot) {
           fetch<1, false>(slot, x, slice, k, V);
           fetch<1, true>(slot + off_e, noise, slice, k, V);
@@ -754,8 +764,8 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         };
         auto run = [&](auto with_draft) {
           using Pass = PassRace<T, decltype(with_draft)::value>;
-          prime<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue);
-          stream<Pass::kDepth>(ring, Pass::kPlanes, slice.steps(1), issue, use);
+          prime<Pass>(ring, slice.steps(1), issue);
+          stream<Pass>(ring, slice.steps(1), issue, use);
         };
         if (fq > 0.f) run(std::true_type());
         else run(std::false_type());
@@ -819,7 +829,7 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(size * p.num_seqs);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = fp32 ? ring_bytes<float>(p.draft) : ring_bytes<__nv_bfloat16>(p.draft);
+  cfg.dynamicSmemBytes = kRingBytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -834,10 +844,10 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
 
 cudaError_t prepare_verify_kernels() {
   const cudaError_t e = cudaFuncSetAttribute(verify_kernel<float>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             ring_bytes<float>(true));
+                                             kRingBytes);
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(verify_kernel<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              ring_bytes<__nv_bfloat16>(true));
+                              kRingBytes);
 }
 
 }  // namespace mcpu
