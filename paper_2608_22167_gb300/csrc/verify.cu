@@ -820,9 +820,9 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
 }  // namespace
 
 cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_t stream) {
-  // blocks a row: as many as keep four per SM (64 rows of 131072 logits: 8 blocks
-  // a row 48 us, 4 50, 2 64, 1 91), two at least (384 rows: 1 block a row 330 us,
-  // 2 257, 4 255, 8 308), but a step of the ring for each
+  // blocks a row: as many as keep four per SM (64 greedy rows of 131072 logits: 8
+  // blocks a row 42 us, 4 50, 2 62, 1 89), four at least (384 sampled fp32 rows:
+  // 2 blocks a row 152 us, 4 144, 8 166), but a step of the ring for each
   int size = 1;
   const int step = PassOne<__nv_bfloat16>::kGroups * 8 * kThreads;
   while (size < kMaxCluster && (size < 4 || 2 * size * p.num_seqs <= 4 * sms) && 2 * size * step <= 2 * p.vocab) size *= 2;
