@@ -10,9 +10,10 @@
 // walked in step, a block of slots at a time, and only as much of the two lists
 // is held as the next moves need.
 //
-// Bound by the moves (K and V rows read and written, scattered 128-byte rows);
-// for rows just past their budget by the chain lengths -> weights -> three
-// histograms -> ranks -> pages -> rows.
+// Bound by the moves (K and V rows read and written, scattered 128-byte rows:
+// 6144 items of 2112 to 2560 keys cut to 2048 move 1.2 GB in 269 us, 70 % of the
+// copy rate); for rows just past their budget by the chain lengths -> weights ->
+// three histograms -> ranks -> pages -> rows (512 items: 19 us).
 #include <type_traits>
 
 #include "keep.cuh"
@@ -32,9 +33,11 @@ __device__ __forceinline__ uint32_t order(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// kThreads threads; the orders of kKeys middle slots and as many pages are held.
-template <int kThreads_, int kKeys_, int kTable_>
+// kThreads threads, kResident blocks of them on an SM; the orders of kKeys middle
+// slots and kTable pages are held; a thread has kFlight rows on their way.
+template <int kThreads_, int kResident_, int kKeys_, int kTable_, int kFlight_>
 struct EvictSmem {
+  static constexpr int kResident = kResident_, kFlight = kFlight_;
   static constexpr int kThreads = kThreads_, kWarps = kThreads / 32, kKeys = kKeys_, kTable = kTable_;
   static constexpr int kBlock = kPer * kThreads;  // slots ranked at a time
   static constexpr int kQueue = 2 * kBlock;       // slots waiting for their partners
@@ -47,7 +50,7 @@ struct EvictSmem {
       int32_t src[kQueue], dst[kQueue];
     };
   };
-  int32_t table[kTable];
+  uint32_t table[kTable];  // first row of a page's tile (a pool's rows are fewer than 2^32: 128 bytes each)
   int32_t scan[2][kWarps];
   uint32_t cutoff;
   int32_t want;
@@ -123,9 +126,10 @@ __device__ __noinline__ Walk walk(S& s, const Ranks r, Walk region, int stop, bo
 }
 
 template <typename S>
-__global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
+__global__ void __launch_bounds__(S::kThreads, S::kResident)
     evict_kernel(const EvictParams p, const __grid_constant__ PoolPtrs pools) {
-  constexpr int kThreads = S::kThreads, kWarps = S::kWarps, kBlock = S::kBlock, kQueue = S::kQueue, kMoves = S::kMoves;
+  constexpr int kThreads = S::kThreads, kWarps = S::kWarps, kBlock = S::kBlock, kQueue = S::kQueue, kMoves = S::kMoves,
+                kFlight = S::kFlight;
   extern __shared__ __align__(16) uint8_t smem[];
   S& s = *reinterpret_cast<S*>(smem);
   grid_dep_launch();
@@ -134,6 +138,7 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int n = p.seq_lens[r];
   const bool speaks = h == 0 && m == 0 && threadIdx.x == 0;
+  const uint32_t rows = (uint32_t)Hkv * kPage;  // of a page
   const int32_t* table = p.block_table + (size_t)r * p.max_pages;
   bool cut = n > p.limit;
   int32_t bits = 0;
@@ -145,7 +150,7 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
     int32_t bad = 0;
     for (int j = page0 + threadIdx.x; j < pages; j += kThreads) {
       const int page = table[j];
-      if (j - page0 < S::kTable) s.table[j - page0] = page;
+      if (j - page0 < S::kTable) s.table[j - page0] = (uint32_t)page * rows;
       if (page < 0 || page >= p.num_pages) bad |= kStatusBadPage;
       else if (p.refs && j < mine && p.refs[page] > 0) bad |= kStatusUnsupportedRow;
     }
@@ -169,14 +174,13 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
   if (!cut) return;
 
   const bool held = pages - page0 <= S::kTable;
-  auto page_of = [&](int slot) { return held ? s.table[slot / kPage - page0] : table[slot / kPage]; };
+  auto first_row = [&](int slot) { return held ? s.table[slot / kPage - page0] : (uint32_t)table[slot / kPage] * rows; };
   // a thread moves one 16-byte piece (of K or of V) of every kThreads / 16-th slot
   constexpr int kLanes = kThreads / kRowVecs;
   const int mine = threadIdx.x / kRowVecs, piece = threadIdx.x % kRowVecs;
   uint8_t* base = pools.p[piece & 8 ? p.num_layers + m : m] + (size_t)h * kTileBytes + (piece & 7) * 16;
-  const int64_t page_bytes = (int64_t)Hkv * kTileBytes;
   auto vec = [&](int slot) {
-    return reinterpret_cast<uint4*>(base + page_of(slot) * page_bytes + slot % kPage * kRowBytes);
+    return reinterpret_cast<uint4*>(base + (uint64_t)(first_row(slot) + (uint32_t)slot % kPage) * kRowBytes);
   };
 
   // ---- the K-th largest weight of the middle: its order, and how many that equal it stay
@@ -280,7 +284,6 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
     __syncthreads();
     const int count = min(min(a.have, b.have) - done, kMoves);
     if (count <= 0) break;
-    constexpr int kFlight = 8;
 #pragma unroll 1
     for (int i0 = mine; i0 < count; i0 += kFlight * kLanes) {
       uint4 v[kFlight];
@@ -298,20 +301,20 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
 
   // ---- the last ones, towards the front: a piece of them at a time, read before it is written
   __syncthreads();
-  constexpr int kHeld = 8, kPiece = kHeld * kLanes;
+  constexpr int kPiece = kFlight * kLanes;
   const bool apart = n - p.budget >= p.last;  // they do not overlap their new places
 #pragma unroll 1
   for (int i0 = 0; i0 < p.last; i0 += kPiece) {
     const int count = min(p.last - i0, kPiece);
-    uint4 v[kHeld];
+    uint4 v[kFlight];
     float weight = 0.f;
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
+    for (int k = 0; k < kFlight; ++k)
       if (mine + k * kLanes < count) v[k] = __ldcs(vec(end + i0 + mine + k * kLanes));
     if (threadIdx.x < count) weight = w[end + i0 + threadIdx.x];
     if (!apart) __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kHeld; ++k)
+    for (int k = 0; k < kFlight; ++k)
       if (mine + k * kLanes < count) *vec(inner + i0 + mine + k * kLanes) = v[k];
     if (threadIdx.x < count) nw[inner + i0 + threadIdx.x] = weight;
     if (!apart) __syncthreads();
@@ -320,8 +323,8 @@ __global__ void __launch_bounds__(S::kThreads, 1024 / S::kThreads)
 
 }  // namespace
 
-using Middle = EvictSmem<256, 4096, 1024>;
-using Large = EvictSmem<512, 8192, 4096>;
+using Middle = EvictSmem<256, 5, 4096, 1024, 4>;
+using Large = EvictSmem<512, 2, 8192, 4096, 6>;
 
 cudaError_t launch_evict(const EvictParams& p, const PoolPtrs& pools, int sms, cudaStream_t stream) {
   const dim3 grid(p.num_kv_heads, p.num_seqs, p.num_layers > 0 ? p.num_layers : 1);
@@ -331,6 +334,10 @@ cudaError_t launch_evict(const EvictParams& p, const PoolPtrs& pools, int sms, c
     LaunchCfg lc(grid, dim3(S::kThreads), sizeof(S), stream, true);
     return cudaLaunchKernelEx(&lc.cfg, kernel, p, pools);
   };
+  // Large blocks as long as all are on the SMs at once (256 items of 8192 to 32768
+  // keys: 130 us, by small ones 238), then small ones, with more of them at
+  // different steps (512 items of 2032 to 2128 keys, from HBM: 25 us, by large
+  // ones 33; 6144 of 2112 to 2560: 269 and 341).
   if (items > 2 * sms) return launch(evict_kernel<Middle>, (Middle*)nullptr);
   return launch(evict_kernel<Large>, (Large*)nullptr);
 }
