@@ -662,10 +662,11 @@ mcpu_status mcpu_copy_pages(void* const* pools, int32_t num_pools, int64_t page_
  * a long prompt alone.
  * decay in [0, 1]; 0 reads no old weights. softmax_scale in [1e-30, 1e30]. A row
  * without queries keeps its weights as they are, and so do slots from S_r on. A
- * query with lse = -inf (it saw nothing) or inf adds nothing to finite keys; a NaN
- * of a key, or of a query that sees it or its lse, makes that key's weight NaN. A row longer than max_slots or its table, or with a path
- * that breaks the rules, is skipped (MCPU_ERR_BAD_LENGTHS); keys of a page
- * outside the pool keep their weights (MCPU_ERR_BAD_PAGE).
+ * query with lse = -inf (it saw nothing) or inf adds nothing to finite keys; a
+ * NaN of a key, or of a query that sees it or its lse, makes that key's weight
+ * NaN. A row longer than max_slots or its table, or with a path that breaks the
+ * rules, is skipped (MCPU_ERR_BAD_LENGTHS); keys of a page outside the pool keep
+ * their weights (MCPU_ERR_BAD_PAGE).
  * Sums are fp32 in a fixed order: the same inputs give the same bits on the
  * same device. workspace: mcpu_weights_workspace_size(dims) bytes, 256-byte
  * aligned, the status word first (zero it once); calls that share one must be
