@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int id = __shfl_sync(0xffffffffu, these, (i & 1) * 16 + (lane & 15));
         const int pk = a.k0 + i * kUnitKeys + (lane & 15) * kPage, pl = min(pk + kPage, a.len) - 1;  // the page's keys
         const bool exists = id >= 0 && id < p.num_pages;
-        const bool seen = pk < a.len && (W == 0 || pl >= C || pl + W > C);
+        const bool seen = pk < a.len && (W == 0 || pl >= C || (int64_t)pl + W > C);
         if (seen && !exists && lane < 16) atomicOr(p.status, kStatusBadPage);
         const uint32_t pages = __ballot_sync(0xffffffffu, exists) & 0xffffu;
         const int y = exists && pk < a.len ? (id * Hkv + a.kvh) * kPage : p.oob_row;

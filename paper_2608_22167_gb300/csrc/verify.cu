@@ -825,7 +825,7 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   // 2 blocks a row 152 us, 4 144, 8 166), but a step of the ring for each
   int size = 1;
   const int step = PassOne<__nv_bfloat16>::kGroups * 8 * kThreads;
-  while (size < kMaxCluster && (size < 4 || 2 * size * p.num_seqs <= 4 * sms) && 2 * size * step <= 2 * p.vocab) size *= 2;
+  while (size < kMaxCluster && (size < 4 || 2 * size * p.num_seqs <= 4 * sms) && size * step <= p.vocab) size *= 2;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(size * p.num_seqs);
   cfg.blockDim = dim3(kThreads);

@@ -296,6 +296,28 @@ def test_offsets_past_32_bits():
 
 
 @gpu
+def test_a_row_and_a_window_of_more_than_2_30_keys():
+    """Slot + window pass 2^31. The keys are zeros, so that a head's weight of a key it sees is exp(-lse) = 1 exactly."""
+    from paper_2608_22167_gb300 import mcpu
+
+    S, W, missing = 1_100_000_000, 1_080_000_000, 1_090_000_000 // 16
+    q = torch.ones(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    kc = torch.zeros(2, 1, 16, 64, dtype=torch.bfloat16, device="cuda")
+    table = torch.ones(1, S // 16, dtype=torch.int32, device="cuda")
+    table[0, missing] = 7  # no such page
+    w = torch.zeros(1, 1, S, device="cuda")
+    lens = torch.tensor([S], dtype=torch.int32, device="cuda")
+    qsl = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    ws = mcpu.new_weights_workspace(mcpu.dims(q, kc, table, lens))
+    mcpu.mcpu_accumulate_weights(q, torch.zeros(1, 1, device="cuda"), kc, table, lens, qsl, W, 0.125, 1.0, w, ws)
+    assert mcpu.mcpu_read_device_status(ws)[1] == mcpu.STATUS_BAD_PAGE
+    w = w.view(-1)
+    first = S - W  # the query's position is S - 1
+    assert not w[:first].any() and not w[16 * missing : 16 * missing + 16].any()
+    assert int((w == 1).sum()) == W - 16
+
+
+@gpu
 def test_weights_of_a_forward_call_sum_to_the_queries():
     """With the log-sum-exps of mcpu_paged_attention_forward a query's weights sum to one (less the sink's share), so
     a kv head's add up to its queries: 300 terms of 2.5e-5 relative, and an lse good to 1e-4."""
