@@ -822,10 +822,10 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
 cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_t stream) {
   // blocks a row: as many as keep four per SM (64 greedy rows of 131072 logits: 8
   // blocks a row 42 us, 4 50, 2 62, 1 89), four at least (384 sampled fp32 rows:
-  // 2 blocks a row 152 us, 4 144, 8 166), but a step of the ring for each
+  // 2 blocks a row 152 us, 4 144, 8 166), but half a group of logits for every
+  // thread (2 rows of 16000: 8 blocks a row 17 us, 4 19, 2 21; of 4000: 2 17, 1 19)
   int size = 1;
-  const int step = PassOne<__nv_bfloat16>::kGroups * 8 * kThreads;
-  while (size < kMaxCluster && (size < 4 || 2 * size * p.num_seqs <= 4 * sms) && size * step <= p.vocab) size *= 2;
+  while (size < kMaxCluster && (size < 4 || 2 * size * p.num_seqs <= 4 * sms) && size * 8 * kThreads <= p.vocab) size *= 2;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(size * p.num_seqs);
   cfg.blockDim = dim3(kThreads);
