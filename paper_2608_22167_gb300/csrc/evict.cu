@@ -102,7 +102,7 @@ __device__ __noinline__ Walk walk(S& s, const Ranks r, Walk region, int stop, bo
   for (int e = 0; e < kPer; ++e) {
     const bool in = j + 32 * e < stop;
     above[e] = __ballot_sync(0xffffffffu, in && u[e] > r.cutoff);
-    same[e] = __ballot_sync(0xffffffffu, in && u[e] == r.cutoff);
+    same[e] = r.ties > 0 ? __ballot_sync(0xffffffffu, in && u[e] == r.cutoff) : 0u;
     counts += __popc(above[e]) + (__popc(same[e]) << 16);
   }
   const int before = warps_scan(counts, s, turn, &all);
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(S::kThreads, S::kResident)
 
   // ---- kept slots at or past inner fill the holes before it, in order
   int ties_before = 0;  // slots equal to the cutoff before inner
-  if (K > 0) {
+  if (ties > 0) {
     int same = 0;
 #pragma unroll 4
     for (int j = first + threadIdx.x; j < inner; j += kThreads) same += key(j) == cutoff;
