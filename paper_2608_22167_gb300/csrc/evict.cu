@@ -23,7 +23,7 @@ namespace mcpu {
 namespace {
 
 constexpr int kPer = 4;                       // slots a thread ranks at a time
-constexpr int kRowVecs = 2 * kRowBytes / 16;  // 16-byte pieces of a slot's K and V
+constexpr int kRowVecs = kRowBytes / 16;  // 16-byte pieces of a slot's K, or V
 constexpr int kBins = 2048;
 
 // Unsigned order of the weights: NaN lowest, the two zeros equal.
@@ -176,12 +176,21 @@ __global__ void __launch_bounds__(S::kThreads, S::kResident)
 
   const bool held = pages - page0 <= S::kTable;
   auto first_row = [&](int slot) { return held ? s.table[slot / kPage - page0] : (uint32_t)table[slot / kPage] * rows; };
-  // a thread moves one 16-byte piece (of K or of V) of every kThreads / 16-th slot
+  // a thread moves one 16-byte piece of K and of V, of every kThreads / 8-th slot
   constexpr int kLanes = kThreads / kRowVecs;
-  const int mine = threadIdx.x / kRowVecs, piece = threadIdx.x % kRowVecs;
-  uint8_t* base = pools.p[piece & 8 ? p.num_layers + m : m] + (size_t)h * kTileBytes + (piece & 7) * 16;
-  auto vec = [&](int slot) {
-    return reinterpret_cast<uint4*>(base + (uint64_t)(first_row(slot) + (uint32_t)slot % kPage) * kRowBytes);
+  const int mine = threadIdx.x / kRowVecs;
+  const size_t head = (size_t)h * kTileBytes + threadIdx.x % kRowVecs * 16;
+  uint8_t *base_k = pools.p[m] + head, *base_v = pools.p[p.num_layers + m] + head;
+  auto offset = [&](int slot) { return (uint64_t)(first_row(slot) + (uint32_t)slot % kPage) * kRowBytes; };
+  auto load = [&](int slot, uint4 (&v)[2]) {
+    const uint64_t at = offset(slot);
+    v[0] = __ldcs(reinterpret_cast<const uint4*>(base_k + at));
+    v[1] = __ldcs(reinterpret_cast<const uint4*>(base_v + at));
+  };
+  auto store = [&](int slot, const uint4 (&v)[2]) {
+    const uint64_t at = offset(slot);
+    *reinterpret_cast<uint4*>(base_k + at) = v[0];
+    *reinterpret_cast<uint4*>(base_v + at) = v[1];
   };
 
   // ---- the K-th largest weight of the middle: its order, and how many that equal it stay
@@ -293,13 +302,13 @@ __global__ void __launch_bounds__(S::kThreads, S::kResident)
     if (count <= 0) break;
 #pragma unroll 1
     for (int i0 = mine; i0 < count; i0 += kFlight * kLanes) {
-      uint4 v[kFlight];
+      uint4 v[kFlight][2];
 #pragma unroll
       for (int k = 0; k < kFlight; ++k)
-        if (i0 + k * kLanes < count) v[k] = __ldcs(vec(s.src[(done + i0 + k * kLanes) % kQueue]));
+        if (i0 + k * kLanes < count) load(s.src[(done + i0 + k * kLanes) % kQueue], v[k]);
 #pragma unroll
       for (int k = 0; k < kFlight; ++k)
-        if (i0 + k * kLanes < count) *vec(s.dst[(done + i0 + k * kLanes) % kQueue]) = v[k];
+        if (i0 + k * kLanes < count) store(s.dst[(done + i0 + k * kLanes) % kQueue], v[k]);
     }
     for (int e = threadIdx.x; e < count; e += kThreads) nw[s.dst[(done + e) % kQueue]] = w[s.src[(done + e) % kQueue]];
     done += count;
@@ -313,16 +322,16 @@ __global__ void __launch_bounds__(S::kThreads, S::kResident)
 #pragma unroll 1
   for (int i0 = 0; i0 < p.last; i0 += kPiece) {
     const int count = min(p.last - i0, kPiece);
-    uint4 v[kFlight];
+    uint4 v[kFlight][2];
     float weight = 0.f;
 #pragma unroll
     for (int k = 0; k < kFlight; ++k)
-      if (mine + k * kLanes < count) v[k] = __ldcs(vec(end + i0 + mine + k * kLanes));
+      if (mine + k * kLanes < count) load(end + i0 + mine + k * kLanes, v[k]);
     if (threadIdx.x < count) weight = w[end + i0 + threadIdx.x];
     if (!apart) __syncthreads();
 #pragma unroll
     for (int k = 0; k < kFlight; ++k)
-      if (mine + k * kLanes < count) *vec(inner + i0 + mine + k * kLanes) = v[k];
+      if (mine + k * kLanes < count) store(inner + i0 + mine + k * kLanes, v[k]);
     if (threadIdx.x < count) nw[inner + i0 + threadIdx.x] = weight;
     if (!apart) __syncthreads();
   }
@@ -330,8 +339,8 @@ __global__ void __launch_bounds__(S::kThreads, S::kResident)
 
 }  // namespace
 
-using Middle = EvictSmem<256, 5, 4096, 1024, 4>;
-using Large = EvictSmem<512, 2, 8192, 4096, 6>;
+using Middle = EvictSmem<256, 5, 4096, 1024, 2>;
+using Large = EvictSmem<512, 2, 8192, 4096, 4>;
 
 cudaError_t launch_evict(const EvictParams& p, const PoolPtrs& pools, int sms, cudaStream_t stream) {
   const dim3 grid(p.num_kv_heads, p.num_seqs, p.num_layers > 0 ? p.num_layers : 1);
