@@ -11,7 +11,7 @@
 // is held as the next moves need.
 //
 // Bound by the moves (K and V rows read and written, scattered 128-byte rows:
-// 6144 items of 2112 to 2560 keys cut to 2048 move 1.2 GB in 260 us, 72 % of the
+// 6144 items of 2112 to 2560 keys cut to 2048 move 1.2 GB in 243 us, 78 % of the
 // copy rate); for rows just past their budget by the chain lengths -> weights ->
 // three histograms -> ranks -> pages -> rows (512 items: 19 us).
 #include <type_traits>
@@ -351,9 +351,9 @@ cudaError_t launch_evict(const EvictParams& p, const PoolPtrs& pools, int sms, c
     return cudaLaunchKernelEx(&lc.cfg, kernel, p, pools);
   };
   // Large blocks as long as all are on the SMs at once (256 items of 8192 to 32768
-  // keys: 130 us, by small ones 238), then small ones, with more of them at
+  // keys: 123 us, by small ones 199), then small ones, with more of them at
   // different steps (512 items of 2032 to 2128 keys, from HBM: 25 us, by large
-  // ones 33; 6144 of 2112 to 2560: 269 and 341).
+  // ones 31; 6144 of 2112 to 2560: 247 and 302).
   if (items > 2 * sms) return launch(evict_kernel<Middle>, (Middle*)nullptr);
   return launch(evict_kernel<Large>, (Large*)nullptr);
 }

@@ -792,6 +792,7 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
     cur = went;
     ++len;
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");  // none in flight when the block ends
   if (rank != 0) return;
   __syncthreads();
   for (int i = threadIdx.x; i < p.max_accept; i += kThreads) {
