@@ -23,6 +23,15 @@
 // path) and their log-sum-exps, 8-15 and 16-23 take the exponentials, blocks in turn (a warp's
 // waits and loads are the other group's work). TMEM: two buffers of 128 columns
 // for each half of a unit's keys.
+//
+// Bound by the keys' way from HBM where queries are few (64 rows of 2047 to 16383
+// keys, 64 / 8 heads, one query each: 642 MB in 105 us, 90 % of the copy rate), by
+// the exponentials where they are many (16 rows of 4096 to 32768 keys, 64 to 2048
+// queries: 3.2 ms; 1024 of a block's 1100 to 1200 cycles, 8 a clock and
+// sub-partition, at the 1.4 GHz that the power limit leaves). There the
+// log-sum-exps as a step of the product took 4.55 ms to 3.56: read for every
+// column from shared memory they needed 128 bytes a clock; and one box for 128
+// contiguous columns, not 16 bytes a lane, 4.43 to 3.22.
 #include "keep.cuh"
 #include "warp_pipe.cuh"
 
@@ -39,9 +48,11 @@ constexpr int kQueryWarps = 3;
 static_assert(kQueryWarps == kQStages, "a stage each");
 constexpr int kThreads = 768, kGroupWarps = 8;  // warps that take the exponentials of a block
 constexpr uint32_t kTmemCols = 512;
-constexpr int kWholeBlocks = 3;  // units of up to so many blocks are never cut
-constexpr int kCostShort = 3;    // of a unit of a row with one block of queries
-constexpr int kMinQuota = 3;
+// Units of up to so many blocks are never cut, and rows of no more need no merge
+// (up to 8: pieces differ too much, the many queries above 3.41 ms, 3 or 1: 3.22).
+constexpr int kWholeBlocks = 3;
+constexpr int kCostShort = 3;  // of a unit of a row with one block of queries (2 to 4: +-1 %)
+constexpr int kMinQuota = 3;   // of a piece: a unit (four rows of 16 to 299 keys: 13 us, at 12 17)
 // A fifth step of the product, over 16 dims of which three are used: 1 for every
 // key, and -lse / scale of a column in three bf16 pieces (24 bits). As 8 x 16
 // byte matrices without swizzle: first dims 0-7 of all rows, then 8-15.

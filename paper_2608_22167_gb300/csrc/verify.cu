@@ -21,6 +21,11 @@
 // loop that is executed stays small (unrolled over as many loads as a slice needs
 // in flight, its instructions came from L2: 14000 cycles for one group of eight).
 //
+// Bound by the chain of a row's nodes where rows are few (64 rows, up to 7 nodes on
+// a path, 131072 bf16 logits: 42 us; a node's first loads, two steps, the
+// exchange), by HBM where they are many (384 rows of fp32 logits: 595 MB in 130
+// us, 68 % of the copy rate).
+//
 // Everything is fp32. Sums are pairs: 8 terms at a time, added by an exact two-sum
 // (a plain chain of additions loses 1e-6 of a peaked distribution's tail).
 // Exponentials by ex2.approx (2^-22).
