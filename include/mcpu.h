@@ -657,9 +657,9 @@ mcpu_status mcpu_copy_pages(void* const* pools, int32_t num_pools, int64_t page_
  * attention call (lse with its sinks), made with the same window.
  * query_path NULL: the queries are all L_r of the row, C_r = S_r - L_r. Else the
  * row's path_len[r] query tokens query_path[r * max_path + i] (numbers in the
- * row, 0 .. L_r - 1), C_r = S_r - path_len[r]: the accepted nodes once
- * mcpu_compact_kv has moved them (with its new_seq_lens), or the last queries of
- * a long prompt alone.
+ * row, 0 .. L_r - 1, in any order and as often as wanted), C_r = S_r -
+ * path_len[r]: the accepted nodes once mcpu_compact_kv has moved them (with its
+ * new_seq_lens), or the last queries of a long prompt alone.
  * decay in [0, 1]; 0 reads no old weights. softmax_scale in [1e-30, 1e30]. A row
  * without queries keeps its weights as they are, and so do slots from S_r on. A
  * query with lse = -inf (it saw nothing) or inf adds nothing to finite keys; a

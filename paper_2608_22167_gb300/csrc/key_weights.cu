@@ -822,8 +822,9 @@ cudaError_t launch_weights(const CUtensorMap& kmap, const CUtensorMap& qmap, con
   LaunchCfg lc(dim3(grid), dim3(kThreads), weights_smem_bytes(), stream, true);
   const cudaError_t e = cudaLaunchKernelEx(&lc.cfg, weights_kernel, kmap, qmap, p);
   if (e != cudaSuccess) return e;
-  // no row has more than kWholeBlocks blocks of queries: nothing is cut
-  const int64_t most = p.path && p.max_path < p.total_q ? p.max_path : p.total_q;
+  // no row has more than kWholeBlocks blocks of queries: nothing is cut (a path
+  // may name a query more than once, and more of them than the step has)
+  const int64_t most = p.path ? p.max_path : p.total_q;
   if (most * p.group <= kWholeBlocks * kCols) return cudaSuccess;
   LaunchCfg mc(dim3(grid), dim3(kUnitKeys), 0, stream, true);
   return cudaLaunchKernelEx(&mc.cfg, merge_weights_kernel, p);

@@ -336,6 +336,15 @@ def test_weights_of_a_forward_call_sum_to_the_queries():
     assert torch.all((w.double().sum(2) - want).abs() <= 2e-4 * want)
 
 
+@gpu
+@pytest.mark.parametrize("window", [0, 700])
+def test_paths_of_more_queries_than_the_step_has(window):
+    """The same queries over and over: more blocks of them than the step's own queries fill, cut between the pieces."""
+    rng = np.random.default_rng(16)
+    path = [rng.integers(0, 40, 200).tolist(), [0, 0, 1]]
+    Batch([5000, 90], [40, 2], 8, 1, seed=17, window=window, path=path).check(decay=0.5)
+
+
 def _args():
     from paper_2608_22167_gb300 import mcpu  # noqa: F401
 
