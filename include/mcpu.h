@@ -548,8 +548,12 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
  * more than MCPU_MAX_TREE_NODES (MCPU_ERR_UNSUPPORTED_ROW) or inconsistent
  * query_start_loc (MCPU_ERR_BAD_LENGTHS).
  * logits, draft_logits: logits_type MCPU_BF16 or MCPU_FP32 elements, any
- * stride >= vocab. Sums and probabilities are fp32 (sums exact to about 2^-22), so
- * that a draw within 1e-6 of a border may fall on either side of it.
+ * stride >= vocab. Everything is fp32, sums are pairs of it: a weight
+ * e^((l - max) / T) is good to 2^-22 + 3 * 2^-24 |l - max| / T, relatively. A
+ * uniform may fall on either side of a child's border that it is as near to as,
+ * relatively, 2^-15 without draft logits, however little of the probability the
+ * rejected children left (|l - max| / T up to 30); with them, where p and M q
+ * cancel, 2^-17 (p / rest + 1 / m) (|l - max| / T up to 8).
  */
 #define MCPU_MAX_TREE_NODES 256
 #define MCPU_BF16 0

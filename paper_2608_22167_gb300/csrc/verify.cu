@@ -4,14 +4,17 @@
 // draft, the residual after rejecting k children of masses m_0 = 1, m_1 .. is
 //   rest(y) = max(p(y) - M q(y), 0),  M = m_0 + .. + m_{k-1},  m_k = sum_y rest(y)
 // because max(max(a, 0) - b, 0) = max(a - b, 0) for b >= 0: only M is carried,
-// no vector. The next token is argmax_y rest(y) / e_y, which for exponential e
-// is y with probability rest(y) / m.
+// no vector. Without a draft a rejected token's p goes to 0, and m is what is
+// left of the sum: a difference down to a quarter of it, then summed anew over the
+// other tokens (1 - p loses the digits of a peaked distribution's tail). The next
+// token is argmax_y rest(y) / e_y, which for exponential e is y with probability
+// rest(y) / m.
 //
 // A cluster of blocks walks a row's tree, a slice of the vocabulary each; only
 // the nodes that the walk visits are read. A node costs one pass over its
 // logits (maximum, its place and the sum together), a rejection with draft
-// probabilities one more, the row's end one with the exponentials; what was
-// read before comes from L2 then. After a pass every warp hands its result to
+// probabilities one more (without, where little is left), the row's end one with
+// the exponentials; what was read before comes from L2 then. After a pass every warp hands its result to
 // all blocks of the cluster (distributed shared memory), and behind one cluster
 // barrier every warp joins them all in the same order: all take the same
 // decisions, and nothing is sent back.
@@ -634,7 +637,10 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
     // ---- the children, in ascending order (every warp alike)
     const float ip = 1.f / (st[0].sum + st[0].low), iq = y ? 1.f / (st[1].sum + st[1].low) : 1.f;
     int went = -1, rejected = 0;
-    float mass = 1.f, gone = 0.f;
+    // The residual's mass is a pair. Without a draft weights are relative to the
+    // maximum, so that the likeliest token's is 1 and goes exactly; `whole` is the
+    // last mass that was formed by adding.
+    float mass = y ? 1.f : st[0].sum, mass_low = y ? 0.f : st[0].low, whole = mass + mass_low, gone = 0.f;
 #pragma unroll 1
     for (int w0 = w1; w0 < L && went < 0 && len < p.max_accept; w0 += 32) {
       if (w0 > w1) {  // trees of more than 32 nodes
@@ -656,7 +662,8 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         if (hit) went = w0 + __ffs(hit) - 1;
         continue;
       }
-      const float px = ex2_approx((lx - st[0].max) * c) * ip, qx = y ? ex2_approx((ly - st[1].max) * c) * iq : 1.f;
+      const float px = ex2_approx((lx - st[0].max) * c) * (y ? ip : 1.f),
+                  qx = y ? ex2_approx((ly - st[1].max) * c) * iq : 1.f;
 #pragma unroll 1
       for (; kids && went < 0; kids &= kids - 1) {
         const int l = __ffs(kids) - 1;
@@ -671,19 +678,22 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
           for (int e = lane; e < rejected; e += 32) again |= s.gone[e] == kt;
           if (__any_sync(0xffffffffu, again)) rest = 0.f;
         }
-        if (ku * mass * kq < rest) {
+        if (ku * (mass + mass_low) * kq < rest) {
           went = w0 + l;
           break;
         }
         ++rejected;
         if (!y) {
-          mass = fmaxf(mass - rest, 0.f);
           __syncwarp();
           s.gone[rejected - 1] = kt;  // (every thread of the block writes the same)
           __syncwarp();
-          continue;
+          add_exact(mass, mass_low, -rest);
+          // A difference is good as long as little has gone. A quarter is left of
+          // what was added up last with the probability of a quarter.
+          if (4.f * (mass + mass_low) >= whole) continue;
+        } else {
+          gone += mass + mass_low;
         }
-        gone += mass;
         // the residual's mass, if another child is to be tried
         bool more = (kids & (kids - 1)) != 0;
         for (int v0 = w0 + 32; v0 < L && !more; v0 += 32) {
@@ -700,21 +710,35 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
         using Pass = PassTwo<T>;
         auto issue = [&](int k, uint8_t* slot) {
           fetch<Pass::kGroups, false>(slot, x, slice, k, V);
-          fetch<Pass::kGroups, true>(slot + Pass::kDraft, y, slice, k, V);
+          if (y) fetch<Pass::kGroups, true>(slot + Pass::kDraft, y, slice, k, V);
         };
         prime<Pass>(ring, slice.steps(Pass::kGroups), issue);
         stream<Pass>(ring, slice.steps(Pass::kGroups), issue, [&](int k, uint8_t* slot) {
 #pragma unroll
           for (int e = 0; e < Pass::kGroups; ++e) {
-            Raw<T> a, b;
+            Raw<T> a;
+            uint64_t w[4];
             take<Pass::kGroups, false>(slot, x, slice, k, e, kNegInf<T>, a);
-            take<Pass::kGroups, true>(slot + Pass::kDraft, y, slice, k, e, kNegInf<T>, b);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = weights2(a, i, neg_x, cc);
+            uint32_t out = 0;  // which of the eight are tokens of rejected children
+            if (y) {
+              take<Pass::kGroups, true>(slot + Pass::kDraft, y, slice, k, e, kNegInf<T>, a);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) w[i] = fma2(w[i], ipp, mul2(weights2(a, i, neg_y, cc), fqq));
+            } else {
+              const int j = slice.group(slice.step(k, Pass::kGroups), e);
+#pragma unroll 1
+              for (int i = 0; i < rejected; ++i) {
+                const uint32_t at = (uint32_t)(s.gone[i] - j);
+                out |= at < 8u ? 1u << at : 0u;
+              }
+            }
             float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint64_t w = fma2(weights2(a, i, neg_x, cc), ipp, mul2(weights2(b, i, neg_y, cc), fqq));
-              sum += fmaxf(lo_f32(w), 0.f) + fmaxf(hi_f32(w), 0.f);
-            }
+            for (int i = 0; i < 4; ++i)
+              sum += (out >> (2 * i) & 1u ? 0.f : fmaxf(lo_f32(w[i]), 0.f)) +
+                     (out >> (2 * i + 1) & 1u ? 0.f : fmaxf(hi_f32(w[i]), 0.f));
             add_exact(z, zl, sum);
           }
         });
@@ -727,7 +751,9 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
           zl += s.sums[turn][e].y;
         }
         warp_add_exact(z, zl);
-        mass = z + zl;
+        mass = z;
+        mass_low = zl;
+        whole = z + zl;
         turn ^= 1;
       }
     }

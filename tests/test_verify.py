@@ -324,6 +324,101 @@ def test_replays_follow_their_inputs_and_other_streams_work():
         _check((path.cpu().numpy(), n.cpu().numpy(), nxt.cpu().numpy(), logp.double().cpu().numpy()), d)
 
 
+def _near(case, got):
+    """The walks of draws that lie next to a border: paths and their lengths as in 64 bits."""
+    want = reference(case)
+    assert np.array_equal(got[0], want[0]) and np.array_equal(got[1], want[1])
+
+
+@gpu
+@pytest.mark.parametrize("vocab,first", [(40, 1), (40, 33), (4099, 1), (4099, 33), (60000, 1)])
+@pytest.mark.parametrize("fp32", [False, True])
+def test_siblings_of_tokens_that_take_almost_all(vocab, first, fp32):
+    """Children left after the likeliest tokens were rejected: what remains, down to 1e-6 of the probability, is as
+    good as the weights themselves. With d = (max - l) / T a weight is off by 2^-22 (its exponential) and 3 2^-24 d
+    (three roundings of its exponent), relatively; here d < 30. Two of them in a quotient: 2 (2^-22 + 3 2^-24 30) =
+    1.12e-5, and 40 2^-24 = 2.4e-6 for the sums. What is left may be a difference down to a quarter of the whole, where
+    the roundings of the whole (12 2^-24 beside its likeliest terms, 2^-22 of what was taken off) count four times:
+    3.8e-6. Draws 2e-5 on either side of a border are decided as in 64 bits."""
+    rng = np.random.default_rng(vocab + first)
+    cases = []
+    for leaders in (1, 2):
+        for rest in (0.3, 0.1, 1e-2, 1e-3, 1e-4, 1e-5, 1e-6):
+            x = rng.standard_normal(vocab)
+            top = rng.choice(vocab, leaders + 2, replace=False)
+            x[top[:leaders]] = -np.inf
+            height = np.log(np.exp(x).sum() * (1 - rest) / rest / leaders)
+            x[top[:leaders]] = height - 0.01 * np.arange(leaders)
+            x = torch.from_numpy(x).to(torch.float32 if fp32 else torch.bfloat16)
+            p = np.exp(x.double().numpy() - x.double().numpy().max())
+            p[top[:leaders]] = 0
+            for kid in range(2):  # the border of the first sibling, or of the second once that is rejected
+                level = p[top[leaders + kid]] / p.sum()
+                p[top[leaders]] = 0
+                for side in (-2e-5, 2e-5):
+                    u = [1 - 2.0 ** -24] * (leaders + kid) + [level * (1 + side)]
+                    cases.append((x, top[: leaders + kid + 1], u))
+    # the children as nodes from `first` on, padding between
+    nodes = first + 4
+    B = len(cases)
+    tokens, parents = np.full((B, nodes), -1), np.zeros((B, nodes), np.int64)
+    parents[:, 0], u = -1, np.full((B, nodes), 0.5, np.float32)
+    logits = torch.zeros(B, nodes, vocab, dtype=cases[0][0].dtype)
+    for r, (x, kids, draws) in enumerate(cases):
+        logits[r, 0] = x
+        tokens[r, 0] = 0
+        tokens[r, first : first + len(kids)] = kids
+        u[r, first : first + len(kids)] = draws
+    logits = logits.view(B * nodes, vocab)
+    noise = np.maximum(rng.exponential(size=(B, vocab)), 1e-6).astype(np.float32)
+    c = dict(x=logits, y=None, logits=logits.double().numpy(), draft=None, tokens=tokens.ravel(), parents=parents.ravel(),
+             qsl=np.arange(0, B * nodes + 1, nodes), heat=np.ones(B, np.float32), u=u.ravel(), noise=noise, most=3)
+    for lo in range(0, B, 8 if vocab > 10000 else B):  # few rows: several blocks each
+        hi = min(B, lo + (8 if vocab > 10000 else B))
+        part = dict(c, x=logits[lo * nodes : hi * nodes], logits=c["logits"][lo * nodes : hi * nodes],
+                    tokens=c["tokens"][lo * nodes : hi * nodes], parents=c["parents"][lo * nodes : hi * nodes],
+                    qsl=c["qsl"][: hi - lo + 1], heat=c["heat"][lo:hi], u=c["u"][lo * nodes : hi * nodes],
+                    noise=noise[lo:hi])
+        got = _call(part)
+        assert got[4] == 0
+        _near(part, got)
+
+
+@gpu
+@pytest.mark.parametrize("fp32", [False, True])
+def test_drafts_close_to_their_target(fp32):
+    """p - q of nearly equal p and q, both good to e = 2^-22 + 3 2^-24 d (see above; d < 8) and twice that with their
+    sums: off by 4 e p, and the residual's mass by as much of the whole. Draws twice that far from a border."""
+    vocab, rng = 2000, np.random.default_rng(23)
+    dtype = torch.float32 if fp32 else torch.bfloat16
+    e = 2.0 ** -22 + 24 * 2.0 ** -24
+    rows = []
+    for noise in (0.1, 0.01, 1e-3):
+        x = torch.from_numpy(rng.standard_normal(vocab)).to(dtype)
+        y = (x.double() + torch.from_numpy(rng.standard_normal(vocab) * noise)).to(dtype)
+        p, q = (torch.softmax(t.double(), 0).numpy() for t in (x, y))
+        r = np.maximum(p - q, 0)
+        m = r.sum()
+        if m == 0:
+            continue
+        kid = int(np.argmax(r / p * (r < m * q)))  # rejected at times, with as much of p left as there is
+        level = r[kid] / m / q[kid]
+        off = 8 * e * (p[kid] / r[kid] + 1 / m)
+        lost = int(np.argmin(p / q))  # rejected by any draw above p / q
+        for side in (-off, off):
+            if 0 < level * (1 + side) < 1:
+                rows.append((x, y, [lost, kid], [1 - 2.0 ** -24, level * (1 + side)]))
+    assert len(rows) >= 4
+    B = len(rows)
+    x = torch.stack([t for r in rows for t in (r[0], r[0], r[0])])
+    y = torch.stack([t for r in rows for t in (r[1], r[1], r[1])])
+    c = dict(x=x, y=y, logits=x.double().numpy(), draft=y.double().numpy(), tokens=np.array([[0] + r[2] for r in rows]).ravel(),
+             parents=np.tile([-1, 0, 0], B), qsl=np.arange(0, 3 * B + 1, 3), heat=np.ones(B, np.float32),
+             u=np.array([[0.5] + r[3] for r in rows], np.float32).ravel(),
+             noise=np.maximum(rng.exponential(size=(B, vocab)), 1e-6).astype(np.float32), most=2)
+    _near(c, _call(c))
+
+
 def _args():
     """Valid arguments (CPU tensors: nothing is launched)."""
     z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t)  # noqa: E731
