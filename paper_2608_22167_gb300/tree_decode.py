@@ -60,7 +60,7 @@ class PagedCache:
                 raise ValueError("the keys of a sliding window are let go by their age")
             self.key_weights = torch.zeros(layers, rows, num_kv_heads, max_pages * PAGE, device=device)
             self.weights_workspace = mcpu.new_weights_workspace(d, device)
-            self.asked = [None] * layers  # (q, lse, scale) of each layer's last attention
+            self.asked = [None] * layers  # (q, lse, scale, window) of each layer's last attention
 
     def check(self):
         """Raises if a call so far has reported a device-side error (synchronises)."""
@@ -94,7 +94,7 @@ class PagedCache:
                                          query_start_loc, tree_mask, positions, sliding_window, scale, out, lse,
                                          self.workspace, sinks=sinks)
         if self.key_weights is not None:
-            self.asked[layer] = (q, lse, scale)
+            self.asked[layer] = (q, lse, scale, sliding_window)
         return out, lse
 
     def verify(self, logits, tokens, parents, query_start_loc, max_accept, temperature=None, draft_logits=None,
@@ -118,16 +118,18 @@ class PagedCache:
     def observe(self, query_start_loc, path=None, path_len=None, decay=1.0):
         """Counts the attention of the last step's queries (those of the accepted nodes, once `keep` has moved their
         keys; None: all) for every layer; earlier weights are multiplied by decay."""
-        for layer, (q, lse, scale) in enumerate(self.asked):
-            mcpu.mcpu_accumulate_weights(q, lse, self.k[layer], self.block_table, self.seq_lens, query_start_loc, 0, scale,
-                                         decay, self.key_weights[layer], self.weights_workspace, query_path=path,
+        for layer, (q, lse, scale, window) in enumerate(self.asked):
+            mcpu.mcpu_accumulate_weights(q, lse, self.k[layer], self.block_table, self.seq_lens, query_start_loc, window,
+                                         scale, decay, self.key_weights[layer], self.weights_workspace, query_path=path,
                                          path_len=path_len)
         self.asked = [None] * len(self.asked)
 
     def evict(self, budget, keep_first=4, keep_last=32, limit=None):
         """Rows of more than `limit` keys (None: budget) are cut to budget: the first, the last, and those that got
         most attention, for every kv head of every layer by itself. Rows that share pages are left alone and reported:
-        their forks would lose the keys too. Positions go on from `seq_lens + evicted`."""
+        their forks would lose the keys too. Positions go on from `seq_lens + evicted`. Layers with a window of at
+        most keep_last stay right, since the last keys stay next to each other: `attend` is given positions less
+        `evicted` there, which are the slots that the window counts."""
         mcpu.mcpu_evict_kv(self.pools, self.key_weights, self.block_table, self.seq_lens, budget if limit is None else limit,
                            budget, keep_first, keep_last, self.key_weights, self.new_lens, self.status,
                            page_refs=self.page_refs)

@@ -260,3 +260,37 @@ def test_a_captured_round_follows_its_inputs():
 def test_windowed_caches_count_no_weights():
     with pytest.raises(ValueError):
         _cache(1, device="cpu", sliding_window=64)
+
+
+@gpu
+def test_layers_with_windows_of_their_own():
+    """Each layer's weights are those of its attention: a query's sum to one, and keys before its window get none (a
+    term is good to 2.2e-5, and 1e-4 of the log-sum-exp)."""
+    from paper_2608_22167_gb300.tree_decode import rope_table, tree_masks
+
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(11)
+    rows, lens, windows = 2, [70, 31], [0, 20, 128]
+    cache = _cache(rows, layers=3)
+    chains = [list(range(-1, n - 1)) for n in lens]
+    qsl = torch.tensor([0, 70, 101], dtype=torch.int32, device="cuda")
+    cache.extend(torch.tensor(lens, device="cuda"))
+    ones, tab = torch.ones(64, device="cuda"), rope_table(200)
+    qs = []
+    for layer, window in enumerate(windows):
+        mask, depth = tree_masks(chains, window)
+        x = torch.randn(sum(lens), HQ + 2 * HKV, 64, generator=gen, device="cuda", dtype=torch.bfloat16)
+        q = cache.append(layer, x[:, :HQ], x[:, HQ:HQ + HKV], x[:, HQ + HKV:], ones, ones, 1e-6, tab, qsl, depth.cuda())
+        cache.attend(layer, q, qsl, mask.cuda(), depth.cuda(), sliding_window=window)
+        qs.append(q)
+    cache.observe(qsl)
+    cache.check()
+    for layer, window in enumerate(windows):
+        for r, n in enumerate(lens):
+            k, q = _keys(cache, layer, r), qs[layer][int(qsl[r]):int(qsl[r + 1])].double().view(n, HKV, -1, 64)
+            x = torch.einsum("nhgd,khd->nhgk", q, k) * 0.125
+            ahead = torch.arange(n, device="cuda")[:, None] - torch.arange(n, device="cuda")
+            hidden = (ahead < 0) | (ahead >= (window or n))
+            want = x.masked_fill(hidden[:, None, None], -torch.inf).softmax(-1).sum((0, 2))
+            got = cache.key_weights[layer, r, :, :n].double()
+            assert torch.all((got - want).abs() <= 1.3e-4 * want + 1e-9)
