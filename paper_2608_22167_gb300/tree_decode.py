@@ -22,6 +22,8 @@ the toy model's projections.
 """
 from __future__ import annotations
 
+from bisect import bisect_left, insort
+
 import torch
 
 from . import mcpu
@@ -29,10 +31,16 @@ from . import mcpu
 PAGE, HEAD_DIM = 16, 64
 
 
+def _span(x):
+    """Where a dense tensor lies."""
+    return x.data_ptr(), x.data_ptr() + x.numel() * x.element_size()
+
+
 class PagedCache:
     """The pools, table, page counts and stack of layers that share a block table. sliding_window > 0: all of them
     attend within that window, and `keep` returns the pages before it. count_weights: `keep` (or `observe`) counts the
-    attention that every key got, for `evict`; `attend` then keeps hold of each layer's q and log-sum-exps until then."""
+    attention that every key got, for `evict`; `attend` keeps hold of each layer's q and log-sum-exps until then, so
+    they are not to be written before, and layers do not share them."""
 
     def __init__(self, layers, rows, max_pages, num_pages, num_q_heads, num_kv_heads, device="cuda", sliding_window=0,
                  count_weights=False):
@@ -55,12 +63,13 @@ class PagedCache:
         self.status = mcpu.status_word(self.workspace)
         self.evicted = torch.zeros(rows, **i32)  # keys that a row has lost: its slot s holds no earlier position than s + evicted
         self.key_weights = self.weights_workspace = None
+        self.asked = [None] * layers  # (q, lse, scale, window) of each layer's last attention, if weights are counted,
+        self.spans = []               # and where its tensors lie: (begin, end, layer), ascending
         if count_weights:
             if sliding_window > 0:
                 raise ValueError("the keys of a sliding window are let go by their age")
             self.key_weights = torch.zeros(layers, rows, num_kv_heads, max_pages * PAGE, device=device)
             self.weights_workspace = mcpu.new_weights_workspace(d, device)
-            self.asked = [None] * layers  # (q, lse, scale, window) of each layer's last attention
 
     def check(self):
         """Raises if a call so far has reported a device-side error (synchronises)."""
@@ -78,7 +87,10 @@ class PagedCache:
 
     def append(self, layer, q, k, v, q_weight, k_weight, eps, cos_sin, query_start_loc, positions=None, q_out=None):
         """Norm, rotation and KV append of a layer's projected q, k and v; returns the rotated q."""
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            self._not_held(layer, q_out)
         mcpu.mcpu_norm_rope_kv_append(q, k, v, q_weight, k_weight, eps, positions, cos_sin, q_out, self.k[layer],
                                       self.v[layer], self.block_table, self.seq_lens, query_start_loc, self.status)
         return q_out
@@ -88,13 +100,16 @@ class PagedCache:
         """Attention of every node over its row's context (in the cache's window, if none is given) and the nodes
         its mask names: in a window the mask has to keep to it too (tree_masks)."""
         sliding_window = self.sliding_window if sliding_window is None else sliding_window
+        self._not_held(layer, q, lse, out)
+        if out is not None and self.key_weights is not None and _span(out)[0] < _span(q)[1] and _span(q)[0] < _span(out)[1]:
+            raise ValueError("the output may not take the place of q, whose attention is yet to be counted")
         out = torch.empty_like(q) if out is None else out
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if lse is None else lse
         mcpu.mcpu_tree_attention_forward(q, self.k[layer], self.v[layer], self.block_table, self.seq_lens,
                                          query_start_loc, tree_mask, positions, sliding_window, scale, out, lse,
                                          self.workspace, sinks=sinks)
         if self.key_weights is not None:
-            self.asked[layer] = (q, lse, scale, sliding_window)
+            self._hold(layer, q, lse, scale, sliding_window)
         return out, lse
 
     def verify(self, logits, tokens, parents, query_start_loc, max_accept, temperature=None, draft_logits=None,
@@ -122,7 +137,7 @@ class PagedCache:
             mcpu.mcpu_accumulate_weights(q, lse, self.k[layer], self.block_table, self.seq_lens, query_start_loc, window,
                                          scale, decay, self.key_weights[layer], self.weights_workspace, query_path=path,
                                          path_len=path_len)
-        self.asked = [None] * len(self.asked)
+        self._let_go()
 
     def evict(self, budget, keep_first=4, keep_last=32, limit=None):
         """Rows of more than `limit` keys (None: budget) are cut to budget: the first, the last, and those that got
@@ -167,6 +182,29 @@ class PagedCache:
         self.seq_lens[rows] = 0
         self.evicted[rows] = 0
         self._release(self.seq_lens)
+
+    def _hold(self, layer, q, lse, scale, sliding_window):
+        self.asked[layer] = (q, lse, scale, sliding_window)
+        self.spans = [s for s in self.spans if s[2] != layer]
+        for x in (q, lse):
+            insort(self.spans, (*_span(x), layer))
+
+    def _not_held(self, layer, *tensors):
+        """Refuses buffers that hold what another layer's attention is yet to be counted from."""
+        for x in tensors if self.spans else ():
+            if x is None or x.numel() == 0:
+                continue
+            begin, end = _span(x)
+            for s in self.spans[max(bisect_left(self.spans, (begin,)) - 1, 0):]:
+                if s[0] >= end:
+                    break
+                if s[1] > begin and s[2] != layer:
+                    raise ValueError("each layer needs q and log-sum-exps of its own until their attention is counted")
+
+    def _let_go(self):
+        """What was held is counted, or can be no more."""
+        self.asked = [None] * len(self.k)
+        self.spans = []
 
     def _release(self, lens, sliding_window=0):
         torch.minimum(self.held_lens, lens, out=self.held_lens)

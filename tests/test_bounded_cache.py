@@ -294,3 +294,23 @@ def test_layers_with_windows_of_their_own():
             want = x.masked_fill(hidden[:, None, None], -torch.inf).softmax(-1).sum((0, 2))
             got = cache.key_weights[layer, r, :, :n].double()
             assert torch.all((got - want).abs() <= 1.3e-4 * want + 1e-9)
+
+
+def test_buffers_that_layers_share_are_refused():
+    """A counting cache holds each layer's q and log-sum-exps until they are counted."""
+    cache = _cache(1, device="cpu")
+    q, lse = torch.zeros(3, 4, HQ, 64, dtype=torch.bfloat16), torch.zeros(3, 4, HQ)
+    cache._hold(0, q[0], lse[0], 0.125, 0)
+    qsl, mask = torch.zeros(2, dtype=torch.int32), torch.zeros(4, 1, dtype=torch.int32)
+    for bad in (dict(q=q[0], lse=lse[1]), dict(q=q[1], lse=lse[0]), dict(q=q.view(12, HQ, 64)[3:7]),
+                dict(q=q[1], lse=lse.view(12, HQ)[3:7]), dict(q=q[1], out=q[0]), dict(q=q[1], out=q[1])):
+        with pytest.raises(ValueError, match="counted"):
+            cache.attend(1, bad.pop("q"), qsl, mask, **bad)
+    kv, ones = torch.zeros(4, HKV, 64, dtype=torch.bfloat16), torch.ones(64)
+    with pytest.raises(ValueError, match="counted"):
+        cache.append(1, q[2], kv, kv, ones, ones, 1e-6, torch.zeros(9, 64), qsl, q_out=q[0])
+    assert cache.asked[1] is None
+    # other buffers, and the layer's own, get as far as the kernels' own checks
+    for good in (dict(layer=1, q=q[1], lse=lse[1]), dict(layer=0, q=q[0], lse=lse[0])):
+        with pytest.raises(ValueError, match="^(?!.*counted)"):
+            cache.attend(good["layer"], good["q"], qsl, mask.double(), lse=good["lse"])
