@@ -165,15 +165,25 @@ class PagedCache:
 
     def fork(self, src_rows, dst_rows):
         """Rows dst_rows (empty) become copies of src_rows: full pages shared, partial last pages copied. Not between
-        a row's `append` and its `keep`, which moves rows inside pages that would be shared by then."""
+        a row's `append` and its `keep`, which moves rows inside pages that would be shared by then. Pairs that do not
+        name two rows are skipped and reported."""
         n = src_rows.shape[0]
+        if self.key_weights is not None and n > 0:
+            # what the kernel skips does as the first pair that it does not, or (none) copies row 0 to itself
+            src, dst = src_rows.long(), dst_rows.long()
+            lens = self.seq_lens[src.clamp(0, self.rows - 1)]
+            pair = (src >= 0) & (src < self.rows) & (dst >= 0) & (dst < self.rows) & (src != dst) & (lens >= 0) & \
+                (lens <= self.block_table.shape[1] * PAGE)
+            first = pair.int().argmax().expand(1)
+            some = pair.any()
+            src = torch.where(pair, src, torch.where(some, src[first], 0))
+            dst = torch.where(pair, dst, torch.where(some, dst[first], 0))
         copy = torch.empty(2, n, dtype=torch.int32, device=src_rows.device)
         mcpu.mcpu_fork_block_tables(self.block_table, self.seq_lens, src_rows, dst_rows, self.page_refs,
                                     self.free_pages, self.free_count, copy[0], copy[1], self.page_scratch, self.status)
         mcpu.mcpu_copy_pages(self.pools, copy[0], copy[1], self.status)
-        src, dst = src_rows.long(), dst_rows.long()
-        self.evicted[dst] = self.evicted[src]
-        if self.key_weights is not None:
+        if self.key_weights is not None and n > 0:
+            self.evicted[dst] = self.evicted[src]
             self.key_weights[:, dst] = self.key_weights[:, src]
         self.held_lens.copy_(self.seq_lens)
 

@@ -314,3 +314,35 @@ def test_buffers_that_layers_share_are_refused():
     for good in (dict(layer=1, q=q[1], lse=lse[1]), dict(layer=0, q=q[0], lse=lse[0])):
         with pytest.raises(ValueError, match="^(?!.*counted)"):
             cache.attend(good["layer"], good["q"], qsl, mask.double(), lse=good["lse"])
+
+
+@gpu
+@pytest.mark.parametrize("counting", [False, True])
+def test_forks_of_rows_that_do_not_exist_change_no_other_row(counting):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(13)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    if counting:
+        cache = _cache(6)
+    else:
+        from paper_2608_22167_gb300.tree_decode import PagedCache
+
+        cache = PagedCache(2, 6, 24, 300, HQ, HKV)
+    lens = [80, 37, 0, 0, 0, 50]
+    _, qsl = _step(cache, gen, [0] * 6, lens, [list(range(-1, n - 1)) for n in lens])
+    if counting:
+        cache.observe(qsl)
+        cache.evict(48, keep_first=2, keep_last=5)
+        assert cache.evicted.tolist() == [32, 0, 0, 0, 0, 2]
+    cache.check()
+    before = (cache.seq_lens.tolist(), cache.evicted.tolist(), None if not counting else cache.key_weights.clone())
+    for src, dst in (([-1, 0, 9, 1, 5, 3], [3, 2, 4, 77, -1, 3]), ([-1], [1]), ([6], [0]), ([1], [6])):
+        cache.fork(torch.tensor(src, **i32), torch.tensor(dst, **i32))
+        assert cache.status.item() == 2
+        cache.status.zero_()
+    lens, evicted, weights = before
+    lens[2], evicted[2] = lens[0], evicted[0]  # the one pair that names two rows
+    assert cache.seq_lens.tolist() == lens and cache.evicted.tolist() == evicted
+    if counting:
+        weights[:, 2] = weights[:, 0]
+        assert torch.equal(cache.key_weights, weights)
