@@ -663,7 +663,8 @@ mcpu_status mcpu_copy_pages(void* const* pools, int32_t num_pools, int64_t page_
  * row's path_len[r] query tokens query_path[r * max_path + i] (numbers in the
  * row, 0 .. L_r - 1, in any order and as often as wanted), C_r = S_r -
  * path_len[r]: the accepted nodes once mcpu_compact_kv has moved them (with its
- * new_seq_lens), or the last queries of a long prompt alone.
+ * new_seq_lens), or the last queries of a long prompt alone. Slots before C_r
+ * that no call has counted have to hold what they start from (0).
  * decay in [0, 1]; 0 reads no old weights. softmax_scale in [1e-30, 1e30]. A row
  * without queries keeps its weights as they are, and so do slots from S_r on. A
  * query with lse = -inf (it saw nothing) or inf adds nothing to finite keys; a
@@ -685,7 +686,9 @@ mcpu_status mcpu_copy_pages(void* const* pools, int32_t num_pools, int64_t page_
  * holes, lowest into lowest; the last keep_last follow in order. K, V and the
  * weights move; new_key_weights (may be key_weights) receives the weights of all
  * slots < new_seq_lens[r], which is budget, or S_r for a row left as it is.
- * Slots past it keep stale contents; mcpu_shrink_block_tables returns their pages.
+ * Slots past it keep stale contents (mcpu_shrink_block_tables returns their
+ * pages), except that in key_weights itself those of a row that was cut become
+ * 0 up to S_r: keys that take them later and are not counted start from nothing.
  * limit >= budget >= keep_first + keep_last, budget >= 1. The slot of a key no
  * longer says its position afterwards: give positions to
  * mcpu_norm_rope_kv_append (it rotates at any, whatever the slot), and do not

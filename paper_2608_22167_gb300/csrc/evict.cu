@@ -335,6 +335,13 @@ __global__ void __launch_bounds__(S::kThreads, S::kResident)
     if (threadIdx.x < count) nw[inner + i0 + threadIdx.x] = weight;
     if (!apart) __syncthreads();
   }
+
+  // ---- slots that are free now: keys that take them start without weight
+  if (p.new_weights == p.weights) {
+    __syncthreads();
+    float* row = p.new_weights + (((size_t)blockIdx.z * p.num_seqs + blockIdx.y) * gridDim.x + blockIdx.x) * p.max_slots;
+    for (int j = p.budget + threadIdx.x; j < n; j += kThreads) row[j] = 0.f;
+  }
 }
 
 }  // namespace

@@ -190,7 +190,9 @@ class PagedCache:
     def drop(self, rows):
         """Frees the rows (int64 indices)."""
         self.seq_lens[rows] = 0
-        self.evicted[rows] = 0
+        if self.key_weights is not None:
+            self.evicted[rows] = 0
+            self.key_weights[:, rows] = 0  # the slots of rows to come start without weights
         self._release(self.seq_lens)
 
     def _hold(self, layer, q, lse, scale, sliding_window):

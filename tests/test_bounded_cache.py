@@ -346,3 +346,33 @@ def test_forks_of_rows_that_do_not_exist_change_no_other_row(counting):
     if counting:
         weights[:, 2] = weights[:, 0]
         assert torch.equal(cache.key_weights, weights)
+
+
+@gpu
+def test_slots_taken_again_start_without_weights():
+    """Rows that are dropped or cut leave no weights behind: where a later step is not counted, its keys have none."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(14)
+    rows, lens = 3, [100, 90, 40]
+    cache = _cache(rows)
+    chains = [list(range(-1, n - 1)) for n in lens]
+    _, qsl = _step(cache, gen, [0] * rows, lens, chains)
+    cache.observe(qsl)
+    cache.drop(torch.tensor([1], device="cuda"))
+    cache.evict(64, keep_first=3, keep_last=10)
+    cache.check()
+    assert cache.seq_lens.tolist() == [64, 0, 40]
+    for r, n in enumerate((64, 0, 40)):
+        assert torch.all(cache.key_weights[:, r, :, :n] > 0) and not cache.key_weights[:, r, :, n:].any()
+    # a prompt, and more of it, that nobody counts; then one token that is counted
+    cache.held_lens.copy_(cache.seq_lens)
+    before = cache.key_weights.clone()
+    _step(cache, gen, [64, 0, 40], [30, 50, 2], [list(range(-1, n - 1)) for n in (30, 50, 2)])
+    cache.held_lens.copy_(cache.seq_lens)
+    _, qsl = _step(cache, gen, [94, 50, 42], [1, 1, 1], [[-1]] * 3)
+    cache.observe(qsl)
+    cache.check()
+    added = cache.key_weights - before
+    g = HQ // HKV
+    want = torch.full((rows,), float(g), device="cuda", dtype=torch.float64)  # one query of g heads a kv head, 2.2e-5 + 1e-4
+    assert torch.all((added.double().sum(3) - want[None, :, None]).abs() <= 1.3e-4 * g + 150 * 2.0 ** -24 * 8)
