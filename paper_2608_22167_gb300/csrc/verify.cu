@@ -561,7 +561,16 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
       const float wm = warp_max(m[d]);
       int at = 0x7fffffff;
       if (greedy) {
-        if (m[d] == wm) {  // the lowest token that has it, among this thread's of that step
+        if (sizeof(T) == 4 && wm == kLowest) {
+          // the value that maxima begin with: no step has raised it, so the first
+          // of the thread's tokens that has it, if any has (else the sum is 0)
+          const int n = z[d] > 0.f ? slice.steps(One::kGroups) * One::kGroups * 8 : 0;
+#pragma unroll 1
+          for (int i = 0; i < n && at == 0x7fffffff; ++i) {
+            const int e = i >> 3, j = slice.group(slice.step(e / One::kGroups, One::kGroups), e % One::kGroups) + (i & 7);
+            if (j >= slice.begin && j < slice.end && at_token(x, j) == wm) at = j;
+          }
+        } else if (m[d] == wm) {  // the lowest token that has it, among this thread's of that step
           const bool held = best_step >= slice.steps(One::kGroups) - One::kDepth;  // it is in the ring still
           uint8_t* slot = ring + best_step % One::kDepth * One::kBytes;
 #pragma unroll 1

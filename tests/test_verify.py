@@ -419,6 +419,24 @@ def test_drafts_close_to_their_target(fp32):
     _near(c, _call(c))
 
 
+@gpu
+@pytest.mark.parametrize("rows", [1, 3, 400])
+@pytest.mark.parametrize("heat", [0.0, 1.0])
+def test_rows_with_nothing_but_the_lowest_value_of_32_bits(rows, heat):
+    vocab = 40000
+    c = _case([1] * rows, vocab, seed=24, fp32=True, heats=(heat,))
+    c["x"][:] = -torch.inf
+    for r in range(rows):
+        at = [39000 - 61 * r, 39990 - r, 39999]
+        c["x"][r, at] = torch.finfo(torch.float32).min
+    c["logits"] = c["x"].double().numpy()
+    got, want = _call(c), reference(c)
+    assert got[4] == 0
+    for g, w in zip(got[:3], want[:3]):
+        assert np.array_equal(g, w)
+    assert np.all(np.abs(got[3] - want[3]) <= 2.0 ** -22)
+
+
 def _args():
     """Valid arguments (CPU tensors: nothing is launched)."""
     z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t)  # noqa: E731
