@@ -81,6 +81,7 @@ class PagedCache:
     def extend(self, new_lens):
         """Row lengths after the next append (int32 [rows]) and the pages for them. What is appended follows the tokens
         that a row holds: pages before that may be shared with other rows."""
+        self._let_go()
         self.seq_lens.copy_(new_lens)
         mcpu.mcpu_grow_block_tables_from(self.block_table, self.seq_lens, self.held_lens, self.free_pages,
                                          self.free_count, self.status)
@@ -132,7 +133,9 @@ class PagedCache:
 
     def observe(self, query_start_loc, path=None, path_len=None, decay=1.0):
         """Counts the attention of the last step's queries (those of the accepted nodes, once `keep` has moved their
-        keys; None: all) for every layer; earlier weights are multiplied by decay."""
+        keys; None: all) for every layer; earlier weights are multiplied by decay. Before `extend` or `evict`, which
+        change what the queries saw."""
+        self._check_counted()
         for layer, (q, lse, scale, window) in enumerate(self.asked):
             mcpu.mcpu_accumulate_weights(q, lse, self.k[layer], self.block_table, self.seq_lens, query_start_loc, window,
                                          scale, decay, self.key_weights[layer], self.weights_workspace, query_path=path,
@@ -145,9 +148,12 @@ class PagedCache:
         their forks would lose the keys too. Positions go on from `seq_lens + evicted`. Layers with a window of at
         most keep_last stay right, since the last keys stay next to each other: `attend` is given positions less
         `evicted` there, which are the slots that the window counts."""
+        if self.key_weights is None:
+            raise ValueError("keys are evicted by the weights of a cache made with count_weights")
         mcpu.mcpu_evict_kv(self.pools, self.key_weights, self.block_table, self.seq_lens, budget if limit is None else limit,
                            budget, keep_first, keep_last, self.key_weights, self.new_lens, self.status,
                            page_refs=self.page_refs)
+        self._let_go()
         self.evicted += self.seq_lens - self.new_lens
         self.seq_lens.copy_(self.new_lens)
         self._release(self.seq_lens)
@@ -155,6 +161,8 @@ class PagedCache:
     def keep(self, query_start_loc, path, path_len, decay=1.0):
         """Keeps the accepted nodes path[r, :path_len[r]] of each row's tree, in every layer, counts their attention
         if weights are counted, and returns the pages behind them."""
+        if self.key_weights is not None:
+            self._check_counted()
         mcpu.mcpu_compact_kv(self.pools, self.block_table, self.seq_lens, query_start_loc, path, path_len,
                              self.new_lens, self.status)
         self.seq_lens.copy_(self.new_lens)
@@ -212,6 +220,12 @@ class PagedCache:
                     break
                 if s[1] > begin and s[2] != layer:
                     raise ValueError("each layer needs q and log-sum-exps of its own until their attention is counted")
+
+    def _check_counted(self):
+        if self.key_weights is None:
+            raise ValueError("attention is counted by a cache made with count_weights")
+        if None in self.asked:
+            raise ValueError(f"layer {self.asked.index(None)} has not attended since the last step was counted")
 
     def _let_go(self):
         """What was held is counted, or can be no more."""

@@ -376,3 +376,34 @@ def test_slots_taken_again_start_without_weights():
     g = HQ // HKV
     want = torch.full((rows,), float(g), device="cuda", dtype=torch.float64)  # one query of g heads a kv head, 2.2e-5 + 1e-4
     assert torch.all((added.double().sum(3) - want[None, :, None]).abs() <= 1.3e-4 * g + 150 * 2.0 ** -24 * 8)
+
+
+def test_steps_that_cannot_be_counted_are_refused():
+    from paper_2608_22167_gb300.tree_decode import PagedCache
+
+    cache, plain = _cache(1, device="cpu"), PagedCache(2, 1, 24, 300, HQ, HKV, device="cpu")
+    qsl, path, n = (torch.zeros(s, dtype=torch.int32) for s in ((2,), (1, 1), (1,)))
+    lens = cache.seq_lens.clone()
+    for held in ([None, None], [(None, None, 0.125, 0), None]):  # nothing attended, or one layer of two
+        cache.asked = list(held)
+        for call in (lambda: cache.observe(qsl), lambda: cache.keep(qsl, path, n)):
+            with pytest.raises(ValueError, match="attended"):
+                call()
+        assert cache.asked == held and torch.equal(cache.seq_lens, lens)
+    for call in (lambda: plain.evict(64), lambda: plain.observe(qsl)):
+        with pytest.raises(ValueError, match="count_weights"):
+            call()
+
+
+@gpu
+def test_what_was_held_is_let_go_where_it_no_longer_fits():
+    """Lengths or slots that changed since the attention would give its weights to other keys."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(12)
+    cache = _cache(1)
+    for change in (lambda: cache.extend(cache.seq_lens + 1), lambda: cache.evict(40)):
+        _, qsl = _step(cache, gen, cache.seq_lens.tolist(), [20], [list(range(-1, 19))])
+        change()
+        with pytest.raises(ValueError, match="attended"):
+            cache.observe(qsl)
+    cache.check()
