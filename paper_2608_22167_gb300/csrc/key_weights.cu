@@ -635,12 +635,26 @@ __global__ void __launch_bounds__(kThreads, 1)
               *reinterpret_cast<uint4*>(base_ptr + (sQ - base) + rq.s * kQBytes + swz128(c, lane & 7)) = v[k];
             }
           }
+          // The last query's once more in the columns that fill the product up, all
+          // but weightless there: seen by the keys that see it, they add nothing that
+          // it does not (zeros would: 0 * inf is NaN).
+          const int spare = -cols & 15;
+          if (spare) {
+            uint8_t* stage = base_ptr + (sQ - base) + rq.s * kQBytes;
+            __syncwarp();
+#pragma unroll 1
+            for (int i = lane; i < 8 * spare; i += 32) {
+              const int c = cols + (i >> 3);
+              *reinterpret_cast<uint4*>(stage + swz128(c, i & 7)) =
+                  *reinterpret_cast<const uint4*>(stage + swz128(cols - g + (c & (g - 1)), i & 7));
+            }
+          }
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           // an infinite lse, of a query that saw nothing too, leaves weights of 0
           const int c = 32 * k + lane;
-          const float x = nl[k] == -INFINITY ? -INFINITY : -nl[k] * p.inv_scale;
+          const float x = c >= cols ? -3e38f : nl[k] == -INFINITY ? -INFINITY : -nl[k] * p.inv_scale;
           const __nv_bfloat16 hi = __float2bfloat16_rn(x);
           const float r1 = x - __bfloat162float(hi);
           const __nv_bfloat16 mid = __float2bfloat16_rn(r1);

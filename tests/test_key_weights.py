@@ -345,6 +345,23 @@ def test_paths_of_more_queries_than_the_step_has(window):
     Batch([5000, 90], [40, 2], 8, 1, seed=17, window=window, path=path).check(decay=0.5)
 
 
+@gpu
+@pytest.mark.parametrize("n", [1, 3, 17])
+def test_keys_with_infinite_scores(n):
+    """A key that every query scores -inf weighs nothing, one scored inf weighs inf: whatever the number of queries."""
+    b = Batch([120, 40], [n, 1], 8, 1, seed=18)
+    b.q[..., 0] = np.abs(b.q[..., 0]) + 1.0
+    (b.qt, b.q) = bf(b.q)
+    for key, value in ((5, -np.inf), (9, np.inf)):
+        page, slot = b.bt[0, key // 16], key % 16
+        b.k[page, 0, slot, 0] = b.kt[page, 0, slot, 0] = value
+    got = b.run().double().cpu().numpy()
+    want, bound = b.reference(0.125, 1.0)
+    assert got[0, 0, 5] == b.old[0, 0, 5] and got[0, 0, 9] == np.inf
+    finite = np.isfinite(want)
+    assert np.all(np.abs(got - want)[finite] <= bound[finite])
+
+
 def _args():
     from paper_2608_22167_gb300 import mcpu  # noqa: F401
 
