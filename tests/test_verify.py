@@ -437,6 +437,21 @@ def test_rows_with_nothing_but_the_lowest_value_of_32_bits(rows, heat):
     assert np.all(np.abs(got[3] - want[3]) <= 2.0 ** -22)
 
 
+@gpu
+@pytest.mark.parametrize("fp32", [False, True])
+def test_greedy_rows_take_what_the_host_takes(fp32):
+    from paper_2608_22167_gb300.tree_decode import accept_greedy
+
+    c = _case(np.arange(1, 65), 500, seed=25, fp32=fp32, heats=(0.0,), spread=0.7)
+    c["parents"] = np.concatenate([np.maximum(random_tree(n, np.random.default_rng(n)), np.where(np.arange(n), 0, -1))
+                                   for n in range(1, 65)])
+    path, length, following, _, status = _call(c)
+    assert status == 0 and length.max() > 2
+    for r, (a, b) in enumerate(zip(c["qsl"], c["qsl"][1:])):
+        want, token = accept_greedy(c["parents"][a:b].tolist(), c["tokens"][a:b].tolist(), c["logits"][a:b].argmax(1))
+        assert path[r, : length[r]].tolist() == want and following[r] == token
+
+
 def _args():
     """Valid arguments (CPU tensors: nothing is launched)."""
     z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t)  # noqa: E731
