@@ -521,7 +521,9 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
  * and p = softmax(logits / T) of the node the walk is at (first node 0, which
  * is always accepted), its children c are tried in ascending order:
  *   draft_logits given:  q = softmax(draft_logits / T) of the same node, from
- *     which its children were drawn;  rest(y) = max(p(y) - M q(y), 0)
+ *     which its children were drawn, each by itself (the same token may come
+ *     twice: children drawn without replacement do not leave the target's
+ *     distribution under this rule);  rest(y) = max(p(y) - M q(y), 0)
  *     accept c iff uniforms[t_c] m q(x_c) < rest(x_c);  else M += m, m = sum_y rest(y)
  *   without (children chosen, not drawn):  rest(y) = p(y), 0 for the tokens of
  *     rejected children;  accept c iff uniforms[t_c] m < rest(x_c);  else m -= rest(x_c)
@@ -698,7 +700,8 @@ mcpu_status mcpu_copy_pages(void* const* pools, int32_t num_pools, int64_t page_
  * [num_pages], or NULL if no page is shared): a row that holds a page with
  * other holders among those of slots [keep_first, budget) is left as it is and
  * reported (MCPU_ERR_UNSUPPORTED_ROW): its keys cannot move without the other
- * rows'. A row with a page outside the pool there or up to S_r is left too
+ * rows'. Rows that share a prompt are cut with keep_first at the end of its full
+ * pages, or past it. A row with a page outside the pool there or up to S_r is left too
  * (MCPU_ERR_BAD_PAGE), and one longer than its table or max_slots
  * (MCPU_ERR_BAD_LENGTHS). new_seq_lens must not be seq_lens.
  */

@@ -357,7 +357,8 @@ __device__ __forceinline__ float fmax3(float a, float b, float c) {
 }
 
 // 2^x with the hardware approximation (MUFU.EX2; subnormal results flush to
-// zero). Used where the result is rounded to bf16 right after.
+// zero), to 2^-22. Rounded to bf16 right after in attention; verify.cu and
+// key_weights.cu add it up in fp32, with that in their bounds.
 __device__ __forceinline__ float ex2_approx(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

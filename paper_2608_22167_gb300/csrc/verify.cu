@@ -25,9 +25,11 @@
 // in flight, its instructions came from L2: 14000 cycles for one group of eight).
 //
 // Bound by the chain of a row's nodes where rows are few (64 rows, up to 7 nodes on
-// a path, 131072 bf16 logits: 42 us; a node's first loads, two steps, the
-// exchange), by HBM where they are many (384 rows of fp32 logits: 595 MB in 130
-// us, 68 % of the copy rate).
+// a path, 131072 bf16 logits: 34 to 50 us from process to process; a node's first
+// loads, two steps, the exchange), with SMs that hold no block for 36 % of the time
+// (512 blocks in places for 456: rows that come late begin as others end); by HBM
+// where they are many (384 rows of fp32 logits: 595 MB in 131 us, 67 % of the copy
+// rate; SMs hold a block for 83 % of the time).
 //
 // Everything is fp32. Sums are pairs: 8 terms at a time, added by an exact two-sum
 // (a plain chain of additions loses 1e-6 of a peaked distribution's tail).
@@ -861,8 +863,9 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
 }  // namespace
 
 cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_t stream) {
-  // blocks a row: as many as keep four per SM (64 greedy rows of 131072 logits: 8
-  // blocks a row 42 us, 4 50, 2 62, 1 89), four at least (384 sampled fp32 rows:
+  // blocks a row: as many as make four per SM, of which three fit at once and the
+  // others begin as rows end (64 greedy rows of 131072 logits: 8 blocks a row 42 us,
+  // 4 50, 2 62, 1 89), four at least (384 sampled fp32 rows:
   // 2 blocks a row 152 us, 4 144, 8 166), but half a group of logits for every
   // thread (2 rows of 16000: 8 blocks a row 17 us, 4 19, 2 21; of 4000: 2 17, 1 19)
   int size = 1;

@@ -144,8 +144,9 @@ class PagedCache:
 
     def evict(self, budget, keep_first=4, keep_last=32, limit=None):
         """Rows of more than `limit` keys (None: budget) are cut to budget: the first, the last, and those that got
-        most attention, for every kv head of every layer by itself. Rows that share pages are left alone and reported:
-        their forks would lose the keys too. Positions go on from `seq_lens + evicted`. Layers with a window of at
+        most attention, for every kv head of every layer by itself. Rows that share pages from keep_first on are left
+        alone and reported, which `check` tells from then on (their forks would lose the keys too): with a common
+        prompt keep_first reaches to the end of its full pages. Positions go on from `seq_lens + evicted`. Layers with a window of at
         most keep_last stay right, since the last keys stay next to each other: `attend` is given positions less
         `evicted` there, which are the slots that the window counts."""
         if self.key_weights is None:

@@ -359,7 +359,7 @@ def test_keys_with_infinite_scores(n):
     want, bound = b.reference(0.125, 1.0)
     assert got[0, 0, 5] == b.old[0, 0, 5] and got[0, 0, 9] == np.inf
     finite = np.isfinite(want)
-    assert np.all(np.abs(got - want)[finite] <= bound[finite])
+    assert np.all(np.abs(got[finite] - want[finite]) <= bound[finite])
 
 
 def _args():
