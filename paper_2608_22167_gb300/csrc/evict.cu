@@ -3,12 +3,12 @@
 // One block per (layer, row, kv head). Of the N = n - first - last middle slots
 // the K = budget - first - last with the highest weight stay: the K-th largest
 // is found by a radix select over the weights' bits (11, 11 and 10 of them, one
-// histogram each, no more once all of a bin stay), and among the slots that equal it the lowest are taken. Kept
-// slots below inner = budget - last stay where they are; there are as many holes
-// below it as kept slots past it, and the i-th of these moves into the i-th
-// hole. The last ones follow as one shift towards the front. Both regions are
-// walked in step, a block of slots at a time, and only as much of the two lists
-// is held as the next moves need.
+// histogram each, no more once all of a bin stay), and among the slots that equal
+// it the lowest are taken. Kept slots below inner = budget - last stay where they
+// are; there are as many holes below it as kept slots past it, and the i-th of
+// these moves into the i-th hole. The last ones follow as one shift towards the
+// front. Both regions are walked in step, a block of slots at a time, and only as
+// much of the two lists is held as the next moves need.
 //
 // Bound by the moves (K and V rows read and written, scattered 128-byte rows:
 // 6144 items of 2112 to 2560 keys cut to 2048 move 1.2 GB in 243 us, 78 % of the

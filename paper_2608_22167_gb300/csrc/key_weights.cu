@@ -27,9 +27,9 @@
 // Bound by the keys' way from HBM where queries are few (64 rows of 2047 to 16383
 // keys, 64 / 8 heads, one query each: 642 MB in 105 us, 90 % of the copy rate).
 // Where they are many, 1024 of a block's 1540 cycles are exponentials, 8 a clock
-// and sub-partition; the others are mostly TMEM loads, which a warp waits for before
-// it uses them (16 rows of 4096 to 32768 keys, 64 to 2048 queries: 3.2 ms, at 1.95 to
-// 2.07 GHz and below the power limit). There the log-sum-exps as a step of the
+// and sub-partition; the stall counted most is the wait for loads, and a warp waits
+// for its TMEM loads before it uses them (16 rows of 4096 to 32768 keys, 64 to 2048
+// queries: 3.2 ms, at 1.95 to 2.07 GHz and below the power limit). There the log-sum-exps as a step of the
 // product took 4.55 ms to 3.56: read for every column from shared memory they needed
 // 128 bytes a clock; and one box for 128 contiguous columns, not 16 bytes a lane,
 // 4.43 to 3.22.

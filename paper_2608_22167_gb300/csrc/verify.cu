@@ -14,10 +14,10 @@
 // the nodes that the walk visits are read. A node costs one pass over its
 // logits (maximum, its place and the sum together), a rejection with draft
 // probabilities one more (without, where little is left), the row's end one with
-// the exponentials; what was read before comes from L2 then. After a pass every warp hands its result to
-// all blocks of the cluster (distributed shared memory), and behind one cluster
-// barrier every warp joins them all in the same order: all take the same
-// decisions, and nothing is sent back.
+// the exponentials; what was read before comes from L2 then. After a pass every
+// warp hands its result to all blocks of the cluster (distributed shared memory),
+// and behind one cluster barrier every warp joins them all in the same order: all
+// take the same decisions, and nothing is sent back.
 //
 // A pass streams the rows through shared memory: every warp copies its part
 // ahead (cp.async) and takes it out again, with no block barrier, so that the
@@ -865,9 +865,8 @@ __global__ void __launch_bounds__(kThreads, 3) verify_kernel(const VerifyParams 
 cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_t stream) {
   // blocks a row: as many as make four per SM, of which three fit at once and the
   // others begin as rows end (64 greedy rows of 131072 logits: 8 blocks a row 42 us,
-  // 4 50, 2 62, 1 89), four at least (384 sampled fp32 rows:
-  // 2 blocks a row 152 us, 4 144, 8 166), but half a group of logits for every
-  // thread (2 rows of 16000: 8 blocks a row 17 us, 4 19, 2 21; of 4000: 2 17, 1 19)
+  // 4 50, 2 62, 1 89), four at least (384 sampled fp32 rows: 2 blocks a row 152 us,
+  // 4 144, 8 166), but half a group of logits for every thread (2 rows of 16000: 8 blocks a row 17 us, 4 19, 2 21; of 4000: 2 17, 1 19)
   int size = 1;
   while (size < kMaxCluster && (size < 4 || 2 * size * p.num_seqs <= 4 * sms) && size * 8 * kThreads <= p.vocab) size *= 2;
   cudaLaunchConfig_t cfg{};
