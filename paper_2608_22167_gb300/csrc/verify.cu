@@ -866,7 +866,8 @@ cudaError_t launch_verify(const VerifyParams& p, bool fp32, int sms, cudaStream_
   // blocks a row: as many as make four per SM, of which three fit at once and the
   // others begin as rows end (64 greedy rows of 131072 logits: 8 blocks a row 42 us,
   // 4 50, 2 62, 1 89), four at least (384 sampled fp32 rows: 2 blocks a row 152 us,
-  // 4 144, 8 166), but half a group of logits for every thread (2 rows of 16000: 8 blocks a row 17 us, 4 19, 2 21; of 4000: 2 17, 1 19)
+  // 4 144, 8 166), but half a group of logits for every thread (2 rows of 16000: 8
+  // blocks a row 17 us, 4 19, 2 21; of 4000: 2 17, 1 19)
   int size = 1;
   while (size < kMaxCluster && (size < 4 || 2 * size * p.num_seqs <= 4 * sms) && size * 8 * kThreads <= p.vocab) size *= 2;
   cudaLaunchConfig_t cfg{};

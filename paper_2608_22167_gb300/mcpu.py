@@ -811,7 +811,7 @@ def _on_one_device(*tensors):
 def _row_stride(x, what, dtypes, rows, width):
     """Elements from one row to the next of a [rows, width] tensor whose rows are dense."""
     if x.dtype not in dtypes or x.dim() != 2 or x.shape[0] != rows or x.shape[1] != width or \
-            (width > 1 and x.stride(1) != 1):
+            (rows > 0 and width > 1 and x.stride(1) != 1):
         raise ValueError(f"{what} must be a [{rows}, {width}] tensor of {' or '.join(map(str, dtypes))} with dense rows")
     stride = x.stride(0) if rows > 1 else width
     if stride < width:

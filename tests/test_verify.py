@@ -488,6 +488,25 @@ def test_binding_refuses_what_it_would_misread():
             mcpu.mcpu_verify_tree(**dict(args, **bad))
 
 
+def test_batches_without_nodes_have_no_rows_to_be_dense():
+    """An empty tensor's strides say nothing (of an array without rows they may be anything)."""
+    from paper_2608_22167_gb300 import mcpu
+
+    args = _args()
+    none = torch.zeros(0, dtype=torch.int32)
+    logits = torch.zeros(0, 30, dtype=torch.bfloat16).as_strided((0, 30), (1, 2))
+    args.update(logits=logits, draft_logits=logits, tokens=none, parents=none, uniforms=none.float())
+    with pytest.raises(ValueError, match="CUDA device"):  # as far as any valid call without a GPU
+        mcpu.mcpu_verify_tree(**args)
+
+
+@gpu
+def test_a_batch_without_nodes():
+    c = _case([0, 0, 0], 50, seed=26)
+    got = _call(c)
+    assert got[4] == 0 and not got[1].any() and np.all(got[2] == -1) and np.all(got[0] == -1) and not got[3].any()
+
+
 def test_host_checks():
     from paper_2608_22167_gb300 import mcpu
 
