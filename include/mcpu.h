@@ -552,10 +552,10 @@ mcpu_status mcpu_tree_attention_forward(const void* q, const void* k_cache, cons
  * logits, draft_logits: logits_type MCPU_BF16 or MCPU_FP32 elements, any
  * stride >= vocab. Everything is fp32, sums are pairs of it: a weight
  * e^((l - max) / T) is good to 2^-22 + 3 * 2^-24 |l - max| / T, relatively, and
- * 0 below 2^-126. A uniform may fall on either side of a child's border that it is as near to as,
- * relatively, 2^-15 without draft logits, however little of the probability the
- * rejected children left (|l - max| / T up to 30); with them, where p and M q
- * cancel, 2^-17 (p / rest + 1 / m) (|l - max| / T up to 8).
+ * 0 below 2^-126. A uniform may fall on either side of a child's border that is,
+ * relatively, as near as 2^-15 without draft logits, however little of the
+ * probability the rejected children left (|l - max| / T up to 30); with them,
+ * where p and M q cancel, 2^-17 (p / rest + 1 / m) (|l - max| / T up to 8).
  */
 #define MCPU_MAX_TREE_NODES 256
 #define MCPU_BF16 0
